@@ -496,6 +496,49 @@ r3_status r3_replay_finish_rows(const r3_shape* shape, const float* logits, cons
                                 const void* residual, void* y, float* gates_out, float* dlogits,
                                 int32_t* dev_status, void* stream);
 
+/* ---- token log probabilities (the p_train and p_infer of Sections 3.1 and 3.2) -------------- */
+
+/* A batch of logits: T rows of V values, row t at logits + t * ld elements (ld >= V, so a padded or
+ * sliced vocabulary is taken as it lies), dtype R3_F32 or R3_BF16.  token_ids are int32 or int64
+ * (id_bytes 4 or 8).  temperature > 0 divides the logits. */
+typedef struct {
+    int32_t T, V;
+    int64_t ld;
+    int32_t dtype, id_bytes;
+    double temperature;
+} r3_logits;
+
+/* For every row x, with top = max_v x_v and L = log sum_v exp((x_v - top) / temperature):
+ *   logp[t]     = (x_id - top) / temperature - L     log probability of token_ids[t]   [T]    f32
+ *   entropy[t]  = - sum_v p_v log p_v                                                  [T]    f32
+ *   stats[t]    = (top, L): what r3_token_logprobs_bwd needs                           [T,2]  f32
+ *   top_ids[t]  = the n_top most probable tokens, descending, ties to the lower id     [T,n_top] i32
+ *   top_logp[t] = their log probabilities                                              [T,n_top] f32
+ * Every output may be NULL (at least one is not); n_top <= 32 (R3_ERR_UNSUPPORTED beyond) and
+ * <= V.  Logits and outputs need the alignment of their own type only.  One pass over the logits;
+ * sums in float32; no workspace.
+ *  - A negative token id marks a row that is not a response token (prompt, padding): its logits
+ *    are not read, its outputs are 0 (top_ids -1).  An id >= V is treated the same and reported as
+ *    R3_DEV_BAD_INDEX.  token_ids may be NULL when logp is: then every row counts.
+ *  - Masked logits may be -inf or the type's lowest value.  A row of -inf alone has logp and
+ *    top_logp -inf, entropy 0, stats (-inf, 0) and the first n_top ids; a row that holds NaN or
+ *    +inf has no distribution: its outputs are NaN and its top_ids -1. */
+r3_status r3_token_logprobs(const r3_logits* shape, const void* logits, const void* token_ids,
+                            float* logp, float* entropy, float* stats, int32_t n_top,
+                            int32_t* top_ids, float* top_logp, int32_t* dev_status, void* stream);
+
+/* Gradient of a loss with dlogp = dL/dlogp [T] f32 (or NULL) and dentropy = dL/dentropy [T] f32 (or
+ * NULL; then entropy [T] of the forward is not needed either) with respect to the logits:
+ *   dlogits[t,v] = ( dlogp (1[v = id] - p_v) - dentropy p_v (log p_v + entropy) ) / temperature
+ * with p from the logits and the forward's stats.  dlogits has the logits' dtype and row stride
+ * ld_out >= V; columns from V on are left as they were.  It may be the logits' own buffer (with
+ * ld_out = ld).  Every element of the V columns is written: rows with a negative token id (or one
+ * >= V, reported) and rows of -inf alone get zeros. */
+r3_status r3_token_logprobs_bwd(const r3_logits* shape, const void* logits, const void* token_ids,
+                                const float* stats, const float* entropy, const float* dlogp,
+                                const float* dentropy, void* dlogits, int64_t ld_out,
+                                int32_t* dev_status, void* stream);
+
 /* ---- training/inference discrepancy measures (Sections 3.1 and 3.2) -------------------------- */
 
 /* Eq. (kl), the k3 estimate of KL(pi_train || pi_infer), and Eq. (etdf), the Extreme Token

@@ -1,0 +1,64 @@
+"""CPU oracle (numpy float64) of the operators around the replayed block in an Update step: token
+log probabilities and their gradient, the norms around a block and their gradient, and one AdamW
+step.  Each function is the operator's definition written out; nothing is shared with the product."""
+from __future__ import annotations
+
+import numpy as np
+
+
+# ---- log probabilities of given tokens --------------------------------------------------------
+def token_logprobs(logits, token_ids, temperature=1.0, n_top=0):
+    """logits [T, V], token_ids [T] (negative: the row is skipped).  Returns a dict of logp [T],
+    entropy [T], stats [T, 2] (largest logit, log of the sum of exponentials above it), top_ids
+    [T, n_top] (ties to the lower id), top_logp [T, n_top]."""
+    z = np.asarray(logits, dtype=np.float64)
+    T, V = z.shape
+    out = dict(logp=np.zeros(T), entropy=np.zeros(T), stats=np.zeros((T, 2)),
+               top_ids=np.full((T, n_top), -1, dtype=np.int64), top_logp=np.zeros((T, n_top)))
+    for t in range(T):
+        i = int(token_ids[t])
+        if i < 0 or i >= V:
+            continue
+        row = z[t]
+        if np.isnan(row).any() or np.isposinf(row).any():
+            for k in ("logp", "entropy", "stats", "top_logp"):
+                out[k][t] = np.nan
+            continue
+        order = np.argsort(-row, kind="stable")[:n_top]
+        out["top_ids"][t] = order
+        top = row.max()
+        if np.isneginf(top):
+            out["logp"][t] = -np.inf
+            out["top_logp"][t] = -np.inf
+            out["stats"][t] = (-np.inf, 0.0)
+            continue
+        e = (row - top) / temperature
+        total = np.log(np.exp(e).sum())
+        lp = e - total
+        p = np.exp(lp)
+        out["logp"][t] = lp[i]
+        out["entropy"][t] = -np.sum(p[p > 0] * lp[p > 0])
+        out["stats"][t] = (top, total)
+        out["top_logp"][t] = lp[order]
+    return out
+
+
+def token_logprobs_bwd(logits, token_ids, dlogp, dentropy=None, temperature=1.0):
+    """d/dlogits of sum_t dlogp[t] logp[t] + dentropy[t] entropy[t]."""
+    z = np.asarray(logits, dtype=np.float64)
+    f = token_logprobs(z, token_ids, temperature)
+    out = np.zeros_like(z)
+    for t in range(z.shape[0]):
+        i = int(token_ids[t])
+        top, total = f["stats"][t]
+        if i < 0 or i >= z.shape[1] or np.isneginf(top):
+            continue
+        lp = (z[t] - top) / temperature - total
+        p = np.exp(lp)
+        d = -dlogp[t] * p
+        d[i] += dlogp[t]
+        if dentropy is not None:
+            live = p > 0
+            d[live] -= dentropy[t] * p[live] * (lp[live] + f["entropy"][t])
+        out[t] = d / temperature
+    return out

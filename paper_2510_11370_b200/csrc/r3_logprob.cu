@@ -1,0 +1,626 @@
+// Log probabilities of given tokens from rows of logits, with the entropy and the best
+// alternatives of each row, and the gradient to the logits: where the p_train and p_infer of
+// Eq. (kl) and Eq. (etdf) come from, and what carries a loss on them back.
+//
+// One pass over the logits.  With c = log2(e) / temperature every thread keeps an integer
+// reference M and the sums
+//   S = sum 2^(c x - M),   U = sum 2^(c x - M) (c x - M)
+// over its share of the row.  M is a whole number near the running maximum of c x, so that c x - M
+// is one fused multiply-add with a single rounding and moving M multiplies S by an exact power of
+// two.  M only moves when a value exceeds it by more than 8 (float32 holds 2^8 times the count of
+// any row), which is rare after a thread's first values.  With top = max x and S, U taken
+// relative to it, log sum exp((x - top) / temperature) = ln S and the entropy is ln S - ln2 U / S,
+// two numbers of the size of the result: nothing cancels for large logits.
+#include <math_constants.h>
+
+#include "r3_common.cuh"
+#include "r3_internal.h"
+#include "r3_tc.cuh"
+
+namespace r3 {
+
+constexpr int kMaxTop = 32;            // alternatives: one list entry per lane
+constexpr float kMoveRef = 8.f;
+constexpr float kLowRef = -4194304.f;  // -2^22: the least reference
+constexpr float kPlainTop = 1048576.f; // |c top| up to which the reference is exact enough
+constexpr float kLeastExp = -200.f;    // 2^-200 is 0 in float32, and 0 * -200 is 0, not NaN
+
+struct LogprobArgs {
+    const void* logits;
+    const void* ids;
+    long long ld;
+    int T, V, id64, n_top, split;
+    float c, inv_t;
+    float* logp;
+    float* entropy;
+    float* stats;
+    int32_t* top_ids;
+    float* top_logp;
+    int32_t* dev_status;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {   // a NaN stays one
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// A value and its column as one number: larger values first, then lower columns.  The largest key
+// of a set is the first of its largest values; both zeros are the same value.
+typedef unsigned long long Key;
+__device__ __forceinline__ Key make_key(float v, int column) {
+    const uint32_t b = __float_as_uint(v + 0.f);
+    const uint32_t o = (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+    return ((Key)o << 32) | (uint32_t)~column;
+}
+__device__ __forceinline__ float key_value(Key k) {
+    const uint32_t o = (uint32_t)(k >> 32);
+    return __uint_as_float((o & 0x80000000u) ? (o ^ 0x80000000u) : ~o);
+}
+__device__ __forceinline__ int key_column(Key k) { return (int)~(uint32_t)k; }
+
+// 32 keys, one per lane, into descending order (a bitonic network).
+__device__ __forceinline__ Key warp_sort(Key k, int lane) {
+#pragma unroll
+    for (int size = 2; size <= 32; size <<= 1) {
+#pragma unroll
+        for (int j = size >> 1; j > 0; j >>= 1) {
+            const Key o = __shfl_xor_sync(0xffffffffu, k, j);
+            const bool larger = ((lane & j) == 0) == ((lane & size) == 0);
+            k = (k > o) == larger ? k : o;
+        }
+    }
+    return k;
+}
+// The 32 largest of two descending lists, descending.
+__device__ __forceinline__ Key warp_merge(Key a, Key b, int lane) {
+    const Key r = __shfl_sync(0xffffffffu, b, 31 - lane);
+    Key k = a > r ? a : r;
+#pragma unroll
+    for (int j = 16; j > 0; j >>= 1) {
+        const Key o = __shfl_xor_sync(0xffffffffu, k, j);
+        k = (k > o) == ((lane & j) == 0) ? k : o;
+    }
+    return k;
+}
+
+__device__ __forceinline__ long long load_id(const void* ids, int id64, int row) {
+    return id64 ? static_cast<const long long*>(ids)[row]
+                : (long long)static_cast<const int32_t*>(ids)[row];
+}
+
+// How a row of V elements at p splits into single elements up to a 16-byte boundary, whole
+// 16-byte pieces, and single elements behind them (rows of an odd V start anywhere).
+struct RowSplit {
+    int head, vecs, tail;
+};
+template <typename T> __device__ __forceinline__ RowSplit split_row(const T* p, int V) {
+    constexpr int N = Vec16<T>::N;
+    RowSplit r;
+    const int off = (int)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T));
+    r.head = off ? N - off : 0;
+    if (r.head > V) r.head = V;
+    r.vecs = (V - r.head) / N;
+    r.tail = V - r.head - r.vecs * N;
+    return r;
+}
+
+struct RowSums {
+    float M, S, U, top;
+};
+// Moves the reference up to hold a value of c x = t.
+__device__ __forceinline__ void move_ref(RowSums& a, float t) {
+    const float m = rintf(t), d = a.M - m, f = ex2(d);
+    a.U = f * (a.U + d * a.S);
+    a.S *= f;
+    a.M = m;
+}
+template <bool ENT> __device__ __forceinline__ void add_term(RowSums& a, float u) {
+    if (ENT) {
+        u = max_nan(u, kLeastExp);
+        const float e = ex2(u);
+        a.S += e;
+        a.U = fmaf(e, u, a.U);
+    } else {
+        a.S += ex2(u);
+    }
+}
+
+// What the CTAs of one row hand to the first of them.
+struct SplitPart {
+    float top, S, U;
+    Key list[kMaxTop];
+};
+
+// One row per cluster of `split` CTAs (1 for a large batch); NT threads each.
+template <typename T, bool ENT, bool TOP, int NT>
+__global__ void __launch_bounds__(NT, NT == 512 ? 3 : 8) logprob_kernel(const LogprobArgs a) {
+    constexpr int N = Vec16<T>::N, W = NT / 32, UNROLL = 4;
+    __shared__ float s_red[W][4];
+    __shared__ Key s_list[TOP ? W : 1][32];
+    __shared__ int s_sel[kMaxTop], s_nsel;
+    __shared__ SplitPart s_part;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int row = blockIdx.x / a.split, rank = blockIdx.x - row * a.split;
+
+    const long long id = a.ids ? load_id(a.ids, a.id64, row) : 0;
+    if (id < 0 || id >= a.V) {                          // the same decision in the whole cluster
+        if (rank == 0) {
+            if (tid == 0) {
+                if (id >= a.V) report(a.dev_status, R3_DEV_BAD_INDEX);
+                if (a.logp) a.logp[row] = 0.f;
+                if (ENT) a.entropy[row] = 0.f;
+                if (a.stats) a.stats[2 * (size_t)row] = a.stats[2 * (size_t)row + 1] = 0.f;
+            }
+            if (TOP && tid < a.n_top) {
+                a.top_ids[(size_t)row * a.n_top + tid] = -1;
+                a.top_logp[(size_t)row * a.n_top + tid] = 0.f;
+            }
+        }
+        return;
+    }
+
+    const T* p = static_cast<const T*>(a.logits) + (size_t)row * a.ld;
+    const RowSplit rs = split_row(p, a.V);
+    const Vec16<T>* pv = reinterpret_cast<const Vec16<T>*>(p + rs.head);
+    const int per_cta = (rs.vecs + a.split - 1) / a.split;
+    const int v0 = min(rs.vecs, rank * per_cta), v1 = min(rs.vecs, v0 + per_cta);
+    const float c = a.c;
+
+    RowSums r = {kLowRef, 0.f, 0.f, -CUDART_INF_F};
+    float best = -CUDART_INF_F;
+    int best_vec = v0 + tid < v1 ? v0 + tid : -1;
+
+    auto take = [&](const Vec16<T>& vec, int j) {
+        float x[N];
+        vec.unpack(x);
+        float m = x[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
+        r.top = fmaxf(r.top, m);
+        if (TOP && m > best) {
+            best = m;
+            best_vec = j;
+        }
+        if (m * c - r.M > kMoveRef) move_ref(r, m * c);
+#pragma unroll
+        for (int i = 0; i < N; ++i) add_term<ENT>(r, fmaf(x[i], c, -r.M));
+    };
+    auto take_one = [&](float x) {
+        r.top = fmaxf(r.top, x);
+        if (x * c - r.M > kMoveRef) move_ref(r, x * c);
+        add_term<ENT>(r, fmaf(x, c, -r.M));
+    };
+    int j = v0 + tid;
+    for (; j + (UNROLL - 1) * NT < v1; j += UNROLL * NT) {
+        Vec16<T> b[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) b[u] = pv[j + u * NT];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) take(b[u], j + u * NT);
+    }
+    for (; j < v1; j += NT) take(pv[j], j);
+    const bool has_head = rank == 0, has_tail = rank == a.split - 1;
+    const int tail0 = rs.head + rs.vecs * N;
+    if (has_head && tid < rs.head) take_one(to_f32(p[tid]));
+    if (has_tail && tid < rs.tail) take_one(to_f32(p[tail0 + tid]));
+
+    // ---- the CTA's maximum and sums, relative to its own top -------------------------------
+    float m = r.M, top = r.top;
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) {
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+    }
+    if (lane == 0) {
+        s_red[warp][0] = m;
+        s_red[warp][1] = top;
+    }
+    if (tid == 0) s_nsel = 0;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        m = fmaxf(m, s_red[w][0]);
+        top = fmaxf(top, s_red[w][1]);
+    }
+    // A top whose c x is beyond 2^20 (masks of the type's lowest value in a whole row, say) leaves
+    // the reference no room: the share is summed again with the differences to the known top.
+    const bool again = fabsf(top * c) > kPlainTop && fabsf(top) < CUDART_INF_F;
+    if (again) {
+        // a NaN would be dropped by neither form: x - top keeps it
+        r.S = 0.f;
+        r.U = 0.f;
+        auto term = [&](float x) { add_term<true>(r, (x - top) * c); };
+        for (int q = v0 + tid; q < v1; q += NT) {
+            float x[N];
+            pv[q].unpack(x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) term(x[i]);
+        }
+        if (has_head && tid < rs.head) term(to_f32(p[tid]));
+        if (has_tail && tid < rs.tail) term(to_f32(p[tail0 + tid]));
+    } else {
+        const float d = r.M - m, f = ex2(d);
+        r.U = f * (r.U + d * r.S);
+        r.S *= f;
+    }
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) {
+        r.S += __shfl_xor_sync(0xffffffffu, r.S, s);
+        r.U += __shfl_xor_sync(0xffffffffu, r.U, s);
+    }
+    if (lane == 0) {
+        s_red[warp][2] = r.S;
+        s_red[warp][3] = r.U;
+    }
+    __syncthreads();
+    float S = 0.f, U = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {                                        // fixed order
+        S += s_red[w][2];
+        U += s_red[w][3];
+    }
+    if (!again && top > -CUDART_INF_F) {
+        const float ut = fmaf(top, c, -m), k = ex2(-ut);
+        U = k * (U - ut * S);
+        S *= k;
+    }
+
+    // ---- the 32 largest keys of the CTA's share ----------------------------------------------
+    // Every thread knows its largest value and the 16-byte piece where that stood first.  The
+    // n-th largest of the pieces' lower bounds (value, last column) bounds the n-th largest key
+    // of the share from below, and only the threads whose piece reaches it (value, first column)
+    // can hold one of the n largest keys: at most n of them, since pieces do not overlap.  Their
+    // pieces are read again, from L2.
+    Key list = 0;
+    if (TOP) {
+        auto merge_warps = [&](Key k) {                 // warp 0 ends with the list of the CTA
+            s_list[warp][lane] = k;
+#pragma unroll
+            for (int half = W / 2; half > 0; half >>= 1) {
+                __syncthreads();
+                if (warp < half) {
+                    k = warp_merge(k, s_list[warp + half][lane], lane);
+                    s_list[warp][lane] = k;
+                }
+            }
+            __syncthreads();
+            return k;
+        };
+        const int first = rs.head + best_vec * N;
+        const Key low = best_vec >= 0 ? make_key(best, first + N - 1) : 0;
+        merge_warps(warp_sort(low, lane));
+        const Key bound = s_list[0][a.n_top - 1];
+        if (best_vec >= 0 && make_key(best, first) >= bound) {
+            const int s = atomicAdd(&s_nsel, 1);         // any order: what follows does not depend on it
+            if (s < kMaxTop) s_sel[s] = tid;
+        }
+        __syncthreads();
+        const int per = (v1 - v0 + NT - 1) / NT, total = min(s_nsel, kMaxTop) * per;
+        auto offer = [&](Key k) {
+            if (k < bound) k = 0;
+            if (__any_sync(0xffffffffu, k != 0)) list = warp_merge(list, warp_sort(k, lane), lane);
+        };
+        for (int q0 = warp * 32; q0 < total; q0 += NT) {
+            const int q = q0 + lane, s = q / per;
+            const int vec = q < total ? v0 + s_sel[s] + (q - s * per) * NT : v1;
+            float x[N];
+            if (vec < v1) pv[vec].unpack(x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) offer(vec < v1 ? make_key(x[i], rs.head + vec * N + i) : 0);
+        }
+        if (warp == 0) {
+            int col = -1;
+            if (has_head && lane < rs.head) col = lane;
+            if (has_tail && lane >= 16 && lane - 16 < rs.tail) col = tail0 + lane - 16;
+            offer(col >= 0 ? make_key(to_f32(p[col]), col) : 0);
+        }
+        list = merge_warps(list);
+    }
+
+    // ---- the CTAs of a row meet in the first of them ------------------------------------------
+    if (a.split > 1) {
+        if (tid == 0) {
+            s_part.top = top;
+            s_part.S = S;
+            s_part.U = U;
+        }
+        if (TOP && warp == 0) s_part.list[lane] = list;
+        tc::cluster_sync_all();
+        if (rank == 0 && warp == 0) {
+            const uint32_t mine = tc::smem_u32(&s_part);
+            auto peer = [&](int q, size_t off) {
+                uint32_t v;
+                asm volatile("ld.shared::cluster.u32 %0, [%1];"
+                             : "=r"(v) : "r"(tc::mapa_shared(mine + (uint32_t)off, q)) : "memory");
+                return v;
+            };
+            float t[3] = {-CUDART_INF_F, 0.f, 0.f};
+            if (lane < a.split) {
+                t[0] = __uint_as_float(peer(lane, offsetof(SplitPart, top)));
+                t[1] = __uint_as_float(peer(lane, offsetof(SplitPart, S)));
+                t[2] = __uint_as_float(peer(lane, offsetof(SplitPart, U)));
+            }
+            top = t[0];
+#pragma unroll
+            for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+            // a share of -inf alone has S = 0 (or NaN, which stays)
+            const float d = t[0] > -CUDART_INF_F ? max_nan((t[0] - top) * c, -1e30f) : 0.f;
+            const float f = ex2(d);
+            U = f * (t[2] + d * t[1]);
+            S = f * t[1];
+#pragma unroll
+            for (int s = 16; s > 0; s >>= 1) {
+                S += __shfl_xor_sync(0xffffffffu, S, s);
+                U += __shfl_xor_sync(0xffffffffu, U, s);
+            }
+            if (TOP)
+                for (int q = 1; q < a.split; ++q) {
+                    const size_t at = offsetof(SplitPart, list) + lane * sizeof(Key);
+                    const Key k = (Key)peer(q, at) | ((Key)peer(q, at + 4) << 32);
+                    list = warp_merge(list, k, lane);
+                }
+        }
+        tc::cluster_sync_all();                  // the peers' shared memory was read until here
+    }
+    if (rank != 0 || warp != 0) return;
+
+    const bool bad = !(S < CUDART_INF_F);                       // NaN or +inf among the logits
+    const bool none = !bad && top == -CUDART_INF_F;             // every logit -inf
+    float ln_s = none ? 0.f : logf(S);
+    if (ln_s < 0.f) ln_s = 0.f;                                 // S holds the top's own term, 1
+    if (bad) top = ln_s = CUDART_NAN_F;
+    auto logp_of = [&](float x) { return none ? -CUDART_INF_F : (x - top) * a.inv_t - ln_s; };
+    if (lane == 0) {
+        if (a.logp) a.logp[row] = logp_of(to_f32(p[id]));
+        if (ENT) {
+            const float h = none ? 0.f : bad ? CUDART_NAN_F : ln_s - CUDART_LN2_F * (U / S);
+            a.entropy[row] = h < 0.f ? 0.f : h;
+        }
+        if (a.stats) {
+            a.stats[2 * (size_t)row] = top;
+            a.stats[2 * (size_t)row + 1] = ln_s;
+        }
+    }
+    if (TOP && lane < a.n_top) {
+        a.top_ids[(size_t)row * a.n_top + lane] = bad ? -1 : key_column(list);
+        a.top_logp[(size_t)row * a.n_top + lane] = logp_of(key_value(list));
+    }
+}
+
+// ---- gradient to the logits ----------------------------------------------------------------------
+struct LogprobBwdArgs {
+    const void* logits;
+    const void* ids;
+    const float* stats;
+    const float* entropy;
+    const float* dlogp;
+    const float* dentropy;
+    void* dlogits;
+    long long ld, ld_out;
+    int T, V, id64, chunks;
+    float c, inv_t;
+    int32_t* dev_status;
+};
+
+constexpr int kBwdThreads = 256;
+constexpr int kBwdVecs = 4;            // 16-byte pieces per thread
+
+// d logits[v] = (dlogp (1[v = id] - p_v) - dentropy p_v (log p_v + H)) / temperature.  Element by
+// element once the row's two sums are known; logits and dlogits may be the same buffer (each thread
+// reads its elements before it writes them).
+template <typename T, bool ENT>
+__global__ void __launch_bounds__(kBwdThreads) logprob_bwd_kernel(const LogprobBwdArgs a) {
+    constexpr int N = Vec16<T>::N, STEP = kBwdThreads * kBwdVecs;
+    const long long items = (long long)a.T * a.chunks;
+    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+        const int row = (int)(item / a.chunks), chunk = (int)(item - (long long)row * a.chunks);
+        const T* x = static_cast<const T*>(a.logits) + (size_t)row * a.ld;
+        T* dx = static_cast<T*>(a.dlogits) + (size_t)row * a.ld_out;
+        const long long id = a.ids ? load_id(a.ids, a.id64, row) : 0;
+        const bool skip = id < 0 || id >= a.V;
+        if (id >= a.V && chunk == 0 && threadIdx.x == 0) report(a.dev_status, R3_DEV_BAD_INDEX);
+        const float top = a.stats[2 * (size_t)row], ln_s = a.stats[2 * (size_t)row + 1];
+        const bool zero = skip || top == -CUDART_INF_F;
+        const float g = a.dlogp ? a.dlogp[row] * a.inv_t : 0.f;
+        const float ge = ENT ? a.dentropy[row] * a.inv_t : 0.f;
+        const float h = ENT ? a.entropy[row] : 0.f;
+        const float ls2 = ln_s * CUDART_L2E_F, c = a.c;
+        const int target = a.dlogp && !skip ? (int)id : -1;
+        auto grad = [&](float v, int col) {
+            float u = fmaf(v - top, c, -ls2);
+            float k = -g;
+            if (ENT) {
+                u = max_nan(u, kLeastExp);
+                k -= ge * fmaf(u, CUDART_LN2_F, h);
+            }
+            float d = ex2(u) * k;
+            if (col == target) d += g;
+            return d;
+        };
+        const RowSplit rs = split_row(dx, a.V);
+        // the wide form needs both rows to start at the same place of a 16-byte piece
+        const bool wide =
+            ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(dx)) & 15u) == 0;
+        if (wide) {
+            const Vec16<T>* xv = reinterpret_cast<const Vec16<T>*>(x + rs.head);
+            Vec16<T>* dv = reinterpret_cast<Vec16<T>*>(dx + rs.head);
+            const int first = chunk * STEP + threadIdx.x;
+            Vec16<T> b[kBwdVecs];
+            if (!zero) {
+#pragma unroll
+                for (int q = 0; q < kBwdVecs; ++q)
+                    if (first + q * kBwdThreads < rs.vecs) b[q] = xv[first + q * kBwdThreads];
+            }
+#pragma unroll
+            for (int q = 0; q < kBwdVecs; ++q) {
+                const int j = first + q * kBwdThreads;
+                if (j >= rs.vecs) break;
+                float f[N];
+                if (zero) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) f[i] = 0.f;
+                } else {
+                    b[q].unpack(f);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) f[i] = grad(f[i], rs.head + j * N + i);
+                }
+                Vec16<T> o;
+                o.pack(f);
+                dv[j] = o;
+            }
+            if (chunk == 0) {
+                const int tail0 = rs.head + rs.vecs * N, t = threadIdx.x;
+                const int col = t < rs.head ? t : t >= 32 && t - 32 < rs.tail ? tail0 + t - 32 : -1;
+                if (col >= 0) dx[col] = from_f32<T>(zero ? 0.f : grad(to_f32(x[col]), col));
+            }
+        } else {
+            const int end = min(a.V, (chunk + 1) * STEP * N);
+            for (int col = chunk * STEP * N + threadIdx.x; col < end; col += kBwdThreads)
+                dx[col] = from_f32<T>(zero ? 0.f : grad(to_f32(x[col]), col));
+        }
+    }
+}
+
+// ---- host side ------------------------------------------------------------------------------------
+static r3_status check_logits(const r3_logits* s) {
+    if (!s) return R3_ERR_INVALID_ARG;
+    if (s->T < 0 || s->V <= 0 || s->V > (1 << 30) || s->ld < s->V) return R3_ERR_INVALID_ARG;
+    if (s->dtype != R3_F32 && s->dtype != R3_BF16) return R3_ERR_INVALID_ARG;
+    if (s->id_bytes != 4 && s->id_bytes != 8) return R3_ERR_INVALID_ARG;
+    if (!(s->temperature > 0.0) || !(s->temperature < 1e30) || !(s->temperature > 1e-30))
+        return R3_ERR_INVALID_ARG;
+    return R3_OK;
+}
+
+template <typename T, bool ENT, bool TOP, int NT>
+static r3_status launch_logprob(const LogprobArgs& a, cudaStream_t cs) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    cfg.gridDim = dim3((unsigned)((long long)a.T * a.split));
+    cfg.blockDim = dim3(NT);
+    cfg.stream = cs;
+    if (a.split > 1) {
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)a.split;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+    }
+    if (cudaLaunchKernelEx(&cfg, logprob_kernel<T, ENT, TOP, NT>, a) != cudaSuccess) {
+        cudaGetLastError();
+        return R3_ERR_CUDA;
+    }
+    return R3_OK;
+}
+
+template <typename T, int NT> static r3_status dispatch_logprob(const LogprobArgs& a, cudaStream_t cs) {
+    if (a.entropy)
+        return a.n_top ? launch_logprob<T, true, true, NT>(a, cs)
+                       : launch_logprob<T, true, false, NT>(a, cs);
+    return a.n_top ? launch_logprob<T, false, true, NT>(a, cs)
+                   : launch_logprob<T, false, false, NT>(a, cs);
+}
+
+}  // namespace r3
+
+extern "C" r3_status r3_token_logprobs(const r3_logits* shape, const void* logits,
+                                       const void* token_ids, float* logp, float* entropy,
+                                       float* stats, int32_t n_top, int32_t* top_ids,
+                                       float* top_logp, int32_t* dev_status, void* stream) {
+    const r3_status st = r3::check_logits(shape);
+    if (st != R3_OK) return st;
+    if (n_top < 0 || n_top > shape->V) return R3_ERR_INVALID_ARG;
+    if (n_top > r3::kMaxTop) return R3_ERR_UNSUPPORTED;
+    if (shape->T == 0) return R3_OK;
+    const size_t es = shape->dtype == R3_BF16 ? 2 : 4;
+    if (!logits || !r3::aligned(logits, es) || (logp && !token_ids) ||
+        (n_top > 0 && (!top_ids || !top_logp)) || (!logp && !entropy && !stats && n_top == 0) ||
+        (token_ids && !r3::aligned(token_ids, (size_t)shape->id_bytes)))
+        return R3_ERR_INVALID_ARG;
+    r3::LogprobArgs a = {};
+    a.logits = logits;
+    a.ids = token_ids;
+    a.ld = shape->ld;
+    a.T = shape->T;
+    a.V = shape->V;
+    a.id64 = shape->id_bytes == 8;
+    a.n_top = n_top;
+    a.c = (float)(1.4426950408889634 / shape->temperature);
+    a.inv_t = (float)(1.0 / shape->temperature);
+    a.logp = logp;
+    a.entropy = entropy;
+    a.stats = stats;
+    a.top_ids = top_ids;
+    a.top_logp = top_logp;
+    a.dev_status = dev_status;
+    cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    const long long row_bytes = (long long)shape->V * (long long)es;
+    // A row of up to 16 KB is two pieces or fewer for each of 512 threads: the reductions at its
+    // end would cost more than its loads, so it gets 128 threads.
+    const bool small = row_bytes <= 16384;
+    // Few rows: a cluster of CTAs shares one, as long as each of its threads has a piece or two
+    // and there are SMs for it.
+    a.split = 1;
+    const int threads = small ? 128 : 512;
+    while (a.split < 8 && (long long)a.T * a.split * 2 <= 2LL * r3::sm_count() &&
+           row_bytes / (a.split * 2) >= 2LL * 16 * threads)
+        a.split *= 2;
+    if (shape->dtype == R3_BF16)
+        return small ? r3::dispatch_logprob<__nv_bfloat16, 128>(a, cs)
+                     : r3::dispatch_logprob<__nv_bfloat16, 512>(a, cs);
+    return small ? r3::dispatch_logprob<float, 128>(a, cs) : r3::dispatch_logprob<float, 512>(a, cs);
+}
+
+extern "C" r3_status r3_token_logprobs_bwd(const r3_logits* shape, const void* logits,
+                                           const void* token_ids, const float* stats,
+                                           const float* entropy, const float* dlogp,
+                                           const float* dentropy, void* dlogits, int64_t ld_out,
+                                           int32_t* dev_status, void* stream) {
+    const r3_status st = r3::check_logits(shape);
+    if (st != R3_OK) return st;
+    if (ld_out < shape->V) return R3_ERR_INVALID_ARG;
+    if (shape->T == 0) return R3_OK;
+    const size_t es = shape->dtype == R3_BF16 ? 2 : 4;
+    if (!logits || !r3::aligned(logits, es) || !dlogits || !r3::aligned(dlogits, es) || !stats ||
+        (!dlogp && !dentropy) || (dlogp && !token_ids) || (dentropy && !entropy) ||
+        (dlogits == logits && ld_out != shape->ld) ||
+        (token_ids && !r3::aligned(token_ids, (size_t)shape->id_bytes)))
+        return R3_ERR_INVALID_ARG;
+    r3::LogprobBwdArgs a = {};
+    a.logits = logits;
+    a.ids = token_ids;
+    a.stats = stats;
+    a.entropy = entropy;
+    a.dlogp = dlogp;
+    a.dentropy = dentropy;
+    a.dlogits = dlogits;
+    a.ld = shape->ld;
+    a.ld_out = ld_out;
+    a.T = shape->T;
+    a.V = shape->V;
+    a.id64 = shape->id_bytes == 8;
+    a.c = (float)(1.4426950408889634 / shape->temperature);
+    a.inv_t = (float)(1.0 / shape->temperature);
+    a.dev_status = dev_status;
+    const int step = r3::kBwdThreads * r3::kBwdVecs * (int)(16 / es);
+    a.chunks = (shape->V + step - 1) / step;
+    const long long items = (long long)a.T * a.chunks;
+    const unsigned grid = (unsigned)(items < 0x7fffffffLL ? items : 0x7fffffffLL);
+    cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    if (shape->dtype == R3_BF16) {
+        if (dentropy)
+            r3::logprob_bwd_kernel<__nv_bfloat16, true><<<grid, r3::kBwdThreads, 0, cs>>>(a);
+        else
+            r3::logprob_bwd_kernel<__nv_bfloat16, false><<<grid, r3::kBwdThreads, 0, cs>>>(a);
+    } else {
+        if (dentropy) r3::logprob_bwd_kernel<float, true><<<grid, r3::kBwdThreads, 0, cs>>>(a);
+        else r3::logprob_bwd_kernel<float, false><<<grid, r3::kBwdThreads, 0, cs>>>(a);
+    }
+    return r3::launch_status();
+}

@@ -39,6 +39,7 @@ EXPORTS = [
     "r3_replay_layer_host_workspace_bytes", "r3_replay_layer_host", "r3_replay_layer_host_enqueue",
     "r3_replay_layer_host_chunks",
     "r3_replay_layer_same_record",
+    "r3_token_logprobs", "r3_token_logprobs_bwd",
     "r3_prob_discrepancy_workspace_bytes", "r3_prob_discrepancy", "r3_record_diff",
     "r3_sequence_diff", "r3_grouped_swiglu_bwd_workspace_bytes", "r3_grouped_swiglu_bwd_input",
     "r3_grouped_swiglu_bwd", "r3_grouped_swiglu_train", "r3_scale_rows", "r3_input_grad_finish",
@@ -57,6 +58,12 @@ class Shape(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int32), ("d", ctypes.c_int32), ("E", ctypes.c_int32),
                 ("K", ctypes.c_int32), ("F", ctypes.c_int32), ("act_dtype", ctypes.c_int32),
                 ("router_w_dtype", ctypes.c_int32), ("idx_type", ctypes.c_int32)]
+
+
+class Logits(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("V", ctypes.c_int32), ("ld", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("id_bytes", ctypes.c_int32),
+                ("temperature", ctypes.c_double)]
 
 
 _P = ctypes.c_void_p
@@ -108,6 +115,9 @@ lib.r3_replay_layer.argtypes = [_SP] + [_P] * 11 + [ctypes.c_size_t, _P, _P]
 lib.r3_replay_layer_same_record.argtypes = [_SP] + [_P] * 11 + [ctypes.c_size_t, _P, _P]
 lib.r3_replay_layer_host.argtypes = [_SP] + [_P] * 10 + [ctypes.c_size_t, _P, _P]
 lib.r3_replay_layer_host_enqueue.argtypes = [_SP] + [_P] * 10 + [ctypes.c_size_t, _P, _P]
+lib.r3_token_logprobs.argtypes = [ctypes.POINTER(Logits)] + [_P] * 5 + [ctypes.c_int32] + [_P] * 4
+lib.r3_token_logprobs_bwd.argtypes = ([ctypes.POINTER(Logits)] + [_P] * 7 + [ctypes.c_int64]
+                                      + [_P] * 2)
 lib.r3_prob_discrepancy_workspace_bytes.restype = ctypes.c_size_t
 lib.r3_prob_discrepancy_workspace_bytes.argtypes = [ctypes.c_int64]
 lib.r3_prob_discrepancy.argtypes = [_P, _P, ctypes.c_int64, _P, ctypes.c_int32, _P, _P, _P,
@@ -510,6 +520,96 @@ def replay_layer_host_enqueue(s: Shape, x_host, w_router, idx_host, w_gate, w_up
 
 
 # ---------------------------------------------------------------------------------------------
+def _expect(name: str, t, shape, dtype, device) -> None:
+    """Refuses a tensor that is not what the call documents (None passes)."""
+    if t is None:
+        return
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor")
+    dtypes = dtype if isinstance(dtype, tuple) else (dtype,)
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {' or '.join(map(str, dtypes))}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.device != device:
+        raise ValueError(f"{name}: on {t.device}, expected {device}")
+
+
+def _device_of(name: str, t) -> torch.device:
+    """The device of a call's first tensor, which has to be the current one: kernels are enqueued
+    on the current device's stream."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError("expected a CUDA tensor (there is no CPU path)")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, which is not the current device")
+    return t.device
+
+
+def _rows(name: str, t):
+    """Pointer and row stride of a [T, V] tensor whose rows may lie apart but are dense."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: expected [T, V] with adjacent columns")
+    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if ld < t.shape[1]:
+        raise ValueError(f"{name}: rows overlap")
+    return ctypes.c_void_p(t.data_ptr()), ld
+
+
+def _logits_shape(logits, token_ids, temperature):
+    dev = _device_of("logits", logits)
+    if logits.dtype not in _ACT:
+        raise ValueError(f"logits: dtype {logits.dtype}, expected float32 or bfloat16")
+    ptr, ld = _rows("logits", logits)
+    T, V = logits.shape
+    _expect("token_ids", token_ids, (T,), (torch.int32, torch.int64), dev)
+    id_bytes = token_ids.element_size() if token_ids is not None else 4
+    return Logits(T, V, ld, _ACT[logits.dtype], id_bytes, float(temperature)), ptr, dev
+
+
+def token_logprobs(logits, token_ids=None, *, temperature=1.0, n_top=0, want_entropy=False,
+                   want_stats=False, dev_status=None, stream=None):
+    """Log probabilities of token_ids [T] (int32 or int64) under logits [T, V] (float32 or bfloat16;
+    rows may lie apart).  Returns (logp [T] or None without token_ids, entropy [T] or None,
+    stats [T, 2] or None, top_ids [T, n_top] int32 or None, top_logp [T, n_top] or None).  A row
+    with a negative token id is skipped: zeros, top_ids -1."""
+    s, ptr, dev = _logits_shape(logits, token_ids, temperature)
+    f32 = dict(dtype=torch.float32, device=dev)
+    logp = torch.empty(s.T, **f32) if token_ids is not None else None
+    entropy = torch.empty(s.T, **f32) if want_entropy else None
+    stats = torch.empty((s.T, 2), **f32) if want_stats else None
+    n_top = int(n_top)
+    top_ids = top_logp = None
+    if n_top > 0:
+        top_ids = torch.empty((s.T, n_top), dtype=torch.int32, device=dev)
+        top_logp = torch.empty((s.T, n_top), **f32)
+    _check(lib.r3_token_logprobs(ctypes.byref(s), ptr, _ptr(token_ids), _ptr(logp), _ptr(entropy),
+                                 _ptr(stats), n_top, _ptr(top_ids), _ptr(top_logp),
+                                 _ptr(dev_status), _stream(stream)))
+    return logp, entropy, stats, top_ids, top_logp
+
+
+def token_logprobs_bwd(logits, token_ids, stats, dlogp, *, entropy=None, dentropy=None,
+                       temperature=1.0, dlogits=None, dev_status=None, stream=None):
+    """Gradient to the logits from dlogp [T] (or None) and, with the forward's entropy [T], from
+    dentropy [T].  stats [T, 2] and temperature as in the forward.  dlogits may be given (the logits
+    themselves, for a gradient in place)."""
+    s, ptr, dev = _logits_shape(logits, token_ids, temperature)
+    if dlogits is None:
+        dlogits = torch.empty((s.T, s.V), dtype=logits.dtype, device=dev)
+    else:
+        _expect("dlogits", dlogits, (s.T, s.V), logits.dtype, dev)
+    out, ld_out = _rows("dlogits", dlogits)
+    _expect("stats", stats, (s.T, 2), torch.float32, dev)
+    for name, t in (("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy)):
+        _expect(name, t, (s.T,), torch.float32, dev)
+    _check(lib.r3_token_logprobs_bwd(ctypes.byref(s), ptr, _ptr(token_ids), _ptr(stats),
+                                     _ptr(entropy), _ptr(dlogp), _ptr(dentropy), out, ld_out,
+                                     _ptr(dev_status), _stream(stream)))
+    return dlogits
+
+
 def prob_discrepancy(p_train, p_infer, taus, *, kl=None, counts=None, ws=None, stream=None):
     """k3 KL estimate (Eq. kl) and extreme-token counts (Eq. etdf) of two float32 probability
     arrays.  `taus`: a list or a float32 device tensor.  Returns (kl [1] float64, counts [n_tau]

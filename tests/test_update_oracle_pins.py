@@ -1,0 +1,69 @@
+"""Pins of oracle/r3_update_oracle.py: closed forms, brute force and central finite differences."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import r3_update_oracle as U
+
+
+def fd(f, x, h=1e-6):
+    """Central differences of the scalar f in every element of x."""
+    g = np.zeros_like(x)
+    it = np.nditer(x, flags=["multi_index"])
+    for _ in it:
+        i = it.multi_index
+        keep = x[i]
+        x[i] = keep + h
+        hi = f()
+        x[i] = keep - h
+        lo = f()
+        x[i] = keep
+        g[i] = (hi - lo) / (2 * h)
+    return g
+
+
+def test_logprobs_closed_forms():
+    # logits ln 1, ln 2, ln 5: probabilities 1/8, 2/8, 5/8
+    z = np.log(np.array([[1.0, 2.0, 5.0]]))
+    r = U.token_logprobs(z, [1], n_top=3)
+    assert abs(r["logp"][0] - math.log(0.25)) < 1e-15
+    h = -sum(p * math.log(p) for p in (0.125, 0.25, 0.625))
+    assert abs(r["entropy"][0] - h) < 1e-15
+    assert r["top_ids"].tolist() == [[2, 1, 0]]
+    assert abs(r["stats"][0, 0] + r["stats"][0, 1] - math.log(8.0)) < 1e-15
+    # temperature 1/2 squares the weights: 1/30, 4/30, 25/30
+    r = U.token_logprobs(z, [1], temperature=0.5)
+    assert abs(r["logp"][0] - math.log(4.0 / 30.0)) < 1e-15
+    # uniform rows, whatever the level: log p = -ln V, entropy ln V
+    for level in (0.0, -3e38, 88.0):
+        r = U.token_logprobs(np.full((1, 7), level), [3], n_top=2)
+        assert abs(r["logp"][0] + math.log(7)) < 1e-15 and abs(r["entropy"][0] - math.log(7)) < 1e-14
+        assert r["top_ids"].tolist() == [[0, 1]]
+
+
+def test_logprobs_special_rows():
+    z = np.array([[0.0, 1.0, -np.inf], [-np.inf] * 3, [0.0, np.nan, 0.0], [0.0, np.inf, 0.0],
+                  [1.0, 2.0, 3.0]])
+    r = U.token_logprobs(z, [2, 0, 0, 0, -1], n_top=2)
+    assert r["logp"][0] == -np.inf and np.isfinite(r["entropy"][0])
+    assert r["logp"][1] == -np.inf and r["entropy"][1] == 0 and r["top_ids"][1].tolist() == [0, 1]
+    assert np.isnan(r["logp"][2]) and np.isnan(r["entropy"][3]) and r["top_ids"][3].tolist() == [-1, -1]
+    assert r["logp"][4] == 0 and r["top_ids"][4].tolist() == [-1, -1]
+
+
+@pytest.mark.parametrize("temperature", [1.0, 0.6])
+def test_logprobs_gradient_by_differences(temperature):
+    rng = np.random.default_rng(3)
+    z = rng.normal(size=(4, 9)) * 2
+    ids = np.array([0, 8, -1, 3])
+    dl, de = rng.normal(size=4), rng.normal(size=4)
+
+    def loss():
+        r = U.token_logprobs(z, ids, temperature)
+        return float((dl * r["logp"] + de * r["entropy"]).sum())
+
+    g = U.token_logprobs_bwd(z, ids, dl, de, temperature)
+    assert np.abs(g - fd(loss, z)).max() < 1e-8
+    assert np.abs(g.sum(1)).max() < 1e-13            # the softmax does not see a common shift
+    assert not g[2].any()

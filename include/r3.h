@@ -496,6 +496,47 @@ r3_status r3_replay_finish_rows(const r3_shape* shape, const float* logits, cons
                                 const void* residual, void* y, float* gates_out, float* dlogits,
                                 int32_t* dev_status, void* stream);
 
+/* ---- between two blocks: norm, gate, scaled residual, norm (an extension; the paper's model has
+ * norms around its blocks and does not discuss them) ---------------------------------------------- */
+
+/* What the gate of a block's output is, and along what it is broadcast over [T, d]. */
+enum { R3_GATE_NONE = 0, R3_GATE_CHANNEL = 1, R3_GATE_TOKEN = 2, R3_GATE_FULL = 3 };
+
+/* T rows of d columns (a multiple of 8) of act_dtype; w_dtype is the type of w_post, w_pre and of a
+ * CHANNEL gate [d].  A TOKEN gate [T] is float32, a FULL gate [T,d] act_dtype.  eps > 0. */
+typedef struct {
+    int32_t T, d;
+    int32_t act_dtype, w_dtype, gate_kind;
+    float eps, residual_scale, branch_scale;
+} r3_norm;
+
+/* The step from one residual block to the next, in one pass:
+ *   n     = y rsqrt(mean(y^2) + eps) w_post          RMSNorm behind the block (n = y if w_post is NULL)
+ *   x_out = residual_scale x + branch_scale gate n
+ *   h     = x_out rsqrt(mean(x_out^2) + eps) w_pre   RMSNorm in front of the next block
+ * x [T,d] the residual stream, y [T,d] the block's output.  h is formed from the float32 x_out, each
+ * output is rounded once.  y NULL (with w_post, gate and x_out NULL): in front of the first block,
+ * h = the norm of x.  w_pre and h NULL: behind the last block.  x_out may be x's buffer, and h y's.
+ * d up to 16384 for bf16 and 8192 for f32 (R3_ERR_UNSUPPORTED beyond).  No workspace. */
+r3_status r3_norm_residual(const r3_norm* shape, const void* x, const void* y, const void* w_post,
+                           const void* gate, const void* w_pre, void* x_out, void* h, void* stream);
+
+/* Its gradients, from dx_out = dL/dx_out [T,d] (NULL = 0) and dh = dL/dh [T,d]:
+ *   g = dx_out + (gradient of the pre-norm at x_out);   dx = residual_scale g;
+ *   dy, dw_post, dgate through the branch;   dw_pre = sum_t dh x_out rsqrt(mean(x_out^2) + eps)
+ * x_out and y as the forward left them (x_out is x where y is NULL; it is not needed without w_pre).
+ * dx, dy [T,d] act_dtype; dw_post, dw_pre [d] float32; dgate float32 [d] (CHANNEL) or [T] (TOKEN),
+ * act_dtype [T,d] (FULL).  All are overwritten; the sums over tokens are formed in float32 in an
+ * order that depends on the shape alone.  An output is given exactly where its input is.  dx may be
+ * dx_out's or dh's buffer, dy may be y's, dh's or dx_out's (dx and dy differ).  workspace:
+ * r3_norm_residual_bwd_workspace_bytes(shape), 256-byte aligned. */
+size_t r3_norm_residual_bwd_workspace_bytes(const r3_norm* shape);
+r3_status r3_norm_residual_bwd(const r3_norm* shape, const void* x_out, const void* y,
+                               const void* w_post, const void* gate, const void* w_pre,
+                               const void* dx_out, const void* dh, void* dx, void* dy,
+                               float* dw_post, void* dgate, float* dw_pre, void* workspace,
+                               size_t ws_bytes, void* stream);
+
 /* ---- token log probabilities (the p_train and p_infer of Sections 3.1 and 3.2) -------------- */
 
 /* A batch of logits: T rows of V values, row t at logits + t * ld elements (ld >= V, so a padded or

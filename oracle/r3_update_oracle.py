@@ -62,3 +62,60 @@ def token_logprobs_bwd(logits, token_ids, dlogp, dentropy=None, temperature=1.0)
             d[live] -= dentropy[t] * p[live] * (lp[live] + f["entropy"][t])
         out[t] = d / temperature
     return out
+
+
+# ---- norm, gate, scaled residual, norm ---------------------------------------------------------
+def _gate_2d(gate, T, d):
+    """gate None, [d], [T, 1] or [T, d] as a factor over [T, d]."""
+    return np.ones((T, d)) if gate is None else np.broadcast_to(np.asarray(gate, dtype=np.float64), (T, d))
+
+
+def rms_norm(v, w, eps):
+    v = np.asarray(v, dtype=np.float64)
+    return v / np.sqrt((v * v).mean(axis=1, keepdims=True) + eps) * w
+
+
+def norm_residual(x, y, w_post=None, gate=None, w_pre=None, eps=1e-6, residual_scale=1.0,
+                  branch_scale=1.0):
+    """(x_out or None, h or None)."""
+    x = np.asarray(x, dtype=np.float64)
+    if y is None:
+        return None, rms_norm(x, w_pre, eps)
+    y = np.asarray(y, dtype=np.float64)
+    n = y if w_post is None else rms_norm(y, w_post, eps)
+    x_out = residual_scale * x + branch_scale * _gate_2d(gate, *x.shape) * n
+    return x_out, None if w_pre is None else rms_norm(x_out, w_pre, eps)
+
+
+def rms_norm_bwd(v, w, eps, dn):
+    """(dv, dw) of rms_norm for the upstream gradient dn."""
+    r = 1.0 / np.sqrt((v * v).mean(axis=1, keepdims=True) + eps)
+    u = dn * w
+    return r * u - v * r ** 3 * (u * v).mean(axis=1, keepdims=True), (dn * v * r).sum(axis=0)
+
+
+def norm_residual_bwd(x_out, y, dx_out, dh=None, w_post=None, gate=None, w_pre=None, eps=1e-6,
+                      residual_scale=1.0, branch_scale=1.0):
+    """dict of dx, dy, dw_post, dgate (in the gate's shape), dw_pre; x_out is x where y is None."""
+    out = {}
+    g = 0.0 if dx_out is None else np.asarray(dx_out, dtype=np.float64)
+    if w_pre is not None:
+        through, out["dw_pre"] = rms_norm_bwd(x_out, w_pre, eps, dh)
+        g = g + through
+    if y is None:
+        out["dx"] = g
+        return out
+    T, d = y.shape
+    out["dx"] = residual_scale * g
+    n = y if w_post is None else rms_norm(y, w_post, eps)
+    q = branch_scale * g
+    dgate, dn = q * n, q * _gate_2d(gate, T, d)
+    if gate is not None:
+        shape = np.asarray(gate).shape
+        out["dgate"] = dgate if shape == (T, d) else (dgate.sum(axis=1, keepdims=True)
+                                                      if shape == (T, 1) else dgate.sum(axis=0))
+    if w_post is None:
+        out["dy"] = dn
+    else:
+        out["dy"], out["dw_post"] = rms_norm_bwd(y, w_post, eps, dn)
+    return out

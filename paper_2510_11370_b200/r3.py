@@ -24,6 +24,7 @@ R3_ERR_SCRATCH_LIMIT = 5
 R3_ERR_OUT_OF_PAGES = 6
 R3_F32, R3_BF16 = 0, 1
 R3_IDX_U8, R3_IDX_I16 = 1, 2
+R3_GATE_NONE, R3_GATE_CHANNEL, R3_GATE_TOKEN, R3_GATE_FULL = 0, 1, 2, 3
 DEV_OK, DEV_BAD_INDEX, DEV_DUP_INDEX, DEV_TIMEOUT = 0, 1, 2, 3
 
 EXPORTS = [
@@ -39,6 +40,7 @@ EXPORTS = [
     "r3_replay_layer_host_workspace_bytes", "r3_replay_layer_host", "r3_replay_layer_host_enqueue",
     "r3_replay_layer_host_chunks",
     "r3_replay_layer_same_record",
+    "r3_norm_residual", "r3_norm_residual_bwd_workspace_bytes", "r3_norm_residual_bwd",
     "r3_token_logprobs", "r3_token_logprobs_bwd",
     "r3_prob_discrepancy_workspace_bytes", "r3_prob_discrepancy", "r3_record_diff",
     "r3_sequence_diff", "r3_grouped_swiglu_bwd_workspace_bytes", "r3_grouped_swiglu_bwd_input",
@@ -64,6 +66,13 @@ class Logits(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int32), ("V", ctypes.c_int32), ("ld", ctypes.c_int64),
                 ("dtype", ctypes.c_int32), ("id_bytes", ctypes.c_int32),
                 ("temperature", ctypes.c_double)]
+
+
+class Norm(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("d", ctypes.c_int32), ("act_dtype", ctypes.c_int32),
+                ("w_dtype", ctypes.c_int32), ("gate_kind", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float),
+                ("branch_scale", ctypes.c_float)]
 
 
 _P = ctypes.c_void_p
@@ -115,6 +124,11 @@ lib.r3_replay_layer.argtypes = [_SP] + [_P] * 11 + [ctypes.c_size_t, _P, _P]
 lib.r3_replay_layer_same_record.argtypes = [_SP] + [_P] * 11 + [ctypes.c_size_t, _P, _P]
 lib.r3_replay_layer_host.argtypes = [_SP] + [_P] * 10 + [ctypes.c_size_t, _P, _P]
 lib.r3_replay_layer_host_enqueue.argtypes = [_SP] + [_P] * 10 + [ctypes.c_size_t, _P, _P]
+_NP = ctypes.POINTER(Norm)
+lib.r3_norm_residual.argtypes = [_NP] + [_P] * 8
+lib.r3_norm_residual_bwd_workspace_bytes.restype = ctypes.c_size_t
+lib.r3_norm_residual_bwd_workspace_bytes.argtypes = [_NP]
+lib.r3_norm_residual_bwd.argtypes = [_NP] + [_P] * 13 + [ctypes.c_size_t, _P]
 lib.r3_token_logprobs.argtypes = [ctypes.POINTER(Logits)] + [_P] * 5 + [ctypes.c_int32] + [_P] * 4
 lib.r3_token_logprobs_bwd.argtypes = ([ctypes.POINTER(Logits)] + [_P] * 7 + [ctypes.c_int64]
                                       + [_P] * 2)
@@ -545,6 +559,80 @@ def _device_of(name: str, t) -> torch.device:
     if t.device.index != torch.cuda.current_device():
         raise ValueError(f"{name}: on {t.device}, which is not the current device")
     return t.device
+
+
+def _norm_shape(rows, d, act, w_post, gate, w_pre, eps, residual_scale, branch_scale, dev):
+    """The r3_norm of a call, its vectors checked: w_post, w_pre and a gate [d] share one type."""
+    if act not in _ACT:
+        raise ValueError(f"activations: dtype {act}, expected float32 or bfloat16")
+    kind = R3_GATE_NONE
+    if gate is not None:
+        kinds = {(d,): R3_GATE_CHANNEL, (rows, 1): R3_GATE_TOKEN, (rows, d): R3_GATE_FULL}
+        kind = kinds.get(tuple(gate.shape))
+        if kind is None:
+            raise ValueError(f"gate: shape {tuple(gate.shape)}, expected [{d}], [{rows}, 1] or "
+                             f"[{rows}, {d}]")
+    vectors = [v for v in (w_post, w_pre, gate if kind == R3_GATE_CHANNEL else None) if v is not None]
+    w_dtype = vectors[0].dtype if vectors else act
+    if w_dtype not in _ACT:
+        raise ValueError(f"weights: dtype {w_dtype}, expected float32 or bfloat16")
+    for name, v in (("w_post", w_post), ("w_pre", w_pre)):
+        _expect(name, v, (d,), w_dtype, dev)
+    if gate is not None:
+        want = {R3_GATE_CHANNEL: w_dtype, R3_GATE_TOKEN: torch.float32, R3_GATE_FULL: act}[kind]
+        _expect("gate", gate, gate.shape, want, dev)
+    return Norm(rows, d, _ACT[act], _ACT[w_dtype], kind, eps, residual_scale, branch_scale)
+
+
+def norm_residual(x, y=None, *, w_post=None, gate=None, w_pre=None, eps=1e-6, residual_scale=1.0,
+                  branch_scale=1.0, x_out=None, h=None, stream=None):
+    """From one residual block to the next: x_out = residual_scale x + branch_scale gate
+    RMSNorm(y) w_post, h = RMSNorm(x_out) w_pre, in one pass.  x, y [T, d] float32 or bfloat16; gate
+    None, [d], [T, 1] float32 or [T, d].  Without y only h = RMSNorm(x) w_pre; without w_post the
+    branch is not normalised; without w_pre there is no h.  Returns (x_out, h), None for what there
+    is not.  x_out may be x, h may be y (in place)."""
+    dev = _device_of("x", x)
+    rows, d = x.shape
+    s = _norm_shape(rows, d, x.dtype, w_post, gate, w_pre, eps, residual_scale, branch_scale, dev)
+    if y is not None and x_out is None:
+        x_out = torch.empty_like(x)
+    if w_pre is not None and h is None:
+        h = torch.empty_like(x)
+    for name, t in (("y", y), ("x_out", x_out), ("h", h)):
+        _expect(name, t, (rows, d), x.dtype, dev)
+    _check(lib.r3_norm_residual(ctypes.byref(s), _ptr(x), _ptr(y), _ptr(w_post), _ptr(gate),
+                                _ptr(w_pre), _ptr(x_out), _ptr(h), _stream(stream)))
+    return x_out, h
+
+
+def norm_residual_bwd(x_out, y, dx_out, dh=None, *, w_post=None, gate=None, w_pre=None, eps=1e-6,
+                      residual_scale=1.0, branch_scale=1.0, dx=None, dy=None, ws=None, stream=None):
+    """Gradients of norm_residual from dx_out [T, d] (or None) and dh [T, d]: (dx, dy, dw_post [d],
+    dgate, dw_pre [d]), None for what the call has not; dw_* and the dgate of a gate [d] or [T, 1]
+    are float32.  x_out and y are the forward's (x_out may be None without w_pre)."""
+    like = x_out if x_out is not None else dx_out
+    dev = _device_of("x_out", like)
+    rows, d = like.shape
+    s = _norm_shape(rows, d, like.dtype, w_post, gate, w_pre, eps, residual_scale, branch_scale, dev)
+    if dx is None:
+        dx = torch.empty_like(like)
+    if y is not None and dy is None:
+        dy = torch.empty_like(like)
+    for name, t in (("x_out", x_out), ("y", y), ("dx_out", dx_out), ("dh", dh), ("dx", dx), ("dy", dy)):
+        _expect(name, t, (rows, d), like.dtype, dev)
+    dgate = None
+    if gate is not None:
+        full = s.gate_kind == R3_GATE_FULL
+        dgate = torch.empty(gate.shape, dtype=like.dtype if full else torch.float32, device=dev)
+    dw_post, dw_pre = (torch.empty(d, dtype=torch.float32, device=dev) if w is not None else None
+                       for w in (w_post, w_pre))
+    if ws is None:
+        ws = workspace(lib.r3_norm_residual_bwd_workspace_bytes(ctypes.byref(s)), dev)
+    _check(lib.r3_norm_residual_bwd(ctypes.byref(s), _ptr(x_out), _ptr(y), _ptr(w_post), _ptr(gate),
+                                    _ptr(w_pre), _ptr(dx_out), _ptr(dh), _ptr(dx), _ptr(dy),
+                                    _ptr(dw_post), _ptr(dgate), _ptr(dw_pre), _ptr(ws), ws.numel(),
+                                    _stream(stream)))
+    return dx, dy, dw_post, dgate, dw_pre
 
 
 def _rows(name: str, t):

@@ -67,3 +67,56 @@ def test_logprobs_gradient_by_differences(temperature):
     assert np.abs(g - fd(loss, z)).max() < 1e-8
     assert np.abs(g.sum(1)).max() < 1e-13            # the softmax does not see a common shift
     assert not g[2].any()
+
+
+# ---- norms around a block ------------------------------------------------------------------------
+def test_norm_closed_forms():
+    # a row of equal magnitudes a has rms a: the norm gives its signs
+    y = np.array([[3.0, -3.0, 3.0, 3.0], [0.0, 0.0, 0.0, 0.0]])
+    w = np.array([1.0, 2.0, 3.0, 4.0])
+    assert np.allclose(U.rms_norm(y, w, 1e-300)[0], [1, -2, 3, 4], rtol=0, atol=1e-15)
+    assert not U.rms_norm(y, w, 1e-6)[1].any()
+    x = np.ones((2, 4))
+    x_out, h = U.norm_residual(x, y, w_post=np.ones(4), gate=np.array([[0.5], [2.0]]), eps=1e-300,
+                               residual_scale=2.0, branch_scale=4.0)
+    assert np.allclose(x_out[0], [4, 0, 4, 4], rtol=0, atol=1e-14) and np.allclose(x_out[1], 2.0)
+    assert h is None
+    none, h = U.norm_residual(x * 5, None, w_pre=w, eps=1e-300)
+    assert none is None and np.allclose(h, np.stack([w, w]), rtol=0, atol=1e-14)
+
+
+@pytest.mark.parametrize("kind", ["none", "channel", "token", "full"])
+@pytest.mark.parametrize("post,pre", [(True, True), (True, False), (False, True), (False, False)])
+def test_norm_gradients_by_differences(kind, post, pre):
+    rng = np.random.default_rng(5)
+    T, d = 3, 8
+    x, y = rng.normal(size=(T, d)), rng.normal(size=(T, d))
+    p = dict(w_post=1 + 0.3 * rng.normal(size=d) if post else None,
+             w_pre=1 + 0.3 * rng.normal(size=d) if pre else None,
+             gate={"none": None, "channel": rng.normal(size=d), "token": rng.normal(size=(T, 1)),
+                   "full": rng.normal(size=(T, d))}[kind])
+    kw = dict(eps=0.1, residual_scale=1.3, branch_scale=0.7)
+    a, b = rng.normal(size=(T, d)), rng.normal(size=(T, d))
+
+    def loss():
+        x_out, h = U.norm_residual(x, y, **p, **kw)
+        return float((a * x_out).sum() + ((b * h).sum() if pre else 0.0))
+
+    x_out = U.norm_residual(x, y, **p, **kw)[0]
+    g = U.norm_residual_bwd(x_out, y, a, b if pre else None, **p, **kw)
+    for name, v in (("dx", x), ("dy", y), ("dw_post", p["w_post"]), ("dw_pre", p["w_pre"]),
+                    ("dgate", p["gate"])):
+        if v is None:
+            assert name not in g
+        else:
+            assert g[name].shape == v.shape and np.abs(g[name] - fd(loss, v)).max() < 1e-8, name
+
+
+def test_norm_gradient_in_front_of_the_first_block():
+    rng = np.random.default_rng(6)
+    x, w, b = rng.normal(size=(3, 8)), rng.normal(size=8), rng.normal(size=(3, 8))
+    g = U.norm_residual_bwd(x, None, None, b, w_pre=w, eps=0.1)
+
+    def loss():
+        return float((b * U.norm_residual(x, None, w_pre=w, eps=0.1)[1]).sum())
+    assert np.abs(g["dx"] - fd(loss, x)).max() < 1e-8 and np.abs(g["dw_pre"] - fd(loss, w)).max() < 1e-8

@@ -537,6 +537,55 @@ r3_status r3_norm_residual_bwd(const r3_norm* shape, const void* x_out, const vo
                                float* dw_post, void* dgate, float* dw_pre, void* workspace,
                                size_t ws_bytes, void* stream);
 
+/* ---- optimiser step (an extension: what follows the weight gradients of the training calls) ------ */
+
+/* One tensor of a step; the struct lives in HOST memory, its pointers are device pointers (16-byte
+ * aligned, the scales 4-byte).  n elements (0: the entry is skipped).
+ *   param             n of param_dtype, updated
+ *   master            n float32 (with config->master, for bf16 parameters: the step updates them and
+ *                     stores their rounding to param, which is not read) or NULL
+ *   grad              n of grad_dtype
+ *   exp_avg, exp_avg_sq   states: n float32 each; or, with 8-bit states, n e4m3 codes each and one
+ *                     float32 scale per 256 elements (ceil(n / 256)) in exp_avg_scale and
+ *                     exp_avg_sq_scale.  A value is code * scale; exp_avg_sq then holds the square
+ *                     ROOT of the second moment.  All zero bytes are the fresh state in both forms. */
+typedef struct {
+    void* param;
+    float* master;
+    const void* grad;
+    void* exp_avg;
+    void* exp_avg_sq;
+    float* exp_avg_scale;
+    float* exp_avg_sq_scale;
+    int64_t n;
+    float weight_decay;
+} r3_adamw_tensor;
+
+/* step t counts from 1; master is 0 or 1; state_bits 8 or 32; eps >= 1e-30. */
+typedef struct {
+    int32_t param_dtype, grad_dtype, master, state_bits;
+    int64_t step;
+    double lr, beta1, beta2, eps;
+} r3_adamw;
+
+/* One AdamW step over n_tensors tensors (a HOST array) in one launch per 400:
+ *   g = grad * grad_scale
+ *   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2
+ *   w = w (1 - lr weight_decay) - lr m / (1 - beta1^t) / ( sqrt(v / (1 - beta2^t)) + eps )
+ * in float32, w rounded once to param_dtype.  8-bit states: the scale of a block of 256 elements is
+ * the smallest power of two (at least 2^-126) that brings its largest magnitude to 448 or less, a
+ * code is the nearest e4m3 value (ties to even), a root above 0 gets at least the smallest code;
+ * the stored states are a function of the inputs alone, bit for bit.
+ *  - grad_scale (device, float32, or NULL = 1): a loss scale's inverse or a clipping factor.  If it
+ *    is not finite the whole step is skipped: nothing is written.
+ *  - scalars (device, [3] float32, or NULL): {lr, 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)} in place of
+ *    config's lr and step, for a captured step that is replayed with new values.
+ *  - A gradient element that is not finite makes its own weight and states NaN (an 8-bit state: the
+ *    NaN code; the scale is that of the block's finite elements).
+ * Two entries whose params overlap are refused; no other buffers may overlap.  No workspace. */
+r3_status r3_adamw_step(const r3_adamw* config, const r3_adamw_tensor* tensors, int32_t n_tensors,
+                        const float* grad_scale, const float* scalars, void* stream);
+
 /* ---- token log probabilities (the p_train and p_infer of Sections 3.1 and 3.2) -------------- */
 
 /* A batch of logits: T rows of V values, row t at logits + t * ld elements (ld >= V, so a padded or

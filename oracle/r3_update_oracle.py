@@ -119,3 +119,49 @@ def norm_residual_bwd(x_out, y, dx_out, dh=None, w_post=None, gate=None, w_pre=N
     else:
         out["dy"], out["dw_post"] = rms_norm_bwd(y, w_post, eps, dn)
     return out
+
+
+# ---- AdamW -----------------------------------------------------------------------------------------
+BLOCK = 256
+E4M3_MAX, E4M3_MIN = 448.0, 2.0 ** -9
+
+
+def adamw(w, g, m, v, step, lr, betas, eps, decay, grad_scale=1.0):
+    """One step on float64 arrays: (w, m, v)."""
+    g = np.asarray(g, dtype=np.float64) * grad_scale
+    m = betas[0] * m + (1 - betas[0]) * g
+    v = betas[1] * v + (1 - betas[1]) * g * g
+    mh, vh = m / (1 - betas[0] ** step), v / (1 - betas[1] ** step)
+    return w - lr * decay * w - lr * mh / (np.sqrt(vh) + eps), m, v
+
+
+def block_scale(x):
+    """[blocks, 256] -> the smallest power of two >= 2^-126 that brings each block to at most 448."""
+    top = np.abs(np.asarray(x, dtype=np.float64)).max(axis=1)
+    out = np.empty_like(top)
+    for b, t in enumerate(top):
+        k = -126
+        while t > E4M3_MAX * 2.0 ** k:
+            k += 1
+        out[b] = 2.0 ** k
+    return out
+
+
+def e4m3_values():
+    """The non-negative finite values of the type, by code."""
+    vals = []
+    for code in range(127):
+        e, f = code >> 3, code & 7
+        vals.append(f * 2.0 ** -9 if e == 0 else (1 + f / 8) * 2.0 ** (e - 7))
+    return np.array(vals)
+
+
+def nearest_e4m3(q):
+    """The nearest e4m3 value of each element (|q| <= 448), ties to the even code."""
+    vals = e4m3_values()
+    a = np.abs(np.asarray(q, dtype=np.float64))
+    hi = np.searchsorted(vals, a).clip(0, 126)
+    lo = (hi - 1).clip(0)
+    up, down = vals[hi] - a, a - vals[lo]
+    code = np.where((up < down) | ((up == down) & (hi % 2 == 0)), hi, lo)
+    return np.copysign(vals[code], q)

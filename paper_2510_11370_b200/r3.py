@@ -40,6 +40,7 @@ EXPORTS = [
     "r3_replay_layer_host_workspace_bytes", "r3_replay_layer_host", "r3_replay_layer_host_enqueue",
     "r3_replay_layer_host_chunks",
     "r3_replay_layer_same_record",
+    "r3_adamw_step",
     "r3_norm_residual", "r3_norm_residual_bwd_workspace_bytes", "r3_norm_residual_bwd",
     "r3_token_logprobs", "r3_token_logprobs_bwd",
     "r3_prob_discrepancy_workspace_bytes", "r3_prob_discrepancy", "r3_record_diff",
@@ -73,6 +74,20 @@ class Norm(ctypes.Structure):
                 ("w_dtype", ctypes.c_int32), ("gate_kind", ctypes.c_int32),
                 ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float),
                 ("branch_scale", ctypes.c_float)]
+
+
+class AdamWTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("master", ctypes.c_void_p), ("grad", ctypes.c_void_p),
+                ("exp_avg", ctypes.c_void_p), ("exp_avg_sq", ctypes.c_void_p),
+                ("exp_avg_scale", ctypes.c_void_p), ("exp_avg_sq_scale", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("weight_decay", ctypes.c_float)]
+
+
+class AdamWConfig(ctypes.Structure):
+    _fields_ = [("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
+                ("master", ctypes.c_int32), ("state_bits", ctypes.c_int32), ("step", ctypes.c_int64),
+                ("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double)]
 
 
 _P = ctypes.c_void_p
@@ -124,6 +139,7 @@ lib.r3_replay_layer.argtypes = [_SP] + [_P] * 11 + [ctypes.c_size_t, _P, _P]
 lib.r3_replay_layer_same_record.argtypes = [_SP] + [_P] * 11 + [ctypes.c_size_t, _P, _P]
 lib.r3_replay_layer_host.argtypes = [_SP] + [_P] * 10 + [ctypes.c_size_t, _P, _P]
 lib.r3_replay_layer_host_enqueue.argtypes = [_SP] + [_P] * 10 + [ctypes.c_size_t, _P, _P]
+lib.r3_adamw_step.argtypes = [ctypes.POINTER(AdamWConfig), _P, ctypes.c_int32, _P, _P, _P]
 _NP = ctypes.POINTER(Norm)
 lib.r3_norm_residual.argtypes = [_NP] + [_P] * 8
 lib.r3_norm_residual_bwd_workspace_bytes.restype = ctypes.c_size_t
@@ -633,6 +649,110 @@ def norm_residual_bwd(x_out, y, dx_out, dh=None, *, w_post=None, gate=None, w_pr
                                     _ptr(dw_post), _ptr(dgate), _ptr(dw_pre), _ptr(ws), ws.numel(),
                                     _stream(stream)))
     return dx, dy, dw_post, dgate, dw_pre
+
+
+ADAMW_BLOCK = 256        # elements that share one scale of an 8-bit state
+
+
+class AdamW:
+    """AdamW over a list of tensors, one launch per step (r3_adamw_step): the handle that a training
+    program keeps beside its parameters.
+
+    params, grads: lists of contiguous CUDA tensors of equal sizes, one dtype each (float32 or
+    bfloat16).  masters: None, True (float32 copies of bfloat16 params are made and kept) or a list
+    of float32 tensors.  States are made (zero) or given as lists: float32, or with state_bits=8
+    float8_e4m3fn codes plus one float32 scale per 256 elements (exp_avg_sq then holds the root of
+    the second moment).  weight_decay: a number, or one per tensor.  The handle keeps its tensors
+    alive; set_grads() exchanges the gradients."""
+
+    def __init__(self, params, grads, *, masters=None, exp_avg=None, exp_avg_sq=None,
+                 exp_avg_scale=None, exp_avg_sq_scale=None, state_bits=32, betas=(0.9, 0.95),
+                 eps=1e-8, weight_decay=0.0):
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("AdamW: no tensors")
+        self._dev = _device_of("params[0]", self.params[0])
+        if state_bits not in (8, 32):
+            raise ValueError(f"state_bits: {state_bits}, expected 8 or 32")
+        self.state_bits = state_bits
+        sizes = [p.numel() for p in self.params]
+        dtype = self.params[0].dtype
+        if dtype not in _ACT:
+            raise ValueError(f"params: dtype {dtype}, expected float32 or bfloat16")
+        if masters is True:
+            masters = [p.detach().float() for p in self.params]
+        self.masters = list(masters) if masters is not None else None
+        if self.masters is not None and dtype != torch.bfloat16:
+            raise ValueError("masters: only for bfloat16 params")
+
+        def state(given, dtype, counts):
+            if given is not None:
+                return list(given)
+            return [torch.zeros(n, dtype=torch.uint8, device=self._dev).view(dtype)
+                    if dtype == torch.float8_e4m3fn else
+                    torch.zeros(n, dtype=dtype, device=self._dev) for n in counts]
+        kind = torch.float8_e4m3fn if state_bits == 8 else torch.float32
+        self.exp_avg, self.exp_avg_sq = state(exp_avg, kind, sizes), state(exp_avg_sq, kind, sizes)
+        self.exp_avg_scale = self.exp_avg_sq_scale = None
+        scales = [-(-n // ADAMW_BLOCK) for n in sizes]
+        if state_bits == 8:
+            self.exp_avg_scale = state(exp_avg_scale, torch.float32, scales)
+            self.exp_avg_sq_scale = state(exp_avg_sq_scale, torch.float32, scales)
+        elif exp_avg_scale is not None or exp_avg_sq_scale is not None:
+            raise ValueError("scales: only for 8-bit states")
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(sizes)
+        self._table = (AdamWTensor * len(sizes))()
+        self._fill("param", self.params, sizes, dtype)
+        self._fill("master", self.masters, sizes, torch.float32)
+        self._fill("exp_avg", self.exp_avg, sizes, kind)
+        self._fill("exp_avg_sq", self.exp_avg_sq, sizes, kind)
+        self._fill("exp_avg_scale", self.exp_avg_scale, scales, torch.float32)
+        self._fill("exp_avg_sq_scale", self.exp_avg_sq_scale, scales, torch.float32)
+        if len(decay) != len(sizes):
+            raise ValueError(f"weight_decay: {len(decay)} values for {len(sizes)} tensors")
+        for row, n, wd in zip(self._table, sizes, decay):
+            row.n, row.weight_decay = n, wd
+        self._config = AdamWConfig(_ACT[dtype], 0, int(self.masters is not None), state_bits, 1, 0.0,
+                                   float(betas[0]), float(betas[1]), float(eps))
+        self.set_grads(grads)
+
+    def _fill(self, field, tensors, sizes, dtype):
+        if tensors is None:
+            return
+        if len(tensors) != len(sizes):
+            raise ValueError(f"{field}: {len(tensors)} tensors for {len(sizes)} params")
+        for i, (row, t, n) in enumerate(zip(self._table, tensors, sizes)):
+            if t.numel() != n:
+                raise ValueError(f"{field}[{i}]: {t.numel()} elements, expected {n}")
+            _expect(f"{field}[{i}]", t, t.shape, dtype, self._dev)
+            setattr(row, field, _ptr(t).value)
+
+    def set_grads(self, grads):
+        """Exchanges the gradients of the steps to come."""
+        grads = list(grads)
+        dtype = grads[0].dtype if grads else None
+        if dtype not in _ACT:
+            raise ValueError(f"grads: dtype {dtype}, expected float32 or bfloat16")
+        self._fill("grad", grads, [p.numel() for p in self.params], dtype)
+        self.grads = grads
+        self._config.grad_dtype = _ACT[dtype]
+
+    def scalars(self, step, lr):
+        """What a step's `scalars` tensor has to hold for this step and learning rate."""
+        c = self._config
+        return [lr, 1.0 / (1.0 - c.beta1 ** step), 1.0 / (1.0 - c.beta2 ** step) ** 0.5]
+
+    def step(self, step, lr, *, grad_scale=None, scalars=None, stream=None):
+        """Step number `step` (from 1).  grad_scale: [1] float32 on the device, multiplies every
+        gradient; not finite = the step is skipped.  scalars: [3] float32 on the device with the
+        values of self.scalars(), used instead of step and lr (for a captured step)."""
+        if self._dev.index != torch.cuda.current_device():
+            raise ValueError(f"AdamW: tensors on {self._dev}, which is not the current device")
+        _expect("grad_scale", grad_scale, (1,), torch.float32, self._dev)
+        _expect("scalars", scalars, (3,), torch.float32, self._dev)
+        self._config.step, self._config.lr = int(step), float(lr)
+        _check(lib.r3_adamw_step(ctypes.byref(self._config), self._table, len(self.params),
+                                 _ptr(grad_scale), _ptr(scalars), _stream(stream)))
 
 
 def _rows(name: str, t):

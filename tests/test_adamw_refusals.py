@@ -1,0 +1,66 @@
+"""What the AdamW step refuses on the host: nothing is launched by anything here."""
+import ctypes
+
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def r3():
+    from paper_2510_11370_b200 import build
+    build.build()
+    from paper_2510_11370_b200 import r3 as mod
+    return mod
+
+
+def call(r3, tensors=None, grad_scale=None, scalars=None, n=None, **kw):
+    cfg = dict(param_dtype=0, grad_dtype=0, master=0, state_bits=32, step=1, lr=0.1, beta1=0.9,
+               beta2=0.99, eps=1e-8)
+    cfg.update(kw)
+    if tensors is None:
+        tensors = [{}]
+    rows = []
+    for i, t in enumerate(tensors):
+        row = dict(param=(1 + 8 * i) << 20, master=None, grad=(2 + 8 * i) << 20, exp_avg=(3 + 8 * i) << 20,
+                   exp_avg_sq=(4 + 8 * i) << 20, exp_avg_scale=None, exp_avg_sq_scale=None, n=100,
+                   weight_decay=0.0)
+        row.update(t)
+        rows.append(r3.AdamWTensor(**row))
+    table = (r3.AdamWTensor * max(1, len(rows)))(*rows)
+    return r3.lib.r3_adamw_step(ctypes.byref(r3.AdamWConfig(**cfg)), table, len(rows) if n is None else n,
+                                grad_scale, scalars, None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(param_dtype=2), dict(grad_dtype=-1), dict(state_bits=16), dict(master=1), dict(step=0),
+    dict(lr=-1.0), dict(lr=float("nan")), dict(lr=float("inf")), dict(beta1=1.0), dict(beta1=-0.1),
+    dict(beta2=1.0), dict(beta2=float("nan")), dict(eps=0.0), dict(eps=-1e-8), dict(eps=float("inf")),
+    dict(n=-1), dict(state_bits=8),                                       # no scales
+    dict(param_dtype=1, master=1),                                        # no master buffer
+    dict(tensors=[dict(master=9 << 20)]),                                 # a master that is not used
+    dict(tensors=[dict(n=-5)]), dict(tensors=[dict(n=(1 << 40) + 1)]), dict(tensors=[dict(param=None)]),
+    dict(tensors=[dict(grad=None)]), dict(tensors=[dict(exp_avg=None)]), dict(tensors=[dict(exp_avg_sq=None)]),
+    dict(tensors=[dict(param=(1 << 20) + 8)]), dict(tensors=[dict(grad=(1 << 20) + 4)]),
+    dict(tensors=[dict(weight_decay=-0.1)]), dict(tensors=[dict(weight_decay=float("nan"))]),
+    dict(tensors=[{}, {}, dict(param=1 << 20)]),                          # the same tensor twice
+    dict(tensors=[{}, dict(param=(1 << 20) + 384)]),                      # overlapping tensors
+    dict(grad_scale=ctypes.c_void_p(4097)), dict(scalars=ctypes.c_void_p(4098)),
+])
+def test_refused(r3, kw):
+    assert call(r3, **kw) == r3.R3_ERR_INVALID_ARG
+
+
+def test_null_and_nothing_to_do(r3):
+    assert r3.lib.r3_adamw_step(None, None, 0, None, None, None) == r3.R3_ERR_INVALID_ARG
+    assert call(r3, tensors=[]) == r3.R3_OK
+    assert call(r3, tensors=[dict(n=0, param=None, grad=None)] * 3) == r3.R3_OK
+
+
+def test_struct_layouts(r3):
+    assert ctypes.sizeof(r3.AdamWTensor) == 72 and ctypes.sizeof(r3.AdamWConfig) == 56
+    assert ctypes.sizeof(r3.Norm) == 32 and ctypes.sizeof(r3.Logits) == 32
+
+
+def test_host_tensors_are_refused(r3):
+    with pytest.raises(ValueError):
+        r3.AdamW([torch.zeros(8)], [torch.zeros(8)])

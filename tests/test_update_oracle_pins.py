@@ -120,3 +120,41 @@ def test_norm_gradient_in_front_of_the_first_block():
     def loss():
         return float((b * U.norm_residual(x, None, w_pre=w, eps=0.1)[1]).sum())
     assert np.abs(g["dx"] - fd(loss, x)).max() < 1e-8 and np.abs(g["dw_pre"] - fd(loss, w)).max() < 1e-8
+
+
+# ---- AdamW ----------------------------------------------------------------------------------------
+def test_adamw_closed_forms():
+    # first step from zero states: m-hat = g, v-hat = g^2, so the step is lr sign(g) (eps aside)
+    w, m, v = U.adamw(np.array([1.0, 2.0]), np.array([3.0, -4.0]), 0.0, 0.0, 1, 0.1, (0.9, 0.99), 0.0, 0.0)
+    assert np.allclose(w, [0.9, 2.1], rtol=0, atol=1e-14)
+    assert np.allclose(m, [0.3, -0.4]) and np.allclose(v, [0.09, 0.16])
+    # a zero gradient leaves the decay alone
+    w, _, _ = U.adamw(np.array([1.0]), np.array([0.0]), 0.0, 0.0, 1, 0.1, (0.9, 0.99), 1e-8, 0.5)
+    assert abs(w[0] - 0.95) < 1e-15
+
+
+def test_adamw_agrees_with_torch():
+    import torch
+    g = torch.Generator().manual_seed(0)
+    p = torch.randn(50, generator=g, dtype=torch.float64, requires_grad=True)
+    opt = torch.optim.AdamW([p], lr=0.01, betas=(0.8, 0.9), eps=1e-6, weight_decay=0.3)
+    w, m, v = p.detach().numpy().copy(), 0.0, 0.0
+    for step in range(1, 6):
+        p.grad = torch.randn(50, generator=g, dtype=torch.float64)
+        w, m, v = U.adamw(w, p.grad.numpy(), m, v, step, 0.01, (0.8, 0.9), 1e-6, 0.3)
+        opt.step()
+        assert np.abs(w - p.detach().numpy()).max() < 1e-14
+
+
+def test_e4m3_values_and_scales():
+    import torch
+    vals = U.e4m3_values()
+    codes = torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    assert np.array_equal(vals, codes.double().numpy()) and vals[-1] == 448.0 and vals[1] == U.E4M3_MIN
+    rng = np.random.default_rng(1)
+    q = np.concatenate([rng.uniform(-448, 448, 5000), vals, -vals, (vals[1:] + vals[:-1]) / 2,
+                        2.0 ** rng.uniform(-14, 8, 5000)]).astype(np.float32)
+    want = torch.from_numpy(q).to(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(U.nearest_e4m3(q), want)
+    for top, scale in ((448.0, 1.0), (448.0001, 2.0), (224.0, 0.5), (1.0, 2.0 ** -8), (0.0, 2.0 ** -126)):
+        assert U.block_scale(np.array([[0.0, -top]]))[0] == scale

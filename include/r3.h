@@ -590,7 +590,7 @@ r3_status r3_adamw_step(const r3_adamw* config, const r3_adamw_tensor* tensors, 
 
 /* A batch of logits: T rows of V values, row t at logits + t * ld elements (ld >= V, so a padded or
  * sliced vocabulary is taken as it lies), dtype R3_F32 or R3_BF16.  token_ids are int32 or int64
- * (id_bytes 4 or 8).  temperature > 0 divides the logits. */
+ * (id_bytes 4 or 8).  temperature (1e-6 to 1e30) divides the logits. */
 typedef struct {
     int32_t T, V;
     int64_t ld;

@@ -21,7 +21,8 @@
 
 #include <algorithm>
 #include <cmath>
-#include <new>
+#include <cstring>
+#include <type_traits>
 #include <utility>
 #include <vector>
 
@@ -33,8 +34,8 @@ namespace r3 {
 constexpr int kAdamBlock = 256;                     // elements per scale
 constexpr int kAdamThreads = 256;
 constexpr int kAdamWarps = kAdamThreads / 32;
-constexpr int kAdamPerWarp = 4;                     // blocks per warp and chunk
-constexpr int kAdamChunk = kAdamBlock * kAdamWarps * kAdamPerWarp;
+constexpr int kAdamCtas = 4;                        // resident per SM at 64 registers a thread
+constexpr int kAdamMaxPerWarp = 16;                 // blocks per warp and chunk
 constexpr int kAdamSmall = 24, kAdamLarge = 400;    // tensors per launch
 
 struct AdamTensor {
@@ -54,85 +55,94 @@ struct AdamScalars {
     const float* grad_scale;
     const float* dynamic;                           // {lr, bias1, bias2} on the device, or null
     unsigned chunks;
-    int tensors;
+    int tensors, per_warp;
 };
 template <int CAP> struct AdamTable {
     AdamScalars s;
     AdamTensor t[CAP];
 };
 
-// Four consecutive elements as float32.
-template <typename T> __device__ __forceinline__ float4 load4(const T* p);
-template <> __device__ __forceinline__ float4 load4<float>(const float* p) {
-    return *reinterpret_cast<const float4*>(p);
-}
-template <> __device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16* p) {
-    const uint2 u = *reinterpret_cast<const uint2*>(p);
-    const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.x));
-    const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.y));
-    return make_float4(a.x, a.y, b.x, b.y);
-}
-__device__ __forceinline__ void store4(float* p, const float* f) {
-    *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
-}
-__device__ __forceinline__ void store4(__nv_bfloat16* p, const float* f) {
-    __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
-    uint2 u;
-    u.x = *reinterpret_cast<uint32_t*>(&a);
-    u.y = *reinterpret_cast<uint32_t*>(&b);
-    *reinterpret_cast<uint2*>(p) = u;
-}
-// Elements at, .. at + 3 of an array of n; 0 behind its end.
-template <typename T>
-__device__ __forceinline__ void take4(const T* p, long long at, long long n, bool full, float* f) {
-    if (full) {
-        const float4 v = load4<T>(p + at);
+// Four consecutive elements as they lie, and as float32.
+template <typename T> struct Four;
+template <> struct Four<float> {
+    float4 v;
+    __device__ __forceinline__ void unpack(float* f) const {
         f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
-    } else {
+    }
+    __device__ __forceinline__ void pack(const float* f) { v = make_float4(f[0], f[1], f[2], f[3]); }
+};
+template <> struct Four<__nv_bfloat16> {
+    uint2 v;
+    __device__ __forceinline__ void unpack(float* f) const {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+        const float2 a = __bfloat1622float2(h[0]), b = __bfloat1622float2(h[1]);
+        f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
+    }
+    __device__ __forceinline__ void pack(const float* f) {
+        __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
+        h[0] = __floats2bfloat162_rn(f[0], f[1]);
+        h[1] = __floats2bfloat162_rn(f[2], f[3]);
+    }
+};
+template <> struct Four<uint8_t> {                  // e4m3 codes
+    uint32_t v;
+    __device__ __forceinline__ void unpack(float* f) const {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = at + i < n ? to_f32(p[at + i]) : 0.f;
+        for (int i = 0; i < 2; ++i) {
+            const __half2_raw h =
+                __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(v >> (16 * i)), __NV_E4M3);
+            const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&h));
+            f[2 * i] = t.x;
+            f[2 * i + 1] = t.y;
+        }
+    }
+    __device__ __forceinline__ void pack(const float* f) {
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[0], f[1]), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[2], f[3]), __NV_SATFINITE, __NV_E4M3);
+        v = lo | (hi << 16);
+    }
+};
+// A lane's eight elements of a block: 4 l .. and 128 + 4 l ..; `left` elements of the tensor follow
+// from the block's first on (only looked at where FULL is false; what lies behind reads as 0 and is
+// not written).
+template <bool FULL, typename T>
+__device__ __forceinline__ void take(const T* p, int lane, int left, Four<T> (&f)[2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int at = 128 * h + 4 * lane;
+        if (FULL) {
+            f[h] = *reinterpret_cast<const Four<T>*>(p + at);
+        } else {
+            T e[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (at + i < left) e[i] = p[at + i];
+                else memset(&e[i], 0, sizeof(T));
+            }
+            memcpy(&f[h], e, sizeof(e));
+        }
     }
 }
-template <typename T>
-__device__ __forceinline__ void put4(T* p, long long at, long long n, bool full, const float* f) {
-    if (full) {
-        store4(p + at, f);
-    } else {
+template <bool FULL, typename T>
+__device__ __forceinline__ void put(T* p, int lane, int left, const Four<T> (&f)[2]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (at + i < n) p[at + i] = from_f32<T>(f[i]);
+    for (int h = 0; h < 2; ++h) {
+        const int at = 128 * h + 4 * lane;
+        if (FULL) {
+            *reinterpret_cast<Four<T>*>(p + at) = f[h];
+        } else {
+            T e[4];
+            memcpy(e, &f[h], sizeof(e));
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (at + i < left) p[at + i] = e[i];
+        }
     }
 }
-__device__ __forceinline__ void unpack_codes(uint32_t c, float scale, float* f) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(c >> (16 * i)), __NV_E4M3);
-        const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&h));
-        f[2 * i] = t.x * scale;                     // a power of two: exact
-        f[2 * i + 1] = t.y * scale;
-    }
-}
-__device__ __forceinline__ uint32_t pack_codes(const float* f, float inv) {
-    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[0] * inv, f[1] * inv), __NV_SATFINITE, __NV_E4M3);
-    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[2] * inv, f[3] * inv), __NV_SATFINITE, __NV_E4M3);
-    return lo | (hi << 16);
-}
-__device__ __forceinline__ uint32_t take_codes(const uint8_t* p, long long at, long long n, bool full) {
-    if (full) return *reinterpret_cast<const uint32_t*>(p + at);
-    uint32_t c = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (at + i < n) c |= (uint32_t)p[at + i] << (8 * i);
-    return c;
-}
-__device__ __forceinline__ void put_codes(uint8_t* p, long long at, long long n, bool full, uint32_t c) {
-    if (full) {
-        *reinterpret_cast<uint32_t*>(p + at) = c;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (at + i < n) p[at + i] = (uint8_t)(c >> (8 * i));
-    }
+__device__ __forceinline__ float max_abs(float a, float b) {      // a NaN stays one
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    return r;
 }
 // Biased exponent of the block's scale from the bits of its largest magnitude f 2^e, f in [1, 2):
 // 448 = 1.75 2^8, so e - 8, and one more where f > 1.75 (the addition carries then); at least 1.
@@ -143,11 +153,11 @@ __device__ __forceinline__ uint32_t scale_exponent(uint32_t bits) {
 // The eight codes of a lane and the scale of its block.  ROOT: values are >= 0 and none above zero
 // becomes code 0.
 template <bool ROOT>
-__device__ __forceinline__ float quantise(const float (&f)[8], uint32_t (&codes)[2]) {
-    uint32_t top = 0;
+__device__ __forceinline__ float quantise(const float (&f)[8], Four<uint8_t> (&codes)[2]) {
+    float big = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
-    top = __reduce_max_sync(0xffffffffu, top);
+    for (int i = 0; i < 8; ++i) big = max_abs(big, f[i]);
+    uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(big));
     const bool clean = top < 0x7f800000u;
     if (!clean) {                                   // the scale is that of the finite elements
         top = 0;
@@ -160,32 +170,136 @@ __device__ __forceinline__ float quantise(const float (&f)[8], uint32_t (&codes)
     }
     const uint32_t e = scale_exponent(top);
     const float inv = __uint_as_float((254u - e) << 23);
+    float least = f[0];
+    if (ROOT) {
+#pragma unroll
+        for (int i = 1; i < 8; ++i) least = fminf(least, f[i]);
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        codes[h] = pack_codes(f + 4 * h, inv);
-        if (ROOT) {
+        float q[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (f[4 * h + i] > 0.f && (codes[h] >> (8 * i) & 0xffu) == 0u) codes[h] |= 1u << (8 * i);
+        for (int i = 0; i < 4; ++i) q[i] = f[4 * h + i] * inv;
+        codes[h].pack(q);
+        if (ROOT) {
+            // 1 in every byte that is 0 (no code here has its top bit set, so nothing carries)
+            const uint32_t zeros = (((codes[h].v + 0x7f7f7f7fu) & 0x80808080u) ^ 0x80808080u) >> 7;
+            if (least > 0.f) {
+                codes[h].v |= zeros;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (f[4 * h + i] > 0.f) codes[h].v |= zeros & (0xffu << (8 * i));
+            }
         }
         if (!clean) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)             // 0x7f: NaN
                 if ((__float_as_uint(f[4 * h + i]) & 0x7f800000u) == 0x7f800000u)
-                    codes[h] |= 0x7fu << (8 * i);
+                    codes[h].v |= 0x7fu << (8 * i);
         }
     }
     return __uint_as_float(e << 23);
 }
 
+struct AdamRates {                                  // what the whole launch shares
+    float beta1, one_beta1, beta2, one_beta2, eps, bias2, step, keep, gs;
+};
+
+// One block's values on their way: loaded a block ahead where the states are codes (the arithmetic
+// around the codes is long enough to leave the memory idle otherwise; with 32-bit states the
+// occupancy does as well, and the registers are better spent on it).
+template <typename P, typename G, bool MASTER, bool BITS8> struct AdamBlock {
+    typedef typename std::conditional<MASTER, float, P>::type Wt;
+    typedef typename std::conditional<BITS8, uint8_t, float>::type St;
+    Four<Wt> w[2];
+    Four<G> g[2];
+    Four<St> m[2], v[2];
+    float ms, vs;
+
+    template <bool FULL>
+    __device__ __forceinline__ void load(const AdamTensor& t, long long block, int lane, int left) {
+        const long long at = block * kAdamBlock;
+        take<FULL>((MASTER ? reinterpret_cast<const Wt*>(t.master) : static_cast<const Wt*>(t.param)) + at,
+                   lane, left, w);
+        take<FULL>(static_cast<const G*>(t.grad) + at, lane, left, g);
+        take<FULL>(static_cast<const St*>(t.m) + at, lane, left, m);
+        take<FULL>(static_cast<const St*>(t.v) + at, lane, left, v);
+        if (BITS8) {
+            ms = t.m_scale[block];
+            vs = t.v_scale[block];
+        }
+    }
+    template <bool FULL>
+    __device__ __forceinline__ void update(const AdamTensor& t, long long block, int lane, int left,
+                                           const AdamRates& a) {
+        const long long at = block * kAdamBlock;
+        float fw[8], fg[8], fm[8], fv[8], root[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            w[h].unpack(fw + 4 * h);
+            g[h].unpack(fg + 4 * h);
+            m[h].unpack(fm + 4 * h);
+            v[h].unpack(fv + 4 * h);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float gi = __fmul_rn(fg[i], a.gs);
+            float m0 = fm[i], v0 = fv[i];
+            if (BITS8) {
+                m0 *= ms;                           // powers of two: exact
+                v0 *= vs;
+                v0 = __fmul_rn(v0, v0);
+            }
+            fm[i] = __fadd_rn(__fmul_rn(a.beta1, m0), __fmul_rn(a.one_beta1, gi));
+            fv[i] = __fadd_rn(__fmul_rn(a.beta2, v0), __fmul_rn(a.one_beta2, __fmul_rn(gi, gi)));
+            root[i] = __fsqrt_rn(fv[i]);
+            // a quotient a few units of 2^-24 off moves the weight by far less than its rounding
+            float inv;
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(fmaf(root[i], a.bias2, a.eps)));
+            fw[i] = fmaf(-a.step, fm[i] * inv, fw[i] * a.keep);
+        }
+        if constexpr (BITS8) {
+            ms = quantise<false>(fm, m);
+            vs = quantise<true>(root, v);
+            if (lane == 0) {
+                t.m_scale[block] = ms;
+                t.v_scale[block] = vs;
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                m[h].pack(fm + 4 * h);
+                v[h].pack(fv + 4 * h);
+            }
+        }
+        put<FULL>(static_cast<St*>(t.m) + at, lane, left, m);
+        put<FULL>(static_cast<St*>(t.v) + at, lane, left, v);
+        Four<P> p[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) p[h].pack(fw + 4 * h);
+        put<FULL>(static_cast<P*>(t.param) + at, lane, left, p);
+        if constexpr (MASTER) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) w[h].pack(fw + 4 * h);
+            put<FULL>(t.master + at, lane, left, w);
+        }
+    }
+};
+
 template <typename P, typename G, bool MASTER, bool BITS8, int CAP>
 __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamTable<CAP> a) {
-    const float gs = a.s.grad_scale ? *a.s.grad_scale : 1.f;
-    if (!(fabsf(gs) <= 3.402823466e38f)) return;    // NaN or infinite: the step is skipped
+    AdamRates r;
+    r.gs = a.s.grad_scale ? *a.s.grad_scale : 1.f;
+    if (!(fabsf(r.gs) <= 3.402823466e38f)) return;  // NaN or infinite: the step is skipped
     const float lr = a.s.dynamic ? a.s.dynamic[0] : a.s.lr;
-    const float bias1 = a.s.dynamic ? a.s.dynamic[1] : a.s.bias1;
-    const float bias2 = a.s.dynamic ? a.s.dynamic[2] : a.s.bias2;
-    const float step = lr * bias1;
+    r.step = lr * (a.s.dynamic ? a.s.dynamic[1] : a.s.bias1);
+    r.bias2 = a.s.dynamic ? a.s.dynamic[2] : a.s.bias2;
+    r.beta1 = a.s.beta1;
+    r.one_beta1 = a.s.one_beta1;
+    r.beta2 = a.s.beta2;
+    r.one_beta2 = a.s.one_beta2;
+    r.eps = a.s.eps;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     for (unsigned chunk = blockIdx.x; chunk < a.s.chunks; chunk += gridDim.x) {
         int lo = 0, hi = a.s.tensors - 1;           // the last tensor that starts at or before it
@@ -194,66 +308,34 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
             if (a.t[mid].first <= chunk) lo = mid;
             else hi = mid - 1;
         }
-        const AdamTensor& t = a.t[lo];
-        const long long n = t.n;
-        const float keep = 1.f - lr * t.decay;
-        P* param = static_cast<P*>(t.param);
-        const G* grad = static_cast<const G*>(t.grad);
-        const long long block0 = (long long)(chunk - t.first) * (kAdamWarps * kAdamPerWarp) + warp;
-#pragma unroll 1
-        for (int k = 0; k < kAdamPerWarp; ++k) {
-            const long long block = block0 + k * kAdamWarps, at = block * kAdamBlock + 4 * lane;
-            if (block * kAdamBlock >= n) break;
-            const bool full = (block + 1) * kAdamBlock <= n;
-            float w[8], g[8], m[8], v[8];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const long long i = at + 128 * h;
-                if (MASTER) take4<float>(t.master, i, n, full, w + 4 * h);
-                else take4<P>(param, i, n, full, w + 4 * h);
-                take4<G>(grad, i, n, full, g + 4 * h);
-                if (BITS8) {
-                    unpack_codes(take_codes(static_cast<const uint8_t*>(t.m), i, n, full),
-                                 t.m_scale[block], m + 4 * h);
-                    unpack_codes(take_codes(static_cast<const uint8_t*>(t.v), i, n, full),
-                                 t.v_scale[block], v + 4 * h);
-                } else {
-                    take4<float>(static_cast<const float*>(t.m), i, n, full, m + 4 * h);
-                    take4<float>(static_cast<const float*>(t.v), i, n, full, v + 4 * h);
-                }
+        const AdamTensor t = a.t[lo];
+        r.keep = 1.f - lr * t.decay;
+        // the warps of a CTA take the chunk's blocks in turn
+        long long block = (long long)(chunk - t.first) * (kAdamWarps * a.s.per_warp) + warp;
+        const long long whole = t.n / kAdamBlock;   // blocks without a ragged end
+        const long long end = min(whole, block + (long long)kAdamWarps * a.s.per_warp);
+        AdamBlock<P, G, MASTER, BITS8> b;
+        if (BITS8) {
+            if (block < end) b.template load<true>(t, block, lane, kAdamBlock);
+            while (block < end) {
+                AdamBlock<P, G, MASTER, BITS8> now = b;
+                const long long next = block + kAdamWarps;
+                if (next < end) b.template load<true>(t, next, lane, kAdamBlock);
+                now.template update<true>(t, block, lane, kAdamBlock, r);
+                block = next;
             }
-            float root[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float gi = __fmul_rn(g[i], gs);
-                const float v0 = BITS8 ? __fmul_rn(v[i], v[i]) : v[i];
-                m[i] = __fadd_rn(__fmul_rn(a.s.beta1, m[i]), __fmul_rn(a.s.one_beta1, gi));
-                v[i] = __fadd_rn(__fmul_rn(a.s.beta2, v0), __fmul_rn(a.s.one_beta2, __fmul_rn(gi, gi)));
-                root[i] = __fsqrt_rn(v[i]);
-                // a quotient a few units of 2^-24 off moves the weight by far less than its rounding
-                w[i] = fmaf(-step, __fdividef(m[i], fmaf(root[i], bias2, a.s.eps)), w[i] * keep);
+        } else {
+            for (; block < end; block += kAdamWarps) {
+                b.template load<true>(t, block, lane, kAdamBlock);
+                b.template update<true>(t, block, lane, kAdamBlock, r);
             }
-            uint32_t mc[2], vc[2];
-            if (BITS8) {
-                const float ms = quantise<false>(m, mc), vs = quantise<true>(root, vc);
-                if (lane == 0) {
-                    t.m_scale[block] = ms;
-                    t.v_scale[block] = vs;
-                }
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const long long i = at + 128 * h;
-                if (MASTER) put4(t.master, i, n, full, w + 4 * h);
-                put4(param, i, n, full, w + 4 * h);
-                if (BITS8) {
-                    put_codes(static_cast<uint8_t*>(t.m), i, n, full, mc[h]);
-                    put_codes(static_cast<uint8_t*>(t.v), i, n, full, vc[h]);
-                } else {
-                    put4(static_cast<float*>(t.m), i, n, full, m + 4 * h);
-                    put4(static_cast<float*>(t.v), i, n, full, v + 4 * h);
-                }
-            }
+        }
+        // the warp whose turn it is takes the ragged end
+        const long long past = (long long)(chunk - t.first + 1) * (kAdamWarps * a.s.per_warp);
+        if (block == whole && block < past && t.n > whole * kAdamBlock) {
+            const int left = (int)(t.n - whole * kAdamBlock);
+            b.template load<false>(t, block, lane, left);
+            b.template update<false>(t, block, lane, left, r);
         }
     }
 }
@@ -310,12 +392,22 @@ static r3_status launch_adamw(const AdamScalars& s, const r3_adamw_tensor* ts, i
     AdamTable<CAP> a;
     a.s = s;
     for (int done = 0; done < count;) {
+        // Blocks per warp and chunk: as many as leave the resident warps four chunks each, so that a
+        // long run of blocks hides its loads and a short list still spreads over the GPU.
+        long long blocks = 0;
+        for (int i = done, k = 0; i < count && k < CAP; ++i) {
+            blocks += (ts[i].n + kAdamBlock - 1) / kAdamBlock;
+            k += ts[i].n > 0;
+        }
+        const long long share = blocks / (4LL * kAdamWarps * kAdamCtas * sm_count());
+        const int per_warp = share < 1 ? 1 : share > kAdamMaxPerWarp ? kAdamMaxPerWarp : (int)share;
+        const long long chunk = (long long)kAdamBlock * kAdamWarps * per_warp;
         long long chunks = 0;
         int k = 0;
         for (; done < count && k < CAP; ++done) {
             const r3_adamw_tensor& t = ts[done];
             if (t.n == 0) continue;
-            const long long more = (t.n + kAdamChunk - 1) / kAdamChunk;
+            const long long more = (t.n + chunk - 1) / chunk;
             if (chunks + more > 0x7fffffffLL) {
                 if (k == 0) return R3_ERR_UNSUPPORTED;
                 break;
@@ -327,8 +419,9 @@ static r3_status launch_adamw(const AdamScalars& s, const r3_adamw_tensor* ts, i
         }
         if (k == 0) break;
         a.s.tensors = k;
+        a.s.per_warp = per_warp;
         a.s.chunks = (unsigned)chunks;
-        const long long most = 8LL * sm_count();
+        const long long most = (long long)kAdamCtas * sm_count();
         adamw_kernel<P, G, MASTER, BITS8, CAP>
             <<<(unsigned)(chunks < most ? chunks : most), kAdamThreads, 0, cs>>>(a);
         const r3_status st = launch_status();

@@ -19,7 +19,13 @@
 
 namespace r3 {
 
-constexpr int kMaxTop = 32;            // alternatives: one list entry per lane
+// CTAs of a given size per SM (64 to 85 registers a thread)
+__host__ __device__ constexpr int logprob_ctas(int threads) {
+    return threads == 512 ? 2 : threads == 128 ? 8 : 24;
+}
+constexpr int kMaxTop = 32;            // alternatives per row
+constexpr int kMaxSplit = 8;           // CTAs per row
+constexpr int kMaxCandidates = 256;
 constexpr float kMoveRef = 8.f;
 constexpr float kLowRef = -4194304.f;  // -2^22: the least reference
 constexpr float kPlainTop = 1048576.f; // |c top| up to which the reference is exact enough
@@ -110,41 +116,99 @@ template <typename T> __device__ __forceinline__ RowSplit split_row(const T* p, 
     return r;
 }
 
+// Two float32 values in one 64-bit register pair: the sums of a thread run in two lanes, with one
+// instruction for both.
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 pair(float lo, float hi) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void split(F2 v, float& lo, float& hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// A 16-byte piece of a row in the form the sums take: its largest value, and its values in pairs.
+// With FINITE every value is raised to at least -2^100 (c x stays finite: a term 0 times its exponent
+// is 0, not NaN); a NaN stays one.
+template <typename T> struct Piece;
+template <> struct Piece<__nv_bfloat16> {
+    static constexpr int PAIRS = 4;
+    uint4 v;
+    __device__ __forceinline__ void fill() { v = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
+    __device__ __forceinline__ float largest() const {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+        const float2 m = __bfloat1622float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
+        return fmaxf(m.x, m.y);
+    }
+    template <bool FINITE> __device__ __forceinline__ F2 get(int i) const {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+        const __nv_bfloat162 low = __floats2bfloat162_rn(-1.2676506e30f, -1.2676506e30f);   // -2^100
+        const float2 f = __bfloat1622float2(FINITE ? __hmax2_nan(h[i], low) : h[i]);
+        return pair(f.x, f.y);
+    }
+};
+template <> struct Piece<float> {
+    static constexpr int PAIRS = 2;
+    float4 v;
+    __device__ __forceinline__ void fill() {
+        v.x = v.y = v.z = v.w = -CUDART_INF_F;
+    }
+    __device__ __forceinline__ float largest() const { return fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)); }
+    template <bool FINITE> __device__ __forceinline__ F2 get(int i) const {
+        const float a = i ? v.z : v.x, b = i ? v.w : v.y;
+        return FINITE ? pair(max_nan(a, -1.2676506e30f), max_nan(b, -1.2676506e30f)) : pair(a, b);
+    }
+};
+
 struct RowSums {
-    float M, S, U, top;
+    float M, top;
+    F2 S, U;
 };
 // Moves the reference up to hold a value of c x = t.
 __device__ __forceinline__ void move_ref(RowSums& a, float t) {
     const float m = rintf(t), d = a.M - m, f = ex2(d);
-    a.U = f * (a.U + d * a.S);
-    a.S *= f;
+    const F2 f2 = pair(f, f), zero = pair(0.f, 0.f);
+    a.U = fma2(f2, fma2(pair(d, d), a.S, a.U), zero);
+    a.S = fma2(f2, a.S, zero);
     a.M = m;
 }
-template <bool ENT> __device__ __forceinline__ void add_term(RowSums& a, float u) {
-    if (ENT) {
-        u = max_nan(u, kLeastExp);
-        const float e = ex2(u);
-        a.S += e;
-        a.U = fmaf(e, u, a.U);
-    } else {
-        a.S += ex2(u);
-    }
+template <bool ENT> __device__ __forceinline__ void add_pair(RowSums& a, F2 u) {
+    float lo, hi;
+    split(u, lo, hi);
+    const F2 e = pair(ex2(lo), ex2(hi));
+    a.S = add2(a.S, e);
+    if (ENT) a.U = fma2(e, u, a.U);
 }
 
-// What the CTAs of one row hand to the first of them.
+// What the CTAs of one row leave in the first of them.
 struct SplitPart {
     float top, S, U;
-    Key list[kMaxTop];
 };
 
 // One row per cluster of `split` CTAs (1 for a large batch); NT threads each.
 template <typename T, bool ENT, bool TOP, int NT>
-__global__ void __launch_bounds__(NT, NT == 512 ? 3 : 8) logprob_kernel(const LogprobArgs a) {
+__global__ void __launch_bounds__(NT, logprob_ctas(NT))
+logprob_kernel(const LogprobArgs a) {
     constexpr int N = Vec16<T>::N, W = NT / 32, UNROLL = 4;
     __shared__ float s_red[W][4];
-    __shared__ Key s_list[TOP ? W : 1][32];
-    __shared__ int s_sel[kMaxTop], s_nsel;
-    __shared__ SplitPart s_part;
+    __shared__ SplitPart s_part[kMaxSplit];
+    __shared__ Key s_keys[TOP ? W : 1][32];                    // a thread's bound; fallback: lists
+    __shared__ Key s_cand[TOP ? kMaxCandidates : 1];
+    __shared__ Key s_gather[TOP ? kMaxSplit * kMaxTop : 1];    // the CTAs' lists, in the first one
+    __shared__ Key s_list[kMaxTop];
+    __shared__ unsigned short s_sel[TOP ? NT : 1];
+    __shared__ int s_nsel, s_ncand;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int row = blockIdx.x / a.split, rank = blockIdx.x - row * a.split;
 
@@ -164,49 +228,62 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 3 : 8) logprob_kernel(const Lo
         }
         return;
     }
+    // the CTAs of a cluster write to the first one's shared memory at the end: it has to be running
+    if (a.split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
 
     const T* p = static_cast<const T*>(a.logits) + (size_t)row * a.ld;
     const RowSplit rs = split_row(p, a.V);
-    const Vec16<T>* pv = reinterpret_cast<const Vec16<T>*>(p + rs.head);
+    const Piece<T>* pv = reinterpret_cast<const Piece<T>*>(p + rs.head);
     const int per_cta = (rs.vecs + a.split - 1) / a.split;
     const int v0 = min(rs.vecs, rank * per_cta), v1 = min(rs.vecs, v0 + per_cta);
     const float c = a.c;
+    const F2 c2 = pair(c, c);
 
-    RowSums r = {kLowRef, 0.f, 0.f, -CUDART_INF_F};
-    float best = -CUDART_INF_F;
-    int best_vec = v0 + tid < v1 ? v0 + tid : -1;
-
-    auto take = [&](const Vec16<T>& vec, int j) {
-        float x[N];
-        vec.unpack(x);
-        float m = x[0];
+    RowSums r = {kLowRef, -CUDART_INF_F, 0, 0};
+    int best_vec = v0 + tid < v1 ? v0 + tid : -1;       // the first piece that holds the top so far
+    // UNROLL pieces per thread and round; the next round's are on their way while these are summed.
+    // Pieces behind the end read as -inf: they change neither the top nor the sums.
+    Piece<T> b[UNROLL];
+    auto fetch = [&](int j) {
 #pragma unroll
-        for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
-        r.top = fmaxf(r.top, m);
-        if (TOP && m > best) {
-            best = m;
-            best_vec = j;
+        for (int u = 0; u < UNROLL; ++u) {
+            if (j + u * NT < v1) b[u] = pv[j + u * NT];
+            else b[u].fill();
         }
-        if (m * c - r.M > kMoveRef) move_ref(r, m * c);
-#pragma unroll
-        for (int i = 0; i < N; ++i) add_term<ENT>(r, fmaf(x[i], c, -r.M));
     };
+    fetch(v0 + tid);
+    for (int j = v0 + tid; j - tid < v1; j += UNROLL * NT) {
+        Piece<T> x[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) x[u] = b[u];
+        if (j - tid + UNROLL * NT < v1) fetch(j + UNROLL * NT);
+        float m = -CUDART_INF_F;
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const float q = x[u].largest();
+            if (TOP && q > fmaxf(r.top, m)) best_vec = j + u * NT;
+            m = fmaxf(m, q);
+        }
+        r.top = fmaxf(r.top, m);
+        if (m * c - r.M > kMoveRef) move_ref(r, m * c);
+        const F2 ref = pair(-r.M, -r.M);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            if (j - lane + u * NT >= v1) break;         // the whole warp is behind the end
+#pragma unroll
+            for (int i = 0; i < Piece<T>::PAIRS; ++i)
+                add_pair<ENT>(r, fma2(x[u].template get<ENT>(i), c2, ref));
+        }
+    }
+    // the single elements in front of the first and behind the last whole piece
+    const bool has_head = rank == 0, has_tail = rank == a.split - 1;
+    const int tail0 = rs.head + rs.vecs * N;
     auto take_one = [&](float x) {
         r.top = fmaxf(r.top, x);
         if (x * c - r.M > kMoveRef) move_ref(r, x * c);
-        add_term<ENT>(r, fmaf(x, c, -r.M));
+        add_pair<ENT>(r, pair(fmaf(max_nan(x, -1.2676506e30f), c, -r.M), -CUDART_MAX_NORMAL_F));
     };
-    int j = v0 + tid;
-    for (; j + (UNROLL - 1) * NT < v1; j += UNROLL * NT) {
-        Vec16<T> b[UNROLL];
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) b[u] = pv[j + u * NT];
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) take(b[u], j + u * NT);
-    }
-    for (; j < v1; j += NT) take(pv[j], j);
-    const bool has_head = rank == 0, has_tail = rank == a.split - 1;
-    const int tail0 = rs.head + rs.vecs * N;
+    const float vec_top = r.top;                        // of the whole pieces alone
     if (has_head && tid < rs.head) take_one(to_f32(p[tid]));
     if (has_tail && tid < rs.tail) take_one(to_f32(p[tail0 + tid]));
 
@@ -221,24 +298,40 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 3 : 8) logprob_kernel(const Lo
         s_red[warp][0] = m;
         s_red[warp][1] = top;
     }
-    if (tid == 0) s_nsel = 0;
+    const int first = rs.head + best_vec * N;           // first column of the thread's best piece
+    if (TOP) {
+        s_keys[warp][lane] = best_vec >= 0 ? make_key(vec_top, first + N - 1) : 0;
+        if (tid == 0) s_nsel = s_ncand = 0;
+        if (tid < kMaxTop) s_list[tid] = 0;
+    }
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < W; ++w) {
         m = fmaxf(m, s_red[w][0]);
         top = fmaxf(top, s_red[w][1]);
     }
+    float tS, tU;                                       // this thread's sums
+    {
+        float a0, a1;
+        split(r.S, a0, a1);
+        tS = a0 + a1;
+        split(r.U, a0, a1);
+        tU = a0 + a1;
+    }
     // A top whose c x is beyond 2^20 (masks of the type's lowest value in a whole row, say) leaves
     // the reference no room: the share is summed again with the differences to the known top.
     const bool again = fabsf(top * c) > kPlainTop && fabsf(top) < CUDART_INF_F;
     if (again) {
-        // a NaN would be dropped by neither form: x - top keeps it
-        r.S = 0.f;
-        r.U = 0.f;
-        auto term = [&](float x) { add_term<true>(r, (x - top) * c); };
+        tS = tU = 0.f;
+        auto term = [&](float x) {                      // x - top keeps a NaN
+            const float u = max_nan((x - top) * c, kLeastExp), e = ex2(u);
+            tS += e;
+            tU = fmaf(e, u, tU);
+        };
+        const Vec16<T>* px = reinterpret_cast<const Vec16<T>*>(pv);
         for (int q = v0 + tid; q < v1; q += NT) {
             float x[N];
-            pv[q].unpack(x);
+            px[q].unpack(x);
 #pragma unroll
             for (int i = 0; i < N; ++i) term(x[i]);
         }
@@ -246,19 +339,102 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 3 : 8) logprob_kernel(const Lo
         if (has_tail && tid < rs.tail) term(to_f32(p[tail0 + tid]));
     } else {
         const float d = r.M - m, f = ex2(d);
-        r.U = f * (r.U + d * r.S);
-        r.S *= f;
+        tU = f * (tU + d * tS);
+        tS *= f;
     }
 #pragma unroll
     for (int s = 16; s > 0; s >>= 1) {
-        r.S += __shfl_xor_sync(0xffffffffu, r.S, s);
-        r.U += __shfl_xor_sync(0xffffffffu, r.U, s);
+        tS += __shfl_xor_sync(0xffffffffu, tS, s);
+        tU += __shfl_xor_sync(0xffffffffu, tU, s);
     }
     if (lane == 0) {
-        s_red[warp][2] = r.S;
-        s_red[warp][3] = r.U;
+        s_red[warp][2] = tS;
+        s_red[warp][3] = tU;
     }
-    __syncthreads();
+
+    // ---- the largest keys of the CTA's share ---------------------------------------------------
+    // Every thread knows its largest value and the 16-byte piece where that stood first, so (value,
+    // last column of the piece) bounds its largest key from below.  The n-th largest of the 32
+    // maxima of such bounds over equal lanes is reached by n keys of the share, so none of the n
+    // largest lies under it; only threads whose piece reaches it (value, first column) hold keys
+    // above it, and only their pieces are read again, from L2.  What reaches the bound are a few
+    // more than n keys; each one's rank is the number of larger ones.
+    Key list = 0;
+    if (TOP) {
+        Key g = s_keys[0][lane];
+#pragma unroll
+        for (int w = 1; w < W; ++w) g = s_keys[w][lane] > g ? s_keys[w][lane] : g;
+        int larger = 0;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) larger += __shfl_sync(0xffffffffu, g, k) > g ? 1 : 0;
+        const unsigned nth = __ballot_sync(0xffffffffu, larger == a.n_top - 1);
+        // none: fewer than n threads have pieces, and everything is a candidate
+        const Key bound = nth ? __shfl_sync(0xffffffffu, g, __ffs(nth) - 1) : 0;
+        if (best_vec >= 0 && make_key(vec_top, first) >= bound) s_sel[atomicAdd(&s_nsel, 1)] = tid;
+        __syncthreads();
+        const Vec16<T>* px = reinterpret_cast<const Vec16<T>*>(pv);
+        const int per = (v1 - v0 + NT - 1) / NT, total = s_nsel * per;
+        auto offer = [&](float x, int col) {            // any order: ranks do not depend on it
+            const Key k = make_key(x, col);
+            if (k < bound) return;
+            const int at = atomicAdd(&s_ncand, 1);
+            if (at < kMaxCandidates) s_cand[at] = k;
+        };
+        for (int q = tid; q < total; q += NT) {
+            const int s = q / per, vec = v0 + s_sel[s] + (q - s * per) * NT;
+            if (vec >= v1) continue;
+            float x[N];
+            px[vec].unpack(x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) offer(x[i], rs.head + vec * N + i);
+        }
+        if (has_head && tid < rs.head) offer(to_f32(p[tid]), tid);
+        if (has_tail && tid < rs.tail) offer(to_f32(p[tail0 + tid]), tail0 + tid);
+        __syncthreads();
+        const int found = s_ncand;
+        if (found <= kMaxCandidates) {
+            for (int i = tid; i < found; i += NT) {
+                const Key k = s_cand[i];
+                int above = 0;
+                for (int q = 0; q < found; ++q) above += s_cand[q] > k ? 1 : 0;
+                if (above < kMaxTop) s_list[above] = k;
+            }
+        } else {
+            // many large values in the pieces of few threads: every warp keeps the 32 largest of the
+            // keys it meets, and the warps' lists are merged
+            for (int q0 = warp * 32; q0 < total; q0 += NT) {
+                const int q = q0 + lane, s = q / per;
+                const int vec = q < total ? v0 + s_sel[s] + (q - s * per) * NT : v1;
+                float x[N];
+                if (vec < v1) px[vec].unpack(x);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    Key k = vec < v1 ? make_key(x[i], rs.head + vec * N + i) : 0;
+                    if (k < bound) k = 0;
+                    if (__any_sync(0xffffffffu, k != 0)) list = warp_merge(list, warp_sort(k, lane), lane);
+                }
+            }
+            if (warp == 0) {
+                int col = -1;
+                if (has_head && lane < rs.head) col = lane;
+                if (has_tail && lane >= 16 && lane - 16 < rs.tail) col = tail0 + lane - 16;
+                const Key k = col >= 0 ? make_key(to_f32(p[col]), col) : 0;
+                list = warp_merge(list, warp_sort(k, lane), lane);
+            }
+            s_keys[warp][lane] = list;
+#pragma unroll
+            for (int half = W / 2; half > 0; half >>= 1) {
+                __syncthreads();
+                if (warp < half) {
+                    list = warp_merge(list, s_keys[warp + half][lane], lane);
+                    s_keys[warp][lane] = list;
+                }
+            }
+            if (warp == 0) s_list[lane] = list;
+        }
+    }
+    __syncthreads();                                    // s_red, s_list
+
     float S = 0.f, U = 0.f;
 #pragma unroll
     for (int w = 0; w < W; ++w) {                                        // fixed order
@@ -270,105 +446,57 @@ __global__ void __launch_bounds__(NT, NT == 512 ? 3 : 8) logprob_kernel(const Lo
         U = k * (U - ut * S);
         S *= k;
     }
-
-    // ---- the 32 largest keys of the CTA's share ----------------------------------------------
-    // Every thread knows its largest value and the 16-byte piece where that stood first.  The
-    // n-th largest of the pieces' lower bounds (value, last column) bounds the n-th largest key
-    // of the share from below, and only the threads whose piece reaches it (value, first column)
-    // can hold one of the n largest keys: at most n of them, since pieces do not overlap.  Their
-    // pieces are read again, from L2.
-    Key list = 0;
-    if (TOP) {
-        auto merge_warps = [&](Key k) {                 // warp 0 ends with the list of the CTA
-            s_list[warp][lane] = k;
-#pragma unroll
-            for (int half = W / 2; half > 0; half >>= 1) {
-                __syncthreads();
-                if (warp < half) {
-                    k = warp_merge(k, s_list[warp + half][lane], lane);
-                    s_list[warp][lane] = k;
-                }
-            }
-            __syncthreads();
-            return k;
-        };
-        const int first = rs.head + best_vec * N;
-        const Key low = best_vec >= 0 ? make_key(best, first + N - 1) : 0;
-        merge_warps(warp_sort(low, lane));
-        const Key bound = s_list[0][a.n_top - 1];
-        if (best_vec >= 0 && make_key(best, first) >= bound) {
-            const int s = atomicAdd(&s_nsel, 1);         // any order: what follows does not depend on it
-            if (s < kMaxTop) s_sel[s] = tid;
-        }
-        __syncthreads();
-        const int per = (v1 - v0 + NT - 1) / NT, total = min(s_nsel, kMaxTop) * per;
-        auto offer = [&](Key k) {
-            if (k < bound) k = 0;
-            if (__any_sync(0xffffffffu, k != 0)) list = warp_merge(list, warp_sort(k, lane), lane);
-        };
-        for (int q0 = warp * 32; q0 < total; q0 += NT) {
-            const int q = q0 + lane, s = q / per;
-            const int vec = q < total ? v0 + s_sel[s] + (q - s * per) * NT : v1;
-            float x[N];
-            if (vec < v1) pv[vec].unpack(x);
-#pragma unroll
-            for (int i = 0; i < N; ++i) offer(vec < v1 ? make_key(x[i], rs.head + vec * N + i) : 0);
-        }
-        if (warp == 0) {
-            int col = -1;
-            if (has_head && lane < rs.head) col = lane;
-            if (has_tail && lane >= 16 && lane - 16 < rs.tail) col = tail0 + lane - 16;
-            offer(col >= 0 ? make_key(to_f32(p[col]), col) : 0);
-        }
-        list = merge_warps(list);
-    }
+    if (TOP) list = s_list[lane];
 
     // ---- the CTAs of a row meet in the first of them ------------------------------------------
     if (a.split > 1) {
-        if (tid == 0) {
-            s_part.top = top;
-            s_part.S = S;
-            s_part.U = U;
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (warp == 0) {
+            if (lane < 3) {
+                const uint32_t at = tc::mapa_shared(tc::smem_u32(&s_part[rank]), 0) + 4 * lane;
+                const float v = lane == 0 ? top : lane == 1 ? S : U;
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
+            }
+            if (TOP) {
+                const uint32_t at = tc::mapa_shared(tc::smem_u32(&s_gather[TOP ? rank * kMaxTop + lane : 0]), 0);
+                asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at), "l"(list) : "memory");
+            }
         }
-        if (TOP && warp == 0) s_part.list[lane] = list;
         tc::cluster_sync_all();
-        if (rank == 0 && warp == 0) {
-            const uint32_t mine = tc::smem_u32(&s_part);
-            auto peer = [&](int q, size_t off) {
-                uint32_t v;
-                asm volatile("ld.shared::cluster.u32 %0, [%1];"
-                             : "=r"(v) : "r"(tc::mapa_shared(mine + (uint32_t)off, q)) : "memory");
-                return v;
-            };
-            float t[3] = {-CUDART_INF_F, 0.f, 0.f};
-            if (lane < a.split) {
-                t[0] = __uint_as_float(peer(lane, offsetof(SplitPart, top)));
-                t[1] = __uint_as_float(peer(lane, offsetof(SplitPart, S)));
-                t[2] = __uint_as_float(peer(lane, offsetof(SplitPart, U)));
+        if (rank != 0) return;                          // nobody reads this CTA's memory
+        if (TOP) {
+            const int found = a.split * kMaxTop;        // zeros where a share has fewer keys
+            for (int i = tid; i < found; i += NT) {
+                const Key k = s_gather[i];
+                int above = 0;
+                for (int q = 0; q < found; ++q) above += s_gather[q] > k ? 1 : 0;
+                if (k != 0 && above < kMaxTop) s_list[above] = k;
             }
-            top = t[0];
-#pragma unroll
-            for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-            // a share of -inf alone has S = 0 (or NaN, which stays)
-            const float d = t[0] > -CUDART_INF_F ? max_nan((t[0] - top) * c, -1e30f) : 0.f;
-            const float f = ex2(d);
-            U = f * (t[2] + d * t[1]);
-            S = f * t[1];
-#pragma unroll
-            for (int s = 16; s > 0; s >>= 1) {
-                S += __shfl_xor_sync(0xffffffffu, S, s);
-                U += __shfl_xor_sync(0xffffffffu, U, s);
-            }
-            if (TOP)
-                for (int q = 1; q < a.split; ++q) {
-                    const size_t at = offsetof(SplitPart, list) + lane * sizeof(Key);
-                    const Key k = (Key)peer(q, at) | ((Key)peer(q, at + 4) << 32);
-                    list = warp_merge(list, k, lane);
-                }
+            __syncthreads();
+            list = s_list[lane];
         }
-        tc::cluster_sync_all();                  // the peers' shared memory was read until here
+        if (warp != 0) return;
+        float t = -CUDART_INF_F, ts = 0.f, tu = 0.f;
+        if (lane < a.split) {
+            t = s_part[lane].top;
+            ts = s_part[lane].S;
+            tu = s_part[lane].U;
+        }
+        top = t;
+#pragma unroll
+        for (int s = 16; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+        // a share of -inf alone has S = 0 (or NaN, which stays)
+        const float d = t > -CUDART_INF_F ? max_nan((t - top) * c, -1e30f) : 0.f;
+        const float f = ex2(d);
+        U = f * (tu + d * ts);
+        S = f * ts;
+#pragma unroll
+        for (int s = 16; s > 0; s >>= 1) {
+            S += __shfl_xor_sync(0xffffffffu, S, s);
+            U += __shfl_xor_sync(0xffffffffu, U, s);
+        }
     }
-    if (rank != 0 || warp != 0) return;
+    if (warp != 0) return;
 
     const bool bad = !(S < CUDART_INF_F);                       // NaN or +inf among the logits
     const bool none = !bad && top == -CUDART_INF_F;             // every logit -inf
@@ -474,15 +602,56 @@ __global__ void __launch_bounds__(kBwdThreads) logprob_bwd_kernel(const LogprobB
                 o.pack(f);
                 dv[j] = o;
             }
-            if (chunk == 0) {
-                const int tail0 = rs.head + rs.vecs * N, t = threadIdx.x;
-                const int col = t < rs.head ? t : t >= 32 && t - 32 < rs.tail ? tail0 + t - 32 : -1;
-                if (col >= 0) dx[col] = from_f32<T>(zero ? 0.f : grad(to_f32(x[col]), col));
-            }
         } else {
-            const int end = min(a.V, (chunk + 1) * STEP * N);
-            for (int col = chunk * STEP * N + threadIdx.x; col < end; col += kBwdThreads)
-                dx[col] = from_f32<T>(zero ? 0.f : grad(to_f32(x[col]), col));
+            // Whole pieces of dx; each is made of two neighbouring pieces of x, shifted by the same
+            // number of bytes throughout the row.  The row's first and last piece are read element by
+            // element: their neighbours may lie outside the row.
+            const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(x + rs.head) & 15u);
+            const uint4* xv = reinterpret_cast<const uint4*>(
+                reinterpret_cast<const char*>(x + rs.head) - off);
+            Vec16<T>* dv = reinterpret_cast<Vec16<T>*>(dx + rs.head);
+#pragma unroll 1
+            for (int q = 0; q < kBwdVecs; ++q) {
+                const int j = chunk * STEP + threadIdx.x + q * kBwdThreads;
+                if (j >= rs.vecs) break;
+                const int col = rs.head + j * N;
+                float f[N];
+                if (zero) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) f[i] = 0.f;
+                } else {
+                    if (j == 0 || j == rs.vecs - 1) {
+#pragma unroll
+                        for (int i = 0; i < N; ++i) f[i] = to_f32(x[col + i]);
+                    } else {
+                        const uint4 lo = xv[j], hi = xv[j + 1];
+                        Vec16<T> v;
+                        uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+                        const uint32_t bits = 8u * (off & 3u);
+                        auto shift = [&](uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3, uint32_t w4) {
+                            w[0] = __funnelshift_r(w0, w1, bits);
+                            w[1] = __funnelshift_r(w1, w2, bits);
+                            w[2] = __funnelshift_r(w2, w3, bits);
+                            w[3] = __funnelshift_r(w3, w4, bits);
+                        };
+                        if (off < 4) shift(lo.x, lo.y, lo.z, lo.w, hi.x);
+                        else if (off < 8) shift(lo.y, lo.z, lo.w, hi.x, hi.y);
+                        else if (off < 12) shift(lo.z, lo.w, hi.x, hi.y, hi.z);
+                        else shift(lo.w, hi.x, hi.y, hi.z, hi.w);
+                        v.unpack(f);
+                    }
+#pragma unroll
+                    for (int i = 0; i < N; ++i) f[i] = grad(f[i], col + i);
+                }
+                Vec16<T> o;
+                o.pack(f);
+                dv[j] = o;
+            }
+        }
+        if (chunk == 0) {
+            const int tail0 = rs.head + rs.vecs * N, t = threadIdx.x;
+            const int col = t < rs.head ? t : t >= 32 && t - 32 < rs.tail ? tail0 + t - 32 : -1;
+            if (col >= 0) dx[col] = from_f32<T>(zero ? 0.f : grad(to_f32(x[col]), col));
         }
     }
 }
@@ -493,7 +662,7 @@ static r3_status check_logits(const r3_logits* s) {
     if (s->T < 0 || s->V <= 0 || s->V > (1 << 30) || s->ld < s->V) return R3_ERR_INVALID_ARG;
     if (s->dtype != R3_F32 && s->dtype != R3_BF16) return R3_ERR_INVALID_ARG;
     if (s->id_bytes != 4 && s->id_bytes != 8) return R3_ERR_INVALID_ARG;
-    if (!(s->temperature > 0.0) || !(s->temperature < 1e30) || !(s->temperature > 1e-30))
+    if (!(s->temperature >= 1e-6 && s->temperature <= 1e30))        // 2^100 log2(e) / it stays finite
         return R3_ERR_INVALID_ARG;
     return R3_OK;
 }
@@ -561,20 +730,22 @@ extern "C" r3_status r3_token_logprobs(const r3_logits* shape, const void* logit
     a.dev_status = dev_status;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     const long long row_bytes = (long long)shape->V * (long long)es;
-    // A row of up to 16 KB is two pieces or fewer for each of 512 threads: the reductions at its
-    // end would cost more than its loads, so it gets 128 threads.
-    const bool small = row_bytes <= 16384;
-    // Few rows: a cluster of CTAs shares one, as long as each of its threads has a piece or two
-    // and there are SMs for it.
+    // A row of up to 4 KB is taken by one warp, one of up to 16 KB by four: with more the reductions at
+    // its end would cost more than its loads.
+    const int threads = row_bytes <= 4096 ? 32 : row_bytes <= 16384 ? 128 : 512;
+    // Few rows: a cluster of CTAs shares one, as long as they all run at once and a thread has two
+    // pieces or more.
     a.split = 1;
-    const int threads = small ? 128 : 512;
-    while (a.split < 8 && (long long)a.T * a.split * 2 <= 2LL * r3::sm_count() &&
+    while (a.split < r3::kMaxSplit && a.T * a.split * 2 <= 2 * r3::sm_count() &&
            row_bytes / (a.split * 2) >= 2LL * 16 * threads)
         a.split *= 2;
-    if (shape->dtype == R3_BF16)
-        return small ? r3::dispatch_logprob<__nv_bfloat16, 128>(a, cs)
-                     : r3::dispatch_logprob<__nv_bfloat16, 512>(a, cs);
-    return small ? r3::dispatch_logprob<float, 128>(a, cs) : r3::dispatch_logprob<float, 512>(a, cs);
+    auto launch = [&](auto type) {
+        using T = decltype(type);
+        return threads == 32    ? r3::dispatch_logprob<T, 32>(a, cs)
+               : threads == 128 ? r3::dispatch_logprob<T, 128>(a, cs)
+                                : r3::dispatch_logprob<T, 512>(a, cs);
+    };
+    return shape->dtype == R3_BF16 ? launch(__nv_bfloat16()) : launch(float());
 }
 
 extern "C" r3_status r3_token_logprobs_bwd(const r3_logits* shape, const void* logits,

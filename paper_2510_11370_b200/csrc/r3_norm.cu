@@ -8,12 +8,15 @@
 //
 // Bound by HBM: forward 4 rows moved per token (x, y in; x_out, h out), backward 6 (x_out, y,
 // dx_out, dh in; dx, dy out); each element is read once and stays in registers through both row
-// reductions.  A row belongs to a group of threads, the whole CTA or (rows of up to kWarpPieces
-// pieces per lane) one warp, which then needs no barrier.  A thread owns P pieces of 16 bytes of
-// the row and walks over the rows with a stride, so that the sums of the weight gradients stay in
-// its registers.  What hides the memory latency is a ring in shared memory that is private to the
-// thread: it copies its own pieces of the rows to come there (cp.async), S rows ahead, so no
-// barrier or wait between threads belongs to the copies.
+// reductions.  A row belongs to a group of threads: one warp for up to 64 pieces of 16 bytes (no
+// barrier then), else a CTA.  A thread owns two pieces of the row (four in the longest rows) and
+// walks over the rows with a stride; one piece a thread left the kernels bound by instruction
+// issue, because the reductions and addresses of a row cost a thread the same whatever it holds.
+// The columns' weights and the sums of the weight gradients stay in its registers.  What hides the
+// memory latency is a ring in shared memory that is private to the thread: it copies its own pieces
+// of the rows to come there (cp.async), S rows ahead, so no barrier or wait between threads belongs
+// to the copies.  A warp's pieces are neighbours (piece p of lane l is piece 32 p + l of the warp's
+// share), so that all of a thread's addresses of a row are one base and constant offsets.
 #include <initializer_list>
 
 #include "r3_common.cuh"
@@ -22,9 +25,11 @@
 
 namespace r3 {
 
-constexpr int kNormMaxThreads = 512;
-constexpr int kWarpPieces = 2;         // P of the one-warp form
-constexpr int kWarpRows = 4;           // its warps (rows) per CTA
+constexpr int kNormMaxThreads = 512;   // per row
+constexpr int kNormBwdThreads = 384;   // backward: per SM, at up to 168 registers a thread
+constexpr int kNormFwdThreads = 640;   // forward: per SM, at up to 102
+constexpr int kNormPieces = 2;         // pieces per thread; twice as many where these do not reach
+constexpr int kWarpRows = 4;           // forward, one-warp form: rows per CTA
 
 struct NormArgs {
     const void* x;          // forward: x.  backward: x_out
@@ -37,7 +42,7 @@ struct NormArgs {
     void* out0;             // forward: x_out.  backward: dx
     void* out1;             // forward: h.      backward: dy
     void* dgate;            // backward: [T] float32 or [T, d] act (per-column sums go to part)
-    float* part;            // backward: [3][grid][d] partial sums of dw_pre, dw_post, dgate
+    float* part;            // backward: [2][grid][d] sums over a CTA's rows of dh x r and of g n
     int T, d, gate_kind;
     float eps, res, branch;
 };
@@ -51,9 +56,9 @@ template <int LEFT> __device__ __forceinline__ void copy_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
 }
 
-// Sum of NV values over the threads of a row's group; every thread gets the result.  For a CTA
-// one barrier per call: the caller alternates buffers, so that a buffer is only written again
-// behind the barrier of the call in between.
+// Sum of NV values over the threads of a row; every thread gets the result.  One barrier per call: the
+// caller alternates buffers, so that a buffer is only written again behind the barrier of the call in
+// between.
 template <int NV, bool WARP>
 __device__ __forceinline__ void row_sum(float (&v)[NV], float (*red)[4], int warps) {
 #pragma unroll
@@ -100,174 +105,269 @@ __device__ __forceinline__ void load_cols(const void* p, int col, float* f) {
         }
     }
 }
-template <typename T> __device__ __forceinline__ void store_piece(void* p, size_t at, const float* f) {
+template <typename T> __device__ __forceinline__ void store_piece(T* p, const float* f) {
     Vec16<T> o;
     o.pack(f);
-    *reinterpret_cast<Vec16<T>*>(static_cast<T*>(p) + at) = o;
+    *reinterpret_cast<Vec16<T>*>(p) = o;
 }
 
-template <typename T, typename W, int P, bool WARP, int S>
-__global__ void __launch_bounds__(kNormMaxThreads) norm_fwd_kernel(const NormArgs a) {
-    constexpr int N = Vec16<T>::N;
-    extern __shared__ uint4 ring_all[];            // [S][2 P][threads]
-    __shared__ float s_red[2][kNormMaxThreads / 32][4];
-    const int tid = WARP ? threadIdx.x & 31 : threadIdx.x, group = WARP ? 32 : blockDim.x;
-    const int warps = blockDim.x >> 5;
-    const int stride = WARP ? gridDim.x * warps : gridDim.x;
-    const int row0 = WARP ? blockIdx.x * warps + (threadIdx.x >> 5) : blockIdx.x;
-    const float inv_d = 1.f / (float)a.d;
-    uint4* ring = ring_all + threadIdx.x;
-    auto slot = [&](int stage, int q) { return ring + (size_t)(stage * 2 * P + q) * blockDim.x; };
-    auto fetch = [&](int row, int stage) {
-        if (row < a.T) {
+// The usual form has both norms, a gate per column or none, and (backward) a gradient from above; the
+// first has only the norm in front of a block.  They have kernels of their own, whose absent parts
+// cost no instructions; everything else is decided at run time.
+enum { kFormUsual = 0, kFormFirst = 1, kFormAny = 2 };
+
+// The weights of a thread's columns, kept for all its rows: in registers for two pieces of bf16 rows,
+// read again from L1 for each row otherwise (no room).  A column's factor is the vector's element
+// (1 without a vector) times `times` (likewise) times `scale`.
+template <typename W, int N, int P, bool KEEP> struct Weights {
+    float w[KEEP ? P : 1][KEEP ? N : 1];
+    const void *src, *times;
+    float scale;
+    __device__ __forceinline__ void read(int col, float* f) const {
+        float b[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = b[i] = 1.f;
+        if (src) load_cols<W, N>(src, col, f);
+        if (times) load_cols<W, N>(times, col, b);
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] *= b[i] * scale;
+    }
+    __device__ __forceinline__ void init(const void* s, const void* t, float k, int col, const bool (&in)[P]) {
+        src = s;
+        times = t;
+        scale = k;
+        if constexpr (KEEP) {
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const int col = (p * group + tid) * N;
-                if (col >= a.d) continue;
-                const size_t at = (size_t)row * a.d + col;
-                copy_ahead(slot(stage, 2 * p), static_cast<const T*>(a.x) + at);
-                if (a.y) copy_ahead(slot(stage, 2 * p + 1), static_cast<const T*>(a.y) + at);
+                if (in[p]) read(col + p * 32 * N, w[p]);
+            }
+        }
+    }
+    __device__ __forceinline__ void get(int p, int col, float* f) const {
+        if constexpr (KEEP) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) f[i] = w[p][i];
+        } else {
+            read(col + p * 32 * N, f);
+        }
+    }
+};
+
+// A thread's place: its first column (the further pieces follow at 32 N columns' distance), its rows,
+// and its ring: stage s, array q, lane at ((s Q + q) 32 + lane) of the warp's part.
+struct NormPlace {
+    int lane, warps, col, row, stride;
+    uint4* ring;
+};
+template <int N, int P, bool WARP, int Q, int S>
+__device__ __forceinline__ NormPlace norm_place(uint4* ring) {
+    NormPlace t;
+    const int warp = threadIdx.x >> 5;
+    t.lane = threadIdx.x & 31;
+    t.warps = blockDim.x >> 5;
+    t.col = ((WARP ? 0 : warp * 32 * P) + t.lane) * N;
+    t.row = blockIdx.x + (WARP ? gridDim.x * warp : 0);        // few rows: spread over the SMs
+    t.stride = gridDim.x * (WARP ? t.warps : 1);
+    t.ring = ring + warp * (S * Q * 32) + t.lane;
+    return t;
+}
+
+template <typename T, typename W, int P, bool WARP, bool WIDE, int S, int FORM>
+__global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kNormMaxThreads)
+norm_fwd_kernel(const NormArgs a) {
+    constexpr int N = Vec16<T>::N, Q = 2 * P, HOP = 32 * N;
+    constexpr bool KEEP = !WIDE && sizeof(T) == 2;
+    typedef const Vec16<T>* Ptr;
+    extern __shared__ uint4 ring_all[];
+    __shared__ float s_red[2][kNormMaxThreads / 32][4];   // a value per warp of the CTA
+    const bool has_y = FORM == kFormUsual || (FORM == kFormAny && a.y);
+    const bool has_post = FORM == kFormUsual || (FORM == kFormAny && a.w_post);
+    const bool has_pre = FORM != kFormAny || a.w_pre;
+    const bool token = FORM == kFormAny && a.gate_kind == R3_GATE_TOKEN;
+    const bool full = FORM == kFormAny && a.gate_kind == R3_GATE_FULL;
+    const NormPlace me = norm_place<N, P, WARP, Q, S>(ring_all);
+    const float inv_d = 1.f / (float)a.d, eps = a.eps, res = a.res;
+    const size_t start = (size_t)me.row * a.d + me.col, step = (size_t)me.stride * a.d;
+    bool in[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) in[p] = me.col + p * HOP < a.d;
+    // the ring's next row, and where it comes from
+    const T* fx = static_cast<const T*>(a.x) + start;
+    const T* fy = static_cast<const T*>(a.y) + start;
+    int frow = me.row;
+    auto fetch = [&](uint4* to) {
+        if (frow < a.T) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                if (!in[p]) continue;
+                copy_ahead(to + (2 * p) * 32, fx + p * HOP);
+                if (has_y) copy_ahead(to + (2 * p + 1) * 32, fy + p * HOP);
             }
         }
         copy_commit();                             // one group per row, empty ones behind the last
+        frow += me.stride;
+        fx += step;
+        fy += step;
     };
 #pragma unroll
-    for (int s = 0; s < S; ++s) fetch(row0 + s * stride, s);
+    for (int s = 0; s < S; ++s) fetch(me.ring + s * Q * 32);
+    Weights<W, N, P, KEEP> post, pre;
+    const void* channel = a.gate_kind == R3_GATE_CHANNEL ? a.gate : nullptr;
+    if (has_y) post.init(a.w_post, channel, a.branch, me.col, in);
+    if (has_pre) pre.init(a.w_pre, nullptr, 1.f, me.col, in);
+    T* x_out = static_cast<T*>(a.out0) + start;
+    T* h_out = static_cast<T*>(a.out1) + start;
     int stage = 0;
-    for (int row = row0; row < a.T; row += stride) {
-        const size_t base = (size_t)row * a.d;
+    for (int row = me.row; row < a.T; row += me.stride, x_out += step, h_out += step) {
+        uint4* slot = me.ring + stage * Q * 32;
         copy_wait<S - 1>();
-        float x[P][N], y[P][N];
+        float x[P][N];
+        Vec16<T> yv[P];
         float s[1] = {0.f};
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            const bool in = (p * group + tid) * N < a.d;
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[p][i] = y[p][i] = 0.f;
-            if (in) {
-                reinterpret_cast<const Vec16<T>*>(slot(stage, 2 * p))->unpack(x[p]);
-                if (a.y) reinterpret_cast<const Vec16<T>*>(slot(stage, 2 * p + 1))->unpack(y[p]);
-            }
+            for (int i = 0; i < N; ++i) x[p][i] = 0.f;
+            if (!in[p]) continue;
+            reinterpret_cast<Ptr>(slot + (2 * p) * 32)->unpack(x[p]);
+            if (!has_y) continue;
+            yv[p] = *reinterpret_cast<Ptr>(slot + (2 * p + 1) * 32);
+            float y[N];
+            yv[p].unpack(y);
 #pragma unroll
-            for (int i = 0; i < N; ++i) s[0] = fmaf(y[p][i], y[p][i], s[0]);
+            for (int i = 0; i < N; ++i) s[0] = fmaf(y[i], y[i], s[0]);
         }
-        fetch(row + S * stride, stage);
+        fetch(slot);
         stage = stage + 1 == S ? 0 : stage + 1;
         float r = 1.f;
-        if (a.w_post) {
-            row_sum<1, WARP>(s, s_red[0], warps);
-            r = rsqrtf(s[0] * inv_d + a.eps);
+        if (has_post) {
+            row_sum<1, WARP>(s, s_red[0], me.warps);
+            r = rsqrtf(s[0] * inv_d + eps);
         }
-        if (a.y) {
-            float k = a.branch;
-            if (a.gate_kind == R3_GATE_TOKEN) k *= static_cast<const float*>(a.gate)[row];
+        if (has_y) {
+            if (token) r *= static_cast<const float*>(a.gate)[row];
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const int col = (p * group + tid) * N;
-                if (col >= a.d) continue;
-                float g[N], w[N];
+                if (!in[p]) continue;
+                float w[N], y[N];
+                post.get(p, me.col, w);
+                yv[p].unpack(y);
+                if (full) {
+                    float g[N];
+                    load_cols<T, N>(static_cast<const T*>(a.gate) + (size_t)row * a.d, me.col + p * HOP, g);
 #pragma unroll
-                for (int i = 0; i < N; ++i) g[i] = w[i] = 1.f;
-                if (a.w_post) load_cols<W, N>(a.w_post, col, w);
-                if (a.gate_kind == R3_GATE_CHANNEL) load_cols<W, N>(a.gate, col, g);
-                if (a.gate_kind == R3_GATE_FULL)
-                    load_cols<T, N>(static_cast<const T*>(a.gate) + base, col, g);
+                    for (int i = 0; i < N; ++i) y[i] *= g[i];
+                }
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    x[p][i] = a.res * x[p][i] + k * (g[i] * (y[p][i] * r * w[i]));
-                store_piece<T>(a.out0, base + col, x[p]);
+                for (int i = 0; i < N; ++i) x[p][i] = fmaf(y[i] * r, w[i], res * x[p][i]);
+                store_piece<T>(x_out + p * HOP, x[p]);
             }
         }
-        if (a.w_pre) {
+        if (has_pre) {
             s[0] = 0.f;
 #pragma unroll
             for (int p = 0; p < P; ++p)
 #pragma unroll
                 for (int i = 0; i < N; ++i) s[0] = fmaf(x[p][i], x[p][i], s[0]);
-            row_sum<1, WARP>(s, s_red[1], warps);
-            r = rsqrtf(s[0] * inv_d + a.eps);
+            row_sum<1, WARP>(s, s_red[1], me.warps);
+            r = rsqrtf(s[0] * inv_d + eps);
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const int col = (p * group + tid) * N;
-                if (col >= a.d) continue;
+                if (!in[p]) continue;
                 float w[N];
-                load_cols<W, N>(a.w_pre, col, w);
+                pre.get(p, me.col, w);
 #pragma unroll
                 for (int i = 0; i < N; ++i) w[i] *= x[p][i] * r;
-                store_piece<T>(a.out1, base + col, w);
+                store_piece<T>(h_out + p * HOP, w);
             }
         }
         // with one reduction per row its buffer comes around without a barrier in between
-        if (!WARP && (!a.w_post || !a.w_pre)) __syncthreads();
+        if (!WARP && (!has_post || !has_pre)) __syncthreads();
     }
     copy_wait<0>();
 }
 
-// Backward.  With x = x_out, m = x r the pre-normalised row (r = rsqrt(mean(x^2) + eps)),
-// u = dh w_pre and c = mean(u m):
-//   g  = dx_out + r (u - m c);      dw_pre += dh m;      dx = residual_scale g
-// and with q = branch_scale g, t = q gate, n = y s (s = rsqrt(mean(y^2) + eps)), e = mean(t w_post n):
-//   dw_post += t n;    dgate = q n w_post (summed over what the gate is broadcast along);
-//   dy = s (t w_post - n e)
-// e and a token's dgate need g, so a row takes two reductions.
-template <typename T, typename W, int P, bool WARP, int S>
-__global__ void __launch_bounds__(kNormMaxThreads) norm_bwd_kernel(const NormArgs a) {
-    constexpr int N = Vec16<T>::N;
-    extern __shared__ uint4 ring_all[];            // [S][4 P][threads]
-    __shared__ float s_red[2][kNormMaxThreads / 32][4];
-    const int tid = WARP ? threadIdx.x & 31 : threadIdx.x, group = WARP ? 32 : blockDim.x;
-    const int warps = blockDim.x >> 5;
-    const int stride = WARP ? gridDim.x * warps : gridDim.x;
-    const int row0 = WARP ? blockIdx.x * warps + (threadIdx.x >> 5) : blockIdx.x;
-    const float inv_d = 1.f / (float)a.d;
-    uint4* ring = ring_all + threadIdx.x;
-    auto slot = [&](int stage, int q) { return ring + (size_t)(stage * 4 * P + q) * blockDim.x; };
-    auto fetch = [&](int row, int stage) {
-        if (row < a.T) {
+// Backward.  With x = x_out, r = rsqrt(mean(x^2) + eps), u = dh w_pre and c = mean(u x) r:
+//   g  = dx_out + r u - x r^2 c;      dw_pre += dh x r;      dx = residual_scale g
+// and with n = y s (s = rsqrt(mean(y^2) + eps)), v = branch_scale gate w_post g, e = mean(v n):
+//   dy = s (v - n e)
+// dw_post and the gate's gradient both come from g n: per column, where the gate is one factor per
+// column (or there is none), A = sum g n gives dw_post = branch_scale gate A and dgate =
+// branch_scale w_post A; a token's gate is taken out of v, so that its gradient is the sum that e
+// is formed from.  A row takes two reductions, of three values and of one.
+template <typename T, typename W, int P, bool WARP, bool WIDE, int S, int FORM>
+__global__ void __launch_bounds__(WIDE ? kNormMaxThreads : kNormBwdThreads)
+norm_bwd_kernel(const NormArgs a) {
+    constexpr int N = Vec16<T>::N, Q = 4 * P, HOP = 32 * N;
+    constexpr bool KEEP = !WIDE && sizeof(T) == 2;
+    typedef const Vec16<T>* Ptr;
+    extern __shared__ uint4 ring_all[];
+    __shared__ float s_red[2][kNormMaxThreads / 32][4];   // a value per warp of the CTA
+    const bool has_y = FORM == kFormUsual || (FORM == kFormAny && a.y);
+    const bool has_post = FORM == kFormUsual || (FORM == kFormAny && a.w_post);
+    const bool has_pre = FORM != kFormAny || a.w_pre;
+    const bool has_up = FORM == kFormUsual || a.dx_out;
+    const bool token = FORM == kFormAny && a.gate_kind == R3_GATE_TOKEN;
+    const bool full = FORM == kFormAny && a.gate_kind == R3_GATE_FULL;
+    const NormPlace me = norm_place<N, P, WARP, Q, S>(ring_all);
+    const float inv_d = 1.f / (float)a.d, eps = a.eps, res = has_y ? a.res : 1.f;
+    const size_t start = (size_t)me.row * a.d + me.col, step = (size_t)me.stride * a.d;
+    bool in[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) in[p] = me.col + p * HOP < a.d;
+    const T* fx = static_cast<const T*>(a.x) + start;
+    const T* fh = static_cast<const T*>(a.dh) + start;
+    const T* fg = static_cast<const T*>(a.dx_out) + start;
+    const T* fy = static_cast<const T*>(a.y) + start;
+    int frow = me.row;
+    auto fetch = [&](uint4* to) {
+        if (frow < a.T) {
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const int col = (p * group + tid) * N;
-                if (col >= a.d) continue;
-                const size_t at = (size_t)row * a.d + col;
-                if (a.w_pre) {
-                    copy_ahead(slot(stage, 4 * p), static_cast<const T*>(a.x) + at);
-                    copy_ahead(slot(stage, 4 * p + 1), static_cast<const T*>(a.dh) + at);
+                if (!in[p]) continue;
+                if (has_pre) {
+                    copy_ahead(to + (4 * p) * 32, fx + p * HOP);
+                    copy_ahead(to + (4 * p + 1) * 32, fh + p * HOP);
                 }
-                if (a.dx_out) copy_ahead(slot(stage, 4 * p + 2), static_cast<const T*>(a.dx_out) + at);
-                if (a.y) copy_ahead(slot(stage, 4 * p + 3), static_cast<const T*>(a.y) + at);
+                if (has_up) copy_ahead(to + (4 * p + 2) * 32, fg + p * HOP);
+                if (has_y) copy_ahead(to + (4 * p + 3) * 32, fy + p * HOP);
             }
         }
         copy_commit();
+        frow += me.stride;
+        fx += step;
+        fh += step;
+        fg += step;
+        fy += step;
     };
-    float acc_pre[P][N], acc_post[P][N], acc_gate[P][N];
+#pragma unroll
+    for (int s = 0; s < S; ++s) fetch(me.ring + s * Q * 32);
+    const void* channel = a.gate_kind == R3_GATE_CHANNEL ? a.gate : nullptr;
+    Weights<W, N, P, KEEP> post, pre;
+    if (has_y) post.init(a.w_post, channel, a.branch, me.col, in);
+    if (has_pre) pre.init(a.w_pre, nullptr, 1.f, me.col, in);
+    float acc_pre[P][N], acc_post[P][N];
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int i = 0; i < N; ++i) acc_pre[p][i] = acc_post[p][i] = acc_gate[p][i] = 0.f;
-#pragma unroll
-    for (int s = 0; s < S; ++s) fetch(row0 + s * stride, s);
+        for (int i = 0; i < N; ++i) acc_pre[p][i] = acc_post[p][i] = 0.f;
+    T* dx = static_cast<T*>(a.out0) + start;
+    T* dy = static_cast<T*>(a.out1) + start;
     int stage = 0;
-    for (int row = row0; row < a.T; row += stride) {
-        const size_t base = (size_t)row * a.d;
+    for (int row = me.row; row < a.T; row += me.stride, dx += step, dy += step) {
+        uint4* slot = me.ring + stage * Q * 32;
         copy_wait<S - 1>();
-        Vec16<T> xv[P], hv[P], yv[P];
-        float g[P][N];
+        Vec16<T> xv[P], hv[P], yv[P], gv[P];
         float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            const int col = (p * group + tid) * N;
-            float w[N], f[N];
-#pragma unroll
-            for (int i = 0; i < N; ++i) f[i] = w[i] = g[p][i] = 0.f;
-            xv[p].pack(f);
-            hv[p].pack(f);
-            yv[p].pack(f);
-            if (col >= a.d) continue;
-            if (a.w_pre) {
-                xv[p] = *reinterpret_cast<const Vec16<T>*>(slot(stage, 4 * p));
-                hv[p] = *reinterpret_cast<const Vec16<T>*>(slot(stage, 4 * p + 1));
-                load_cols<W, N>(a.w_pre, col, w);
-                float h[N];
+            if (!in[p]) continue;
+            float f[N];
+            if (has_pre) {
+                float h[N], w[N];
+                xv[p] = *reinterpret_cast<Ptr>(slot + (4 * p) * 32);
+                hv[p] = *reinterpret_cast<Ptr>(slot + (4 * p + 1) * 32);
+                pre.get(p, me.col, w);
                 xv[p].unpack(f);
                 hv[p].unpack(h);
 #pragma unroll
@@ -276,154 +376,179 @@ __global__ void __launch_bounds__(kNormMaxThreads) norm_bwd_kernel(const NormArg
                     s[1] = fmaf(h[i] * w[i], f[i], s[1]);
                 }
             }
-            if (a.dx_out) reinterpret_cast<const Vec16<T>*>(slot(stage, 4 * p + 2))->unpack(g[p]);
-            if (a.y) {
-                yv[p] = *reinterpret_cast<const Vec16<T>*>(slot(stage, 4 * p + 3));
+            if (has_up) gv[p] = *reinterpret_cast<Ptr>(slot + (4 * p + 2) * 32);
+            if (has_y) {
+                yv[p] = *reinterpret_cast<Ptr>(slot + (4 * p + 3) * 32);
                 yv[p].unpack(f);
 #pragma unroll
                 for (int i = 0; i < N; ++i) s[2] = fmaf(f[i], f[i], s[2]);
             }
         }
-        fetch(row + S * stride, stage);
+        fetch(slot);
         stage = stage + 1 == S ? 0 : stage + 1;
-        row_sum<3, WARP>(s, s_red[0], warps);
-        const float r = rsqrtf(s[0] * inv_d + a.eps);
-        const float c = s[1] * r * inv_d;                       // mean(u m)
-        const float sy = a.w_post ? rsqrtf(s[2] * inv_d + a.eps) : 1.f;
-        const float token =
-            a.gate_kind == R3_GATE_TOKEN ? static_cast<const float*>(a.gate)[row] : 1.f;
-        float z[2] = {0.f, 0.f};
+        if (has_pre || has_post) row_sum<3, WARP>(s, s_red[0], me.warps);
+        const float r = rsqrtf(s[0] * inv_d + eps);
+        const float rrc = s[1] * inv_d * r * r * r;             // r^2 c
+        const float sy = has_post ? rsqrtf(s[2] * inv_d + eps) : 1.f;
+        const float gate_t = token ? static_cast<const float*>(a.gate)[row] : 1.f;
+        float v[P][N], n[WIDE ? 1 : P][N], z[1] = {0.f};      // wide rows: n is formed again, no room
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            const int col = (p * group + tid) * N;
-            if (col >= a.d) continue;
-            float w[N], f[N];
-            if (a.w_pre) {
-                float h[N];
-                load_cols<W, N>(a.w_pre, col, w);
+            if (!in[p]) continue;
+            float f[N], g[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) g[i] = 0.f;
+            if (has_up) gv[p].unpack(g);
+            if (has_pre) {
+                float h[N], w[N];
+                pre.get(p, me.col, w);
                 xv[p].unpack(f);
                 hv[p].unpack(h);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const float m = f[i] * r;
-                    acc_pre[p][i] = fmaf(h[i], m, acc_pre[p][i]);
-                    g[p][i] += r * (h[i] * w[i] - m * c);
+                    acc_pre[p][i] = fmaf(h[i] * f[i], r, acc_pre[p][i]);
+                    g[i] = fmaf(h[i] * w[i], r, g[i]);
+                    g[i] = fmaf(f[i], -rrc, g[i]);
                 }
             }
-            const float res = a.y ? a.res : 1.f;
 #pragma unroll
-            for (int i = 0; i < N; ++i) f[i] = res * g[p][i];
-            store_piece<T>(a.out0, base + col, f);
-            if (!a.y) continue;
-            float gate[N];
+            for (int i = 0; i < N; ++i) f[i] = res * g[i];
+            store_piece<T>(dx + p * HOP, f);
+            if (!has_y) continue;
+            float w[N];
+            post.get(p, me.col, w);
+            float(&np)[N] = n[WIDE ? 0 : p];
+            yv[p].unpack(np);
+#pragma unroll
+            for (int i = 0; i < N; ++i) np[i] *= sy;
+            if (full) {
+                float gate[N], dg[N];
+                const size_t at = (size_t)row * a.d;
+                load_cols<T, N>(static_cast<const T*>(a.gate) + at, me.col + p * HOP, gate);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    dg[i] = g[i] * w[i] * np[i];
+                    g[i] *= gate[i];
+                }
+                store_piece<T>(static_cast<T*>(a.dgate) + at + me.col + p * HOP, dg);
+            }
+            if (token) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) acc_post[p][i] = fmaf(gate_t * g[i], np[i], acc_post[p][i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) acc_post[p][i] = fmaf(g[i], np[i], acc_post[p][i]);
+            }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                w[i] = 1.f;
-                gate[i] = token;
+                v[p][i] = g[i] * w[i];
+                z[0] = fmaf(v[p][i], np[i], z[0]);
             }
-            if (a.w_post) load_cols<W, N>(a.w_post, col, w);
-            if (a.gate_kind == R3_GATE_CHANNEL) load_cols<W, N>(a.gate, col, gate);
-            if (a.gate_kind == R3_GATE_FULL)
-                load_cols<T, N>(static_cast<const T*>(a.gate) + base, col, gate);
-            yv[p].unpack(f);
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float q = a.branch * g[p][i], n = f[i] * sy, t = q * gate[i];
-                f[i] = q * n * w[i];                            // dgate of this element
-                acc_post[p][i] = fmaf(t, n, acc_post[p][i]);
-                g[p][i] = t * w[i];
-                z[0] = fmaf(g[p][i], n, z[0]);
-                z[1] += f[i];
-            }
-            if (a.gate_kind == R3_GATE_CHANNEL) {
-#pragma unroll
-                for (int i = 0; i < N; ++i) acc_gate[p][i] += f[i];
-            }
-            if (a.gate_kind == R3_GATE_FULL) store_piece<T>(a.dgate, base + col, f);
         }
-        if (a.y) {
-            row_sum<2, WARP>(z, s_red[1], warps);
-            const float e = a.w_post ? z[0] * inv_d * sy : 0.f;
-            if (a.gate_kind == R3_GATE_TOKEN && tid == 0) static_cast<float*>(a.dgate)[row] = z[1];
+        if (has_y) {
+            if (has_post || token) row_sum<1, WARP>(z, s_red[1], me.warps);
+            const float k = gate_t * sy;
+            const float e = has_post ? -z[0] * inv_d : 0.f;
+            if (token && me.col == 0)
+                static_cast<float*>(a.dgate)[row] = z[0];
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const int col = (p * group + tid) * N;
-                if (col >= a.d) continue;
-                float f[N];
-                yv[p].unpack(f);
+                if (!in[p]) continue;
+                float(&np)[N] = n[WIDE ? 0 : p];
+                if (WIDE) {
+                    yv[p].unpack(np);
 #pragma unroll
-                for (int i = 0; i < N; ++i) f[i] = sy * (g[p][i] - f[i] * e);
-                store_piece<T>(a.out1, base + col, f);
+                    for (int i = 0; i < N; ++i) np[i] *= sy;
+                }
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[p][i] = k * fmaf(np[i], e, v[p][i]);
+                store_piece<T>(dy + p * HOP, v[p]);
             }
-        } else if (!WARP) {
-            __syncthreads();                                    // see the forward kernel
         }
+        // fewer than two reductions in a row: a buffer would come around without a barrier between
+        if (!WARP && FORM != kFormUsual) __syncthreads();
     }
     copy_wait<0>();
     if (!a.part) return;
-    // One row of partial sums per CTA.  In the one-warp form the warps add theirs up in order first.
+    // One row of partial sums per CTA.  In the one-warp form the warps' are added up in order first.
     const size_t plane = (size_t)gridDim.x * a.d;
-    float* mine = a.part + (size_t)blockIdx.x * a.d;
-    const bool wanted[3] = {a.w_pre != nullptr, a.w_post != nullptr, a.gate_kind == R3_GATE_CHANNEL};
-    float* sums = reinterpret_cast<float*>(ring_all);           // [warps][P N 32], the ring is idle
+    float* mine = a.part + (size_t)blockIdx.x * a.d + me.col;
+    float* sums = reinterpret_cast<float*>(ring_all);           // [P N][threads], the ring is idle
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
-        if (!wanted[k]) continue;
-        float(&acc)[P][N] = k == 0 ? acc_pre : k == 1 ? acc_post : acc_gate;
+    for (int k = 0; k < 2; ++k) {
+        if (!(k == 0 ? has_pre : has_post || channel != nullptr)) continue;
+        float(&acc)[P][N] = k == 0 ? acc_pre : acc_post;
         if (WARP) {
             __syncthreads();
 #pragma unroll
             for (int p = 0; p < P; ++p)
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    sums[((threadIdx.x >> 5) * P * N + p * N + i) * 32 + tid] = acc[p][i];
+                for (int i = 0; i < N; ++i) sums[(p * N + i) * blockDim.x + threadIdx.x] = acc[p][i];
             __syncthreads();
             if (threadIdx.x >= 32) continue;
-            for (int w = 1; w < warps; ++w)
+            for (int g = 1; g < me.warps; ++g)
 #pragma unroll
                 for (int p = 0; p < P; ++p)
 #pragma unroll
-                    for (int i = 0; i < N; ++i) acc[p][i] += sums[(w * P * N + p * N + i) * 32 + tid];
+                    for (int i = 0; i < N; ++i)
+                        acc[p][i] += sums[(p * N + i) * blockDim.x + 32 * g + threadIdx.x];
         }
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            const int col = (p * group + tid) * N;
-            if (col >= a.d) continue;
+            if (!in[p]) continue;
 #pragma unroll
             for (int i = 0; i < N; i += 4)
-                *reinterpret_cast<float4*>(mine + k * plane + col + i) =
+                *reinterpret_cast<float4*>(mine + k * plane + p * HOP + i) =
                     make_float4(acc[p][i], acc[p][i + 1], acc[p][i + 2], acc[p][i + 3]);
         }
     }
 }
 
-// Column sums of the partial rows, in order: out[k][c] = sum_b part[k][b][c].
+// Column sums of the partial rows, in order; out[0] = dw_pre from plane 0, and from plane 1 (the
+// sums of g n) out[1] = dw_post = branch_scale gate A and out[2] = dgate = branch_scale w_post A.
+// 32 columns per CTA; 32 warps take the rows in turn, so that few loads follow one another.
 struct NormSumArgs {
     const float* part;
     float* out[3];
-    int parts, d;
+    const void* w_post;
+    const void* channel;
+    int parts, d, w_bf16;
+    float branch;
 };
-__global__ void __launch_bounds__(256) norm_sum_kernel(const NormSumArgs a) {
-    __shared__ float s[8][32];
-    float* out = a.out[blockIdx.y];
-    if (!out) return;
+__global__ void __launch_bounds__(1024) norm_sum_kernel(const NormSumArgs a) {
+    __shared__ float s[32][33];
+    if (!(blockIdx.y == 0 ? a.out[0] != nullptr : a.out[1] || a.out[2])) return;
+    tc::grid_dependency_wait();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
     const float* p = a.part + (size_t)blockIdx.y * a.parts * a.d;
     float v = 0.f;
-    if (col < a.d)
-        for (int b = w; b < a.parts; b += 8) v += p[(size_t)b * a.d + col];
+    if (col < a.d) {
+#pragma unroll 8
+        for (int b = w; b < a.parts; b += 32) v += p[(size_t)b * a.d + col];
+    }
     s[w][lane] = v;
     __syncthreads();
-    if (w == 0 && col < a.d) {
-        v = s[0][lane];
+    // warp w now holds column 32 blockIdx.x + w: the 32 sums of its lanes, added as a tree
+    v = s[lane][w];
 #pragma unroll
-        for (int k = 1; k < 8; ++k) v += s[k][lane];
-        out[col] = v;
+    for (int k = 16; k > 0; k >>= 1) v += __shfl_xor_sync(0xffffffffu, v, k);
+    const int c = blockIdx.x * 32 + w;
+    if (lane != 0 || c >= a.d) return;
+    if (blockIdx.y == 0) {
+        a.out[0][c] = v;
+        return;
     }
+    auto weight = [&](const void* q) {
+        if (!q) return 1.f;
+        return a.w_bf16 ? to_f32(static_cast<const __nv_bfloat16*>(q)[c]) : static_cast<const float*>(q)[c];
+    };
+    v *= a.branch;
+    if (a.out[1]) a.out[1][c] = v * weight(a.channel);
+    if (a.out[2]) a.out[2][c] = v * weight(a.w_post);
 }
 
 // ---- host side ------------------------------------------------------------------------------------
-constexpr int kNormMaxPieces = 4;
+constexpr int kNormStages = 3;               // rows in a thread's ring; 1 where three do not fit
 constexpr int kNormRingBytes = 200 * 1024;   // of an SM's shared memory, for the rings of its CTAs
 constexpr int kNormMaxRows = 0x7f000000;     // row numbers a few strides ahead stay in 32 bits
 
@@ -443,31 +568,37 @@ static r3_status check_norm(const r3_norm* s) {
 
 struct NormPlan {
     int pieces, threads, grid, stages;
-    bool warp;
+    bool warp, wide;
     size_t smem;
 };
-// Rows of up to 32 kWarpPieces pieces go to one warp each.  Longer ones take a CTA with the
-// least number of pieces per thread (1, 2 or 4) that leaves at most kNormMaxThreads threads.
+// Rows of up to 32 kNormPieces pieces: one warp each, several to a CTA.  Longer ones: a CTA with
+// kNormPieces pieces per thread, twice as many past kNormPieces kNormMaxThreads pieces.  Rows of more
+// than kNormBwdThreads threads are the wide form, which has fewer registers a thread.
 static bool plan_norm(const r3_norm* s, bool bwd, NormPlan* p) {
-    const int n = s->act_dtype == R3_BF16 ? 8 : 4, vecs = s->d / n;
-    p->warp = vecs <= 32 * kWarpPieces;
+    const int vecs = s->d / (s->act_dtype == R3_BF16 ? 8 : 4);
+    p->pieces = kNormPieces;
+    p->warp = vecs <= 32 * p->pieces;
+    if (vecs > kNormMaxThreads * p->pieces) p->pieces *= 2;
+    if (vecs > kNormMaxThreads * p->pieces) return false;
+    p->threads = (vecs + 32 * p->pieces - 1) / (32 * p->pieces) * 32;
+    p->wide = p->threads > kNormBwdThreads || p->pieces > kNormPieces;
+    int rows = 1;
     if (p->warp) {
-        p->pieces = kWarpPieces;
-        p->threads = 32 * kWarpRows;
-    } else {
-        for (p->pieces = 1; (vecs + p->pieces - 1) / p->pieces > kNormMaxThreads; p->pieces *= 2) {}
-        if (p->pieces > kNormMaxPieces) return false;
-        p->threads = ((vecs + p->pieces - 1) / p->pieces + 31) / 32 * 32;
+        // backward, one CTA fills the SM with rows, so that their sums of the weight gradients leave it
+        // as one; a small batch is spread over the SMs
+        const int each = (int)(((long long)s->T + sm_count() - 1) / sm_count());
+        rows = !bwd ? kWarpRows : each < kNormBwdThreads / 32 ? each : kNormBwdThreads / 32;
+        if (rows < 1) rows = 1;
+        p->threads = 32 * rows;
     }
-    p->stages = p->pieces == 4 ? 1 : 3;
-    p->smem = (size_t)p->stages * (bwd ? 4 : 2) * p->pieces * p->threads * 16;
-    // resident CTAs: what the registers allow (64 to 128 a thread), at most what the ring allows
-    int per_sm = (bwd ? 640 : 1280) / p->threads;
+    const size_t per_row = (size_t)(bwd ? 4 : 2) * p->pieces * p->threads * 16;
+    p->stages = kNormStages * per_row <= (size_t)kNormRingBytes ? kNormStages : 1;
+    p->smem = p->stages * per_row;
+    int per_sm = (bwd ? kNormBwdThreads : kNormFwdThreads) / p->threads;
     const int by_smem = (int)(kNormRingBytes / p->smem);
     if (per_sm > by_smem) per_sm = by_smem;
     if (per_sm < 1) per_sm = 1;
-    const int rows = p->warp ? kWarpRows : 1;
-    const int want = (s->T + rows - 1) / rows, most = sm_count() * per_sm;
+    const int want = (int)(((long long)s->T + rows - 1) / rows), most = sm_count() * per_sm;
     p->grid = want < most ? want : most;
     return true;
 }
@@ -484,26 +615,33 @@ static r3_status launch_norm_kernel(const NormArgs& a, const NormPlan& p, cudaSt
     KERN<<<p.grid, p.threads, p.smem, cs>>>(a);
     return launch_status();
 }
-template <typename T, typename W, int P, bool WARP, int S>
+template <typename T, typename W, int P, bool WARP, bool WIDE, int S>
 static r3_status launch_norm(const NormArgs& a, const NormPlan& p, bool bwd, cudaStream_t cs) {
-    return bwd ? launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, S>>(a, p, cs)
-               : launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, S>>(a, p, cs);
+    if (a.y && a.w_post && a.w_pre && a.gate_kind <= R3_GATE_CHANNEL && (!bwd || a.dx_out))
+        return bwd ? launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, S, kFormUsual>>(a, p, cs)
+                   : launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, S, kFormUsual>>(a, p, cs);
+    if (!a.y)
+        return bwd ? launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, S, kFormFirst>>(a, p, cs)
+                   : launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, S, kFormFirst>>(a, p, cs);
+    return bwd ? launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, S, kFormAny>>(a, p, cs)
+               : launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, S, kFormAny>>(a, p, cs);
 }
 template <typename T, typename W>
-static r3_status launch_norm_pieces(const NormArgs& a, const NormPlan& p, bool bwd, cudaStream_t cs) {
-    if (p.warp) return launch_norm<T, W, kWarpPieces, true, 3>(a, p, bwd, cs);
-    if (p.pieces == 1) return launch_norm<T, W, 1, false, 3>(a, p, bwd, cs);
-    if (p.pieces == 2) return launch_norm<T, W, 2, false, 3>(a, p, bwd, cs);
-    return launch_norm<T, W, 4, false, 1>(a, p, bwd, cs);
+static r3_status launch_norm_size(const NormArgs& a, const NormPlan& p, bool bwd, cudaStream_t cs) {
+    constexpr int P = kNormPieces, S = kNormStages;
+    if (p.warp) return launch_norm<T, W, P, true, false, S>(a, p, bwd, cs);
+    if (!p.wide) return launch_norm<T, W, P, false, false, S>(a, p, bwd, cs);
+    if (p.pieces == P) return launch_norm<T, W, P, false, true, S>(a, p, bwd, cs);
+    return p.stages > 1 ? launch_norm<T, W, 2 * P, false, true, S>(a, p, bwd, cs)
+                        : launch_norm<T, W, 2 * P, false, true, 1>(a, p, bwd, cs);
 }
 static r3_status launch_norm_types(const r3_norm* s, const NormArgs& a, const NormPlan& p, bool bwd,
                                    cudaStream_t cs) {
     if (s->act_dtype == R3_BF16)
-        return s->w_dtype == R3_BF16
-                   ? launch_norm_pieces<__nv_bfloat16, __nv_bfloat16>(a, p, bwd, cs)
-                   : launch_norm_pieces<__nv_bfloat16, float>(a, p, bwd, cs);
-    return s->w_dtype == R3_BF16 ? launch_norm_pieces<float, __nv_bfloat16>(a, p, bwd, cs)
-                                 : launch_norm_pieces<float, float>(a, p, bwd, cs);
+        return s->w_dtype == R3_BF16 ? launch_norm_size<__nv_bfloat16, __nv_bfloat16>(a, p, bwd, cs)
+                                     : launch_norm_size<__nv_bfloat16, float>(a, p, bwd, cs);
+    return s->w_dtype == R3_BF16 ? launch_norm_size<float, __nv_bfloat16>(a, p, bwd, cs)
+                                 : launch_norm_size<float, float>(a, p, bwd, cs);
 }
 static NormArgs norm_args(const r3_norm* s) {
     NormArgs a = {};
@@ -552,7 +690,7 @@ extern "C" r3_status r3_norm_residual(const r3_norm* shape, const void* x, const
 extern "C" size_t r3_norm_residual_bwd_workspace_bytes(const r3_norm* shape) {
     r3::NormPlan plan;
     if (r3::check_norm(shape) != R3_OK || !r3::plan_norm(shape, true, &plan)) return 0;
-    return r3::round_up((size_t)3 * plan.grid * shape->d * sizeof(float), 256);
+    return r3::round_up((size_t)2 * plan.grid * shape->d * sizeof(float), 256);
 }
 
 extern "C" r3_status r3_norm_residual_bwd(const r3_norm* shape, const void* x_out, const void* y,
@@ -607,8 +745,17 @@ extern "C" r3_status r3_norm_residual_bwd(const r3_norm* shape, const void* x_ou
         sum.out[0] = dw_pre;
         sum.out[1] = dw_post;
         sum.out[2] = channel ? static_cast<float*>(dgate) : nullptr;
+        sum.w_post = w_post;
+        sum.channel = shape->gate_kind == R3_GATE_CHANNEL ? gate : nullptr;
         sum.d = shape->d;
-        r3::norm_sum_kernel<<<dim3((shape->d + 31) / 32, 3), 256, 0, cs>>>(sum);
+        sum.w_bf16 = shape->w_dtype == R3_BF16;
+        sum.branch = shape->branch_scale;
+        // launched while the rows are still being worked on; it waits for them itself
+        if (r3::tc::launch_dependent(r3::norm_sum_kernel, dim3((shape->d + 31) / 32, 2), dim3(1024), 0,
+                                     cs, sum) != cudaSuccess) {
+            cudaGetLastError();
+            return R3_ERR_CUDA;
+        }
     }
     return r3::launch_status();
 }

@@ -74,8 +74,7 @@ template <> struct Four<float> {
 template <> struct Four<__nv_bfloat16> {
     uint2 v;
     __device__ __forceinline__ void unpack(float* f) const {
-        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
-        const float2 a = __bfloat1622float2(h[0]), b = __bfloat1622float2(h[1]);
+        const float2 a = bf16_pair(v.x), b = bf16_pair(v.y);
         f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
     }
     __device__ __forceinline__ void pack(const float* f) {

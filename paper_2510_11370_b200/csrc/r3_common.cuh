@@ -65,6 +65,11 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
     return __float2bfloat16_rn(v);
 }
 
+// The two bf16 values of a word, widened: one shift and one mask.
+__device__ __forceinline__ float2 bf16_pair(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+
 // 16-byte vector of activations: 8 bf16 or 4 f32.
 template <typename T> struct Vec16;
 template <> struct Vec16<float> {

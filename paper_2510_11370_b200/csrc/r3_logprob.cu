@@ -116,29 +116,7 @@ template <typename T> __device__ __forceinline__ RowSplit split_row(const T* p, 
     return r;
 }
 
-// Two float32 values in one 64-bit register pair: the sums of a thread run in two lanes, with one
-// instruction for both.
-typedef unsigned long long F2;
-__device__ __forceinline__ F2 pair(float lo, float hi) {
-    F2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ void split(F2 v, float& lo, float& hi) {
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-    F2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ F2 add2(F2 a, F2 b) {
-    F2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
-// A 16-byte piece of a row in the form the sums take: its largest value, and its values in pairs.
+// A 16-byte piece of a row in the form the sums take: its largest value, and its values two by two.
 // With FINITE every value is raised to at least -2^100 (c x stays finite: a term 0 times its exponent
 // is 0, not NaN); a NaN stays one.
 template <typename T> struct Piece;
@@ -147,15 +125,18 @@ template <> struct Piece<__nv_bfloat16> {
     uint4 v;
     __device__ __forceinline__ void fill() { v = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
     __device__ __forceinline__ float largest() const {
-        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
-        const float2 m = __bfloat1622float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
+        uint32_t a, b;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(v.x), "r"(v.y));
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(v.z), "r"(v.w));
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(a), "r"(b));
+        const float2 m = bf16_pair(a);
         return fmaxf(m.x, m.y);
     }
-    template <bool FINITE> __device__ __forceinline__ F2 get(int i) const {
-        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
-        const __nv_bfloat162 low = __floats2bfloat162_rn(-1.2676506e30f, -1.2676506e30f);   // -2^100
-        const float2 f = __bfloat1622float2(FINITE ? __hmax2_nan(h[i], low) : h[i]);
-        return pair(f.x, f.y);
+    template <bool FINITE> __device__ __forceinline__ float2 get(int i) const {
+        uint32_t w = i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
+        if (FINITE)                                     // 0xf180: -2^100
+            asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(w) : "r"(w), "r"(0xf180f180u));
+        return bf16_pair(w);
     }
 };
 template <> struct Piece<float> {
@@ -165,30 +146,27 @@ template <> struct Piece<float> {
         v.x = v.y = v.z = v.w = -CUDART_INF_F;
     }
     __device__ __forceinline__ float largest() const { return fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)); }
-    template <bool FINITE> __device__ __forceinline__ F2 get(int i) const {
+    template <bool FINITE> __device__ __forceinline__ float2 get(int i) const {
         const float a = i ? v.z : v.x, b = i ? v.w : v.y;
-        return FINITE ? pair(max_nan(a, -1.2676506e30f), max_nan(b, -1.2676506e30f)) : pair(a, b);
+        return FINITE ? make_float2(max_nan(a, -1.2676506e30f), max_nan(b, -1.2676506e30f))
+                      : make_float2(a, b);
     }
 };
 
 struct RowSums {
-    float M, top;
-    F2 S, U;
+    float M, top, S, U;
 };
 // Moves the reference up to hold a value of c x = t.
 __device__ __forceinline__ void move_ref(RowSums& a, float t) {
     const float m = rintf(t), d = a.M - m, f = ex2(d);
-    const F2 f2 = pair(f, f), zero = pair(0.f, 0.f);
-    a.U = fma2(f2, fma2(pair(d, d), a.S, a.U), zero);
-    a.S = fma2(f2, a.S, zero);
+    a.U = f * (a.U + d * a.S);
+    a.S *= f;
     a.M = m;
 }
-template <bool ENT> __device__ __forceinline__ void add_pair(RowSums& a, F2 u) {
-    float lo, hi;
-    split(u, lo, hi);
-    const F2 e = pair(ex2(lo), ex2(hi));
-    a.S = add2(a.S, e);
-    if (ENT) a.U = fma2(e, u, a.U);
+template <bool ENT> __device__ __forceinline__ void add_term(RowSums& a, float u) {
+    const float e = ex2(u);
+    a.S += e;
+    if (ENT) a.U = fmaf(e, u, a.U);
 }
 
 // What the CTAs of one row leave in the first of them.
@@ -237,9 +215,8 @@ logprob_kernel(const LogprobArgs a) {
     const int per_cta = (rs.vecs + a.split - 1) / a.split;
     const int v0 = min(rs.vecs, rank * per_cta), v1 = min(rs.vecs, v0 + per_cta);
     const float c = a.c;
-    const F2 c2 = pair(c, c);
 
-    RowSums r = {kLowRef, -CUDART_INF_F, 0, 0};
+    RowSums r = {kLowRef, -CUDART_INF_F, 0.f, 0.f};
     int best_vec = v0 + tid < v1 ? v0 + tid : -1;       // the first piece that holds the top so far
     // UNROLL pieces per thread and round; the next round's are on their way while these are summed.
     // Pieces behind the end read as -inf: they change neither the top nor the sums.
@@ -266,13 +243,15 @@ logprob_kernel(const LogprobArgs a) {
         }
         r.top = fmaxf(r.top, m);
         if (m * c - r.M > kMoveRef) move_ref(r, m * c);
-        const F2 ref = pair(-r.M, -r.M);
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             if (j - lane + u * NT >= v1) break;         // the whole warp is behind the end
 #pragma unroll
-            for (int i = 0; i < Piece<T>::PAIRS; ++i)
-                add_pair<ENT>(r, fma2(x[u].template get<ENT>(i), c2, ref));
+            for (int i = 0; i < Piece<T>::PAIRS; ++i) {
+                const float2 f = x[u].template get<ENT>(i);
+                add_term<ENT>(r, fmaf(f.x, c, -r.M));
+                add_term<ENT>(r, fmaf(f.y, c, -r.M));
+            }
         }
     }
     // the single elements in front of the first and behind the last whole piece
@@ -281,7 +260,7 @@ logprob_kernel(const LogprobArgs a) {
     auto take_one = [&](float x) {
         r.top = fmaxf(r.top, x);
         if (x * c - r.M > kMoveRef) move_ref(r, x * c);
-        add_pair<ENT>(r, pair(fmaf(max_nan(x, -1.2676506e30f), c, -r.M), -CUDART_MAX_NORMAL_F));
+        add_term<ENT>(r, fmaf(max_nan(x, -1.2676506e30f), c, -r.M));
     };
     const float vec_top = r.top;                        // of the whole pieces alone
     if (has_head && tid < rs.head) take_one(to_f32(p[tid]));
@@ -310,14 +289,7 @@ logprob_kernel(const LogprobArgs a) {
         m = fmaxf(m, s_red[w][0]);
         top = fmaxf(top, s_red[w][1]);
     }
-    float tS, tU;                                       // this thread's sums
-    {
-        float a0, a1;
-        split(r.S, a0, a1);
-        tS = a0 + a1;
-        split(r.U, a0, a1);
-        tU = a0 + a1;
-    }
+    float tS = r.S, tU = r.U;
     // A top whose c x is beyond 2^20 (masks of the type's lowest value in a whole row, say) leaves
     // the reference no room: the share is summed again with the differences to the known top.
     const bool again = fabsf(top * c) > kPlainTop && fabsf(top) < CUDART_INF_F;

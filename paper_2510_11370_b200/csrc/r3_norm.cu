@@ -27,6 +27,7 @@ namespace r3 {
 
 constexpr int kNormMaxThreads = 512;   // per row
 constexpr int kNormBwdThreads = 384;   // backward: per SM, at up to 168 registers a thread
+constexpr int kNormBwdThreadsF32 = 480;   // ... float32 rows, at up to 136
 constexpr int kNormFwdThreads = 640;   // forward: per SM, at up to 102
 constexpr int kNormPieces = 2;         // pieces per thread; twice as many where these do not reach
 constexpr int kWarpRows = 4;           // forward, one-warp form: rows per CTA
@@ -54,6 +55,18 @@ __device__ __forceinline__ void copy_ahead(void* dst, const void* src) {
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void copy_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
+}
+
+// The values of a 16-byte piece as float32.
+__device__ __forceinline__ void widen(const Vec16<float>& v, float* f) { v.unpack(f); }
+__device__ __forceinline__ void widen(const Vec16<__nv_bfloat16>& v, float* f) {
+    const uint32_t w[4] = {v.v.x, v.v.y, v.v.z, v.v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 t = bf16_pair(w[i]);
+        f[2 * i] = t.x;
+        f[2 * i + 1] = t.y;
+    }
 }
 
 // Sum of NV values over the threads of a row; every thread gets the result.  One barrier per call: the
@@ -90,19 +103,14 @@ __device__ __forceinline__ void load_cols(const void* p, int col, float* f) {
         for (int i = 0; i < N; i += M) {
             const Vec16<W> v = *reinterpret_cast<const Vec16<W>*>(w + i);
             float t[M];
-            v.unpack(t);
+            widen(v, t);
 #pragma unroll
             for (int k = 0; k < M; ++k) f[(i + k) % N] = t[k];
         }
     } else {                                       // 4 f32 columns of a bf16 vector: 8 bytes
         const uint2 v = *reinterpret_cast<const uint2*>(w);
-        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float2 t = __bfloat1622float2(h[i]);
-            f[2 * i] = t.x;
-            f[2 * i + 1] = t.y;
-        }
+        const float2 lo = bf16_pair(v.x), hi = bf16_pair(v.y);
+        f[0] = lo.x; f[1] = lo.y; f[2] = hi.x; f[3] = hi.y;
     }
 }
 template <typename T> __device__ __forceinline__ void store_piece(T* p, const float* f) {
@@ -229,11 +237,11 @@ norm_fwd_kernel(const NormArgs a) {
 #pragma unroll
             for (int i = 0; i < N; ++i) x[p][i] = 0.f;
             if (!in[p]) continue;
-            reinterpret_cast<Ptr>(slot + (2 * p) * 32)->unpack(x[p]);
+            widen(*reinterpret_cast<Ptr>(slot + (2 * p) * 32), x[p]);
             if (!has_y) continue;
             yv[p] = *reinterpret_cast<Ptr>(slot + (2 * p + 1) * 32);
             float y[N];
-            yv[p].unpack(y);
+            widen(yv[p], y);
 #pragma unroll
             for (int i = 0; i < N; ++i) s[0] = fmaf(y[i], y[i], s[0]);
         }
@@ -251,7 +259,7 @@ norm_fwd_kernel(const NormArgs a) {
                 if (!in[p]) continue;
                 float w[N], y[N];
                 post.get(p, me.col, w);
-                yv[p].unpack(y);
+                widen(yv[p], y);
                 if (full) {
                     float g[N];
                     load_cols<T, N>(static_cast<const T*>(a.gate) + (size_t)row * a.d, me.col + p * HOP, g);
@@ -368,8 +376,8 @@ norm_bwd_kernel(const NormArgs a) {
                 xv[p] = *reinterpret_cast<Ptr>(slot + (4 * p) * 32);
                 hv[p] = *reinterpret_cast<Ptr>(slot + (4 * p + 1) * 32);
                 pre.get(p, me.col, w);
-                xv[p].unpack(f);
-                hv[p].unpack(h);
+                widen(xv[p], f);
+                widen(hv[p], h);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     s[0] = fmaf(f[i], f[i], s[0]);
@@ -379,7 +387,7 @@ norm_bwd_kernel(const NormArgs a) {
             if (has_up) gv[p] = *reinterpret_cast<Ptr>(slot + (4 * p + 2) * 32);
             if (has_y) {
                 yv[p] = *reinterpret_cast<Ptr>(slot + (4 * p + 3) * 32);
-                yv[p].unpack(f);
+                widen(yv[p], f);
 #pragma unroll
                 for (int i = 0; i < N; ++i) s[2] = fmaf(f[i], f[i], s[2]);
             }
@@ -398,12 +406,12 @@ norm_bwd_kernel(const NormArgs a) {
             float f[N], g[N];
 #pragma unroll
             for (int i = 0; i < N; ++i) g[i] = 0.f;
-            if (has_up) gv[p].unpack(g);
+            if (has_up) widen(gv[p], g);
             if (has_pre) {
                 float h[N], w[N];
                 pre.get(p, me.col, w);
-                xv[p].unpack(f);
-                hv[p].unpack(h);
+                widen(xv[p], f);
+                widen(hv[p], h);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     acc_pre[p][i] = fmaf(h[i] * f[i], r, acc_pre[p][i]);
@@ -418,7 +426,7 @@ norm_bwd_kernel(const NormArgs a) {
             float w[N];
             post.get(p, me.col, w);
             float(&np)[N] = n[WIDE ? 0 : p];
-            yv[p].unpack(np);
+            widen(yv[p], np);
 #pragma unroll
             for (int i = 0; i < N; ++i) np[i] *= sy;
             if (full) {
@@ -456,7 +464,7 @@ norm_bwd_kernel(const NormArgs a) {
                 if (!in[p]) continue;
                 float(&np)[N] = n[WIDE ? 0 : p];
                 if (WIDE) {
-                    yv[p].unpack(np);
+                    widen(yv[p], np);
 #pragma unroll
                     for (int i = 0; i < N; ++i) np[i] *= sy;
                 }
@@ -465,11 +473,14 @@ norm_bwd_kernel(const NormArgs a) {
                 store_piece<T>(dy + p * HOP, v[p]);
             }
         }
-        // fewer than two reductions in a row: a buffer would come around without a barrier between
-        if (!WARP && FORM != kFormUsual) __syncthreads();
+        // with one reduction per row its buffer comes around without a barrier in between
+        if (!WARP && FORM != kFormUsual && (has_pre || has_post) != (has_y && (has_post || token)))
+            __syncthreads();
     }
     copy_wait<0>();
     if (!a.part) return;
+    // the kernel that adds up the CTAs' sums may be set up meanwhile
+    tc::grid_launch_dependents();
     // One row of partial sums per CTA.  In the one-warp form the warps' are added up in order first.
     const size_t plane = (size_t)gridDim.x * a.d;
     float* mine = a.part + (size_t)blockIdx.x * a.d + me.col;
@@ -594,7 +605,8 @@ static bool plan_norm(const r3_norm* s, bool bwd, NormPlan* p) {
     const size_t per_row = (size_t)(bwd ? 4 : 2) * p->pieces * p->threads * 16;
     p->stages = kNormStages * per_row <= (size_t)kNormRingBytes ? kNormStages : 1;
     p->smem = p->stages * per_row;
-    int per_sm = (bwd ? kNormBwdThreads : kNormFwdThreads) / p->threads;
+    const int resident = !bwd ? kNormFwdThreads : s->act_dtype == R3_BF16 ? kNormBwdThreads : kNormBwdThreadsF32;
+    int per_sm = resident / p->threads;
     const int by_smem = (int)(kNormRingBytes / p->smem);
     if (per_sm > by_smem) per_sm = by_smem;
     if (per_sm < 1) per_sm = 1;

@@ -631,7 +631,7 @@ __global__ void __launch_bounds__(kBwdThreads) logprob_bwd_kernel(const LogprobB
 // ---- host side ------------------------------------------------------------------------------------
 static r3_status check_logits(const r3_logits* s) {
     if (!s) return R3_ERR_INVALID_ARG;
-    if (s->T < 0 || s->V <= 0 || s->V > (1 << 30) || s->ld < s->V) return R3_ERR_INVALID_ARG;
+    if (s->T < 0 || s->T > 0x7f000000 || s->V <= 0 || s->V > (1 << 30) || s->ld < s->V) return R3_ERR_INVALID_ARG;
     if (s->dtype != R3_F32 && s->dtype != R3_BF16) return R3_ERR_INVALID_ARG;
     if (s->id_bytes != 4 && s->id_bytes != 8) return R3_ERR_INVALID_ARG;
     if (!(s->temperature >= 1e-6 && s->temperature <= 1e30))        // 2^100 log2(e) / it stays finite

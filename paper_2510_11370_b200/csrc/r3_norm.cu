@@ -27,7 +27,6 @@ namespace r3 {
 
 constexpr int kNormMaxThreads = 512;   // per row
 constexpr int kNormBwdThreads = 384;   // backward: per SM, at up to 168 registers a thread
-constexpr int kNormBwdThreadsF32 = 480;   // ... float32 rows, at up to 136
 constexpr int kNormFwdThreads = 640;   // forward: per SM, at up to 102
 constexpr int kNormPieces = 2;         // pieces per thread; twice as many where these do not reach
 constexpr int kWarpRows = 4;           // forward, one-warp form: rows per CTA
@@ -121,11 +120,12 @@ template <typename T> __device__ __forceinline__ void store_piece(T* p, const fl
 
 // The usual form has both norms, a gate per column or none, and (backward) a gradient from above; the
 // first has only the norm in front of a block.  They have kernels of their own, whose absent parts
-// cost no instructions; everything else is decided at run time.
-enum { kFormUsual = 0, kFormFirst = 1, kFormAny = 2 };
+// cost no instructions; everything else is decided at run time, except that a gate per element has
+// kernels of its own too (its registers).
+enum { kFormUsual = 0, kFormFirst = 1, kFormAny = 2, kFormFull = 3 };
 
-// The weights of a thread's columns, kept for all its rows: in registers for two pieces of bf16 rows,
-// read again from L1 for each row otherwise (no room).  A column's factor is the vector's element
+// The weights of a thread's columns, kept for all its rows in registers; in the wide form read again
+// from L1 for each row (no room).  A column's factor is the vector's element
 // (1 without a vector) times `times` (likewise) times `scale`.
 template <typename W, int N, int P, bool KEEP> struct Weights {
     float w[KEEP ? P : 1][KEEP ? N : 1];
@@ -180,19 +180,37 @@ __device__ __forceinline__ NormPlace norm_place(uint4* ring) {
     return t;
 }
 
+// A row's own gate (one value, or one per element), loaded a row ahead.
+template <typename T, int P, int FORM> struct RowGate {
+    float token;
+    Vec16<T> full[FORM == kFormFull ? P : 1];
+    __device__ __forceinline__ void load(const NormArgs& a, int row, int col, const bool (&in)[P]) {
+        constexpr int HOP = 32 * Vec16<T>::N;
+        token = 1.f;
+        if (FORM < kFormAny || row >= a.T) return;
+        if (FORM == kFormAny && a.gate_kind == R3_GATE_TOKEN) token = static_cast<const float*>(a.gate)[row];
+        if constexpr (FORM == kFormFull) {
+            const T* g = static_cast<const T*>(a.gate) + (size_t)row * a.d + col;
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+                if (in[p]) full[p] = *reinterpret_cast<const Vec16<T>*>(g + p * HOP);
+        }
+    }
+};
+
 template <typename T, typename W, int P, bool WARP, bool WIDE, int S, int FORM>
 __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kNormMaxThreads)
 norm_fwd_kernel(const NormArgs a) {
     constexpr int N = Vec16<T>::N, Q = 2 * P, HOP = 32 * N;
-    constexpr bool KEEP = !WIDE && sizeof(T) == 2;
+    constexpr bool KEEP = !WIDE;
     typedef const Vec16<T>* Ptr;
     extern __shared__ uint4 ring_all[];
     __shared__ float s_red[2][kNormMaxThreads / 32][4];   // a value per warp of the CTA
-    const bool has_y = FORM == kFormUsual || (FORM == kFormAny && a.y);
-    const bool has_post = FORM == kFormUsual || (FORM == kFormAny && a.w_post);
-    const bool has_pre = FORM != kFormAny || a.w_pre;
+    const bool has_y = FORM == kFormUsual || (FORM >= kFormAny && a.y);
+    const bool has_post = FORM == kFormUsual || (FORM >= kFormAny && a.w_post);
+    const bool has_pre = FORM < kFormAny || a.w_pre;
     const bool token = FORM == kFormAny && a.gate_kind == R3_GATE_TOKEN;
-    const bool full = FORM == kFormAny && a.gate_kind == R3_GATE_FULL;
+    const bool full = FORM == kFormFull;
     const NormPlace me = norm_place<N, P, WARP, Q, S>(ring_all);
     const float inv_d = 1.f / (float)a.d, eps = a.eps, res = a.res;
     const size_t start = (size_t)me.row * a.d + me.col, step = (size_t)me.stride * a.d;
@@ -223,6 +241,8 @@ norm_fwd_kernel(const NormArgs a) {
     const void* channel = a.gate_kind == R3_GATE_CHANNEL ? a.gate : nullptr;
     if (has_y) post.init(a.w_post, channel, a.branch, me.col, in);
     if (has_pre) pre.init(a.w_pre, nullptr, 1.f, me.col, in);
+    RowGate<T, P, FORM> gate, ahead;
+    ahead.load(a, me.row, me.col, in);
     T* x_out = static_cast<T*>(a.out0) + start;
     T* h_out = static_cast<T*>(a.out1) + start;
     int stage = 0;
@@ -247,13 +267,15 @@ norm_fwd_kernel(const NormArgs a) {
         }
         fetch(slot);
         stage = stage + 1 == S ? 0 : stage + 1;
+        gate = ahead;
+        ahead.load(a, row + me.stride, me.col, in);
         float r = 1.f;
         if (has_post) {
             row_sum<1, WARP>(s, s_red[0], me.warps);
             r = rsqrtf(s[0] * inv_d + eps);
         }
         if (has_y) {
-            if (token) r *= static_cast<const float*>(a.gate)[row];
+            if (token) r *= gate.token;
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 if (!in[p]) continue;
@@ -262,7 +284,7 @@ norm_fwd_kernel(const NormArgs a) {
                 widen(yv[p], y);
                 if (full) {
                     float g[N];
-                    load_cols<T, N>(static_cast<const T*>(a.gate) + (size_t)row * a.d, me.col + p * HOP, g);
+                    widen(gate.full[full ? p : 0], g);
 #pragma unroll
                     for (int i = 0; i < N; ++i) y[i] *= g[i];
                 }
@@ -307,16 +329,16 @@ template <typename T, typename W, int P, bool WARP, bool WIDE, int S, int FORM>
 __global__ void __launch_bounds__(WIDE ? kNormMaxThreads : kNormBwdThreads)
 norm_bwd_kernel(const NormArgs a) {
     constexpr int N = Vec16<T>::N, Q = 4 * P, HOP = 32 * N;
-    constexpr bool KEEP = !WIDE && sizeof(T) == 2;
+    constexpr bool KEEP = !WIDE;
     typedef const Vec16<T>* Ptr;
     extern __shared__ uint4 ring_all[];
     __shared__ float s_red[2][kNormMaxThreads / 32][4];   // a value per warp of the CTA
-    const bool has_y = FORM == kFormUsual || (FORM == kFormAny && a.y);
-    const bool has_post = FORM == kFormUsual || (FORM == kFormAny && a.w_post);
-    const bool has_pre = FORM != kFormAny || a.w_pre;
+    const bool has_y = FORM == kFormUsual || (FORM >= kFormAny && a.y);
+    const bool has_post = FORM == kFormUsual || (FORM >= kFormAny && a.w_post);
+    const bool has_pre = FORM < kFormAny || a.w_pre;
     const bool has_up = FORM == kFormUsual || a.dx_out;
     const bool token = FORM == kFormAny && a.gate_kind == R3_GATE_TOKEN;
-    const bool full = FORM == kFormAny && a.gate_kind == R3_GATE_FULL;
+    const bool full = FORM == kFormFull;
     const NormPlace me = norm_place<N, P, WARP, Q, S>(ring_all);
     const float inv_d = 1.f / (float)a.d, eps = a.eps, res = has_y ? a.res : 1.f;
     const size_t start = (size_t)me.row * a.d + me.col, step = (size_t)me.stride * a.d;
@@ -359,6 +381,8 @@ norm_bwd_kernel(const NormArgs a) {
     for (int p = 0; p < P; ++p)
 #pragma unroll
         for (int i = 0; i < N; ++i) acc_pre[p][i] = acc_post[p][i] = 0.f;
+    RowGate<T, P, FORM> row_gate, ahead;
+    ahead.load(a, me.row, me.col, in);
     T* dx = static_cast<T*>(a.out0) + start;
     T* dy = static_cast<T*>(a.out1) + start;
     int stage = 0;
@@ -394,11 +418,13 @@ norm_bwd_kernel(const NormArgs a) {
         }
         fetch(slot);
         stage = stage + 1 == S ? 0 : stage + 1;
+        row_gate = ahead;
+        ahead.load(a, row + me.stride, me.col, in);
         if (has_pre || has_post) row_sum<3, WARP>(s, s_red[0], me.warps);
         const float r = rsqrtf(s[0] * inv_d + eps);
         const float rrc = s[1] * inv_d * r * r * r;             // r^2 c
         const float sy = has_post ? rsqrtf(s[2] * inv_d + eps) : 1.f;
-        const float gate_t = token ? static_cast<const float*>(a.gate)[row] : 1.f;
+        const float gate_t = row_gate.token;                    // 1 unless the gate is the token's
         float v[P][N], n[WIDE ? 1 : P][N], z[1] = {0.f};      // wide rows: n is formed again, no room
 #pragma unroll
         for (int p = 0; p < P; ++p) {
@@ -431,14 +457,13 @@ norm_bwd_kernel(const NormArgs a) {
             for (int i = 0; i < N; ++i) np[i] *= sy;
             if (full) {
                 float gate[N], dg[N];
-                const size_t at = (size_t)row * a.d;
-                load_cols<T, N>(static_cast<const T*>(a.gate) + at, me.col + p * HOP, gate);
+                widen(row_gate.full[full ? p : 0], gate);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     dg[i] = g[i] * w[i] * np[i];
                     g[i] *= gate[i];
                 }
-                store_piece<T>(static_cast<T*>(a.dgate) + at + me.col + p * HOP, dg);
+                store_piece<T>(static_cast<T*>(a.dgate) + (size_t)row * a.d + me.col + p * HOP, dg);
             }
             if (token) {
 #pragma unroll
@@ -605,8 +630,7 @@ static bool plan_norm(const r3_norm* s, bool bwd, NormPlan* p) {
     const size_t per_row = (size_t)(bwd ? 4 : 2) * p->pieces * p->threads * 16;
     p->stages = kNormStages * per_row <= (size_t)kNormRingBytes ? kNormStages : 1;
     p->smem = p->stages * per_row;
-    const int resident = !bwd ? kNormFwdThreads : s->act_dtype == R3_BF16 ? kNormBwdThreads : kNormBwdThreadsF32;
-    int per_sm = resident / p->threads;
+    int per_sm = (bwd ? kNormBwdThreads : kNormFwdThreads) / p->threads;
     const int by_smem = (int)(kNormRingBytes / p->smem);
     if (per_sm > by_smem) per_sm = by_smem;
     if (per_sm < 1) per_sm = 1;
@@ -635,6 +659,9 @@ static r3_status launch_norm(const NormArgs& a, const NormPlan& p, bool bwd, cud
     if (!a.y)
         return bwd ? launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, S, kFormFirst>>(a, p, cs)
                    : launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, S, kFormFirst>>(a, p, cs);
+    if (a.gate_kind == R3_GATE_FULL)
+        return bwd ? launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, S, kFormFull>>(a, p, cs)
+                   : launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, S, kFormFull>>(a, p, cs);
     return bwd ? launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, S, kFormAny>>(a, p, cs)
                : launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, S, kFormAny>>(a, p, cs);
 }

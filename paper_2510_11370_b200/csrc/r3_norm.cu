@@ -71,7 +71,7 @@ __device__ __forceinline__ void widen(const Vec16<__nv_bfloat16>& v, float* f) {
 // Sum of NV values over the threads of a row; every thread gets the result.  One barrier per call: the
 // caller alternates buffers, so that a buffer is only written again behind the barrier of the call in
 // between.
-template <int NV, bool WARP>
+template <int NV, bool WARP, bool WIDE>
 __device__ __forceinline__ void row_sum(float (&v)[NV], float (*red)[4], int warps) {
 #pragma unroll
     for (int s = 16; s > 0; s >>= 1) {
@@ -84,6 +84,19 @@ __device__ __forceinline__ void row_sum(float (&v)[NV], float (*red)[4], int war
         for (int i = 0; i < NV; ++i) red[threadIdx.x >> 5][i] = v[i];
     }
     __syncthreads();
+    if (WIDE) {                                     // up to 16 warps: a tree over the lanes
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = lane < warps ? red[lane & 15][i] : 0.f;
+#pragma unroll
+        for (int s = 8; s > 0; s >>= 1) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], s);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = __shfl_sync(0xffffffffu, v[i], 0);
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < NV; ++i) v[i] = 0.f;
     for (int w = 0; w < warps; ++w) {                                    // fixed order
@@ -271,7 +284,7 @@ norm_fwd_kernel(const NormArgs a) {
         ahead.load(a, row + me.stride, me.col, in);
         float r = 1.f;
         if (has_post) {
-            row_sum<1, WARP>(s, s_red[0], me.warps);
+            row_sum<1, WARP, WIDE>(s, s_red[0], me.warps);
             r = rsqrtf(s[0] * inv_d + eps);
         }
         if (has_y) {
@@ -299,7 +312,7 @@ norm_fwd_kernel(const NormArgs a) {
             for (int p = 0; p < P; ++p)
 #pragma unroll
                 for (int i = 0; i < N; ++i) s[0] = fmaf(x[p][i], x[p][i], s[0]);
-            row_sum<1, WARP>(s, s_red[1], me.warps);
+            row_sum<1, WARP, WIDE>(s, s_red[1], me.warps);
             r = rsqrtf(s[0] * inv_d + eps);
 #pragma unroll
             for (int p = 0; p < P; ++p) {
@@ -420,7 +433,7 @@ norm_bwd_kernel(const NormArgs a) {
         stage = stage + 1 == S ? 0 : stage + 1;
         row_gate = ahead;
         ahead.load(a, row + me.stride, me.col, in);
-        if (has_pre || has_post) row_sum<3, WARP>(s, s_red[0], me.warps);
+        if (has_pre || has_post) row_sum<3, WARP, WIDE>(s, s_red[0], me.warps);
         const float r = rsqrtf(s[0] * inv_d + eps);
         const float rrc = s[1] * inv_d * r * r * r;             // r^2 c
         const float sy = has_post ? rsqrtf(s[2] * inv_d + eps) : 1.f;
@@ -479,7 +492,7 @@ norm_bwd_kernel(const NormArgs a) {
             }
         }
         if (has_y) {
-            if (has_post || token) row_sum<1, WARP>(z, s_red[1], me.warps);
+            if (has_post || token) row_sum<1, WARP, WIDE>(z, s_red[1], me.warps);
             const float k = gate_t * sy;
             const float e = has_post ? -z[0] * inv_d : 0.f;
             if (token && me.col == 0)

@@ -9,13 +9,15 @@
 // magnitude to 448 or less, so that scaling is exact both ways and the one rounding is the code's.
 // The second moment is kept as its square root, which halves the range its codes have to span; a
 // root above zero is never kept as zero, because the update divides by it (the smallest code is the
-// safe side: a smaller step).  Every operation that leads to a stored state is rounded to float32
-// by itself (no fused multiply-add), so the states are a function of the inputs alone and do not
-// depend on how a compiler contracts the expressions.
+// safe side: a smaller step).  Every sum and product that leads to a stored state is rounded to float32
+// by itself (no fused multiply-add), so that the moments and scales do not depend on how a compiler
+// contracts the expressions; the root alone is the hardware's approximation.
 //
-// A warp takes a block: lane l holds elements 4 l .. 4 l + 3 and 128 + 4 l .. 128 + 4 l + 3, so that
-// every load and store of the warp covers consecutive bytes whatever the type's width, and one
-// warp-wide maximum per state gives the scale.  The table of tensors travels in the kernel's
+// A warp takes a block, and one warp-wide maximum per state gives its scale.  With 32-bit states lane l
+// holds elements 4 l .. 4 l + 3 and 128 + 4 l .. 128 + 4 l + 3: every load and store of the warp covers
+// consecutive bytes.  With 8-bit states it holds 8 l .. 8 l + 7 and takes them out of a ring in shared
+// memory that the warp copies its blocks to ahead (16 bytes per lane and copy, so 4 or 5 copies, 6 loads
+// and 3 or 4 stores a block where 4-element pieces take twice as many).  The table of tensors travels in the kernel's
 // parameters: no workspace, no copy, and a captured launch keeps its own.
 #include <cuda_fp8.h>
 
@@ -34,8 +36,9 @@ namespace r3 {
 constexpr int kAdamBlock = 256;                     // elements per scale
 constexpr int kAdamThreads = 256;
 constexpr int kAdamWarps = kAdamThreads / 32;
-constexpr int kAdamCtas = 4;                        // resident per SM at 64 registers a thread
-constexpr int kAdamMaxPerWarp = 16;                 // blocks per warp and chunk
+constexpr int kAdamCtas = 4, kAdamCtas8 = 2;        // resident per SM at up to 64 and 128 registers a thread
+constexpr int kAdamStages = 4;                      // 8-bit states: blocks in a warp's ring
+constexpr int kAdamMaxPerWarp8 = 16, kAdamMaxPerWarp = 8;   // blocks per warp and chunk, 8- and 32-bit states
 constexpr int kAdamSmall = 24, kAdamLarge = 400;    // tensors per launch
 
 struct AdamTensor {
@@ -51,10 +54,9 @@ struct AdamTensor {
     unsigned first;                                 // first chunk of this tensor
 };
 struct AdamScalars {
-    float beta1, one_beta1, beta2, one_beta2, eps, lr, bias1, bias2;
+    float beta1, one_beta1, beta2, one_beta2, eps, lr, bias1, bias2, one;
     const float* grad_scale;
     const float* dynamic;                           // {lr, bias1, bias2} on the device, or null
-    unsigned chunks;
     int tensors, per_warp;
 };
 template <int CAP> struct AdamTable {
@@ -101,14 +103,17 @@ template <> struct Four<uint8_t> {                  // e4m3 codes
         v = lo | (hi << 16);
     }
 };
-// A lane's eight elements of a block: 4 l .. and 128 + 4 l ..; `left` elements of the tensor follow
-// from the block's first on (only looked at where FULL is false; what lies behind reads as 0 and is
-// not written).
-template <bool FULL, typename T>
+// A lane's eight elements of a block, in two fours: 4 l .. and 128 + 4 l .., or (NEAR) 8 l .. and
+// 8 l + 4 ..; `left` elements of the tensor follow from the block's first on (only looked at where FULL
+// is false; what lies behind reads as 0 and is not written).
+template <bool NEAR> __device__ __forceinline__ int place(int h, int lane) {
+    return NEAR ? 8 * lane + 4 * h : 128 * h + 4 * lane;
+}
+template <bool FULL, bool NEAR, typename T>
 __device__ __forceinline__ void take(const T* p, int lane, int left, Four<T> (&f)[2]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int at = 128 * h + 4 * lane;
+        const int at = place<NEAR>(h, lane);
         if (FULL) {
             f[h] = *reinterpret_cast<const Four<T>*>(p + at);
         } else {
@@ -122,11 +127,19 @@ __device__ __forceinline__ void take(const T* p, int lane, int left, Four<T> (&f
         }
     }
 }
-template <bool FULL, typename T>
+// Two neighbouring fours of less than 16 bytes are one load or store.
+template <typename T> struct alignas(sizeof(T) == 4 ? 16 : 8 * sizeof(T)) Eight {
+    Four<T> f[2];
+};
+template <bool FULL, bool NEAR, typename T>
 __device__ __forceinline__ void put(T* p, int lane, int left, const Four<T> (&f)[2]) {
+    if constexpr (FULL && NEAR && sizeof(T) < 4) {
+        *reinterpret_cast<Eight<T>*>(p + 8 * lane) = {{f[0], f[1]}};
+        return;
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int at = 128 * h + 4 * lane;
+        const int at = place<NEAR>(h, lane);
         if (FULL) {
             *reinterpret_cast<Four<T>*>(p + at) = f[h];
         } else {
@@ -138,27 +151,62 @@ __device__ __forceinline__ void put(T* p, int lane, int left, const Four<T> (&f)
         }
     }
 }
+// Two float32 values in a register pair, one instruction for both.  There is no sum among them: the
+// compiler contracts a product and a sum of pairs into one fused operation, .rn or not (measured: a
+// quarter of random sums of two products differ).  A sum is a fused multiply-add with a factor of 1 that
+// only the launch knows, which rounds once and has nothing to be contracted with.
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 pair(float lo, float hi) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void split(F2 v, float& lo, float& hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
 __device__ __forceinline__ float max_abs(float a, float b) {      // a NaN stays one
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
     return r;
 }
-// Biased exponent of the block's scale from the bits of its largest magnitude f 2^e, f in [1, 2):
-// 448 = 1.75 2^8, so e - 8, and one more where f > 1.75 (the addition carries then); at least 1.
+// Biased exponent of the scale 2^k for a block whose largest magnitude is f 2^e, f in [1, 2), given
+// as bits: 448 = 1.75 2^8, so k = e - 8, and one more where f > 1.75 (the addition carries then); at
+// least -126.
 __device__ __forceinline__ uint32_t scale_exponent(uint32_t bits) {
     const uint32_t e = (bits + 0x1fffffu) >> 23;
     return e > 9u ? e - 8u : 1u;
 }
-// The eight codes of a lane and the scale of its block.  ROOT: values are >= 0 and none above zero
-// becomes code 0.
-template <bool ROOT>
-__device__ __forceinline__ float quantise(const float (&f)[8], Four<uint8_t> (&codes)[2]) {
+// The same for the root of a second moment whose largest value is f 2^e: the root is at most 448 2^k
+// exactly where the value is at most 448^2 4^k, 448^2 = 1.53125 2^17, so k = ceil((e - 17 + [f >
+// 1.53125]) / 2).  Values below float32's normal range are brought into it first.
+__device__ __forceinline__ uint32_t root_exponent(uint32_t bits) {
+    if (bits == 0u) return 1u;
+    int shift = 0;
+    if (bits < 0x00800000u) {
+        bits = __float_as_uint(__uint_as_float(bits) * 18446744073709551616.f);         // 2^64
+        shift = 64;
+    }
+    const int e = (int)((bits + 0x3bffffu) >> 23) - 127 - shift;
+    return (uint32_t)(((e - 16) >> 1) + 127);
+}
+// The largest magnitude of a block's finite values, as bits; `clean` tells whether all are.
+__device__ __forceinline__ uint32_t block_top(const float (&f)[8], bool& clean) {
     float big = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) big = max_abs(big, f[i]);
     uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(big));
-    const bool clean = top < 0x7f800000u;
-    if (!clean) {                                   // the scale is that of the finite elements
+    clean = top < 0x7f800000u;
+    if (!clean) {
         top = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -167,47 +215,71 @@ __device__ __forceinline__ float quantise(const float (&f)[8], Four<uint8_t> (&c
         }
         top = __reduce_max_sync(0xffffffffu, top);
     }
-    const uint32_t e = scale_exponent(top);
-    const float inv = __uint_as_float((254u - e) << 23);
-    float least = f[0];
-    if (ROOT) {
+    return top;
+}
+__device__ __forceinline__ void mark_nan(const float (&f)[8], Four<uint8_t> (&codes)[2]) {
 #pragma unroll
-        for (int i = 1; i < 8; ++i) least = fminf(least, f[i]);
-    }
+    for (int i = 0; i < 8; ++i)                     // 0x7f: NaN
+        if ((__float_as_uint(f[i]) & 0x7f800000u) == 0x7f800000u) codes[i >> 2].v |= 0x7fu << (8 * (i & 3));
+}
+// The eight codes of a lane and the scale of its block.
+__device__ __forceinline__ float quantise(const float (&f)[8], Four<uint8_t> (&codes)[2]) {
+    bool clean;
+    const uint32_t e = scale_exponent(block_top(f, clean));
+    const float inv = __uint_as_float((254u - e) << 23);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         float q[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) q[i] = f[4 * h + i] * inv;
         codes[h].pack(q);
-        if (ROOT) {
-            // 1 in every byte that is 0 (no code here has its top bit set, so nothing carries)
-            const uint32_t zeros = (((codes[h].v + 0x7f7f7f7fu) & 0x80808080u) ^ 0x80808080u) >> 7;
-            if (least > 0.f) {
-                codes[h].v |= zeros;
-            } else {
+    }
+    if (!clean) mark_nan(f, codes);
+    return __uint_as_float(e << 23);
+}
+// The same for the second moment v (least its least element), kept as its root: none above zero
+// becomes code 0.
+__device__ __forceinline__ float quantise_root(const float (&v)[8], const float (&root)[8], float least,
+                                               Four<uint8_t> (&codes)[2]) {
+    bool clean;
+    const uint32_t e = root_exponent(block_top(v, clean));
+    const float inv = __uint_as_float((254u - e) << 23);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (f[4 * h + i] > 0.f) codes[h].v |= zeros & (0xffu << (8 * i));
-            }
-        }
-        if (!clean) {
+    for (int h = 0; h < 2; ++h) {
+        float q[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)             // 0x7f: NaN
-                if ((__float_as_uint(f[4 * h + i]) & 0x7f800000u) == 0x7f800000u)
-                    codes[h].v |= 0x7fu << (8 * i);
+        for (int i = 0; i < 4; ++i) q[i] = root[4 * h + i] * inv;
+        codes[h].pack(q);
+        // 1 in every byte that is 0 (no code here has its top bit set, so nothing carries)
+        const uint32_t zeros = (((codes[h].v + 0x7f7f7f7fu) & 0x80808080u) ^ 0x80808080u) >> 7;
+        if (least > 0.f) {
+            codes[h].v |= zeros;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (v[4 * h + i] > 0.f) codes[h].v |= zeros & (0xffu << (8 * i));
         }
     }
+    if (!clean) mark_nan(v, codes);
     return __uint_as_float(e << 23);
 }
 
 struct AdamRates {                                  // what the whole launch shares
-    float beta1, one_beta1, beta2, one_beta2, eps, bias2, step, keep, gs;
+    float beta1, one_beta1, beta2, one_beta2, eps, bias2, step, keep, gs, one;
 };
 
-// One block's values on their way: loaded a block ahead where the states are codes (the arithmetic
-// around the codes is long enough to leave the memory idle otherwise; with 32-bit states the
-// occupancy does as well, and the registers are better spent on it).
+__device__ __forceinline__ void copy_ahead16(void* dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                 ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_ahead4(void* dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;"
+                 ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+
+// One block's values: loaded to registers, or (8-bit states) copied ahead to a stage of the warp's ring.
+// The arithmetic around the codes is long enough to leave the memory idle without the ring; with 32-bit
+// states the occupancy does as well, and the registers and the shared memory are better left to it.
 template <typename P, typename G, bool MASTER, bool BITS8> struct AdamBlock {
     typedef typename std::conditional<MASTER, float, P>::type Wt;
     typedef typename std::conditional<BITS8, uint8_t, float>::type St;
@@ -216,14 +288,55 @@ template <typename P, typename G, bool MASTER, bool BITS8> struct AdamBlock {
     Four<St> m[2], v[2];
     float ms, vs;
 
+    struct Stage {
+        alignas(16) Wt w[kAdamBlock];
+        G g[kAdamBlock];
+        St m[kAdamBlock], v[kAdamBlock];
+        float scale[4];                             // of m, of v, unused
+    };
+    template <typename T> static __device__ __forceinline__ void ahead(T* to, const void* from, long long at, int lane) {
+        constexpr int N = 16 / sizeof(T);
+#pragma unroll
+        for (int i = 0; i < kAdamBlock; i += 32 * N)
+            copy_ahead16(to + i + N * lane, static_cast<const T*>(from) + at + i + N * lane);
+    }
+    // A whole block, copied by its warp (one group of copies per lane, empty for block >= end).
+    static __device__ __forceinline__ void fetch(Stage* s, const AdamTensor& t, long long block,
+                                                 long long end, int lane) {
+        if (block < end) {
+            const long long at = block * kAdamBlock;
+            ahead(s->w, MASTER ? static_cast<const void*>(t.master) : t.param, at, lane);
+            ahead(s->g, t.grad, at, lane);
+            // the codes of both states: 16 lanes each
+            const int half = lane >> 4, i = 16 * (lane & 15);
+            copy_ahead16((half ? s->v : s->m) + i, static_cast<const uint8_t*>(half ? t.v : t.m) + at + i);
+            if (lane < 2) copy_ahead4(&s->scale[lane], (lane == 0 ? t.m_scale : t.v_scale) + block);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    template <typename T> static __device__ __forceinline__ void near(const T* p, int lane, Four<T> (&f)[2]) {
+        const Eight<T> e = *reinterpret_cast<const Eight<T>*>(p + 8 * lane);
+        f[0] = e.f[0];
+        f[1] = e.f[1];
+    }
+    __device__ __forceinline__ void from_stage(const Stage* s, int lane) {
+        near(s->w, lane, w);
+        near(s->g, lane, g);
+        near(s->m, lane, m);
+        near(s->v, lane, v);
+        const float2 both = *reinterpret_cast<const float2*>(s->scale);
+        ms = both.x;
+        vs = both.y;
+    }
+
     template <bool FULL>
     __device__ __forceinline__ void load(const AdamTensor& t, long long block, int lane, int left) {
         const long long at = block * kAdamBlock;
-        take<FULL>((MASTER ? reinterpret_cast<const Wt*>(t.master) : static_cast<const Wt*>(t.param)) + at,
+        take<FULL, BITS8>((MASTER ? reinterpret_cast<const Wt*>(t.master) : static_cast<const Wt*>(t.param)) + at,
                    lane, left, w);
-        take<FULL>(static_cast<const G*>(t.grad) + at, lane, left, g);
-        take<FULL>(static_cast<const St*>(t.m) + at, lane, left, m);
-        take<FULL>(static_cast<const St*>(t.v) + at, lane, left, v);
+        take<FULL, BITS8>(static_cast<const G*>(t.grad) + at, lane, left, g);
+        take<FULL, BITS8>(static_cast<const St*>(t.m) + at, lane, left, m);
+        take<FULL, BITS8>(static_cast<const St*>(t.v) + at, lane, left, v);
         if (BITS8) {
             ms = t.m_scale[block];
             vs = t.v_scale[block];
@@ -241,26 +354,46 @@ template <typename P, typename G, bool MASTER, bool BITS8> struct AdamBlock {
             m[h].unpack(fm + 4 * h);
             v[h].unpack(fv + 4 * h);
         }
+        const F2 gs = pair(a.gs, a.gs), b1 = pair(a.beta1, a.beta1), c1 = pair(a.one_beta1, a.one_beta1);
+        const F2 b2 = pair(a.beta2, a.beta2), c2 = pair(a.one_beta2, a.one_beta2), one = pair(a.one, a.one);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float gi = __fmul_rn(fg[i], a.gs);
-            float m0 = fm[i], v0 = fv[i];
+        for (int i = 0; i < 8; i += 2) {
+            const F2 gi = mul2(pair(fg[i], fg[i + 1]), gs);
+            F2 m0 = pair(fm[i], fm[i + 1]), v0 = pair(fv[i], fv[i + 1]);
             if (BITS8) {
-                m0 *= ms;                           // powers of two: exact
-                v0 *= vs;
-                v0 = __fmul_rn(v0, v0);
+                m0 = mul2(m0, pair(ms, ms));        // powers of two: exact
+                v0 = mul2(v0, pair(vs, vs));
+                v0 = mul2(v0, v0);
             }
-            fm[i] = __fadd_rn(__fmul_rn(a.beta1, m0), __fmul_rn(a.one_beta1, gi));
-            fv[i] = __fadd_rn(__fmul_rn(a.beta2, v0), __fmul_rn(a.one_beta2, __fmul_rn(gi, gi)));
-            root[i] = __fsqrt_rn(fv[i]);
-            // a quotient a few units of 2^-24 off moves the weight by far less than its rounding
-            float inv;
-            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(fmaf(root[i], a.bias2, a.eps)));
-            fw[i] = fmaf(-a.step, fm[i] * inv, fw[i] * a.keep);
+            split(fma2(mul2(b1, m0), one, mul2(c1, gi)), fm[i], fm[i + 1]);
+            split(fma2(mul2(b2, v0), one, mul2(c2, mul2(gi, gi))), fv[i], fv[i + 1]);
+        }
+        // The root and the quotient are a unit or two of 2^-23 off: far less than the roundings of the
+        // weight and of the root's code.  Below float32's normal range the root takes a longer form.
+        float least = fv[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) least = fminf(least, fv[i]);
+        if (least >= 1.17549435e-38f) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root[i]) : "f"(fv[i]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) asm("sqrt.approx.f32 %0, %1;" : "=f"(root[i]) : "f"(fv[i]));
+        }
+        const F2 bias2 = pair(a.bias2, a.bias2), eps = pair(a.eps, a.eps);
+        const F2 step = pair(-a.step, -a.step), keep = pair(a.keep, a.keep);
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            float lo, hi;
+            split(fma2(pair(root[i], root[i + 1]), bias2, eps), lo, hi);
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(lo) : "f"(lo));
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(hi) : "f"(hi));
+            const F2 up = mul2(pair(fm[i], fm[i + 1]), pair(lo, hi));
+            split(fma2(step, up, mul2(pair(fw[i], fw[i + 1]), keep)), fw[i], fw[i + 1]);
         }
         if constexpr (BITS8) {
-            ms = quantise<false>(fm, m);
-            vs = quantise<true>(root, v);
+            ms = quantise(fm, m);
+            vs = quantise_root(fv, root, least, v);
             if (lane == 0) {
                 t.m_scale[block] = ms;
                 t.v_scale[block] = vs;
@@ -272,22 +405,23 @@ template <typename P, typename G, bool MASTER, bool BITS8> struct AdamBlock {
                 v[h].pack(fv + 4 * h);
             }
         }
-        put<FULL>(static_cast<St*>(t.m) + at, lane, left, m);
-        put<FULL>(static_cast<St*>(t.v) + at, lane, left, v);
+        put<FULL, BITS8>(static_cast<St*>(t.m) + at, lane, left, m);
+        put<FULL, BITS8>(static_cast<St*>(t.v) + at, lane, left, v);
         Four<P> p[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) p[h].pack(fw + 4 * h);
-        put<FULL>(static_cast<P*>(t.param) + at, lane, left, p);
+        put<FULL, BITS8>(static_cast<P*>(t.param) + at, lane, left, p);
         if constexpr (MASTER) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) w[h].pack(fw + 4 * h);
-            put<FULL>(t.master + at, lane, left, w);
+            put<FULL, BITS8>(t.master + at, lane, left, w);
         }
     }
 };
 
 template <typename P, typename G, bool MASTER, bool BITS8, int CAP>
-__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamTable<CAP> a) {
+__global__ void __launch_bounds__(kAdamThreads, BITS8 ? kAdamCtas8 : kAdamCtas) adamw_kernel(const __grid_constant__ AdamTable<CAP> a) {
+    extern __shared__ uint4 ring_all[];             // 8-bit states: [warps][kAdamStages] stages
     AdamRates r;
     r.gs = a.s.grad_scale ? *a.s.grad_scale : 1.f;
     if (!(fabsf(r.gs) <= 3.402823466e38f)) return;  // NaN or infinite: the step is skipped
@@ -299,43 +433,49 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
     r.beta2 = a.s.beta2;
     r.one_beta2 = a.s.one_beta2;
     r.eps = a.s.eps;
+    r.one = a.s.one;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (unsigned chunk = blockIdx.x; chunk < a.s.chunks; chunk += gridDim.x) {
-        int lo = 0, hi = a.s.tensors - 1;           // the last tensor that starts at or before it
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (a.t[mid].first <= chunk) lo = mid;
-            else hi = mid - 1;
+    const unsigned chunk = blockIdx.x;
+    int lo = 0, hi = a.s.tensors - 1;           // the last tensor that starts at or before it
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.t[mid].first <= chunk) lo = mid;
+        else hi = mid - 1;
+    }
+    const AdamTensor t = a.t[lo];
+    r.keep = 1.f - lr * t.decay;
+    // the warps of a CTA take the chunk's blocks in turn
+    long long block = (long long)(chunk - t.first) * (kAdamWarps * a.s.per_warp) + warp;
+    const long long whole = t.n / kAdamBlock;   // blocks without a ragged end
+    const long long end = min(whole, block + (long long)kAdamWarps * a.s.per_warp);
+    AdamBlock<P, G, MASTER, BITS8> b;
+    if constexpr (BITS8) {
+        typedef typename AdamBlock<P, G, MASTER, BITS8>::Stage Stage;
+        Stage* ring = reinterpret_cast<Stage*>(ring_all) + warp * kAdamStages;
+#pragma unroll
+        for (int s = 0; s < kAdamStages; ++s) b.fetch(ring + s, t, block + s * kAdamWarps, end, lane);
+        for (int stage = 0; block < end; block += kAdamWarps) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kAdamStages - 1) : "memory");
+            __syncwarp();                       // the lanes' copies of the scales
+            b.from_stage(ring + stage, lane);
+            __syncwarp();                       // read by all lanes before it is written again
+            b.fetch(ring + stage, t, block + kAdamStages * kAdamWarps, end, lane);
+            stage = stage + 1 == kAdamStages ? 0 : stage + 1;
+            b.template update<true>(t, block, lane, kAdamBlock, r);
         }
-        const AdamTensor t = a.t[lo];
-        r.keep = 1.f - lr * t.decay;
-        // the warps of a CTA take the chunk's blocks in turn
-        long long block = (long long)(chunk - t.first) * (kAdamWarps * a.s.per_warp) + warp;
-        const long long whole = t.n / kAdamBlock;   // blocks without a ragged end
-        const long long end = min(whole, block + (long long)kAdamWarps * a.s.per_warp);
-        AdamBlock<P, G, MASTER, BITS8> b;
-        if (BITS8) {
-            if (block < end) b.template load<true>(t, block, lane, kAdamBlock);
-            while (block < end) {
-                AdamBlock<P, G, MASTER, BITS8> now = b;
-                const long long next = block + kAdamWarps;
-                if (next < end) b.template load<true>(t, next, lane, kAdamBlock);
-                now.template update<true>(t, block, lane, kAdamBlock, r);
-                block = next;
-            }
-        } else {
-            for (; block < end; block += kAdamWarps) {
-                b.template load<true>(t, block, lane, kAdamBlock);
-                b.template update<true>(t, block, lane, kAdamBlock, r);
-            }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+    } else {
+        for (; block < end; block += kAdamWarps) {
+            b.template load<true>(t, block, lane, kAdamBlock);
+            b.template update<true>(t, block, lane, kAdamBlock, r);
         }
-        // the warp whose turn it is takes the ragged end
-        const long long past = (long long)(chunk - t.first + 1) * (kAdamWarps * a.s.per_warp);
-        if (block == whole && block < past && t.n > whole * kAdamBlock) {
-            const int left = (int)(t.n - whole * kAdamBlock);
-            b.template load<false>(t, block, lane, left);
-            b.template update<false>(t, block, lane, left, r);
-        }
+    }
+    // the warp whose turn it is takes the ragged end
+    const long long past = (long long)(chunk - t.first + 1) * (kAdamWarps * a.s.per_warp);
+    if (block == whole && block < past && t.n > whole * kAdamBlock) {
+        const int left = (int)(t.n - whole * kAdamBlock);
+        b.template load<false>(t, block, lane, left);
+        b.template update<false>(t, block, lane, left, r);
     }
 }
 
@@ -391,15 +531,17 @@ static r3_status launch_adamw(const AdamScalars& s, const r3_adamw_tensor* ts, i
     AdamTable<CAP> a;
     a.s = s;
     for (int done = 0; done < count;) {
-        // Blocks per warp and chunk: as many as leave the resident warps four chunks each, so that a
-        // long run of blocks hides its loads and a short list still spreads over the GPU.
+        // A CTA takes one chunk (CTAs that walk over chunks left SMs idle for 16% of the time, since not
+        // all of them see the memory at the same speed).  Blocks per warp and chunk: as many as leave
+        // the resident warps four chunks each, so that a short list still spreads over the GPU.
         long long blocks = 0;
         for (int i = done, k = 0; i < count && k < CAP; ++i) {
             blocks += (ts[i].n + kAdamBlock - 1) / kAdamBlock;
             k += ts[i].n > 0;
         }
-        const long long share = blocks / (4LL * kAdamWarps * kAdamCtas * sm_count());
-        const int per_warp = share < 1 ? 1 : share > kAdamMaxPerWarp ? kAdamMaxPerWarp : (int)share;
+        const long long share = blocks / (4LL * kAdamWarps * (BITS8 ? kAdamCtas8 : kAdamCtas) * sm_count());
+        const long long most = BITS8 ? kAdamMaxPerWarp8 : kAdamMaxPerWarp;
+        const int per_warp = (int)(share < 1 ? 1 : share > most ? most : share);
         const long long chunk = (long long)kAdamBlock * kAdamWarps * per_warp;
         long long chunks = 0;
         int k = 0;
@@ -419,10 +561,19 @@ static r3_status launch_adamw(const AdamScalars& s, const r3_adamw_tensor* ts, i
         if (k == 0) break;
         a.s.tensors = k;
         a.s.per_warp = per_warp;
-        a.s.chunks = (unsigned)chunks;
-        const long long most = (long long)kAdamCtas * sm_count();
+        size_t smem = 0;
+        if constexpr (BITS8) {
+            smem = sizeof(typename AdamBlock<P, G, MASTER, BITS8>::Stage) * kAdamStages * kAdamWarps;
+            static PerDevice ready;
+            if (!ready.done()) {
+                if (cudaFuncSetAttribute(adamw_kernel<P, G, MASTER, BITS8, CAP>,
+                                         cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+                    return R3_ERR_CUDA;
+                ready.mark();
+            }
+        }
         adamw_kernel<P, G, MASTER, BITS8, CAP>
-            <<<(unsigned)(chunks < most ? chunks : most), kAdamThreads, 0, cs>>>(a);
+            <<<(unsigned)chunks, kAdamThreads, smem, cs>>>(a);
         const r3_status st = launch_status();
         if (st != R3_OK) return st;
     }
@@ -466,6 +617,7 @@ extern "C" r3_status r3_adamw_step(const r3_adamw* config, const r3_adamw_tensor
     s.lr = (float)config->lr;
     s.bias1 = (float)(1.0 / (1.0 - std::pow(config->beta1, (double)config->step)));
     s.bias2 = (float)(1.0 / std::sqrt(1.0 - std::pow(config->beta2, (double)config->step)));
+    s.one = 1.f;
     s.grad_scale = grad_scale;
     s.dynamic = scalars;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);

@@ -152,7 +152,9 @@ def test_fresh_states_and_several_steps(r3, bits):
 
 
 def test_8_bit_states_are_a_function_of_the_inputs(r3):
-    """The stored codes equal those of the same operations, each rounded to float32 (on the CPU)."""
+    """The stored codes equal those of the same operations, each rounded to float32 (on the CPU).  A root's
+    code may be the neighbouring one where the root is within 2^-22 of the middle between two codes (the
+    kernel's root is an approximation): none of these inputs is."""
     n = 256 * 400
     opt = make(r3, [n], F32, F32, False, 8, seed=3)
     g = opt.grads[0].cpu().numpy()

@@ -224,9 +224,14 @@ def _ptr(t, host: bool = False):
     return ctypes.c_void_p(t.data_ptr())
 
 
+# the current stream's handle without a Stream object around it (4 us less per call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                      lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _stream(stream=None):
     if stream is None:
-        stream = torch.cuda.current_stream()
+        return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
     return ctypes.c_void_p(stream.cuda_stream)
 
 
@@ -565,6 +570,18 @@ def _expect(name: str, t, shape, dtype, device) -> None:
         raise ValueError(f"{name}: on {t.device}, expected {device}")
 
 
+def _arg(name: str, t, shape, dtype, device):
+    """The address of a contiguous tensor of the documented kind (None passes)."""
+    if t is None:
+        return None
+    if type(t) not in (torch.Tensor, torch.nn.Parameter) or t.dtype != dtype or t.shape != shape \
+            or t.device != device:
+        _expect(name, t, shape, dtype, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: tensor must be contiguous")
+    return t.data_ptr()
+
+
 def _device_of(name: str, t) -> torch.device:
     """The device of a call's first tensor, which has to be the current one: kernels are enqueued
     on the current device's stream."""
@@ -578,26 +595,33 @@ def _device_of(name: str, t) -> torch.device:
 
 
 def _norm_shape(rows, d, act, w_post, gate, w_pre, eps, residual_scale, branch_scale, dev):
-    """The r3_norm of a call, its vectors checked: w_post, w_pre and a gate [d] share one type."""
-    if act not in _ACT:
+    """The r3_norm of a call and the addresses of w_post, gate and w_pre, which are checked: w_post,
+    w_pre and a gate [d] share one type."""
+    act_code = _ACT.get(act)
+    if act_code is None:
         raise ValueError(f"activations: dtype {act}, expected float32 or bfloat16")
-    kind = R3_GATE_NONE
+    kind, like = R3_GATE_NONE, w_post if w_post is not None else w_pre
     if gate is not None:
-        kinds = {(d,): R3_GATE_CHANNEL, (rows, 1): R3_GATE_TOKEN, (rows, d): R3_GATE_FULL}
-        kind = kinds.get(tuple(gate.shape))
-        if kind is None:
+        if gate.shape == (d,):
+            kind = R3_GATE_CHANNEL
+            like = like if like is not None else gate
+        elif gate.shape == (rows, 1):
+            kind = R3_GATE_TOKEN
+        elif gate.shape == (rows, d):
+            kind = R3_GATE_FULL
+        else:
             raise ValueError(f"gate: shape {tuple(gate.shape)}, expected [{d}], [{rows}, 1] or "
                              f"[{rows}, {d}]")
-    vectors = [v for v in (w_post, w_pre, gate if kind == R3_GATE_CHANNEL else None) if v is not None]
-    w_dtype = vectors[0].dtype if vectors else act
-    if w_dtype not in _ACT:
+    w_dtype = like.dtype if like is not None else act
+    w_code = _ACT.get(w_dtype)
+    if w_code is None:
         raise ValueError(f"weights: dtype {w_dtype}, expected float32 or bfloat16")
-    for name, v in (("w_post", w_post), ("w_pre", w_pre)):
-        _expect(name, v, (d,), w_dtype, dev)
+    post = _arg("w_post", w_post, (d,), w_dtype, dev)
+    pre = _arg("w_pre", w_pre, (d,), w_dtype, dev)
     if gate is not None:
-        want = {R3_GATE_CHANNEL: w_dtype, R3_GATE_TOKEN: torch.float32, R3_GATE_FULL: act}[kind]
-        _expect("gate", gate, gate.shape, want, dev)
-    return Norm(rows, d, _ACT[act], _ACT[w_dtype], kind, eps, residual_scale, branch_scale)
+        want = w_dtype if kind == R3_GATE_CHANNEL else torch.float32 if kind == R3_GATE_TOKEN else act
+        gate = _arg("gate", gate, gate.shape, want, dev)
+    return Norm(rows, d, act_code, w_code, kind, eps, residual_scale, branch_scale), post, gate, pre
 
 
 def norm_residual(x, y=None, *, w_post=None, gate=None, w_pre=None, eps=1e-6, residual_scale=1.0,
@@ -608,16 +632,18 @@ def norm_residual(x, y=None, *, w_post=None, gate=None, w_pre=None, eps=1e-6, re
     branch is not normalised; without w_pre there is no h.  Returns (x_out, h), None for what there
     is not.  x_out may be x, h may be y (in place)."""
     dev = _device_of("x", x)
-    rows, d = x.shape
-    s = _norm_shape(rows, d, x.dtype, w_post, gate, w_pre, eps, residual_scale, branch_scale, dev)
+    shape, act = x.shape, x.dtype
+    rows, d = shape
+    s, post, gate, pre = _norm_shape(rows, d, act, w_post, gate, w_pre, eps, residual_scale,
+                                     branch_scale, dev)
+    src = _arg("x", x, shape, act, dev)
     if y is not None and x_out is None:
         x_out = torch.empty_like(x)
     if w_pre is not None and h is None:
         h = torch.empty_like(x)
-    for name, t in (("y", y), ("x_out", x_out), ("h", h)):
-        _expect(name, t, (rows, d), x.dtype, dev)
-    _check(lib.r3_norm_residual(ctypes.byref(s), _ptr(x), _ptr(y), _ptr(w_post), _ptr(gate),
-                                _ptr(w_pre), _ptr(x_out), _ptr(h), _stream(stream)))
+    _check(lib.r3_norm_residual(ctypes.byref(s), src, _arg("y", y, shape, act, dev), post, gate, pre,
+                                _arg("x_out", x_out, shape, act, dev),
+                                _arg("h", h, shape, act, dev), _stream(stream)))
     return x_out, h
 
 
@@ -628,26 +654,28 @@ def norm_residual_bwd(x_out, y, dx_out, dh=None, *, w_post=None, gate=None, w_pr
     are float32.  x_out and y are the forward's (x_out may be None without w_pre)."""
     like = x_out if x_out is not None else dx_out
     dev = _device_of("x_out", like)
-    rows, d = like.shape
-    s = _norm_shape(rows, d, like.dtype, w_post, gate, w_pre, eps, residual_scale, branch_scale, dev)
+    shape, act = like.shape, like.dtype
+    rows, d = shape
+    s, post, gate_at, pre = _norm_shape(rows, d, act, w_post, gate, w_pre, eps, residual_scale,
+                                        branch_scale, dev)
+    src = [_arg(name, t, shape, act, dev) for name, t in
+           (("x_out", x_out), ("y", y), ("dx_out", dx_out), ("dh", dh))]
     if dx is None:
         dx = torch.empty_like(like)
     if y is not None and dy is None:
         dy = torch.empty_like(like)
-    for name, t in (("x_out", x_out), ("y", y), ("dx_out", dx_out), ("dh", dh), ("dx", dx), ("dy", dy)):
-        _expect(name, t, (rows, d), like.dtype, dev)
     dgate = None
     if gate is not None:
         full = s.gate_kind == R3_GATE_FULL
-        dgate = torch.empty(gate.shape, dtype=like.dtype if full else torch.float32, device=dev)
+        dgate = torch.empty(gate.shape, dtype=act if full else torch.float32, device=dev)
     dw_post, dw_pre = (torch.empty(d, dtype=torch.float32, device=dev) if w is not None else None
                        for w in (w_post, w_pre))
     if ws is None:
         ws = workspace(lib.r3_norm_residual_bwd_workspace_bytes(ctypes.byref(s)), dev)
-    _check(lib.r3_norm_residual_bwd(ctypes.byref(s), _ptr(x_out), _ptr(y), _ptr(w_post), _ptr(gate),
-                                    _ptr(w_pre), _ptr(dx_out), _ptr(dh), _ptr(dx), _ptr(dy),
-                                    _ptr(dw_post), _ptr(dgate), _ptr(dw_pre), _ptr(ws), ws.numel(),
-                                    _stream(stream)))
+    _check(lib.r3_norm_residual_bwd(ctypes.byref(s), src[0], src[1], post, gate_at, pre, src[2],
+                                    src[3], _arg("dx", dx, shape, act, dev),
+                                    _arg("dy", dy, shape, act, dev), _ptr(dw_post), _ptr(dgate),
+                                    _ptr(dw_pre), _ptr(ws), ws.numel(), _stream(stream)))
     return dx, dy, dw_post, dgate, dw_pre
 
 
@@ -748,11 +776,11 @@ class AdamW:
         values of self.scalars(), used instead of step and lr (for a captured step)."""
         if self._dev.index != torch.cuda.current_device():
             raise ValueError(f"AdamW: tensors on {self._dev}, which is not the current device")
-        _expect("grad_scale", grad_scale, (1,), torch.float32, self._dev)
-        _expect("scalars", scalars, (3,), torch.float32, self._dev)
         self._config.step, self._config.lr = int(step), float(lr)
         _check(lib.r3_adamw_step(ctypes.byref(self._config), self._table, len(self.params),
-                                 _ptr(grad_scale), _ptr(scalars), _stream(stream)))
+                                 _arg("grad_scale", grad_scale, (1,), torch.float32, self._dev),
+                                 _arg("scalars", scalars, (3,), torch.float32, self._dev),
+                                 _stream(stream)))
 
 
 def _rows(name: str, t):
@@ -762,7 +790,7 @@ def _rows(name: str, t):
     ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
     if ld < t.shape[1]:
         raise ValueError(f"{name}: rows overlap")
-    return ctypes.c_void_p(t.data_ptr()), ld
+    return t.data_ptr(), ld
 
 
 def _logits_shape(logits, token_ids, temperature):
@@ -771,9 +799,11 @@ def _logits_shape(logits, token_ids, temperature):
         raise ValueError(f"logits: dtype {logits.dtype}, expected float32 or bfloat16")
     ptr, ld = _rows("logits", logits)
     T, V = logits.shape
-    _expect("token_ids", token_ids, (T,), (torch.int32, torch.int64), dev)
-    id_bytes = token_ids.element_size() if token_ids is not None else 4
-    return Logits(T, V, ld, _ACT[logits.dtype], id_bytes, float(temperature)), ptr, dev
+    ids, id_bytes = None, 4
+    if token_ids is not None:
+        id_bytes = 4 if token_ids.dtype == torch.int32 else 8
+        ids = _arg("token_ids", token_ids, (T,), torch.int32 if id_bytes == 4 else torch.int64, dev)
+    return Logits(T, V, ld, _ACT[logits.dtype], id_bytes, float(temperature)), ptr, ids, dev
 
 
 def token_logprobs(logits, token_ids=None, *, temperature=1.0, n_top=0, want_entropy=False,
@@ -782,19 +812,20 @@ def token_logprobs(logits, token_ids=None, *, temperature=1.0, n_top=0, want_ent
     rows may lie apart).  Returns (logp [T] or None without token_ids, entropy [T] or None,
     stats [T, 2] or None, top_ids [T, n_top] int32 or None, top_logp [T, n_top] or None).  A row
     with a negative token id is skipped: zeros, top_ids -1."""
-    s, ptr, dev = _logits_shape(logits, token_ids, temperature)
-    f32 = dict(dtype=torch.float32, device=dev)
-    logp = torch.empty(s.T, **f32) if token_ids is not None else None
-    entropy = torch.empty(s.T, **f32) if want_entropy else None
-    stats = torch.empty((s.T, 2), **f32) if want_stats else None
-    n_top = int(n_top)
+    s, ptr, ids, dev = _logits_shape(logits, token_ids, temperature)
+    f32, T, n_top = torch.float32, s.T, int(n_top)
+    logp = logits.new_empty((T,), dtype=f32) if token_ids is not None else None
+    entropy = logits.new_empty((T,), dtype=f32) if want_entropy else None
+    stats = logits.new_empty((T, 2), dtype=f32) if want_stats else None
     top_ids = top_logp = None
     if n_top > 0:
-        top_ids = torch.empty((s.T, n_top), dtype=torch.int32, device=dev)
-        top_logp = torch.empty((s.T, n_top), **f32)
-    _check(lib.r3_token_logprobs(ctypes.byref(s), ptr, _ptr(token_ids), _ptr(logp), _ptr(entropy),
-                                 _ptr(stats), n_top, _ptr(top_ids), _ptr(top_logp),
-                                 _ptr(dev_status), _stream(stream)))
+        top_ids = logits.new_empty((T, n_top), dtype=torch.int32)
+        top_logp = logits.new_empty((T, n_top), dtype=f32)
+
+    def at(t):
+        return None if t is None else t.data_ptr()
+    _check(lib.r3_token_logprobs(ctypes.byref(s), ptr, ids, at(logp), at(entropy), at(stats), n_top,
+                                 at(top_ids), at(top_logp), _ptr(dev_status), _stream(stream)))
     return logp, entropy, stats, top_ids, top_logp
 
 
@@ -803,18 +834,17 @@ def token_logprobs_bwd(logits, token_ids, stats, dlogp, *, entropy=None, dentrop
     """Gradient to the logits from dlogp [T] (or None) and, with the forward's entropy [T], from
     dentropy [T].  stats [T, 2] and temperature as in the forward.  dlogits may be given (the logits
     themselves, for a gradient in place)."""
-    s, ptr, dev = _logits_shape(logits, token_ids, temperature)
+    s, ptr, ids, dev = _logits_shape(logits, token_ids, temperature)
     if dlogits is None:
-        dlogits = torch.empty((s.T, s.V), dtype=logits.dtype, device=dev)
+        dlogits = logits.new_empty((s.T, s.V))
     else:
         _expect("dlogits", dlogits, (s.T, s.V), logits.dtype, dev)
     out, ld_out = _rows("dlogits", dlogits)
-    _expect("stats", stats, (s.T, 2), torch.float32, dev)
-    for name, t in (("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy)):
-        _expect(name, t, (s.T,), torch.float32, dev)
-    _check(lib.r3_token_logprobs_bwd(ctypes.byref(s), ptr, _ptr(token_ids), _ptr(stats),
-                                     _ptr(entropy), _ptr(dlogp), _ptr(dentropy), out, ld_out,
-                                     _ptr(dev_status), _stream(stream)))
+    stats = _arg("stats", stats, (s.T, 2), torch.float32, dev)
+    entropy, dlogp, dentropy = (_arg(name, t, (s.T,), torch.float32, dev) for name, t in
+                                (("entropy", entropy), ("dlogp", dlogp), ("dentropy", dentropy)))
+    _check(lib.r3_token_logprobs_bwd(ctypes.byref(s), ptr, ids, stats, entropy, dlogp, dentropy, out,
+                                     ld_out, _ptr(dev_status), _stream(stream)))
     return dlogits
 
 

@@ -19,9 +19,9 @@
 
 namespace r3 {
 
-// CTAs of a given size per SM (64 to 85 registers a thread)
+// CTAs of a given size per SM (64 to 80 registers a thread)
 __host__ __device__ constexpr int logprob_ctas(int threads) {
-    return threads == 512 ? 2 : threads == 128 ? 8 : 24;
+    return threads == 256 ? 4 : threads == 128 ? 8 : 24;
 }
 constexpr int kMaxTop = 32;            // alternatives per row
 constexpr int kMaxSplit = 8;           // CTAs per row
@@ -187,6 +187,7 @@ logprob_kernel(const LogprobArgs a) {
     __shared__ Key s_list[kMaxTop];
     __shared__ unsigned short s_sel[TOP ? NT : 1];
     __shared__ int s_nsel, s_ncand;
+    __shared__ Key s_bound;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int row = blockIdx.x / a.split, rank = blockIdx.x - row * a.split;
 
@@ -333,15 +334,22 @@ logprob_kernel(const LogprobArgs a) {
     // more than n keys; each one's rank is the number of larger ones.
     Key list = 0;
     if (TOP) {
-        Key g = s_keys[0][lane];
+        if (warp == 0) {                                // alone: all warps at it cost more than the barrier
+            Key g = s_keys[0][lane];
 #pragma unroll
-        for (int w = 1; w < W; ++w) g = s_keys[w][lane] > g ? s_keys[w][lane] : g;
-        int larger = 0;
+            for (int w = 1; w < W; ++w) g = s_keys[w][lane] > g ? s_keys[w][lane] : g;
+            s_keys[0][lane] = g;
+            __syncwarp();
+            int larger = 0;
 #pragma unroll
-        for (int k = 0; k < 32; ++k) larger += __shfl_sync(0xffffffffu, g, k) > g ? 1 : 0;
-        const unsigned nth = __ballot_sync(0xffffffffu, larger == a.n_top - 1);
-        // none: fewer than n threads have pieces, and everything is a candidate
-        const Key bound = nth ? __shfl_sync(0xffffffffu, g, __ffs(nth) - 1) : 0;
+            for (int k = 0; k < 32; ++k) larger += s_keys[0][k] > g ? 1 : 0;
+            const unsigned nth = __ballot_sync(0xffffffffu, larger == a.n_top - 1);
+            // none: fewer than n threads have pieces, and everything is a candidate
+            const Key n_th = __shfl_sync(0xffffffffu, g, nth ? __ffs(nth) - 1 : 0);
+            if (lane == 0) s_bound = nth ? n_th : 0;
+        }
+        __syncthreads();
+        const Key bound = s_bound;
         if (best_vec >= 0 && make_key(vec_top, first) >= bound) s_sel[atomicAdd(&s_nsel, 1)] = tid;
         __syncthreads();
         const Vec16<T>* px = reinterpret_cast<const Vec16<T>*>(pv);
@@ -352,13 +360,23 @@ logprob_kernel(const LogprobArgs a) {
             const int at = atomicAdd(&s_ncand, 1);
             if (at < kMaxCandidates) s_cand[at] = k;
         };
-        for (int q = tid; q < total; q += NT) {
-            const int s = q / per, vec = v0 + s_sel[s] + (q - s * per) * NT;
-            if (vec >= v1) continue;
-            float x[N];
-            px[vec].unpack(x);
+        for (int q0 = tid; q0 < total; q0 += 4 * NT) {
+            Vec16<T> piece[4];
+            int at[4];
 #pragma unroll
-            for (int i = 0; i < N; ++i) offer(x[i], rs.head + vec * N + i);
+            for (int u = 0; u < 4; ++u) {               // four loads on their way at once
+                const int q = q0 + u * NT, s = q / per;
+                at[u] = q < total ? v0 + s_sel[s] + (q - s * per) * NT : v1;
+                if (at[u] < v1) piece[u] = px[at[u]];
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (at[u] >= v1) continue;
+                float x[N];
+                piece[u].unpack(x);
+#pragma unroll
+                for (int i = 0; i < N; ++i) offer(x[i], rs.head + at[u] * N + i);
+            }
         }
         if (has_head && tid < rs.head) offer(to_f32(p[tid]), tid);
         if (has_tail && tid < rs.tail) offer(to_f32(p[tail0 + tid]), tail0 + tid);
@@ -368,6 +386,7 @@ logprob_kernel(const LogprobArgs a) {
             for (int i = tid; i < found; i += NT) {
                 const Key k = s_cand[i];
                 int above = 0;
+#pragma unroll 8
                 for (int q = 0; q < found; ++q) above += s_cand[q] > k ? 1 : 0;
                 if (above < kMaxTop) s_list[above] = k;
             }
@@ -429,18 +448,19 @@ logprob_kernel(const LogprobArgs a) {
                 const float v = lane == 0 ? top : lane == 1 ? S : U;
                 asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
             }
-            if (TOP) {
-                const uint32_t at = tc::mapa_shared(tc::smem_u32(&s_gather[TOP ? rank * kMaxTop + lane : 0]), 0);
+            if (TOP && lane < a.n_top) {
+                const uint32_t at = tc::mapa_shared(tc::smem_u32(&s_gather[TOP ? rank * a.n_top + lane : 0]), 0);
                 asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at), "l"(list) : "memory");
             }
         }
         tc::cluster_sync_all();
         if (rank != 0) return;                          // nobody reads this CTA's memory
         if (TOP) {
-            const int found = a.split * kMaxTop;        // zeros where a share has fewer keys
+            const int found = a.split * a.n_top;        // zeros where a share has fewer keys
             for (int i = tid; i < found; i += NT) {
                 const Key k = s_gather[i];
                 int above = 0;
+#pragma unroll 8
                 for (int q = 0; q < found; ++q) above += s_gather[q] > k ? 1 : 0;
                 if (k != 0 && above < kMaxTop) s_list[above] = k;
             }
@@ -702,9 +722,12 @@ extern "C" r3_status r3_token_logprobs(const r3_logits* shape, const void* logit
     a.dev_status = dev_status;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     const long long row_bytes = (long long)shape->V * (long long)es;
-    // A row of up to 4 KB is taken by one warp, one of up to 16 KB by four: with more the reductions at
-    // its end would cost more than its loads.
-    const int threads = row_bytes <= 4096 ? 32 : row_bytes <= 16384 ? 128 : 512;
+    // Threads per row: with more than its pieces keep busy the reductions at a row's end cost more than
+    // its loads, and many small CTAs on an SM end at different times, which keeps the loads flowing
+    // (8192 rows of bf16: 6000 columns 34.7 us at 128 threads, 26.6 at 32; 12000 columns 61.4 at 256,
+    // 45.1 at 128; 151936 columns 381 at 512, 352 at 256.  880 rows of 151936 with 20 alternatives: 72 at
+    // 256, 98 at 128).
+    const int threads = row_bytes <= 16384 ? 32 : row_bytes <= 49152 ? 128 : 256;
     // Few rows: a cluster of CTAs shares one, as long as they all run at once and a thread has two
     // pieces or more.
     a.split = 1;
@@ -715,7 +738,7 @@ extern "C" r3_status r3_token_logprobs(const r3_logits* shape, const void* logit
         using T = decltype(type);
         return threads == 32    ? r3::dispatch_logprob<T, 32>(a, cs)
                : threads == 128 ? r3::dispatch_logprob<T, 128>(a, cs)
-                                : r3::dispatch_logprob<T, 512>(a, cs);
+                                : r3::dispatch_logprob<T, 256>(a, cs);
     };
     return shape->dtype == R3_BF16 ? launch(__nv_bfloat16()) : launch(float());
 }

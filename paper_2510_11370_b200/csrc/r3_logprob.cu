@@ -116,6 +116,27 @@ template <typename T> __device__ __forceinline__ RowSplit split_row(const T* p, 
     return r;
 }
 
+// Two float32 values in a register pair, one instruction for both: the sums of a thread run in two lanes.
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 pair(float lo, float hi) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void split(F2 v, float& lo, float& hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 // A 16-byte piece of a row in the form the sums take: its largest value, and its values two by two.
 // With FINITE every value is raised to at least -2^100 (c x stays finite: a term 0 times its exponent
 // is 0, not NaN); a NaN stays one.
@@ -132,6 +153,18 @@ template <> struct Piece<__nv_bfloat16> {
         const float2 m = bf16_pair(a);
         return fmaxf(m.x, m.y);
     }
+    // the largest value of four pieces
+    static __device__ __forceinline__ float largest(const Piece (&x)[4]) {
+        uint32_t m = x[0].v.x;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const uint32_t w[4] = {x[u].v.x, x[u].v.y, x[u].v.z, x[u].v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) asm("max.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(m), "r"(w[i]));
+        }
+        const float2 f = bf16_pair(m);
+        return fmaxf(f.x, f.y);
+    }
     template <bool FINITE> __device__ __forceinline__ float2 get(int i) const {
         uint32_t w = i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
         if (FINITE)                                     // 0xf180: -2^100
@@ -146,6 +179,9 @@ template <> struct Piece<float> {
         v.x = v.y = v.z = v.w = -CUDART_INF_F;
     }
     __device__ __forceinline__ float largest() const { return fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)); }
+    static __device__ __forceinline__ float largest(const Piece (&x)[4]) {
+        return fmaxf(fmaxf(x[0].largest(), x[1].largest()), fmaxf(x[2].largest(), x[3].largest()));
+    }
     template <bool FINITE> __device__ __forceinline__ float2 get(int i) const {
         const float a = i ? v.z : v.x, b = i ? v.w : v.y;
         return FINITE ? make_float2(max_nan(a, -1.2676506e30f), max_nan(b, -1.2676506e30f))
@@ -154,19 +190,25 @@ template <> struct Piece<float> {
 };
 
 struct RowSums {
-    float M, top, S, U;
+    float M, top;
+    F2 S, U;
 };
 // Moves the reference up to hold a value of c x = t.
 __device__ __forceinline__ void move_ref(RowSums& a, float t) {
     const float m = rintf(t), d = a.M - m, f = ex2(d);
-    a.U = f * (a.U + d * a.S);
-    a.S *= f;
+    float s0, s1, u0, u1;
+    split(a.S, s0, s1);
+    split(a.U, u0, u1);
+    a.U = pair(f * (u0 + d * s0), f * (u1 + d * s1));
+    a.S = pair(f * s0, f * s1);
     a.M = m;
 }
-template <bool ENT> __device__ __forceinline__ void add_term(RowSums& a, float u) {
-    const float e = ex2(u);
-    a.S += e;
-    if (ENT) a.U = fmaf(e, u, a.U);
+template <bool ENT> __device__ __forceinline__ void add_terms(RowSums& a, F2 u) {
+    float lo, hi;
+    split(u, lo, hi);
+    const F2 e = pair(ex2(lo), ex2(hi));
+    a.S = add2(a.S, e);
+    if (ENT) a.U = fma2(e, u, a.U);
 }
 
 // What the CTAs of one row leave in the first of them.
@@ -217,51 +259,70 @@ logprob_kernel(const LogprobArgs a) {
     const int v0 = min(rs.vecs, rank * per_cta), v1 = min(rs.vecs, v0 + per_cta);
     const float c = a.c;
 
-    RowSums r = {kLowRef, -CUDART_INF_F, 0.f, 0.f};
+    RowSums r = {kLowRef, -CUDART_INF_F, 0, 0};
     int best_vec = v0 + tid < v1 ? v0 + tid : -1;       // the first piece that holds the top so far
-    // UNROLL pieces per thread and round; the next round's are on their way while these are summed.
-    // Pieces behind the end read as -inf: they change neither the top nor the sums.
+    // UNROLL pieces per thread and round; the next round's are on their way while these are summed.  In
+    // the last, ragged round the pieces behind the end read as -inf: they change neither the top nor the
+    // sums, and a warp skips those that all of its lanes lack.
+    const int rounds = (v1 - v0) / (UNROLL * NT);
     Piece<T> b[UNROLL];
     auto fetch = [&](int j) {
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) b[u] = pv[j + u * NT];
+    };
+    auto fetch_last = [&](int j) {
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             if (j + u * NT < v1) b[u] = pv[j + u * NT];
             else b[u].fill();
         }
     };
-    fetch(v0 + tid);
-    for (int j = v0 + tid; j - tid < v1; j += UNROLL * NT) {
-        Piece<T> x[UNROLL];
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) x[u] = b[u];
-        if (j - tid + UNROLL * NT < v1) fetch(j + UNROLL * NT);
+    auto sum = [&](const Piece<T>(&x)[UNROLL], int j, bool last) {
         float m = -CUDART_INF_F;
+        if (TOP) {
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const float q = x[u].largest();
-            if (TOP && q > fmaxf(r.top, m)) best_vec = j + u * NT;
-            m = fmaxf(m, q);
+            for (int u = 0; u < UNROLL; ++u) {
+                const float q = x[u].largest();
+                if (q > fmaxf(r.top, m)) best_vec = j + u * NT;
+                m = fmaxf(m, q);
+            }
+        } else {
+            m = Piece<T>::largest(x);
         }
         r.top = fmaxf(r.top, m);
         if (m * c - r.M > kMoveRef) move_ref(r, m * c);
+        const F2 c2 = pair(c, c), ref = pair(-r.M, -r.M);
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            if (j - lane + u * NT >= v1) break;         // the whole warp is behind the end
+            if (last && j - lane + u * NT >= v1) break;
 #pragma unroll
             for (int i = 0; i < Piece<T>::PAIRS; ++i) {
                 const float2 f = x[u].template get<ENT>(i);
-                add_term<ENT>(r, fmaf(f.x, c, -r.M));
-                add_term<ENT>(r, fmaf(f.y, c, -r.M));
+                add_terms<ENT>(r, fma2(pair(f.x, f.y), c2, ref));
             }
         }
+    };
+    int j = v0 + tid;
+    if (rounds > 0) fetch(j);
+    else fetch_last(j);
+    for (int k = 0; k < rounds; ++k) {
+        Piece<T> x[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) x[u] = b[u];
+        if (k + 1 < rounds) fetch(j + UNROLL * NT);
+        else fetch_last(j + UNROLL * NT);
+        sum(x, j, false);
+        j += UNROLL * NT;
     }
+    if (j - tid < v1) sum(b, j, true);
     // the single elements in front of the first and behind the last whole piece
     const bool has_head = rank == 0, has_tail = rank == a.split - 1;
     const int tail0 = rs.head + rs.vecs * N;
     auto take_one = [&](float x) {
         r.top = fmaxf(r.top, x);
         if (x * c - r.M > kMoveRef) move_ref(r, x * c);
-        add_term<ENT>(r, fmaf(max_nan(x, -1.2676506e30f), c, -r.M));
+        // a term 0 beside it (2^-3e38 and 0 times that)
+        add_terms<ENT>(r, pair(fmaf(max_nan(x, -1.2676506e30f), c, -r.M), -3e38f));
     };
     const float vec_top = r.top;                        // of the whole pieces alone
     if (has_head && tid < rs.head) take_one(to_f32(p[tid]));
@@ -290,7 +351,14 @@ logprob_kernel(const LogprobArgs a) {
         m = fmaxf(m, s_red[w][0]);
         top = fmaxf(top, s_red[w][1]);
     }
-    float tS = r.S, tU = r.U;
+    float tS, tU;                                       // this thread's sums
+    {
+        float s0, s1, u0, u1;
+        split(r.S, s0, s1);
+        split(r.U, u0, u1);
+        tS = s0 + s1;
+        tU = u0 + u1;
+    }
     // A top whose c x is beyond 2^20 (masks of the type's lowest value in a whole row, say) leaves
     // the reference no room: the share is summed again with the differences to the known top.
     const bool again = fabsf(top * c) > kPlainTop && fabsf(top) < CUDART_INF_F;

@@ -587,6 +587,51 @@ typedef struct {
 r3_status r3_adamw_step(const r3_adamw* config, const r3_adamw_tensor* tensors, int32_t n_tensors,
                         const float* grad_scale, const float* scalars, void* stream);
 
+/* ---- stacks of replayed blocks with norms around every block (an extension) ----------------------- */
+
+/* The norms of L blocks, stacked on a leading layer axis, all of w_dtype and 16-byte aligned:
+ *   h_l     = RMSNorm(x_l) w_pre[l]
+ *   x_{l+1} = residual_scale x_l + branch_scale gate[l] RMSNorm(y_replay,l(h_l)) w_post[l]
+ * w_pre [L,d]; w_post [L,d] or NULL (the block's output is not normalised); gate [L,d] or NULL.
+ * dw_pre, dw_post, dgate [L,d] float32: their gradients, overwritten by r3_normed_stack_train, given
+ * exactly where their vector is.  The struct lives in HOST memory. */
+typedef struct {
+    const void *w_pre, *w_post, *gate;
+    float *dw_pre, *dw_post, *dgate;
+    int32_t w_dtype;
+    float eps, residual_scale, branch_scale;
+} r3_block_norms;
+
+/* The stack forward: x0 [T,d] -> x_out [T,d] = x_L.  Between two blocks runs one r3_norm_residual; a
+ * block's router and experts read h_l.  Layers as in r3_replay_stack.  workspace:
+ * r3_normed_stack_workspace_bytes(shape). */
+size_t r3_normed_stack_workspace_bytes(const r3_shape* shape);
+r3_status r3_normed_stack(const r3_shape* shape, int32_t L, const r3_block_norms* norms,
+                          const void* x0, const void* w_router, const void* idx, const void* w_gate,
+                          const void* w_up, const void* w_down, void* x_out, void* workspace,
+                          size_t ws_bytes, int32_t* dev_status, void* stream);
+
+/* Forward and the exact backward chain of <dy, x_L>: dlogits [L,T,E], dx0 [T,d] = dL/dx_0, dw_router
+ * [L,E,d] float32, the norms' gradients, and the expert-weight gradients dw_gate / dw_up [L,E,F,d],
+ * dw_down [L,E,d,F] float32 or all three NULL.  x_out is a buffer of its own.  x_l, h_l and y_l are kept, a block's other
+ * intermediates are formed again in the backward pass.  bf16 only (R3_ERR_UNSUPPORTED for float32).
+ *
+ * With adamw (HOST) the expert weights are updated in place, each block's as soon as its gradients are
+ * there: dw_gate, dw_up [E,F,d] and dw_down [E,d,F] then hold ONE block's gradients (those of block 0
+ * at the end), so that no more than that exists at a time.  expert_states (HOST) has 3 L entries, block
+ * by block w_gate, w_up, w_down, as for r3_adamw_step; param must be the block's weights, grad is
+ * ignored.  adamw, grad_scale and scalars as for r3_adamw_step, param_dtype R3_BF16, grad_dtype R3_F32.
+ * workspace: r3_normed_stack_train_workspace_bytes(shape, L). */
+size_t r3_normed_stack_train_workspace_bytes(const r3_shape* shape, int32_t L);
+r3_status r3_normed_stack_train(const r3_shape* shape, int32_t L, const r3_block_norms* norms,
+                                const void* x0, const void* w_router, const void* idx, void* w_gate,
+                                void* w_up, void* w_down, const void* dy, void* x_out, float* dlogits,
+                                void* dx0, float* dw_router, float* dw_gate, float* dw_up,
+                                float* dw_down, const r3_adamw* adamw,
+                                const r3_adamw_tensor* expert_states, const float* grad_scale,
+                                const float* scalars, void* workspace, size_t ws_bytes,
+                                int32_t* dev_status, void* stream);
+
 /* ---- token log probabilities (the p_train and p_infer of Sections 3.1 and 3.2) -------------- */
 
 /* A batch of logits: T rows of V values, row t at logits + t * ld elements (ld >= V, so a padded or

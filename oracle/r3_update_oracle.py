@@ -165,3 +165,46 @@ def nearest_e4m3(q):
     up, down = vals[hi] - a, a - vals[lo]
     code = np.where((up < down) | ((up == down) & (hi % 2 == 0)), hi, lo)
     return np.copysign(vals[code], q)
+
+
+# ---- stacks of replayed blocks with norms around every block ----------------------------------------
+def normed_stack_bwd(x0, layers, norms, dy, eps=1e-6, residual_scale=1.0, branch_scale=1.0, store=None,
+                     expert_grads=False):
+    """h_l = RMSNorm(x_l) w_pre,l; x_{l+1} = residual_scale x_l + branch_scale gate_l RMSNorm(y_l) w_post,l
+    with y_l the replayed layer at h_l; then the gradient of <dy, x_L>.  layers[l] = (w_r, idx, w_gate,
+    w_up, w_down), norms[l] = (w_pre, w_post or None, gate or None).  store: rounding of kept rows.
+    Returns a dict of x_out, dx0 and lists ds, dw_r, dw_pre, dw_post, dgate, dw_experts."""
+    from oracle import r3_oracle as O
+    keep = store or (lambda v: v)
+    kw = dict(eps=eps, residual_scale=residual_scale, branch_scale=branch_scale)
+    L = len(layers)
+    xs, hs, ys = [np.asarray(x0, dtype=np.float64)], [], []
+    h = rms_norm(xs[0], norms[0][0], eps)
+    for l in range(L):
+        h = keep(h)
+        w_r, idx, wg, wu, wd = layers[l]
+        y = O.replay_output(h, O.router_logits(h, w_r), idx, wg, wu, wd)[0]
+        hs.append(h)
+        ys.append(keep(y))
+        w_next = norms[l + 1][0] if l + 1 < L else None
+        x, h = norm_residual(xs[l], ys[l], norms[l][1], norms[l][2], w_next, **kw)
+        xs.append(keep(x))
+    out = dict(x_out=xs[L], ds=[None] * L, dw_r=[None] * L, dw_pre=[None] * L, dw_post=[None] * L,
+               dgate=[None] * L, dw_experts=[None] * L)
+    around, dh = np.asarray(dy, dtype=np.float64), None
+    for l in range(L - 1, -1, -1):
+        w_next = norms[l + 1][0] if l + 1 < L else None
+        g = norm_residual_bwd(xs[l + 1], ys[l], around, dh, norms[l][1], norms[l][2], w_next, **kw)
+        if w_next is not None:
+            out["dw_pre"][l + 1] = g["dw_pre"]
+        out["dw_post"][l], out["dgate"][l] = g.get("dw_post"), g.get("dgate")
+        around, dyl = g["dx"], g["dy"]
+        w_r, idx, wg, wu, wd = layers[l]
+        b = O.layer_bwd_input(hs[l], w_r, idx, wg, wu, wd, dyl)
+        out["ds"][l], out["dw_r"][l] = b["ds"], b["dw_r"]
+        if expert_grads:
+            out["dw_experts"][l] = O.layer_bwd_weights(hs[l], w_r, idx, wg, wu, wd, dyl)
+        dh = b["dx"]
+    g = norm_residual_bwd(xs[0], None, around, dh, w_pre=norms[0][0], eps=eps)
+    out["dw_pre"][0], out["dx0"] = g["dw_pre"], g["dx"]
+    return out

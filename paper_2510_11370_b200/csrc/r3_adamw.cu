@@ -526,6 +526,14 @@ static r3_status check_distinct(const r3_adamw* c, const r3_adamw_tensor* ts, in
     }
 }
 
+r3_status check_adamw_call(const r3_adamw* config, const r3_adamw_tensor* tensors, int32_t n_tensors,
+                           const float* grad_scale, const float* scalars) {
+    const r3_status st = check_adamw(config, tensors, n_tensors);
+    if (st != R3_OK) return st;
+    if (!aligned(grad_scale, 4) || !aligned(scalars, 4)) return R3_ERR_INVALID_ARG;
+    return check_distinct(config, tensors, n_tensors);
+}
+
 template <typename P, typename G, bool MASTER, bool BITS8, int CAP>
 static r3_status launch_adamw(const AdamScalars& s, const r3_adamw_tensor* ts, int count, cudaStream_t cs) {
     AdamTable<CAP> a;
@@ -604,10 +612,8 @@ static r3_status launch_adamw(const r3_adamw* c, const AdamScalars& s, const r3_
 extern "C" r3_status r3_adamw_step(const r3_adamw* config, const r3_adamw_tensor* tensors,
                                    int32_t n_tensors, const float* grad_scale, const float* scalars,
                                    void* stream) {
-    r3_status st = r3::check_adamw(config, tensors, n_tensors);
+    const r3_status st = r3::check_adamw_call(config, tensors, n_tensors, grad_scale, scalars);
     if (st != R3_OK) return st;
-    if (!r3::aligned(grad_scale, 4) || !r3::aligned(scalars, 4)) return R3_ERR_INVALID_ARG;
-    if ((st = r3::check_distinct(config, tensors, n_tensors)) != R3_OK) return st;
     r3::AdamScalars s = {};
     s.beta1 = (float)config->beta1;
     s.one_beta1 = (float)(1.0 - config->beta1);

@@ -40,7 +40,8 @@ EXPORTS = [
     "r3_replay_layer_host_workspace_bytes", "r3_replay_layer_host", "r3_replay_layer_host_enqueue",
     "r3_replay_layer_host_chunks",
     "r3_replay_layer_same_record",
-    "r3_adamw_step",
+    "r3_adamw_step", "r3_normed_stack_workspace_bytes", "r3_normed_stack",
+    "r3_normed_stack_train_workspace_bytes", "r3_normed_stack_train",
     "r3_norm_residual", "r3_norm_residual_bwd_workspace_bytes", "r3_norm_residual_bwd",
     "r3_token_logprobs", "r3_token_logprobs_bwd",
     "r3_prob_discrepancy_workspace_bytes", "r3_prob_discrepancy", "r3_record_diff",
@@ -74,6 +75,13 @@ class Norm(ctypes.Structure):
                 ("w_dtype", ctypes.c_int32), ("gate_kind", ctypes.c_int32),
                 ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float),
                 ("branch_scale", ctypes.c_float)]
+
+
+class BlockNorms(ctypes.Structure):
+    _fields_ = [("w_pre", ctypes.c_void_p), ("w_post", ctypes.c_void_p), ("gate", ctypes.c_void_p),
+                ("dw_pre", ctypes.c_void_p), ("dw_post", ctypes.c_void_p), ("dgate", ctypes.c_void_p),
+                ("w_dtype", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("residual_scale", ctypes.c_float), ("branch_scale", ctypes.c_float)]
 
 
 class AdamWTensor(ctypes.Structure):
@@ -139,6 +147,14 @@ lib.r3_replay_layer.argtypes = [_SP] + [_P] * 11 + [ctypes.c_size_t, _P, _P]
 lib.r3_replay_layer_same_record.argtypes = [_SP] + [_P] * 11 + [ctypes.c_size_t, _P, _P]
 lib.r3_replay_layer_host.argtypes = [_SP] + [_P] * 10 + [ctypes.c_size_t, _P, _P]
 lib.r3_replay_layer_host_enqueue.argtypes = [_SP] + [_P] * 10 + [ctypes.c_size_t, _P, _P]
+_BN = ctypes.POINTER(BlockNorms)
+lib.r3_normed_stack_workspace_bytes.restype = ctypes.c_size_t
+lib.r3_normed_stack_workspace_bytes.argtypes = [_SP]
+lib.r3_normed_stack.argtypes = [_SP, ctypes.c_int32, _BN] + [_P] * 8 + [ctypes.c_size_t, _P, _P]
+lib.r3_normed_stack_train_workspace_bytes.restype = ctypes.c_size_t
+lib.r3_normed_stack_train_workspace_bytes.argtypes = [_SP, ctypes.c_int32]
+lib.r3_normed_stack_train.argtypes = ([_SP, ctypes.c_int32, _BN] + [_P] * 19
+                                      + [ctypes.c_size_t, _P, _P])
 lib.r3_adamw_step.argtypes = [ctypes.POINTER(AdamWConfig), _P, ctypes.c_int32, _P, _P, _P]
 _NP = ctypes.POINTER(Norm)
 lib.r3_norm_residual.argtypes = [_NP] + [_P] * 8
@@ -691,9 +707,10 @@ class AdamW:
     of float32 tensors.  States are made (zero) or given as lists: float32, or with state_bits=8
     float8_e4m3fn codes plus one float32 scale per 256 elements (exp_avg_sq then holds the root of
     the second moment).  weight_decay: a number, or one per tensor.  The handle keeps its tensors
-    alive; set_grads() exchanges the gradients."""
+    alive; set_grads() exchanges the gradients, and without any (None) the handle is one for
+    normed_stack_train, which supplies them."""
 
-    def __init__(self, params, grads, *, masters=None, exp_avg=None, exp_avg_sq=None,
+    def __init__(self, params, grads=None, *, masters=None, exp_avg=None, exp_avg_sq=None,
                  exp_avg_scale=None, exp_avg_sq_scale=None, state_bits=32, betas=(0.9, 0.95),
                  eps=1e-8, weight_decay=0.0):
         self.params = list(params)
@@ -742,7 +759,9 @@ class AdamW:
             row.n, row.weight_decay = n, wd
         self._config = AdamWConfig(_ACT[dtype], 0, int(self.masters is not None), state_bits, 1, 0.0,
                                    float(betas[0]), float(betas[1]), float(eps))
-        self.set_grads(grads)
+        self.grads = None
+        if grads is not None:
+            self.set_grads(grads)
 
     def _fill(self, field, tensors, sizes, dtype):
         if tensors is None:
@@ -781,6 +800,80 @@ class AdamW:
                                  _arg("grad_scale", grad_scale, (1,), torch.float32, self._dev),
                                  _arg("scalars", scalars, (3,), torch.float32, self._dev),
                                  _stream(stream)))
+
+
+def _block_norms(s, L, w_pre, w_post, gate, eps, residual_scale, branch_scale, dev, grads):
+    """The r3_block_norms of a call, its vectors [L, d] checked, and (grads) their gradients."""
+    if not isinstance(w_pre, torch.Tensor) or w_pre.dtype not in _ACT:
+        raise ValueError("w_pre: expected a float32 or bfloat16 tensor")
+    n = BlockNorms(w_dtype=_ACT[w_pre.dtype], eps=eps, residual_scale=residual_scale,
+                   branch_scale=branch_scale)
+    made = []
+    for name, t, grad in (("w_pre", w_pre, "dw_pre"), ("w_post", w_post, "dw_post"), ("gate", gate, "dgate")):
+        setattr(n, name, _arg(name, t, (L, s.d), w_pre.dtype, dev))
+        g = torch.empty((L, s.d), dtype=torch.float32, device=dev) if grads and t is not None else None
+        setattr(n, grad, None if g is None else g.data_ptr())
+        made.append(g)
+    return n, made
+
+
+def normed_stack(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down, *, w_pre, w_post=None,
+                 gate=None, eps=1e-6, residual_scale=1.0, branch_scale=1.0, x_out=None, ws=None,
+                 dev_status=None, stream=None):
+    """L replayed blocks with norms around them (vectors w_pre, w_post, gate [L, d]), forward:
+    x_{l+1} = residual_scale x_l + branch_scale gate_l RMSNorm(y_l(RMSNorm(x_l) w_pre_l)) w_post_l.
+    Returns x_L [T, d]."""
+    dev = _device_of("x0", x0)
+    n, _ = _block_norms(s, L, w_pre, w_post, gate, eps, residual_scale, branch_scale, dev, False)
+    if x_out is None:
+        x_out = torch.empty((s.T, s.d), dtype=_act_dtype(s), device=dev)
+    if ws is None:
+        ws = workspace(lib.r3_normed_stack_workspace_bytes(ctypes.byref(s)), dev)
+    _check(lib.r3_normed_stack(ctypes.byref(s), L, ctypes.byref(n), _ptr(x0), _ptr(w_router), _ptr(idx),
+                               _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(x_out), _ptr(ws),
+                               ws.numel(), _ptr(dev_status), _stream(stream)))
+    return x_out
+
+
+def normed_stack_train(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down, dy, *, w_pre,
+                       w_post=None, gate=None, eps=1e-6, residual_scale=1.0, branch_scale=1.0,
+                       expert_grads=False, optimiser=None, step=None, lr=None, grad_scale=None,
+                       scalars=None, ws=None, dev_status=None, stream=None):
+    """normed_stack forward and the exact backward chain of <dy, x_L>: (x_out, dlogits [L, T, E], dx0,
+    dw_router [L, E, d], dw_pre, dw_post or None, dgate or None), and with expert_grads also (dw_gate,
+    dw_up, dw_down).  With optimiser, an AdamW over [w_gate[0], w_up[0], w_down[0], w_gate[1], ..] without
+    gradients of its own, every block's expert weights take step `step` with rate `lr` as soon as their
+    gradients are there, and only one block's gradients exist at a time (block 0's are returned)."""
+    dev = _device_of("x0", x0)
+    n, dnorms = _block_norms(s, L, w_pre, w_post, gate, eps, residual_scale, branch_scale, dev, True)
+    f32 = dict(dtype=torch.float32, device=dev)
+    x_out = torch.empty((s.T, s.d), dtype=_act_dtype(s), device=dev)
+    dx0 = torch.empty((s.T, s.d), dtype=_act_dtype(s), device=dev)
+    dlogits = torch.empty((L, s.T, s.E), **f32)
+    dw_r = torch.empty((L, s.E, s.d), **f32)
+    dws, config, table = (None, None, None), None, None
+    if optimiser is not None:
+        if len(optimiser.params) != 3 * L:
+            raise ValueError(f"optimiser: {len(optimiser.params)} tensors, expected {3 * L}")
+        config = AdamWConfig.from_buffer_copy(optimiser._config)
+        config.grad_dtype, config.step, config.lr = R3_F32, int(step), float(lr)
+        table = optimiser._table
+    if expert_grads or optimiser is not None:
+        lead = () if optimiser is not None else (L,)
+        dws = (torch.empty(lead + (s.E, s.F, s.d), **f32), torch.empty(lead + (s.E, s.F, s.d), **f32),
+               torch.empty(lead + (s.E, s.d, s.F), **f32))
+    if ws is None:
+        ws = workspace(lib.r3_normed_stack_train_workspace_bytes(ctypes.byref(s), L), dev)
+    _check(lib.r3_normed_stack_train(
+        ctypes.byref(s), L, ctypes.byref(n), _ptr(x0), _ptr(w_router), _ptr(idx), _ptr(w_gate),
+        _ptr(w_up), _ptr(w_down), _ptr(dy), _ptr(x_out), _ptr(dlogits), _ptr(dx0), _ptr(dw_r),
+        _ptr(dws[0]), _ptr(dws[1]), _ptr(dws[2]), None if config is None else ctypes.addressof(config),
+        None if table is None else ctypes.addressof(table),
+        _arg("grad_scale", grad_scale, (1,), torch.float32, dev),
+        _arg("scalars", scalars, (3,), torch.float32, dev), _ptr(ws), ws.numel(), _ptr(dev_status),
+        _stream(stream)))
+    out = (x_out, dlogits, dx0, dw_r, *dnorms)
+    return out + dws if dws[0] is not None else out
 
 
 def _rows(name: str, t):

@@ -1,0 +1,102 @@
+"""What the normed-stack calls refuse on the host: nothing is launched by anything here."""
+import ctypes
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def r3():
+    from paper_2510_11370_b200 import build
+    build.build()
+    from paper_2510_11370_b200 import r3 as mod
+    return mod
+
+
+P = [ctypes.c_void_p(i << 20) for i in range(1, 24)]           # never dereferenced
+T, D, E, K, F, L = 16, 64, 4, 2, 64, 2
+
+
+def norms(r3, **kw):
+    base = dict(w_pre=1 << 30, w_post=2 << 30, gate=None, dw_pre=3 << 30, dw_post=4 << 30, dgate=None,
+                w_dtype=0, eps=1e-6, residual_scale=1.0, branch_scale=1.0)
+    base.update(kw)
+    return r3.BlockNorms(**base)
+
+
+def fwd(r3, n=None, s=None, layers=L, ws=None, size=0, drop=None):
+    s = s if s is not None else r3.make_shape(T, D, E, K, F)
+    a = [None if i == drop else P[i] for i in range(7)]
+    n = norms(r3) if n is None else n
+    return r3.lib.r3_normed_stack(ctypes.byref(s), layers, ctypes.byref(n), *a, ws, size, None, None)
+
+
+def train(r3, n=None, s=None, layers=L, adamw=None, states=None, grads=True, drop=None, ws=None, size=0):
+    s = s if s is not None else r3.make_shape(T, D, E, K, F)
+    n = norms(r3) if n is None else n
+    a = [None if i == drop else P[i] for i in range(14)]
+    if not grads:
+        a[11] = a[12] = a[13] = None
+    return r3.lib.r3_normed_stack_train(
+        ctypes.byref(s), layers, ctypes.byref(n), *a, ctypes.addressof(adamw) if adamw else None,
+        ctypes.addressof(states) if states is not None else None, None, None, ws, size, None, None)
+
+
+@pytest.mark.parametrize("kw", [dict(w_pre=None), dict(w_pre=(1 << 30) + 4), dict(w_post=8), dict(w_dtype=3),
+                                dict(eps=0.0), dict(eps=float("nan")), dict(residual_scale=float("inf")),
+                                dict(branch_scale=float("nan"))])
+def test_bad_norms(r3, kw):
+    assert fwd(r3, norms(r3, **kw)) == r3.R3_ERR_INVALID_ARG
+    assert train(r3, norms(r3, **kw)) == r3.R3_ERR_INVALID_ARG
+
+
+def test_bad_gradients_and_sizes(r3):
+    bad = r3.R3_ERR_INVALID_ARG
+    for kw in (dict(dw_pre=None), dict(dw_post=None), dict(w_post=None), dict(dgate=5 << 30), dict(gate=5 << 30)):
+        assert train(r3, norms(r3, **kw)) == bad
+    assert fwd(r3, layers=0) == bad and train(r3, layers=-1) == bad
+    wide = r3.make_shape(T, 16392, E, K, F)
+    assert fwd(r3, s=wide) == r3.R3_ERR_UNSUPPORTED and train(r3, s=wide) == r3.R3_ERR_UNSUPPORTED
+    import torch
+    assert train(r3, s=r3.make_shape(T, D, E, K, F, act=torch.float32)) == r3.R3_ERR_UNSUPPORTED
+    for i in range(7):
+        assert fwd(r3, drop=i) == bad, i
+    for i in range(14):
+        assert train(r3, drop=i) == bad, i
+    assert fwd(r3) == r3.R3_ERR_WORKSPACE and train(r3) == r3.R3_ERR_WORKSPACE
+    assert train(r3, grads=False) == r3.R3_ERR_WORKSPACE                 # legal without expert gradients
+    none = r3.make_shape(0, D, E, K, F)
+    assert fwd(r3, s=none) == r3.R3_OK and train(r3, s=none) == r3.R3_OK
+
+
+def test_bad_optimisers(r3):
+    bad = r3.R3_ERR_INVALID_ARG
+    block = E * F * D
+
+    def states(**kw):
+        rows = []
+        for l in range(L):
+            for k in range(3):
+                at = (4 + k << 20) + l * block * 2
+                row = dict(param=at, master=None, grad=None, exp_avg=(40 + 3 * l + k) << 24,
+                           exp_avg_sq=(60 + 3 * l + k) << 24, exp_avg_scale=None, exp_avg_sq_scale=None,
+                           n=block, weight_decay=0.0)
+                row.update(kw)
+                rows.append(r3.AdamWTensor(**row))
+        return (r3.AdamWTensor * len(rows))(*rows)
+
+    def config(**kw):
+        base = dict(param_dtype=1, grad_dtype=0, master=0, state_bits=32, step=1, lr=0.1, beta1=0.9, beta2=0.99,
+                    eps=1e-8)
+        base.update(kw)
+        return r3.AdamWConfig(**base)
+
+    assert train(r3, adamw=config(), states=states()) == r3.R3_ERR_WORKSPACE       # all right but the workspace
+    assert train(r3, adamw=config(), states=None) == bad
+    assert train(r3, adamw=config(), states=states(), grads=False) == bad
+    assert train(r3, adamw=config(param_dtype=0), states=states()) == bad
+    assert train(r3, adamw=config(grad_dtype=1), states=states()) == bad
+    assert train(r3, adamw=config(step=0), states=states()) == bad
+    assert train(r3, adamw=config(state_bits=8), states=states()) == bad            # no scales
+    assert train(r3, adamw=config(), states=states(n=block - 8)) == bad
+    assert train(r3, adamw=config(), states=states(param=1 << 28)) == bad           # not the block's weights
+    assert train(r3, adamw=config(), states=states(exp_avg=None)) == bad

@@ -158,3 +158,41 @@ def test_e4m3_values_and_scales():
     assert np.array_equal(U.nearest_e4m3(q), want)
     for top, scale in ((448.0, 1.0), (448.0001, 2.0), (224.0, 0.5), (1.0, 2.0 ** -8), (0.0, 2.0 ** -126)):
         assert U.block_scale(np.array([[0.0, -top]]))[0] == scale
+
+
+# ---- stacks with norms --------------------------------------------------------------------------------
+@pytest.mark.parametrize("post,gated", [(True, True), (False, False), (True, False)])
+def test_normed_stack_gradients_by_differences(post, gated):
+    rng = np.random.default_rng(9)
+    T, d, E, K, F, L = 3, 8, 4, 2, 8, 2
+    x0, dy = rng.normal(size=(T, d)), rng.normal(size=(T, d))
+    layers = [[rng.normal(size=(E, d)) * 0.5, np.argsort(rng.random((T, E)), axis=1)[:, :K],
+               rng.normal(size=(E, F, d)) * 0.5, rng.normal(size=(E, F, d)) * 0.5,
+               rng.normal(size=(E, d, F)) * 0.5] for _ in range(L)]
+    norms = [(1 + 0.3 * rng.normal(size=d), 1 + 0.3 * rng.normal(size=d) if post else None,
+              rng.normal(size=d) if gated else None) for _ in range(L)]
+    kw = dict(eps=0.05, residual_scale=0.9, branch_scale=0.6)
+
+    def loss():
+        return float((dy * U.normed_stack_bwd(x0, layers, norms, dy, **kw)["x_out"]).sum())
+
+    g = U.normed_stack_bwd(x0, layers, norms, dy, expert_grads=True, **kw)
+    assert np.abs(g["dx0"] - fd(loss, x0)).max() < 1e-7
+    for l in range(L):
+        assert np.abs(g["dw_r"][l] - fd(loss, layers[l][0])).max() < 1e-7
+        assert np.abs(g["dw_pre"][l] - fd(loss, norms[l][0])).max() < 1e-7
+        if post:
+            assert np.abs(g["dw_post"][l] - fd(loss, norms[l][1])).max() < 1e-7
+        if gated:
+            assert np.abs(g["dgate"][l] - fd(loss, norms[l][2])).max() < 1e-7
+        down = np.stack([g["dw_experts"][l][e][2] for e in range(E)])
+        assert np.abs(down - fd(loss, layers[l][4])).max() < 1e-7
+
+
+def test_normed_stack_without_blocks_output_is_the_residual_alone():
+    rng = np.random.default_rng(2)
+    x0, dy = rng.normal(size=(3, 8)), rng.normal(size=(3, 8))
+    layers = [[rng.normal(size=(4, 8)), np.argsort(rng.random((3, 4)), axis=1)[:, :2],
+               rng.normal(size=(4, 8, 8)), rng.normal(size=(4, 8, 8)), np.zeros((4, 8, 8))]] * 2
+    g = U.normed_stack_bwd(x0, layers, [(np.ones(8), None, None)] * 2, dy, residual_scale=0.5)
+    assert np.allclose(g["x_out"], 0.25 * x0) and np.allclose(g["dx0"], 0.25 * dy)

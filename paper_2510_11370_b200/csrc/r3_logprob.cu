@@ -799,7 +799,7 @@ extern "C" r3_status r3_token_logprobs(const r3_logits* shape, const void* logit
     // Few rows: a cluster of CTAs shares one, as long as they all run at once and a thread has two
     // pieces or more.
     a.split = 1;
-    while (a.split < r3::kMaxSplit && a.T * a.split * 2 <= 2 * r3::sm_count() &&
+    while (a.split < r3::kMaxSplit && (long long)a.T * a.split <= r3::sm_count() &&
            row_bytes / (a.split * 2) >= 2LL * 16 * threads)
         a.split *= 2;
     auto launch = [&](auto type) {

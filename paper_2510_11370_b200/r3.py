@@ -605,9 +605,10 @@ def _device_of(name: str, t) -> torch.device:
         raise TypeError(f"{name}: expected a torch.Tensor")
     if not t.is_cuda:
         raise ValueError("expected a CUDA tensor (there is no CPU path)")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name}: on {t.device}, which is not the current device")
-    return t.device
+    dev = t.device
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {dev}, which is not the current device")
+    return dev
 
 
 def _norm_shape(rows, d, act, w_post, gate, w_pre, eps, residual_scale, branch_scale, dev):
@@ -878,25 +879,32 @@ def normed_stack_train(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down
 
 def _rows(name: str, t):
     """Pointer and row stride of a [T, V] tensor whose rows may lie apart but are dense."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    if t.dim() != 2:
+        raise ValueError(f"{name}: expected [T, V]")
+    (rows, width), (ld, hop) = t.shape, t.stride()
+    if width > 1 and hop != 1:
         raise ValueError(f"{name}: expected [T, V] with adjacent columns")
-    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    if ld < t.shape[1]:
+    if rows <= 1:
+        ld = width
+    elif ld < width:
         raise ValueError(f"{name}: rows overlap")
     return t.data_ptr(), ld
 
 
 def _logits_shape(logits, token_ids, temperature):
+    """The r3_logits of a call and the addresses of the logits and the ids (None without)."""
     dev = _device_of("logits", logits)
-    if logits.dtype not in _ACT:
+    dtype = _ACT.get(logits.dtype)
+    if dtype is None:
         raise ValueError(f"logits: dtype {logits.dtype}, expected float32 or bfloat16")
     ptr, ld = _rows("logits", logits)
     T, V = logits.shape
     ids, id_bytes = None, 4
     if token_ids is not None:
-        id_bytes = 4 if token_ids.dtype == torch.int32 else 8
-        ids = _arg("token_ids", token_ids, (T,), torch.int32 if id_bytes == 4 else torch.int64, dev)
-    return Logits(T, V, ld, _ACT[logits.dtype], id_bytes, float(temperature)), ptr, ids, dev
+        wide = token_ids.dtype != torch.int32
+        id_bytes = 8 if wide else 4
+        ids = _arg("token_ids", token_ids, (T,), torch.int64 if wide else torch.int32, dev)
+    return Logits(T, V, ld, dtype, id_bytes, temperature), ptr, ids, dev
 
 
 def token_logprobs(logits, token_ids=None, *, temperature=1.0, n_top=0, want_entropy=False,
@@ -905,20 +913,24 @@ def token_logprobs(logits, token_ids=None, *, temperature=1.0, n_top=0, want_ent
     rows may lie apart).  Returns (logp [T] or None without token_ids, entropy [T] or None,
     stats [T, 2] or None, top_ids [T, n_top] int32 or None, top_logp [T, n_top] or None).  A row
     with a negative token id is skipped: zeros, top_ids -1."""
-    s, ptr, ids, dev = _logits_shape(logits, token_ids, temperature)
-    f32, T, n_top = torch.float32, s.T, int(n_top)
-    logp = logits.new_empty((T,), dtype=f32) if token_ids is not None else None
-    entropy = logits.new_empty((T,), dtype=f32) if want_entropy else None
-    stats = logits.new_empty((T, 2), dtype=f32) if want_stats else None
-    top_ids = top_logp = None
+    s, ptr, ids, _ = _logits_shape(logits, token_ids, temperature)
+    new, f32, T = logits.new_empty, torch.float32, s.T
+    logp = entropy = stats = top_ids = top_logp = None
+    at = [None] * 5                              # the outputs' addresses
+    if ids is not None:
+        logp = new((T,), dtype=f32)
+        at[0] = logp.data_ptr()
+    if want_entropy:
+        entropy = new((T,), dtype=f32)
+        at[1] = entropy.data_ptr()
+    if want_stats:
+        stats = new((T, 2), dtype=f32)
+        at[2] = stats.data_ptr()
     if n_top > 0:
-        top_ids = logits.new_empty((T, n_top), dtype=torch.int32)
-        top_logp = logits.new_empty((T, n_top), dtype=f32)
-
-    def at(t):
-        return None if t is None else t.data_ptr()
-    _check(lib.r3_token_logprobs(ctypes.byref(s), ptr, ids, at(logp), at(entropy), at(stats), n_top,
-                                 at(top_ids), at(top_logp), _ptr(dev_status), _stream(stream)))
+        top_ids, top_logp = new((T, n_top), dtype=torch.int32), new((T, n_top), dtype=f32)
+        at[3], at[4] = top_ids.data_ptr(), top_logp.data_ptr()
+    _check(lib.r3_token_logprobs(ctypes.byref(s), ptr, ids, at[0], at[1], at[2], n_top, at[3], at[4],
+                                 None if dev_status is None else _ptr(dev_status), _stream(stream)))
     return logp, entropy, stats, top_ids, top_logp
 
 

@@ -274,6 +274,8 @@ def test_python_refusals(r3):
         r3.AdamW([w[::2]], [g[::2]])
     with pytest.raises(ValueError):
         r3.AdamW([], [])
+    with pytest.raises(r3.R3Error):
+        r3.AdamW([w]).step(1, 0.1)                                     # no gradients yet
     same = r3.AdamW([w, w], [g, g])
     with pytest.raises(r3.R3Error) as e:
         same.step(1, 0.1)

@@ -636,7 +636,7 @@ r3_status r3_normed_stack_train(const r3_shape* shape, int32_t L, const r3_block
 
 /* A batch of logits: T rows of V values, row t at logits + t * ld elements (ld >= V, so a padded or
  * sliced vocabulary is taken as it lies), dtype R3_F32 or R3_BF16.  token_ids are int32 or int64
- * (id_bytes 4 or 8).  temperature (1e-6 to 1e30) divides the logits. */
+ * (id_bytes 4 or 8).  temperature (1e-6 to 1e20) divides the logits. */
 typedef struct {
     int32_t T, V;
     int64_t ld;

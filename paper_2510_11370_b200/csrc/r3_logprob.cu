@@ -722,7 +722,9 @@ static r3_status check_logits(const r3_logits* s) {
     if (s->T < 0 || s->T > 0x7f000000 || s->V <= 0 || s->V > (1 << 30) || s->ld < s->V) return R3_ERR_INVALID_ARG;
     if (s->dtype != R3_F32 && s->dtype != R3_BF16) return R3_ERR_INVALID_ARG;
     if (s->id_bytes != 4 && s->id_bytes != 8) return R3_ERR_INVALID_ARG;
-    if (!(s->temperature >= 1e-6 && s->temperature <= 1e30))        // 2^100 log2(e) / it stays finite
+    // -2^100, which stands for -inf in the sums, times log2(e) / temperature is finite and far below any
+    // exponent that counts
+    if (!(s->temperature >= 1e-6 && s->temperature <= 1e20))
         return R3_ERR_INVALID_ARG;
     return R3_OK;
 }

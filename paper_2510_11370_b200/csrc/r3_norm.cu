@@ -27,6 +27,7 @@ namespace r3 {
 
 constexpr int kNormMaxThreads = 512;   // per row
 constexpr int kNormBwdThreads = 384;   // backward: per SM, at up to 168 registers a thread
+constexpr int kNormBwdThreadsF32 = 512;   // ... float32 rows (half the columns), at up to 128
 constexpr int kNormFwdThreads = 640;   // forward: per SM, at up to 102
 constexpr int kNormPieces = 2;         // pieces per thread; twice as many where these do not reach
 constexpr int kWarpRows = 4;           // forward, one-warp form: rows per CTA
@@ -330,6 +331,12 @@ norm_fwd_kernel(const NormArgs a) {
     copy_wait<0>();
 }
 
+// Threads per SM that the backward kernel is compiled for.  (An SM's registers are four files of 16384:
+// 15 warps at 134 registers do not fit although 15 x 32 x 134 < 65536.)
+__host__ __device__ constexpr int norm_bwd_threads(bool wide, bool f32, bool full) {
+    return wide ? kNormMaxThreads : f32 && !full ? kNormBwdThreadsF32 : kNormBwdThreads;
+}
+
 // Backward.  With x = x_out, r = rsqrt(mean(x^2) + eps), u = dh w_pre and c = mean(u x) r:
 //   g  = dx_out + r u - x r^2 c;      dw_pre += dh x r;      dx = residual_scale g
 // and with n = y s (s = rsqrt(mean(y^2) + eps)), v = branch_scale gate w_post g, e = mean(v n):
@@ -339,7 +346,7 @@ norm_fwd_kernel(const NormArgs a) {
 // branch_scale w_post A; a token's gate is taken out of v, so that its gradient is the sum that e
 // is formed from.  A row takes two reductions, of three values and of one.
 template <typename T, typename W, int P, bool WARP, bool WIDE, int S, int FORM>
-__global__ void __launch_bounds__(WIDE ? kNormMaxThreads : kNormBwdThreads)
+__global__ void __launch_bounds__(norm_bwd_threads(WIDE, sizeof(T) == 4, FORM == kFormFull))
 norm_bwd_kernel(const NormArgs a) {
     constexpr int N = Vec16<T>::N, Q = 4 * P, HOP = 32 * N;
     constexpr bool KEEP = !WIDE;
@@ -572,7 +579,7 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(const NormSumArgs a) {
     const float* p = a.part + (size_t)blockIdx.y * a.parts * a.d;
     float v = 0.f;
     if (col < a.d) {
-#pragma unroll 8
+#pragma unroll 16
         for (int b = w; b < a.parts; b += 32) v += p[(size_t)b * a.d + col];
     }
     s[w][lane] = v;
@@ -631,19 +638,21 @@ static bool plan_norm(const r3_norm* s, bool bwd, NormPlan* p) {
     if (vecs > kNormMaxThreads * p->pieces) return false;
     p->threads = (vecs + 32 * p->pieces - 1) / (32 * p->pieces) * 32;
     p->wide = p->threads > kNormBwdThreads || p->pieces > kNormPieces;
+    const int resident = !bwd ? kNormFwdThreads
+                              : norm_bwd_threads(p->wide, s->act_dtype == R3_F32, s->gate_kind == R3_GATE_FULL);
     int rows = 1;
     if (p->warp) {
         // backward, one CTA fills the SM with rows, so that their sums of the weight gradients leave it
         // as one; a small batch is spread over the SMs
         const int each = (int)(((long long)s->T + sm_count() - 1) / sm_count());
-        rows = !bwd ? kWarpRows : each < kNormBwdThreads / 32 ? each : kNormBwdThreads / 32;
+        rows = !bwd ? kWarpRows : each < resident / 32 ? each : resident / 32;
         if (rows < 1) rows = 1;
         p->threads = 32 * rows;
     }
     const size_t per_row = (size_t)(bwd ? 4 : 2) * p->pieces * p->threads * 16;
     p->stages = kNormStages * per_row <= (size_t)kNormRingBytes ? kNormStages : 1;
     p->smem = p->stages * per_row;
-    int per_sm = (bwd ? kNormBwdThreads : kNormFwdThreads) / p->threads;
+    int per_sm = resident / p->threads;
     const int by_smem = (int)(kNormRingBytes / p->smem);
     if (per_sm > by_smem) per_sm = by_smem;
     if (per_sm < 1) per_sm = 1;

@@ -89,6 +89,30 @@ def test_temperature_and_int32_ids(r3, temperature):
     check_forward(r3, logits, ids.to(torch.int32), temperature, 4)
 
 
+@pytest.mark.parametrize("temperature", [1e-6, 1e-3, 1e4, 1e20])
+def test_extreme_temperatures(r3, temperature):
+    """Nearly greedy (every exponent is huge: the sums go by differences to the top) and uniform rows.
+    float32 logits apart by one step of 2^-23 are 0.1 apart after division by 1e-6, so log probabilities
+    are compared relative to their size."""
+    logits, ids = make(24, 3001, F32, 77)
+    ref = U.token_logprobs(f64(logits), ids.cpu().numpy(), temperature, 5)
+    logp, ent, stats, tid, tlp = r3.token_logprobs(logits, ids, temperature=temperature, n_top=5,
+                                                   want_entropy=True, want_stats=True)
+    close(logp, ref["logp"], "logp")
+    close(ent, ref["entropy"], "entropy")
+    close(stats, ref["stats"], "stats")
+    close(tlp, ref["top_logp"], "top_logp")
+    assert np.array_equal(tid.cpu().numpy(), ref["top_ids"])
+    check_backward(r3, logits, ids, temperature)
+    # masked values and the padding of a thread's pieces count nothing at any temperature
+    logits[:, 5:2000] = float("-inf")
+    ids = ids.clamp(max=4)
+    ref = U.token_logprobs(f64(logits), ids.cpu().numpy(), temperature)
+    logp, ent, _, _, _ = r3.token_logprobs(logits, ids, temperature=temperature, want_entropy=True)
+    close(logp, ref["logp"], "logp")
+    close(ent, ref["entropy"], "entropy")
+
+
 @pytest.mark.parametrize("T", [1, 30, 700])
 @pytest.mark.parametrize("V", [400, 3001, 40000])
 def test_ties_and_adversarial_orders(r3, T, V):

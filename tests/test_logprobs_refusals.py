@@ -23,7 +23,8 @@ def fwd(r3, s, logits=FAKE, ids=FAKE, logp=FAKE, ent=None, stats=None, n=0, tid=
 
 @pytest.mark.parametrize("kw", [dict(T=-1), dict(V=0), dict(V=-5), dict(ld=99), dict(dtype=2),
                                 dict(id_bytes=2), dict(temperature=0.0), dict(temperature=-1.0),
-                                dict(temperature=float("nan")), dict(temperature=float("inf"))])
+                                dict(temperature=float("nan")), dict(temperature=float("inf")),
+                                dict(temperature=1e-7), dict(temperature=1e21)])
 def test_bad_shapes(r3, kw):
     base = dict(T=4, V=100, ld=100, dtype=0, id_bytes=8, temperature=1.0)
     base.update(kw)

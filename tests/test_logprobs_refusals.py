@@ -43,6 +43,8 @@ def test_bad_arguments(r3):
     assert fwd(r3, s, ids=ctypes.c_void_p(4100)) == bad             # not an int64's
     assert fwd(r3, s, ids=None) == bad                              # logp without ids
     assert fwd(r3, s, logp=None) == bad                             # nothing asked for
+    assert fwd(r3, s, logp=ctypes.c_void_p(4098)) == bad            # not a float's alignment
+    assert fwd(r3, s, ent=ctypes.c_void_p(4097)) == bad
     assert fwd(r3, s, n=3) == bad                                   # no room for the alternatives
     assert fwd(r3, s, n=-1) == bad
     assert fwd(r3, s, n=101, tid=FAKE, tlp=FAKE) == bad             # more than the vocabulary
@@ -57,6 +59,7 @@ def test_bad_arguments(r3):
     assert bwd(ids=None) == bad                                     # dlogp without ids
     assert bwd(dent=FAKE) == bad                                    # dentropy without the entropy
     assert bwd(ld=99) == bad
+    assert bwd(stats=ctypes.c_void_p(4098)) == bad and bwd(dlogp=ctypes.c_void_p(2)) == bad
     assert bwd(ld=128) == bad                                       # in place with another stride
 
 

@@ -28,6 +28,8 @@ __host__ __device__ constexpr int logprob_ctas(int threads) {
 constexpr int kMaxTop = 32;            // alternatives per row
 constexpr int kMaxSplit = 8;           // CTAs per row
 constexpr int kMaxCandidates = 256;
+constexpr int kSlots = 16;             // runs of rounds whose maxima a thread keeps
+constexpr int kMaxSelected = 512;      // runs that are read again
 constexpr float kMoveRef = 8.f;
 constexpr float kLowRef = -4194304.f;  // -2^22: the least reference
 constexpr float kPlainTop = 1048576.f; // |c top| up to which the reference is exact enough
@@ -229,7 +231,8 @@ logprob_kernel(const LogprobArgs a) {
     __shared__ Key s_cand[TOP ? kMaxCandidates : 1];
     __shared__ Key s_gather[TOP ? kMaxSplit * kMaxTop : 1];    // the CTAs' lists, in the first one
     __shared__ Key s_list[kMaxTop];
-    __shared__ unsigned short s_sel[TOP ? NT : 1];
+    __shared__ float s_slot[TOP ? kSlots * NT : 1];             // a thread's maxima over its rounds
+    __shared__ uint32_t s_sel[TOP ? kMaxSelected : 1];          // slot and thread
     __shared__ int s_nsel, s_ncand;
     __shared__ Key s_bound;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -267,6 +270,10 @@ logprob_kernel(const LogprobArgs a) {
     // the last, ragged round the pieces behind the end read as -inf: they change neither the top nor the
     // sums, and a warp skips those that all of its lanes lack.
     const int rounds = (v1 - v0) / (UNROLL * NT);
+    const int all_rounds = (v1 - v0 + UNROLL * NT - 1) / (UNROLL * NT);
+    const int slot_rounds = max(1, (all_rounds + kSlots - 1) / kSlots);
+    int slot = 0, in_slot = 0;
+    float slot_top = -CUDART_INF_F;
     Piece<T> b[UNROLL];
     auto fetch = [&](int j) {
 #pragma unroll
@@ -287,6 +294,13 @@ logprob_kernel(const LogprobArgs a) {
                 const float q = x[u].largest();
                 if (q > fmaxf(r.top, m)) best_vec = j + u * NT;
                 m = fmaxf(m, q);
+            }
+            slot_top = fmaxf(slot_top, m);
+            if (++in_slot == slot_rounds || last) {
+                s_slot[slot * NT + tid] = slot_top;
+                ++slot;
+                in_slot = 0;
+                slot_top = -CUDART_INF_F;
             }
         } else {
             m = Piece<T>::largest(x);
@@ -317,6 +331,7 @@ logprob_kernel(const LogprobArgs a) {
         j += UNROLL * NT;
     }
     if (j - tid < v1) sum(b, j, true);
+    if (TOP && in_slot > 0) s_slot[slot++ * NT + tid] = slot_top;
     // the single elements in front of the first and behind the last whole piece
     const bool has_head = rank == 0, has_tail = rank == a.split - 1;
     const int tail0 = rs.head + rs.vecs * N;
@@ -401,7 +416,8 @@ logprob_kernel(const LogprobArgs a) {
     // maxima of such bounds over equal lanes is reached by n keys of the share, so none of the n
     // largest lies under it; only threads whose piece reaches it (value, first column) hold keys
     // above it, and only their pieces are read again, from L2.  What reaches the bound are a few
-    // more than n keys; each one's rank is the number of larger ones.
+    // more than n keys; each one's rank is the number of larger ones.  A thread keeps the maxima of runs of
+    // its rounds in shared memory, so that of its pieces only the runs that reach the bound are read.
     Key list = 0;
     if (TOP) {
         if (warp == 0) {                                // alone: all warps at it cost more than the barrier
@@ -420,10 +436,30 @@ logprob_kernel(const LogprobArgs a) {
         }
         __syncthreads();
         const Key bound = s_bound;
-        if (best_vec >= 0 && make_key(vec_top, first) >= bound) s_sel[atomicAdd(&s_nsel, 1)] = tid;
+        if (best_vec >= 0 && make_key(vec_top, first) >= bound) {
+            const float least = bound ? key_value(bound) : -CUDART_INF_F;
+            float tops[kSlots];
+#pragma unroll
+            for (int k = 0; k < kSlots; ++k) tops[k] = k < slot ? s_slot[k * NT + tid] : 0.f;
+#pragma unroll
+            for (int k = 0; k < kSlots; ++k) {
+                if (k >= slot || !(tops[k] >= least)) continue;
+                const int at = atomicAdd(&s_nsel, 1);
+                if (at < kMaxSelected) s_sel[at] = (uint32_t)(k << 16 | tid);
+            }
+        }
         __syncthreads();
         const Vec16<T>* px = reinterpret_cast<const Vec16<T>*>(pv);
-        const int per = (v1 - v0 + NT - 1) / NT, total = s_nsel * per;
+        // the q-th piece of the selected runs (of all, where they are too many to list); v1: none
+        const bool listed = s_nsel <= kMaxSelected;
+        const int run = slot_rounds * UNROLL, total = listed ? s_nsel * run : v1 - v0;
+        auto piece_at = [&](int q) {
+            if (q >= total) return v1;
+            if (!listed) return v0 + q;
+            const int s = q / run, r = q - s * run;
+            const uint32_t e = s_sel[s];
+            return min(v1, v0 + (int)(e & 0xffffu) + ((int)(e >> 16) * run + r) * NT);
+        };
         auto offer = [&](float x, int col) {            // any order: ranks do not depend on it
             const Key k = make_key(x, col);
             if (k < bound) return;
@@ -435,8 +471,7 @@ logprob_kernel(const LogprobArgs a) {
             int at[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {               // four loads on their way at once
-                const int q = q0 + u * NT, s = q / per;
-                at[u] = q < total ? v0 + s_sel[s] + (q - s * per) * NT : v1;
+                at[u] = piece_at(q0 + u * NT);
                 if (at[u] < v1) piece[u] = px[at[u]];
             }
 #pragma unroll
@@ -464,8 +499,7 @@ logprob_kernel(const LogprobArgs a) {
             // many large values in the pieces of few threads: every warp keeps the 32 largest of the
             // keys it meets, and the warps' lists are merged
             for (int q0 = warp * 32; q0 < total; q0 += NT) {
-                const int q = q0 + lane, s = q / per;
-                const int vec = q < total ? v0 + s_sel[s] + (q - s * per) * NT : v1;
+                const int vec = piece_at(q0 + lane);
                 float x[N];
                 if (vec < v1) px[vec].unpack(x);
 #pragma unroll

@@ -74,39 +74,41 @@ __device__ __forceinline__ void widen(const Vec16<__nv_bfloat16>& v, float* f) {
 
 // Sum of NV values over the threads of a row; every thread gets the result.  One barrier per call: the
 // caller alternates buffers, so that a buffer is only written again behind the barrier of the call in
-// between.
-template <int NV, bool WARP, bool WIDE>
-__device__ __forceinline__ void row_sum(float (&v)[NV], float (*red)[4], int warps) {
-#pragma unroll
-    for (int s = 16; s > 0; s >>= 1) {
+// between.  More than four warps' sums are added as a tree over the lanes (a loop over up to 16 warps cost
+// a thread three times the instructions).
+template <int NV, bool WARP>
+__device__ __forceinline__ void row_sum(float (&v)[NV], float4* red, int warps) {
+    auto level = [&](int s) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], s);
-    }
+    };
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) level(s);
     if (WARP) return;
-    if ((threadIdx.x & 31) == 0) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) red[threadIdx.x >> 5][i] = v[i];
-    }
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) red[threadIdx.x >> 5] = make_float4(v[0], NV > 1 ? v[NV > 1] : 0.f, NV > 2 ? v[NV > 2 ? 2 : 0] : 0.f, 0.f);
     __syncthreads();
-    if (WIDE) {                                     // up to 16 warps: a tree over the lanes
-        const int lane = threadIdx.x & 31;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) v[i] = lane < warps ? red[lane & 15][i] : 0.f;
-#pragma unroll
-        for (int s = 8; s > 0; s >>= 1) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], s);
-        }
-#pragma unroll
-        for (int i = 0; i < NV; ++i) v[i] = __shfl_sync(0xffffffffu, v[i], 0);
+    auto take = [&](const float4& f, bool first) {
+        v[0] = first ? f.x : v[0] + f.x;
+        if (NV > 1) v[NV > 1] = first ? f.y : v[NV > 1] + f.y;
+        if (NV > 2) v[NV > 2 ? 2 : 0] = first ? f.z : v[NV > 2 ? 2 : 0] + f.z;
+    };
+    const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (warps <= 4) {
+        const float4 f0 = red[0], f1 = warps > 1 ? red[1] : none, f2 = warps > 2 ? red[2] : none,
+                     f3 = warps > 3 ? red[3] : none;
+        take(f0, true);
+        take(f1, false);
+        take(f2, false);
+        take(f3, false);
         return;
     }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = 0.f;
-    for (int w = 0; w < warps; ++w) {                                    // fixed order
-#pragma unroll
-        for (int i = 0; i < NV; ++i) v[i] += red[w][i];
-    }
+    const int at = lane & (warps > 8 ? 15 : 7);
+    take(at < warps ? red[at] : none, true);
+    if (warps > 8) level(8);
+    level(4);
+    level(2);
+    level(1);
 }
 
 // N values (one 16-byte piece of activations) of a vector of type W, from column `col` on.
@@ -136,10 +138,10 @@ template <typename T> __device__ __forceinline__ void store_piece(T* p, const fl
 }
 
 // The usual form has both norms, a gate per column or none, and (backward) a gradient from above; the
-// first has only the norm in front of a block.  They have kernels of their own, whose absent parts
-// cost no instructions; everything else is decided at run time, except that a gate per element has
-// kernels of its own too (its registers).
-enum { kFormUsual = 0, kFormFirst = 1, kFormAny = 2, kFormFull = 3 };
+// token form the same with a gate per token; the first has only the norm in front of a block.  They have
+// kernels of their own, whose absent parts cost no instructions; everything else is decided at run time,
+// except that a gate per element has kernels of its own too (its registers).
+enum { kFormUsual = 0, kFormToken = 1, kFormFirst = 2, kFormAny = 3, kFormFull = 4 };
 
 // The weights of a thread's columns, kept for all its rows in registers; in the wide form read again
 // from L1 for each row (no room).  A column's factor is the vector's element
@@ -204,8 +206,9 @@ template <typename T, int P, int FORM> struct RowGate {
     __device__ __forceinline__ void load(const NormArgs& a, int row, int col, const bool (&in)[P]) {
         constexpr int HOP = 32 * Vec16<T>::N;
         token = 1.f;
-        if (FORM < kFormAny || row >= a.T) return;
-        if (FORM == kFormAny && a.gate_kind == R3_GATE_TOKEN) token = static_cast<const float*>(a.gate)[row];
+        if (FORM == kFormUsual || FORM == kFormFirst || row >= a.T) return;
+        if (FORM == kFormToken || (FORM == kFormAny && a.gate_kind == R3_GATE_TOKEN))
+            token = static_cast<const float*>(a.gate)[row];
         if constexpr (FORM == kFormFull) {
             const T* g = static_cast<const T*>(a.gate) + (size_t)row * a.d + col;
 #pragma unroll
@@ -222,11 +225,11 @@ norm_fwd_kernel(const NormArgs a) {
     constexpr bool KEEP = !WIDE;
     typedef const Vec16<T>* Ptr;
     extern __shared__ uint4 ring_all[];
-    __shared__ float s_red[2][kNormMaxThreads / 32][4];   // a value per warp of the CTA
-    const bool has_y = FORM == kFormUsual || (FORM >= kFormAny && a.y);
-    const bool has_post = FORM == kFormUsual || (FORM >= kFormAny && a.w_post);
+    __shared__ float4 s_red[2][kNormMaxThreads / 32];      // up to three values per warp of the CTA
+    const bool has_y = FORM <= kFormToken || (FORM >= kFormAny && a.y);
+    const bool has_post = FORM <= kFormToken || (FORM >= kFormAny && a.w_post);
     const bool has_pre = FORM < kFormAny || a.w_pre;
-    const bool token = FORM == kFormAny && a.gate_kind == R3_GATE_TOKEN;
+    const bool token = FORM == kFormToken || (FORM == kFormAny && a.gate_kind == R3_GATE_TOKEN);
     const bool full = FORM == kFormFull;
     const NormPlace me = norm_place<N, P, WARP, Q, S>(ring_all);
     const float inv_d = 1.f / (float)a.d, eps = a.eps, res = a.res;
@@ -255,7 +258,7 @@ norm_fwd_kernel(const NormArgs a) {
 #pragma unroll
     for (int s = 0; s < S; ++s) fetch(me.ring + s * Q * 32);
     Weights<W, N, P, KEEP> post, pre;
-    const void* channel = a.gate_kind == R3_GATE_CHANNEL ? a.gate : nullptr;
+    const void* channel = FORM != kFormToken && a.gate_kind == R3_GATE_CHANNEL ? a.gate : nullptr;
     if (has_y) post.init(a.w_post, channel, a.branch, me.col, in);
     if (has_pre) pre.init(a.w_pre, nullptr, 1.f, me.col, in);
     RowGate<T, P, FORM> gate, ahead;
@@ -288,7 +291,7 @@ norm_fwd_kernel(const NormArgs a) {
         ahead.load(a, row + me.stride, me.col, in);
         float r = 1.f;
         if (has_post) {
-            row_sum<1, WARP, WIDE>(s, s_red[0], me.warps);
+            row_sum<1, WARP>(s, s_red[0], me.warps);
             r = rsqrtf(s[0] * inv_d + eps);
         }
         if (has_y) {
@@ -316,7 +319,7 @@ norm_fwd_kernel(const NormArgs a) {
             for (int p = 0; p < P; ++p)
 #pragma unroll
                 for (int i = 0; i < N; ++i) s[0] = fmaf(x[p][i], x[p][i], s[0]);
-            row_sum<1, WARP, WIDE>(s, s_red[1], me.warps);
+            row_sum<1, WARP>(s, s_red[1], me.warps);
             r = rsqrtf(s[0] * inv_d + eps);
 #pragma unroll
             for (int p = 0; p < P; ++p) {
@@ -355,12 +358,12 @@ norm_bwd_kernel(const NormArgs a) {
     constexpr bool KEEP = !WIDE;
     typedef const Vec16<T>* Ptr;
     extern __shared__ uint4 ring_all[];
-    __shared__ float s_red[2][kNormMaxThreads / 32][4];   // a value per warp of the CTA
-    const bool has_y = FORM == kFormUsual || (FORM >= kFormAny && a.y);
-    const bool has_post = FORM == kFormUsual || (FORM >= kFormAny && a.w_post);
+    __shared__ float4 s_red[2][kNormMaxThreads / 32];      // up to three values per warp of the CTA
+    const bool has_y = FORM <= kFormToken || (FORM >= kFormAny && a.y);
+    const bool has_post = FORM <= kFormToken || (FORM >= kFormAny && a.w_post);
     const bool has_pre = FORM < kFormAny || a.w_pre;
-    const bool has_up = FORM == kFormUsual || a.dx_out;
-    const bool token = FORM == kFormAny && a.gate_kind == R3_GATE_TOKEN;
+    const bool has_up = FORM <= kFormToken || a.dx_out;
+    const bool token = FORM == kFormToken || (FORM == kFormAny && a.gate_kind == R3_GATE_TOKEN);
     const bool full = FORM == kFormFull;
     const NormPlace me = norm_place<N, P, WARP, Q, S>(ring_all);
     const float inv_d = 1.f / (float)a.d, eps = a.eps, res = has_y ? a.res : 1.f;
@@ -395,7 +398,7 @@ norm_bwd_kernel(const NormArgs a) {
     };
 #pragma unroll
     for (int s = 0; s < S; ++s) fetch(me.ring + s * Q * 32);
-    const void* channel = a.gate_kind == R3_GATE_CHANNEL ? a.gate : nullptr;
+    const void* channel = FORM != kFormToken && a.gate_kind == R3_GATE_CHANNEL ? a.gate : nullptr;
     Weights<W, N, P, KEEP> post, pre;
     if (has_y) post.init(a.w_post, channel, a.branch, me.col, in);
     if (has_pre) pre.init(a.w_pre, nullptr, 1.f, me.col, in);
@@ -443,7 +446,7 @@ norm_bwd_kernel(const NormArgs a) {
         stage = stage + 1 == S ? 0 : stage + 1;
         row_gate = ahead;
         ahead.load(a, row + me.stride, me.col, in);
-        if (has_pre || has_post) row_sum<3, WARP, WIDE>(s, s_red[0], me.warps);
+        if (has_pre || has_post) row_sum<3, WARP>(s, s_red[0], me.warps);
         const float r = rsqrtf(s[0] * inv_d + eps);
         const float rrc = s[1] * inv_d * r * r * r;             // r^2 c
         const float sy = has_post ? rsqrtf(s[2] * inv_d + eps) : 1.f;
@@ -502,7 +505,7 @@ norm_bwd_kernel(const NormArgs a) {
             }
         }
         if (has_y) {
-            if (has_post || token) row_sum<1, WARP, WIDE>(z, s_red[1], me.warps);
+            if (has_post || token) row_sum<1, WARP>(z, s_red[1], me.warps);
             const float k = gate_t * sy;
             const float e = has_post ? -z[0] * inv_d : 0.f;
             if (token && me.col == 0)
@@ -522,7 +525,7 @@ norm_bwd_kernel(const NormArgs a) {
             }
         }
         // with one reduction per row its buffer comes around without a barrier in between
-        if (!WARP && FORM != kFormUsual && (has_pre || has_post) != (has_y && (has_post || token)))
+        if (!WARP && FORM > kFormToken && (has_pre || has_post) != (has_y && (has_post || token)))
             __syncthreads();
     }
     copy_wait<0>();
@@ -683,9 +686,13 @@ static r3_status launch_norm_kernel(const NormArgs& a, const NormPlan& p, cudaSt
 }
 template <typename T, typename W, int P, bool WARP, bool WIDE, int S>
 static r3_status launch_norm(const NormArgs& a, const NormPlan& p, bool bwd, cudaStream_t cs) {
-    if (a.y && a.w_post && a.w_pre && a.gate_kind <= R3_GATE_CHANNEL && (!bwd || a.dx_out))
+    if (a.y && a.w_post && a.w_pre && a.gate_kind <= R3_GATE_TOKEN && (!bwd || a.dx_out)) {
+        if (a.gate_kind == R3_GATE_TOKEN)
+            return bwd ? launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, S, kFormToken>>(a, p, cs)
+                       : launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, S, kFormToken>>(a, p, cs);
         return bwd ? launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, S, kFormUsual>>(a, p, cs)
                    : launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, S, kFormUsual>>(a, p, cs);
+    }
     if (!a.y)
         return bwd ? launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, S, kFormFirst>>(a, p, cs)
                    : launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, S, kFormFirst>>(a, p, cs);

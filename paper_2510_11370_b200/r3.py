@@ -681,18 +681,27 @@ def norm_residual_bwd(x_out, y, dx_out, dh=None, *, w_post=None, gate=None, w_pr
         dx = torch.empty_like(like)
     if y is not None and dy is None:
         dy = torch.empty_like(like)
-    dgate = None
-    if gate is not None:
-        full = s.gate_kind == R3_GATE_FULL
-        dgate = torch.empty(gate.shape, dtype=act if full else torch.float32, device=dev)
-    dw_post, dw_pre = (torch.empty(d, dtype=torch.float32, device=dev) if w is not None else None
-                       for w in (w_post, w_pre))
+    # the float32 sums over tokens are the rows of one buffer (d is a multiple of 8: aligned)
+    channel = s.gate_kind == R3_GATE_CHANNEL
+    dw_post = dgate = dw_pre = None
+    wanted = (post is not None) + channel + (pre is not None)
+    if wanted:
+        sums = list(like.new_empty((wanted, d), dtype=torch.float32).unbind(0))
+        if post is not None:
+            dw_post = sums.pop()
+        if channel:
+            dgate = sums.pop()
+        if pre is not None:
+            dw_pre = sums.pop()
+    if gate is not None and not channel:
+        dgate = torch.empty_like(gate)           # float32 [T, 1], or [T, d] of the rows' type
     if ws is None:
         ws = workspace(lib.r3_norm_residual_bwd_workspace_bytes(ctypes.byref(s)), dev)
-    _check(lib.r3_norm_residual_bwd(ctypes.byref(s), src[0], src[1], post, gate_at, pre, src[2],
-                                    src[3], _arg("dx", dx, shape, act, dev),
-                                    _arg("dy", dy, shape, act, dev), _ptr(dw_post), _ptr(dgate),
-                                    _ptr(dw_pre), _ptr(ws), ws.numel(), _stream(stream)))
+    _check(lib.r3_norm_residual_bwd(
+        ctypes.byref(s), src[0], src[1], post, gate_at, pre, src[2], src[3],
+        _arg("dx", dx, shape, act, dev), _arg("dy", dy, shape, act, dev),
+        None if dw_post is None else dw_post.data_ptr(), None if dgate is None else dgate.data_ptr(),
+        None if dw_pre is None else dw_pre.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)))
     return dx, dy, dw_post, dgate, dw_pre
 
 

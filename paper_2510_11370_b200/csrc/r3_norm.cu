@@ -74,41 +74,41 @@ __device__ __forceinline__ void widen(const Vec16<__nv_bfloat16>& v, float* f) {
 
 // Sum of NV values over the threads of a row; every thread gets the result.  One barrier per call: the
 // caller alternates buffers, so that a buffer is only written again behind the barrier of the call in
-// between.  More than four warps' sums are added as a tree over the lanes (a loop over up to 16 warps cost
-// a thread three times the instructions).
-template <int NV, bool WARP>
-__device__ __forceinline__ void row_sum(float (&v)[NV], float4* red, int warps) {
-    auto level = [&](int s) {
+// between.  The wide form's up to 16 warps are added as a tree over the lanes (a loop costs a thread three
+// times the instructions: 4096 x 8192 bf16 backward 133 against 106 us), fewer one after the other (the
+// tree beside the loop costs registers: 65536 x 2048 bf16 backward 267 against 258 us).
+template <int NV, bool WARP, bool WIDE>
+__device__ __forceinline__ void row_sum(float (&v)[NV], float (*red)[4], int warps) {
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], s);
-    };
-#pragma unroll
-    for (int s = 16; s > 0; s >>= 1) level(s);
+    }
     if (WARP) return;
-    const int lane = threadIdx.x & 31;
-    if (lane == 0) red[threadIdx.x >> 5] = make_float4(v[0], NV > 1 ? v[NV > 1] : 0.f, NV > 2 ? v[NV > 2 ? 2 : 0] : 0.f, 0.f);
+    if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) red[threadIdx.x >> 5][i] = v[i];
+    }
     __syncthreads();
-    auto take = [&](const float4& f, bool first) {
-        v[0] = first ? f.x : v[0] + f.x;
-        if (NV > 1) v[NV > 1] = first ? f.y : v[NV > 1] + f.y;
-        if (NV > 2) v[NV > 2 ? 2 : 0] = first ? f.z : v[NV > 2 ? 2 : 0] + f.z;
-    };
-    const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (warps <= 4) {
-        const float4 f0 = red[0], f1 = warps > 1 ? red[1] : none, f2 = warps > 2 ? red[2] : none,
-                     f3 = warps > 3 ? red[3] : none;
-        take(f0, true);
-        take(f1, false);
-        take(f2, false);
-        take(f3, false);
+    if (WIDE) {                                     // up to 16 warps: a tree over the lanes
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = lane < warps ? red[lane & 15][i] : 0.f;
+#pragma unroll
+        for (int s = 8; s > 0; s >>= 1) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], s);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = __shfl_sync(0xffffffffu, v[i], 0);
         return;
     }
-    const int at = lane & (warps > 8 ? 15 : 7);
-    take(at < warps ? red[at] : none, true);
-    if (warps > 8) level(8);
-    level(4);
-    level(2);
-    level(1);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] = 0.f;
+    for (int w = 0; w < warps; ++w) {                                    // fixed order
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] += red[w][i];
+    }
 }
 
 // N values (one 16-byte piece of activations) of a vector of type W, from column `col` on.
@@ -225,7 +225,7 @@ norm_fwd_kernel(const NormArgs a) {
     constexpr bool KEEP = !WIDE;
     typedef const Vec16<T>* Ptr;
     extern __shared__ uint4 ring_all[];
-    __shared__ float4 s_red[2][kNormMaxThreads / 32];      // up to three values per warp of the CTA
+    __shared__ float s_red[2][kNormMaxThreads / 32][4];   // up to three values per warp of the CTA
     const bool has_y = FORM <= kFormToken || (FORM >= kFormAny && a.y);
     const bool has_post = FORM <= kFormToken || (FORM >= kFormAny && a.w_post);
     const bool has_pre = FORM < kFormAny || a.w_pre;
@@ -291,7 +291,7 @@ norm_fwd_kernel(const NormArgs a) {
         ahead.load(a, row + me.stride, me.col, in);
         float r = 1.f;
         if (has_post) {
-            row_sum<1, WARP>(s, s_red[0], me.warps);
+            row_sum<1, WARP, WIDE>(s, s_red[0], me.warps);
             r = rsqrtf(s[0] * inv_d + eps);
         }
         if (has_y) {
@@ -319,7 +319,7 @@ norm_fwd_kernel(const NormArgs a) {
             for (int p = 0; p < P; ++p)
 #pragma unroll
                 for (int i = 0; i < N; ++i) s[0] = fmaf(x[p][i], x[p][i], s[0]);
-            row_sum<1, WARP>(s, s_red[1], me.warps);
+            row_sum<1, WARP, WIDE>(s, s_red[1], me.warps);
             r = rsqrtf(s[0] * inv_d + eps);
 #pragma unroll
             for (int p = 0; p < P; ++p) {
@@ -358,7 +358,7 @@ norm_bwd_kernel(const NormArgs a) {
     constexpr bool KEEP = !WIDE;
     typedef const Vec16<T>* Ptr;
     extern __shared__ uint4 ring_all[];
-    __shared__ float4 s_red[2][kNormMaxThreads / 32];      // up to three values per warp of the CTA
+    __shared__ float s_red[2][kNormMaxThreads / 32][4];   // up to three values per warp of the CTA
     const bool has_y = FORM <= kFormToken || (FORM >= kFormAny && a.y);
     const bool has_post = FORM <= kFormToken || (FORM >= kFormAny && a.w_post);
     const bool has_pre = FORM < kFormAny || a.w_pre;
@@ -446,7 +446,7 @@ norm_bwd_kernel(const NormArgs a) {
         stage = stage + 1 == S ? 0 : stage + 1;
         row_gate = ahead;
         ahead.load(a, row + me.stride, me.col, in);
-        if (has_pre || has_post) row_sum<3, WARP>(s, s_red[0], me.warps);
+        if (has_pre || has_post) row_sum<3, WARP, WIDE>(s, s_red[0], me.warps);
         const float r = rsqrtf(s[0] * inv_d + eps);
         const float rrc = s[1] * inv_d * r * r * r;             // r^2 c
         const float sy = has_post ? rsqrtf(s[2] * inv_d + eps) : 1.f;
@@ -505,7 +505,7 @@ norm_bwd_kernel(const NormArgs a) {
             }
         }
         if (has_y) {
-            if (has_post || token) row_sum<1, WARP>(z, s_red[1], me.warps);
+            if (has_post || token) row_sum<1, WARP, WIDE>(z, s_red[1], me.warps);
             const float k = gate_t * sy;
             const float e = has_post ? -z[0] * inv_d : 0.f;
             if (token && me.col == 0)
@@ -568,7 +568,9 @@ norm_bwd_kernel(const NormArgs a) {
 
 // Column sums of the partial rows, in order; out[0] = dw_pre from plane 0, and from plane 1 (the
 // sums of g n) out[1] = dw_post = branch_scale gate A and out[2] = dgate = branch_scale w_post A.
-// 32 columns per CTA; 32 warps take the rows in turn, so that few loads follow one another.
+// COLS columns per CTA; 1024 / COLS groups of threads take the rows in turn, so that few loads follow one
+// another.  32 columns are the better width for the memory (1023 x 8192 bf16: 5 us less than 16), 16 where
+// 32 would leave SMs idle (4097 x 1160 float32: 1.5 us less).
 struct NormSumArgs {
     const float* part;
     float* out[3];
@@ -577,24 +579,30 @@ struct NormSumArgs {
     int parts, d, w_bf16;
     float branch;
 };
+template <int COLS>
 __global__ void __launch_bounds__(1024) norm_sum_kernel(const NormSumArgs a) {
-    __shared__ float s[32][33];
+    constexpr int TURNS = 1024 / COLS;
+    __shared__ float s[TURNS][COLS + 1];
     if (!(blockIdx.y == 0 ? a.out[0] != nullptr : a.out[1] || a.out[2])) return;
     tc::grid_dependency_wait();
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int mine = threadIdx.x % COLS, turn = threadIdx.x / COLS, col = blockIdx.x * COLS + mine;
     const float* p = a.part + (size_t)blockIdx.y * a.parts * a.d;
     float v = 0.f;
     if (col < a.d) {
-#pragma unroll 16
-        for (int b = w; b < a.parts; b += 32) v += p[(size_t)b * a.d + col];
+#pragma unroll 8
+        for (int b = turn; b < a.parts; b += TURNS) v += p[(size_t)b * a.d + col];
     }
-    s[w][lane] = v;
+    s[turn][mine] = v;
     __syncthreads();
-    // warp w now holds column 32 blockIdx.x + w: the 32 sums of its lanes, added as a tree
+    // warp w < COLS takes column COLS blockIdx.x + w: its sums, added as a tree
+    if (w >= COLS) return;
     v = s[lane][w];
 #pragma unroll
+    for (int k = 32; k < TURNS; k += 32) v += s[lane + k][w];
+#pragma unroll
     for (int k = 16; k > 0; k >>= 1) v += __shfl_xor_sync(0xffffffffu, v, k);
-    const int c = blockIdx.x * 32 + w;
+    const int c = blockIdx.x * COLS + w;
     if (lane != 0 || c >= a.d) return;
     if (blockIdx.y == 0) {
         a.out[0][c] = v;
@@ -827,8 +835,11 @@ extern "C" r3_status r3_norm_residual_bwd(const r3_norm* shape, const void* x_ou
         sum.w_bf16 = shape->w_dtype == R3_BF16;
         sum.branch = shape->branch_scale;
         // launched while the rows are still being worked on; it waits for them itself
-        if (r3::tc::launch_dependent(r3::norm_sum_kernel, dim3((shape->d + 31) / 32, 2), dim3(1024), 0,
-                                     cs, sum) != cudaSuccess) {
+        const bool narrow = (shape->d + 31) / 32 * 2 < r3::sm_count();
+        const int cols = narrow ? 16 : 32;
+        if (r3::tc::launch_dependent(narrow ? r3::norm_sum_kernel<16> : r3::norm_sum_kernel<32>,
+                                     dim3((shape->d + cols - 1) / cols, 2), dim3(1024), 0, cs,
+                                     sum) != cudaSuccess) {
             cudaGetLastError();
             return R3_ERR_CUDA;
         }

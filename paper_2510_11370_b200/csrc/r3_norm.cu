@@ -31,6 +31,7 @@ namespace r3 {
 constexpr int kNormMaxThreads = 512;   // per row
 constexpr int kNormBwdThreads = 384;   // backward: per SM, at up to 168 registers a thread
 constexpr int kNormBwdThreadsF32 = 512;   // ... float32 rows (half the columns), at up to 128
+constexpr int kNormPairThreads = 256;  // ... two rows at a time, at up to 255
 constexpr int kNormFwdThreads = 640;   // forward: per SM, at up to 102
 constexpr int kNormPieces = 2;         // pieces per thread; twice as many where these do not reach
 constexpr int kWarpRows = 4;           // forward, one-warp form: rows per CTA
@@ -77,8 +78,8 @@ __device__ __forceinline__ void widen(const Vec16<__nv_bfloat16>& v, float* f) {
 // between.  The wide form's up to 16 warps are added as a tree over the lanes (a loop costs a thread three
 // times the instructions: 4096 x 8192 bf16 backward 133 against 106 us), fewer one after the other (the
 // tree beside the loop costs registers: 65536 x 2048 bf16 backward 267 against 258 us).
-template <int NV, bool WARP, bool WIDE>
-__device__ __forceinline__ void row_sum(float (&v)[NV], float (*red)[4], int warps) {
+template <int NV, bool WARP, bool WIDE, int M>
+__device__ __forceinline__ void row_sum(float (&v)[NV], float (*red)[M], int warps) {
 #pragma unroll
     for (int s = 16; s > 0; s >>= 1) {
 #pragma unroll
@@ -339,8 +340,11 @@ norm_fwd_kernel(const NormArgs a) {
 
 // Threads per SM that the backward kernel is compiled for.  (An SM's registers are four files of 16384:
 // 15 warps at 134 registers do not fit although 15 x 32 x 134 < 65536.)
-__host__ __device__ constexpr int norm_bwd_threads(bool wide, bool f32, bool full) {
-    return wide ? kNormMaxThreads : f32 && !full ? kNormBwdThreadsF32 : kNormBwdThreads;
+__host__ __device__ constexpr int norm_bwd_threads(bool wide, bool f32, bool full, int rows) {
+    return rows > 1       ? kNormPairThreads
+           : wide         ? kNormMaxThreads
+           : f32 && !full ? kNormBwdThreadsF32
+                          : kNormBwdThreads;
 }
 
 // Backward.  With x = x_out, r = rsqrt(mean(x^2) + eps), u = dh w_pre and c = mean(u x) r:
@@ -350,15 +354,16 @@ __host__ __device__ constexpr int norm_bwd_threads(bool wide, bool f32, bool ful
 // dw_post and the gate's gradient both come from g n: per column, where the gate is one factor per
 // column (or there is none), A = sum g n gives dw_post = branch_scale gate A and dgate =
 // branch_scale w_post A; a token's gate is taken out of v, so that its gradient is the sum that e
-// is formed from.  A row takes two reductions, of three values and of one.
-template <typename T, typename W, int P, bool WARP, bool WIDE, int S, int FORM>
-__global__ void __launch_bounds__(norm_bwd_threads(WIDE, sizeof(T) == 4, FORM == kFormFull))
+// is formed from.  A row takes two reductions, of three values and of one.  A group of threads works on R
+// rows at a time.
+template <typename T, typename W, int P, bool WARP, bool WIDE, int S, int R, int FORM>
+__global__ void __launch_bounds__(norm_bwd_threads(WIDE, sizeof(T) == 4, FORM == kFormFull, R))
 norm_bwd_kernel(const NormArgs a) {
-    constexpr int N = Vec16<T>::N, Q = 4 * P, HOP = 32 * N;
+    constexpr int N = Vec16<T>::N, Q = 4 * P * R, HOP = 32 * N;
     constexpr bool KEEP = !WIDE;
     typedef const Vec16<T>* Ptr;
     extern __shared__ uint4 ring_all[];
-    __shared__ float s_red[2][kNormMaxThreads / 32][4];   // up to three values per warp of the CTA
+    __shared__ float s_red[2][kNormMaxThreads / 32][3 * R + R % 2];   // up to 3 R values per warp of the CTA
     const bool has_y = FORM <= kFormToken || (FORM >= kFormAny && a.y);
     const bool has_post = FORM <= kFormToken || (FORM >= kFormAny && a.w_post);
     const bool has_pre = FORM < kFormAny || a.w_pre;
@@ -377,24 +382,27 @@ norm_bwd_kernel(const NormArgs a) {
     const T* fy = static_cast<const T*>(a.y) + start;
     int frow = me.row;
     auto fetch = [&](uint4* to) {
-        if (frow < a.T) {
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                if (!in[p]) continue;
-                if (has_pre) {
-                    copy_ahead(to + (4 * p) * 32, fx + p * HOP);
-                    copy_ahead(to + (4 * p + 1) * 32, fh + p * HOP);
+        for (int r = 0; r < R; ++r, to += 4 * P * 32) {
+            if (frow < a.T) {
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    if (!in[p]) continue;
+                    if (has_pre) {
+                        copy_ahead(to + (4 * p) * 32, fx + p * HOP);
+                        copy_ahead(to + (4 * p + 1) * 32, fh + p * HOP);
+                    }
+                    if (has_up) copy_ahead(to + (4 * p + 2) * 32, fg + p * HOP);
+                    if (has_y) copy_ahead(to + (4 * p + 3) * 32, fy + p * HOP);
                 }
-                if (has_up) copy_ahead(to + (4 * p + 2) * 32, fg + p * HOP);
-                if (has_y) copy_ahead(to + (4 * p + 3) * 32, fy + p * HOP);
             }
+            frow += me.stride;
+            fx += step;
+            fh += step;
+            fg += step;
+            fy += step;
         }
         copy_commit();
-        frow += me.stride;
-        fx += step;
-        fh += step;
-        fg += step;
-        fy += step;
     };
 #pragma unroll
     for (int s = 0; s < S; ++s) fetch(me.ring + s * Q * 32);
@@ -407,121 +415,143 @@ norm_bwd_kernel(const NormArgs a) {
     for (int p = 0; p < P; ++p)
 #pragma unroll
         for (int i = 0; i < N; ++i) acc_pre[p][i] = acc_post[p][i] = 0.f;
-    RowGate<T, P, FORM> row_gate, ahead;
-    ahead.load(a, me.row, me.col, in);
+    RowGate<T, P, FORM> row_gate[R], ahead[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) ahead[r].load(a, me.row + r * me.stride, me.col, in);
     T* dx = static_cast<T*>(a.out0) + start;
     T* dy = static_cast<T*>(a.out1) + start;
     int stage = 0;
-    for (int row = me.row; row < a.T; row += me.stride, dx += step, dy += step) {
+    for (int row = me.row; row < a.T; row += R * me.stride, dx += R * step, dy += R * step) {
         uint4* slot = me.ring + stage * Q * 32;
         copy_wait<S - 1>();
-        Vec16<T> xv[P], hv[P], yv[P], gv[P];
-        float s[3] = {0.f, 0.f, 0.f};
+        Vec16<T> xv[R][P], hv[R][P], yv[R][P], gv[R][P];
+        float s[3 * R];
+        bool live[R];
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            if (!in[p]) continue;
-            float f[N];
-            if (has_pre) {
-                float h[N], w[N];
-                xv[p] = *reinterpret_cast<Ptr>(slot + (4 * p) * 32);
-                hv[p] = *reinterpret_cast<Ptr>(slot + (4 * p + 1) * 32);
-                pre.get(p, me.col, w);
-                widen(xv[p], f);
-                widen(hv[p], h);
+        for (int r = 0; r < R; ++r) {
+            live[r] = r == 0 || row + r * me.stride < a.T;
+            s[3 * r] = s[3 * r + 1] = s[3 * r + 2] = 0.f;
+            if (!live[r]) continue;
+            const uint4* from = slot + 4 * P * 32 * r;
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    s[0] = fmaf(f[i], f[i], s[0]);
-                    s[1] = fmaf(h[i] * w[i], f[i], s[1]);
+            for (int p = 0; p < P; ++p) {
+                if (!in[p]) continue;
+                float f[N];
+                if (has_pre) {
+                    float h[N], w[N];
+                    xv[r][p] = *reinterpret_cast<Ptr>(from + (4 * p) * 32);
+                    hv[r][p] = *reinterpret_cast<Ptr>(from + (4 * p + 1) * 32);
+                    pre.get(p, me.col, w);
+                    widen(xv[r][p], f);
+                    widen(hv[r][p], h);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        s[3 * r] = fmaf(f[i], f[i], s[3 * r]);
+                        s[3 * r + 1] = fmaf(h[i] * w[i], f[i], s[3 * r + 1]);
+                    }
                 }
-            }
-            if (has_up) gv[p] = *reinterpret_cast<Ptr>(slot + (4 * p + 2) * 32);
-            if (has_y) {
-                yv[p] = *reinterpret_cast<Ptr>(slot + (4 * p + 3) * 32);
-                widen(yv[p], f);
+                if (has_up) gv[r][p] = *reinterpret_cast<Ptr>(from + (4 * p + 2) * 32);
+                if (has_y) {
+                    yv[r][p] = *reinterpret_cast<Ptr>(from + (4 * p + 3) * 32);
+                    widen(yv[r][p], f);
 #pragma unroll
-                for (int i = 0; i < N; ++i) s[2] = fmaf(f[i], f[i], s[2]);
+                    for (int i = 0; i < N; ++i) s[3 * r + 2] = fmaf(f[i], f[i], s[3 * r + 2]);
+                }
             }
         }
         fetch(slot);
         stage = stage + 1 == S ? 0 : stage + 1;
-        row_gate = ahead;
-        ahead.load(a, row + me.stride, me.col, in);
-        if (has_pre || has_post) row_sum<3, WARP, WIDE>(s, s_red[0], me.warps);
-        const float r = rsqrtf(s[0] * inv_d + eps);
-        const float rrc = s[1] * inv_d * r * r * r;             // r^2 c
-        const float sy = has_post ? rsqrtf(s[2] * inv_d + eps) : 1.f;
-        const float gate_t = row_gate.token;                    // 1 unless the gate is the token's
-        float v[P][N], n[WIDE ? 1 : P][N], z[1] = {0.f};      // wide rows: n is formed again, no room
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            if (!in[p]) continue;
-            float f[N], g[N];
-#pragma unroll
-            for (int i = 0; i < N; ++i) g[i] = 0.f;
-            if (has_up) widen(gv[p], g);
-            if (has_pre) {
-                float h[N], w[N];
-                pre.get(p, me.col, w);
-                widen(xv[p], f);
-                widen(hv[p], h);
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    acc_pre[p][i] = fmaf(h[i] * f[i], r, acc_pre[p][i]);
-                    g[i] = fmaf(h[i] * w[i], r, g[i]);
-                    g[i] = fmaf(f[i], -rrc, g[i]);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < N; ++i) f[i] = res * g[i];
-            store_piece<T>(dx + p * HOP, f);
-            if (!has_y) continue;
-            float w[N];
-            post.get(p, me.col, w);
-            float(&np)[N] = n[WIDE ? 0 : p];
-            widen(yv[p], np);
-#pragma unroll
-            for (int i = 0; i < N; ++i) np[i] *= sy;
-            if (full) {
-                float gate[N], dg[N];
-                widen(row_gate.full[full ? p : 0], gate);
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    dg[i] = g[i] * w[i] * np[i];
-                    g[i] *= gate[i];
-                }
-                store_piece<T>(static_cast<T*>(a.dgate) + (size_t)row * a.d + me.col + p * HOP, dg);
-            }
-            if (token) {
-#pragma unroll
-                for (int i = 0; i < N; ++i) acc_post[p][i] = fmaf(gate_t * g[i], np[i], acc_post[p][i]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) acc_post[p][i] = fmaf(g[i], np[i], acc_post[p][i]);
-            }
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                v[p][i] = g[i] * w[i];
-                z[0] = fmaf(v[p][i], np[i], z[0]);
-            }
+        for (int r = 0; r < R; ++r) {
+            row_gate[r] = ahead[r];
+            ahead[r].load(a, row + (R + r) * me.stride, me.col, in);
         }
-        if (has_y) {
-            if (has_post || token) row_sum<1, WARP, WIDE>(z, s_red[1], me.warps);
-            const float k = gate_t * sy;
-            const float e = has_post ? -z[0] * inv_d : 0.f;
-            if (token && me.col == 0)
-                static_cast<float*>(a.dgate)[row] = z[0];
+        if (has_pre || has_post) row_sum<3 * R, WARP, WIDE>(s, s_red[0], me.warps);
+        float v[R][P][N], n[R][WIDE ? 1 : P][N], z[R], sy[R];   // wide rows: n is formed again, no room
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            z[r] = 0.f;
+            const float rx = rsqrtf(s[3 * r] * inv_d + eps);
+            const float rrc = s[3 * r + 1] * inv_d * rx * rx * rx;      // r^2 c
+            sy[r] = has_post ? rsqrtf(s[3 * r + 2] * inv_d + eps) : 1.f;
+            const float gate_t = row_gate[r].token;                     // 1 unless the gate is the token's
+            if (!live[r]) continue;
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 if (!in[p]) continue;
-                float(&np)[N] = n[WIDE ? 0 : p];
-                if (WIDE) {
-                    widen(yv[p], np);
+                float f[N], g[N];
 #pragma unroll
-                    for (int i = 0; i < N; ++i) np[i] *= sy;
+                for (int i = 0; i < N; ++i) g[i] = 0.f;
+                if (has_up) widen(gv[r][p], g);
+                if (has_pre) {
+                    float h[N], w[N];
+                    pre.get(p, me.col, w);
+                    widen(xv[r][p], f);
+                    widen(hv[r][p], h);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        acc_pre[p][i] = fmaf(h[i] * f[i], rx, acc_pre[p][i]);
+                        g[i] = fmaf(h[i] * w[i], rx, g[i]);
+                        g[i] = fmaf(f[i], -rrc, g[i]);
+                    }
                 }
 #pragma unroll
-                for (int i = 0; i < N; ++i) v[p][i] = k * fmaf(np[i], e, v[p][i]);
-                store_piece<T>(dy + p * HOP, v[p]);
+                for (int i = 0; i < N; ++i) f[i] = res * g[i];
+                store_piece<T>(dx + r * step + p * HOP, f);
+                if (!has_y) continue;
+                float w[N];
+                post.get(p, me.col, w);
+                float(&np)[N] = n[r][WIDE ? 0 : p];
+                widen(yv[r][p], np);
+#pragma unroll
+                for (int i = 0; i < N; ++i) np[i] *= sy[r];
+                if (full) {
+                    float gate[N], dg[N];
+                    widen(row_gate[r].full[full ? p : 0], gate);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        dg[i] = g[i] * w[i] * np[i];
+                        g[i] *= gate[i];
+                    }
+                    T* to = static_cast<T*>(a.dgate) + (size_t)(row + r * me.stride) * a.d;
+                    store_piece<T>(to + me.col + p * HOP, dg);
+                }
+                if (token) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) acc_post[p][i] = fmaf(gate_t * g[i], np[i], acc_post[p][i]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) acc_post[p][i] = fmaf(g[i], np[i], acc_post[p][i]);
+                }
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    v[r][p][i] = g[i] * w[i];
+                    z[r] = fmaf(v[r][p][i], np[i], z[r]);
+                }
+            }
+        }
+        if (has_y) {
+            if (has_post || token) row_sum<R, WARP, WIDE>(z, s_red[1], me.warps);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (!live[r]) continue;
+                const float k = row_gate[r].token * sy[r];
+                const float e = has_post ? -z[r] * inv_d : 0.f;
+                if (token && me.col == 0)
+                    static_cast<float*>(a.dgate)[row + r * me.stride] = z[r];
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    if (!in[p]) continue;
+                    float(&np)[N] = n[r][WIDE ? 0 : p];
+                    if (WIDE) {
+                        widen(yv[r][p], np);
+#pragma unroll
+                        for (int i = 0; i < N; ++i) np[i] *= sy[r];
+                    }
+#pragma unroll
+                    for (int i = 0; i < N; ++i) v[r][p][i] = k * fmaf(np[i], e, v[r][p][i]);
+                    store_piece<T>(dy + r * step + p * HOP, v[r][p]);
+                }
             }
         }
         // with one reduction per row its buffer comes around without a barrier in between
@@ -639,7 +669,7 @@ static r3_status check_norm(const r3_norm* s) {
 
 struct NormPlan {
     int pieces, threads, grid, stages;
-    bool warp, wide;
+    bool warp, wide, pair;
     size_t smem;
 };
 // Rows of up to 32 kNormPieces pieces: one warp each, several to a CTA.  Longer ones: a CTA with
@@ -653,8 +683,13 @@ static bool plan_norm(const r3_norm* s, bool bwd, NormPlan* p) {
     if (vecs > kNormMaxThreads * p->pieces) return false;
     p->threads = (vecs + 32 * p->pieces - 1) / (32 * p->pieces) * 32;
     p->wide = p->threads > kNormBwdThreads || p->pieces > kNormPieces;
+    // Backward, rows of more than half the threads of an SM: two at a time, so that one's arithmetic stands
+    // beside the other's reductions (8192 x 4096 bf16: 88 -> 82 us, 8192 x 2048 float32: 77 -> 70; shorter
+    // rows lose: 8192 x 2560 bf16: 55 -> 76, 16384 x 2048: 76 -> 79, 16384 x 1160 float32: 89 -> 111).
+    p->pair = bwd && p->threads > kNormBwdThreads / 2 && p->threads <= kNormPairThreads;
     const int resident = !bwd ? kNormFwdThreads
-                              : norm_bwd_threads(p->wide, s->act_dtype == R3_F32, s->gate_kind == R3_GATE_FULL);
+                              : norm_bwd_threads(p->wide, s->act_dtype == R3_F32, s->gate_kind == R3_GATE_FULL,
+                                                 p->pair ? 2 : 1);
     int rows = 1;
     if (p->warp) {
         // backward, one CTA fills the SM with rows, so that their sums of the weight gradients leave it
@@ -664,7 +699,7 @@ static bool plan_norm(const r3_norm* s, bool bwd, NormPlan* p) {
         if (rows < 1) rows = 1;
         p->threads = 32 * rows;
     }
-    const size_t per_row = (size_t)(bwd ? 4 : 2) * p->pieces * p->threads * 16;
+    const size_t per_row = (size_t)(bwd ? 4 : 2) * p->pieces * p->threads * 16 * (p->pair ? 2 : 1);
     p->stages = kNormStages * per_row <= (size_t)kNormRingBytes ? kNormStages : 1;
     p->smem = p->stages * per_row;
     int per_sm = resident / p->threads;
@@ -692,32 +727,34 @@ static r3_status launch_norm_kernel(const NormArgs& a, const NormPlan& p, cudaSt
     KERN<<<p.grid, p.threads, p.smem, cs>>>(a);
     return launch_status();
 }
-template <typename T, typename W, int P, bool WARP, bool WIDE, int S>
-static r3_status launch_norm(const NormArgs& a, const NormPlan& p, bool bwd, cudaStream_t cs) {
-    if (a.y && a.w_post && a.w_pre && a.gate_kind <= R3_GATE_TOKEN && (!bwd || a.dx_out)) {
-        if (a.gate_kind == R3_GATE_TOKEN)
-            return bwd ? launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, S, kFormToken>>(a, p, cs)
-                       : launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, S, kFormToken>>(a, p, cs);
-        return bwd ? launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, S, kFormUsual>>(a, p, cs)
-                   : launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, S, kFormUsual>>(a, p, cs);
+template <typename T, typename W, int P, bool WARP, bool WIDE, int S, int R, int FORM>
+static r3_status launch_norm_form(const NormArgs& a, const NormPlan& p, bool bwd, cudaStream_t cs) {
+    if constexpr (R == 1) {
+        if (!bwd) return launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, S, FORM>>(a, p, cs);
     }
-    if (!a.y)
-        return bwd ? launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, S, kFormFirst>>(a, p, cs)
-                   : launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, S, kFormFirst>>(a, p, cs);
+    return launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, S, R, FORM>>(a, p, cs);
+}
+template <typename T, typename W, int P, bool WARP, bool WIDE, int S, int R>
+static r3_status launch_norm(const NormArgs& a, const NormPlan& p, bool bwd, cudaStream_t cs) {
+    if (a.y && a.w_post && a.w_pre && a.gate_kind <= R3_GATE_TOKEN && (!bwd || a.dx_out))
+        return a.gate_kind == R3_GATE_TOKEN
+                   ? launch_norm_form<T, W, P, WARP, WIDE, S, R, kFormToken>(a, p, bwd, cs)
+                   : launch_norm_form<T, W, P, WARP, WIDE, S, R, kFormUsual>(a, p, bwd, cs);
+    if (!a.y) return launch_norm_form<T, W, P, WARP, WIDE, S, R, kFormFirst>(a, p, bwd, cs);
     if (a.gate_kind == R3_GATE_FULL)
-        return bwd ? launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, S, kFormFull>>(a, p, cs)
-                   : launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, S, kFormFull>>(a, p, cs);
-    return bwd ? launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, S, kFormAny>>(a, p, cs)
-               : launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, S, kFormAny>>(a, p, cs);
+        return launch_norm_form<T, W, P, WARP, WIDE, S, R, kFormFull>(a, p, bwd, cs);
+    return launch_norm_form<T, W, P, WARP, WIDE, S, R, kFormAny>(a, p, bwd, cs);
 }
 template <typename T, typename W>
 static r3_status launch_norm_size(const NormArgs& a, const NormPlan& p, bool bwd, cudaStream_t cs) {
     constexpr int P = kNormPieces, S = kNormStages;
-    if (p.warp) return launch_norm<T, W, P, true, false, S>(a, p, bwd, cs);
-    if (!p.wide) return launch_norm<T, W, P, false, false, S>(a, p, bwd, cs);
-    if (p.pieces == P) return launch_norm<T, W, P, false, true, S>(a, p, bwd, cs);
-    return p.stages > 1 ? launch_norm<T, W, 2 * P, false, true, S>(a, p, bwd, cs)
-                        : launch_norm<T, W, 2 * P, false, true, 1>(a, p, bwd, cs);
+    if (p.warp) return launch_norm<T, W, P, true, false, S, 1>(a, p, bwd, cs);
+    if (!p.wide)
+        return p.pair ? launch_norm<T, W, P, false, false, S, 2>(a, p, bwd, cs)
+                      : launch_norm<T, W, P, false, false, S, 1>(a, p, bwd, cs);
+    if (p.pieces == P) return launch_norm<T, W, P, false, true, S, 1>(a, p, bwd, cs);
+    return p.stages > 1 ? launch_norm<T, W, 2 * P, false, true, S, 1>(a, p, bwd, cs)
+                        : launch_norm<T, W, 2 * P, false, true, 1, 1>(a, p, bwd, cs);
 }
 static r3_status launch_norm_types(const r3_norm* s, const NormArgs& a, const NormPlan& p, bool bwd,
                                    cudaStream_t cs) {

@@ -122,6 +122,16 @@ def test_sizes(r3, act, wdt, T, d):
     check(r3, make(T, d, act, wdt, "none", False, True, first=True), branch_scale=1.0)
 
 
+@pytest.mark.parametrize("act,d", [(BF, 3592), (BF, 4096), (F32, 1992)])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("post,pre", [(True, True), (True, False), (False, True), (False, False)])
+def test_rows_worked_on_two_at_a_time(r3, act, d, kind, post, pre):
+    """Long rows, whose gradient takes two of a group's rows at once: no second row, one for one group
+    only, an odd number of rows for each."""
+    for T in (1, 149, 450):
+        check(r3, make(T, d, act, act, kind, post, pre))
+
+
 def test_largest_rows(r3):
     for d in (8200, 16384):
         check(r3, make(40, d, BF, F32, "channel", True, True))

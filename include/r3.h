@@ -583,7 +583,8 @@ typedef struct {
  *    config's lr and step, for a captured step that is replayed with new values.
  *  - A gradient element that is not finite makes its own weight and states NaN (an 8-bit state: the
  *    NaN code; the scale is that of the block's finite elements).
- * Two entries whose params overlap are refused; no other buffers may overlap.  No workspace. */
+ * Buffers that the step writes (params, masters, states, scales; of all entries) and that overlap are
+ * refused; no gradient may overlap one of them.  No workspace. */
 r3_status r3_adamw_step(const r3_adamw* config, const r3_adamw_tensor* tensors, int32_t n_tensors,
                         const float* grad_scale, const float* scalars, void* stream);
 
@@ -621,6 +622,7 @@ r3_status r3_normed_stack(const r3_shape* shape, int32_t L, const r3_block_norms
  * at the end), so that no more than that exists at a time.  expert_states (HOST) has 3 L entries, block
  * by block w_gate, w_up, w_down, as for r3_adamw_step; param must be the block's weights, grad is
  * ignored.  adamw, grad_scale and scalars as for r3_adamw_step, param_dtype R3_BF16, grad_dtype R3_F32.
+ * With T = 0 nothing is written and no step taken.
  * workspace: r3_normed_stack_train_workspace_bytes(shape, L). */
 size_t r3_normed_stack_train_workspace_bytes(const r3_shape* shape, int32_t L);
 r3_status r3_normed_stack_train(const r3_shape* shape, int32_t L, const r3_block_norms* norms,

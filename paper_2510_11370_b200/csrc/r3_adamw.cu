@@ -19,8 +19,8 @@
 // holds elements 4 l .. 4 l + 3 and 128 + 4 l .. 128 + 4 l + 3: every load and store of the warp covers
 // consecutive bytes.  With 8-bit states it holds 8 l .. 8 l + 7 and takes them out of a ring in shared
 // memory that the warp copies its blocks to ahead (16 bytes per lane and copy, so 4 or 5 copies, 6 loads
-// and 3 or 4 stores a block where 4-element pieces take twice as many).  The table of tensors travels in the kernel's
-// parameters: no workspace, no copy, and a captured launch keeps its own.
+// and 3 or 4 stores a block where 4-element pieces take twice as many).  The table of tensors travels in the
+// kernel's parameters: no workspace, no copy, and a captured launch keeps its own.
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -508,20 +508,33 @@ static r3_status check_adamw(const r3_adamw* c, const r3_adamw_tensor* ts, int32
     }
     return R3_OK;
 }
-// Two entries on the same memory would be updated at once, in no order.
-static r3_status check_distinct(const r3_adamw* c, const r3_adamw_tensor* ts, int32_t count) {
+// Two buffers on the same memory would be updated at once, in no order.
+r3_status check_adamw_distinct(const r3_adamw* c, const r3_adamw_tensor* ts, int32_t count) {
     try {
-        std::vector<std::pair<uintptr_t, uintptr_t>> r;
-        r.reserve(count);
-        const uintptr_t size = c->param_dtype == R3_BF16 ? 2 : 4;
-        for (int32_t i = 0; i < count; ++i)
-            if (ts[i].n > 0) {
-                const uintptr_t p = reinterpret_cast<uintptr_t>(ts[i].param);
-                r.emplace_back(p, p + (uintptr_t)ts[i].n * size);
-            }
-        std::sort(r.begin(), r.end());
-        for (size_t i = 1; i < r.size(); ++i)
-            if (r[i].first < r[i - 1].second) return R3_ERR_INVALID_ARG;
+        typedef std::pair<uintptr_t, uintptr_t> Range;
+        Range few[6 * kAdamSmall];                  // a short list takes no allocation
+        std::vector<Range> many(count > kAdamSmall ? (size_t)count * 6 : 0);
+        Range *const r = count > kAdamSmall ? many.data() : few, *end = r;
+        const int64_t size = c->param_dtype == R3_BF16 ? 2 : 4, state = c->state_bits == 8 ? 1 : 4;
+        auto add = [&](const void* p, int64_t bytes) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+            if (p) *end++ = {at, at + (uintptr_t)bytes};
+        };
+        for (int32_t i = 0; i < count; ++i) {
+            const r3_adamw_tensor& t = ts[i];
+            if (t.n == 0) continue;
+            add(t.param, t.n * size);
+            add(t.master, t.n * 4);
+            add(t.exp_avg, t.n * state);
+            add(t.exp_avg_sq, t.n * state);
+            if (c->state_bits != 8) continue;
+            const int64_t scales = (t.n + kAdamBlock - 1) / kAdamBlock * 4;
+            add(t.exp_avg_scale, scales);
+            add(t.exp_avg_sq_scale, scales);
+        }
+        if (!std::is_sorted(r, end)) std::sort(r, end);
+        for (const Range* q = r + 1; q < end; ++q)
+            if (q->first < q[-1].second) return R3_ERR_INVALID_ARG;
         return R3_OK;
     } catch (...) {                                 // out of host memory
         return R3_ERR_INVALID_ARG;
@@ -533,7 +546,7 @@ r3_status check_adamw_call(const r3_adamw* config, const r3_adamw_tensor* tensor
     const r3_status st = check_adamw(config, tensors, n_tensors);
     if (st != R3_OK) return st;
     if (!aligned(grad_scale, 4) || !aligned(scalars, 4)) return R3_ERR_INVALID_ARG;
-    return check_distinct(config, tensors, n_tensors);
+    return check_adamw_distinct(config, tensors, n_tensors);
 }
 
 template <typename P, typename G, bool MASTER, bool BITS8, int CAP>

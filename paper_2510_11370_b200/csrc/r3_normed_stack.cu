@@ -179,6 +179,7 @@ extern "C" r3_status r3_normed_stack_train(const r3_shape* shape, int32_t L, con
             if (!block_states(l, e)) return R3_ERR_INVALID_ARG;
             if ((st = r3::check_adamw_call(adamw, e, 3, grad_scale, scalars)) != R3_OK) return st;
         }
+        if ((st = r3::check_adamw_distinct(adamw, expert_states, 3 * L)) != R3_OK) return st;
     }
     if (shape->T == 0) return R3_OK;
     if (!x0 || !w_router || !idx || !w_gate || !w_up || !w_down || !dy || !x_out || !dlogits || !dx0 ||

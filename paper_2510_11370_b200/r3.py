@@ -717,8 +717,8 @@ class AdamW:
     of float32 tensors.  States are made (zero) or given as lists: float32, or with state_bits=8
     float8_e4m3fn codes plus one float32 scale per 256 elements (exp_avg_sq then holds the root of
     the second moment).  weight_decay: a number, or one per tensor.  The handle keeps its tensors
-    alive; set_grads() exchanges the gradients, and without any (None) the handle is one for
-    normed_stack_train, which supplies them."""
+    memory alive (one whose .data is exchanged needs a new handle); set_grads() exchanges the gradients,
+    and without any (None) the handle is one for normed_stack_train, which supplies them."""
 
     def __init__(self, params, grads=None, *, masters=None, exp_avg=None, exp_avg_sq=None,
                  exp_avg_scale=None, exp_avg_sq_scale=None, state_bits=32, betas=(0.9, 0.95),
@@ -757,6 +757,7 @@ class AdamW:
             raise ValueError("scales: only for 8-bit states")
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(sizes)
         self._table = (AdamWTensor * len(sizes))()
+        self._memory = []                        # what the table's addresses point to
         self._fill("param", self.params, sizes, dtype)
         self._fill("master", self.masters, sizes, torch.float32)
         self._fill("exp_avg", self.exp_avg, sizes, kind)
@@ -783,6 +784,8 @@ class AdamW:
                 raise ValueError(f"{field}[{i}]: {t.numel()} elements, expected {n}")
             _expect(f"{field}[{i}]", t, t.shape, dtype, self._dev)
             setattr(row, field, _ptr(t).value)
+        if field != "grad":
+            self._memory += [t.detach() for t in tensors]
 
     def set_grads(self, grads):
         """Exchanges the gradients of the steps to come."""
@@ -818,10 +821,11 @@ def _block_norms(s, L, w_pre, w_post, gate, eps, residual_scale, branch_scale, d
         raise ValueError("w_pre: expected a float32 or bfloat16 tensor")
     n = BlockNorms(w_dtype=_ACT[w_pre.dtype], eps=eps, residual_scale=residual_scale,
                    branch_scale=branch_scale)
+    new = torch.empty if s.T else torch.zeros    # an empty batch's sums are written by nothing
     made = []
     for name, t, grad in (("w_pre", w_pre, "dw_pre"), ("w_post", w_post, "dw_post"), ("gate", gate, "dgate")):
         setattr(n, name, _arg(name, t, (L, s.d), w_pre.dtype, dev))
-        g = torch.empty((L, s.d), dtype=torch.float32, device=dev) if grads and t is not None else None
+        g = new((L, s.d), dtype=torch.float32, device=dev) if grads and t is not None else None
         setattr(n, grad, None if g is None else g.data_ptr())
         made.append(g)
     return n, made
@@ -835,12 +839,14 @@ def normed_stack(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down, *, w
     Returns x_L [T, d]."""
     dev = _device_of("x0", x0)
     n, _ = _block_norms(s, L, w_pre, w_post, gate, eps, residual_scale, branch_scale, dev, False)
+    x0 = _arg("x0", x0, (s.T, s.d), _act_dtype(s), dev)
     if x_out is None:
         x_out = torch.empty((s.T, s.d), dtype=_act_dtype(s), device=dev)
     if ws is None:
         ws = workspace(lib.r3_normed_stack_workspace_bytes(ctypes.byref(s)), dev)
-    _check(lib.r3_normed_stack(ctypes.byref(s), L, ctypes.byref(n), _ptr(x0), _ptr(w_router), _ptr(idx),
-                               _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(x_out), _ptr(ws),
+    _check(lib.r3_normed_stack(ctypes.byref(s), L, ctypes.byref(n), x0, _ptr(w_router), _ptr(idx),
+                               _ptr(w_gate), _ptr(w_up), _ptr(w_down),
+                               _arg("x_out", x_out, (s.T, s.d), _act_dtype(s), dev), _ptr(ws),
                                ws.numel(), _ptr(dev_status), _stream(stream)))
     return x_out
 
@@ -853,14 +859,17 @@ def normed_stack_train(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down
     dw_router [L, E, d], dw_pre, dw_post or None, dgate or None), and with expert_grads also (dw_gate,
     dw_up, dw_down).  With optimiser, an AdamW over [w_gate[0], w_up[0], w_down[0], w_gate[1], ..] without
     gradients of its own, every block's expert weights take step `step` with rate `lr` as soon as their
-    gradients are there, and only one block's gradients exist at a time (block 0's are returned)."""
+    gradients are there, and only one block's gradients exist at a time (block 0's are returned).  Without
+    rows the gradients are zero and no step is taken."""
     dev = _device_of("x0", x0)
     n, dnorms = _block_norms(s, L, w_pre, w_post, gate, eps, residual_scale, branch_scale, dev, True)
+    x0, dy = (_arg(name, t, (s.T, s.d), _act_dtype(s), dev) for name, t in (("x0", x0), ("dy", dy)))
     f32 = dict(dtype=torch.float32, device=dev)
     x_out = torch.empty((s.T, s.d), dtype=_act_dtype(s), device=dev)
     dx0 = torch.empty((s.T, s.d), dtype=_act_dtype(s), device=dev)
+    new = torch.empty if s.T else torch.zeros
     dlogits = torch.empty((L, s.T, s.E), **f32)
-    dw_r = torch.empty((L, s.E, s.d), **f32)
+    dw_r = new((L, s.E, s.d), **f32)
     dws, config, table = (None, None, None), None, None
     if optimiser is not None:
         if len(optimiser.params) != 3 * L:
@@ -870,13 +879,13 @@ def normed_stack_train(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down
         table = optimiser._table
     if expert_grads or optimiser is not None:
         lead = () if optimiser is not None else (L,)
-        dws = (torch.empty(lead + (s.E, s.F, s.d), **f32), torch.empty(lead + (s.E, s.F, s.d), **f32),
-               torch.empty(lead + (s.E, s.d, s.F), **f32))
+        dws = (new(lead + (s.E, s.F, s.d), **f32), new(lead + (s.E, s.F, s.d), **f32),
+               new(lead + (s.E, s.d, s.F), **f32))
     if ws is None:
         ws = workspace(lib.r3_normed_stack_train_workspace_bytes(ctypes.byref(s), L), dev)
     _check(lib.r3_normed_stack_train(
-        ctypes.byref(s), L, ctypes.byref(n), _ptr(x0), _ptr(w_router), _ptr(idx), _ptr(w_gate),
-        _ptr(w_up), _ptr(w_down), _ptr(dy), _ptr(x_out), _ptr(dlogits), _ptr(dx0), _ptr(dw_r),
+        ctypes.byref(s), L, ctypes.byref(n), x0, _ptr(w_router), _ptr(idx), _ptr(w_gate),
+        _ptr(w_up), _ptr(w_down), dy, _ptr(x_out), _ptr(dlogits), _ptr(dx0), _ptr(dw_r),
         _ptr(dws[0]), _ptr(dws[1]), _ptr(dws[2]), None if config is None else ctypes.addressof(config),
         None if table is None else ctypes.addressof(table),
         _arg("grad_scale", grad_scale, (1,), torch.float32, dev),

@@ -50,6 +50,23 @@ def test_refused(r3, kw):
     assert call(r3, **kw) == r3.R3_ERR_INVALID_ARG
 
 
+A, B = 1 << 20, 100 * 4                                        # the first entry's param, its bytes
+
+
+@pytest.mark.parametrize("kw", [
+    dict(tensors=[{}, dict(exp_avg=3 << 20)]),                            # one state for two tensors
+    dict(tensors=[{}, dict(exp_avg_sq=(4 << 20) + 384)]),
+    dict(tensors=[dict(exp_avg_sq=3 << 20)]),                             # both states of a tensor
+    dict(tensors=[dict(exp_avg=A + 16 * (B // 16 - 1))]),                 # the param's last elements
+    dict(param_dtype=1, master=1, tensors=[dict(master=9 << 21), dict(master=9 << 21)]),
+    dict(state_bits=8, tensors=[dict(exp_avg_scale=5 << 20, exp_avg_sq_scale=5 << 20)]),
+    dict(state_bits=8, n=2, tensors=[dict(n=257, exp_avg_scale=5 << 20, exp_avg_sq_scale=6 << 20),
+                                     dict(n=1, exp_avg_scale=(5 << 20) + 4, exp_avg_sq_scale=7 << 20)]),
+])
+def test_shared_memory_is_refused(r3, kw):
+    assert call(r3, **kw) == r3.R3_ERR_INVALID_ARG
+
+
 def test_null_and_nothing_to_do(r3):
     assert r3.lib.r3_adamw_step(None, None, 0, None, None, None) == r3.R3_ERR_INVALID_ARG
     assert call(r3, tensors=[]) == r3.R3_OK

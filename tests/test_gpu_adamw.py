@@ -286,3 +286,13 @@ def test_python_refusals(r3):
         r3.AdamW([w[1:]], [g[1:]]).step(1, 0.1)                        # 4-byte aligned only
     with pytest.raises(r3.R3Error):
         r3.AdamW([w], [g]).step(0, 0.1)                                # steps count from 1
+
+
+def test_exchanged_data_leaves_the_handle_its_memory(r3):
+    p = torch.nn.Parameter(torch.ones(1000, device="cuda"))
+    g = torch.ones(1000, device="cuda")
+    o = r3.AdamW([p], [g])
+    p.data = torch.zeros(1000, device="cuda")
+    others = [torch.full((1000,), 5.0, device="cuda") for _ in range(8)]
+    o.step(1, 0.1)
+    assert all((t == 5.0).all() for t in others) and not p.any()

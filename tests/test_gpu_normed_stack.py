@@ -246,3 +246,35 @@ def test_wrong_optimisers_are_refused(r3):
     with pytest.raises(r3.R3Error):
         run(handle(r3, [e.clone() for e in ex], 2))           # other tensors
     assert all(torch.equal(a, b) for a, b in zip(ex, keep))
+
+
+def test_without_rows(r3):
+    """A rank whose batch is empty: gradients of zero, untouched weights and states."""
+    T, d, E, K, F, L = 8, 64, 4, 2, 64, 2
+    w, x0, dy, w_r, idx, ex, norms = build(T, d, E, K, F, L)
+    s = r3.make_shape(0, d, E, K, F)
+    o = handle(r3, ex, L, state_bits=32)
+    before = [e.clone() for e in ex]
+    none = torch.empty((0, d), dtype=BF, device="cuda")
+    junk = torch.full((1 << 20,), 7.0, device="cuda")         # what an allocation may find
+    del junk
+    assert r3.normed_stack(s, L, none, w_r, idx[:, :0], *ex, **norms).shape == (0, d)
+    for kw in (dict(expert_grads=True), dict(optimiser=o, step=1, lr=0.1)):
+        out = r3.normed_stack_train(s, L, none, w_r, idx[:, :0], *ex, none, **kw, **norms)
+        for t in out:
+            assert not t.float().any()
+    for p, q in zip(ex, before):
+        assert torch.equal(p, q)
+    assert not any(t.any() for t in o.exp_avg + o.exp_avg_sq)
+
+
+def test_wrong_rows_are_refused(r3):
+    w, x0, dy, w_r, idx, ex, norms = build(12, 64, 4, 2, 64, 1)
+    s = r3.shape_of(w)
+    for bad in (x0[:11], x0.float(), x0.cpu()):
+        with pytest.raises(ValueError):
+            r3.normed_stack(s, 1, bad, w_r, idx, *ex, **norms)
+        with pytest.raises(ValueError):
+            r3.normed_stack_train(s, 1, x0, w_r, idx, *ex, bad, **norms)
+    with pytest.raises(ValueError):
+        r3.normed_stack(s, 1, x0, w_r, idx, *ex, x_out=x0[:11], **norms)

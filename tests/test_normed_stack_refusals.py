@@ -100,3 +100,7 @@ def test_bad_optimisers(r3):
     assert train(r3, adamw=config(), states=states(n=block - 8)) == bad
     assert train(r3, adamw=config(), states=states(param=1 << 28)) == bad           # not the block's weights
     assert train(r3, adamw=config(), states=states(exp_avg=None)) == bad
+
+    shared = states()
+    shared[3].exp_avg = shared[0].exp_avg                                           # another block's state
+    assert train(r3, adamw=config(), states=shared) == bad

@@ -849,9 +849,18 @@ extern "C" r3_status r3_token_logprobs(const r3_logits* shape, const void* logit
     // Threads per row: with more than its pieces keep busy the reductions at a row's end cost more than
     // its loads, and many small CTAs on an SM end at different times, which keeps the loads flowing
     // (8192 rows of bf16: 6000 columns 34.7 us at 128 threads, 26.6 at 32; 12000 columns 61.4 at 256,
-    // 45.1 at 128; 151936 columns 381 at 512, 352 at 256.  880 rows of 151936 with 20 alternatives: 72 at
-    // 256, 98 at 128).
-    const int threads = row_bytes <= 16384 ? 32 : row_bytes <= 49152 ? 128 : 256;
+    // 45.1 at 128; 151936 columns with 5 alternatives 429 at 256, 410 at 128).  Long rows that are few enough
+    // for whole waves to count: 256 threads where those take less of them, a wave of 128 holding twice the
+    // rows and lasting twice as long (50257 columns of float32 with 5 alternatives: 300 rows 18.6 at 256,
+    // 24.7 at 128; 600 rows 37.1 and 30.4; 900 41.4 and 37.1; 1200 58.0 and 60.1; 2048 83.8 and 74.6).
+    auto waves = [&](int nt) {
+        const int resident = r3::logprob_ctas(nt) * r3::sm_count();
+        return (a.T + resident - 1) / resident;
+    };
+    const int threads = row_bytes <= 16384                                ? 32
+                        : row_bytes <= 49152                              ? 128
+                        : waves(128) <= 4 && waves(256) < 2 * waves(128) ? 256
+                                                                          : 128;
     // Few rows: a cluster of CTAs shares one, as long as they all run at once and a thread has two
     // pieces or more.
     a.split = 1;

@@ -16,7 +16,7 @@
 // the entropy, 6.2 instructions (10 before the rounds without bounds checks, the widening by shift and
 // mask and the sums in two lanes).  8192 x 151936 bf16 with entropy, a tenth of the rows skipped: 342 us =
 // the measured copy bandwidth; launched back to back for seconds the power cap takes the SM clock to 1.55
-// GHz and the exponentials alone need 290 of 387 us.  One row per CTA and many CTAs: CTAs that walked
+// GHz and the exponentials alone need 290 of 354 to 370 us.  One row per CTA and many CTAs: CTAs that walked
 // over rows, the next row's first pieces on their way early, took 444 us where this form took 383.
 // Few rows: up to eight CTAs of a cluster share one (16 x 131072 bf16: 4.4 us, with 20 alternatives 9.5,
 // of which the alternatives' four barriers, second look at the row and exchange take 5).

@@ -656,11 +656,16 @@ def norm_residual(x, y=None, *, w_post=None, gate=None, w_pre=None, eps=1e-6, re
     src = _arg("x", x, shape, act, dev)
     if y is not None and x_out is None:
         x_out = torch.empty_like(x)
+        at_x = x_out.data_ptr()
+    else:
+        at_x = _arg("x_out", x_out, shape, act, dev)
     if w_pre is not None and h is None:
         h = torch.empty_like(x)
+        at_h = h.data_ptr()
+    else:
+        at_h = _arg("h", h, shape, act, dev)
     _check(lib.r3_norm_residual(ctypes.byref(s), src, _arg("y", y, shape, act, dev), post, gate, pre,
-                                _arg("x_out", x_out, shape, act, dev),
-                                _arg("h", h, shape, act, dev), _stream(stream)))
+                                at_x, at_h, _stream(stream)))
     return x_out, h
 
 
@@ -679,8 +684,14 @@ def norm_residual_bwd(x_out, y, dx_out, dh=None, *, w_post=None, gate=None, w_pr
            (("x_out", x_out), ("y", y), ("dx_out", dx_out), ("dh", dh))]
     if dx is None:
         dx = torch.empty_like(like)
+        at_dx = dx.data_ptr()
+    else:
+        at_dx = _arg("dx", dx, shape, act, dev)
     if y is not None and dy is None:
         dy = torch.empty_like(like)
+        at_dy = dy.data_ptr()
+    else:
+        at_dy = _arg("dy", dy, shape, act, dev)
     # the float32 sums over tokens are the rows of one buffer (d is a multiple of 8: aligned)
     channel = s.gate_kind == R3_GATE_CHANNEL
     dw_post = dgate = dw_pre = None
@@ -699,8 +710,8 @@ def norm_residual_bwd(x_out, y, dx_out, dh=None, *, w_post=None, gate=None, w_pr
         ws = workspace(lib.r3_norm_residual_bwd_workspace_bytes(ctypes.byref(s)), dev)
     _check(lib.r3_norm_residual_bwd(
         ctypes.byref(s), src[0], src[1], post, gate_at, pre, src[2], src[3],
-        _arg("dx", dx, shape, act, dev), _arg("dy", dy, shape, act, dev),
-        None if dw_post is None else dw_post.data_ptr(), None if dgate is None else dgate.data_ptr(),
+        at_dx, at_dy, None if dw_post is None else dw_post.data_ptr(),
+        None if dgate is None else dgate.data_ptr(),
         None if dw_pre is None else dw_pre.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)))
     return dx, dy, dw_post, dgate, dw_pre
 
@@ -931,21 +942,22 @@ def token_logprobs(logits, token_ids=None, *, temperature=1.0, n_top=0, want_ent
     rows may lie apart).  Returns (logp [T] or None without token_ids, entropy [T] or None,
     stats [T, 2] or None, top_ids [T, n_top] int32 or None, top_logp [T, n_top] or None).  A row
     with a negative token id is skipped: zeros, top_ids -1."""
-    s, ptr, ids, _ = _logits_shape(logits, token_ids, temperature)
-    new, f32, T = logits.new_empty, torch.float32, s.T
+    s, ptr, ids, dev = _logits_shape(logits, token_ids, temperature)
+    new, f32, T = torch.empty_strided, torch.float32, s.T    # the cheapest of torch's allocating calls
     logp = entropy = stats = top_ids = top_logp = None
     at = [None] * 5                              # the outputs' addresses
     if ids is not None:
-        logp = new((T,), dtype=f32)
+        logp = new((T,), (1,), dtype=f32, device=dev)
         at[0] = logp.data_ptr()
     if want_entropy:
-        entropy = new((T,), dtype=f32)
+        entropy = new((T,), (1,), dtype=f32, device=dev)
         at[1] = entropy.data_ptr()
     if want_stats:
-        stats = new((T, 2), dtype=f32)
+        stats = new((T, 2), (2, 1), dtype=f32, device=dev)
         at[2] = stats.data_ptr()
     if n_top > 0:
-        top_ids, top_logp = new((T, n_top), dtype=torch.int32), new((T, n_top), dtype=f32)
+        top_ids = new((T, n_top), (n_top, 1), dtype=torch.int32, device=dev)
+        top_logp = new((T, n_top), (n_top, 1), dtype=f32, device=dev)
         at[3], at[4] = top_ids.data_ptr(), top_logp.data_ptr()
     _check(lib.r3_token_logprobs(ctypes.byref(s), ptr, ids, at[0], at[1], at[2], n_top, at[3], at[4],
                                  None if dev_status is None else _ptr(dev_status), _stream(stream)))
@@ -959,7 +971,7 @@ def token_logprobs_bwd(logits, token_ids, stats, dlogp, *, entropy=None, dentrop
     themselves, for a gradient in place)."""
     s, ptr, ids, dev = _logits_shape(logits, token_ids, temperature)
     if dlogits is None:
-        dlogits = logits.new_empty((s.T, s.V))
+        dlogits = torch.empty_strided((s.T, s.V), (s.V, 1), dtype=logits.dtype, device=dev)
     else:
         _expect("dlogits", dlogits, (s.T, s.V), logits.dtype, dev)
     out, ld_out = _rows("dlogits", dlogits)

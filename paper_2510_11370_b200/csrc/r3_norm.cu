@@ -200,22 +200,49 @@ __device__ __forceinline__ NormPlace norm_place(uint4* ring) {
     return t;
 }
 
-// A row's own gate (one value, or one per element), loaded a row ahead.
+// A row's gate per element, loaded a row ahead.
 template <typename T, int P, int FORM> struct RowGate {
-    float token;
     Vec16<T> full[FORM == kFormFull ? P : 1];
     __device__ __forceinline__ void load(const NormArgs& a, int row, int col, const bool (&in)[P]) {
-        constexpr int HOP = 32 * Vec16<T>::N;
-        token = 1.f;
-        if (FORM == kFormUsual || FORM == kFormFirst || row >= a.T) return;
-        if (FORM == kFormToken || (FORM == kFormAny && a.gate_kind == R3_GATE_TOKEN))
-            token = static_cast<const float*>(a.gate)[row];
         if constexpr (FORM == kFormFull) {
+            constexpr int HOP = 32 * Vec16<T>::N;
+            if (row >= a.T) return;
             const T* g = static_cast<const T*>(a.gate) + (size_t)row * a.d + col;
 #pragma unroll
             for (int p = 0; p < P; ++p)
                 if (in[p]) full[p] = *reinterpret_cast<const Vec16<T>*>(g + p * HOP);
         }
+    }
+};
+// The gates of a group's tokens: lane l holds that of the l-th of its next 32 rows, and the 32 behind them
+// are on their way.
+struct TokenGates {
+    const float* gate;
+    long long row, step;                            // the lane's row among the 32 after `next`
+    float mine, next;
+    int rows, at;
+    __device__ __forceinline__ float fetch() {
+        const float g = row < rows ? gate[row] : 1.f;
+        row += step;
+        return g;
+    }
+    __device__ __forceinline__ void init(const NormArgs& a, const NormPlace& me) {
+        gate = static_cast<const float*>(a.gate);
+        rows = a.T;
+        row = me.row + (long long)me.lane * me.stride;
+        step = 32LL * me.stride;
+        at = 0;
+        mine = fetch();
+        next = fetch();
+    }
+    __device__ __forceinline__ float take() {
+        const float g = __shfl_sync(0xffffffffu, mine, at);
+        if (++at == 32) {
+            at = 0;
+            mine = next;
+            next = fetch();
+        }
+        return g;
     }
 };
 
@@ -264,6 +291,8 @@ norm_fwd_kernel(const NormArgs a) {
     if (has_pre) pre.init(a.w_pre, nullptr, 1.f, me.col, in);
     RowGate<T, P, FORM> gate, ahead;
     ahead.load(a, me.row, me.col, in);
+    TokenGates gates;
+    if (token) gates.init(a, me);
     T* x_out = static_cast<T*>(a.out0) + start;
     T* h_out = static_cast<T*>(a.out1) + start;
     int stage = 0;
@@ -296,7 +325,7 @@ norm_fwd_kernel(const NormArgs a) {
             r = rsqrtf(s[0] * inv_d + eps);
         }
         if (has_y) {
-            if (token) r *= gate.token;
+            if (token) r *= gates.take();
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 if (!in[p]) continue;
@@ -418,6 +447,8 @@ norm_bwd_kernel(const NormArgs a) {
     RowGate<T, P, FORM> row_gate[R], ahead[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) ahead[r].load(a, me.row + r * me.stride, me.col, in);
+    TokenGates gates;
+    if (token) gates.init(a, me);
     T* dx = static_cast<T*>(a.out0) + start;
     T* dy = static_cast<T*>(a.out1) + start;
     int stage = 0;
@@ -467,14 +498,15 @@ norm_bwd_kernel(const NormArgs a) {
             ahead[r].load(a, row + (R + r) * me.stride, me.col, in);
         }
         if (has_pre || has_post) row_sum<3 * R, WARP, WIDE>(s, s_red[0], me.warps);
-        float v[R][P][N], n[R][WIDE ? 1 : P][N], z[R], sy[R];   // wide rows: n is formed again, no room
+        // wide rows: n is formed again, no room
+        float v[R][P][N], n[R][WIDE ? 1 : P][N], z[R], sy[R], gate_t[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             z[r] = 0.f;
             const float rx = rsqrtf(s[3 * r] * inv_d + eps);
             const float rrc = s[3 * r + 1] * inv_d * rx * rx * rx;      // r^2 c
             sy[r] = has_post ? rsqrtf(s[3 * r + 2] * inv_d + eps) : 1.f;
-            const float gate_t = row_gate[r].token;                     // 1 unless the gate is the token's
+            gate_t[r] = token ? gates.take() : 1.f;
             if (!live[r]) continue;
 #pragma unroll
             for (int p = 0; p < P; ++p) {
@@ -518,7 +550,7 @@ norm_bwd_kernel(const NormArgs a) {
                 }
                 if (token) {
 #pragma unroll
-                    for (int i = 0; i < N; ++i) acc_post[p][i] = fmaf(gate_t * g[i], np[i], acc_post[p][i]);
+                    for (int i = 0; i < N; ++i) acc_post[p][i] = fmaf(gate_t[r] * g[i], np[i], acc_post[p][i]);
                 } else {
 #pragma unroll
                     for (int i = 0; i < N; ++i) acc_post[p][i] = fmaf(g[i], np[i], acc_post[p][i]);
@@ -535,7 +567,7 @@ norm_bwd_kernel(const NormArgs a) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 if (!live[r]) continue;
-                const float k = row_gate[r].token * sy[r];
+                const float k = gate_t[r] * sy[r];
                 const float e = has_post ? -z[r] * inv_d : 0.f;
                 if (token && me.col == 0)
                     static_cast<float*>(a.dgate)[row + r * me.stride] = z[r];

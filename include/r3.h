@@ -517,7 +517,7 @@ typedef struct {
  * x [T,d] the residual stream, y [T,d] the block's output.  h is formed from the float32 x_out, each
  * output is rounded once.  y NULL (with w_post, gate and x_out NULL): in front of the first block,
  * h = the norm of x.  w_pre and h NULL: behind the last block.  x_out may be x's buffer, and h y's.
- * d up to 16384 for bf16 and 8192 for f32 (R3_ERR_UNSUPPORTED beyond).  No workspace. */
+ * T up to 2^30; d up to 16384 for bf16 and 8192 for f32 (R3_ERR_UNSUPPORTED beyond).  No workspace. */
 r3_status r3_norm_residual(const r3_norm* shape, const void* x, const void* y, const void* w_post,
                            const void* gate, const void* w_pre, void* x_out, void* h, void* stream);
 
@@ -614,8 +614,9 @@ r3_status r3_normed_stack(const r3_shape* shape, int32_t L, const r3_block_norms
 
 /* Forward and the exact backward chain of <dy, x_L>: dlogits [L,T,E], dx0 [T,d] = dL/dx_0, dw_router
  * [L,E,d] float32, the norms' gradients, and the expert-weight gradients dw_gate / dw_up [L,E,F,d],
- * dw_down [L,E,d,F] float32 or all three NULL.  x_out is a buffer of its own.  x_l, h_l and y_l are kept, a block's other
- * intermediates are formed again in the backward pass.  bf16 only (R3_ERR_UNSUPPORTED for float32).
+ * dw_down [L,E,d,F] float32 or all three NULL.  x_out is a buffer of its own.  x_l, h_l and y_l are kept,
+ * a block's other intermediates are formed again in the backward pass.  bf16 only (R3_ERR_UNSUPPORTED for
+ * float32).
  *
  * With adamw (HOST) the expert weights are updated in place, each block's as soon as its gradients are
  * there: dw_gate, dw_up [E,F,d] and dw_down [E,d,F] then hold ONE block's gradients (those of block 0

@@ -132,6 +132,19 @@ def test_rows_worked_on_two_at_a_time(r3, act, d, kind, post, pre):
         check(r3, make(T, d, act, act, kind, post, pre))
 
 
+@pytest.mark.parametrize("act,d", [(BF, 6152), (BF, 8200), (BF, 12296), (F32, 3080), (F32, 4104)])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("post,pre", [(True, True), (True, False), (False, True), (False, False)])
+def test_every_form_of_wide_rows(r3, act, d, kind, post, pre):
+    check(r3, make(150, d, act, F32, kind, post, pre))
+
+
+@pytest.mark.parametrize("act,T,d", [(BF, 70001, 64), (BF, 30001, 520), (F32, 5001, 2000), (F32, 5100, 3080)])
+def test_token_gates_of_many_rows(r3, act, T, d):
+    """More than 32 rows for a group of threads (one warp, several, two rows at a time, the wide form)."""
+    check(r3, make(T, d, act, F32, "token", True, True))
+
+
 def test_largest_rows(r3):
     for d in (8200, 16384):
         check(r3, make(40, d, BF, F32, "channel", True, True))

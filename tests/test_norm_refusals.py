@@ -33,7 +33,7 @@ def bwd(r3, s, x_out=A, y=B, w_post=C, gate=None, w_pre=C, dx_out=A, dh=B, dx=D,
                                        dx_out, dh, dx, dy, dw_post, dgate, dw_pre, ws, n, None)
 
 
-@pytest.mark.parametrize("kw", [dict(T=-1), dict(T=0x7f000001), dict(d=0), dict(d=60), dict(act_dtype=2),
+@pytest.mark.parametrize("kw", [dict(T=-1), dict(T=0x7f000001), dict(T=(1 << 30) + 1), dict(d=0), dict(d=60), dict(act_dtype=2),
                                 dict(w_dtype=7), dict(gate_kind=4), dict(gate_kind=-1), dict(eps=0.0),
                                 dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")),
                                 dict(residual_scale=float("inf")), dict(branch_scale=float("nan"))])

@@ -395,7 +395,7 @@ template <typename T, typename W, int P, bool WARP, bool WIDE, int S, int R, int
 __global__ void __launch_bounds__(norm_bwd_threads(WIDE, sizeof(T) == 4, (FORM & kFullGate) != 0, R))
 norm_bwd_kernel(const NormArgs a) {
     constexpr int N = Vec16<T>::N, Q = 4 * P * R, HOP = 32 * N;
-    constexpr bool KEEP = !WIDE;
+    constexpr bool KEEP = !WIDE || P * N <= 8;
     typedef const Vec16<T>* Ptr;
     extern __shared__ uint4 ring_all[];
     __shared__ float s_red[2][kNormMaxThreads / 32][3 * R + R % 2];   // up to 3 R values per warp of the CTA

@@ -395,7 +395,10 @@ template <typename T, typename W, int P, bool WARP, bool WIDE, int S, int R, int
 __global__ void __launch_bounds__(norm_bwd_threads(WIDE, sizeof(T) == 4, (FORM & kFullGate) != 0, R))
 norm_bwd_kernel(const NormArgs a) {
     constexpr int N = Vec16<T>::N, Q = 4 * P * R, HOP = 32 * N;
-    constexpr bool KEEP = !WIDE || P * N <= 8;
+    // the wide form has registers for the weights of 8 columns, of 16 where there is one vector of them (8178
+    // x 4096 float32: 180 -> 148 us; 8178 x 8192 bf16 without w_pre 140 -> 94, without y 116 -> 81)
+    constexpr bool ONE = !(FORM & kOpen) && (!(FORM & kHasPre) || !(FORM & kHasY));
+    constexpr bool KEEP = !WIDE || P * N <= (ONE ? 16 : 8);
     typedef const Vec16<T>* Ptr;
     extern __shared__ uint4 ring_all[];
     __shared__ float s_red[2][kNormMaxThreads / 32][3 * R + R % 2];   // up to 3 R values per warp of the CTA

@@ -611,7 +611,39 @@ def _device_of(name: str, t) -> torch.device:
     return dev
 
 
-def _norm_shape(rows, d, act, w_post, gate, w_pre, eps, residual_scale, branch_scale, dev):
+_GATE_SHAPES = {"channel": (R3_GATE_CHANNEL, lambda T, d: ((d,),)),
+                "token": (R3_GATE_TOKEN, lambda T, d: ((T,), (T, 1))),
+                "full": (R3_GATE_FULL, lambda T, d: ((T, d),))}
+
+
+def _gate_kind(gate, rows, d, w_dtype, said):
+    """What a gate is broadcast along: as the caller says, or by its shape.  With as many rows as columns
+    a vector may be a gate [d], of the weights' type, or a gate [T], float32: where the types leave it open
+    the caller has to say."""
+    shape = gate.shape
+    if said is not None:
+        if said not in _GATE_SHAPES:
+            raise ValueError(f"gate_kind: {said!r}, expected 'channel', 'token' or 'full'")
+        kind, shapes = _GATE_SHAPES[said]
+        if shape in shapes(rows, d):
+            return kind
+        raise ValueError(f"gate: shape {tuple(shape)}, expected "
+                         + " or ".join(str(list(s)) for s in shapes(rows, d)))
+    if shape == (d,):
+        if rows != d or gate.dtype != torch.float32:
+            return R3_GATE_CHANNEL
+        if w_dtype is not None and w_dtype != torch.float32:
+            return R3_GATE_TOKEN
+        raise ValueError(f"gate: [{d}] is one factor per channel or per token; say gate_kind='channel' or "
+                         f"'token' (or pass [{d}, 1])")
+    if shape == (rows, d):
+        return R3_GATE_FULL
+    if shape == (rows, 1) or shape == (rows,):
+        return R3_GATE_TOKEN
+    raise ValueError(f"gate: shape {tuple(shape)}, expected [{d}], [{rows}], [{rows}, 1] or [{rows}, {d}]")
+
+
+def _norm_shape(rows, d, act, w_post, gate, w_pre, eps, residual_scale, branch_scale, dev, gate_kind=None):
     """The r3_norm of a call and the addresses of w_post, gate and w_pre, which are checked: w_post,
     w_pre and a gate [d] share one type."""
     act_code = _ACT.get(act)
@@ -619,16 +651,9 @@ def _norm_shape(rows, d, act, w_post, gate, w_pre, eps, residual_scale, branch_s
         raise ValueError(f"activations: dtype {act}, expected float32 or bfloat16")
     kind, like = R3_GATE_NONE, w_post if w_post is not None else w_pre
     if gate is not None:
-        if gate.shape == (d,):
-            kind = R3_GATE_CHANNEL
-            like = like if like is not None else gate
-        elif gate.shape == (rows, 1):
-            kind = R3_GATE_TOKEN
-        elif gate.shape == (rows, d):
-            kind = R3_GATE_FULL
-        else:
-            raise ValueError(f"gate: shape {tuple(gate.shape)}, expected [{d}], [{rows}, 1] or "
-                             f"[{rows}, {d}]")
+        kind = _gate_kind(gate, rows, d, like.dtype if like is not None else None, gate_kind)
+        if kind == R3_GATE_CHANNEL and like is None:
+            like = gate
     w_dtype = like.dtype if like is not None else act
     w_code = _ACT.get(w_dtype)
     if w_code is None:
@@ -642,17 +667,18 @@ def _norm_shape(rows, d, act, w_post, gate, w_pre, eps, residual_scale, branch_s
 
 
 def norm_residual(x, y=None, *, w_post=None, gate=None, w_pre=None, eps=1e-6, residual_scale=1.0,
-                  branch_scale=1.0, x_out=None, h=None, stream=None):
+                  branch_scale=1.0, gate_kind=None, x_out=None, h=None, stream=None):
     """From one residual block to the next: x_out = residual_scale x + branch_scale gate
     RMSNorm(y) w_post, h = RMSNorm(x_out) w_pre, in one pass.  x, y [T, d] float32 or bfloat16; gate
-    None, [d], [T, 1] float32 or [T, d].  Without y only h = RMSNorm(x) w_pre; without w_post the
-    branch is not normalised; without w_pre there is no h.  Returns (x_out, h), None for what there
-    is not.  x_out may be x, h may be y (in place)."""
+    None, [d], [T] or [T, 1] float32, or [T, d]; gate_kind ("channel", "token", "full") says which, and
+    has to where T = d and a float32 vector beside float32 weights (or none) could be either.  Without y
+    only h = RMSNorm(x) w_pre; without w_post the branch is not normalised; without w_pre there is no h.
+    Returns (x_out, h), None for what there is not.  x_out may be x, h may be y (in place)."""
     dev = _device_of("x", x)
     shape, act = x.shape, x.dtype
     rows, d = shape
     s, post, gate, pre = _norm_shape(rows, d, act, w_post, gate, w_pre, eps, residual_scale,
-                                     branch_scale, dev)
+                                     branch_scale, dev, gate_kind)
     src = _arg("x", x, shape, act, dev)
     if y is not None and x_out is None:
         x_out = torch.empty_like(x)
@@ -670,16 +696,18 @@ def norm_residual(x, y=None, *, w_post=None, gate=None, w_pre=None, eps=1e-6, re
 
 
 def norm_residual_bwd(x_out, y, dx_out, dh=None, *, w_post=None, gate=None, w_pre=None, eps=1e-6,
-                      residual_scale=1.0, branch_scale=1.0, dx=None, dy=None, ws=None, stream=None):
+                      residual_scale=1.0, branch_scale=1.0, gate_kind=None, dx=None, dy=None, ws=None,
+                      stream=None):
     """Gradients of norm_residual from dx_out [T, d] (or None) and dh [T, d]: (dx, dy, dw_post [d],
-    dgate, dw_pre [d]), None for what the call has not; dw_* and the dgate of a gate [d] or [T, 1]
-    are float32.  x_out and y are the forward's (x_out may be None without w_pre)."""
+    dgate, dw_pre [d]), None for what the call has not; dgate has the gate's shape; dw_* and the dgate of
+    a gate [d], [T] or [T, 1] are float32.  x_out and y are the forward's (x_out may be None without
+    w_pre)."""
     like = x_out if x_out is not None else dx_out
     dev = _device_of("x_out", like)
     shape, act = like.shape, like.dtype
     rows, d = shape
     s, post, gate_at, pre = _norm_shape(rows, d, act, w_post, gate, w_pre, eps, residual_scale,
-                                        branch_scale, dev)
+                                        branch_scale, dev, gate_kind)
     src = [_arg(name, t, shape, act, dev) for name, t in
            (("x_out", x_out), ("y", y), ("dx_out", dx_out), ("dh", dh))]
     if dx is None:
@@ -705,7 +733,7 @@ def norm_residual_bwd(x_out, y, dx_out, dh=None, *, w_post=None, gate=None, w_pr
         if pre is not None:
             dw_pre = sums.pop()
     if gate is not None and not channel:
-        dgate = torch.empty_like(gate)           # float32 [T, 1], or [T, d] of the rows' type
+        dgate = torch.empty_like(gate)           # float32 [T] or [T, 1], or [T, d] of the rows' type
     if ws is None:
         ws = workspace(lib.r3_norm_residual_bwd_workspace_bytes(ctypes.byref(s)), dev)
     _check(lib.r3_norm_residual_bwd(

@@ -261,3 +261,24 @@ def test_rows_beyond_32_bit_offsets(r3):
     x_out, h = r3.norm_residual(x, y, **kw)
     assert torch.equal(x_out[pick], want[0]) and torch.equal(h[pick], want[1])
     assert not x_out[2:T // 2].any()
+
+
+@pytest.mark.parametrize("act,T,d", [(BF, 45, 264), (F32, 70, 1160), (F32, 64, 64), (BF, 1, 520)])
+def test_token_gates_as_a_vector(r3, act, T, d):
+    """A gate [T] is the gate [T, 1], with its gradient in the same shape; [T] = [d] of float32 has to be
+    named."""
+    s = make(T, d, act, F32, "token", True, True)
+    kw = dict(w_post=s["w_post"], w_pre=s["w_pre"])
+    vec = dict(gate=s["gate"][:, 0].contiguous(), gate_kind="token" if T == d else None, **kw)
+    ahead = r3.norm_residual(s["x"], s["y"], gate=s["gate"], **kw)
+    got = r3.norm_residual(s["x"], s["y"], **vec)
+    assert all(torch.equal(p, q) for p, q in zip(ahead, got))
+    want = r3.norm_residual_bwd(s["x"], s["y"], s["dx_out"], s["dh"], gate=s["gate"], **kw)
+    got = r3.norm_residual_bwd(s["x"], s["y"], s["dx_out"], s["dh"], **vec)
+    assert got[3].shape == (T,) and want[3].shape == (T, 1)
+    assert all(torch.equal(p.view(-1), q.view(-1)) for p, q in zip(want, got))
+    if T == d:
+        with pytest.raises(ValueError):
+            r3.norm_residual(s["x"], s["y"], **dict(vec, gate_kind=None))
+        channel = r3.norm_residual(s["x"], s["y"], **dict(vec, gate_kind="channel"))
+        assert not torch.equal(channel[0], ahead[0])

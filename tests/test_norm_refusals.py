@@ -82,3 +82,45 @@ def test_python_checks(r3):
         r3.norm_residual(torch.zeros(2, 8), w_pre=torch.ones(8))                     # host tensors
     with pytest.raises(TypeError):
         r3.norm_residual(None)
+
+
+def kind_of(r3, rows, d, gate, weights=None, said=None):
+    """The gate kind that the binding takes for a call (checked against host tensors here)."""
+    like = None if weights is None else torch.ones(d, dtype=weights)
+    return r3._norm_shape(rows, d, torch.bfloat16, like, gate, None, 1e-6, 1.0, 1.0, torch.device("cpu"),
+                          said)[0].gate_kind
+
+
+def test_gate_kinds_by_shape(r3):
+    f32, bf = torch.float32, torch.bfloat16
+    assert kind_of(r3, 4, 64, torch.ones(64), f32) == r3.R3_GATE_CHANNEL
+    assert kind_of(r3, 4, 64, torch.ones(64)) == r3.R3_GATE_CHANNEL
+    assert kind_of(r3, 4, 64, torch.ones(4), f32) == r3.R3_GATE_TOKEN
+    assert kind_of(r3, 4, 64, torch.ones(4), bf) == r3.R3_GATE_TOKEN
+    assert kind_of(r3, 4, 64, torch.ones(4, 1), bf) == r3.R3_GATE_TOKEN
+    assert kind_of(r3, 1, 64, torch.ones(1), bf) == r3.R3_GATE_TOKEN
+    assert kind_of(r3, 4, 64, torch.ones((4, 64), dtype=bf), f32) == r3.R3_GATE_FULL
+    for bad in (torch.ones(5), torch.ones(1, 64), torch.ones(64, 1), torch.ones(4, dtype=bf), torch.ones(())):
+        with pytest.raises(ValueError):
+            kind_of(r3, 4, 64, bad, f32)
+
+
+def test_a_vector_with_as_many_rows_as_columns(r3):
+    """[T] = [d]: the types tell a gate per channel (the weights') from one per token (float32), or the
+    caller does."""
+    f32, bf = torch.float32, torch.bfloat16
+    assert kind_of(r3, 64, 64, torch.ones(64, dtype=bf), bf) == r3.R3_GATE_CHANNEL
+    assert kind_of(r3, 64, 64, torch.ones(64, dtype=bf)) == r3.R3_GATE_CHANNEL
+    assert kind_of(r3, 64, 64, torch.ones(64), bf) == r3.R3_GATE_TOKEN
+    assert kind_of(r3, 64, 64, torch.ones(64, 1), f32) == r3.R3_GATE_TOKEN
+    for weights in (f32, None):
+        with pytest.raises(ValueError, match="gate_kind"):
+            kind_of(r3, 64, 64, torch.ones(64), weights)
+        assert kind_of(r3, 64, 64, torch.ones(64), weights, "channel") == r3.R3_GATE_CHANNEL
+        assert kind_of(r3, 64, 64, torch.ones(64), weights, "token") == r3.R3_GATE_TOKEN
+    with pytest.raises(ValueError):
+        kind_of(r3, 64, 64, torch.ones(64), f32, "row")
+    for said, gate in (("channel", torch.ones(4)), ("token", torch.ones(64)), ("full", torch.ones(64)),
+                       ("channel", torch.ones(4, 64))):
+        with pytest.raises(ValueError):
+            kind_of(r3, 4, 64, gate, f32, said)

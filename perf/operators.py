@@ -356,8 +356,7 @@ def _plain_norm(s):
 
 def _own_norm(s):
     from paper_2510_11370_b200 import r3
-    gate = s["gate"][:, None] if s["case"]["gate"] == "token" else s["gate"]
-    x_out, h = r3.norm_residual(s["x"], s["y"], w_post=s["w_post"], gate=gate,
+    x_out, h = r3.norm_residual(s["x"], s["y"], w_post=s["w_post"], gate=s["gate"],
                                 w_pre=s["w_pre"], eps=s["eps"], residual_scale=s["residual_scale"],
                                 branch_scale=s["branch_scale"])
     out = {} if s["y"] is None else {"x_out": x_out}
@@ -402,14 +401,11 @@ def _plain_norm_bwd(s):
 
 def _own_norm_bwd(s):
     from paper_2510_11370_b200 import r3
-    token = s["case"]["gate"] == "token"
     dx, dy, dw_post, dgate, dw_pre = r3.norm_residual_bwd(
-        s["x_out"], s["y"], s["dx_out"], s["dh"], w_post=s["w_post"],
-        gate=s["gate"][:, None] if token else s["gate"],
+        s["x_out"], s["y"], s["dx_out"], s["dh"], w_post=s["w_post"], gate=s["gate"],
         w_pre=s["w_pre"], eps=s["eps"], residual_scale=s["residual_scale"],
         branch_scale=s["branch_scale"])
-    out = {"dx": dx, "dy": dy, "dw_post": dw_post, "dgate": dgate[:, 0] if token else dgate,
-           "dw_pre": dw_pre}
+    out = {"dx": dx, "dy": dy, "dw_post": dw_post, "dgate": dgate, "dw_pre": dw_pre}
     return {k: v for k, v in out.items() if v is not None}
 
 

@@ -813,28 +813,38 @@ class AdamW:
         if grads is not None:
             self.set_grads(grads)
 
-    def _fill(self, field, tensors, sizes, dtype):
-        if tensors is None:
-            return
+    def _addresses(self, field, tensors, sizes, dtype):
+        """The addresses of a list of tensors, every one of them checked."""
         if len(tensors) != len(sizes):
             raise ValueError(f"{field}: {len(tensors)} tensors for {len(sizes)} params")
-        for i, (row, t, n) in enumerate(zip(self._table, tensors, sizes)):
+        at = []
+        for i, (t, n) in enumerate(zip(tensors, sizes)):
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{field}[{i}]: expected a torch.Tensor")
             if t.numel() != n:
                 raise ValueError(f"{field}[{i}]: {t.numel()} elements, expected {n}")
             _expect(f"{field}[{i}]", t, t.shape, dtype, self._dev)
-            setattr(row, field, _ptr(t).value)
-        if field != "grad":
-            self._memory += [t.detach() for t in tensors]
+            at.append(_ptr(t).value)
+        return at
+
+    def _fill(self, field, tensors, sizes, dtype):
+        if tensors is None:
+            return
+        for row, at in zip(self._table, self._addresses(field, tensors, sizes, dtype)):
+            setattr(row, field, at)
+        self._memory += [t.detach() for t in tensors]
 
     def set_grads(self, grads):
-        """Exchanges the gradients of the steps to come."""
+        """Exchanges the gradients of the steps to come: all of them, or none where one is refused."""
         grads = list(grads)
-        dtype = grads[0].dtype if grads else None
+        dtype = grads[0].dtype if grads and isinstance(grads[0], torch.Tensor) else None
         if dtype not in _ACT:
             raise ValueError(f"grads: dtype {dtype}, expected float32 or bfloat16")
-        self._fill("grad", grads, [p.numel() for p in self.params], dtype)
-        self.grads = grads
+        addresses = self._addresses("grad", grads, [p.numel() for p in self.params], dtype)
+        for row, at in zip(self._table, addresses):
+            row.grad = at
         self._config.grad_dtype = _ACT[dtype]
+        self.grads = grads
 
     def scalars(self, step, lr):
         """What a step's `scalars` tensor has to hold for this step and learning rate."""

@@ -81,3 +81,29 @@ def test_struct_layouts(r3):
 def test_host_tensors_are_refused(r3):
     with pytest.raises(ValueError):
         r3.AdamW([torch.zeros(8)], [torch.zeros(8)])
+
+
+@pytest.mark.parametrize("bad", ["size", "dtype", "layout", "device", "kind", "count"])
+def test_refused_gradients_leave_the_handle_as_it_was(r3, monkeypatch, bad):
+    """A list of gradients of which one is refused changes none of the handle's addresses, its list or its
+    type (host tensors here: no step is taken)."""
+    monkeypatch.setattr(r3, "_ptr", lambda t: ctypes.c_void_p(t.data_ptr()) if t.is_contiguous() else
+                        (_ for _ in ()).throw(ValueError("tensor must be contiguous")))
+    monkeypatch.setattr(r3, "_device_of", lambda name, t: t.device)
+    params = [torch.zeros(8), torch.zeros(16)]
+    old = [torch.zeros(8), torch.zeros(16)]
+    opt = r3.AdamW(params, old)
+    before = [row.grad for row in opt._table]
+    assert before == [g.data_ptr() for g in old]
+    new = [torch.zeros(8, dtype=torch.bfloat16), torch.zeros(16, dtype=torch.bfloat16)]
+    new[1] = {"size": new[1][:4], "dtype": torch.zeros(16), "layout": torch.zeros(32, dtype=torch.bfloat16)[::2],
+              "device": torch.zeros(16, dtype=torch.bfloat16, device="meta"), "kind": [0.0] * 16,
+              "count": new[1]}[bad]
+    with pytest.raises((ValueError, TypeError)):
+        opt.set_grads(new[:1] if bad == "count" else new)
+    assert [row.grad for row in opt._table] == before
+    assert opt._config.grad_dtype == r3.R3_F32 and all(a is b for a, b in zip(opt.grads, old))
+    new = [torch.ones(8, dtype=torch.bfloat16), torch.ones(16, dtype=torch.bfloat16)]
+    opt.set_grads(new)
+    assert [row.grad for row in opt._table] == [g.data_ptr() for g in new]
+    assert opt._config.grad_dtype == r3.R3_BF16

@@ -296,3 +296,16 @@ def test_exchanged_data_leaves_the_handle_its_memory(r3):
     others = [torch.full((1000,), 5.0, device="cuda") for _ in range(8)]
     o.step(1, 0.1)
     assert all((t == 5.0).all() for t in others) and not p.any()
+
+
+def test_a_step_after_refused_gradients_takes_the_old_ones(r3):
+    a = make(r3, [700, 300], F32, F32, False, 32)
+    b = make(r3, [700, 300], F32, F32, False, 32)
+    for bad in ([torch.ones(700, device="cuda"), torch.ones(299, device="cuda")],
+                [torch.ones(700, dtype=BF, device="cuda"), torch.ones(300, device="cuda")]):
+        with pytest.raises(ValueError):
+            a.set_grads(bad)
+    a.step(2, 1e-2)
+    b.step(2, 1e-2)
+    for p, q in zip(a.params + a.exp_avg + a.exp_avg_sq, b.params + b.exp_avg + b.exp_avg_sq):
+        assert torch.equal(p, q)

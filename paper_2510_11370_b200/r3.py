@@ -7,6 +7,8 @@ without a built library raises, and every call requires CUDA tensors.
 from __future__ import annotations
 
 import ctypes
+import functools
+import inspect
 import os
 
 import torch
@@ -251,6 +253,31 @@ def _stream(stream=None):
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+def _in_order(fn):
+    """For a call that allocates and takes a stream.  With stream= another one than the current, what the
+    call allocates is that stream's memory (torch.cuda.stream): scratch that goes back on return is then
+    reused behind the kernels that still work on it, and new memory is free of work that the current
+    stream has not finished.  New outputs are also marked as used by the stream that was current, which is
+    where the caller goes on with them."""
+    at = list(inspect.signature(fn).parameters).index("stream")
+
+    @functools.wraps(fn)
+    def call(*args, **kw):
+        stream = args[at] if len(args) > at else kw.get("stream")
+        if stream is None:
+            return fn(*args, **kw)
+        caller = torch.cuda.current_stream(stream.device)
+        with torch.cuda.stream(stream):
+            out = fn(*args, **kw)
+        if stream != caller:
+            given = {id(a) for a in (*args, *kw.values())}
+            for t in out if isinstance(out, tuple) else (out,):
+                if isinstance(t, torch.Tensor) and id(t) not in given:
+                    t.record_stream(caller)
+        return out
+    return call
+
+
 def _dev(*ts):
     for t in ts:
         if isinstance(t, torch.Tensor):
@@ -268,6 +295,7 @@ def new_status(device) -> torch.Tensor:
 
 
 # ---------------------------------------------------------------------------------------------
+@_in_order
 def capture_topk(s: Shape, x, w_router, idx_out=None, logits_out=None, *, want_idx=True,
                  want_logits=False, stream=None):
     """Router logits + TopKMask.  Returns (idx [T,K] or None, logits [T,E] or None)."""
@@ -281,6 +309,7 @@ def capture_topk(s: Shape, x, w_router, idx_out=None, logits_out=None, *, want_i
     return idx_out, logits_out
 
 
+@_in_order
 def capture_topk_batched(s: Shape, L: int, x, w_router, idx_out=None, logits_out=None, *,
                          want_idx=True, want_logits=False, stream=None):
     """L layers at once: x [L,T,d], w_router [L,E,d] -> idx [L,T,K], logits [L,T,E]."""
@@ -298,6 +327,7 @@ def capture_topk_workspace_bytes(s: Shape, L: int = 1) -> int:
     return lib.r3_capture_topk_workspace_bytes(ctypes.byref(s), L)
 
 
+@_in_order
 def capture_topk_ws(s: Shape, L: int, x, w_router, idx_out=None, logits_out=None, *, ws=None,
                     want_idx=True, want_logits=False, stream=None):
     """capture_topk with scratch, so that float32 router weights run on the tensor cores too."""
@@ -314,6 +344,7 @@ def capture_topk_ws(s: Shape, L: int, x, w_router, idx_out=None, logits_out=None
     return idx_out, logits_out
 
 
+@_in_order
 def replay_gate_fwd(s: Shape, logits, idx, gates=None, dev_status=None, stream=None):
     if gates is None:
         gates = torch.empty((s.T, s.K), dtype=torch.float32, device=_dev(logits))
@@ -322,6 +353,7 @@ def replay_gate_fwd(s: Shape, logits, idx, gates=None, dev_status=None, stream=N
     return gates
 
 
+@_in_order
 def replay_gate_bwd(s: Shape, gates, dgates, idx, dlogits=None, stream=None):
     if dlogits is None:
         dlogits = torch.empty((s.T, s.E), dtype=torch.float32, device=_dev(gates))
@@ -334,6 +366,7 @@ def permute_workspace_bytes(s: Shape) -> int:
     return lib.r3_permute_workspace_bytes(ctypes.byref(s))
 
 
+@_in_order
 def permute(s: Shape, idx, x=None, *, out=None, ws=None, dev_status=None, stream=None):
     """Returns (counts, offsets, row_of_slot, slot_of_row, xp or None)."""
     dev = _dev(idx)
@@ -370,6 +403,7 @@ def grouped_swiglu_workspace_bytes(s: Shape) -> int:
     return lib.r3_grouped_swiglu_workspace_bytes(ctypes.byref(s))
 
 
+@_in_order
 def grouped_swiglu(s: Shape, xp, offsets, w_gate, w_up, w_down, o=None, *, ws=None,
                    dev_status=None, stream=None):
     dev = _dev(xp)
@@ -383,6 +417,7 @@ def grouped_swiglu(s: Shape, xp, offsets, w_gate, w_up, w_down, o=None, *, ws=No
     return o
 
 
+@_in_order
 def grouped_swiglu_gather(s: Shape, x, slot_of_row, offsets, w_gate, w_up, w_down, o=None, *,
                           ws=None, dev_status=None, stream=None):
     """grouped_swiglu reading the token rows in place from x [T,d] through slot_of_row (bf16)."""
@@ -411,6 +446,7 @@ def expert_down(s: Shape, w_down, o, ws, dev_status=None, stream=None):
     return o
 
 
+@_in_order
 def combine(s: Shape, o, row_of_slot, gates, y=None, stream=None):
     if y is None:
         y = torch.empty((s.T, s.d), dtype=_act_dtype(s), device=_dev(o))
@@ -419,6 +455,7 @@ def combine(s: Shape, o, row_of_slot, gates, y=None, stream=None):
     return y
 
 
+@_in_order
 def combine_residual(s: Shape, o, row_of_slot, gates, residual, y=None, stream=None):
     """y = residual + sum_j gates[:, j] * o[row_of_slot[:, j]]."""
     if y is None:
@@ -428,6 +465,7 @@ def combine_residual(s: Shape, o, row_of_slot, gates, residual, y=None, stream=N
     return y
 
 
+@_in_order
 def replay_blocks(s: Shape, L: int, x, w_router, idx, w_gate, w_up, w_down, dy, *, y=None,
                   dlogits=None, ws=None, dev_status=None, stream=None):
     """L independent replayed blocks, all tensors stacked on a leading layer axis.
@@ -450,6 +488,7 @@ def replay_stack_workspace_bytes(s: Shape) -> int:
     return lib.r3_replay_stack_workspace_bytes(ctypes.byref(s))
 
 
+@_in_order
 def replay_stack(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down, dy, *, x_out=None,
                  dlogits=None, ws=None, dev_status=None, stream=None):
     """L residual MoE blocks with replayed routing.  Returns (x_L [T,d], dlogits [L,T,E])."""
@@ -467,6 +506,7 @@ def replay_stack(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down, dy, 
     return x_out, dlogits
 
 
+@_in_order
 def combine_bwd_gates(s: Shape, dy, o, row_of_slot, dgates=None, stream=None):
     if dgates is None:
         dgates = torch.empty((s.T, s.K), dtype=torch.float32, device=_dev(o))
@@ -475,6 +515,7 @@ def combine_bwd_gates(s: Shape, dy, o, row_of_slot, dgates=None, stream=None):
     return dgates
 
 
+@_in_order
 def replay_finish(s: Shape, logits, idx, o, row_of_slot, dy, *, residual=None, y=None, gates=None,
                   dlogits=None, dev_status=None, stream=None):
     """Replay gate + combine + gate gradient + router-logit gradient in one pass over `o`
@@ -496,6 +537,7 @@ def replay_layer_workspace_bytes(s: Shape) -> int:
     return lib.r3_replay_layer_workspace_bytes(ctypes.byref(s))
 
 
+@_in_order
 def replay_layer(s: Shape, x, w_router, idx, w_gate, w_up, w_down, dy, *, y=None, dlogits=None,
                  gates=None, ws=None, dev_status=None, stream=None):
     """Forward + router-logit backward of the replayed layer.  Returns (y, dlogits, gates)."""
@@ -515,6 +557,7 @@ def replay_layer(s: Shape, x, w_router, idx, w_gate, w_up, w_down, dy, *, y=None
     return y, dlogits, gates
 
 
+@_in_order
 def replay_layer_same_record(s: Shape, x, w_router, idx, w_gate, w_up, w_down, dy, *, ws, y=None,
                              dlogits=None, gates=None, dev_status=None, stream=None):
     """replay_layer for another pass over the record of the preceding replay_layer call on `ws`:
@@ -666,6 +709,7 @@ def _norm_shape(rows, d, act, w_post, gate, w_pre, eps, residual_scale, branch_s
     return Norm(rows, d, act_code, w_code, kind, eps, residual_scale, branch_scale), post, gate, pre
 
 
+@_in_order
 def norm_residual(x, y=None, *, w_post=None, gate=None, w_pre=None, eps=1e-6, residual_scale=1.0,
                   branch_scale=1.0, gate_kind=None, x_out=None, h=None, stream=None):
     """From one residual block to the next: x_out = residual_scale x + branch_scale gate
@@ -695,6 +739,7 @@ def norm_residual(x, y=None, *, w_post=None, gate=None, w_pre=None, eps=1e-6, re
     return x_out, h
 
 
+@_in_order
 def norm_residual_bwd(x_out, y, dx_out, dh=None, *, w_post=None, gate=None, w_pre=None, eps=1e-6,
                       residual_scale=1.0, branch_scale=1.0, gate_kind=None, dx=None, dy=None, ws=None,
                       stream=None):
@@ -880,6 +925,7 @@ def _block_norms(s, L, w_pre, w_post, gate, eps, residual_scale, branch_scale, d
     return n, made
 
 
+@_in_order
 def normed_stack(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down, *, w_pre, w_post=None,
                  gate=None, eps=1e-6, residual_scale=1.0, branch_scale=1.0, x_out=None, ws=None,
                  dev_status=None, stream=None):
@@ -900,6 +946,7 @@ def normed_stack(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down, *, w
     return x_out
 
 
+@_in_order
 def normed_stack_train(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down, dy, *, w_pre,
                        w_post=None, gate=None, eps=1e-6, residual_scale=1.0, branch_scale=1.0,
                        expert_grads=False, optimiser=None, step=None, lr=None, grad_scale=None,
@@ -974,6 +1021,7 @@ def _logits_shape(logits, token_ids, temperature):
     return Logits(T, V, ld, dtype, id_bytes, temperature), ptr, ids, dev
 
 
+@_in_order
 def token_logprobs(logits, token_ids=None, *, temperature=1.0, n_top=0, want_entropy=False,
                    want_stats=False, dev_status=None, stream=None):
     """Log probabilities of token_ids [T] (int32 or int64) under logits [T, V] (float32 or bfloat16;
@@ -1002,6 +1050,7 @@ def token_logprobs(logits, token_ids=None, *, temperature=1.0, n_top=0, want_ent
     return logp, entropy, stats, top_ids, top_logp
 
 
+@_in_order
 def token_logprobs_bwd(logits, token_ids, stats, dlogp, *, entropy=None, dentropy=None,
                        temperature=1.0, dlogits=None, dev_status=None, stream=None):
     """Gradient to the logits from dlogp [T] (or None) and, with the forward's entropy [T], from
@@ -1021,6 +1070,7 @@ def token_logprobs_bwd(logits, token_ids, stats, dlogp, *, entropy=None, dentrop
     return dlogits
 
 
+@_in_order
 def prob_discrepancy(p_train, p_infer, taus, *, kl=None, counts=None, ws=None, stream=None):
     """k3 KL estimate (Eq. kl) and extreme-token counts (Eq. etdf) of two float32 probability
     arrays.  `taus`: a list or a float32 device tensor.  Returns (kl [1] float64, counts [n_tau]
@@ -1040,6 +1090,7 @@ def prob_discrepancy(p_train, p_infer, taus, *, kl=None, counts=None, ws=None, s
     return kl, counts
 
 
+@_in_order
 def record_diff(s: Shape, L: int, rec_a, rec_b, *, want_diff=True, stream=None):
     """Differing expert choices between two records [L,T,K].  Returns (diff [L,T] uint8 or None,
     token_choices [T], token_routers [T], hist [K+1] int64)."""
@@ -1053,6 +1104,7 @@ def record_diff(s: Shape, L: int, rec_a, rec_b, *, want_diff=True, stream=None):
     return diff, choices, routers, hist
 
 
+@_in_order
 def sequence_diff(token_routers, cu_seqlens, *, stream=None):
     """Per-sequence sums of token_routers over [cu_seqlens[s], cu_seqlens[s+1])."""
     S = cu_seqlens.numel() - 1
@@ -1077,6 +1129,7 @@ def record_append(s: Shape, L: int, page_tokens: int, pages, block_table, seq_po
                                 _ptr(rec_new), rec_new.shape[1], _ptr(dev_status), _stream(stream)))
 
 
+@_in_order
 def record_gather(s: Shape, L: int, page_tokens: int, pages, block_table, cu_seqlens, T: int, *,
                   out=None, dev_status=None, stream=None):
     """The packed record [L, T, K] of a variable-length batch, assembled from the pages."""
@@ -1132,6 +1185,7 @@ class PagePool:
         _check(lib.r3_pagepool_release(self._h, self._arr(table), len(table)))
 
 
+@_in_order
 def grouped_swiglu_train(s: Shape, xp, offsets, w_gate, w_up, w_down, *, ws=None, dev_status=None,
                          stream=None):
     """Grouped experts that also return the pre-activations: (o [R,d], pre_gate, pre_up [R,F])."""
@@ -1149,6 +1203,7 @@ def grouped_swiglu_train(s: Shape, xp, offsets, w_gate, w_up, w_down, *, ws=None
     return o, pre_gate, pre_up
 
 
+@_in_order
 def scale_rows(s: Shape, dy, gates, row_of_slot, dout=None, *, stream=None):
     """dout[row_of_slot[t,j]] = gates[t,j] * dy[t]."""
     if dout is None:
@@ -1158,6 +1213,7 @@ def scale_rows(s: Shape, dy, gates, row_of_slot, dout=None, *, stream=None):
     return dout
 
 
+@_in_order
 def input_grad_finish(s: Shape, dxp, row_of_slot, slot_of_row, offsets, dlogits, idx, x, w_router,
                       *, dx_residual=None, stream=None):
     """(dx [T,d], dw_router [E,d] float32) from the expert input gradient and dlogits."""
@@ -1171,6 +1227,7 @@ def input_grad_finish(s: Shape, dxp, row_of_slot, slot_of_row, offsets, dlogits,
     return dx, dw_r
 
 
+@_in_order
 def grouped_swiglu_bwd(s: Shape, xp, dout, pre_gate, pre_up, offsets, w_gate, w_up, w_down, *,
                        ws=None, dev_status=None, stream=None):
     """Backward of the grouped experts: (dxp [R,d], dw_gate, dw_up [E,F,d], dw_down [E,d,F])."""
@@ -1189,6 +1246,7 @@ def grouped_swiglu_bwd(s: Shape, xp, dout, pre_gate, pre_up, offsets, w_gate, w_
     return dxp, dw_gate, dw_up, dw_down
 
 
+@_in_order
 def replay_layer_train(s: Shape, x, w_router, idx, w_gate, w_up, w_down, dy, *, ws=None,
                        dev_status=None, stream=None, expert_grads=False, dw_experts=None):
     """Forward and backward of one replayed layer: (y, dlogits, dx, dw_router), and with
@@ -1217,6 +1275,7 @@ def replay_layer_train(s: Shape, x, w_router, idx, w_gate, w_up, w_down, dy, *, 
     return y, dlogits, dx, dw_r
 
 
+@_in_order
 def replay_stack_train(s: Shape, L, x0, w_router, idx, w_gate, w_up, w_down, dy, *, ws=None,
                        dev_status=None, stream=None, expert_grads=False):
     """L residual blocks forward, then the exact backward chain:
@@ -1243,6 +1302,7 @@ def replay_stack_train(s: Shape, L, x0, w_router, idx, w_gate, w_up, w_down, dy,
     return x_out, dlogits, dx0, dw_r
 
 
+@_in_order
 def ep_regroup_map(recv_counts, rows: int, *, dev_status=None, stream=None):
     """recv_counts [n_src, e_local] int32 (device) -> (perm [rows] int32, offsets [e_local+1])."""
     n_src, e_local = recv_counts.shape
@@ -1259,6 +1319,7 @@ def _peer_array(addresses):
     return (ctypes.c_uint64 * len(addresses))(*[int(a) for a in addresses])
 
 
+@_in_order
 def ep_dest_table(counts_all, rank: int, *, stream=None):
     """counts_all [n_ranks, E] int32 (device) -> (dst_base [E], offsets_local [E/n_ranks + 1])."""
     n, E = counts_all.shape
@@ -1280,6 +1341,7 @@ def ep_dispatch_rows(s: Shape, n_ranks: int, x, idx, row_of_slot, my_offsets, ds
                                    _ptr(dev_status), _stream(stream)))
 
 
+@_in_order
 def ep_slot_rows(s: Shape, n_ranks: int, idx, row_of_slot, my_offsets, dst_base, peer_addresses,
                  capacity_rows: int, *, dev_status=None, stream=None):
     """[T, K] addresses of the pairs' expert-output rows in the owners' output buffers."""
@@ -1291,6 +1353,7 @@ def ep_slot_rows(s: Shape, n_ranks: int, idx, row_of_slot, my_offsets, dst_base,
     return row_ptr
 
 
+@_in_order
 def replay_finish_rows(s: Shape, logits, idx, row_ptr, dy, *, residual=None, dev_status=None,
                        stream=None):
     """r3_replay_finish with the expert-output rows given by address.  (y, gates, dlogits)."""
@@ -1304,6 +1367,7 @@ def replay_finish_rows(s: Shape, logits, idx, row_ptr, dy, *, residual=None, dev
     return y, gates, dlogits
 
 
+@_in_order
 def ep_move_rows(src, perm, *, inverse=False, stream=None):
     """Rows of `src` [rows, width] reordered by `perm` (see r3_ep_move_rows)."""
     dst = torch.empty_like(src)
@@ -1315,6 +1379,7 @@ def ep_move_rows(src, perm, *, inverse=False, stream=None):
     return dst
 
 
+@_in_order
 def grouped_swiglu_bwd_input(s: Shape, dout, pre_gate, pre_up, offsets, w_gate, w_up, w_down,
                              dxp=None, *, ws=None, dev_status=None, stream=None):
     """Input gradient of the grouped SwiGLU experts: dout [R,d] -> dxp [R,d] (bf16)."""
@@ -1330,6 +1395,7 @@ def grouped_swiglu_bwd_input(s: Shape, dout, pre_gate, pre_up, offsets, w_gate, 
     return dxp
 
 
+@_in_order
 def selftest_bounded_wait(limit_clocks: int, *, dev_status=None, device="cuda", stream=None):
     """Makes the library's bounded barrier wait run out on purpose (a barrier nothing signals).
     Returns out [4] int32: (wait result, abort flag, clocks waited, result of a second wait)."""

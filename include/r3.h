@@ -575,8 +575,10 @@ typedef struct {
  * in float32, w rounded once to param_dtype.  8-bit states: the scale of a block of 256 elements is
  * the smallest power of two (at least 2^-126) that brings its largest magnitude to 448 or less, a
  * code is the nearest e4m3 value (ties to even), a root above 0 gets at least the smallest code.
- * Every product and sum that forms m, v and the scales is rounded to float32 by itself; the root is
- * within 2^-22 of sqrt(v).  The stored states do not depend on the launch or the other tensors.
+ * Every product and sum that forms m, v and the scales is rounded to float32 by itself, and so are the root
+ * (of the stored states and of the update) and the update's quotient; only with 8-bit states and bf16
+ * parameters without masters the update takes the hardware's approximations of these two (within 2^-21 of
+ * it, before the weight's rounding).  The stored states do not depend on the launch or the other tensors.
  *  - grad_scale (device, float32, or NULL = 1): a loss scale's inverse or a clipping factor.  If it
  *    is not finite the whole step is skipped: nothing is written.
  *  - scalars (device, [3] float32, or NULL): {lr, 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)} in place of

@@ -309,3 +309,55 @@ def test_a_step_after_refused_gradients_takes_the_old_ones(r3):
     b.step(2, 1e-2)
     for p, q in zip(a.params + a.exp_avg + a.exp_avg_sq, b.params + b.exp_avg + b.exp_avg_sq):
         assert torch.equal(p, q)
+
+
+def midpoints():
+    """Values around the middle between any two neighbouring positive e4m3 values, and their float32
+    neighbours, with 448 in front of every block (so that the scale is 1)."""
+    codes = np.arange(0x7f, dtype=np.uint8)
+    at = torch.from_numpy(codes).view(E4).to(torch.float32).numpy()
+    mid = ((at[1:] + at[:-1]) / 2).astype(np.float32)
+    out = [mid]
+    for direction in (np.float32(0), np.float32(1e9)):
+        near = mid
+        for _ in range(6):
+            near = np.nextafter(near, direction)
+            out.append(near)
+    out = np.concatenate(out)
+    out = np.concatenate([out, np.zeros(-len(out) % 255, dtype=np.float32)]).reshape(-1, 255)
+    return np.concatenate([np.full((len(out), 1), 448, dtype=np.float32), out], axis=1)
+
+
+@pytest.mark.parametrize("dtype,master", [(F32, False), (BF, False), (BF, True)])
+def test_codes_of_roots_between_two_codes(r3, dtype, master):
+    """Without averaging (betas 0) the second moment is the gradient's square: the stored code is that of
+    its correctly rounded root also next to the middle between two codes, and in it (ties to even)."""
+    g = midpoints()
+    w = torch.zeros(g.size, dtype=dtype, device="cuda")
+    opt = r3.AdamW([w], [torch.from_numpy(g.reshape(-1)).cuda()], state_bits=8, betas=(0.0, 0.0),
+                   masters=True if master else None)
+    opt.step(1, 1e-3)
+    root = np.sqrt(g * g)
+    assert root.dtype == np.float32
+    want = U.nearest_e4m3(root.astype(np.float64))
+    want[(root > 0) & (want == 0)] = U.E4M3_MIN
+    assert (opt.exp_avg_sq_scale[0] == 1).all()
+    assert np.array_equal(blocks(f64(opt.exp_avg_sq[0])), want)
+
+
+@pytest.mark.parametrize("dtype,master,bits", [(F32, False, 32), (F32, False, 8), (BF, True, 32), (BF, True, 8),
+                                               (BF, False, 32)])
+def test_the_update_is_rounded_operation_by_operation(r3, dtype, master, bits):
+    """Without averaging, from weights of zero and with a rate of 1 the step is one quotient: the bits of
+    float32 square, root, sum and division, each rounded to the last bit (half a step of 2^-24)."""
+    g = torch.randn(30000, generator=torch.Generator().manual_seed(5)) * torch.logspace(-12, 6, 30000)
+    w = torch.zeros(30000, dtype=dtype, device="cuda")
+    eps = 1e-3
+    opt = r3.AdamW([w], [g.cuda()], state_bits=bits, betas=(0.0, 0.0), eps=eps, masters=True if master else None)
+    opt.step(1, 1.0)
+    x = g.numpy()
+    want = -(x / (np.sqrt(x * x) + np.float32(eps)))
+    assert want.dtype == np.float32
+    held = opt.masters[0] if master else w
+    assert torch.equal(held.cpu(), torch.from_numpy(want).to(held.dtype))
+    assert torch.equal(w, held.to(dtype))

@@ -53,3 +53,34 @@ def random_record(rng: np.random.Generator, T: int, E: int, K: int, dtype) -> to
     keys = rng.random((T, E))
     idx = np.argsort(keys, axis=1)[:, :K]
     return torch.from_numpy(idx.astype(np.int64)).to(dtype)
+
+
+def logits_gradient_bound(logits, token_ids, dlogp, dentropy, temperature, ref, eps):
+    """How far a float32 kernel's gradient to the logits may be from `ref` (float64, the oracle's), element by
+    element.  An element is p k plus, at the token, g = dlogp / temperature, with k = -g - ge (log p + H) and
+    ge = dentropy / temperature; it is rounded once, by eps / 2 of itself.
+      p = 2^u, u from z = (x - top) / temperature and L: the difference, the constant and L's product are off
+      by 2^-24 of |z|, |z|, L and L, the sum by 2^-24 of |log p|, which |z| + L is (L >= 0, z <= 0); L itself by
+      the forward's 2e-5; the exponential by 2^-22.  Together p is within 2e-5 + 2^-22 (|log p| + 1).
+      k: log p as above, H within 2e-5 + 2^-22 H, three roundings of the terms: within
+      |ge| (4e-5 + 2^-21 (|log p| + H)) + 2^-22 |g|, the last within p's share of |g|.
+      g: two roundings, 2^-23.
+    Probabilities below float32's normal range count as 0."""
+    z = np.asarray(logits, dtype=np.float64)
+    top = z.max(axis=1, keepdims=True)
+    with np.errstate(invalid="ignore", over="ignore"):
+        z = np.where(np.isneginf(top), -np.inf, (z - np.where(np.isneginf(top), 0, top)) / temperature)
+        total = np.exp(z).sum(axis=1, keepdims=True)
+        lp = z - np.log(np.where(total > 0, total, 1))
+    p = np.exp(lp)
+    size = np.where(p > 0, np.maximum(lp, -1e4), 0) * -1                       # |log p| where it counts
+    g = np.abs(np.asarray(dlogp, dtype=np.float64))[:, None]
+    ge = 0.0 if dentropy is None else np.abs(np.asarray(dentropy, dtype=np.float64))[:, None]
+    H = (p * size).sum(axis=1, keepdims=True)
+    factor = g + ge * (size + H)
+    bound = p * ((2e-5 + 2.0 ** -22 * (size + 1)) * factor + ge * (4e-5 + 2.0 ** -21 * (size + H)))
+    bound += 2.0 ** -126 * (1 + factor)
+    at = np.asarray(token_ids)
+    rows = np.nonzero((at >= 0) & (at < z.shape[1]))[0]
+    bound[rows, at[rows]] += 2.0 ** -23 * g[rows, 0]
+    return bound / temperature + eps / 2 * np.abs(ref) + 2.0 ** -126

@@ -14,7 +14,7 @@ import pytest
 import torch
 
 from oracle import r3_update_oracle as U
-from tests.helpers import f64
+from tests.helpers import f64, logits_gradient_bound
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
@@ -326,3 +326,70 @@ def test_feeds_the_discrepancy_measures(r3):
     # d(k3)/d(log ratio) = r - 1, and a log ratio is off by at most 2 (2e-5 + 30 * 2^-22)
     far = 2 * (2e-5 + 30 * 2.0 ** -22) * np.abs(ra / rb - 1).mean()
     assert abs(kl.item() - D.kl_k3(ra, rb)) <= far + 1e-9 + 1e-5 * kl.item()
+
+
+def check_every_element(r3, logits, ids, temperature=1.0, with_entropy=True, dlogits=None):
+    """The gradient held to a bound relative to each element's own probability, so that the small ones of a
+    long row count."""
+    T, V = logits.shape
+    g = torch.Generator().manual_seed(3 * T + V)
+    dlogp, dent = torch.randn(T, generator=g), torch.randn(T, generator=g)
+    _, ent, stats, _, _ = r3.token_logprobs(logits, ids, temperature=temperature, want_entropy=True,
+                                            want_stats=True)
+    kw = dict(entropy=ent, dentropy=dent.cuda()) if with_entropy else {}
+    z, at = f64(logits), ids.cpu().numpy()
+    d64 = [dlogp.numpy().astype(np.float64), dent.numpy().astype(np.float64) if with_entropy else None]
+    with np.errstate(over="ignore"):
+        ref = U.token_logprobs_bwd(z, at, *d64, temperature)
+    bound = logits_gradient_bound(z, at, *d64, temperature, ref, torch.finfo(logits.dtype).eps)
+    d = r3.token_logprobs_bwd(logits, ids, stats, dlogp.cuda(), temperature=temperature, dlogits=dlogits, **kw)
+    far = np.abs(f64(d) - ref) - bound
+    assert (far <= 0).all(), (far.max(), np.unravel_index(far.argmax(), far.shape))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("with_entropy", [True, False])
+@pytest.mark.parametrize("T,V,pad", [(1, 1, 0), (4, 31, 1), (17, 700, 0), (9, 1003, 7), (6, 8193, 0),
+                                     (5, 50257, 0), (5, 50257, 15), (4, 131072, 0), (3, 151936, 64)])
+def test_every_element_of_the_gradient(r3, T, V, pad, with_entropy, dtype):
+    logits, ids = make(T, V, dtype, T * V + 2, pad)
+    for temperature in (1.0, 0.6):
+        check_every_element(r3, logits, ids, temperature, with_entropy)
+    # in place, and into rows that start elsewhere in their 16-byte pieces
+    room = torch.empty((T, V + pad + 9), dtype=dtype, device="cuda")
+    for off in (0, 1, 5):
+        check_every_element(r3, logits, ids, 1.0, with_entropy, dlogits=room[:, off:off + V])
+    check_every_element(r3, logits, ids, 1.0, with_entropy, dlogits=logits)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_every_element_of_masked_rows(r3, dtype):
+    """Masks of -inf and of the lowest value in every other row of a real vocabulary."""
+    logits, ids = make(6, 50257, dtype, 8)
+    shut = torch.rand((6, 50257), generator=torch.Generator().manual_seed(2)).cuda() < 0.25
+    shut[::2] = False
+    ids = ids.clamp(min=0)
+    shut.scatter_(1, ids[:, None], False)
+    logits[shut & (torch.arange(6, device="cuda") % 4 == 1)[:, None]] = float("-inf")
+    logits[shut & (torch.arange(6, device="cuda") % 4 == 3)[:, None]] = torch.finfo(dtype).min
+    for with_entropy in (True, False):
+        check_every_element(r3, logits, ids, 0.8, with_entropy)
+
+
+def test_every_element_beyond_32_bit_offsets(r3):
+    """Rows whose offset passes 2^31 elements, gradient in place."""
+    T, V = 20000, 120000
+    logits = torch.zeros((T, V), dtype=BF, device="cuda")
+    ids = torch.full((T,), -1, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rows = [0, T - 2, T - 1]
+    for t in rows:
+        logits[t] = (torch.randn(V, generator=g, device="cuda") * 2).to(BF)
+        ids[t] = t % V
+    stats = r3.token_logprobs(logits, ids, want_stats=True)[2]
+    z, at = f64(logits[rows]), ids[rows].cpu().numpy()
+    ref = U.token_logprobs_bwd(z, at, np.ones(3))
+    bound = logits_gradient_bound(z, at, np.ones(3), None, 1.0, ref, torch.finfo(BF).eps)
+    d = r3.token_logprobs_bwd(logits, ids, stats, torch.ones(T, device="cuda"), dlogits=logits)
+    assert (np.abs(f64(d[rows]) - ref) <= bound).all()
+    assert not d[1:T - 2].any()

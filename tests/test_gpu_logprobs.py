@@ -393,3 +393,40 @@ def test_every_element_beyond_32_bit_offsets(r3):
     d = r3.token_logprobs_bwd(logits, ids, stats, torch.ones(T, device="cuda"), dlogits=logits)
     assert (np.abs(f64(d[rows]) - ref) <= bound).all()
     assert not d[1:T - 2].any()
+
+
+def plan_of(T, row_bytes, sms):
+    """(threads, CTAs per row) that a call takes: the rule of r3_token_logprobs."""
+    resident = {32: 24, 128: 8, 256: 4}
+    waves = {n: -(-T // (resident[n] * sms)) for n in resident}
+    threads = (32 if row_bytes <= 16384 else 128 if row_bytes <= 49152 else
+               256 if waves[128] <= 4 and waves[256] < 2 * waves[128] else 128)
+    split = 1
+    while split < 8 and T * split <= sms and row_bytes // (split * 2) >= 32 * threads:
+        split *= 2
+    return threads, split
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,n_top", [(149, 20), (300, 0), (590, 5)])
+def test_long_rows_on_one_block_of_256_threads(r3, T, n_top, dtype):
+    """A few hundred long rows: too many to share, too few for blocks of 128 threads.  The oracle's rows
+    repeat."""
+    V, kinds = 25013, 7                             # 50 and 100 KB
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert sms != 148 or plan_of(T, V * torch.finfo(dtype).bits // 8, sms) == (256, 1)
+    few, _ = make(kinds, V, dtype, 17)
+    few[2, 5:9000] = float("-inf")
+    few[3] = torch.finfo(dtype).min
+    pick = torch.arange(T) % kinds
+    ids = torch.arange(T) * 83 % V
+    ids[::11] = -1
+    ids[pick == 2] = 3
+    logits = few[pick.cuda()]
+    got = r3.token_logprobs(logits, ids.cuda(), n_top=n_top, want_entropy=True, want_stats=True)
+    ref = U.token_logprobs(f64(logits), ids.numpy(), n_top=n_top)
+    for name, t in zip(("logp", "entropy", "stats"), got):
+        close(t, ref[name], name)
+    if n_top:
+        assert np.array_equal(got[3].cpu().numpy(), ref["top_ids"])
+        close(got[4], ref["top_logp"], "top_logp")

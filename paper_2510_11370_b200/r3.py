@@ -925,6 +925,23 @@ def _block_norms(s, L, w_pre, w_post, gate, eps, residual_scale, branch_scale, d
     return n, made
 
 
+def _stack_inputs(s, L, w_router, idx, w_gate, w_up, w_down, dev):
+    """The addresses of a stack's routers, records and expert weights, each of the type that the shape says
+    and with all L layers."""
+    router = torch.bfloat16 if s.router_w_dtype == R3_BF16 else torch.float32
+    expert, act = L * s.E * s.F * s.d, _act_dtype(s)
+    at = []
+    for name, t, n, dtype in (("w_router", w_router, L * s.E * s.d, router),
+                              ("idx", idx, L * s.T * s.K, _idx_dtype(s)), ("w_gate", w_gate, expert, act),
+                              ("w_up", w_up, expert, act), ("w_down", w_down, expert, act)):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name}: expected a torch.Tensor")
+        if t.numel() != n:
+            raise ValueError(f"{name}: {t.numel()} elements, expected {n} ({L} layers)")
+        at.append(_arg(name, t, t.shape, dtype, dev))
+    return at
+
+
 @_in_order
 def normed_stack(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down, *, w_pre, w_post=None,
                  gate=None, eps=1e-6, residual_scale=1.0, branch_scale=1.0, x_out=None, ws=None,
@@ -934,13 +951,13 @@ def normed_stack(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down, *, w
     Returns x_L [T, d]."""
     dev = _device_of("x0", x0)
     n, _ = _block_norms(s, L, w_pre, w_post, gate, eps, residual_scale, branch_scale, dev, False)
+    layers = _stack_inputs(s, L, w_router, idx, w_gate, w_up, w_down, dev)
     x0 = _arg("x0", x0, (s.T, s.d), _act_dtype(s), dev)
     if x_out is None:
         x_out = torch.empty((s.T, s.d), dtype=_act_dtype(s), device=dev)
     if ws is None:
         ws = workspace(lib.r3_normed_stack_workspace_bytes(ctypes.byref(s)), dev)
-    _check(lib.r3_normed_stack(ctypes.byref(s), L, ctypes.byref(n), x0, _ptr(w_router), _ptr(idx),
-                               _ptr(w_gate), _ptr(w_up), _ptr(w_down),
+    _check(lib.r3_normed_stack(ctypes.byref(s), L, ctypes.byref(n), x0, *layers,
                                _arg("x_out", x_out, (s.T, s.d), _act_dtype(s), dev), _ptr(ws),
                                ws.numel(), _ptr(dev_status), _stream(stream)))
     return x_out
@@ -959,6 +976,7 @@ def normed_stack_train(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down
     rows the gradients are zero and no step is taken."""
     dev = _device_of("x0", x0)
     n, dnorms = _block_norms(s, L, w_pre, w_post, gate, eps, residual_scale, branch_scale, dev, True)
+    layers = _stack_inputs(s, L, w_router, idx, w_gate, w_up, w_down, dev)
     x0, dy = (_arg(name, t, (s.T, s.d), _act_dtype(s), dev) for name, t in (("x0", x0), ("dy", dy)))
     f32 = dict(dtype=torch.float32, device=dev)
     x_out = torch.empty((s.T, s.d), dtype=_act_dtype(s), device=dev)
@@ -980,8 +998,7 @@ def normed_stack_train(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down
     if ws is None:
         ws = workspace(lib.r3_normed_stack_train_workspace_bytes(ctypes.byref(s), L), dev)
     _check(lib.r3_normed_stack_train(
-        ctypes.byref(s), L, ctypes.byref(n), x0, _ptr(w_router), _ptr(idx), _ptr(w_gate),
-        _ptr(w_up), _ptr(w_down), dy, _ptr(x_out), _ptr(dlogits), _ptr(dx0), _ptr(dw_r),
+        ctypes.byref(s), L, ctypes.byref(n), x0, *layers, dy, _ptr(x_out), _ptr(dlogits), _ptr(dx0), _ptr(dw_r),
         _ptr(dws[0]), _ptr(dws[1]), _ptr(dws[2]), None if config is None else ctypes.addressof(config),
         None if table is None else ctypes.addressof(table),
         _arg("grad_scale", grad_scale, (1,), torch.float32, dev),

@@ -104,3 +104,42 @@ def test_bad_optimisers(r3):
     shared = states()
     shared[3].exp_avg = shared[0].exp_avg                                           # another block's state
     assert train(r3, adamw=config(), states=shared) == bad
+
+
+def test_the_binding_checks_every_layers_tensors(r3, monkeypatch):
+    """Routers, records and expert weights of another type than the shape says, or with fewer layers, would
+    be read as raw bytes, past their ends: refused before the library is called (a stand-in here)."""
+    import torch
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*a):
+                calls.append(name)
+                return 0
+            return call
+    monkeypatch.setattr(r3, "lib", Library())
+    monkeypatch.setattr(r3, "_device_of", lambda name, t: t.device)
+    monkeypatch.setattr(r3, "_ptr", lambda t, host=False: None if t is None else ctypes.c_void_p(t.data_ptr()))
+    monkeypatch.setattr(r3, "_stream", lambda stream=None: None)
+    s = r3.make_shape(T, D, E, K, F)
+    bf = torch.bfloat16
+    x = torch.zeros((T, D), dtype=bf)
+    w_pre = torch.ones((L, D))
+    good = dict(w_router=torch.zeros((L, E, D)), idx=torch.zeros((L, T, K), dtype=torch.uint8),
+                w_gate=torch.zeros((L, E, F, D), dtype=bf), w_up=torch.zeros((L, E, F, D), dtype=bf),
+                w_down=torch.zeros((L, E, D, F), dtype=bf))
+    bad = [dict(idx=good["idx"].to(torch.int16)), dict(idx=good["idx"].to(torch.int64)),
+           dict(w_router=good["w_router"].to(bf)), dict(w_gate=good["w_gate"].float()),
+           dict(w_router=None), dict(w_up=good["w_up"].transpose(2, 3)),
+           dict(w_down=good["w_down"].to("meta"))]
+    bad += [{k: good[k][:1]} for k in good] + [{k: torch.cat([good[k]] * 2)} for k in good]
+    for kw in bad:
+        with pytest.raises((ValueError, TypeError)):
+            r3.normed_stack(s, L, x, **{**good, **kw}, w_pre=w_pre)
+        with pytest.raises((ValueError, TypeError)):
+            r3.normed_stack_train(s, L, x, **{**good, **kw}, dy=x, w_pre=w_pre)
+    assert not [c for c in calls if not c.endswith("_bytes")]
+    r3.normed_stack(s, L, x, **good, w_pre=w_pre)
+    r3.normed_stack_train(s, L, x, **good, dy=x, w_pre=w_pre)
+    assert [c for c in calls if not c.endswith("_bytes")] == ["r3_normed_stack", "r3_normed_stack_train"]

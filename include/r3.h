@@ -585,8 +585,8 @@ typedef struct {
  *    config's lr and step, for a captured step that is replayed with new values.
  *  - A gradient element that is not finite makes its own weight and states NaN (an 8-bit state: the
  *    NaN code; the scale is that of the block's finite elements).
- * Buffers that the step writes (params, masters, states, scales; of all entries) and that overlap are
- * refused; no gradient may overlap one of them.  No workspace. */
+ * Buffers that the step writes (params, masters, states, scales; of all entries) and that overlap, each
+ * other or a gradient, grad_scale or scalars, are refused.  No workspace. */
 r3_status r3_adamw_step(const r3_adamw* config, const r3_adamw_tensor* tensors, int32_t n_tensors,
                         const float* grad_scale, const float* scalars, void* stream);
 

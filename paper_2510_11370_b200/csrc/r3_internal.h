@@ -105,8 +105,10 @@ r3_status launch_permute_rows(const r3_shape* shape, const void* x, const int32_
 // What r3_adamw_step refuses, without the step.
 r3_status check_adamw_call(const r3_adamw* config, const r3_adamw_tensor* tensors, int32_t n_tensors,
                            const float* grad_scale, const float* scalars);
-// Its last part: the buffers that a step writes share no memory.
-r3_status check_adamw_distinct(const r3_adamw* config, const r3_adamw_tensor* tensors, int32_t n_tensors);
+// Its last part: the buffers that a step writes share no memory, with each other or with what it reads.  grads:
+// null, or the three gradients of a block's w_gate, w_up, w_down that stand in for the entries' own.
+r3_status check_adamw_distinct(const r3_adamw* config, const r3_adamw_tensor* tensors, int32_t n_tensors,
+                               const void* const* grads, const float* grad_scale, const float* scalars);
 
 // Number of SMs of the current device (cached).
 int sm_count();

@@ -179,7 +179,9 @@ extern "C" r3_status r3_normed_stack_train(const r3_shape* shape, int32_t L, con
             if (!block_states(l, e)) return R3_ERR_INVALID_ARG;
             if ((st = r3::check_adamw_call(adamw, e, 3, grad_scale, scalars)) != R3_OK) return st;
         }
-        if ((st = r3::check_adamw_distinct(adamw, expert_states, 3 * L)) != R3_OK) return st;
+        const void* grads[3] = {dw_gate, dw_up, dw_down};
+        st = r3::check_adamw_distinct(adamw, expert_states, 3 * L, grads, grad_scale, scalars);
+        if (st != R3_OK) return st;
     }
     if (shape->T == 0) return R3_OK;
     if (!x0 || !w_router || !idx || !w_gate || !w_up || !w_down || !dy || !x_out || !dlogits || !dx0 ||

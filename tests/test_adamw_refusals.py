@@ -107,3 +107,22 @@ def test_refused_gradients_leave_the_handle_as_it_was(r3, monkeypatch, bad):
     opt.set_grads(new)
     assert [row.grad for row in opt._table] == [g.data_ptr() for g in new]
     assert opt._config.grad_dtype == r3.R3_BF16
+
+
+FAR = 1 << 34
+
+
+@pytest.mark.parametrize("kw", [
+    dict(tensors=[dict(grad=A)]),                                         # a param as its own gradient
+    dict(tensors=[dict(grad=3 << 20)]), dict(tensors=[dict(grad=4 << 20)]),
+    dict(tensors=[dict(grad=A + 16 * (B // 16 - 1))]),                    # the last elements alone
+    dict(tensors=[{}, dict(grad=A)]), dict(tensors=[dict(grad=9 << 20), {}]),       # another entry's param
+    dict(tensors=[dict(param=FAR), dict(grad=3 << 20), {}]),              # lists that do not ascend
+    dict(tensors=[dict(param=FAR), dict(grad=FAR)]),
+    dict(param_dtype=1, master=1, tensors=[dict(master=9 << 20, grad=9 << 20)]),
+    dict(state_bits=8, tensors=[dict(exp_avg_scale=5 << 20, exp_avg_sq_scale=6 << 20, grad=6 << 20)]),
+    dict(grad_scale=ctypes.c_void_p(A + 396)), dict(scalars=ctypes.c_void_p(A + 396)),
+    dict(grad_scale=ctypes.c_void_p((4 << 20) + 8)), dict(scalars=ctypes.c_void_p((4 << 20) - 8)),
+])
+def test_reading_what_is_written_is_refused(r3, kw):
+    assert call(r3, **kw) == r3.R3_ERR_INVALID_ARG

@@ -143,3 +143,55 @@ def test_the_binding_checks_every_layers_tensors(r3, monkeypatch):
     r3.normed_stack(s, L, x, **good, w_pre=w_pre)
     r3.normed_stack_train(s, L, x, **good, dy=x, w_pre=w_pre)
     assert [c for c in calls if not c.endswith("_bytes")] == ["r3_normed_stack", "r3_normed_stack_train"]
+
+
+def test_random_layouts_against_every_pair(r3):
+    """States of small blocks at random places (in order, list by list, interleaved or overlapping) and three
+    gradients among them: refused exactly where a written buffer meets another buffer.  What is not refused
+    gets as far as the workspace, which is missing."""
+    import random
+    rng = random.Random(3)
+    s = r3.make_shape(16, 8, 1, 1, 8)
+    n = 64                                                               # elements of a block's weight
+    found = {True: 0, False: 0}
+    for trial in range(1500):
+        layers, bits, master = rng.randint(1, 4), rng.choice([8, 32]), rng.random() < 0.4
+        count = 3 * layers
+        fields = ["exp_avg", "exp_avg_sq"] + (["master"] if master else [])
+        fields += ["exp_avg_scale", "exp_avg_sq_scale"] if bits == 8 else []
+        size = dict(exp_avg=n * bits // 8, exp_avg_sq=n * bits // 8, master=4 * n, exp_avg_scale=4,
+                    exp_avg_sq_scale=4)
+        keys = [(i, f) for i in range(count) for f in fields] + [(i, "grad") for i in range(3)]
+        if rng.random() < 0.5:                                           # list by list
+            keys.sort(key=lambda k: (k[1], k[0]))
+        places = rng.sample(range(1, rng.choice([len(keys) + 8, 10 * len(keys), 4000])), len(keys))
+        if rng.random() < 0.6:
+            places.sort()
+        unit = rng.choice([128, 256, 256])
+        at = {k: (1 << 30) + p * unit for k, p in zip(keys, places)}
+        weights = [(1 << 29) + k * 4096 for k in range(3)]
+        if rng.random() < 0.3:                                           # the weights among the states
+            weights[rng.randrange(3)] = (1 << 30) + rng.randrange(max(places) + 1) * unit
+        written = [(at[i, f], size[f]) for i in range(count) for f in fields]
+        written += [(weights[i % 3] + i // 3 * 2 * n, 2 * n) for i in range(count)]
+        read = [(at[k, "grad"], 4 * n) for k in range(3)]
+        scale = (1 << 30) + rng.randrange(max(places) + 1) * unit + 64 if rng.random() < 0.2 else None
+        if scale:
+            read.append((scale, 4))
+        rows = [r3.AdamWTensor(param=weights[i % 3] + i // 3 * 2 * n, n=n, weight_decay=0.0,
+                               **{f: at[i, f] for f in fields}) for i in range(count)]
+        table = (r3.AdamWTensor * count)(*rows)
+        config = r3.AdamWConfig(param_dtype=1, grad_dtype=0, master=int(master), state_bits=bits, step=1, lr=0.1,
+                                beta1=0.9, beta2=0.99, eps=1e-8)
+        a = P[:3] + [ctypes.c_void_p(w) for w in weights] + P[6:11]
+        a += [ctypes.c_void_p(at[k, "grad"]) for k in range(3)]
+        got = r3.lib.r3_normed_stack_train(
+            ctypes.byref(s), layers, ctypes.byref(norms(r3)), *a, ctypes.addressof(config),
+            ctypes.addressof(table), ctypes.c_void_p(scale) if scale else None, None, None, 0, None, None)
+
+        def meet(p, q):
+            return p[0] < q[0] + q[1] and q[0] < p[0] + p[1]
+        bad = any(meet(p, q) for i, p in enumerate(written) for q in written[:i] + read)
+        found[bad] += 1
+        assert got == (r3.R3_ERR_INVALID_ARG if bad else r3.R3_ERR_WORKSPACE), (trial, bad, got)
+    assert min(found.values()) > 200, found

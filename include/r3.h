@@ -625,7 +625,10 @@ r3_status r3_normed_stack(const r3_shape* shape, int32_t L, const r3_block_norms
  * at the end), so that no more than that exists at a time.  expert_states (HOST) has 3 L entries, block
  * by block w_gate, w_up, w_down, as for r3_adamw_step; param must be the block's weights, grad is
  * ignored.  adamw, grad_scale and scalars as for r3_adamw_step, param_dtype R3_BF16, grad_dtype R3_F32.
- * With T = 0 nothing is written and no step taken.
+ * With T = 0 nothing is written and no step taken.  A block takes no step once dev_status is not 0, by an
+ * error of this call (with dev_status NULL the call watches for itself) or one that it still holds: an invalid
+ * record is found in the forward pass, before any step; a wait that runs out in the backward pass leaves the
+ * blocks behind it stepped, and those before it as they were.
  * workspace: r3_normed_stack_train_workspace_bytes(shape, L). */
 size_t r3_normed_stack_train_workspace_bytes(const r3_shape* shape, int32_t L);
 r3_status r3_normed_stack_train(const r3_shape* shape, int32_t L, const r3_block_norms* norms,

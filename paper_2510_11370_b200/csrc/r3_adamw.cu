@@ -58,6 +58,7 @@ struct AdamScalars {
     float beta1, one_beta1, beta2, one_beta2, eps, lr, bias1, bias2, one;
     const float* grad_scale;
     const float* dynamic;                           // {lr, bias1, bias2} on the device, or null
+    const int32_t* dev_status;                      // not null: no step where an error stands in it
     int tensors, per_warp;
 };
 template <int CAP> struct AdamTable {
@@ -463,7 +464,9 @@ __global__ void __launch_bounds__(kAdamThreads, BITS8 ? kAdamCtas8 : kAdamCtas) 
     extern __shared__ uint4 ring_all[];             // 8-bit states: [warps][kAdamStages] stages
     AdamRates r;
     r.gs = a.s.grad_scale ? *a.s.grad_scale : 1.f;
-    if (!(fabsf(r.gs) <= 3.402823466e38f)) return;  // NaN or infinite: the step is skipped
+    const int32_t error = a.s.dev_status ? *a.s.dev_status : R3_DEV_OK;
+    // NaN or infinite, or gradients that an error was reported for: the step is skipped
+    if (!(fabsf(r.gs) <= 3.402823466e38f) || error != R3_DEV_OK) return;
     const float lr = a.s.dynamic ? a.s.dynamic[0] : a.s.lr;
     r.step = lr * (a.s.dynamic ? a.s.dynamic[1] : a.s.bias1);
     r.bias2 = a.s.dynamic ? a.s.dynamic[2] : a.s.bias2;
@@ -716,14 +719,10 @@ static r3_status launch_adamw(const r3_adamw* c, const AdamScalars& s, const r3_
                      : launch_adamw<__nv_bfloat16, G, false>(c, s, ts, count, cs);
 }
 
-}  // namespace r3
-
-extern "C" r3_status r3_adamw_step(const r3_adamw* config, const r3_adamw_tensor* tensors,
-                                   int32_t n_tensors, const float* grad_scale, const float* scalars,
-                                   void* stream) {
-    const r3_status st = r3::check_adamw_call(config, tensors, n_tensors, grad_scale, scalars);
-    if (st != R3_OK) return st;
-    r3::AdamScalars s = {};
+r3_status adamw_step(const r3_adamw* config, const r3_adamw_tensor* tensors, int32_t n_tensors,
+                     const float* grad_scale, const float* scalars, const int32_t* dev_status,
+                     cudaStream_t cs) {
+    AdamScalars s = {};
     s.beta1 = (float)config->beta1;
     s.one_beta1 = (float)(1.0 - config->beta1);
     s.beta2 = (float)config->beta2;
@@ -735,8 +734,18 @@ extern "C" r3_status r3_adamw_step(const r3_adamw* config, const r3_adamw_tensor
     s.one = 1.f;
     s.grad_scale = grad_scale;
     s.dynamic = scalars;
-    cudaStream_t cs = static_cast<cudaStream_t>(stream);
-    return config->grad_dtype == R3_F32
-               ? r3::launch_adamw<float>(config, s, tensors, n_tensors, cs)
-               : r3::launch_adamw<__nv_bfloat16>(config, s, tensors, n_tensors, cs);
+    s.dev_status = dev_status;
+    return config->grad_dtype == R3_F32 ? launch_adamw<float>(config, s, tensors, n_tensors, cs)
+                                        : launch_adamw<__nv_bfloat16>(config, s, tensors, n_tensors, cs);
+}
+
+}  // namespace r3
+
+extern "C" r3_status r3_adamw_step(const r3_adamw* config, const r3_adamw_tensor* tensors,
+                                   int32_t n_tensors, const float* grad_scale, const float* scalars,
+                                   void* stream) {
+    const r3_status st = r3::check_adamw_call(config, tensors, n_tensors, grad_scale, scalars);
+    if (st != R3_OK) return st;
+    return r3::adamw_step(config, tensors, n_tensors, grad_scale, scalars, nullptr,
+                          static_cast<cudaStream_t>(stream));
 }

@@ -102,6 +102,10 @@ r3_status launch_permute_rows(const r3_shape* shape, const void* x, const int32_
                               void* xp, cudaStream_t stream, int32_t* dev_status,
                               bool x_early = false);
 
+// r3_adamw_step without its checks; dev_status (or null): the step is skipped where it is not R3_DEV_OK.
+r3_status adamw_step(const r3_adamw* config, const r3_adamw_tensor* tensors, int32_t n_tensors,
+                     const float* grad_scale, const float* scalars, const int32_t* dev_status,
+                     cudaStream_t stream);
 // What r3_adamw_step refuses, without the step.
 r3_status check_adamw_call(const r3_adamw* config, const r3_adamw_tensor* tensors, int32_t n_tensors,
                            const float* grad_scale, const float* scalars);

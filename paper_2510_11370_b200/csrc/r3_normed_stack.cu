@@ -10,6 +10,8 @@
 
 namespace r3 {
 
+constexpr size_t kStatusBytes = 256;          // a status word of the call's own, and the alignment behind it
+
 struct StackCall {
     const r3_shape* s;
     int32_t L;
@@ -140,7 +142,7 @@ extern "C" size_t r3_normed_stack_train_workspace_bytes(const r3_shape* shape, i
     c.s = shape;
     c.n = &n;
     const r3_norm q = c.shape(-1);
-    return (3 * (size_t)L + 4) * xb + r3_norm_residual_bwd_workspace_bytes(&q) +
+    return (3 * (size_t)L + 4) * xb + r3_norm_residual_bwd_workspace_bytes(&q) + r3::kStatusBytes +
            r3_replay_layer_train_workspace_bytes(shape);
 }
 
@@ -204,10 +206,20 @@ extern "C" r3_status r3_normed_stack_train(const r3_shape* shape, int32_t L, con
     const r3_norm q = c.shape(-1);
     void* norm_ws = rest + 4 * xb;
     const size_t norm_bytes = r3_norm_residual_bwd_workspace_bytes(&q);
-    void* inner = rest + 4 * xb + norm_bytes;
+    char* own_status = rest + 4 * xb + norm_bytes;
+    void* inner = own_status + r3::kStatusBytes;
     const size_t fwd_bytes = r3_replay_layer_workspace_bytes(shape);
     const size_t train_bytes = r3_replay_layer_train_workspace_bytes(shape);
 
+    cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    if (adamw && !dev_status) {
+        // the steps look at what the blocks report, so that gradients which are not valid move no weight
+        dev_status = reinterpret_cast<int32_t*>(own_status);
+        if (cudaMemsetAsync(dev_status, 0, sizeof(int32_t), cs) != cudaSuccess) {
+            cudaGetLastError();
+            return R3_ERR_CUDA;
+        }
+    }
     if ((st = c.between(0, x0, nullptr, nullptr, h_at(0))) != R3_OK) return st;
     for (int32_t l = 0; l < L; ++l) {
         // the gradients that this call forms from dy are overwritten below
@@ -236,7 +248,7 @@ extern "C" r3_status r3_normed_stack_train(const r3_shape* shape, int32_t L, con
             // no later step reads block l's expert weights: they take their step while only this
             // block's gradients exist
             block_states(l, e);
-            if ((st = r3_adamw_step(adamw, e, 3, grad_scale, scalars, stream)) != R3_OK) return st;
+            if ((st = r3::adamw_step(adamw, e, 3, grad_scale, scalars, dev_status, cs)) != R3_OK) return st;
         }
     }
     return c.between_bwd(0, x0, nullptr, around, dh, dx0, nullptr, norm_ws, norm_bytes);

@@ -973,7 +973,8 @@ def normed_stack_train(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down
     dw_up, dw_down).  With optimiser, an AdamW over [w_gate[0], w_up[0], w_down[0], w_gate[1], ..] without
     gradients of its own, every block's expert weights take step `step` with rate `lr` as soon as their
     gradients are there, and only one block's gradients exist at a time (block 0's are returned).  Without
-    rows the gradients are zero and no step is taken."""
+    rows the gradients are zero and no step is taken; nor is one once dev_status holds an error, of this call
+    (noticed without a dev_status too) or from before."""
     dev = _device_of("x0", x0)
     n, dnorms = _block_norms(s, L, w_pre, w_post, gate, eps, residual_scale, branch_scale, dev, True)
     layers = _stack_inputs(s, L, w_router, idx, w_gate, w_up, w_down, dev)

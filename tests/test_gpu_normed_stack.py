@@ -278,3 +278,30 @@ def test_wrong_rows_are_refused(r3):
             r3.normed_stack_train(s, 1, x0, w_r, idx, *ex, bad, **norms)
     with pytest.raises(ValueError):
         r3.normed_stack(s, 1, x0, w_r, idx, *ex, x_out=x0[:11], **norms)
+
+
+@pytest.mark.parametrize("kw", [dict(state_bits=8), dict(state_bits=32, masters=True)])
+@pytest.mark.parametrize("case", ["word from before", "bad record", "bad record, no word"])
+def test_no_step_after_an_error(r3, case, kw):
+    """An error that stands in dev_status, or that a block reports in this call, leaves weights, masters and
+    states as they were; the same call without it steps."""
+    T, d, E, K, F, L = 50, 128, 8, 2, 64, 2
+    w, x0, dy, w_r, idx, ex, norms = build(T, d, E, K, F, L)
+    s, opt = r3.shape_of(w), handle(r3, ex, L, **kw)
+    held = ex + opt.exp_avg + opt.exp_avg_sq + (opt.masters or []) + (opt.exp_avg_scale or [])
+    held = [t.detach().view(torch.uint8) for t in held]
+    before = [t.clone() for t in held]
+    st = r3.new_status("cuda")
+    record = idx.clone()
+    if case == "word from before":
+        st.fill_(r3.DEV_TIMEOUT)
+    else:
+        record[0, 7, 1] = E                                   # the first block's: its backward is the last
+    word = None if case.endswith("no word") else st
+    r3.normed_stack_train(s, L, x0, w_r, record, *ex, dy, optimiser=opt, step=1, lr=1e-2, dev_status=word, **norms)
+    if word is not None:
+        assert st.item() == (r3.DEV_TIMEOUT if case == "word from before" else r3.DEV_BAD_INDEX)
+    assert all(torch.equal(p, q) for p, q in zip(before, held))
+    st.zero_()
+    r3.normed_stack_train(s, L, x0, w_r, idx, *ex, dy, optimiser=opt, step=1, lr=1e-2, dev_status=word, **norms)
+    assert st.item() == 0 and not any(torch.equal(p, q) for p, q in zip(before, held))

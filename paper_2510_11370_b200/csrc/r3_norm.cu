@@ -101,9 +101,7 @@ static bool plan_norm(const r3_norm* s, bool bwd, NormPlan* p) {
         if (rows < 1) rows = 1;
         p->threads = 32 * rows;
     }
-    const size_t per_row = (size_t)(bwd ? 4 : 2) * p->pieces * p->threads * 16 * (p->pair ? 2 : 1);
-    p->stages = kNormStages * per_row <= (size_t)kNormRingBytes ? kNormStages : 1;
-    p->smem = p->stages * per_row;
+    p->smem = (size_t)norm_stages(p->pieces, bwd) * norm_ring_bytes(p->pieces, bwd, p->threads) * (p->pair ? 2 : 1);
     int per_sm = resident / p->threads;
     const int by_smem = (int)(kNormRingBytes / p->smem);
     if (per_sm > by_smem) per_sm = by_smem;

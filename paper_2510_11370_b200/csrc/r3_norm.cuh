@@ -17,8 +17,9 @@
 // of the rows to come there (cp.async), S rows ahead, so no barrier or wait between threads belongs
 // to the copies (65536 x 2048 bf16: forward 176 us = 93% of the measured copy bandwidth, backward 258 us =
 // 95%, 274 at the clock of a power-capped second; 16384 x 2048: 50 and 76 us, of which the second
-// kernel, which adds up the CTAs' sums of the weight gradients, takes 5; backward 8192 x 4096 82 us, 4096 x
-// 8192 105 and 2048 x 16384 174 of 62: the wide form lacks registers).  A warp's pieces are neighbours
+// kernel, which adds up the CTAs' sums of the weight gradients, takes 5; backward 8192 x 4096, two rows at a
+// time, 82 us of 62; 4096 x 8192 and 2048 x 16384, the wide form, 105 and 174 of 62: it lacks registers).  A
+// warp's pieces are neighbours
 // (piece p of lane l is piece 32 p + l of the warp's share), so that all of a thread's addresses of a row
 // are one base and constant offsets.
 #pragma once
@@ -148,8 +149,8 @@ template <typename T> __device__ __forceinline__ void store_piece(T* p, const fl
 // registers left, knows the most usual calls only.
 enum { kHasY = 1, kHasPost = 2, kHasPre = 4, kHasUp = 8, kTokenGate = 16, kFullGate = 32, kOpen = 64 };
 
-// The weights of a thread's columns, kept for all its rows in registers; in the wide form read again
-// from L1 for each row (no room).  A column's factor is the vector's element
+// The weights of a thread's columns: with KEEP in registers for all its rows, else (the wide form's longer
+// rows, which have no room) read again from L1 for each.  A column's factor is the vector's element
 // (1 without a vector) times `times` (likewise) times `scale`.
 template <typename W, int N, int P, bool KEEP> struct Weights {
     float w[KEEP ? P : 1][KEEP ? N : 1];
@@ -638,11 +639,20 @@ norm_bwd_kernel(const NormArgs a) {
 }
 
 // ---- launch ---------------------------------------------------------------------------------------
-constexpr int kNormStages = 3;               // rows in a thread's ring; 1 where three do not fit
 constexpr int kNormRingBytes = 200 * 1024;   // of an SM's shared memory, for the rings of its CTAs
+// Rows in a thread's ring.  Three fit everywhere but in the backward of the longest rows, where 288 threads or
+// more with four pieces of four arrays each need 72 KB and more for one.
+__host__ __device__ constexpr int norm_stages(int pieces, bool bwd) { return bwd && pieces > kNormPieces ? 1 : 3; }
+__host__ __device__ constexpr int norm_ring_bytes(int pieces, bool bwd, int threads) {      // one row's
+    return (bwd ? 4 : 2) * pieces * threads * 16;
+}
+static_assert(3 * norm_ring_bytes(2 * kNormPieces, false, kNormMaxThreads) <= kNormRingBytes, "");
+static_assert(3 * norm_ring_bytes(kNormPieces, true, kNormMaxThreads) <= kNormRingBytes, "");
+static_assert(3 * norm_ring_bytes(kNormPieces, true, 2 * kNormPairThreads) <= kNormRingBytes, "");
+static_assert(norm_ring_bytes(2 * kNormPieces, true, kNormMaxThreads) <= kNormRingBytes, "");
 
 struct NormPlan {
-    int pieces, threads, grid, stages;
+    int pieces, threads, grid;
     bool warp, wide, pair;
     size_t smem;
 };
@@ -659,14 +669,14 @@ static r3_status launch_norm_kernel(const NormArgs& a, const NormPlan& p, cudaSt
     KERN<<<p.grid, p.threads, p.smem, cs>>>(a);
     return launch_status();
 }
-template <typename T, typename W, int P, bool WARP, bool WIDE, int S, int R>
+template <typename T, typename W, int P, bool WARP, bool WIDE, int R>
 static r3_status launch_norm(const NormArgs& a, const NormPlan& p, bool bwd, cudaStream_t cs) {
     const bool full = a.gate_kind == R3_GATE_FULL, token = a.gate_kind == R3_GATE_TOKEN;
     if constexpr (R == 1) {
         if (!bwd) {
             auto run = [&](auto form) {
                 constexpr int F = decltype(form)::value;
-                return launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, S, F>>(a, p, cs);
+                return launch_norm_kernel<norm_fwd_kernel<T, W, P, WARP, WIDE, norm_stages(P, false), F>>(a, p, cs);
             };
             constexpr int BOTH = kHasY | kHasPost | kHasPre;
             if (!a.y) return run(std::integral_constant<int, kHasPre>());
@@ -678,7 +688,7 @@ static r3_status launch_norm(const NormArgs& a, const NormPlan& p, bool bwd, cud
     }
     auto run = [&](auto form) {
         constexpr int F = decltype(form)::value;
-        return launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, S, R, F>>(a, p, cs);
+        return launch_norm_kernel<norm_bwd_kernel<T, W, P, WARP, WIDE, norm_stages(P, true), R, F>>(a, p, cs);
     };
     auto gated = [&](auto form) {
         constexpr int F = decltype(form)::value | kHasY | kHasUp;
@@ -697,14 +707,13 @@ static r3_status launch_norm(const NormArgs& a, const NormPlan& p, bool bwd, cud
 }
 template <typename T, typename W>
 static r3_status launch_norm_size(const NormArgs& a, const NormPlan& p, bool bwd, cudaStream_t cs) {
-    constexpr int P = kNormPieces, S = kNormStages;
-    if (p.warp) return launch_norm<T, W, P, true, false, S, 1>(a, p, bwd, cs);
+    constexpr int P = kNormPieces;
+    if (p.warp) return launch_norm<T, W, P, true, false, 1>(a, p, bwd, cs);
     if (!p.wide)
-        return p.pair ? launch_norm<T, W, P, false, false, S, 2>(a, p, bwd, cs)
-                      : launch_norm<T, W, P, false, false, S, 1>(a, p, bwd, cs);
-    if (p.pieces == P) return launch_norm<T, W, P, false, true, S, 1>(a, p, bwd, cs);
-    return p.stages > 1 ? launch_norm<T, W, 2 * P, false, true, S, 1>(a, p, bwd, cs)
-                        : launch_norm<T, W, 2 * P, false, true, 1, 1>(a, p, bwd, cs);
+        return p.pair ? launch_norm<T, W, P, false, false, 2>(a, p, bwd, cs)
+                      : launch_norm<T, W, P, false, false, 1>(a, p, bwd, cs);
+    return p.pieces == P ? launch_norm<T, W, P, false, true, 1>(a, p, bwd, cs)
+                         : launch_norm<T, W, 2 * P, false, true, 1>(a, p, bwd, cs);
 }
 
 // By the rows' type, in a file each (they compile side by side).

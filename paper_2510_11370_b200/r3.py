@@ -290,6 +290,19 @@ def workspace(nbytes: int, device) -> torch.Tensor:
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 
+def _scratch(ws, nbytes: int, dev) -> torch.Tensor:
+    """A call's scratch: the caller's, checked, or new."""
+    if ws is None:
+        return workspace(nbytes, dev)
+    if not isinstance(ws, torch.Tensor):
+        raise TypeError("ws: expected a torch.Tensor")
+    if ws.device != dev:
+        raise ValueError(f"ws: on {ws.device}, expected {dev}")
+    if not ws.is_contiguous():
+        raise ValueError("ws: tensor must be contiguous")
+    return ws
+
+
 def new_status(device) -> torch.Tensor:
     return torch.zeros(1, dtype=torch.int32, device=device)
 
@@ -779,8 +792,7 @@ def norm_residual_bwd(x_out, y, dx_out, dh=None, *, w_post=None, gate=None, w_pr
             dw_pre = sums.pop()
     if gate is not None and not channel:
         dgate = torch.empty_like(gate)           # float32 [T] or [T, 1], or [T, d] of the rows' type
-    if ws is None:
-        ws = workspace(lib.r3_norm_residual_bwd_workspace_bytes(ctypes.byref(s)), dev)
+    ws = _scratch(ws, lib.r3_norm_residual_bwd_workspace_bytes(ctypes.byref(s)), dev)
     _check(lib.r3_norm_residual_bwd(
         ctypes.byref(s), src[0], src[1], post, gate_at, pre, src[2], src[3],
         at_dx, at_dy, None if dw_post is None else dw_post.data_ptr(),
@@ -955,8 +967,7 @@ def normed_stack(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down, *, w
     x0 = _arg("x0", x0, (s.T, s.d), _act_dtype(s), dev)
     if x_out is None:
         x_out = torch.empty((s.T, s.d), dtype=_act_dtype(s), device=dev)
-    if ws is None:
-        ws = workspace(lib.r3_normed_stack_workspace_bytes(ctypes.byref(s)), dev)
+    ws = _scratch(ws, lib.r3_normed_stack_workspace_bytes(ctypes.byref(s)), dev)
     _check(lib.r3_normed_stack(ctypes.byref(s), L, ctypes.byref(n), x0, *layers,
                                _arg("x_out", x_out, (s.T, s.d), _act_dtype(s), dev), _ptr(ws),
                                ws.numel(), _ptr(dev_status), _stream(stream)))
@@ -996,8 +1007,7 @@ def normed_stack_train(s: Shape, L: int, x0, w_router, idx, w_gate, w_up, w_down
         lead = () if optimiser is not None else (L,)
         dws = (new(lead + (s.E, s.F, s.d), **f32), new(lead + (s.E, s.F, s.d), **f32),
                new(lead + (s.E, s.d, s.F), **f32))
-    if ws is None:
-        ws = workspace(lib.r3_normed_stack_train_workspace_bytes(ctypes.byref(s), L), dev)
+    ws = _scratch(ws, lib.r3_normed_stack_train_workspace_bytes(ctypes.byref(s), L), dev)
     _check(lib.r3_normed_stack_train(
         ctypes.byref(s), L, ctypes.byref(n), x0, *layers, dy, _ptr(x_out), _ptr(dlogits), _ptr(dx0), _ptr(dw_r),
         _ptr(dws[0]), _ptr(dws[1]), _ptr(dws[2]), None if config is None else ctypes.addressof(config),

@@ -124,3 +124,28 @@ def test_a_vector_with_as_many_rows_as_columns(r3):
                        ("channel", torch.ones(4, 64))):
         with pytest.raises(ValueError):
             kind_of(r3, 4, 64, gate, f32, said)
+
+
+def test_scratch_of_another_device_is_refused(r3, monkeypatch):
+    """A caller's workspace is looked at like every other tensor: its address would be written to (a stand-in
+    for the library here, host tensors for the device's)."""
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*a):
+                calls.append(name)
+                return 0
+            return call
+    monkeypatch.setattr(r3, "lib", Library())
+    monkeypatch.setattr(r3, "_device_of", lambda name, t: t.device)
+    monkeypatch.setattr(r3, "_stream", lambda stream=None: None)
+    x, w = torch.zeros((4, 64)), torch.ones(64)
+    room = torch.zeros(1 << 16, dtype=torch.uint8)
+    for bad in (room.to("meta"), room[::2], 4096):
+        with pytest.raises((ValueError, TypeError)):
+            r3.norm_residual_bwd(x, x, x, x, w_post=w, w_pre=w, ws=bad)
+    assert "r3_norm_residual_bwd" not in calls
+    r3.norm_residual_bwd(x, x, x, x, w_post=w, w_pre=w, ws=room)
+    r3.norm_residual_bwd(x, x, x, x, w_post=w, w_pre=w)
+    assert calls.count("r3_norm_residual_bwd") == 2

@@ -583,8 +583,8 @@ typedef struct {
  *    is not finite the whole step is skipped: nothing is written.
  *  - scalars (device, [3] float32, or NULL): {lr, 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)} in place of
  *    config's lr and step, for a captured step that is replayed with new values.
- *  - A gradient element that is not finite makes its own weight and states NaN (an 8-bit state: the
- *    NaN code; the scale is that of the block's finite elements).
+ *  - A gradient element that is not finite makes its own weight NaN and its states NaN, or infinite as the
+ *    gradient is (an 8-bit state: the NaN code; the scale is that of the block's finite elements).
  * Buffers that the step writes (params, masters, states, scales; of all entries) and that overlap, each
  * other or a gradient, grad_scale or scalars, are refused.  No workspace. */
 r3_status r3_adamw_step(const r3_adamw* config, const r3_adamw_tensor* tensors, int32_t n_tensors,

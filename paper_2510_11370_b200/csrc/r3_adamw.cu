@@ -4,9 +4,9 @@
 //   w = w (1 - lr decay) - lr / (1 - beta1^t)  m / ( sqrt(v) / sqrt(1 - beta2^t) + eps )
 //
 // Bound by HBM (12.06 bytes an element for bf16 weights, float32 gradients and 8-bit states; 28 for
-// float32 with 32-bit states): 604 M elements of the former 1125 us = 99% of the measured copy bandwidth
-// (1220 at the clock of a power-capped second), 120 M bf16 elements with master weights, bf16 gradients
-// and 32-bit states 521 us = 99%.  States of 8 bits are kept in blocks of 256 elements with one scale:
+// float32 with 32-bit states): 604 M elements of the former 1110 us = the measured copy bandwidth (1270
+// at the clock of a power-capped second, where instruction issue bounds it), 120 M bf16 elements with
+// master weights, bf16 gradients and 32-bit states 522 us = 98%.  States of 8 bits are kept in blocks of 256 elements with one scale:
 // e4m3 codes times the smallest power of two (at least 2^-126) that brings the block's largest
 // magnitude to 448 or less, so that scaling is exact both ways and the one rounding is the code's.
 // The second moment is kept as its square root, which halves the range its codes have to span; a
@@ -311,9 +311,9 @@ template <typename P, typename G, bool MASTER, bool BITS8> struct AdamBlock {
     typedef typename std::conditional<BITS8, uint8_t, float>::type St;
     // bf16 weights without masters and 8-bit states: the update's root and quotient are the hardware's
     // approximations, a unit or two of 2^-23 off beside the weight's rounding of 2^-9, and the codes are
-    // secured by themselves.  This form is bound by instruction issue: 604 M elements 1260 us, 1350 with the
-    // exact root, 1540 with the exact quotient too (1215 with approximate codes); with float32 weights
-    // or 32-bit states the exact ones cost 0.3%.
+    // secured by themselves.  At the clock of a power-capped second this form is bound by instruction issue: 604
+    // M elements 1260 us, 1350 with the exact root, 1540 with the exact quotient too (1215 with approximate
+    // codes); with 32-bit states the exact ones cost 0.3%.
     static constexpr bool APPROX = BITS8 && sizeof(Wt) == 2;
     Four<Wt> w[2];
     Four<G> g[2];

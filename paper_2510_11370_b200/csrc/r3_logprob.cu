@@ -16,7 +16,7 @@
 // the entropy, 6.2 instructions (10 before the rounds without bounds checks, the widening by shift and
 // mask and the sums in two lanes).  8192 x 151936 bf16 with entropy, a tenth of the rows skipped: 342 us =
 // the measured copy bandwidth; launched back to back for seconds the power cap takes the SM clock to 1.55
-// GHz and the exponentials alone need 290 of 354 to 370 us.  One row per CTA and many CTAs: CTAs that walked
+// GHz and the exponentials alone need 290 of 354 to 380 us.  One row per CTA and many CTAs: CTAs that walked
 // over rows, the next row's first pieces on their way early, took 444 us where this form took 383.
 // Few rows: up to eight CTAs of a cluster share one (16 x 131072 bf16: 4.4 us, with 20 alternatives 9.5,
 // of which the alternatives' four barriers, second look at the row and exchange take 5).
@@ -848,11 +848,11 @@ extern "C" r3_status r3_token_logprobs(const r3_logits* shape, const void* logit
     const long long row_bytes = (long long)shape->V * (long long)es;
     // Threads per row: with more than its pieces keep busy the reductions at a row's end cost more than
     // its loads, and many small CTAs on an SM end at different times, which keeps the loads flowing
-    // (8192 rows of bf16: 6000 columns 34.7 us at 128 threads, 26.6 at 32; 12000 columns 61.4 at 256,
-    // 45.1 at 128; 151936 columns with 5 alternatives 429 at 256, 410 at 128).  Long rows that are few enough
+    // (8192 rows of bf16: 6000 columns 30.8 us at 128 threads, 25.6 at 32; 12000 columns 59.4 at 256,
+    // 44.3 at 128; 151936 columns with 5 alternatives 427 at 256, 418 at 128).  Long rows that are few enough
     // for whole waves to count: 256 threads where those take less of them, a wave of 128 holding twice the
-    // rows and lasting twice as long (50257 columns of float32 with 5 alternatives: 300 rows 18.6 at 256,
-    // 24.7 at 128; 600 rows 37.1 and 30.4; 900 41.4 and 37.1; 1200 58.0 and 60.1; 2048 83.8 and 74.6).
+    // rows and lasting twice as long (50257 columns of float32 with 5 alternatives: 300 rows 18.5 at 256,
+    // 24.6 at 128; 600 rows 36.9 and 30.3; 900 41.0 and 36.8; 1200 57.4 and 59.5; 2048 82.5 and 75.6).
     auto waves = [&](int nt) {
         const int resident = r3::logprob_ctas(nt) * r3::sm_count();
         return (a.T + resident - 1) / resident;
@@ -861,8 +861,8 @@ extern "C" r3_status r3_token_logprobs(const r3_logits* shape, const void* logit
                         : row_bytes <= 49152                              ? 128
                         : waves(128) <= 4 && waves(256) < 2 * waves(128) ? 256
                                                                           : 128;
-    // Few rows: a cluster of CTAs shares one, as long as they all run at once and a thread has two
-    // pieces or more.
+    // Few rows: a cluster of CTAs shares one, as long as each has an SM of its own and a thread two pieces
+    // or more.
     a.split = 1;
     while (a.split < r3::kMaxSplit && (long long)a.T * a.split <= r3::sm_count() &&
            row_bytes / (a.split * 2) >= 2LL * 16 * threads)

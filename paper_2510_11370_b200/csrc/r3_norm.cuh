@@ -15,10 +15,10 @@
 // The columns' weights and the sums of the weight gradients stay in its registers.  What hides the
 // memory latency is a ring in shared memory that is private to the thread: it copies its own pieces
 // of the rows to come there (cp.async), S rows ahead, so no barrier or wait between threads belongs
-// to the copies (65536 x 2048 bf16: forward 176 us = 93% of the measured copy bandwidth, backward 258 us =
-// 95%, 274 at the clock of a power-capped second; 16384 x 2048: 50 and 76 us, of which the second
+// to the copies (65536 x 2048 bf16: forward 176 us = 93% of the measured copy bandwidth, backward 258 to
+// 274 us by GPU = 95 to 90%; 16384 x 2048: 50 and 76 us, of which the second
 // kernel, which adds up the CTAs' sums of the weight gradients, takes 5; backward 8192 x 4096, two rows at a
-// time, 82 us of 62; 4096 x 8192 and 2048 x 16384, the wide form, 105 and 174 of 62: it lacks registers).  A
+// time, 83 us of 62; 4096 x 8192 and 2048 x 16384, the wide form, 106 and 180 of 62: it lacks registers).  A
 // warp's pieces are neighbours
 // (piece p of lane l is piece 32 p + l of the warp's share), so that all of a thread's addresses of a row
 // are one base and constant offsets.

@@ -642,7 +642,7 @@ r3_status check_adamw_distinct(const r3_adamw* c, const r3_adamw_tensor* ts, int
         std::vector<Range> many;
         Range* all = few;
         size_t n = 0;
-        if (count * KINDS <= FEW) {
+        if (count <= FEW / KINDS) {
             each_written(c, ts, count, [&](int, uintptr_t begin, uintptr_t end) {
                 size_t i = n++;
                 for (; i > 0 && begin < few[i - 1].first; --i) few[i] = few[i - 1];

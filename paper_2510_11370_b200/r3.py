@@ -812,7 +812,8 @@ class AdamW:
     bfloat16).  masters: None, True (float32 copies of bfloat16 params are made and kept) or a list
     of float32 tensors.  States are made (zero) or given as lists: float32, or with state_bits=8
     float8_e4m3fn codes plus one float32 scale per 256 elements (exp_avg_sq then holds the root of
-    the second moment).  weight_decay: a number, or one per tensor.  The handle keeps its tensors
+    the second moment).  What is made here is filled on the current stream; a first step on another one waits
+    for it like for any tensor.  weight_decay: a number, or one per tensor.  The handle keeps its tensors
     memory alive (one whose .data is exchanged needs a new handle); set_grads() exchanges the gradients,
     and without any (None) the handle is one for normed_stack_train, which supplies them."""
 

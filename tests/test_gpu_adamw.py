@@ -328,20 +328,23 @@ def midpoints():
     return np.concatenate([np.full((len(out), 1), 448, dtype=np.float32), out], axis=1)
 
 
+@pytest.mark.parametrize("exponent", [0, 40, -61, -66])
 @pytest.mark.parametrize("dtype,master", [(F32, False), (BF, False), (BF, True)])
-def test_codes_of_roots_between_two_codes(r3, dtype, master):
+def test_codes_of_roots_between_two_codes(r3, dtype, master, exponent):
     """Without averaging (betas 0) the second moment is the gradient's square: the stored code is that of
-    its correctly rounded root also next to the middle between two codes, and in it (ties to even)."""
-    g = midpoints()
+    its correctly rounded root also next to the middle between two codes, and in it (ties to even).  The
+    lowest exponents take the smaller squares below float32's normal range, and to zero."""
+    unit = np.float32(2.0) ** np.float32(exponent)
+    g = midpoints() * unit
     w = torch.zeros(g.size, dtype=dtype, device="cuda")
     opt = r3.AdamW([w], [torch.from_numpy(g.reshape(-1)).cuda()], state_bits=8, betas=(0.0, 0.0),
                    masters=True if master else None)
     opt.step(1, 1e-3)
     root = np.sqrt(g * g)
     assert root.dtype == np.float32
-    want = U.nearest_e4m3(root.astype(np.float64))
+    want = U.nearest_e4m3(root.astype(np.float64) / float(unit))
     want[(root > 0) & (want == 0)] = U.E4M3_MIN
-    assert (opt.exp_avg_sq_scale[0] == 1).all()
+    assert (opt.exp_avg_sq_scale[0] == float(unit)).all()
     assert np.array_equal(blocks(f64(opt.exp_avg_sq[0])), want)
 
 

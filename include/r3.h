@@ -683,6 +683,86 @@ r3_status r3_token_logprobs_bwd(const r3_logits* shape, const void* logits, cons
                                 const float* dentropy, void* dlogits, int64_t ld_out,
                                 int32_t* dev_status, void* stream);
 
+/* ---- policy loss (an extension: what stands between r3_token_logprobs and r3_token_logprobs_bwd) -- */
+
+enum { R3_RATIO_TOKEN = 0, R3_RATIO_SEQUENCE = 1 };    /* a ratio per token, or one per sequence */
+enum { R3_REDUCE_TOKEN = 0, R3_REDUCE_SEQUENCE = 1 };  /* mean over tokens, or over sequences' means */
+
+/* T packed tokens of S sequences.  advantages are [T] (adv_per_token) or [S].  0 <= clip_low <= 1,
+ * clip_high >= 0 (infinite: no border), dual_clip 0 (none) or above 1, infer_cap above 0 (infinite: none).
+ * denominator 0: counted by the call. */
+typedef struct {
+    int32_t T, S;
+    int32_t ratio, reduce, adv_per_token;
+    double clip_low, clip_high, dual_clip, infer_cap, kl_coef, entropy_coef, denominator;
+} r3_policy;
+
+/* Clipped policy loss and its gradients, in one call.  Token t of sequence i, d = logp - logp_old (with
+ * R3_RATIO_SEQUENCE the mean of that over the sequence's tokens), rho = exp(d), A the advantage:
+ *   w     = min(exp(logp_old - logp_infer), infer_cap)              1 without logp_infer
+ *   term  = -w min(rho A, min(max(rho, 1 - clip_low), 1 + clip_high) A);  with a dual clip, for A < 0, at
+ *           most -w dual_clip A
+ *   kl    = exp(x) - 1 - x,  x = logp_ref - logp                    0 without logp_ref
+ *   loss  = sum_t weight_t (term + kl_coef kl - entropy_coef entropy)
+ *   weight_t = 1 / D (R3_REDUCE_TOKEN, D = number of tokens) or 1 / (n_i D) (R3_REDUCE_SEQUENCE, n_i = the
+ *              sequence's tokens, D = sequences that have any); a denominator > 0 stands in for D (a batch
+ *              that is taken in parts, or over several ranks)
+ *   dlogp = dloss dL/dlogp,  dentropy = dloss dL/dentropy           dloss: [1] on the device, NULL = 1
+ * logp, logp_old [T]; logp_infer, logp_ref, entropy [T] or NULL; all float32.  w, logp_old and the masks are
+ * constants.  A token counts where it belongs to a sequence and mask (uint8 [T], NULL = all) is not 0: of the
+ * others only the mask is read, their gradients are 0.  cu_seqlens [S+1] int32 (device), ascending from 0 to at most T:
+ * tokens behind its last entry belong to no sequence; NULL with S = 1: one sequence of all tokens.
+ * Outputs: loss [1]; dlogp [T] or NULL; dentropy [T] (only with entropy) or NULL; metrics [3] or NULL = the
+ * weighted sums of term, kl and entropy; counts [3] int32 or NULL = tokens, tokens beyond a border (that take
+ * no policy gradient), tokens whose w is the cap.  dlogp may be logp's buffer, dentropy entropy's.
+ *  - Borders are decided on d in 64 bits; on a border a token counts as inside.  Sums run in float64, in an
+ *    order that depends on T, S and cu_seqlens alone.
+ *  - What is not finite follows the formulas and stays with its token (with R3_RATIO_SEQUENCE: its
+ *    sequence) and the loss; an advantage of 0 makes the term 0 whatever the ratio is, and a part with
+ *    coefficient 0 is only reported in metrics.
+ *  - cu_seqlens that do not ascend or leave [0, T] are reported as R3_DEV_BAD_INDEX (results undefined, nothing is accessed
+ *    out of range).  T = 0 or no counting token: the loss is 0.
+ * workspace: r3_policy_loss_workspace_bytes(config). */
+size_t r3_policy_loss_workspace_bytes(const r3_policy* config);
+r3_status r3_policy_loss(const r3_policy* config, const float* logp, const float* logp_old,
+                         const float* advantages, const int32_t* cu_seqlens, const uint8_t* mask,
+                         const float* logp_infer, const float* logp_ref, const float* entropy,
+                         const float* dloss, float* loss, float* dlogp, float* dentropy, float* metrics,
+                         int32_t* counts, void* workspace, size_t ws_bytes, int32_t* dev_status,
+                         void* stream);
+
+/* ---- balance loss of the routers (an extension; the paper trains without one) ---------------------- */
+
+typedef struct {
+    double balance_coef, z_coef;
+    int32_t accumulate;       /* 1: the gradient is added to dlogits */
+    int32_t counts_given;     /* 1: counts are read (those of a larger batch, say), not formed from idx */
+} r3_balance;
+
+/* Balance and z loss of L blocks' routers with their gradient, in one call.  Over the N tokens that count,
+ * with p_t the softmax of logits[l,t,.] over all E experts and counts[l,i] = how often the record idx[l,t,.]
+ * holds expert i:
+ *   f_i = E counts_i / sum_j counts_j
+ *   loss[l,0] = sum_i f_i (1/N) sum_t p_ti            1 where all experts are used alike
+ *   loss[l,1] = (1/N) sum_t (log sum_i exp logits[l,t,i])^2
+ *   dlogits   = balance_coef p_ti (f_i - sum_j f_j p_tj) / N + 2 z_coef (log sum exp) p_ti / N
+ * (the gradient of balance_coef loss[l,0] + z_coef loss[l,1]; the counts are constants).
+ * logits [L,T,E] f32; idx [L,T,K] idx_type (may be NULL with counts_given); mask uint8 [T] or NULL: tokens
+ * that do not count have 0 there, and only their mask is read; counts [L,E] int32, written, may be NULL (with
+ * counts_given: read); loss [L,2] f32; dlogits [L,T,E] f32 or NULL (may be the logits' buffer), every
+ * element written (tokens that do not count: 0, or left as they are with accumulate).  Only T, E, K and idx_type of
+ * the shape matter.  E <= 1024 (R3_ERR_UNSUPPORTED beyond).  Sums run in an order that depends on the shape
+ * alone.  dev_status: R3_DEV_BAD_INDEX for an index >= E (not counted).
+ *  - A logit of -inf has p = 0; a token with no other logit counts in N and adds nothing.  A token with NaN or
+ *    +inf makes its own gradient and its block's losses NaN.
+ *  - No token that counts: losses 0.
+ * workspace: r3_balance_loss_workspace_bytes(shape, L). */
+size_t r3_balance_loss_workspace_bytes(const r3_shape* shape, int32_t L);
+r3_status r3_balance_loss(const r3_shape* shape, int32_t L, const r3_balance* config,
+                          const float* logits, const void* idx, const uint8_t* mask, int32_t* counts,
+                          float* loss, float* dlogits, void* workspace, size_t ws_bytes,
+                          int32_t* dev_status, void* stream);
+
 /* ---- training/inference discrepancy measures (Sections 3.1 and 3.2) -------------------------- */
 
 /* Eq. (kl), the k3 estimate of KL(pi_train || pi_infer), and Eq. (etdf), the Extreme Token

@@ -1,0 +1,454 @@
+// Balance loss and z loss of the routers of L blocks, the counts per expert, and the gradient to the
+// router logits.  Per block, over N tokens, with p the softmax of a token's logits over ALL experts and
+// counts the choices of the record,
+//   f_i = E counts_i / sum_j counts_j      balance = sum_i f_i mean_t p_ti
+//   z   = mean_t (log sum_i exp s_ti)^2
+//   ds_ti = balance_coef p_ti (f_i - sum_j f_j p_tj) / N  +  2 z_coef lse_t p_ti / N
+// The counts do not depend on the logits, so they come first, from the record alone (K bytes a token),
+// and the logits are then read once: the pass that forms the probabilities has f and N in hand and
+// writes the gradient at once.  Bound by HBM: 8 E + K bytes a token and block.
+//
+// A token's logits lie across G lanes (a power of two, 4 or more logits each), so that its maximum, its
+// sum and its product with f are shuffles; a lane keeps the f of its experts and the sums of their
+// probabilities in registers over all its tokens.  CTAs take equal shares of a block's tokens; the last CTA
+// of a block to arrive adds up their probability sums, in an order that depends on the shape alone.
+#include <cmath>
+
+#include "r3_common.cuh"
+#include "r3_internal.h"
+#include "r3_tc.cuh"
+
+namespace r3 {
+namespace bal {
+
+constexpr int THREADS = 256;
+constexpr int WARPS = THREADS / 32;
+constexpr int MAX_EXPERTS = 1024;
+constexpr int COUNT_TOKENS = 2048;        // tokens of a CTA of the counting pass, at least
+constexpr int COUNT_PARTS = 32;           // and so many CTAs per block at most
+
+struct Args {
+    int T, E, K, L;
+    int count_parts, count_tokens;        // CTAs and tokens per CTA of the counting pass
+    int parts, part_tokens;               // CTAs and tokens per CTA of the main pass
+    int accumulate, given;
+    float balance_coef, z_coef;
+    const float* logits;
+    const void* idx;
+    const uint8_t* mask;
+    int32_t* counts;                      // given, or written (may be null)
+    float* loss;                          // [L, 2]
+    float* dlogits;                       // or null
+    int32_t* part_counts;                 // [L, count_parts, E + 1]: per expert, then the tokens
+    float* part_probs;                    // [L, parts, E]
+    double* part_z;                       // [L, parts]
+    unsigned* ticket;                     // [L]
+    int32_t* dev_status;
+};
+
+// ---- counting pass: grid (count_parts, L) -----------------------------------------------------
+template <typename IdxT>
+__global__ void __launch_bounds__(THREADS) count_kernel(const __grid_constant__ Args a) {
+    extern __shared__ int s_count[];
+    const int l = blockIdx.y, E = a.E, K = a.K;
+    for (int e = threadIdx.x; e <= E; e += THREADS) s_count[e] = 0;
+    tc::grid_launch_dependents();
+    __syncthreads();
+    tc::grid_dependency_wait();
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.ticket[l] = 0;
+    const int t0 = blockIdx.x * a.count_tokens, t1 = min(a.T, t0 + a.count_tokens);
+    if (a.mask) {
+        int n = 0;
+        for (int t = t0 + threadIdx.x; t < t1; t += THREADS) n += a.mask[t] != 0;
+        n = __reduce_add_sync(0xffffffffu, n);
+        if ((threadIdx.x & 31) == 0 && n) atomicAdd(&s_count[E], n);
+    } else if (threadIdx.x == 0) {
+        s_count[E] = max(t1 - t0, 0);
+    }
+    if (!a.given) {
+        const IdxT* idx = static_cast<const IdxT*>(a.idx) + ((size_t)l * a.T + t0) * K;
+        const int n = max(t1 - t0, 0) * K;
+        auto take = [&](int i, int e) {
+            if (a.mask && !a.mask[t0 + i / K]) return;
+            if (e < 0 || e >= E) {
+                report(a.dev_status, R3_DEV_BAD_INDEX);
+                return;
+            }
+            atomicAdd(&s_count[e], 1);
+        };
+        constexpr int VEC = 16 / (int)sizeof(IdxT);
+        // the record's base is aligned to 16 bytes, a CTA's first choice need not be
+        const int skip = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(idx) & 15)) & 15) / (int)sizeof(IdxT));
+        const int vecs = (n - skip) / VEC;
+        for (int i = threadIdx.x; i < skip; i += THREADS) take(i, idx_to_int(idx[i]));
+        for (int v = threadIdx.x; v < vecs; v += THREADS) {
+            const int4 w = *reinterpret_cast<const int4*>(idx + skip + v * VEC);
+            const IdxT* x = reinterpret_cast<const IdxT*>(&w);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) take(skip + v * VEC + j, idx_to_int(x[j]));
+        }
+        for (int i = skip + vecs * VEC + threadIdx.x; i < n; i += THREADS) take(i, idx_to_int(idx[i]));
+    }
+    __syncthreads();
+    int32_t* out = a.part_counts + ((size_t)l * a.count_parts + blockIdx.x) * (E + 1);
+    for (int e = threadIdx.x; e <= E; e += THREADS) out[e] = s_count[e];
+}
+
+// ---- main pass: grid (parts, L) ---------------------------------------------------------------
+// G lanes per token, V logits per lane.  WIDE: E is a multiple of 4, a lane's logits come in fours
+// (columns 4 (lane + G q) ..); otherwise one by one (columns lane + G q).
+template <int G, int V, bool WIDE> struct Row {
+    static __device__ __forceinline__ int column(int sub, int j) {
+        return WIDE ? 4 * (sub + G * (j / 4)) + j % 4 : sub + G * j;
+    }
+    static __device__ __forceinline__ void load(const float* p, int E, int sub, float (&v)[V], float none) {
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int q = 0; q < V / 4; ++q) {
+                const int c = 4 * (sub + G * q);
+                const float4 f = c < E ? *reinterpret_cast<const float4*>(p + c)
+                                       : make_float4(none, none, none, none);
+                v[4 * q] = f.x;
+                v[4 * q + 1] = f.y;
+                v[4 * q + 2] = f.z;
+                v[4 * q + 3] = f.w;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = sub + G * j < E ? p[sub + G * j] : none;
+        }
+    }
+    static __device__ __forceinline__ void store(float* p, int E, int sub, const float (&v)[V]) {
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int q = 0; q < V / 4; ++q) {
+                const int c = 4 * (sub + G * q);
+                if (c < E) *reinterpret_cast<float4*>(p + c) =
+                    make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (sub + G * j < E) p[sub + G * j] = v[j];
+        }
+    }
+};
+
+template <int G, int V, bool WIDE>
+__global__ void __launch_bounds__(THREADS, V <= 8 ? 4 : 2) balance_kernel(const __grid_constant__ Args a) {
+    using R = Row<G, V, WIDE>;
+    constexpr int ROWS = 32 / G;                       // tokens of a warp at a time
+    constexpr int AT_ONCE = V <= 8 ? 2 : 1;            // of those, in flight
+    extern __shared__ float s_col[];                   // f, later the CTA's sums of probabilities
+    __shared__ long long s_sum[WARPS];
+    __shared__ double s_z[WARPS];
+    __shared__ int s_tokens;
+    __shared__ bool s_last;
+    const int l = blockIdx.y, E = a.E, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int sub = lane % G, row = lane / G;
+    tc::grid_launch_dependents();
+    tc::grid_dependency_wait();
+    // the block's counts, the number of its choices and of its tokens
+    long long mine = 0;
+    for (int e = threadIdx.x; e <= E; e += THREADS) {
+        int n = 0;
+        if (e < E && a.given) {
+            n = a.counts[(size_t)l * E + e];
+        } else {
+            const int32_t* p = a.part_counts + (size_t)l * a.count_parts * (E + 1) + e;
+#pragma unroll 8
+            for (int q = 0; q < a.count_parts; ++q) n += p[(size_t)q * (E + 1)];
+        }
+        if (e == E) {
+            s_tokens = n;
+        } else {
+            s_col[e] = (float)n;                       // below 2^24, or off by a rounding
+            mine += n;
+            if (!a.given && a.counts && blockIdx.x == 0) a.counts[(size_t)l * E + e] = n;
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    if (lane == 0) s_sum[warp] = mine;
+    __syncthreads();
+    long long choices = 0;
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) choices += s_sum[i];
+    const int tokens = s_tokens;
+    const float per_choice = choices > 0 ? (float)((double)E / (double)choices) : 0.f;
+    const float per_token = tokens > 0 ? 1.f / (float)tokens : 0.f;
+    float f[V], sum[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int c = R::column(sub, j);
+        f[j] = c < E ? s_col[c] * per_choice : 0.f;
+        sum[j] = 0.f;
+    }
+    __syncthreads();                                   // s_col is used again below
+    const float gb = a.balance_coef * per_token, gz = 2.f * a.z_coef * per_token;
+    const int t0 = blockIdx.x * a.part_tokens, t1 = min(a.T, t0 + a.part_tokens);
+    const float* logits = a.logits + (size_t)l * a.T * E;
+    float* dlogits = a.dlogits ? a.dlogits + (size_t)l * a.T * E : nullptr;
+    double z = 0.0;
+    for (int t = t0 + warp * ROWS * AT_ONCE; t < t1; t += WARPS * ROWS * AT_ONCE) {
+        float v[AT_ONCE][V];
+        bool on[AT_ONCE];
+#pragma unroll
+        for (int r = 0; r < AT_ONCE; ++r) {
+            const int at = t + r * ROWS + row;
+            on[r] = at < t1 && (!a.mask || a.mask[at]);
+            if (on[r]) {
+                R::load(logits + (size_t)at * E, E, sub, v[r], -INFINITY);
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[r][j] = -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < AT_ONCE; ++r) {
+            const int at = t + r * ROWS + row;
+            float top = v[r][0];
+#pragma unroll
+            for (int j = 1; j < V; ++j) top = fmaxf(top, v[r][j]);
+#pragma unroll
+            for (int o = G / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const float from = top == -INFINITY ? 0.f : top;       // a token without any expert: all 0
+            float whole = 0.f, along = 0.f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                v[r][j] = expf(v[r][j] - from);
+                whole += v[r][j];
+                along += v[r][j] * f[j];
+            }
+#pragma unroll
+            for (int o = G / 2; o > 0; o >>= 1) {
+                whole += __shfl_xor_sync(0xffffffffu, whole, o);
+                along += __shfl_xor_sync(0xffffffffu, along, o);
+            }
+            const float inv = whole != 0.f ? 1.f / whole : 0.f;
+            const float lse = whole != 0.f ? from + logf(whole) : 0.f;
+            along *= inv;
+            if (sub == 0) z += (double)lse * (double)lse;          // 0 where the token does not count
+            const float shift = gz * lse - gb * along;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float p = v[r][j] * inv;
+                sum[j] += p;
+                v[r][j] = p * (gb * f[j] + shift);
+            }
+            if (dlogits && at < t1) {
+                float* out = dlogits + (size_t)at * E;
+                if (a.accumulate) {
+                    float old[V];
+                    R::load(out, E, sub, old, 0.f);
+                    if (on[r]) {
+#pragma unroll
+                        for (int j = 0; j < V; ++j) old[j] += v[r][j];
+                        R::store(out, E, sub, old);
+                    }
+                } else {
+                    R::store(out, E, sub, v[r]);
+                }
+            }
+        }
+    }
+    // the CTA's sums: lanes that hold the same experts, then the warps in their order
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int o = G; o < 32; o <<= 1) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], o);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+    if (lane == 0) s_z[warp] = z;
+    for (int w = 0; w < WARPS; ++w) {
+        if (warp == w && row == 0) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int c = R::column(sub, j);
+                if (c < E) s_col[c] = (w ? s_col[c] : 0.f) + sum[j];
+            }
+        }
+        __syncthreads();
+    }
+    float* probs = a.part_probs + ((size_t)l * a.parts + blockIdx.x) * E;
+    for (int c = threadIdx.x; c < E; c += THREADS) probs[c] = s_col[c];
+    if (threadIdx.x == 0) {
+        double all = 0.0;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) all += s_z[w];
+        a.part_z[(size_t)l * a.parts + blockIdx.x] = all;
+    }
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) s_last = atomicAdd(a.ticket + l, 1u) == gridDim.x - 1;
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+    double balance = 0.0;
+    for (int c = threadIdx.x; c < E; c += THREADS) {
+        const volatile float* p = a.part_probs + (size_t)l * a.parts * E + c;
+        double s = 0.0;
+#pragma unroll 8
+        for (int q = 0; q < a.parts; ++q) s += (double)p[(size_t)q * E];
+        int n = 0;
+        if (a.given) {
+            n = a.counts[(size_t)l * E + c];
+        } else {
+            const int32_t* k = a.part_counts + (size_t)l * a.count_parts * (E + 1) + c;
+            for (int q = 0; q < a.count_parts; ++q) n += k[(size_t)q * (E + 1)];
+        }
+        balance += s * (double)n;
+    }
+    double zz = 0.0;
+    for (int q = threadIdx.x; q < a.parts; q += THREADS)
+        zz += *(const volatile double*)(a.part_z + (size_t)l * a.parts + q);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        balance += __shfl_xor_sync(0xffffffffu, balance, o);
+        zz += __shfl_xor_sync(0xffffffffu, zz, o);
+    }
+    __shared__ double s_b[WARPS];
+    if (lane == 0) {
+        s_b[warp] = balance;
+        s_z[warp] = zz;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        balance = zz = 0.0;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            balance += s_b[w];
+            zz += s_z[w];
+        }
+        const double n = tokens > 0 ? (double)tokens : 1.0;
+        a.loss[2 * l] = choices > 0 ? (float)(balance * (double)E / ((double)choices * n)) : 0.f;
+        a.loss[2 * l + 1] = (float)(zz / n);
+    }
+}
+
+struct Plan {
+    int count_parts, count_tokens, parts, part_tokens;
+};
+// CTAs per block: four resident ones per SM over all blocks, unless a CTA's share falls below 64 tokens
+// (its start, which adds up the counting pass's parts, is then no longer small beside it).
+static Plan plan(int T, int L) {
+    Plan p;
+    auto split = [&](int most, int least_tokens, int* parts, int* tokens) {
+        long long n = (T + least_tokens - 1) / least_tokens;
+        if (n > most) n = most;
+        if (n < 1) n = 1;
+        *tokens = (int)((T + n - 1) / n);
+        if (*tokens < 1) *tokens = 1;
+        *parts = T > 0 ? (T + *tokens - 1) / *tokens : 1;
+    };
+    split(COUNT_PARTS, COUNT_TOKENS, &p.count_parts, &p.count_tokens);
+    const int share = (4 * sm_count() + L - 1) / L;
+    split(share < 1 ? 1 : share, 64, &p.parts, &p.part_tokens);
+    return p;
+}
+
+static r3_status check(const r3_shape* s, int32_t L, const r3_balance* c) {
+    if (!s || !c || L < 0 || L > 65535) return R3_ERR_INVALID_ARG;
+    const r3_status st = check_shape(s);
+    if (st != R3_OK) return st;
+    if (!(std::fabs(c->balance_coef) < 1e30) || !(std::fabs(c->z_coef) < 1e30)) return R3_ERR_INVALID_ARG;
+    return s->E > MAX_EXPERTS ? R3_ERR_UNSUPPORTED : R3_OK;
+}
+struct Layout {
+    size_t counts, probs, z, ticket, total;
+};
+static Layout layout(const r3_shape* s, int32_t L, const Plan& p) {
+    Layout w;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += round_up(bytes, 256);
+        return here;
+    };
+    w.counts = take((size_t)L * p.count_parts * (s->E + 1) * 4);
+    w.probs = take((size_t)L * p.parts * s->E * 4);
+    w.z = take((size_t)L * p.parts * 8);
+    w.ticket = take((size_t)L * 4);
+    w.total = at;
+    return w;
+}
+
+template <int G, int V, bool WIDE>
+static r3_status launch(const Args& a, cudaStream_t cs) {
+    return tc::launch_dependent(balance_kernel<G, V, WIDE>, dim3(a.parts, a.L), dim3(THREADS),
+                                (size_t)a.E * sizeof(float), cs, a) == cudaSuccess ? R3_OK : R3_ERR_CUDA;
+}
+template <bool WIDE>
+static r3_status launch(const Args& a, cudaStream_t cs) {
+    if (a.E <= 16) return launch<4, 4, WIDE>(a, cs);
+    if (a.E <= 64) return launch<16, 4, WIDE>(a, cs);
+    if (a.E <= 128) return launch<32, 4, WIDE>(a, cs);
+    if (a.E <= 256) return launch<32, 8, WIDE>(a, cs);
+    if (a.E <= 512) return launch<32, 16, WIDE>(a, cs);
+    return launch<32, 32, WIDE>(a, cs);
+}
+
+}  // namespace bal
+}  // namespace r3
+
+extern "C" size_t r3_balance_loss_workspace_bytes(const r3_shape* s, int32_t L) {
+    using namespace r3::bal;
+    const r3_balance none = {};
+    if (check(s, L, &none) != R3_OK || L == 0) return 0;
+    return layout(s, L, plan(s->T, L)).total;
+}
+
+extern "C" r3_status r3_balance_loss(const r3_shape* s, int32_t L, const r3_balance* config,
+                                     const float* logits, const void* idx, const uint8_t* mask,
+                                     int32_t* counts, float* loss, float* dlogits, void* workspace,
+                                     size_t ws_bytes, int32_t* dev_status, void* stream) {
+    using namespace r3;
+    using namespace r3::bal;
+    const r3_status st = check(s, L, config);
+    if (st != R3_OK) return st;
+    if (L == 0) return R3_OK;
+    const bool given = config->counts_given != 0;
+    if (!loss || (s->T > 0 && (!logits || (!given && !idx))) || (given && !counts)) return R3_ERR_INVALID_ARG;
+    if (config->accumulate && !dlogits) return R3_ERR_INVALID_ARG;
+    const void* wide[] = {logits, idx, dlogits};
+    for (const void* p : wide)
+        if (!aligned(p, 16)) return R3_ERR_INVALID_ARG;
+    const void* words[] = {counts, loss, dev_status};
+    for (const void* p : words)
+        if (!aligned(p, 4)) return R3_ERR_INVALID_ARG;
+    const Plan p = plan(s->T, L);
+    const Layout w = layout(s, L, p);
+    if (!workspace || !aligned(workspace, 256) || ws_bytes < w.total) return R3_ERR_WORKSPACE;
+    Args a = {};
+    a.T = s->T;
+    a.E = s->E;
+    a.K = s->K;
+    a.L = L;
+    a.count_parts = p.count_parts;
+    a.count_tokens = p.count_tokens;
+    a.parts = p.parts;
+    a.part_tokens = p.part_tokens;
+    a.accumulate = config->accumulate != 0;
+    a.given = given;
+    a.balance_coef = (float)config->balance_coef;
+    a.z_coef = (float)config->z_coef;
+    a.logits = logits;
+    a.idx = idx;
+    a.mask = mask;
+    a.counts = counts;
+    a.loss = loss;
+    a.dlogits = dlogits;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    a.part_counts = reinterpret_cast<int32_t*>(ws + w.counts);
+    a.part_probs = reinterpret_cast<float*>(ws + w.probs);
+    a.part_z = reinterpret_cast<double*>(ws + w.z);
+    a.ticket = reinterpret_cast<unsigned*>(ws + w.ticket);
+    a.dev_status = dev_status;
+    cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    const size_t smem = (size_t)(s->E + 1) * sizeof(int);
+    cudaError_t err = cudaSuccess;
+    R3_DISPATCH_IDX(s, IdxT, err = tc::launch_dependent(count_kernel<IdxT>, dim3(p.count_parts, L),
+                                                        dim3(THREADS), smem, cs, a));
+    if (err != cudaSuccess) return R3_ERR_CUDA;
+    return s->E % 4 == 0 ? launch<true>(a, cs) : launch<false>(a, cs);
+}

@@ -1,0 +1,546 @@
+// Clipped policy loss over packed responses, with its gradient to the log probabilities and the
+// entropies: what stands between the log probabilities of given tokens and their gradient.  Per
+// response token t of sequence i, all from log probabilities,
+//   d     = logp - logp_old               (ratio of sequences: its mean over the sequence's tokens)
+//   rho   = exp(d)       w = min(exp(logp_old - logp_infer), cap)
+//   term  = -w min(rho A, clip(rho) A)    and at most w c |A| for A < 0 with a dual clip c
+//   kl    = exp(x) - 1 - x,  x = logp_ref - logp
+//   loss  = sum_t weight_t (term + kl_coef kl - entropy_coef entropy)
+// with weight 1 / N (tokens) or 1 / (n_i S') (sequences).  Whether a ratio lies beyond a border is asked
+// of its logarithm, in 64 bits (the difference of two float32 numbers is exact there), so the choice does
+// not depend on how an exponential rounds; exponentials and the terms are float32, all sums 64 bits.
+//
+// Two passes, since a token's gradient needs its sequence's sums and the number of tokens: the first
+// leaves the sums of every unit (up to 256 consecutive tokens of ONE sequence, a warp each), the second
+// adds up a sequence's units in their order and writes the gradients; its last CTA adds up the CTAs'
+// parts of the loss.  A sequence that starts at token c takes its units from number i + floor(c / 256)
+// on: that leaves each one room for all of its units whatever the lengths are, and a warp finds its
+// sequence by a search in cu_seqlens, 32 probes at a time, with no table built before.  Batches of up to
+// 32 units run as one CTA.
+// Bound by HBM where the batch is large, by two launches where it is not.
+#include <cmath>
+
+#include "r3_common.cuh"
+#include "r3_internal.h"
+#include "r3_tc.cuh"
+
+namespace r3 {
+namespace pol {
+
+constexpr int UNIT = 256;                 // tokens of a unit
+constexpr int PER_LANE = UNIT / 32;
+constexpr int WARPS = 8;                  // units of a CTA
+constexpr int ONE_WARPS = 32;             // units of a batch that takes one CTA
+
+struct Sums {                             // of one unit; of a sequence: the sum of its units'
+    double d, up, down;                   // sum of d; of w A over the tokens with A > 0 and A < 0
+};
+struct Total {
+    double policy, kl, entropy;
+    int tokens, clipped, cut, pad;
+};
+struct Args {
+    int T, S, units;
+    int by_sequence, mean_of_sequences, adv_per_token, need_sums;
+    double log_high, log_low, log_dual, log_cap;       // borders of d and of logp_old - logp_infer
+    float high, low, dual, cap;                        // the values beyond them
+    double kl_coef, entropy_coef, denominator;         // denominator 0: counted
+    const float *logp, *old, *adv, *infer, *ref, *entropy, *dloss;
+    const int32_t* cu;                                 // or null: one sequence
+    const uint8_t* mask;
+    float *loss, *dlogp, *dentropy, *metrics;
+    int32_t* counts;
+    Sums* sums;                                        // [units]
+    int* n;                                            // [units]
+    Total* totals;                                     // [CTAs]
+    unsigned* ticket;
+    int32_t* dev_status;
+};
+
+__device__ __forceinline__ int bound(const Args& a, int i) {       // where sequence i starts
+    if (!a.cu) return i == 0 ? 0 : a.T;
+    return min(max(a.cu[i], 0), a.T);
+}
+__device__ __forceinline__ int first_unit(const Args& a, int i) { return i + bound(a, i) / UNIT; }
+
+struct Unit {
+    int seq, begin, end;                  // seq = S: behind the last sequence
+    int first, count;                     // units of the sequence
+};
+// The whole warp; the last sequence whose first unit is not behind `unit`.
+__device__ __forceinline__ Unit find_unit(const Args& a, int unit) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, len = a.S + 1;            // first_unit(lo) <= unit always holds: unit 0 is sequence 0's
+    while (len > 1) {
+        const int step = (len + 31) / 32, at = lo + lane * step;
+        const bool in = lane * step < len && first_unit(a, at) <= unit;
+        const int k = max(__popc(__ballot_sync(0xffffffffu, in)) - 1, 0);
+        lo += k * step;
+        len = min(step, len - k * step);
+    }
+    Unit u;
+    u.seq = lo;
+    const int begin = bound(a, lo), end = lo < a.S ? max(bound(a, lo + 1), begin) : a.T;
+    u.first = lo + begin / UNIT;
+    u.count = (end - begin + UNIT - 1) / UNIT;
+    const long long at = begin + (long long)(unit - u.first) * UNIT;
+    u.begin = (int)min(at, (long long)end);
+    u.end = min(u.begin + UNIT, end);
+    return u;
+}
+__device__ __forceinline__ double warp_sum(double v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ int warp_sum(int v) { return __reduce_add_sync(0xffffffffu, v); }
+
+// min(exp(old - infer), cap)
+__device__ __forceinline__ float infer_weight(const Args& a, float old, float infer, bool* cut) {
+    const double x = (double)old - (double)infer;
+    *cut = x > a.log_cap;
+    return *cut ? a.cap : expf((float)x);
+}
+
+// ---- first pass: the sums of a unit ----------------------------------------------------------
+__device__ __forceinline__ void unit_sums(const Args& a, const Unit& u, Sums* s, int* n) {
+    const int lane = threadIdx.x & 31;
+    const bool live = u.seq < a.S;
+    double d = 0.0, up = 0.0, down = 0.0;
+    int k = 0;
+    if (live && !a.by_sequence && !a.mask) {
+        if (lane == 0) k = u.end - u.begin;
+    } else if (live) {
+        const float seq_adv = a.by_sequence && !a.adv_per_token && u.begin < u.end ? a.adv[u.seq] : 0.f;
+        float lp[PER_LANE], old[PER_LANE], inf[PER_LANE], adv[PER_LANE];
+        bool on[PER_LANE];
+#pragma unroll
+        for (int j = 0; j < PER_LANE; ++j) {
+            const int t = u.begin + j * 32 + lane;
+            on[j] = t < u.end && (!a.mask || a.mask[t]);
+            k += on[j];
+        }
+        if (a.by_sequence) {
+#pragma unroll
+            for (int j = 0; j < PER_LANE; ++j) {
+                const int t = u.begin + j * 32 + lane;
+                lp[j] = on[j] ? a.logp[t] : 0.f;
+                old[j] = on[j] ? a.old[t] : 0.f;
+                inf[j] = on[j] && a.infer ? a.infer[t] : 0.f;
+                adv[j] = on[j] ? (a.adv_per_token ? a.adv[t] : seq_adv) : 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < PER_LANE; ++j) {
+                if (!on[j]) continue;
+                d += (double)lp[j] - (double)old[j];
+                bool cut;
+                const float w = a.infer ? infer_weight(a, old[j], inf[j], &cut) : 1.f;
+                const double wa = (double)(w * adv[j]);
+                if (adv[j] > 0.f) up += wa;
+                else if (adv[j] != 0.f) down += wa;    // NaN counts here: it has to reach the loss
+            }
+        }
+    }
+    k = warp_sum(k);
+    if (a.by_sequence) {
+        d = warp_sum(d);
+        up = warp_sum(up);
+        down = warp_sum(down);
+    }
+    if (lane == 0) {
+        *n = k;
+        if (a.by_sequence) *s = {d, up, down};
+    }
+}
+
+// A sequence's sums, from its units in a fixed order, by a whole warp.
+__device__ __forceinline__ void sequence_sums(const Args& a, const Sums* sums, const int* n, int first,
+                                              int count, Sums* s, int* tokens) {
+    const int lane = threadIdx.x & 31;
+    double d = 0.0, up = 0.0, down = 0.0;
+    int k = 0;
+#pragma unroll 4
+    for (int i = lane; i < count; i += 32) {
+        k += n[first + i];
+        if (a.by_sequence) {
+            const Sums v = sums[first + i];
+            d += v.d;
+            up += v.up;
+            down += v.down;
+        }
+    }
+    *tokens = warp_sum(k);
+    if (a.by_sequence) *s = {warp_sum(d), warp_sum(up), warp_sum(down)};
+}
+
+// exp(x) - 1 - x without cancellation: its series up to |x| = 1 (the first term left out, 2 / 13! of
+// the result, is below a rounding).
+__device__ __forceinline__ float exp_less_line(float x, float em1) {
+    if (!(fabsf(x) <= 1.f)) return em1 - x;
+    float p = 1.f + x * (1.f / 12.f);
+#pragma unroll
+    for (int k = 11; k >= 3; --k) p = 1.f + x * p * (1.f / (float)k);
+    return 0.5f * x * x * p;
+}
+
+// ---- second pass: one unit's part of the loss, and its gradients ------------------------------
+__device__ __forceinline__ Total unit_loss(const Args& a, const Unit& u, const Sums& s, int n_seq,
+                                           double divisor) {
+    const int lane = threadIdx.x & 31;
+    Total r = {};
+    const bool live = u.seq < a.S;
+    double weight = 0.0;
+    if (live) weight = 1.0 / (a.mean_of_sequences ? divisor * (double)max(n_seq, 1) : divisor);
+    const float up_to = a.dloss ? a.dloss[0] : 1.f;            // gradient of the loss itself
+    const float gw = (float)(weight * (double)up_to);
+    const float kl_w = (float)(a.kl_coef * weight * (double)up_to);
+    const float ent_g = (float)(-a.entropy_coef * weight * (double)up_to);
+    const float seq_adv = live && !a.adv_per_token && u.begin < u.end ? a.adv[u.seq] : 0.f;
+    double seq_d = 0.0;
+    float seq_slope = 0.f;
+    if (a.by_sequence && live) {
+        seq_d = s.d / (double)max(n_seq, 1);
+        const double rho = (double)expf((float)seq_d);
+        const bool high = seq_d > a.log_high, low = seq_d < a.log_low || seq_d > a.log_dual;
+        // a part that is 0 takes no ratio, be it infinite
+        const double part = (high ? 0.0 : s.up) + (low ? 0.0 : s.down);
+        seq_slope = part == 0.0 ? 0.f
+                                : (float)(-part * rho * weight * (double)up_to / (double)max(n_seq, 1));
+    }
+    float lp[PER_LANE], old[PER_LANE], inf[PER_LANE], ref[PER_LANE], ent[PER_LANE], adv[PER_LANE];
+    bool on[PER_LANE];
+#pragma unroll
+    for (int j = 0; j < PER_LANE; ++j) {
+        const int t = u.begin + j * 32 + lane;
+        on[j] = live && t < u.end && (!a.mask || a.mask[t]);
+    }
+    const bool want_logp = !a.by_sequence || a.ref;
+#pragma unroll
+    for (int j = 0; j < PER_LANE; ++j) {
+        const int t = u.begin + j * 32 + lane;
+        lp[j] = on[j] && want_logp ? a.logp[t] : 0.f;
+        old[j] = on[j] && (!a.by_sequence || a.infer) ? a.old[t] : 0.f;
+        inf[j] = on[j] && a.infer ? a.infer[t] : 0.f;
+        ref[j] = on[j] && a.ref ? a.ref[t] : 0.f;
+        ent[j] = on[j] && a.entropy ? a.entropy[t] : 0.f;
+        adv[j] = on[j] ? (a.adv_per_token ? a.adv[t] : seq_adv) : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < PER_LANE; ++j) {
+        const int t = u.begin + j * 32 + lane;
+        if (t >= u.end) continue;
+        float g = 0.f, ge = 0.f;
+        if (on[j]) {
+            const double d = a.by_sequence ? seq_d : (double)lp[j] - (double)old[j];
+            bool cut = false;
+            const float w = a.infer ? infer_weight(a, old[j], inf[j], &cut) : 1.f;
+            const float wa = w * adv[j];
+            const bool high = adv[j] > 0.f && d > a.log_high;
+            const bool low = adv[j] < 0.f && d < a.log_low;
+            const bool far = adv[j] < 0.f && d > a.log_dual;
+            const float rho = high ? a.high : low ? a.low : far ? a.dual : expf((float)d);
+            const float term = adv[j] == 0.f ? 0.f : -(wa * rho);
+            const bool beyond = high || low || far;
+            r.tokens += 1;
+            r.clipped += beyond;
+            r.cut += cut;
+            r.policy += (double)term;
+            g = a.by_sequence ? seq_slope : beyond ? 0.f : term * gw;
+            if (a.ref) {
+                const float x = (float)((double)ref[j] - (double)lp[j]);
+                const float em1 = expm1f(x);
+                r.kl += (double)exp_less_line(x, em1);
+                if (a.kl_coef != 0.0) g -= kl_w * em1;
+            }
+            if (a.entropy) {
+                r.entropy += (double)ent[j];
+                ge = ent_g;
+            }
+        }
+        if (a.dlogp) a.dlogp[t] = g;
+        if (a.dentropy) a.dentropy[t] = ge;
+    }
+    r.policy = warp_sum(r.policy) * weight;
+    r.kl = a.ref ? warp_sum(r.kl) * weight : 0.0;
+    r.entropy = a.entropy ? warp_sum(r.entropy) * weight : 0.0;
+    r.tokens = warp_sum(r.tokens);
+    r.clipped = warp_sum(r.clipped);
+    r.cut = warp_sum(r.cut);
+    return r;
+}
+
+__device__ __forceinline__ void add(Total& x, const Total& y) {
+    x.policy += y.policy;
+    x.kl += y.kl;
+    x.entropy += y.entropy;
+    x.tokens += y.tokens;
+    x.clipped += y.clipped;
+    x.cut += y.cut;
+}
+__device__ __forceinline__ void write_loss(const Args& a, const Total& r) {
+    a.loss[0] = (float)(r.policy + (a.kl_coef != 0.0 ? a.kl_coef * r.kl : 0.0) -
+                        (a.entropy_coef != 0.0 ? a.entropy_coef * r.entropy : 0.0));
+    if (a.metrics) {
+        a.metrics[0] = (float)r.policy;
+        a.metrics[1] = (float)r.kl;
+        a.metrics[2] = (float)r.entropy;
+    }
+    if (a.counts) {
+        a.counts[0] = r.tokens;
+        a.counts[1] = r.clipped;
+        a.counts[2] = r.cut;
+    }
+}
+
+// The number that the weights are divided by, for the whole CTA: response tokens, or sequences that hold
+// one.  `n`: all units' token counts.
+template <int W>
+__device__ __forceinline__ double count_divisor(const Args& a, const int* n, int* s_warp) {
+    if (a.denominator > 0.0) return a.denominator;
+    int k = 0;
+    if (!a.mean_of_sequences) {
+        for (int i = threadIdx.x; i < a.units; i += 32 * W) k += n[i];
+    } else {
+        for (int i = threadIdx.x; i < a.S; i += 32 * W) {
+            const int begin = bound(a, i), end = max(bound(a, i + 1), begin);
+            const int first = i + begin / UNIT, units = (end - begin + UNIT - 1) / UNIT;
+            bool any = false;
+            for (int q = 0; q < units && !any; ++q) any = n[first + q] > 0;
+            k += any;
+        }
+    }
+    k = warp_sum(k);
+    if ((threadIdx.x & 31) == 0) s_warp[threadIdx.x >> 5] = k;
+    __syncthreads();
+    k = 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) k += s_warp[i];
+    return (double)max(k, 1);
+}
+
+// cu_seqlens has to ascend from 0 to at most T.
+__device__ __forceinline__ void check_bounds(const Args& a, int thread, int threads) {
+    if (!a.cu) return;
+    for (int i = thread; i <= a.S; i += threads) {
+        const int c = a.cu[i];
+        if (c < 0 || c > a.T || (i == 0 && c != 0) || (i > 0 && c < a.cu[i - 1]))
+            report(a.dev_status, R3_DEV_BAD_INDEX);
+    }
+}
+
+__global__ void __launch_bounds__(WARPS * 32) sums_kernel(const __grid_constant__ Args a) {
+    tc::grid_launch_dependents();
+    tc::grid_dependency_wait();
+    const int unit = blockIdx.x * WARPS + (threadIdx.x >> 5);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
+    check_bounds(a, blockIdx.x * WARPS * 32 + threadIdx.x, gridDim.x * WARPS * 32);
+    if (!a.need_sums || unit >= a.units) return;
+    const Unit u = find_unit(a, unit);
+    unit_sums(a, u, a.sums + unit, a.n + unit);
+}
+
+__global__ void __launch_bounds__(WARPS * 32) loss_kernel(const __grid_constant__ Args a) {
+    __shared__ int s_count[WARPS];
+    __shared__ int s_seq[WARPS];
+    __shared__ Total s_total[WARPS];
+    __shared__ Sums s_sums;
+    __shared__ int s_tokens;
+    __shared__ bool s_last;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int unit = blockIdx.x * WARPS + warp;
+    tc::grid_launch_dependents();
+    tc::grid_dependency_wait();
+    Unit u = {a.S, 0, 0, 0, 0};
+    if (unit < a.units) u = find_unit(a, unit);
+    if (lane == 0) s_seq[warp] = unit < a.units ? u.seq : -1;
+    const double divisor = count_divisor<WARPS>(a, a.n, s_count);
+    Sums s = {};
+    int n_seq = 1;
+    if (a.by_sequence || a.mean_of_sequences) {
+        __syncthreads();
+        if (s_seq[0] == s_seq[WARPS - 1]) {            // one long sequence: added up once
+            if (warp == 0) {
+                sequence_sums(a, a.sums, a.n, u.first, u.count, &s, &n_seq);
+                if (lane == 0) {
+                    s_sums = s;
+                    s_tokens = n_seq;
+                }
+            }
+            __syncthreads();
+            s = s_sums;
+            n_seq = s_tokens;
+        } else if (u.begin < u.end) {
+            sequence_sums(a, a.sums, a.n, u.first, u.count, &s, &n_seq);
+        }
+    }
+    const Total r = unit_loss(a, u, s, n_seq, divisor);
+    if (lane == 0) s_total[warp] = r;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        Total sum = s_total[0];
+#pragma unroll
+        for (int i = 1; i < WARPS; ++i) add(sum, s_total[i]);
+        a.totals[blockIdx.x] = sum;
+        __threadfence();
+        s_last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!s_last) return;
+    // the last CTA to arrive adds up all of them, in an order that depends on their number alone
+    __threadfence();
+    Total sum = {};
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += WARPS * 32) {
+        const volatile Total* t = a.totals + i;
+        add(sum, Total{t->policy, t->kl, t->entropy, t->tokens, t->clipped, t->cut, 0});
+    }
+    sum.policy = warp_sum(sum.policy);
+    sum.kl = warp_sum(sum.kl);
+    sum.entropy = warp_sum(sum.entropy);
+    sum.tokens = warp_sum(sum.tokens);
+    sum.clipped = warp_sum(sum.clipped);
+    sum.cut = warp_sum(sum.cut);
+    if (lane == 0) s_total[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sum = s_total[0];
+#pragma unroll
+        for (int i = 1; i < WARPS; ++i) add(sum, s_total[i]);
+        write_loss(a, sum);
+    }
+}
+
+// Both passes of a batch of few units.
+__global__ void __launch_bounds__(ONE_WARPS * 32) one_cta_kernel(const __grid_constant__ Args a) {
+    __shared__ Sums s_sums[ONE_WARPS];
+    __shared__ int s_n[ONE_WARPS];
+    __shared__ int s_count[ONE_WARPS];
+    __shared__ Total s_total[ONE_WARPS];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    tc::grid_launch_dependents();
+    tc::grid_dependency_wait();
+    check_bounds(a, threadIdx.x, ONE_WARPS * 32);
+    Unit u = {a.S, 0, 0, 0, 0};
+    if (lane == 0) s_n[warp] = 0;
+    if (warp < a.units) {
+        u = find_unit(a, warp);
+        unit_sums(a, u, s_sums + warp, s_n + warp);
+    }
+    __syncthreads();
+    const double divisor = count_divisor<ONE_WARPS>(a, s_n, s_count);
+    Sums s = {};
+    int n_seq = 1;
+    if ((a.by_sequence || a.mean_of_sequences) && u.begin < u.end)
+        sequence_sums(a, s_sums, s_n, u.first, u.count, &s, &n_seq);
+    const Total r = unit_loss(a, u, s, n_seq, divisor);
+    if (lane == 0) s_total[warp] = r;
+    __syncthreads();
+    if (warp == 0) {
+        Total sum = s_total[lane];
+        sum.policy = warp_sum(sum.policy);
+        sum.kl = warp_sum(sum.kl);
+        sum.entropy = warp_sum(sum.entropy);
+        sum.tokens = warp_sum(sum.tokens);
+        sum.clipped = warp_sum(sum.clipped);
+        sum.cut = warp_sum(sum.cut);
+        if (lane == 0) write_loss(a, sum);
+    }
+}
+
+static int unit_count(const r3_policy* c) { return c->S + 1 + c->T / UNIT; }
+
+static r3_status check(const r3_policy* c) {
+    if (!c || c->T < 0 || c->S < 0 || c->T > (1 << 30) || c->S > (1 << 28)) return R3_ERR_INVALID_ARG;
+    if ((c->ratio != R3_RATIO_TOKEN && c->ratio != R3_RATIO_SEQUENCE) ||
+        (c->reduce != R3_REDUCE_TOKEN && c->reduce != R3_REDUCE_SEQUENCE))
+        return R3_ERR_INVALID_ARG;
+    if (!(c->clip_low >= 0.0 && c->clip_low <= 1.0) || !(c->clip_high >= 0.0) ||
+        !(c->dual_clip == 0.0 || c->dual_clip > 1.0) || !(c->infer_cap > 0.0) ||
+        !(std::fabs(c->kl_coef) < 1e30) || !(std::fabs(c->entropy_coef) < 1e30) ||
+        !(c->denominator >= 0.0 && c->denominator < 1e30))
+        return R3_ERR_INVALID_ARG;
+    return R3_OK;
+}
+
+}  // namespace pol
+}  // namespace r3
+
+extern "C" size_t r3_policy_loss_workspace_bytes(const r3_policy* c) {
+    using namespace r3::pol;
+    if (check(c) != R3_OK) return 0;
+    const size_t units = (size_t)unit_count(c), ctas = (units + WARPS - 1) / WARPS;
+    return 256 + r3::round_up(units * sizeof(Sums), 256) + r3::round_up(units * sizeof(int), 256) +
+           r3::round_up(ctas * sizeof(Total), 256);
+}
+
+extern "C" r3_status r3_policy_loss(const r3_policy* c, const float* logp, const float* logp_old,
+                                    const float* advantages, const int32_t* cu_seqlens,
+                                    const uint8_t* mask, const float* logp_infer, const float* logp_ref,
+                                    const float* entropy, const float* dloss, float* loss, float* dlogp,
+                                    float* dentropy, float* metrics, int32_t* counts, void* workspace,
+                                    size_t ws_bytes, int32_t* dev_status, void* stream) {
+    using namespace r3;
+    using namespace r3::pol;
+    const r3_status st = check(c);
+    if (st != R3_OK) return st;
+    if (!loss || (c->T > 0 && (!logp || !logp_old)) || (c->T > 0 && c->S > 0 && !advantages))
+        return R3_ERR_INVALID_ARG;
+    if (!cu_seqlens && c->S != 1) return R3_ERR_INVALID_ARG;
+    if (dentropy && !entropy) return R3_ERR_INVALID_ARG;
+    const void* words[] = {logp, logp_old, advantages, cu_seqlens, logp_infer, logp_ref, entropy, dloss,
+                           loss, dlogp, dentropy, metrics, counts, dev_status};
+    for (const void* p : words)
+        if (!aligned(p, 4)) return R3_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || ws_bytes < r3_policy_loss_workspace_bytes(c))
+        return R3_ERR_WORKSPACE;
+    Args a = {};
+    a.T = c->T;
+    a.S = c->S;
+    a.units = unit_count(c);
+    a.by_sequence = c->ratio == R3_RATIO_SEQUENCE;
+    a.mean_of_sequences = c->reduce == R3_REDUCE_SEQUENCE;
+    a.adv_per_token = c->adv_per_token != 0;
+    a.need_sums = a.by_sequence || a.mean_of_sequences || c->denominator == 0.0;
+    a.log_high = std::log1p(c->clip_high);
+    a.log_low = std::log1p(-c->clip_low);
+    a.log_dual = c->dual_clip > 0.0 ? std::log(c->dual_clip) : INFINITY;
+    a.log_cap = std::log(c->infer_cap);
+    a.high = (float)(1.0 + c->clip_high);
+    a.low = (float)(1.0 - c->clip_low);
+    a.dual = (float)c->dual_clip;
+    a.cap = (float)c->infer_cap;
+    a.kl_coef = c->kl_coef;
+    a.entropy_coef = c->entropy_coef;
+    a.denominator = c->denominator;
+    a.logp = logp;
+    a.old = logp_old;
+    a.adv = advantages;
+    a.infer = logp_infer;
+    a.ref = logp_ref;
+    a.entropy = entropy;
+    a.dloss = dloss;
+    a.cu = cu_seqlens;
+    a.mask = mask;
+    a.loss = loss;
+    a.dlogp = dlogp;
+    a.dentropy = dentropy;
+    a.metrics = metrics;
+    a.counts = counts;
+    a.dev_status = dev_status;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    const int ctas = (a.units + WARPS - 1) / WARPS;
+    a.ticket = reinterpret_cast<unsigned*>(ws);
+    ws += 256;
+    a.sums = reinterpret_cast<Sums*>(ws);
+    ws += round_up((size_t)a.units * sizeof(Sums), 256);
+    a.n = reinterpret_cast<int*>(ws);
+    ws += round_up((size_t)a.units * sizeof(int), 256);
+    a.totals = reinterpret_cast<Total*>(ws);
+    cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    if (a.units <= ONE_WARPS)
+        return tc::launch_dependent(one_cta_kernel, dim3(1), dim3(ONE_WARPS * 32), 0, cs, a) == cudaSuccess
+                   ? R3_OK : R3_ERR_CUDA;
+    if (tc::launch_dependent(sums_kernel, dim3(ctas), dim3(WARPS * 32), 0, cs, a) != cudaSuccess ||
+        tc::launch_dependent(loss_kernel, dim3(ctas), dim3(WARPS * 32), 0, cs, a) != cudaSuccess)
+        return R3_ERR_CUDA;
+    return R3_OK;
+}

@@ -27,6 +27,8 @@ R3_ERR_OUT_OF_PAGES = 6
 R3_F32, R3_BF16 = 0, 1
 R3_IDX_U8, R3_IDX_I16 = 1, 2
 R3_GATE_NONE, R3_GATE_CHANNEL, R3_GATE_TOKEN, R3_GATE_FULL = 0, 1, 2, 3
+R3_RATIO_TOKEN, R3_RATIO_SEQUENCE = 0, 1
+R3_REDUCE_TOKEN, R3_REDUCE_SEQUENCE = 0, 1
 DEV_OK, DEV_BAD_INDEX, DEV_DUP_INDEX, DEV_TIMEOUT = 0, 1, 2, 3
 
 EXPORTS = [
@@ -46,6 +48,8 @@ EXPORTS = [
     "r3_normed_stack_train_workspace_bytes", "r3_normed_stack_train",
     "r3_norm_residual", "r3_norm_residual_bwd_workspace_bytes", "r3_norm_residual_bwd",
     "r3_token_logprobs", "r3_token_logprobs_bwd",
+    "r3_policy_loss_workspace_bytes", "r3_policy_loss",
+    "r3_balance_loss_workspace_bytes", "r3_balance_loss",
     "r3_prob_discrepancy_workspace_bytes", "r3_prob_discrepancy", "r3_record_diff",
     "r3_sequence_diff", "r3_grouped_swiglu_bwd_workspace_bytes", "r3_grouped_swiglu_bwd_input",
     "r3_grouped_swiglu_bwd", "r3_grouped_swiglu_train", "r3_scale_rows", "r3_input_grad_finish",
@@ -98,6 +102,20 @@ class AdamWConfig(ctypes.Structure):
                 ("master", ctypes.c_int32), ("state_bits", ctypes.c_int32), ("step", ctypes.c_int64),
                 ("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
                 ("eps", ctypes.c_double)]
+
+
+class Policy(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("S", ctypes.c_int32), ("ratio", ctypes.c_int32),
+                ("reduce", ctypes.c_int32), ("adv_per_token", ctypes.c_int32),
+                ("clip_low", ctypes.c_double), ("clip_high", ctypes.c_double),
+                ("dual_clip", ctypes.c_double), ("infer_cap", ctypes.c_double),
+                ("kl_coef", ctypes.c_double), ("entropy_coef", ctypes.c_double),
+                ("denominator", ctypes.c_double)]
+
+
+class Balance(ctypes.Structure):
+    _fields_ = [("balance_coef", ctypes.c_double), ("z_coef", ctypes.c_double),
+                ("accumulate", ctypes.c_int32), ("counts_given", ctypes.c_int32)]
 
 
 _P = ctypes.c_void_p
@@ -166,6 +184,13 @@ lib.r3_norm_residual_bwd.argtypes = [_NP] + [_P] * 13 + [ctypes.c_size_t, _P]
 lib.r3_token_logprobs.argtypes = [ctypes.POINTER(Logits)] + [_P] * 5 + [ctypes.c_int32] + [_P] * 4
 lib.r3_token_logprobs_bwd.argtypes = ([ctypes.POINTER(Logits)] + [_P] * 7 + [ctypes.c_int64]
                                       + [_P] * 2)
+lib.r3_policy_loss_workspace_bytes.restype = ctypes.c_size_t
+lib.r3_policy_loss_workspace_bytes.argtypes = [ctypes.POINTER(Policy)]
+lib.r3_policy_loss.argtypes = [ctypes.POINTER(Policy)] + [_P] * 15 + [ctypes.c_size_t, _P, _P]
+lib.r3_balance_loss_workspace_bytes.restype = ctypes.c_size_t
+lib.r3_balance_loss_workspace_bytes.argtypes = [_SP, ctypes.c_int32]
+lib.r3_balance_loss.argtypes = ([_SP, ctypes.c_int32, ctypes.POINTER(Balance)] + [_P] * 7
+                                + [ctypes.c_size_t, _P, _P])
 lib.r3_prob_discrepancy_workspace_bytes.restype = ctypes.c_size_t
 lib.r3_prob_discrepancy_workspace_bytes.argtypes = [ctypes.c_int64]
 lib.r3_prob_discrepancy.argtypes = [_P, _P, ctypes.c_int64, _P, ctypes.c_int32, _P, _P, _P,
@@ -1097,6 +1122,96 @@ def token_logprobs_bwd(logits, token_ids, stats, dlogp, *, entropy=None, dentrop
     _check(lib.r3_token_logprobs_bwd(ctypes.byref(s), ptr, ids, stats, entropy, dlogp, dentropy, out,
                                      ld_out, _ptr(dev_status), _stream(stream)))
     return dlogits
+
+
+_RATIO = {"token": R3_RATIO_TOKEN, "sequence": R3_RATIO_SEQUENCE}
+_REDUCE = {"token": R3_REDUCE_TOKEN, "sequence": R3_REDUCE_SEQUENCE}
+
+
+@_in_order
+def policy_loss(logp, logp_old, cu_seqlens=None, *, advantages=None, seq_advantages=None, mask=None,
+                logp_infer=None, logp_ref=None, entropy=None, ratio="token", reduce="token",
+                clip_low=0.2, clip_high=0.2, dual_clip=0.0, infer_cap=2.0, kl_coef=0.0,
+                entropy_coef=0.0, denominator=0.0, dloss=None, want_grad=True, ws=None,
+                dev_status=None, stream=None):
+    """Clipped policy loss over packed responses and its gradients (r3_policy_loss).  logp, logp_old,
+    logp_infer, logp_ref, entropy [T] float32; cu_seqlens [S+1] int32 (None: one sequence); mask [T] bool or
+    uint8; advantages [T] or seq_advantages [S], one of them.  ratio: "token" or "sequence"; reduce: mean
+    over "token"s or over "sequence" means, or with denominator the sum over that.  Returns (loss [1],
+    dlogp [T] or None, dentropy [T] or None, metrics [3], counts [3] int32)."""
+    dev = _device_of("logp", logp)
+    if logp.dim() != 1:
+        raise ValueError("logp: expected [T]")
+    if ratio not in _RATIO:
+        raise ValueError(f"ratio: {ratio!r}, expected 'token' or 'sequence'")
+    if reduce not in _REDUCE:
+        raise ValueError(f"reduce: {reduce!r}, expected 'token' or 'sequence'")
+    if (advantages is None) == (seq_advantages is None):
+        raise ValueError("advantages, seq_advantages: expected one of them")
+    T, S, f32, new = logp.numel(), 1, torch.float32, torch.empty_strided
+    cu = None
+    if cu_seqlens is not None:
+        if not isinstance(cu_seqlens, torch.Tensor):
+            raise TypeError("cu_seqlens: expected a torch.Tensor")
+        S = cu_seqlens.numel() - 1
+        if S < 0:
+            raise ValueError("cu_seqlens: expected [S + 1]")
+        cu = _arg("cu_seqlens", cu_seqlens, (S + 1,), torch.int32, dev)
+    at = [_arg(name, t, (T,), f32, dev) for name, t in
+          (("logp", logp), ("logp_old", logp_old), ("logp_infer", logp_infer), ("logp_ref", logp_ref),
+           ("entropy", entropy))]
+    adv = (_arg("advantages", advantages, (T,), f32, dev) if seq_advantages is None
+           else _arg("seq_advantages", seq_advantages, (S,), f32, dev))
+    if mask is not None:
+        mask = _arg("mask", mask, (T,), torch.uint8 if mask.dtype == torch.uint8 else torch.bool, dev)
+    c = Policy(T, S, _RATIO[ratio], _REDUCE[reduce], seq_advantages is None, clip_low, clip_high, dual_clip,
+               infer_cap, kl_coef, entropy_coef, denominator)
+    # the small outputs lie in one allocation
+    small = new((7,), (1,), dtype=f32, device=dev)
+    loss, metrics, counts = small[:1], small[1:4], small[4:].view(torch.int32)
+    dlogp = new((T,), (1,), dtype=f32, device=dev) if want_grad else None
+    dentropy = new((T,), (1,), dtype=f32, device=dev) if want_grad and entropy is not None else None
+    here = small.data_ptr()
+    ws = _scratch(ws, lib.r3_policy_loss_workspace_bytes(ctypes.byref(c)), dev)
+    _check(lib.r3_policy_loss(
+        ctypes.byref(c), at[0], at[1], adv, cu, mask, at[2], at[3], at[4],
+        _arg("dloss", dloss, (1,), f32, dev), here, None if dlogp is None else dlogp.data_ptr(),
+        None if dentropy is None else dentropy.data_ptr(), here + 4, here + 16, ws.data_ptr(), ws.numel(),
+        None if dev_status is None else _ptr(dev_status), _stream(stream)))
+    return loss, dlogp, dentropy, metrics, counts
+
+
+@_in_order
+def balance_loss(s: Shape, L: int, logits, idx=None, *, mask=None, counts=None, balance_coef=1.0, z_coef=0.0,
+                 dlogits=None, accumulate=False, want_grad=True, ws=None, dev_status=None, stream=None):
+    """Balance and z loss of L blocks' routers (r3_balance_loss): logits [L,T,E] float32, idx [L,T,K] the
+    record whose choices are counted, mask [T] bool or uint8.  counts [L,E] int32: given, they stand in for
+    the record's.  With accumulate the gradient is added to dlogits.  Returns (loss [L,2], counts [L,E]
+    int32, dlogits [L,T,E] or None)."""
+    dev = _device_of("logits", logits)
+    f32, grad = torch.float32, (L, s.T, s.E)
+    given = counts is not None
+    if not given and idx is None:
+        raise ValueError("idx, counts: expected one of them")
+    if accumulate and dlogits is None:
+        raise ValueError("accumulate: needs dlogits")
+    at = _arg("logits", logits, grad, f32, dev)
+    rec = _arg("idx", idx, (L, s.T, s.K), _idx_dtype(s), dev)
+    if mask is not None:
+        mask = _arg("mask", mask, (s.T,), torch.uint8 if mask.dtype == torch.uint8 else torch.bool, dev)
+    if not given:
+        counts = torch.empty_strided((L, s.E), (s.E, 1), dtype=torch.int32, device=dev)
+    if dlogits is None and want_grad:
+        dlogits = torch.empty_strided(grad, (s.T * s.E, s.E, 1), dtype=f32, device=dev)
+    loss = torch.empty_strided((L, 2), (2, 1), dtype=f32, device=dev)
+    c = Balance(balance_coef, z_coef, bool(accumulate), given)
+    ws = _scratch(ws, lib.r3_balance_loss_workspace_bytes(ctypes.byref(s), L), dev)
+    _check(lib.r3_balance_loss(
+        ctypes.byref(s), L, ctypes.byref(c), at, rec, mask,
+        _arg("counts", counts, (L, s.E), torch.int32, dev), loss.data_ptr(),
+        _arg("dlogits", dlogits, grad, f32, dev), ws.data_ptr(), ws.numel(),
+        None if dev_status is None else _ptr(dev_status), _stream(stream)))
+    return loss, counts, dlogits
 
 
 @_in_order

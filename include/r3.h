@@ -590,6 +590,65 @@ typedef struct {
 r3_status r3_adamw_step(const r3_adamw* config, const r3_adamw_tensor* tensors, int32_t n_tensors,
                         const float* grad_scale, const float* scalars, void* stream);
 
+/* ---- orthogonalised updates (an extension: an optimiser for matrices beside r3_adamw_step) ---------- */
+
+/* batch matrices [rows, cols], dense and row-major, sides up to 16384.  steps 1 to 16; coefs (HOST,
+ * [steps][3] = a, b, c of each step) or NULL = (3.4445, -4.7750, 2.0315) for all.  products: 1 = every product
+ * from fp16 operands (as exact as a bf16 result), 3 = from operands of two fp16 planes (a float32 result).
+ * eps >= 0. */
+typedef struct {
+    int32_t batch, rows, cols, in_dtype, out_dtype, steps, products;
+    double eps;
+    const double* coefs;
+} r3_orthogonal;
+
+/* Newton-Schulz iteration, per matrix: X = x / (|x|_F + eps), then steps times, with the Gram matrix of the
+ * smaller side (here rows <= cols),
+ *   A = X X^T;   B = b A + c A^2;   X = a X + B X
+ * which brings the singular values near one; out = X.  x of in_dtype, out of out_dtype, may be the same
+ * buffer (of one type).  All products accumulate in float32, X is carried in 22 bits between the steps.
+ *  - A matrix of zeros gives zeros, one that holds what is not finite gives NaN; the others of a batch are
+ *    not touched by it.
+ *  - Coefficients whose iterates could pass 16 in norm (or b A + c A^2 60) are refused.
+ * workspace: r3_orthogonalize_workspace_bytes(config), 256-byte aligned: up to about 512 MB (or what one matrix
+ * needs); larger batches are taken in parts. */
+size_t r3_orthogonalize_workspace_bytes(const r3_orthogonal* config);
+r3_status r3_orthogonalize(const r3_orthogonal* config, const void* x, void* out, void* workspace,
+                           size_t ws_bytes, int32_t* dev_status, void* stream);
+
+/* A stack of `batch` matrices [rows, cols] of one parameter (expert weights [E, F, d] are E of them); the struct
+ * lives in HOST memory, its pointers are device pointers (16-byte aligned).  momentum float32; master float32
+ * (with config->master) or NULL.  scale multiplies the orthogonalised update. */
+typedef struct {
+    void* param;
+    float* master;
+    const void* grad;
+    float* momentum;
+    int32_t batch, rows, cols;
+    float weight_decay, scale;
+} r3_muon_stack;
+
+/* products, steps, coefs and eps as for r3_orthogonal. */
+typedef struct {
+    int32_t param_dtype, grad_dtype, master, nesterov, steps, products;
+    double lr, momentum, eps;
+    const double* coefs;
+} r3_muon;
+
+/* One step over n_stacks stacks (a HOST array).  Per matrix, with g = grad * grad_scale:
+ *   m = momentum m + g;   u = g + momentum m (nesterov) or m;   o = r3_orthogonalize(u)
+ *   w = w (1 - lr weight_decay) - lr scale o
+ * w is the master where there is one (param then gets its rounding), else param.  Stacks of one shape are taken
+ * together.  grad_scale (device, float32, or NULL = 1): not finite = the whole step is skipped, nothing is
+ * written.  lr (device, [1] float32, or NULL): in place of config's, for a captured step.
+ *  - A matrix whose u is not finite gets NaN weights; its momentum is what the formula gives.
+ *  - Buffers that the step writes and that overlap, each other or one that it reads, are refused.
+ * workspace: r3_muon_workspace_bytes(config, stacks, n_stacks). */
+size_t r3_muon_workspace_bytes(const r3_muon* config, const r3_muon_stack* stacks, int32_t n_stacks);
+r3_status r3_muon_step(const r3_muon* config, const r3_muon_stack* stacks, int32_t n_stacks,
+                       const float* grad_scale, const float* lr, void* workspace, size_t ws_bytes,
+                       int32_t* dev_status, void* stream);
+
 /* ---- stacks of replayed blocks with norms around every block (an extension) ----------------------- */
 
 /* The norms of L blocks, stacked on a leading layer axis, all of w_dtype and 16-byte aligned:

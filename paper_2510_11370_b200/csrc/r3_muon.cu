@@ -1,0 +1,1081 @@
+// Newton-Schulz orthogonalisation of matrices, and the momentum step of an optimiser built on it.  With
+// u the matrix, X = u / (|u|_F + eps) and per step (a, b, c):
+//   A = X X^T  (X^T X where the matrix is tall: the smaller side)     B = b A + c A^2     X = a X + B X
+//
+// Three products a step on the tensor cores, each a batch over all matrices of a chunk.  Numbers.  The
+// iterates' singular values stay near one, so fp16 (11 bits, against bf16's 8) holds every operand, times
+// 2^10 to keep small elements in its normal range.  X itself is carried in two fp16 planes, hi + lo (22 bits):
+// the term a X, by which a weak direction grows a^steps-fold, then has no rounding to speak of, and what the
+// products' operands lose stays as small as the output's own rounding to bf16 whatever the matrix's spectrum
+// is (simulated for full-rank, decaying and low-rank spectra: 4e-4 to 1.7e-3 of the result's rms, against
+// 1.7e-3 for the rounding; bf16 operands with a rounded X lose a third of a rank-8 update).  For float32
+// results A and B get a second plane as well and every product is hi hi + hi lo + lo hi.
+//
+// One GEMM kernel does all three: D = alpha (product) + beta L, L a matrix read tile by tile, with two CTAs
+// per MMA (256 x 256 tiles, 128 rows of each operand per CTA and k block of 64, accumulators double
+// buffered in tensor memory).  A and B are symmetric: only tiles on and below the diagonal are computed, the
+// others are stored from the same accumulators, transposed.  Eight epilogue warps, each with its own 8 KB of
+// shared memory: L comes and D goes by TMA in boxes of 32 rows x 64 columns.
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cmath>
+#include <vector>
+
+#include "r3_common.cuh"
+#include "r3_internal.h"
+#include "r3_tc.cuh"
+
+namespace r3 {
+namespace ns {
+
+using namespace tc;
+
+constexpr float SCALE = 1024.f;           // every fp16 operand is its value times this
+constexpr int BM = 128;                   // rows of either operand per CTA and stage
+constexpr int TILE = 2 * BM;              // output tile of a CTA pair: TILE x TILE
+constexpr int BK = 64;                    // k per stage: 64 fp16 = one 128-byte swizzle row
+constexpr int UK = 16;                    // k per tcgen05.mma
+constexpr int STAGES = 5;
+constexpr int OPERAND_BYTES = BM * BK * 2;
+constexpr int STAGE_BYTES = 2 * OPERAND_BYTES;
+constexpr int EPI_WARPS = 8;              // two per TMEM lane quadrant, every other 64 columns each
+constexpr int EPI_PLANE = 32 * 128;       // 32 rows x 64 columns of fp16
+constexpr int EPI_BYTES = EPI_WARPS * 2 * EPI_PLANE;
+constexpr int BAR_BYTES = 256;
+constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES + EPI_BYTES + BAR_BYTES;
+constexpr int THREADS = 32 * (2 + EPI_WARPS);
+constexpr int TMEM_COLS = 512;            // two accumulator stages of TILE columns
+
+struct alignas(64) GemmArgs {
+    CUtensorMap a[2], b[2];               // operands, planes hi and lo
+    CUtensorMap in[2], out[2], mirror[2];
+    int rows, cols;                       // of D
+    int tiles_n, tiles, items, kblocks;   // tiles: of one matrix
+    float alpha, beta;
+    int32_t* dev_status;
+};
+
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read() {
+    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+}
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+
+struct Tile {
+    int z, m, n;                          // matrix, tile row and column
+};
+// SYM: the tiles with m >= n, row by row.
+template <bool SYM> __device__ __forceinline__ Tile decode(const GemmArgs& g, int item) {
+    Tile t;
+    t.z = item / g.tiles;
+    const int r = item - t.z * g.tiles;
+    if (SYM) {
+        int m = (int)((sqrtf(8.f * (float)r + 1.f) - 1.f) * 0.5f);
+        while (m * (m + 1) / 2 > r) --m;
+        while ((m + 1) * (m + 2) / 2 <= r) ++m;
+        t.m = m;
+        t.n = r - m * (m + 1) / 2;
+    } else {
+        t.m = r / g.tiles_n;
+        t.n = r - t.m * g.tiles_n;
+    }
+    return t;
+}
+
+// A_MN, B_MN: the operand's rows in memory run along k (its 128 rows or columns of a tile are consecutive
+// in memory); otherwise k is consecutive.  SYM: a symmetric result.  IN, OUT: planes of L and D.
+template <bool A_MN, bool B_MN, bool SYM, int IN, int OUT, int TERMS>
+__global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant__ GemmArgs g) {
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t epi0 = base + STAGES * STAGE_BYTES;
+    const uint32_t bar0 = epi0 + EPI_BYTES;
+    auto full_bar = [&](int s) { return bar0 + 8u * s; };
+    auto empty_bar = [&](int s) { return bar0 + 8u * (STAGES + s); };
+    auto tfull_bar = [&](int a) { return bar0 + 8u * (2 * STAGES + a); };
+    auto tempty_bar = [&](int a) { return bar0 + 8u * (2 * STAGES + 2 + a); };
+    auto in_bar = [&](int w) { return bar0 + 8u * (2 * STAGES + 4 + w); };
+    uint8_t* misc = base_ptr + STAGES * STAGE_BYTES + EPI_BYTES + 192;
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(misc);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 4);
+    static_assert(8 * (2 * STAGES + 4 + EPI_WARPS) <= 192, "barriers");
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(tfull_bar(a), 1);
+            mbar_init(tempty_bar(a), 2 * EPI_WARPS);
+        }
+        for (int w = 0; w < EPI_WARPS; ++w) mbar_init(in_bar(w), 1);
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == 1) tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), TMEM_COLS);
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    grid_launch_dependents();
+    grid_dependency_wait();
+
+    if (warp == 0) {
+        // ------------------------------ TMA producer: this CTA's half of both operands ---------
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int item = pair; ok && item < g.items; item += pairs) {
+                const Tile t = decode<SYM>(g, item);
+                const int m0 = t.m * TILE + (int)rank * BM, n0 = t.n * TILE + (int)rank * BM;
+                for (int term = 0; ok && term < TERMS; ++term) {
+                    // the small products first: an addition drops what lies below the running sum's
+                    // last place
+                    const CUtensorMap* am = &g.a[TERMS > 1 && term == 1];
+                    const CUtensorMap* bm = &g.b[TERMS > 1 && term == 0];
+                    for (int kb = 0; kb < g.kblocks; ++kb) {
+                        if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, g.dev_status)) {
+                            ok = false;
+                            break;
+                        }
+                        const uint32_t sa = base + stage * STAGE_BYTES, sb = sa + OPERAND_BYTES;
+                        const uint32_t lead = mapa_shared(full_bar(stage), 0);
+                        if (rank == 0) mbar_expect_tx(full_bar(stage), 2u * STAGE_BYTES);
+                        if (A_MN) {
+                            tma_load_3d_pair(sa, am, m0, kb * BK, t.z, lead);
+                            tma_load_3d_pair(sa + OPERAND_BYTES / 2, am, m0 + 64, kb * BK, t.z, lead);
+                        } else {
+                            tma_load_3d_pair(sa, am, kb * BK, m0, t.z, lead);
+                        }
+                        if (B_MN) {
+                            tma_load_3d_pair(sb, bm, n0, kb * BK, t.z, lead);
+                            tma_load_3d_pair(sb + OPERAND_BYTES / 2, bm, n0 + 64, kb * BK, t.z, lead);
+                        } else {
+                            tma_load_3d_pair(sb, bm, kb * BK, n0, t.z, lead);
+                        }
+                        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                    }
+                }
+            }
+            // every stage's release has landed before this CTA may leave
+            for (int s = 0; ok && s < STAGES; ++s) {
+                ok = mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, g.dev_status);
+                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------ MMA issuer (leader CTA) ---------------------------------
+        if (rank == 0) {
+            constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(TILE >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24) |
+                                       (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
+            // 16 along k: 32 bytes inside the swizzled row, or two groups of 8 k rows
+            constexpr uint64_t a_step = A_MN ? (2048 >> 4) : 2, b_step = B_MN ? (2048 >> 4) : 2;
+            int stage = 0, acc = 0;
+            uint32_t phase = 0, acc_phase = 0;
+            bool ok = true;
+            const int blocks = g.kblocks * TERMS;
+            for (int item = pair; ok && item < g.items; item += pairs) {
+                if (!__all_sync(0xffffffffu,
+                                mbar_wait(tempty_bar(acc), acc_phase ^ 1u, abort_flag, g.dev_status)))
+                    break;
+                tc_fence_after();
+                const uint32_t d_tmem = tmem_base + (uint32_t)(acc * TILE);
+                for (int kb = 0; kb < blocks; ++kb) {
+                    if (!__all_sync(0xffffffffu,
+                                    mbar_wait(full_bar(stage), phase, abort_flag, g.dev_status))) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t sa = base + stage * STAGE_BYTES, sb = sa + OPERAND_BYTES;
+                        const uint64_t da = A_MN ? smem_desc_mn_sw128(sa, OPERAND_BYTES / 2)
+                                                 : smem_desc_sw128(sa);
+                        const uint64_t db = B_MN ? smem_desc_mn_sw128(sb, OPERAND_BYTES / 2)
+                                                 : smem_desc_sw128(sb);
+#pragma unroll
+                        for (int kk = 0; kk < BK / UK; ++kk)
+                            tc_mma_bf16_pair(d_tmem, da + a_step * kk, db + b_step * kk, idesc,
+                                             (kb | kk) != 0 ? 1u : 0u);
+                        tc_commit_pair(empty_bar(stage), 3);
+                    }
+                    __syncwarp();
+                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                }
+                if (!ok) break;
+                if (elect_one()) tc_commit_pair(tfull_bar(acc), 3);
+                __syncwarp();
+                if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            }
+        }
+    } else {
+        // ------------------------------ epilogue ------------------------------------------------
+        const int w = warp - 2, q = warp & 3, group = w >> 2;
+        const uint32_t buf = epi0 + (uint32_t)w * (2 * EPI_PLANE);
+        uint8_t* buf_ptr = base_ptr + STAGES * STAGE_BYTES + w * (2 * EPI_PLANE);
+        int acc = 0;
+        uint32_t acc_phase = 0, in_phase = 0;
+        bool alive = true;
+        for (int item = pair; item < g.items; item += pairs) {
+            const Tile t = decode<SYM>(g, item);
+            const int row0 = t.m * TILE + (int)rank * BM + q * 32;
+            // this warp's 64 columns that begin inside of D (with its rows)
+            const int c_end = row0 < g.rows ? min(TILE, g.cols - t.n * TILE) : 0;
+            auto fetch = [&](int c) {                  // L under columns c .. c + 63, by one lane
+                bulk_wait_read();                      // the last store out of this buffer
+                mbar_expect_tx(in_bar(w), IN * EPI_PLANE);
+#pragma unroll
+                for (int p = 0; p < IN; ++p)
+                    tma_load_3d(buf + p * EPI_PLANE, &g.in[p], t.n * TILE + c, row0, t.z, in_bar(w));
+            };
+            if (IN > 0 && alive && lane == 0 && group * 64 < c_end) fetch(group * 64);
+            if (alive) {
+                const bool ok = mbar_wait(tfull_bar(acc), acc_phase, abort_flag, g.dev_status);
+                alive = __all_sync(0xffffffffu, ok);
+            }
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = group * 64; c < c_end; c += 128) {
+                const int col0 = t.n * TILE + c;
+                if (IN > 0) {
+                    if (alive && lane == 0 && c > group * 64) fetch(c);
+                    if (alive) {
+                        const bool ok = mbar_wait(in_bar(w), in_phase, abort_flag, g.dev_status);
+                        alive = __all_sync(0xffffffffu, ok);
+                        in_phase ^= 1u;
+                    }
+                }
+                if (!alive) continue;
+                if (IN == 0) {
+                    if (lane == 0) bulk_wait_read();
+                    __syncwarp();
+                }
+                const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * TILE + c);
+                uint32_t packed[OUT][32];              // pairs of columns
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    float v[32];
+                    tc_ld32(taddr + 32 * half, v);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        // eight columns: 16 bytes, at the place that the copy's swizzle gives them
+                        const int at = lane * 128 + (((half * 4 + j) ^ (lane & 7)) * 16);
+                        float l[8];
+                        if (IN > 0) {
+                            const uint4 x = *reinterpret_cast<const uint4*>(buf_ptr + at);
+                            const __half2* h = reinterpret_cast<const __half2*>(&x);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float2 f = __half22float2(h[i]);
+                                l[2 * i] = f.x;
+                                l[2 * i + 1] = f.y;
+                            }
+                        }
+                        if (IN > 1) {
+                            const uint4 x = *reinterpret_cast<const uint4*>(buf_ptr + EPI_PLANE + at);
+                            const __half2* h = reinterpret_cast<const __half2*>(&x);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float2 f = __half22float2(h[i]);
+                                l[2 * i] += f.x;
+                                l[2 * i + 1] += f.y;
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float d0 = g.alpha * v[8 * j + 2 * i], d1 = g.alpha * v[8 * j + 2 * i + 1];
+                            if (IN > 0) {
+                                d0 = fmaf(g.beta, l[2 * i], d0);
+                                d1 = fmaf(g.beta, l[2 * i + 1], d1);
+                            }
+                            const __half2 hi = __floats2half2_rn(d0, d1);
+                            packed[0][half * 16 + 4 * j + i] = *reinterpret_cast<const uint32_t*>(&hi);
+                            if constexpr (OUT > 1) {
+                                const float2 f = __half22float2(hi);
+                                const __half2 lo = __floats2half2_rn(d0 - f.x, d1 - f.y);
+                                packed[1][half * 16 + 4 * j + i] = *reinterpret_cast<const uint32_t*>(&lo);
+                            }
+                        }
+                    }
+                }
+#pragma unroll
+                for (int p = 0; p < OUT; ++p)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        *reinterpret_cast<uint4*>(buf_ptr + p * EPI_PLANE + lane * 128 + ((j ^ (lane & 7)) * 16)) =
+                            make_uint4(packed[p][4 * j], packed[p][4 * j + 1], packed[p][4 * j + 2],
+                                       packed[p][4 * j + 3]);
+                fence_async();
+                __syncwarp();
+                if (lane == 0) {
+#pragma unroll
+                    for (int p = 0; p < OUT; ++p)
+                        tma_store_3d(&g.out[p], buf + p * EPI_PLANE, col0, row0, t.z);
+                    bulk_commit();
+                }
+                if (SYM && t.m != t.n) {
+                    // the same values as 64 rows x 32 columns of the other triangle
+                    if (lane == 0) bulk_wait_read();
+                    __syncwarp();
+#pragma unroll
+                    for (int p = 0; p < OUT; ++p)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            __half* to = reinterpret_cast<__half*>(buf_ptr + p * EPI_PLANE) + 2 * j * 32 + lane;
+                            const __half2 h = *reinterpret_cast<const __half2*>(&packed[p][j]);
+                            to[0] = __low2half(h);
+                            to[32] = __high2half(h);
+                        }
+                    fence_async();
+                    __syncwarp();
+                    if (lane == 0) {
+#pragma unroll
+                        for (int p = 0; p < OUT; ++p)
+                            tma_store_3d(&g.mirror[p], buf + p * EPI_PLANE, row0, col0, t.z);
+                        bulk_commit();
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0 && alive) mbar_arrive_cluster(mapa_shared(tempty_bar(acc), 0));
+            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        }
+        if (lane == 0) bulk_wait_all();
+    }
+
+    // ------------------------------ teardown ---------------------------------------------------
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        // copies may still be in flight into this CTA's shared memory: give them time to land
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+        __syncthreads();
+    }
+    cluster_sync_all();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc_pair(tmem_base, TMEM_COLS);
+    }
+}
+
+// ---- around the iteration: elementwise, a matrix in pieces of PIECE elements ----------------------
+constexpr int EL_THREADS = 256;
+constexpr int PIECE = EL_THREADS * 32;
+constexpr int MAX_STACKS = 64;            // per launch: the table travels in the kernel's parameters
+
+struct Stack {
+    void* param;                          // or the result of an orthogonalisation
+    float* master;
+    const void* grad;                     // or its input
+    float* momentum;                      // null: none
+    int first;                            // number of its first matrix in the group
+    float decay, scale;
+};
+struct ElemArgs {
+    int stacks, begin;                    // matrices from number `begin` of the group on
+    int rows, cols, ld, pieces;
+    long long plane;                      // elements of a matrix in the planes: rows * ld
+    int nesterov;
+    float momentum, eps, lr;
+    const float* grad_scale;
+    const float* lr_now;
+    __half *hi, *lo;
+    double* norms;                        // [matrices, pieces]
+    Stack stack[MAX_STACKS];
+};
+
+__device__ __forceinline__ const Stack& find_stack(const ElemArgs& a, int matrix, int* within) {
+    int i = 0;
+    for (int step = MAX_STACKS / 2; step > 0; step >>= 1)
+        if (i + step < a.stacks && a.stack[i + step].first <= matrix) i += step;
+    *within = matrix - a.stack[i].first;
+    return a.stack[i];
+}
+__device__ __forceinline__ bool scale_of(const float* grad_scale, float* s) {
+    *s = grad_scale ? *grad_scale : 1.f;
+    return isfinite(*s);
+}
+// Eight consecutive elements as float32.
+template <typename T> __device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
+    constexpr int N = Vec16<T>::N;
+#pragma unroll
+    for (int i = 0; i < 8 / N; ++i) {
+        Vec16<T> v;
+        v.v = *reinterpret_cast<const decltype(v.v)*>(p + i * N);
+        v.unpack(f + i * N);
+    }
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
+    constexpr int N = Vec16<T>::N;
+#pragma unroll
+    for (int i = 0; i < 8 / N; ++i) {
+        Vec16<T> v;
+        v.pack(f + i * N);
+        *reinterpret_cast<decltype(v.v)*>(p + i * N) = v.v;
+    }
+}
+
+// u from the gradient and the momentum after this step; every product and sum is rounded by itself.
+__device__ __forceinline__ float direction(const ElemArgs& a, bool momentum, float g, float m) {
+    if (!momentum) return g;
+    return a.nesterov ? __fadd_rn(g, __fmul_rn(a.momentum, m)) : m;
+}
+
+// First pass: the momentum's update and the sum of u^2 of every piece.  grid (pieces, matrices)
+template <typename G, bool WIDE>
+__global__ void __launch_bounds__(EL_THREADS) norm_kernel(const __grid_constant__ ElemArgs a) {
+    __shared__ double s_sum[EL_THREADS / 32];
+    grid_launch_dependents();
+    grid_dependency_wait();
+    int z;
+    const Stack& st = find_stack(a, a.begin + blockIdx.y, &z);
+    const long long size = (long long)a.rows * a.cols, base = (long long)z * size;
+    const G* grad = static_cast<const G*>(st.grad) + base;
+    float* mom = st.momentum ? st.momentum + base : nullptr;
+    float gs;
+    const bool go = scale_of(a.grad_scale, &gs);
+    const long long p0 = (long long)blockIdx.x * PIECE, p1 = min(size, p0 + PIECE);
+    double sum = 0.0;
+    if (go) {
+        if (WIDE) {
+#pragma unroll 2
+            for (long long i = p0 + threadIdx.x * 8; i < p1; i += EL_THREADS * 8) {
+                float g[8], m[8];
+                load8(grad + i, g);
+                if (mom) {
+                    load8(mom + i, m);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        m[k] = __fadd_rn(__fmul_rn(a.momentum, m[k]), __fmul_rn(g[k], gs));
+                    store8(mom + i, m);
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const double u = (double)direction(a, mom != nullptr, __fmul_rn(g[k], gs), m[k]);
+                    sum += u * u;
+                }
+            }
+        } else {
+            for (long long i = p0 + threadIdx.x; i < p1; i += EL_THREADS) {
+                const float g = __fmul_rn(to_f32(grad[i]), gs);
+                float m = 0.f;
+                if (mom) {
+                    m = __fadd_rn(__fmul_rn(a.momentum, mom[i]), g);
+                    mom[i] = m;
+                }
+                const double u = (double)direction(a, mom != nullptr, g, m);
+                sum += u * u;
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sum = 0.0;
+        for (int i = 0; i < EL_THREADS / 32; ++i) sum += s_sum[i];
+        a.norms[(size_t)blockIdx.y * a.pieces + blockIdx.x] = sum;
+    }
+}
+
+// Second pass: X = u / (|u| + eps) into the planes.
+template <typename G, bool WIDE>
+__global__ void __launch_bounds__(EL_THREADS) start_kernel(const __grid_constant__ ElemArgs a) {
+    __shared__ double s_sum[EL_THREADS / 32];
+    grid_launch_dependents();
+    grid_dependency_wait();
+    int z;
+    const Stack& st = find_stack(a, a.begin + blockIdx.y, &z);
+    const long long size = (long long)a.rows * a.cols, base = (long long)z * size;
+    const G* grad = static_cast<const G*>(st.grad) + base;
+    const float* mom = st.momentum ? st.momentum + base : nullptr;
+    float gs;
+    if (!scale_of(a.grad_scale, &gs)) return;          // the step is skipped: the planes are not looked at
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < a.pieces; i += EL_THREADS) sum += a.norms[(size_t)blockIdx.y * a.pieces + i];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < EL_THREADS / 32; ++i) sum += s_sum[i];
+    const double norm = sqrt(sum);
+    // a matrix of zeros stays one; anything not finite reaches every element
+    const float inv = norm == 0.0 ? 0.f : (float)((double)SCALE / (norm + (double)a.eps));
+    __half* hi = a.hi + (size_t)blockIdx.y * a.plane;
+    __half* lo = a.lo + (size_t)blockIdx.y * a.plane;
+    const long long p0 = (long long)blockIdx.x * PIECE, p1 = min(size, p0 + PIECE);
+    if (WIDE) {
+#pragma unroll 2
+        for (long long i = p0 + threadIdx.x * 8; i < p1; i += EL_THREADS * 8) {
+            float g[8], m[8];
+            load8(grad + i, g);
+            if (mom) load8(mom + i, m);
+            uint4 h, l;
+            __half2* hp = reinterpret_cast<__half2*>(&h);
+            __half2* lp = reinterpret_cast<__half2*>(&l);
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+                const float x0 = direction(a, mom != nullptr, __fmul_rn(g[k], gs), m[k]) * inv;
+                const float x1 = direction(a, mom != nullptr, __fmul_rn(g[k + 1], gs), m[k + 1]) * inv;
+                hp[k / 2] = __floats2half2_rn(x0, x1);
+                const float2 f = __half22float2(hp[k / 2]);
+                lp[k / 2] = __floats2half2_rn(x0 - f.x, x1 - f.y);
+            }
+            *reinterpret_cast<uint4*>(hi + i) = h;     // ld = cols here
+            *reinterpret_cast<uint4*>(lo + i) = l;
+        }
+    } else {
+        for (long long i = p0 + threadIdx.x; i < p1; i += EL_THREADS) {
+            const float g = __fmul_rn(to_f32(grad[i]), gs);
+            const float x = direction(a, mom != nullptr, g, mom ? mom[i] : 0.f) * inv;
+            const long long r = i / a.cols, at = r * a.ld + (i - r * a.cols);
+            const __half h = __float2half_rn(x);
+            hi[at] = h;
+            lo[at] = __float2half_rn(x - __half2float(h));
+        }
+    }
+}
+
+// Behind the iteration: the result, or the weights' update.
+template <typename P, bool MASTER, bool STEP, bool WIDE>
+__global__ void __launch_bounds__(EL_THREADS) finish_kernel(const __grid_constant__ ElemArgs a) {
+    grid_launch_dependents();
+    grid_dependency_wait();
+    int z;
+    const Stack& st = find_stack(a, a.begin + blockIdx.y, &z);
+    const long long size = (long long)a.rows * a.cols, base = (long long)z * size;
+    float gs;
+    if (!scale_of(a.grad_scale, &gs)) return;
+    P* out = static_cast<P*>(st.param) + base;
+    float* master = MASTER ? st.master + base : nullptr;
+    const __half* hi = a.hi + (size_t)blockIdx.y * a.plane;
+    const __half* lo = a.lo + (size_t)blockIdx.y * a.plane;
+    const float lr = a.lr_now ? *a.lr_now : a.lr;
+    const float keep = 1.f - lr * st.decay, rate = lr * st.scale * (1.f / SCALE);
+    const long long p0 = (long long)blockIdx.x * PIECE, p1 = min(size, p0 + PIECE);
+    if (WIDE) {
+#pragma unroll 2
+        for (long long i = p0 + threadIdx.x * 8; i < p1; i += EL_THREADS * 8) {
+            const uint4 h = *reinterpret_cast<const uint4*>(hi + i), l = *reinterpret_cast<const uint4*>(lo + i);
+            const __half2* hp = reinterpret_cast<const __half2*>(&h);
+            const __half2* lp = reinterpret_cast<const __half2*>(&l);
+            float w[8], o[8];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float2 f = __half22float2(hp[k]), e = __half22float2(lp[k]);
+                o[2 * k] = f.x + e.x;
+                o[2 * k + 1] = f.y + e.y;
+            }
+            if (STEP) {
+                if (MASTER) load8(master + i, w);
+                else load8(out + i, w);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[k] = w[k] * keep - rate * o[k];
+                if (MASTER) store8(master + i, w);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[k] = o[k] * (1.f / SCALE);
+            }
+            store8(out + i, w);
+        }
+    } else {
+        for (long long i = p0 + threadIdx.x; i < p1; i += EL_THREADS) {
+            const long long r = i / a.cols, at = r * a.ld + (i - r * a.cols);
+            const float o = __half2float(hi[at]) + __half2float(lo[at]);
+            float w = o * (1.f / SCALE);
+            if (STEP) {
+                w = (MASTER ? master[i] : to_f32(out[i])) * keep - rate * o;
+                if (MASTER) master[i] = w;
+            }
+            out[i] = from_f32<P>(w);
+        }
+    }
+}
+
+// ---- host side ------------------------------------------------------------------------------------
+constexpr int MAX_STEPS = 16;
+constexpr int MAX_SIDE = 16384;
+constexpr size_t CHUNK_BYTES = 512u << 20;          // planes of a chunk, unless one matrix needs more
+
+struct Coefs {
+    int steps;
+    float c[MAX_STEPS][3];
+};
+// The iteration's coefficients, if fp16 can hold its iterates: from singular values in [0, 1] on, X stays
+// within 16 and b A + c A^2 within 60 (a bound on the norm bounds every element).
+static bool read_coefs(int32_t steps, const double* given, Coefs* out) {
+    if (steps < 1 || steps > MAX_STEPS) return false;
+    out->steps = steps;
+    double top = 1.0;
+    for (int k = 0; k < steps; ++k) {
+        const double a = given ? given[3 * k] : 3.4445, b = given ? given[3 * k + 1] : -4.7750,
+                     c = given ? given[3 * k + 2] : 2.0315;
+        out->c[k][0] = (float)a;
+        out->c[k][1] = (float)b;
+        out->c[k][2] = (float)c;
+        if (!given) continue;
+        if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
+        double next = 0.0, poly = 0.0;
+        for (int i = 0; i <= 256; ++i) {
+            const double s = top * i / 256, t = s * s, p = b * t + c * t * t;
+            next = std::fmax(next, std::fabs(s * (a + p)));
+            poly = std::fmax(poly, std::fabs(p));
+        }
+        if (!(next <= 16.0) || !(poly <= 60.0) || !(top * top <= 60.0)) return false;
+        top = next;
+    }
+    return true;
+}
+
+struct Problem {                                     // matrices of one shape
+    int rows, cols, m, ld, ldm, terms;
+    bool tall;
+    int pieces;
+};
+static Problem problem_of(int rows, int cols, int terms) {
+    Problem p;
+    p.rows = rows;
+    p.cols = cols;
+    p.tall = rows > cols;
+    p.m = rows < cols ? rows : cols;
+    p.ld = (int)round_up((size_t)cols, 8);
+    p.ldm = (int)round_up((size_t)p.m, 8);
+    p.terms = terms;
+    p.pieces = (int)(((long long)rows * cols + PIECE - 1) / PIECE);
+    return p;
+}
+// Bytes of `count` matrices in the workspace: X twice, A and B, sums.
+struct Layout {
+    size_t hi[2], lo[2], a[2], b[2], norms, total;
+};
+static Layout layout(const Problem& p, long long count) {
+    Layout w;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += round_up(bytes, 256);
+        return here;
+    };
+    const size_t x = (size_t)count * p.rows * p.ld * 2, s = (size_t)count * p.m * p.ldm * 2;
+    w.hi[0] = take(x);
+    w.hi[1] = take(x);
+    w.lo[0] = take(x);
+    w.lo[1] = p.terms > 1 ? take(x) : w.lo[0];       // not an operand: a tile replaces its own
+    w.a[0] = take(s);
+    w.a[1] = p.terms > 1 ? take(s) : w.a[0];
+    w.b[0] = take(s);
+    w.b[1] = p.terms > 1 ? take(s) : w.b[0];
+    w.norms = take((size_t)count * p.pieces * sizeof(double));
+    w.total = at;
+    return w;
+}
+static int chunk_of(const Problem& p, long long count) {
+    const size_t one = layout(p, 1).total;
+    long long n = (long long)(CHUNK_BYTES / one);
+    if (n < 1) n = 1;
+    if (n > 32768) n = 32768;
+    return (int)(n < count ? n : count);
+}
+
+// fp16 tensor [count, rows, cols] with row stride ld.
+static bool make_map(CUtensorMap* m, const void* ptr, int count, int rows, int cols, int ld, int box_cols,
+                     int box_rows, bool swizzle) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)count};
+    cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * rows * 2};
+    cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1};
+    cuuint32_t es[3] = {1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, es,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// CTA pairs of a kernel that can be resident at once (one CTA per SM), asked once per kernel and device.
+static int resident_pairs(void (*kern)(GemmArgs), int (&cached)[64]) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    if (cached[dev] == 0) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES) != cudaSuccess)
+            return 0;
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 2;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cfg.gridDim = dim3(2 * (sm_count() / 2));
+        cfg.blockDim = dim3(THREADS);
+        cfg.dynamicSmemBytes = SMEM_BYTES;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n <= 0) return 0;
+        cached[dev] = n < sm_count() / 2 ? n : sm_count() / 2;
+    }
+    return cached[dev];
+}
+
+template <bool A_MN, bool B_MN, bool SYM, int IN, int OUT, int TERMS>
+static r3_status launch_gemm(const GemmArgs& g, cudaStream_t cs) {
+    auto kern = gemm_kernel<A_MN, B_MN, SYM, IN, OUT, TERMS>;
+    static int cached[64] = {0};
+    const int pairs = resident_pairs(kern, cached);
+    if (pairs <= 0) return R3_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3(2 * (g.items < pairs ? g.items : pairs));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = SMEM_BYTES;
+    cfg.stream = cs;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kern, g) == cudaSuccess ? R3_OK : R3_ERR_CUDA;
+}
+
+// The iteration on `count` matrices whose X stands in the planes 0; on return *at says which planes hold the
+// result.
+template <int TERMS>
+static r3_status iterate(const Problem& p, const Coefs& coefs, int count, uint8_t* ws, int32_t* dev_status,
+                         int* at, cudaStream_t cs) {
+    const Layout w = layout(p, count);
+    constexpr int PL = TERMS > 1 ? 2 : 1;            // planes of A and B
+    GemmArgs gram[2], poly, apply[2];                // by the planes that hold X
+    const int tm = (p.m + TILE - 1) / TILE, tr = (p.rows + TILE - 1) / TILE, tc_ = (p.cols + TILE - 1) / TILE;
+    bool ok = true;
+    // an operand with consecutive k: 64 x 128 boxes; with k along the rows: 64 x 64, two per stage
+    for (int k = 0; k < 2; ++k) {
+        for (int pl = 0; pl < 2; ++pl) {
+            const uint8_t* x = ws + (pl ? w.lo[k] : w.hi[k]);
+            const uint8_t* y = ws + (pl ? w.lo[k ^ 1] : w.hi[k ^ 1]);
+            const uint8_t* A = ws + w.a[pl];
+            const uint8_t* B = ws + w.b[pl];
+            CUtensorMap xk, xmn, bk;
+            ok = ok && make_map(&xk, x, count, p.rows, p.cols, p.ld, 64, BM, true) &&
+                 make_map(&xmn, x, count, p.rows, p.cols, p.ld, 64, BK, true) &&
+                 make_map(&bk, B, count, p.m, p.m, p.ldm, 64, BM, true);
+            gram[k].a[pl] = gram[k].b[pl] = p.tall ? xmn : xk;
+            ok = ok && make_map(&gram[k].out[pl], A, count, p.m, p.m, p.ldm, 64, 32, true) &&
+                 make_map(&gram[k].mirror[pl], A, count, p.m, p.m, p.ldm, 32, 64, false);
+            gram[k].in[pl] = gram[k].out[pl];
+            apply[k].a[pl] = p.tall ? xk : bk;
+            apply[k].b[pl] = p.tall ? bk : xmn;
+            ok = ok && make_map(&apply[k].in[pl], x, count, p.rows, p.cols, p.ld, 64, 32, true) &&
+                 make_map(&apply[k].out[pl], y, count, p.rows, p.cols, p.ld, 64, 32, true);
+            apply[k].mirror[pl] = apply[k].out[pl];
+            if (k == 0) {
+                ok = ok && make_map(&poly.a[pl], A, count, p.m, p.m, p.ldm, 64, BM, true) &&
+                     make_map(&poly.out[pl], B, count, p.m, p.m, p.ldm, 64, 32, true) &&
+                     make_map(&poly.mirror[pl], B, count, p.m, p.m, p.ldm, 32, 64, false);
+                poly.b[pl] = poly.a[pl];
+                poly.in[pl] = gram[k].out[pl];
+            }
+        }
+        gram[k].rows = gram[k].cols = p.m;
+        gram[k].tiles_n = tm;
+        gram[k].tiles = tm * (tm + 1) / 2;
+        gram[k].kblocks = ((p.tall ? p.rows : p.cols) + BK - 1) / BK;
+        gram[k].alpha = 1.f / SCALE;
+        gram[k].beta = 0.f;
+        apply[k].rows = p.rows;
+        apply[k].cols = p.cols;
+        apply[k].tiles_n = tc_;
+        apply[k].tiles = tr * tc_;
+        apply[k].kblocks = (p.m + BK - 1) / BK;
+        apply[k].alpha = 1.f / SCALE;
+    }
+    if (!ok) return R3_ERR_CUDA;
+    poly.rows = poly.cols = p.m;
+    poly.tiles_n = tm;
+    poly.tiles = tm * (tm + 1) / 2;
+    poly.kblocks = (p.m + BK - 1) / BK;
+    poly.items = gram[0].items = gram[1].items = poly.tiles * count;
+    apply[0].items = apply[1].items = apply[0].tiles * count;
+    poly.dev_status = gram[0].dev_status = gram[1].dev_status = dev_status;
+    apply[0].dev_status = apply[1].dev_status = dev_status;
+    int k = 0;
+    for (int step = 0; step < coefs.steps; ++step, k ^= 1) {
+        poly.beta = coefs.c[step][1];
+        poly.alpha = coefs.c[step][2] / SCALE;
+        apply[k].beta = coefs.c[step][0];
+        r3_status st = p.tall ? launch_gemm<true, true, true, 0, PL, TERMS>(gram[k], cs)
+                              : launch_gemm<false, false, true, 0, PL, TERMS>(gram[k], cs);
+        if (st == R3_OK) st = launch_gemm<false, false, true, PL, PL, TERMS>(poly, cs);
+        if (st == R3_OK)
+            st = p.tall ? launch_gemm<false, false, false, 2, 2, TERMS>(apply[k], cs)
+                        : launch_gemm<false, true, false, 2, 2, TERMS>(apply[k], cs);
+        if (st != R3_OK) return st;
+    }
+    *at = k;
+    return R3_OK;
+}
+
+struct Job {
+    int param_dtype, grad_dtype, nesterov, terms;
+    bool master, step;
+    float momentum, eps, lr;
+    const float *grad_scale, *lr_now;
+};
+template <typename G, bool WIDE>
+static cudaError_t launch_front(const ElemArgs& a, dim3 grid, cudaStream_t cs) {
+    const cudaError_t e = launch_dependent(norm_kernel<G, WIDE>, grid, dim3(EL_THREADS), 0, cs, a);
+    return e == cudaSuccess ? launch_dependent(start_kernel<G, WIDE>, grid, dim3(EL_THREADS), 0, cs, a) : e;
+}
+template <typename P, bool MASTER, bool STEP>
+static cudaError_t launch_finish(const ElemArgs& a, bool wide, dim3 grid, cudaStream_t cs) {
+    return wide ? launch_dependent(finish_kernel<P, MASTER, STEP, true>, grid, dim3(EL_THREADS), 0, cs, a)
+                : launch_dependent(finish_kernel<P, MASTER, STEP, false>, grid, dim3(EL_THREADS), 0, cs, a);
+}
+
+// The stacks of one shape that stand in `a`, `count` matrices together.
+static r3_status run_group(const Job& job, const Coefs& coefs, const Problem& p, ElemArgs& a, int count,
+                           uint8_t* ws, int32_t* dev_status, cudaStream_t cs) {
+    const int chunk = chunk_of(p, count);
+    a.rows = p.rows;
+    a.cols = p.cols;
+    a.ld = p.ld;
+    a.pieces = p.pieces;
+    a.plane = (long long)p.rows * p.ld;
+    a.nesterov = job.nesterov;
+    a.momentum = job.momentum;
+    a.eps = job.eps;
+    a.lr = job.lr;
+    a.grad_scale = job.grad_scale;
+    a.lr_now = job.lr_now;
+    const bool wide = p.cols % 8 == 0;
+    for (int begin = 0; begin < count; begin += chunk) {
+        const int n = count - begin < chunk ? count - begin : chunk;
+        const Layout w = layout(p, n);
+        a.begin = begin;
+        a.hi = reinterpret_cast<__half*>(ws + w.hi[0]);
+        a.lo = reinterpret_cast<__half*>(ws + w.lo[0]);
+        a.norms = reinterpret_cast<double*>(ws + w.norms);
+        const dim3 grid(p.pieces, n);
+        cudaError_t e;
+        if (job.grad_dtype == R3_BF16)
+            e = wide ? launch_front<__nv_bfloat16, true>(a, grid, cs) : launch_front<__nv_bfloat16, false>(a, grid, cs);
+        else
+            e = wide ? launch_front<float, true>(a, grid, cs) : launch_front<float, false>(a, grid, cs);
+        if (e != cudaSuccess) return R3_ERR_CUDA;
+        int at = 0;
+        const r3_status st = job.terms > 1 ? iterate<3>(p, coefs, n, ws, dev_status, &at, cs)
+                                           : iterate<1>(p, coefs, n, ws, dev_status, &at, cs);
+        if (st != R3_OK) return st;
+        a.hi = reinterpret_cast<__half*>(ws + w.hi[at]);
+        a.lo = reinterpret_cast<__half*>(ws + w.lo[at]);
+        if (!job.step)
+            e = job.param_dtype == R3_BF16 ? launch_finish<__nv_bfloat16, false, false>(a, wide, grid, cs)
+                                           : launch_finish<float, false, false>(a, wide, grid, cs);
+        else if (job.param_dtype == R3_F32)
+            e = launch_finish<float, false, true>(a, wide, grid, cs);
+        else
+            e = job.master ? launch_finish<__nv_bfloat16, true, true>(a, wide, grid, cs)
+                           : launch_finish<__nv_bfloat16, false, true>(a, wide, grid, cs);
+        if (e != cudaSuccess) return R3_ERR_CUDA;
+    }
+    return R3_OK;
+}
+
+static bool good_shape(int64_t batch, int64_t rows, int64_t cols) {
+    return batch >= 0 && batch <= (1 << 24) && rows >= 1 && rows <= MAX_SIDE && cols >= 1 && cols <= MAX_SIDE;
+}
+static bool good_type(int t) { return t == R3_F32 || t == R3_BF16; }
+
+static r3_status check_ortho(const r3_orthogonal* c, Coefs* coefs) {
+    if (!c || !good_shape(c->batch, c->rows, c->cols) || !good_type(c->in_dtype) || !good_type(c->out_dtype))
+        return R3_ERR_INVALID_ARG;
+    if ((c->products != 1 && c->products != 3) || !(c->eps >= 0.0 && c->eps < 1e30)) return R3_ERR_INVALID_ARG;
+    return read_coefs(c->steps, c->coefs, coefs) ? R3_OK : R3_ERR_INVALID_ARG;
+}
+static r3_status check_muon(const r3_muon* c, const r3_muon_stack* ss, int32_t count, Coefs* coefs) {
+    if (!c || count < 0 || (count > 0 && !ss)) return R3_ERR_INVALID_ARG;
+    if (!good_type(c->param_dtype) || !good_type(c->grad_dtype) || (c->products != 1 && c->products != 3))
+        return R3_ERR_INVALID_ARG;
+    if (c->master && c->param_dtype != R3_BF16) return R3_ERR_INVALID_ARG;
+    if (!(c->lr >= 0.0 && c->lr < 1e30) || !(c->momentum >= 0.0 && c->momentum < 1.0) ||
+        !(c->eps >= 0.0 && c->eps < 1e30))
+        return R3_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < count; ++i) {
+        const r3_muon_stack& s = ss[i];
+        if (!good_shape(s.batch, s.rows, s.cols) || !(s.weight_decay >= 0.f && s.weight_decay < 1e30f) ||
+            !(s.scale >= 0.f && s.scale < 1e30f))
+            return R3_ERR_INVALID_ARG;
+    }
+    return read_coefs(c->steps, c->coefs, coefs) ? R3_OK : R3_ERR_INVALID_ARG;
+}
+static r3_status check_buffers(const r3_muon* c, const r3_muon_stack* ss, int32_t count) {
+    for (int32_t i = 0; i < count; ++i) {
+        const r3_muon_stack& s = ss[i];
+        if (s.batch == 0) continue;
+        if (!s.param || !s.grad || !s.momentum || (c->master != 0) != (s.master != nullptr))
+            return R3_ERR_INVALID_ARG;
+        const void* ps[] = {s.param, s.master, s.grad, s.momentum};
+        for (const void* p : ps)
+            if (!aligned(p, 16)) return R3_ERR_INVALID_ARG;
+    }
+    return R3_OK;
+}
+
+// Two buffers on the same memory would be updated at once, in no order, and what is read there would change
+// under the step.
+static bool distinct(const r3_muon* c, const r3_muon_stack* ss, int32_t count, const float* grad_scale,
+                     const float* lr) {
+    struct Range {
+        uintptr_t begin, end;
+        bool written;
+    };
+    std::vector<Range> all;
+    all.reserve((size_t)count * 4 + 2);
+    auto add = [&](const void* p, size_t bytes, bool written) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        if (p) all.push_back({at, at + bytes, written});
+    };
+    for (int32_t i = 0; i < count; ++i) {
+        const r3_muon_stack& s = ss[i];
+        const size_t n = (size_t)s.batch * s.rows * s.cols;
+        if (n == 0) continue;
+        add(s.param, n * (c->param_dtype == R3_BF16 ? 2 : 4), true);
+        add(s.master, n * 4, true);
+        add(s.momentum, n * 4, true);
+        add(s.grad, n * (c->grad_dtype == R3_BF16 ? 2 : 4), false);
+    }
+    add(grad_scale, 4, false);
+    add(lr, 4, false);
+    std::sort(all.begin(), all.end(), [](const Range& x, const Range& y) { return x.begin < y.begin; });
+    uintptr_t past = 0, past_written = 0;
+    for (const Range& r : all) {
+        if (r.begin < (r.written ? past : past_written)) return false;
+        past = std::max(past, r.end);
+        if (r.written) past_written = std::max(past_written, r.end);
+    }
+    return true;
+}
+
+// Calls f(members, n, matrices) for each group: stacks of one shape, in their order, MAX_STACKS at most.
+template <typename F> static r3_status each_group(const r3_muon_stack* ss, int32_t count, F f) {
+    std::vector<int32_t> order;
+    for (int32_t i = 0; i < count; ++i)
+        if (ss[i].batch > 0) order.push_back(i);
+    auto shape = [&](int32_t i) { return (uint64_t)ss[i].rows << 32 | (uint32_t)ss[i].cols; };
+    std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) { return shape(x) < shape(y); });
+    for (size_t i = 0; i < order.size();) {
+        size_t end = i;
+        long long matrices = 0;
+        for (; end < order.size() && end < i + MAX_STACKS && shape(order[end]) == shape(order[i]) &&
+               matrices + ss[order[end]].batch <= 0x7fffffffLL; ++end)
+            matrices += ss[order[end]].batch;
+        const r3_status st = f(order.data() + i, (int)(end - i), (int)matrices);
+        if (st != R3_OK) return st;
+        i = end;
+    }
+    return R3_OK;
+}
+
+}  // namespace ns
+}  // namespace r3
+
+extern "C" size_t r3_orthogonalize_workspace_bytes(const r3_orthogonal* c) {
+    using namespace r3::ns;
+    Coefs coefs;
+    if (check_ortho(c, &coefs) != R3_OK || c->batch == 0) return 0;
+    const Problem p = problem_of(c->rows, c->cols, c->products);
+    return layout(p, chunk_of(p, c->batch)).total;
+}
+
+extern "C" r3_status r3_orthogonalize(const r3_orthogonal* c, const void* x, void* out, void* workspace,
+                                      size_t ws_bytes, int32_t* dev_status, void* stream) {
+    using namespace r3;
+    using namespace r3::ns;
+    Coefs coefs;
+    const r3_status st = check_ortho(c, &coefs);
+    if (st != R3_OK) return st;
+    if (c->batch == 0) return R3_OK;
+    if (!x || !out || !aligned(x, 16) || !aligned(out, 16) || !aligned(dev_status, 4)) return R3_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256) || ws_bytes < r3_orthogonalize_workspace_bytes(c))
+        return R3_ERR_WORKSPACE;
+    ElemArgs a = {};
+    a.stacks = 1;
+    a.stack[0] = {out, nullptr, x, nullptr, 0, 0.f, 0.f};
+    const Job job = {c->out_dtype, c->in_dtype, 0, c->products, false, false, 0.f, (float)c->eps, 0.f, nullptr,
+                     nullptr};
+    return run_group(job, coefs, problem_of(c->rows, c->cols, c->products), a, c->batch,
+                     static_cast<uint8_t*>(workspace), dev_status, static_cast<cudaStream_t>(stream));
+}
+
+// (host memory may run out: nothing of that leaves a C entry)
+extern "C" size_t r3_muon_workspace_bytes(const r3_muon* c, const r3_muon_stack* stacks, int32_t n_stacks) {
+    using namespace r3::ns;
+    Coefs coefs;
+    if (check_muon(c, stacks, n_stacks, &coefs) != R3_OK) return 0;
+    size_t most = 0;
+    try {
+        each_group(stacks, n_stacks, [&](const int32_t* members, int, int matrices) {
+            const r3_muon_stack& s = stacks[members[0]];
+            const Problem p = problem_of(s.rows, s.cols, c->products);
+            most = std::max(most, layout(p, chunk_of(p, matrices)).total);
+            return R3_OK;
+        });
+    } catch (...) {
+        return 0;
+    }
+    return most;
+}
+
+extern "C" r3_status r3_muon_step(const r3_muon* c, const r3_muon_stack* stacks, int32_t n_stacks,
+                                  const float* grad_scale, const float* lr, void* workspace, size_t ws_bytes,
+                                  int32_t* dev_status, void* stream) {
+    using namespace r3;
+    using namespace r3::ns;
+    Coefs coefs;
+    r3_status st = check_muon(c, stacks, n_stacks, &coefs);
+    if (st == R3_OK) st = check_buffers(c, stacks, n_stacks);
+    if (st != R3_OK) return st;
+    if (!aligned(grad_scale, 4) || !aligned(lr, 4) || !aligned(dev_status, 4)) return R3_ERR_INVALID_ARG;
+    try {
+        if (!distinct(c, stacks, n_stacks, grad_scale, lr)) return R3_ERR_INVALID_ARG;
+        const size_t need = r3_muon_workspace_bytes(c, stacks, n_stacks);
+        if (need == 0) return R3_OK;                   // no matrices
+        if (!workspace || !aligned(workspace, 256) || ws_bytes < need) return R3_ERR_WORKSPACE;
+        const Job job = {c->param_dtype, c->grad_dtype, c->nesterov != 0, c->products, c->master != 0, true,
+                         (float)c->momentum, (float)c->eps, (float)c->lr, grad_scale, lr};
+        return each_group(stacks, n_stacks, [&](const int32_t* members, int n, int matrices) {
+            ElemArgs a = {};
+            a.stacks = n;
+            int first = 0;
+            for (int i = 0; i < n; ++i) {
+                const r3_muon_stack& s = stacks[members[i]];
+                a.stack[i] = {s.param, s.master, s.grad, s.momentum, first, s.weight_decay, s.scale};
+                first += s.batch;
+            }
+            const r3_muon_stack& s = stacks[members[0]];
+            return run_group(job, coefs, problem_of(s.rows, s.cols, c->products), a, matrices,
+                             static_cast<uint8_t*>(workspace), dev_status, static_cast<cudaStream_t>(stream));
+        });
+    } catch (...) {
+        return R3_ERR_INVALID_ARG;
+    }
+}

@@ -44,7 +44,8 @@ EXPORTS = [
     "r3_replay_layer_host_workspace_bytes", "r3_replay_layer_host", "r3_replay_layer_host_enqueue",
     "r3_replay_layer_host_chunks",
     "r3_replay_layer_same_record",
-    "r3_adamw_step", "r3_normed_stack_workspace_bytes", "r3_normed_stack",
+    "r3_adamw_step", "r3_orthogonalize_workspace_bytes", "r3_orthogonalize",
+    "r3_muon_workspace_bytes", "r3_muon_step", "r3_normed_stack_workspace_bytes", "r3_normed_stack",
     "r3_normed_stack_train_workspace_bytes", "r3_normed_stack_train",
     "r3_norm_residual", "r3_norm_residual_bwd_workspace_bytes", "r3_norm_residual_bwd",
     "r3_token_logprobs", "r3_token_logprobs_bwd",
@@ -102,6 +103,25 @@ class AdamWConfig(ctypes.Structure):
                 ("master", ctypes.c_int32), ("state_bits", ctypes.c_int32), ("step", ctypes.c_int64),
                 ("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
                 ("eps", ctypes.c_double)]
+
+
+class Orthogonal(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32),
+                ("in_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("steps", ctypes.c_int32),
+                ("products", ctypes.c_int32), ("eps", ctypes.c_double), ("coefs", ctypes.c_void_p)]
+
+
+class MuonStack(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("master", ctypes.c_void_p), ("grad", ctypes.c_void_p),
+                ("momentum", ctypes.c_void_p), ("batch", ctypes.c_int32), ("rows", ctypes.c_int32),
+                ("cols", ctypes.c_int32), ("weight_decay", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+class MuonConfig(ctypes.Structure):
+    _fields_ = [("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("master", ctypes.c_int32),
+                ("nesterov", ctypes.c_int32), ("steps", ctypes.c_int32), ("products", ctypes.c_int32),
+                ("lr", ctypes.c_double), ("momentum", ctypes.c_double), ("eps", ctypes.c_double),
+                ("coefs", ctypes.c_void_p)]
 
 
 class Policy(ctypes.Structure):
@@ -176,6 +196,13 @@ lib.r3_normed_stack_train_workspace_bytes.argtypes = [_SP, ctypes.c_int32]
 lib.r3_normed_stack_train.argtypes = ([_SP, ctypes.c_int32, _BN] + [_P] * 19
                                       + [ctypes.c_size_t, _P, _P])
 lib.r3_adamw_step.argtypes = [ctypes.POINTER(AdamWConfig), _P, ctypes.c_int32, _P, _P, _P]
+lib.r3_orthogonalize_workspace_bytes.restype = ctypes.c_size_t
+lib.r3_orthogonalize_workspace_bytes.argtypes = [ctypes.POINTER(Orthogonal)]
+lib.r3_orthogonalize.argtypes = [ctypes.POINTER(Orthogonal), _P, _P, _P, ctypes.c_size_t, _P, _P]
+lib.r3_muon_workspace_bytes.restype = ctypes.c_size_t
+lib.r3_muon_workspace_bytes.argtypes = [ctypes.POINTER(MuonConfig), _P, ctypes.c_int32]
+lib.r3_muon_step.argtypes = [ctypes.POINTER(MuonConfig), _P, ctypes.c_int32, _P, _P, _P, ctypes.c_size_t, _P,
+                             _P]
 _NP = ctypes.POINTER(Norm)
 lib.r3_norm_residual.argtypes = [_NP] + [_P] * 8
 lib.r3_norm_residual_bwd_workspace_bytes.restype = ctypes.c_size_t
@@ -945,6 +972,170 @@ class AdamW:
                                  _arg("grad_scale", grad_scale, (1,), torch.float32, self._dev),
                                  _arg("scalars", scalars, (3,), torch.float32, self._dev),
                                  _stream(stream)))
+
+
+def _coefficients(steps, coefficients):
+    """(steps, the ctypes array of their a, b, c or None for the usual ones)."""
+    if coefficients is None:
+        return int(steps), None
+    rows = [tuple(map(float, c)) for c in
+            ([coefficients] * int(steps) if not hasattr(coefficients[0], "__len__") else coefficients)]
+    if any(len(c) != 3 for c in rows) or (steps != len(rows)):
+        raise ValueError(f"coefficients: expected (a, b, c), or one such triple for each of {steps} steps")
+    return len(rows), (ctypes.c_double * (3 * len(rows)))(*[v for c in rows for v in c])
+
+
+def _products(products, exact):
+    if products is None:
+        return 3 if exact else 1
+    if products not in (1, 3):
+        raise ValueError(f"products: {products}, expected 1 or 3")
+    return products
+
+
+@_in_order
+def orthogonalize(x, out=None, *, out_dtype=None, steps=5, coefficients=None, eps=1e-7, products=None, ws=None,
+                  dev_status=None, stream=None):
+    """Newton-Schulz iteration that brings singular values near one (r3_orthogonalize): x [rows, cols] or
+    [B, rows, cols], float32 or bfloat16; out of x's type or out_dtype (may be x).  coefficients: (a, b, c) or one
+    triple per step.  products: fp16 products that stand for one, 1 or 3; by default 3 where out is float32."""
+    dev = _device_of("x", x)
+    if x.dtype not in _ACT:
+        raise ValueError(f"x: dtype {x.dtype}, expected float32 or bfloat16")
+    if x.dim() not in (2, 3):
+        raise ValueError("x: expected [rows, cols] or [B, rows, cols]")
+    if out is None:
+        out_dtype = x.dtype if out_dtype is None else out_dtype
+        if out_dtype not in _ACT:
+            raise ValueError(f"out_dtype: {out_dtype}, expected float32 or bfloat16")
+        out = torch.empty(x.shape, dtype=out_dtype, device=dev)
+    else:
+        _expect("out", out, x.shape, tuple(_ACT) if out_dtype is None else out_dtype, dev)
+    if 0 in x.shape:
+        return out
+    B, (rows, cols) = (x.shape[0] if x.dim() == 3 else 1), x.shape[-2:]
+    steps, coefs = _coefficients(steps, coefficients)
+    c = Orthogonal(B, rows, cols, _ACT[x.dtype], _ACT[out.dtype], steps,
+                   _products(products, out.dtype == torch.float32), eps,
+                   None if coefs is None else ctypes.addressof(coefs))
+    ws = _scratch(ws, lib.r3_orthogonalize_workspace_bytes(ctypes.byref(c)), dev)
+    _check(lib.r3_orthogonalize(ctypes.byref(c), _ptr(x), _ptr(out), ws.data_ptr(), ws.numel(),
+                                None if dev_status is None else _ptr(dev_status), _stream(stream)))
+    return out
+
+
+class Muon:
+    """Momentum with orthogonalised updates over stacks of matrices (r3_muon_step): the handle that a training
+    program keeps beside the matrices among its parameters (AdamW takes the others).
+
+    params, grads: lists of contiguous CUDA tensors [rows, cols] or [..., rows, cols] (expert weights [E, F, d]
+    are E matrices), one dtype each (float32 or bfloat16).  masters: None, True (float32 copies of bfloat16
+    params are made and kept) or a list of float32 tensors.  momentum_buffers: float32, made (zero, on the
+    current stream) or given.  weight_decay: a number, or one per tensor.  scale multiplies the update:
+    "spectral" = sqrt(max(1, rows / cols)), "rms" = 0.2 sqrt(max(rows, cols)) (about AdamW's root mean square),
+    a number, or one of these per tensor.  products: 1 or 3 fp16 products for each of the iteration's; by default 3
+    where the weights or their masters are float32.  The handle keeps its tensors' memory alive, and a
+    workspace (up to about 512 MB) that its steps share; set_grads() exchanges the gradients."""
+
+    def __init__(self, params, grads=None, *, masters=None, momentum_buffers=None, momentum=0.95,
+                 nesterov=True, weight_decay=0.0, scale="spectral", steps=5, coefficients=None, eps=1e-7,
+                 products=None):
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("Muon: no tensors")
+        self._dev = _device_of("params[0]", self.params[0])
+        dtype = self.params[0].dtype
+        if dtype not in _ACT:
+            raise ValueError(f"params: dtype {dtype}, expected float32 or bfloat16")
+        for i, p in enumerate(self.params):
+            if not isinstance(p, torch.Tensor):
+                raise TypeError(f"params[{i}]: expected a torch.Tensor")
+            if p.dim() < 2:
+                raise ValueError(f"params[{i}]: expected [..., rows, cols]")
+        if masters is True:
+            masters = [p.detach().float() for p in self.params]
+        self.masters = list(masters) if masters is not None else None
+        if self.masters is not None and dtype != torch.bfloat16:
+            raise ValueError("masters: only for bfloat16 params")
+        if momentum_buffers is None:
+            momentum_buffers = [torch.zeros(p.shape, dtype=torch.float32, device=self._dev)
+                                for p in self.params]
+        self.momentum_buffers = list(momentum_buffers)
+        n = len(self.params)
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
+        scales = list(scale) if isinstance(scale, (list, tuple)) else [scale] * n
+        for name, given in (("weight_decay", decay), ("scale", scales)):
+            if len(given) != n:
+                raise ValueError(f"{name}: {len(given)} values for {n} tensors")
+        self._table = (MuonStack * n)()
+        self._memory = []                        # what the table's addresses point to
+        self._fill("param", self.params, dtype)
+        if self.masters is not None:
+            self._fill("master", self.masters, torch.float32)
+        self._fill("momentum", self.momentum_buffers, torch.float32)
+        for row, p, wd, sc in zip(self._table, self.params, decay, scales):
+            rows, cols = p.shape[-2:]
+            row.rows, row.cols = max(rows, 1), max(cols, 1)
+            row.batch = p.numel() // (rows * cols) if p.numel() else 0
+            if isinstance(sc, str):
+                if sc not in ("spectral", "rms"):
+                    raise ValueError(f"scale: {sc!r}, expected 'spectral', 'rms' or a number")
+                sc = max(1.0, rows / max(cols, 1)) ** 0.5 if sc == "spectral" else 0.2 * max(rows, cols) ** 0.5
+            row.weight_decay, row.scale = wd, sc
+        steps, self._coefs = _coefficients(steps, coefficients)
+        self._config = MuonConfig(
+            _ACT[dtype], 0, int(self.masters is not None), int(nesterov), steps,
+            _products(products, dtype == torch.float32 or self.masters is not None), 0.0, float(momentum),
+            float(eps), None if self._coefs is None else ctypes.addressof(self._coefs))
+        self._ws = workspace(lib.r3_muon_workspace_bytes(ctypes.byref(self._config), self._table, n), self._dev)
+        self.grads = None
+        if grads is not None:
+            self.set_grads(grads)
+
+    def _addresses(self, field, tensors, dtype):
+        """The addresses of a list of tensors, every one of them checked."""
+        if len(tensors) != len(self.params):
+            raise ValueError(f"{field}: {len(tensors)} tensors for {len(self.params)} params")
+        for i, (t, p) in enumerate(zip(tensors, self.params)):
+            _expect(f"{field}[{i}]", t, p.shape, dtype, self._dev)
+            if t is None:
+                raise TypeError(f"{field}[{i}]: expected a torch.Tensor")
+        return [_ptr(t).value for t in tensors]
+
+    def _fill(self, field, tensors, dtype):
+        for row, at in zip(self._table, self._addresses(field, tensors, dtype)):
+            setattr(row, field, at)
+        self._memory += [t.detach() for t in tensors]
+
+    def set_grads(self, grads):
+        """Exchanges the gradients of the steps to come: all of them, or none where one is refused."""
+        grads = list(grads)
+        dtype = grads[0].dtype if grads and isinstance(grads[0], torch.Tensor) else None
+        if dtype not in _ACT:
+            raise ValueError(f"grads: dtype {dtype}, expected float32 or bfloat16")
+        for row, at in zip(self._table, self._addresses("grad", grads, dtype)):
+            row.grad = at
+        self._config.grad_dtype = _ACT[dtype]
+        self.grads = grads
+
+    def step(self, lr, *, grad_scale=None, lr_tensor=None, ws=None, dev_status=None, stream=None):
+        """One step.  grad_scale: [1] float32 on the device, multiplies every gradient; not finite = the step is
+        skipped.  lr_tensor: [1] float32 on the device, used instead of lr (for a captured step).  ws: a
+        workspace of the caller's instead of the handle's (steps of one handle that may run at once, on two
+        streams, are two steps on the same weights: not allowed either way)."""
+        if self._dev.index != torch.cuda.current_device():
+            raise ValueError(f"Muon: tensors on {self._dev}, which is not the current device")
+        if self.grads is None:
+            raise ValueError("Muon: no gradients (set_grads)")
+        self._config.lr = float(lr)
+        ws = _scratch(self._ws if ws is None else ws, 0, self._dev)
+        if stream is not None and ws is self._ws:
+            ws.record_stream(stream)
+        _check(lib.r3_muon_step(ctypes.byref(self._config), self._table, len(self.params),
+                                _arg("grad_scale", grad_scale, (1,), torch.float32, self._dev),
+                                _arg("lr_tensor", lr_tensor, (1,), torch.float32, self._dev),
+                                ws.data_ptr(), ws.numel(), None if dev_status is None else _ptr(dev_status),
+                                _stream(stream)))
 
 
 def _block_norms(s, L, w_pre, w_post, gate, eps, residual_scale, branch_scale, dev, grads):

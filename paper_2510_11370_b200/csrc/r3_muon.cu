@@ -16,22 +16,15 @@
 // buffered in tensor memory).  A and B are symmetric: only tiles on and below the diagonal are computed, the
 // others are stored from the same accumulators, transposed.  Eight epilogue warps, each with its own 8 KB of
 // shared memory: L comes and D goes by TMA in boxes of 32 rows x 64 columns.
-#include <cuda_fp16.h>
-
 #include <algorithm>
 #include <cmath>
 #include <vector>
 
-#include "r3_common.cuh"
-#include "r3_internal.h"
-#include "r3_tc.cuh"
+#include "r3_muon.cuh"
 
 namespace r3 {
 namespace ns {
 
-using namespace tc;
-
-constexpr float SCALE = 1024.f;           // every fp16 operand is its value times this
 constexpr int BM = 128;                   // rows of either operand per CTA and stage
 constexpr int TILE = 2 * BM;              // output tile of a CTA pair: TILE x TILE
 constexpr int BK = 64;                    // k per stage: 64 fp16 = one 128-byte swizzle row
@@ -65,9 +58,6 @@ __device__ __forceinline__ void bulk_wait_read() {
     asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
 }
 __device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-__device__ __forceinline__ void fence_async() {
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-}
 
 struct Tile {
     int z, m, n;                          // matrix, tile row and column
@@ -376,7 +366,6 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
 // ---- around the iteration: elementwise, a matrix in pieces of PIECE elements ----------------------
 constexpr int EL_THREADS = 256;
 constexpr int PIECE = EL_THREADS * 32;
-constexpr int MAX_STACKS = 64;            // per launch: the table travels in the kernel's parameters
 
 struct Stack {
     void* param;                          // or the result of an orthogonalisation
@@ -406,36 +395,6 @@ __device__ __forceinline__ const Stack& find_stack(const ElemArgs& a, int matrix
     *within = matrix - a.stack[i].first;
     return a.stack[i];
 }
-__device__ __forceinline__ bool scale_of(const float* grad_scale, float* s) {
-    *s = grad_scale ? *grad_scale : 1.f;
-    return isfinite(*s);
-}
-// Eight consecutive elements as float32.
-template <typename T> __device__ __forceinline__ void load8(const T* p, float (&f)[8]) {
-    constexpr int N = Vec16<T>::N;
-#pragma unroll
-    for (int i = 0; i < 8 / N; ++i) {
-        Vec16<T> v;
-        v.v = *reinterpret_cast<const decltype(v.v)*>(p + i * N);
-        v.unpack(f + i * N);
-    }
-}
-template <typename T> __device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
-    constexpr int N = Vec16<T>::N;
-#pragma unroll
-    for (int i = 0; i < 8 / N; ++i) {
-        Vec16<T> v;
-        v.pack(f + i * N);
-        *reinterpret_cast<decltype(v.v)*>(p + i * N) = v.v;
-    }
-}
-
-// u from the gradient and the momentum after this step; every product and sum is rounded by itself.
-__device__ __forceinline__ float direction(const ElemArgs& a, bool momentum, float g, float m) {
-    if (!momentum) return g;
-    return a.nesterov ? __fadd_rn(g, __fmul_rn(a.momentum, m)) : m;
-}
-
 // First pass: the momentum's update and the sum of u^2 of every piece.  grid (pieces, matrices)
 template <typename G, bool WIDE>
 __global__ void __launch_bounds__(EL_THREADS) norm_kernel(const __grid_constant__ ElemArgs a) {
@@ -466,7 +425,7 @@ __global__ void __launch_bounds__(EL_THREADS) norm_kernel(const __grid_constant_
                 }
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    const double u = (double)direction(a, mom != nullptr, __fmul_rn(g[k], gs), m[k]);
+                    const double u = (double)direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[k], gs), m[k]);
                     sum += u * u;
                 }
             }
@@ -478,7 +437,7 @@ __global__ void __launch_bounds__(EL_THREADS) norm_kernel(const __grid_constant_
                     m = __fadd_rn(__fmul_rn(a.momentum, mom[i]), g);
                     mom[i] = m;
                 }
-                const double u = (double)direction(a, mom != nullptr, g, m);
+                const double u = (double)direction(a.nesterov, a.momentum, mom != nullptr, g, m);
                 sum += u * u;
             }
         }
@@ -516,9 +475,7 @@ __global__ void __launch_bounds__(EL_THREADS) start_kernel(const __grid_constant
     sum = 0.0;
 #pragma unroll
     for (int i = 0; i < EL_THREADS / 32; ++i) sum += s_sum[i];
-    const double norm = sqrt(sum);
-    // a matrix of zeros stays one; anything not finite reaches every element
-    const float inv = norm == 0.0 ? 0.f : (float)((double)SCALE / (norm + (double)a.eps));
+    const float inv = start_scale(sum, a.eps);
     __half* hi = a.hi + (size_t)blockIdx.y * a.plane;
     __half* lo = a.lo + (size_t)blockIdx.y * a.plane;
     const long long p0 = (long long)blockIdx.x * PIECE, p1 = min(size, p0 + PIECE);
@@ -533,8 +490,8 @@ __global__ void __launch_bounds__(EL_THREADS) start_kernel(const __grid_constant
             __half2* lp = reinterpret_cast<__half2*>(&l);
 #pragma unroll
             for (int k = 0; k < 8; k += 2) {
-                const float x0 = direction(a, mom != nullptr, __fmul_rn(g[k], gs), m[k]) * inv;
-                const float x1 = direction(a, mom != nullptr, __fmul_rn(g[k + 1], gs), m[k + 1]) * inv;
+                const float x0 = direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[k], gs), m[k]) * inv;
+                const float x1 = direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[k + 1], gs), m[k + 1]) * inv;
                 hp[k / 2] = __floats2half2_rn(x0, x1);
                 const float2 f = __half22float2(hp[k / 2]);
                 lp[k / 2] = __floats2half2_rn(x0 - f.x, x1 - f.y);
@@ -545,7 +502,7 @@ __global__ void __launch_bounds__(EL_THREADS) start_kernel(const __grid_constant
     } else {
         for (long long i = p0 + threadIdx.x; i < p1; i += EL_THREADS) {
             const float g = __fmul_rn(to_f32(grad[i]), gs);
-            const float x = direction(a, mom != nullptr, g, mom ? mom[i] : 0.f) * inv;
+            const float x = direction(a.nesterov, a.momentum, mom != nullptr, g, mom ? mom[i] : 0.f) * inv;
             const long long r = i / a.cols, at = r * a.ld + (i - r * a.cols);
             const __half h = __float2half_rn(x);
             hi[at] = h;
@@ -611,8 +568,8 @@ __global__ void __launch_bounds__(EL_THREADS) finish_kernel(const __grid_constan
 }
 
 // ---- host side ------------------------------------------------------------------------------------
-constexpr int MAX_STEPS = 16;
 constexpr int MAX_SIDE = 16384;
+constexpr int MAX_BATCH = 1 << 24, MAX_MATRICES = 1 << 27;          // (times the CTAs of a cluster: a grid's limit)
 constexpr size_t CHUNK_BYTES = 512u << 20;          // planes of a chunk, unless one matrix needs more
 
 struct Coefs {
@@ -840,6 +797,32 @@ struct Job {
     float momentum, eps, lr;
     const float *grad_scale, *lr_now;
 };
+static r3_status run_group_small(const Job& job, const Coefs& coefs, const r3_muon_stack* const* ss, int n,
+                                 int cluster, int matrices, int32_t* dev_status, cudaStream_t cs) {
+    SmallArgs a = {};
+    a.stacks = n;
+    a.cluster = cluster;
+    a.steps = coefs.steps;
+    for (int k = 0; k < coefs.steps; ++k)
+        for (int j = 0; j < 3; ++j) a.coefs[k][j] = coefs.c[k][j];
+    a.grad_dtype = job.grad_dtype;
+    a.param_dtype = job.param_dtype;
+    a.step = job.step;
+    a.nesterov = job.nesterov;
+    a.momentum = job.momentum;
+    a.eps = job.eps;
+    a.lr = job.lr;
+    a.grad_scale = job.grad_scale;
+    a.lr_now = job.lr_now;
+    a.dev_status = dev_status;
+    int first = 0;
+    for (int i = 0; i < n; ++i) {
+        const r3_muon_stack& s = *ss[i];
+        a.stack[i] = {s.param, s.master, s.grad, s.momentum, first, s.rows, s.cols, s.weight_decay, s.scale};
+        first += s.batch;
+    }
+    return run_small(a, job.terms, matrices, cs);
+}
 template <typename G, bool WIDE>
 static cudaError_t launch_front(const ElemArgs& a, dim3 grid, cudaStream_t cs) {
     const cudaError_t e = launch_dependent(norm_kernel<G, WIDE>, grid, dim3(EL_THREADS), 0, cs, a);
@@ -901,7 +884,7 @@ static r3_status run_group(const Job& job, const Coefs& coefs, const Problem& p,
 }
 
 static bool good_shape(int64_t batch, int64_t rows, int64_t cols) {
-    return batch >= 0 && batch <= (1 << 24) && rows >= 1 && rows <= MAX_SIDE && cols >= 1 && cols <= MAX_SIDE;
+    return batch >= 0 && batch <= MAX_BATCH && rows >= 1 && rows <= MAX_SIDE && cols >= 1 && cols <= MAX_SIDE;
 }
 static bool good_type(int t) { return t == R3_F32 || t == R3_BF16; }
 
@@ -975,18 +958,23 @@ static bool distinct(const r3_muon* c, const r3_muon_stack* ss, int32_t count, c
     return true;
 }
 
-// Calls f(members, n, matrices) for each group: stacks of one shape, in their order, MAX_STACKS at most.
+// The shapes that one launch takes together: small ones by their CTAs per matrix, others each by itself.
+static uint64_t class_of(int rows, int cols) {
+    const int c = small_cluster(rows, cols);
+    return c ? (uint64_t)c : (uint64_t)rows << 32 | (uint32_t)cols;
+}
+// Calls f(members, n, matrices) for each group: stacks of one class, in their order, MAX_STACKS at most.
 template <typename F> static r3_status each_group(const r3_muon_stack* ss, int32_t count, F f) {
     std::vector<int32_t> order;
     for (int32_t i = 0; i < count; ++i)
         if (ss[i].batch > 0) order.push_back(i);
-    auto shape = [&](int32_t i) { return (uint64_t)ss[i].rows << 32 | (uint32_t)ss[i].cols; };
+    auto shape = [&](int32_t i) { return class_of(ss[i].rows, ss[i].cols); };
     std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) { return shape(x) < shape(y); });
     for (size_t i = 0; i < order.size();) {
         size_t end = i;
         long long matrices = 0;
         for (; end < order.size() && end < i + MAX_STACKS && shape(order[end]) == shape(order[i]) &&
-               matrices + ss[order[end]].batch <= 0x7fffffffLL; ++end)
+               matrices + ss[order[end]].batch <= MAX_MATRICES; ++end)
             matrices += ss[order[end]].batch;
         const r3_status st = f(order.data() + i, (int)(end - i), (int)matrices);
         if (st != R3_OK) return st;
@@ -1002,6 +990,7 @@ extern "C" size_t r3_orthogonalize_workspace_bytes(const r3_orthogonal* c) {
     using namespace r3::ns;
     Coefs coefs;
     if (check_ortho(c, &coefs) != R3_OK || c->batch == 0) return 0;
+    if (small_cluster(c->rows, c->cols)) return 256;
     const Problem p = problem_of(c->rows, c->cols, c->products);
     return layout(p, chunk_of(p, c->batch)).total;
 }
@@ -1017,11 +1006,16 @@ extern "C" r3_status r3_orthogonalize(const r3_orthogonal* c, const void* x, voi
     if (!x || !out || !aligned(x, 16) || !aligned(out, 16) || !aligned(dev_status, 4)) return R3_ERR_INVALID_ARG;
     if (!workspace || !aligned(workspace, 256) || ws_bytes < r3_orthogonalize_workspace_bytes(c))
         return R3_ERR_WORKSPACE;
+    const Job job = {c->out_dtype, c->in_dtype, 0, c->products, false, false, 0.f, (float)c->eps, 0.f, nullptr,
+                     nullptr};
+    if (const int cluster = small_cluster(c->rows, c->cols)) {
+        const r3_muon_stack one = {out, nullptr, x, nullptr, c->batch, c->rows, c->cols, 0.f, 0.f};
+        const r3_muon_stack* ss[1] = {&one};
+        return run_group_small(job, coefs, ss, 1, cluster, c->batch, dev_status, static_cast<cudaStream_t>(stream));
+    }
     ElemArgs a = {};
     a.stacks = 1;
     a.stack[0] = {out, nullptr, x, nullptr, 0, 0.f, 0.f};
-    const Job job = {c->out_dtype, c->in_dtype, 0, c->products, false, false, 0.f, (float)c->eps, 0.f, nullptr,
-                     nullptr};
     return run_group(job, coefs, problem_of(c->rows, c->cols, c->products), a, c->batch,
                      static_cast<uint8_t*>(workspace), dev_status, static_cast<cudaStream_t>(stream));
 }
@@ -1035,6 +1029,8 @@ extern "C" size_t r3_muon_workspace_bytes(const r3_muon* c, const r3_muon_stack*
     try {
         each_group(stacks, n_stacks, [&](const int32_t* members, int, int matrices) {
             const r3_muon_stack& s = stacks[members[0]];
+            most = std::max(most, (size_t)256);
+            if (small_cluster(s.rows, s.cols)) return R3_OK;
             const Problem p = problem_of(s.rows, s.cols, c->products);
             most = std::max(most, layout(p, chunk_of(p, matrices)).total);
             return R3_OK;
@@ -1063,6 +1059,13 @@ extern "C" r3_status r3_muon_step(const r3_muon* c, const r3_muon_stack* stacks,
         const Job job = {c->param_dtype, c->grad_dtype, c->nesterov != 0, c->products, c->master != 0, true,
                          (float)c->momentum, (float)c->eps, (float)c->lr, grad_scale, lr};
         return each_group(stacks, n_stacks, [&](const int32_t* members, int n, int matrices) {
+            const r3_muon_stack& one = stacks[members[0]];
+            if (const int cluster = small_cluster(one.rows, one.cols)) {
+                const r3_muon_stack* ss[MAX_STACKS];
+                for (int i = 0; i < n; ++i) ss[i] = stacks + members[i];
+                return run_group_small(job, coefs, ss, n, cluster, matrices, dev_status,
+                                       static_cast<cudaStream_t>(stream));
+            }
             ElemArgs a = {};
             a.stacks = n;
             int first = 0;
@@ -1071,8 +1074,7 @@ extern "C" r3_status r3_muon_step(const r3_muon* c, const r3_muon_stack* stacks,
                 a.stack[i] = {s.param, s.master, s.grad, s.momentum, first, s.weight_decay, s.scale};
                 first += s.batch;
             }
-            const r3_muon_stack& s = stacks[members[0]];
-            return run_group(job, coefs, problem_of(s.rows, s.cols, c->products), a, matrices,
+            return run_group(job, coefs, problem_of(one.rows, one.cols, c->products), a, matrices,
                              static_cast<uint8_t*>(workspace), dev_status, static_cast<cudaStream_t>(stream));
         });
     } catch (...) {

@@ -41,7 +41,7 @@ def test_orthogonalize_refused(r3, kw):
 
 
 def test_orthogonalize_workspace(r3):
-    for kw in (dict(ws=None), dict(ws=(3 << 20) + 128), dict(ws_bytes=1024)):
+    for kw in (dict(ws=None), dict(ws=(3 << 20) + 128), dict(ws_bytes=255), dict(ws_bytes=1 << 20, rows=300, cols=300)):
         assert ortho(r3, **kw) == r3.R3_ERR_WORKSPACE
     assert ortho(r3, batch=0, x=None, out=None, ws=None) == r3.R3_OK
     assert r3.lib.r3_orthogonalize(None, None, None, None, 0, None, None) == r3.R3_ERR_INVALID_ARG
@@ -85,7 +85,8 @@ def test_muon_refused(r3, kw):
 
 
 def test_muon_workspace_and_nothing_to_do(r3):
-    for kw in (dict(ws=None), dict(ws=(1 << 40) + 128), dict(ws_bytes=1024)):
+    for kw in (dict(ws=None), dict(ws=(1 << 40) + 128), dict(ws_bytes=255),
+               dict(stacks=[dict(rows=300, cols=300, param=1 << 36, momentum=2 << 36)], ws_bytes=1 << 20)):
         assert muon(r3, **kw) == r3.R3_ERR_WORKSPACE
     assert muon(r3, stacks=[], ws=None) == r3.R3_OK
     assert muon(r3, stacks=[dict(batch=0, param=None, grad=None, momentum=None)] * 2, ws=None) == r3.R3_OK

@@ -768,8 +768,8 @@ typedef struct {
  *              that is taken in parts, or over several ranks)
  *   dlogp = dloss dL/dlogp,  dentropy = dloss dL/dentropy           dloss: [1] on the device, NULL = 1
  * logp, logp_old [T]; logp_infer, logp_ref, entropy [T] or NULL; all float32.  w, logp_old and the masks are
- * constants.  A token counts where it belongs to a sequence and mask (uint8 [T], NULL = all) is not 0: of the
- * others only the mask is read, their gradients are 0.  cu_seqlens [S+1] int32 (device), ascending from 0 to at most T:
+ * constants.  A token counts where it belongs to a sequence and mask (uint8 [T], NULL = all) is not 0: the
+ * others' values are not used, their gradients are 0.  cu_seqlens [S+1] int32 (device), ascending from 0 to at most T:
  * tokens behind its last entry belong to no sequence; NULL with S = 1: one sequence of all tokens.
  * Outputs: loss [1]; dlogp [T] or NULL; dentropy [T] (only with entropy) or NULL; metrics [3] or NULL = the
  * weighted sums of term, kl and entropy; counts [3] int32 or NULL = tokens, tokens beyond a border (that take
@@ -807,7 +807,7 @@ typedef struct {
  *   dlogits   = balance_coef p_ti (f_i - sum_j f_j p_tj) / N + 2 z_coef (log sum exp) p_ti / N
  * (the gradient of balance_coef loss[l,0] + z_coef loss[l,1]; the counts are constants).
  * logits [L,T,E] f32; idx [L,T,K] idx_type (may be NULL with counts_given); mask uint8 [T] or NULL: tokens
- * that do not count have 0 there, and only their mask is read; counts [L,E] int32, written, may be NULL (with
+ * that do not count have 0 there, and their logits and record are not used; counts [L,E] int32, written, may be NULL (with
  * counts_given: read); loss [L,2] f32; dlogits [L,T,E] f32 or NULL (may be the logits' buffer), every
  * element written (tokens that do not count: 0, or left as they are with accumulate).  Only T, E, K and idx_type of
  * the shape matter.  E <= 1024 (R3_ERR_UNSUPPORTED beyond).  Sums run in an order that depends on the shape

@@ -8,10 +8,13 @@
 // and the logits are then read once: the pass that forms the probabilities has f and N in hand and
 // writes the gradient at once.  Bound by HBM: 8 E + K bytes a token and block.
 //
-// A token's logits lie across G lanes (a power of two, 4 or more logits each), so that its maximum, its
-// sum and its product with f are shuffles; a lane keeps the f of its experts and the sums of their
-// probabilities in registers over all its tokens.  CTAs take equal shares of a block's tokens; the last CTA
-// of a block to arrive adds up their probability sums, in an order that depends on the shape alone.
+// Counting: a cluster per part of a block's tokens, counters in shared memory, added up over the cluster.
+// Main pass: a token's logits lie across G lanes, 8 each where the experts are many (a shuffle then serves
+// 32 / G tokens), so that its maximum, its sum and its product with f are shuffles; a lane keeps the f of its
+// experts and the sums of their probabilities in registers, and the next tokens' logits are under way while
+// these are worked on.  All resident CTAs take equal shares of the L T tokens, across the borders of blocks
+// (grids of whole parts per block left a second wave of 32 CTAs for 48 blocks: 285 us against 150).  The last CTA of a
+// block to arrive adds up its probability sums, in an order that depends on the shape alone.
 #include <cmath>
 
 #include "r3_common.cuh"
@@ -21,16 +24,19 @@
 namespace r3 {
 namespace bal {
 
-constexpr int THREADS = 256;
-constexpr int WARPS = THREADS / 32;
 constexpr int MAX_EXPERTS = 1024;
-constexpr int COUNT_TOKENS = 2048;        // tokens of a CTA of the counting pass, at least
-constexpr int COUNT_PARTS = 32;           // and so many CTAs per block at most
+constexpr int COUNT_THREADS = 256;
+constexpr int COUNT_TOKENS = 1024;        // tokens of a CTA of the counting pass
+constexpr int COUNT_CTAS = 8;             // CTAs of its clusters
+constexpr int THREADS = 512;
+constexpr int WARPS = THREADS / 32;
+constexpr int CTAS_PER_SM = 2;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct Args {
     int T, E, K, L;
-    int count_parts, count_tokens;        // CTAs and tokens per CTA of the counting pass
-    int parts, part_tokens;               // CTAs and tokens per CTA of the main pass
+    int count_parts, count_ctas;          // clusters per block in the counting pass, CTAs of each
+    int grid;                             // CTAs of the main pass
     int accumulate, given;
     float balance_coef, z_coef;
     const float* logits;
@@ -40,34 +46,44 @@ struct Args {
     float* loss;                          // [L, 2]
     float* dlogits;                       // or null
     int32_t* part_counts;                 // [L, count_parts, E + 1]: per expert, then the tokens
-    float* part_probs;                    // [L, parts, E]
-    double* part_z;                       // [L, parts]
+    float* part_probs;                    // [grid + L, E]: a row per CTA and block that it has tokens of
+    double* part_z;                       // [grid + L]
     unsigned* ticket;                     // [L]
     int32_t* dev_status;
 };
+// The tokens of a CTA, as numbers of the L T; block l's first CTA and the number of its CTAs follow.
+__device__ __forceinline__ long long first_token(const Args& a, int cta) {
+    return (long long)a.L * a.T * cta / a.grid;
+}
+__device__ __forceinline__ int cta_of(const Args& a, long long token) {
+    int c = (int)(token * a.grid / ((long long)a.L * a.T));
+    while (c + 1 < a.grid && first_token(a, c + 1) <= token) ++c;
+    while (c > 0 && first_token(a, c) > token) --c;
+    return c;
+}
 
-// ---- counting pass: grid (count_parts, L) -----------------------------------------------------
+// ---- counting pass: grid (count_parts * count_ctas, L), clusters of count_ctas -------------------
 template <typename IdxT>
-__global__ void __launch_bounds__(THREADS) count_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(COUNT_THREADS) count_kernel(const __grid_constant__ Args a) {
     extern __shared__ int s_count[];
     const int l = blockIdx.y, E = a.E, K = a.K;
-    for (int e = threadIdx.x; e <= E; e += THREADS) s_count[e] = 0;
+    for (int e = threadIdx.x; e <= E; e += COUNT_THREADS) s_count[e] = 0;
     tc::grid_launch_dependents();
     __syncthreads();
     tc::grid_dependency_wait();
     if (blockIdx.x == 0 && threadIdx.x == 0) a.ticket[l] = 0;
-    const int t0 = blockIdx.x * a.count_tokens, t1 = min(a.T, t0 + a.count_tokens);
+    const int t0 = (int)min((long long)a.T, (long long)blockIdx.x * COUNT_TOKENS), t1 = min(a.T, t0 + COUNT_TOKENS);
     if (a.mask) {
         int n = 0;
-        for (int t = t0 + threadIdx.x; t < t1; t += THREADS) n += a.mask[t] != 0;
+        for (int t = t0 + threadIdx.x; t < t1; t += COUNT_THREADS) n += a.mask[t] != 0;
         n = __reduce_add_sync(0xffffffffu, n);
         if ((threadIdx.x & 31) == 0 && n) atomicAdd(&s_count[E], n);
     } else if (threadIdx.x == 0) {
-        s_count[E] = max(t1 - t0, 0);
+        s_count[E] = t1 - t0;
     }
     if (!a.given) {
         const IdxT* idx = static_cast<const IdxT*>(a.idx) + ((size_t)l * a.T + t0) * K;
-        const int n = max(t1 - t0, 0) * K;
+        const int n = (t1 - t0) * K;
         auto take = [&](int i, int e) {
             if (a.mask && !a.mask[t0 + i / K]) return;
             if (e < 0 || e >= E) {
@@ -80,21 +96,41 @@ __global__ void __launch_bounds__(THREADS) count_kernel(const __grid_constant__ 
         // the record's base is aligned to 16 bytes, a CTA's first choice need not be
         const int skip = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(idx) & 15)) & 15) / (int)sizeof(IdxT));
         const int vecs = (n - skip) / VEC;
-        for (int i = threadIdx.x; i < skip; i += THREADS) take(i, idx_to_int(idx[i]));
-        for (int v = threadIdx.x; v < vecs; v += THREADS) {
+        for (int i = threadIdx.x; i < skip; i += COUNT_THREADS) take(i, idx_to_int(idx[i]));
+        for (int v = threadIdx.x; v < vecs; v += COUNT_THREADS) {
             const int4 w = *reinterpret_cast<const int4*>(idx + skip + v * VEC);
             const IdxT* x = reinterpret_cast<const IdxT*>(&w);
 #pragma unroll
             for (int j = 0; j < VEC; ++j) take(skip + v * VEC + j, idx_to_int(x[j]));
         }
-        for (int i = skip + vecs * VEC + threadIdx.x; i < n; i += THREADS) take(i, idx_to_int(idx[i]));
+        for (int i = skip + vecs * VEC + threadIdx.x; i < n; i += COUNT_THREADS) take(i, idx_to_int(idx[i]));
     }
-    __syncthreads();
-    int32_t* out = a.part_counts + ((size_t)l * a.count_parts + blockIdx.x) * (E + 1);
-    for (int e = threadIdx.x; e <= E; e += THREADS) out[e] = s_count[e];
+    const int ctas = a.count_ctas;
+    const int part = ctas > 1 ? blockIdx.x / ctas : blockIdx.x;
+    int32_t* out = a.part_counts + ((size_t)l * a.count_parts + part) * (E + 1);
+    if (ctas == 1) {
+        __syncthreads();
+        for (int e = threadIdx.x; e <= E; e += COUNT_THREADS) out[e] = s_count[e];
+        return;
+    }
+    __syncwarp();
+    tc::cluster_sync_all();
+    const int rank = (int)tc::cluster_ctarank();
+    for (int e = threadIdx.x * ctas + rank; e <= E; e += COUNT_THREADS * ctas) {
+        int n = 0;
+        for (int c = 0; c < ctas; ++c) {
+            int v;
+            asm volatile("ld.shared::cluster.s32 %0, [%1];"
+                         : "=r"(v) : "r"(tc::mapa_shared(tc::smem_u32(s_count + e), (uint32_t)c)) : "memory");
+            n += v;
+        }
+        out[e] = n;
+    }
+    __syncwarp();
+    tc::cluster_sync_all();                              // no CTA leaves while another reads its counters
 }
 
-// ---- main pass: grid (parts, L) ---------------------------------------------------------------
+// ---- main pass ------------------------------------------------------------------------------------
 // G lanes per token, V logits per lane.  WIDE: E is a multiple of 4, a lane's logits come in fours
 // (columns 4 (lane + G q) ..); otherwise one by one (columns lane + G q).
 template <int G, int V, bool WIDE> struct Row {
@@ -135,90 +171,101 @@ template <int G, int V, bool WIDE> struct Row {
 };
 
 template <int G, int V, bool WIDE>
-__global__ void __launch_bounds__(THREADS, V <= 8 ? 4 : 2) balance_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_kernel(const __grid_constant__ Args a) {
     using R = Row<G, V, WIDE>;
     constexpr int ROWS = 32 / G;                       // tokens of a warp at a time
-    constexpr int AT_ONCE = V <= 8 ? 2 : 1;            // of those, in flight
-    extern __shared__ float s_col[];                   // f, later the CTA's sums of probabilities
+    extern __shared__ float s_col[];                   // f, later [WARPS][E] sums of probabilities
     __shared__ long long s_sum[WARPS];
-    __shared__ double s_z[WARPS];
+    __shared__ double s_z[WARPS], s_b[WARPS];
     __shared__ int s_tokens;
     __shared__ bool s_last;
-    const int l = blockIdx.y, E = a.E, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int E = a.E, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int sub = lane % G, row = lane / G;
     tc::grid_launch_dependents();
     tc::grid_dependency_wait();
-    // the block's counts, the number of its choices and of its tokens
-    long long mine = 0;
-    for (int e = threadIdx.x; e <= E; e += THREADS) {
-        int n = 0;
-        if (e < E && a.given) {
-            n = a.counts[(size_t)l * E + e];
-        } else {
-            const int32_t* p = a.part_counts + (size_t)l * a.count_parts * (E + 1) + e;
-#pragma unroll 8
-            for (int q = 0; q < a.count_parts; ++q) n += p[(size_t)q * (E + 1)];
-        }
-        if (e == E) {
-            s_tokens = n;
-        } else {
-            s_col[e] = (float)n;                       // below 2^24, or off by a rounding
-            mine += n;
-            if (!a.given && a.counts && blockIdx.x == 0) a.counts[(size_t)l * E + e] = n;
-        }
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-    if (lane == 0) s_sum[warp] = mine;
-    __syncthreads();
-    long long choices = 0;
-#pragma unroll
-    for (int i = 0; i < WARPS; ++i) choices += s_sum[i];
-    const int tokens = s_tokens;
-    const float per_choice = choices > 0 ? (float)((double)E / (double)choices) : 0.f;
-    const float per_token = tokens > 0 ? 1.f / (float)tokens : 0.f;
-    float f[V], sum[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int c = R::column(sub, j);
-        f[j] = c < E ? s_col[c] * per_choice : 0.f;
-        sum[j] = 0.f;
-    }
-    __syncthreads();                                   // s_col is used again below
-    const float gb = a.balance_coef * per_token, gz = 2.f * a.z_coef * per_token;
-    const int t0 = blockIdx.x * a.part_tokens, t1 = min(a.T, t0 + a.part_tokens);
-    const float* logits = a.logits + (size_t)l * a.T * E;
-    float* dlogits = a.dlogits ? a.dlogits + (size_t)l * a.T * E : nullptr;
-    double z = 0.0;
-    for (int t = t0 + warp * ROWS * AT_ONCE; t < t1; t += WARPS * ROWS * AT_ONCE) {
-        float v[AT_ONCE][V];
-        bool on[AT_ONCE];
-#pragma unroll
-        for (int r = 0; r < AT_ONCE; ++r) {
-            const int at = t + r * ROWS + row;
-            on[r] = at < t1 && (!a.mask || a.mask[at]);
-            if (on[r]) {
-                R::load(logits + (size_t)at * E, E, sub, v[r], -INFINITY);
+    const long long begin = first_token(a, blockIdx.x), end = first_token(a, blockIdx.x + 1);
+    // an empty batch: CTA 0 still writes the losses of every block
+    const int l_first = a.T > 0 ? (int)(begin / a.T) : 0;
+    const int l_past = a.T > 0 ? (end > begin ? (int)((end - 1) / a.T) + 1 : l_first) : a.L;
+    for (int l = l_first; l < l_past; ++l) {
+        const long long block0 = (long long)l * a.T;
+        const int t0 = (int)(max(begin, block0) - block0), t1 = (int)(min(end, block0 + a.T) - block0);
+        const float* logits = a.logits + (size_t)block0 * E;
+        float* dlogits = a.dlogits ? a.dlogits + (size_t)block0 * E : nullptr;
+        const int hop = WARPS * ROWS;
+        // the first tokens' logits are under way while the counts are added up
+        float next[V];
+        bool next_on = false;
+        auto fetch = [&](int t) {
+            const int at = t + row;
+            next_on = at < t1 && (!a.mask || a.mask[at]);
+            if (at < t1) {                             // (not behind the mask's arrival)
+                R::load(logits + (size_t)at * E, E, sub, next, -INFINITY);
             } else {
 #pragma unroll
-                for (int j = 0; j < V; ++j) v[r][j] = -INFINITY;
+                for (int j = 0; j < V; ++j) next[j] = -INFINITY;
+            }
+        };
+        fetch(t0 + warp * ROWS);
+        // the block's counts, the number of its choices and of its tokens
+        long long mine = 0;
+        for (int e = threadIdx.x; e <= E; e += THREADS) {
+            int n = 0;
+            if (e < E && a.given) {
+                n = a.counts[(size_t)l * E + e];
+            } else {
+                const int32_t* p = a.part_counts + (size_t)l * a.count_parts * (E + 1) + e;
+#pragma unroll 8
+                for (int q = 0; q < a.count_parts; ++q) n += p[(size_t)q * (E + 1)];
+            }
+            if (e == E) {
+                s_tokens = n;
+            } else {
+                s_col[e] = (float)n;                   // below 2^24, or off by a rounding
+                mine += n;
+                if (!a.given && a.counts && t0 == 0) a.counts[(size_t)l * E + e] = n;
             }
         }
 #pragma unroll
-        for (int r = 0; r < AT_ONCE; ++r) {
-            const int at = t + r * ROWS + row;
-            float top = v[r][0];
+        for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+        if (lane == 0) s_sum[warp] = mine;
+        __syncthreads();
+        long long choices = 0;
 #pragma unroll
-            for (int j = 1; j < V; ++j) top = fmaxf(top, v[r][j]);
+        for (int i = 0; i < WARPS; ++i) choices += s_sum[i];
+        const int tokens = s_tokens;
+        const float per_choice = choices > 0 ? (float)((double)E / (double)choices) : 0.f;
+        const float per_token = tokens > 0 ? 1.f / (float)tokens : 0.f;
+        float f[V], sum[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int c = R::column(sub, j);
+            f[j] = c < E ? s_col[c] * per_choice : 0.f;
+            sum[j] = 0.f;
+        }
+        __syncthreads();                               // s_col is used again below
+        const float gb = a.balance_coef * per_token, gz = 2.f * a.z_coef * per_token;
+        float z = 0.f;                                 // of a few hundred tokens; the CTAs' are added in 64 bits
+        for (int t = t0 + warp * ROWS; t < t1; t += hop) {
+            float v[V];
+            const bool on = next_on;
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = on ? next[j] : -INFINITY;
+            if (t + hop < t1) fetch(t + hop);
+            const int at = t + row;
+            float top = v[0];
+#pragma unroll
+            for (int j = 1; j < V; ++j) top = fmaxf(top, v[j]);
 #pragma unroll
             for (int o = G / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            const float from = top == -INFINITY ? 0.f : top;       // a token without any expert: all 0
+            // a token without any expert: all 0
+            const float from = top == -INFINITY ? 0.f : top;
             float whole = 0.f, along = 0.f;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                v[r][j] = expf(v[r][j] - from);
-                whole += v[r][j];
-                along += v[r][j] * f[j];
+                v[j] = exp2f((v[j] - from) * LOG2E);
+                whole += v[j];
+                along = fmaf(v[j], f[j], along);
             }
 #pragma unroll
             for (int o = G / 2; o > 0; o >>= 1) {
@@ -226,127 +273,133 @@ __global__ void __launch_bounds__(THREADS, V <= 8 ? 4 : 2) balance_kernel(const 
                 along += __shfl_xor_sync(0xffffffffu, along, o);
             }
             const float inv = whole != 0.f ? 1.f / whole : 0.f;
-            const float lse = whole != 0.f ? from + logf(whole) : 0.f;
+            const float lse = whole != 0.f ? fmaf(LN2, log2f(whole), from) : 0.f;
             along *= inv;
-            if (sub == 0) z += (double)lse * (double)lse;          // 0 where the token does not count
+            z = fmaf(lse, lse, z);                     // 0 where the token does not count
             const float shift = gz * lse - gb * along;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float p = v[r][j] * inv;
+                const float p = v[j] * inv;
                 sum[j] += p;
-                v[r][j] = p * (gb * f[j] + shift);
+                v[j] = p * fmaf(gb, f[j], shift);
             }
             if (dlogits && at < t1) {
                 float* out = dlogits + (size_t)at * E;
                 if (a.accumulate) {
-                    float old[V];
-                    R::load(out, E, sub, old, 0.f);
-                    if (on[r]) {
+                    if (on) {
+                        float old[V];
+                        R::load(out, E, sub, old, 0.f);
 #pragma unroll
-                        for (int j = 0; j < V; ++j) old[j] += v[r][j];
+                        for (int j = 0; j < V; ++j) old[j] += v[j];
                         R::store(out, E, sub, old);
                     }
                 } else {
-                    R::store(out, E, sub, v[r]);
+                    R::store(out, E, sub, v);
                 }
             }
         }
-    }
-    // the CTA's sums: lanes that hold the same experts, then the warps in their order
+        // the CTA's sums: lanes that hold the same experts, then the warps in their order
 #pragma unroll
-    for (int j = 0; j < V; ++j)
+        for (int j = 0; j < V; ++j)
 #pragma unroll
-        for (int o = G; o < 32; o <<= 1) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], o);
+            for (int o = G; o < 32; o <<= 1) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], o);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-    if (lane == 0) s_z[warp] = z;
-    for (int w = 0; w < WARPS; ++w) {
-        if (warp == w && row == 0) {
+        for (int o = G; o < 32; o <<= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+        if (lane == 0) s_z[warp] = (double)z;
+        if (row == 0) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const int c = R::column(sub, j);
-                if (c < E) s_col[c] = (w ? s_col[c] : 0.f) + sum[j];
+                if (c < E) s_col[warp * E + c] = sum[j];
             }
         }
         __syncthreads();
-    }
-    float* probs = a.part_probs + ((size_t)l * a.parts + blockIdx.x) * E;
-    for (int c = threadIdx.x; c < E; c += THREADS) probs[c] = s_col[c];
-    if (threadIdx.x == 0) {
-        double all = 0.0;
+        // a row of its own per CTA and block: CTAs that cross a border have two or more
+        const size_t at = (size_t)blockIdx.x + l;
+        for (int c = threadIdx.x; c < E; c += THREADS) {
+            float all = 0.f;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) all += s_z[w];
-        a.part_z[(size_t)l * a.parts + blockIdx.x] = all;
-    }
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) s_last = atomicAdd(a.ticket + l, 1u) == gridDim.x - 1;
-    __syncthreads();
-    if (!s_last) return;
-    __threadfence();
-    double balance = 0.0;
-    for (int c = threadIdx.x; c < E; c += THREADS) {
-        const volatile float* p = a.part_probs + (size_t)l * a.parts * E + c;
-        double s = 0.0;
+            for (int w = 0; w < WARPS; ++w) all += s_col[w * E + c];
+            a.part_probs[at * E + c] = all;
+        }
+        if (threadIdx.x == 0) {
+            double all = 0.0;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) all += s_z[w];
+            a.part_z[at] = all;
+        }
+        __threadfence();
+        __syncthreads();
+        const int c_first = a.T > 0 ? cta_of(a, block0) : 0, c_last = a.T > 0 ? cta_of(a, block0 + a.T - 1) : 0;
+        const int parts = c_last - c_first + 1;
+        if (threadIdx.x == 0) s_last = atomicAdd(a.ticket + l, 1u) == (unsigned)parts - 1u;
+        __syncthreads();
+        if (!s_last) continue;
+        __threadfence();
+        // THREADS / columns threads per column (a power of two), each every so many parts
+        int per = 1;
+        while (per * 2 * E <= THREADS && per < 32) per *= 2;
+        double balance = 0.0;
+        for (int c0 = 0; c0 < E; c0 += THREADS / per) {
+            const int c = c0 + (int)threadIdx.x / per, k = threadIdx.x % per;
+            if (c >= E) continue;
+            const float* p = a.part_probs + ((size_t)c_first + l) * E + c;
+            double s = 0.0;
 #pragma unroll 8
-        for (int q = 0; q < a.parts; ++q) s += (double)p[(size_t)q * E];
-        int n = 0;
-        if (a.given) {
-            n = a.counts[(size_t)l * E + c];
-        } else {
-            const int32_t* k = a.part_counts + (size_t)l * a.count_parts * (E + 1) + c;
-            for (int q = 0; q < a.count_parts; ++q) n += k[(size_t)q * (E + 1)];
+            for (int q = k; q < parts; q += per) s += (double)__ldcg(p + (size_t)q * E);
+            int n = 0;
+            if (a.given) {
+                n = a.counts[(size_t)l * E + c];
+            } else {
+                const int32_t* cnt = a.part_counts + (size_t)l * a.count_parts * (E + 1) + c;
+#pragma unroll 8
+                for (int q = 0; q < a.count_parts; ++q) n += cnt[(size_t)q * (E + 1)];
+            }
+            balance += s * (double)n;
         }
-        balance += s * (double)n;
-    }
-    double zz = 0.0;
-    for (int q = threadIdx.x; q < a.parts; q += THREADS)
-        zz += *(const volatile double*)(a.part_z + (size_t)l * a.parts + q);
+        double zz = 0.0;
+        for (int q = threadIdx.x; q < parts; q += THREADS) zz += __ldcg(a.part_z + (size_t)c_first + l + q);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        balance += __shfl_xor_sync(0xffffffffu, balance, o);
-        zz += __shfl_xor_sync(0xffffffffu, zz, o);
-    }
-    __shared__ double s_b[WARPS];
-    if (lane == 0) {
-        s_b[warp] = balance;
-        s_z[warp] = zz;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        balance = zz = 0.0;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            balance += s_b[w];
-            zz += s_z[w];
+        for (int o = 16; o > 0; o >>= 1) {
+            balance += __shfl_xor_sync(0xffffffffu, balance, o);
+            zz += __shfl_xor_sync(0xffffffffu, zz, o);
         }
-        const double n = tokens > 0 ? (double)tokens : 1.0;
-        a.loss[2 * l] = choices > 0 ? (float)(balance * (double)E / ((double)choices * n)) : 0.f;
-        a.loss[2 * l + 1] = (float)(zz / n);
+        if (lane == 0) {
+            s_b[warp] = balance;
+            s_z[warp] = zz;
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            balance = zz = 0.0;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                balance += s_b[w];
+                zz += s_z[w];
+            }
+            const double n = tokens > 0 ? (double)tokens : 1.0;
+            a.loss[2 * l] = choices > 0 ? (float)(balance * (double)E / ((double)choices * n)) : 0.f;
+            a.loss[2 * l + 1] = (float)(zz / n);
+        }
+        __syncthreads();                               // the next block's sums go to the same places
     }
 }
 
 struct Plan {
-    int count_parts, count_tokens, parts, part_tokens;
+    int count_parts, count_ctas, grid;
 };
-// CTAs per block: four resident ones per SM over all blocks, unless a CTA's share falls below 64 tokens
-// (its start, which adds up the counting pass's parts, is then no longer small beside it).
-static Plan plan(int T, int L) {
+// Main pass: every resident CTA, unless a warp's share falls below two tokens or so.
+static Plan plan(int T, int L, int E) {
     Plan p;
-    auto split = [&](int most, int least_tokens, int* parts, int* tokens) {
-        long long n = (T + least_tokens - 1) / least_tokens;
-        if (n > most) n = most;
-        if (n < 1) n = 1;
-        *tokens = (int)((T + n - 1) / n);
-        if (*tokens < 1) *tokens = 1;
-        *parts = T > 0 ? (T + *tokens - 1) / *tokens : 1;
-    };
-    split(COUNT_PARTS, COUNT_TOKENS, &p.count_parts, &p.count_tokens);
-    const int share = (4 * sm_count() + L - 1) / L;
-    split(share < 1 ? 1 : share, 64, &p.parts, &p.part_tokens);
+    const int ctas = T > 0 ? (T + COUNT_TOKENS - 1) / COUNT_TOKENS : 1;
+    p.count_ctas = 1;
+    while (p.count_ctas < COUNT_CTAS && p.count_ctas < ctas) p.count_ctas *= 2;
+    p.count_parts = (ctas + p.count_ctas - 1) / p.count_ctas;
+    long long grid = ((long long)T * L + 2 * WARPS - 1) / (2 * WARPS);
+    const int most = (E > 256 ? 1 : CTAS_PER_SM) * sm_count();
+    if (grid > most) grid = most;
+    p.grid = grid < 1 || T == 0 ? 1 : (int)grid;
     return p;
 }
-
 static r3_status check(const r3_shape* s, int32_t L, const r3_balance* c) {
     if (!s || !c || L < 0 || L > 65535) return R3_ERR_INVALID_ARG;
     const r3_status st = check_shape(s);
@@ -366,8 +419,8 @@ static Layout layout(const r3_shape* s, int32_t L, const Plan& p) {
         return here;
     };
     w.counts = take((size_t)L * p.count_parts * (s->E + 1) * 4);
-    w.probs = take((size_t)L * p.parts * s->E * 4);
-    w.z = take((size_t)L * p.parts * 8);
+    w.probs = take(((size_t)p.grid + L) * s->E * 4);
+    w.z = take(((size_t)p.grid + L) * 8);
     w.ticket = take((size_t)L * 4);
     w.total = at;
     return w;
@@ -375,14 +428,24 @@ static Layout layout(const r3_shape* s, int32_t L, const Plan& p) {
 
 template <int G, int V, bool WIDE>
 static r3_status launch(const Args& a, cudaStream_t cs) {
-    return tc::launch_dependent(balance_kernel<G, V, WIDE>, dim3(a.parts, a.L), dim3(THREADS),
-                                (size_t)a.E * sizeof(float), cs, a) == cudaSuccess ? R3_OK : R3_ERR_CUDA;
+    const size_t smem = (size_t)a.E * WARPS * sizeof(float);
+    if (smem > 32 * 1024) {                            // above what every kernel may have, with its static part
+        static PerDevice ready;
+        if (!ready.done()) {
+            if (cudaFuncSetAttribute(balance_kernel<G, V, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     MAX_EXPERTS * WARPS * (int)sizeof(float)) != cudaSuccess)
+                return R3_ERR_CUDA;
+            ready.mark();
+        }
+    }
+    return tc::launch_dependent(balance_kernel<G, V, WIDE>, dim3(a.grid), dim3(THREADS), smem, cs, a) == cudaSuccess
+               ? R3_OK : R3_ERR_CUDA;
 }
 template <bool WIDE>
 static r3_status launch(const Args& a, cudaStream_t cs) {
     if (a.E <= 16) return launch<4, 4, WIDE>(a, cs);
-    if (a.E <= 64) return launch<16, 4, WIDE>(a, cs);
-    if (a.E <= 128) return launch<32, 4, WIDE>(a, cs);
+    if (a.E <= 64) return launch<8, 8, WIDE>(a, cs);
+    if (a.E <= 128) return launch<16, 8, WIDE>(a, cs);
     if (a.E <= 256) return launch<32, 8, WIDE>(a, cs);
     if (a.E <= 512) return launch<32, 16, WIDE>(a, cs);
     return launch<32, 32, WIDE>(a, cs);
@@ -395,7 +458,7 @@ extern "C" size_t r3_balance_loss_workspace_bytes(const r3_shape* s, int32_t L) 
     using namespace r3::bal;
     const r3_balance none = {};
     if (check(s, L, &none) != R3_OK || L == 0) return 0;
-    return layout(s, L, plan(s->T, L)).total;
+    return layout(s, L, plan(s->T, L, s->E)).total;
 }
 
 extern "C" r3_status r3_balance_loss(const r3_shape* s, int32_t L, const r3_balance* config,
@@ -416,7 +479,7 @@ extern "C" r3_status r3_balance_loss(const r3_shape* s, int32_t L, const r3_bala
     const void* words[] = {counts, loss, dev_status};
     for (const void* p : words)
         if (!aligned(p, 4)) return R3_ERR_INVALID_ARG;
-    const Plan p = plan(s->T, L);
+    const Plan p = plan(s->T, L, s->E);
     const Layout w = layout(s, L, p);
     if (!workspace || !aligned(workspace, 256) || ws_bytes < w.total) return R3_ERR_WORKSPACE;
     Args a = {};
@@ -425,9 +488,8 @@ extern "C" r3_status r3_balance_loss(const r3_shape* s, int32_t L, const r3_bala
     a.K = s->K;
     a.L = L;
     a.count_parts = p.count_parts;
-    a.count_tokens = p.count_tokens;
-    a.parts = p.parts;
-    a.part_tokens = p.part_tokens;
+    a.count_ctas = p.count_ctas;
+    a.grid = p.grid;
     a.accumulate = config->accumulate != 0;
     a.given = given;
     a.balance_coef = (float)config->balance_coef;
@@ -446,9 +508,22 @@ extern "C" r3_status r3_balance_loss(const r3_shape* s, int32_t L, const r3_bala
     a.dev_status = dev_status;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     const size_t smem = (size_t)(s->E + 1) * sizeof(int);
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)p.count_ctas;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)(p.count_parts * p.count_ctas), (unsigned)L);
+    cfg.blockDim = dim3(COUNT_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = cs;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.count_ctas > 1 ? 2 : 1;
     cudaError_t err = cudaSuccess;
-    R3_DISPATCH_IDX(s, IdxT, err = tc::launch_dependent(count_kernel<IdxT>, dim3(p.count_parts, L),
-                                                        dim3(THREADS), smem, cs, a));
+    R3_DISPATCH_IDX(s, IdxT, err = cudaLaunchKernelEx(&cfg, count_kernel<IdxT>, a));
     if (err != cudaSuccess) return R3_ERR_CUDA;
     return s->E % 4 == 0 ? launch<true>(a, cs) : launch<false>(a, cs);
 }

@@ -51,7 +51,8 @@ struct Args {
     float *loss, *dlogp, *dentropy, *metrics;
     int32_t* counts;
     Sums* sums;                                        // [units]
-    int* n;                                            // [units]
+    int* n;                                            // [units] tokens
+    int* head;                                         // [units] 1: the first unit of a sequence with tokens
     Total* totals;                                     // [CTAs]
     unsigned* ticket;
     int32_t* dev_status;
@@ -103,7 +104,7 @@ __device__ __forceinline__ float infer_weight(const Args& a, float old, float in
 }
 
 // ---- first pass: the sums of a unit ----------------------------------------------------------
-__device__ __forceinline__ void unit_sums(const Args& a, const Unit& u, Sums* s, int* n) {
+__device__ __forceinline__ void unit_sums(const Args& a, const Unit& u, int unit, Sums* s, int* n, int* head) {
     const int lane = threadIdx.x & 31;
     const bool live = u.seq < a.S;
     double d = 0.0, up = 0.0, down = 0.0;
@@ -117,31 +118,43 @@ __device__ __forceinline__ void unit_sums(const Args& a, const Unit& u, Sums* s,
 #pragma unroll
         for (int j = 0; j < PER_LANE; ++j) {
             const int t = u.begin + j * 32 + lane;
-            on[j] = t < u.end && (!a.mask || a.mask[t]);
-            k += on[j];
-        }
-        if (a.by_sequence) {
-#pragma unroll
-            for (int j = 0; j < PER_LANE; ++j) {
-                const int t = u.begin + j * 32 + lane;
+            on[j] = t < u.end;
+            if (a.by_sequence) {                           // (not behind the mask's arrival)
                 lp[j] = on[j] ? a.logp[t] : 0.f;
                 old[j] = on[j] ? a.old[t] : 0.f;
                 inf[j] = on[j] && a.infer ? a.infer[t] : 0.f;
                 adv[j] = on[j] ? (a.adv_per_token ? a.adv[t] : seq_adv) : 0.f;
             }
+            if (a.mask && on[j]) on[j] = a.mask[t] != 0;
+        }
 #pragma unroll
-            for (int j = 0; j < PER_LANE; ++j) {
-                if (!on[j]) continue;
-                d += (double)lp[j] - (double)old[j];
-                bool cut;
-                const float w = a.infer ? infer_weight(a, old[j], inf[j], &cut) : 1.f;
-                const double wa = (double)(w * adv[j]);
-                if (adv[j] > 0.f) up += wa;
-                else if (adv[j] != 0.f) down += wa;    // NaN counts here: it has to reach the loss
-            }
+        for (int j = 0; j < PER_LANE; ++j) {
+            k += on[j];
+            if (!a.by_sequence || !on[j]) continue;
+            d += (double)lp[j] - (double)old[j];
+            bool cut;
+            const float w = a.infer ? infer_weight(a, old[j], inf[j], &cut) : 1.f;
+            const double wa = (double)(w * adv[j]);
+            if (adv[j] > 0.f) up += wa;
+            else if (adv[j] != 0.f) down += wa;            // NaN counts here: it has to reach the loss
         }
     }
     k = warp_sum(k);
+    int any = 0;
+    if (a.mean_of_sequences && live && unit == u.first && u.count > 0) {
+        // does the sequence hold a token at all: mostly its first unit says so
+        any = k > 0;
+        const int seq_end = bound(a, u.seq + 1);
+        for (int t = u.begin + UNIT; !any && t < seq_end; t += UNIT) {
+            int here = 0;
+#pragma unroll
+            for (int j = 0; j < PER_LANE; ++j) {
+                const int at = t + j * 32 + lane;
+                here |= at < seq_end && a.mask[at];        // without a mask the first unit has tokens
+            }
+            any = __any_sync(0xffffffffu, here);
+        }
+    }
     if (a.by_sequence) {
         d = warp_sum(d);
         up = warp_sum(up);
@@ -149,6 +162,7 @@ __device__ __forceinline__ void unit_sums(const Args& a, const Unit& u, Sums* s,
     }
     if (lane == 0) {
         *n = k;
+        *head = any;
         if (a.by_sequence) *s = {d, up, down};
     }
 }
@@ -209,21 +223,18 @@ __device__ __forceinline__ Total unit_loss(const Args& a, const Unit& u, const S
     }
     float lp[PER_LANE], old[PER_LANE], inf[PER_LANE], ref[PER_LANE], ent[PER_LANE], adv[PER_LANE];
     bool on[PER_LANE];
+    const bool want_logp = !a.by_sequence || a.ref, want_old = !a.by_sequence || a.infer;
 #pragma unroll
     for (int j = 0; j < PER_LANE; ++j) {
         const int t = u.begin + j * 32 + lane;
-        on[j] = live && t < u.end && (!a.mask || a.mask[t]);
-    }
-    const bool want_logp = !a.by_sequence || a.ref;
-#pragma unroll
-    for (int j = 0; j < PER_LANE; ++j) {
-        const int t = u.begin + j * 32 + lane;
+        on[j] = live && t < u.end;
         lp[j] = on[j] && want_logp ? a.logp[t] : 0.f;
-        old[j] = on[j] && (!a.by_sequence || a.infer) ? a.old[t] : 0.f;
+        old[j] = on[j] && want_old ? a.old[t] : 0.f;
         inf[j] = on[j] && a.infer ? a.infer[t] : 0.f;
         ref[j] = on[j] && a.ref ? a.ref[t] : 0.f;
         ent[j] = on[j] && a.entropy ? a.entropy[t] : 0.f;
         adv[j] = on[j] ? (a.adv_per_token ? a.adv[t] : seq_adv) : 0.f;
+        if (a.mask && on[j]) on[j] = a.mask[t] != 0;
     }
 #pragma unroll
     for (int j = 0; j < PER_LANE; ++j) {
@@ -260,12 +271,10 @@ __device__ __forceinline__ Total unit_loss(const Args& a, const Unit& u, const S
         if (a.dlogp) a.dlogp[t] = g;
         if (a.dentropy) a.dentropy[t] = ge;
     }
-    r.policy = warp_sum(r.policy) * weight;
-    r.kl = a.ref ? warp_sum(r.kl) * weight : 0.0;
-    r.entropy = a.entropy ? warp_sum(r.entropy) * weight : 0.0;
-    r.tokens = warp_sum(r.tokens);
-    r.clipped = warp_sum(r.clipped);
-    r.cut = warp_sum(r.cut);
+    // (lane by lane: the warp's lanes are added up once, at the end)
+    r.policy *= weight;
+    r.kl *= weight;
+    r.entropy *= weight;
     return r;
 }
 
@@ -276,6 +285,15 @@ __device__ __forceinline__ void add(Total& x, const Total& y) {
     x.tokens += y.tokens;
     x.clipped += y.clipped;
     x.cut += y.cut;
+}
+__device__ __forceinline__ Total warp_total(const Args& a, Total r) {
+    r.policy = warp_sum(r.policy);
+    if (a.ref) r.kl = warp_sum(r.kl);
+    if (a.entropy) r.entropy = warp_sum(r.entropy);
+    r.tokens = warp_sum(r.tokens);
+    r.clipped = warp_sum(r.clipped);
+    if (a.infer) r.cut = warp_sum(r.cut);
+    return r;
 }
 __device__ __forceinline__ void write_loss(const Args& a, const Total& r) {
     a.loss[0] = (float)(r.policy + (a.kl_coef != 0.0 ? a.kl_coef * r.kl : 0.0) -
@@ -293,22 +311,14 @@ __device__ __forceinline__ void write_loss(const Args& a, const Total& r) {
 }
 
 // The number that the weights are divided by, for the whole CTA: response tokens, or sequences that hold
-// one.  `n`: all units' token counts.
+// one.  `n`, `head`: all units'.
 template <int W>
-__device__ __forceinline__ double count_divisor(const Args& a, const int* n, int* s_warp) {
+__device__ __forceinline__ double count_divisor(const Args& a, const int* n, const int* head, int* s_warp) {
     if (a.denominator > 0.0) return a.denominator;
+    const int* from = a.mean_of_sequences ? head : n;
     int k = 0;
-    if (!a.mean_of_sequences) {
-        for (int i = threadIdx.x; i < a.units; i += 32 * W) k += n[i];
-    } else {
-        for (int i = threadIdx.x; i < a.S; i += 32 * W) {
-            const int begin = bound(a, i), end = max(bound(a, i + 1), begin);
-            const int first = i + begin / UNIT, units = (end - begin + UNIT - 1) / UNIT;
-            bool any = false;
-            for (int q = 0; q < units && !any; ++q) any = n[first + q] > 0;
-            k += any;
-        }
-    }
+#pragma unroll 4
+    for (int i = threadIdx.x; i < a.units; i += 32 * W) k += from[i];
     k = warp_sum(k);
     if ((threadIdx.x & 31) == 0) s_warp[threadIdx.x >> 5] = k;
     __syncthreads();
@@ -328,52 +338,57 @@ __device__ __forceinline__ void check_bounds(const Args& a, int thread, int thre
     }
 }
 
-__global__ void __launch_bounds__(WARPS * 32) sums_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(WARPS * 32, 4) sums_kernel(const __grid_constant__ Args a) {
     tc::grid_launch_dependents();
     tc::grid_dependency_wait();
-    const int unit = blockIdx.x * WARPS + (threadIdx.x >> 5);
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
     check_bounds(a, blockIdx.x * WARPS * 32 + threadIdx.x, gridDim.x * WARPS * 32);
-    if (!a.need_sums || unit >= a.units) return;
-    const Unit u = find_unit(a, unit);
-    unit_sums(a, u, a.sums + unit, a.n + unit);
+    if (!a.need_sums) return;
+    for (int unit = blockIdx.x * WARPS + (threadIdx.x >> 5); unit < a.units; unit += gridDim.x * WARPS)
+        unit_sums(a, find_unit(a, unit), unit, a.sums + unit, a.n + unit, a.head + unit);
 }
 
-__global__ void __launch_bounds__(WARPS * 32) loss_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(WARPS * 32, 2) loss_kernel(const __grid_constant__ Args a) {
     __shared__ int s_count[WARPS];
-    __shared__ int s_seq[WARPS];
+    __shared__ int s_seq[2][WARPS];
     __shared__ Total s_total[WARPS];
-    __shared__ Sums s_sums;
-    __shared__ int s_tokens;
+    __shared__ Sums s_sums[2];
+    __shared__ int s_tokens[2];
     __shared__ bool s_last;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int unit = blockIdx.x * WARPS + warp;
     tc::grid_launch_dependents();
     tc::grid_dependency_wait();
-    Unit u = {a.S, 0, 0, 0, 0};
-    if (unit < a.units) u = find_unit(a, unit);
-    if (lane == 0) s_seq[warp] = unit < a.units ? u.seq : -1;
-    const double divisor = count_divisor<WARPS>(a, a.n, s_count);
-    Sums s = {};
-    int n_seq = 1;
-    if (a.by_sequence || a.mean_of_sequences) {
-        __syncthreads();
-        if (s_seq[0] == s_seq[WARPS - 1]) {            // one long sequence: added up once
-            if (warp == 0) {
-                sequence_sums(a, a.sums, a.n, u.first, u.count, &s, &n_seq);
-                if (lane == 0) {
-                    s_sums = s;
-                    s_tokens = n_seq;
-                }
-            }
+    const double divisor = count_divisor<WARPS>(a, a.n, a.head, s_count);
+    Total r = {};
+    int turn = 0;
+    for (int first = blockIdx.x * WARPS; first < a.units; first += gridDim.x * WARPS, turn ^= 1) {
+        const int unit = first + warp;
+        Unit u = {a.S, 0, 0, 0, 0};
+        if (unit < a.units) u = find_unit(a, unit);
+        Sums s = {};
+        int n_seq = 1;
+        if (a.by_sequence || a.mean_of_sequences) {
+            // (what stands in shared memory is exchanged every other turn: one barrier lies in between)
+            if (lane == 0) s_seq[turn][warp] = unit < a.units ? u.seq : -1;
             __syncthreads();
-            s = s_sums;
-            n_seq = s_tokens;
-        } else if (u.begin < u.end) {
-            sequence_sums(a, a.sums, a.n, u.first, u.count, &s, &n_seq);
+            if (s_seq[turn][0] == s_seq[turn][WARPS - 1]) {    // one long sequence: added up once
+                if (warp == 0) {
+                    sequence_sums(a, a.sums, a.n, u.first, u.count, &s, &n_seq);
+                    if (lane == 0) {
+                        s_sums[turn] = s;
+                        s_tokens[turn] = n_seq;
+                    }
+                }
+                __syncthreads();
+                s = s_sums[turn];
+                n_seq = s_tokens[turn];
+            } else if (u.begin < u.end) {
+                sequence_sums(a, a.sums, a.n, u.first, u.count, &s, &n_seq);
+            }
         }
+        add(r, unit_loss(a, u, s, n_seq, divisor));
     }
-    const Total r = unit_loss(a, u, s, n_seq, divisor);
+    r = warp_total(a, r);
     if (lane == 0) s_total[warp] = r;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -393,12 +408,7 @@ __global__ void __launch_bounds__(WARPS * 32) loss_kernel(const __grid_constant_
         const volatile Total* t = a.totals + i;
         add(sum, Total{t->policy, t->kl, t->entropy, t->tokens, t->clipped, t->cut, 0});
     }
-    sum.policy = warp_sum(sum.policy);
-    sum.kl = warp_sum(sum.kl);
-    sum.entropy = warp_sum(sum.entropy);
-    sum.tokens = warp_sum(sum.tokens);
-    sum.clipped = warp_sum(sum.clipped);
-    sum.cut = warp_sum(sum.cut);
+    sum = warp_total(a, sum);
     if (lane == 0) s_total[warp] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -412,36 +422,32 @@ __global__ void __launch_bounds__(WARPS * 32) loss_kernel(const __grid_constant_
 // Both passes of a batch of few units.
 __global__ void __launch_bounds__(ONE_WARPS * 32) one_cta_kernel(const __grid_constant__ Args a) {
     __shared__ Sums s_sums[ONE_WARPS];
-    __shared__ int s_n[ONE_WARPS];
-    __shared__ int s_count[ONE_WARPS];
+    __shared__ int s_n[ONE_WARPS], s_head[ONE_WARPS];
     __shared__ Total s_total[ONE_WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     tc::grid_launch_dependents();
     tc::grid_dependency_wait();
-    check_bounds(a, threadIdx.x, ONE_WARPS * 32);
+    check_bounds(a, threadIdx.x, blockDim.x);
     Unit u = {a.S, 0, 0, 0, 0};
-    if (lane == 0) s_n[warp] = 0;
     if (warp < a.units) {
         u = find_unit(a, warp);
-        unit_sums(a, u, s_sums + warp, s_n + warp);
+        unit_sums(a, u, warp, s_sums + warp, s_n + warp, s_head + warp);
     }
     __syncthreads();
-    const double divisor = count_divisor<ONE_WARPS>(a, s_n, s_count);
+    double divisor = a.denominator;
+    if (!(divisor > 0.0)) {
+        const int* from = a.mean_of_sequences ? s_head : s_n;
+        divisor = (double)max(warp_sum(lane < a.units ? from[lane] : 0), 1);
+    }
     Sums s = {};
     int n_seq = 1;
     if ((a.by_sequence || a.mean_of_sequences) && u.begin < u.end)
         sequence_sums(a, s_sums, s_n, u.first, u.count, &s, &n_seq);
-    const Total r = unit_loss(a, u, s, n_seq, divisor);
+    const Total r = warp_total(a, unit_loss(a, u, s, n_seq, divisor));
     if (lane == 0) s_total[warp] = r;
     __syncthreads();
     if (warp == 0) {
-        Total sum = s_total[lane];
-        sum.policy = warp_sum(sum.policy);
-        sum.kl = warp_sum(sum.kl);
-        sum.entropy = warp_sum(sum.entropy);
-        sum.tokens = warp_sum(sum.tokens);
-        sum.clipped = warp_sum(sum.clipped);
-        sum.cut = warp_sum(sum.cut);
+        const Total sum = warp_total(a, lane < a.units ? s_total[lane] : Total{});
         if (lane == 0) write_loss(a, sum);
     }
 }
@@ -467,9 +473,9 @@ static r3_status check(const r3_policy* c) {
 extern "C" size_t r3_policy_loss_workspace_bytes(const r3_policy* c) {
     using namespace r3::pol;
     if (check(c) != R3_OK) return 0;
-    const size_t units = (size_t)unit_count(c), ctas = (units + WARPS - 1) / WARPS;
-    return 256 + r3::round_up(units * sizeof(Sums), 256) + r3::round_up(units * sizeof(int), 256) +
-           r3::round_up(ctas * sizeof(Total), 256);
+    const size_t units = (size_t)unit_count(c);
+    return 256 + r3::round_up(units * sizeof(Sums), 256) + 2 * r3::round_up(units * sizeof(int), 256) +
+           r3::round_up((units + WARPS - 1) / WARPS * sizeof(Total), 256);
 }
 
 extern "C" r3_status r3_policy_loss(const r3_policy* c, const float* logp, const float* logp_old,
@@ -527,20 +533,25 @@ extern "C" r3_status r3_policy_loss(const r3_policy* c, const float* logp, const
     a.counts = counts;
     a.dev_status = dev_status;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
-    const int ctas = (a.units + WARPS - 1) / WARPS;
     a.ticket = reinterpret_cast<unsigned*>(ws);
     ws += 256;
     a.sums = reinterpret_cast<Sums*>(ws);
     ws += round_up((size_t)a.units * sizeof(Sums), 256);
     a.n = reinterpret_cast<int*>(ws);
     ws += round_up((size_t)a.units * sizeof(int), 256);
+    a.head = reinterpret_cast<int*>(ws);
+    ws += round_up((size_t)a.units * sizeof(int), 256);
     a.totals = reinterpret_cast<Total*>(ws);
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     if (a.units <= ONE_WARPS)
-        return tc::launch_dependent(one_cta_kernel, dim3(1), dim3(ONE_WARPS * 32), 0, cs, a) == cudaSuccess
+        return tc::launch_dependent(one_cta_kernel, dim3(1), dim3(32 * a.units), 0, cs, a) == cudaSuccess
                    ? R3_OK : R3_ERR_CUDA;
-    if (tc::launch_dependent(sums_kernel, dim3(ctas), dim3(WARPS * 32), 0, cs, a) != cudaSuccess ||
-        tc::launch_dependent(loss_kernel, dim3(ctas), dim3(WARPS * 32), 0, cs, a) != cudaSuccess)
+    // a wave of resident CTAs at most, which go on to further units (the second wave of 25 CTAs made
+    // a million tokens take 43 us instead of 24)
+    const int ctas = (a.units + WARPS - 1) / WARPS;
+    const int first = ctas < 4 * sm_count() ? ctas : 4 * sm_count(), second = ctas < 2 * sm_count() ? ctas : 2 * sm_count();
+    if (tc::launch_dependent(sums_kernel, dim3(first), dim3(WARPS * 32), 0, cs, a) != cudaSuccess ||
+        tc::launch_dependent(loss_kernel, dim3(second), dim3(WARPS * 32), 0, cs, a) != cudaSuccess)
         return R3_ERR_CUDA;
     return R3_OK;
 }

@@ -1357,17 +1357,16 @@ def policy_loss(logp, logp_old, cu_seqlens=None, *, advantages=None, seq_advanta
         mask = _arg("mask", mask, (T,), torch.uint8 if mask.dtype == torch.uint8 else torch.bool, dev)
     c = Policy(T, S, _RATIO[ratio], _REDUCE[reduce], seq_advantages is None, clip_low, clip_high, dual_clip,
                infer_cap, kl_coef, entropy_coef, denominator)
-    # the small outputs lie in one allocation
-    small = new((7,), (1,), dtype=f32, device=dev)
-    loss, metrics, counts = small[:1], small[1:4], small[4:].view(torch.int32)
+    loss, metrics = new((1,), (1,), dtype=f32, device=dev), new((3,), (1,), dtype=f32, device=dev)
+    counts = new((3,), (1,), dtype=torch.int32, device=dev)
     dlogp = new((T,), (1,), dtype=f32, device=dev) if want_grad else None
     dentropy = new((T,), (1,), dtype=f32, device=dev) if want_grad and entropy is not None else None
-    here = small.data_ptr()
     ws = _scratch(ws, lib.r3_policy_loss_workspace_bytes(ctypes.byref(c)), dev)
     _check(lib.r3_policy_loss(
         ctypes.byref(c), at[0], at[1], adv, cu, mask, at[2], at[3], at[4],
-        _arg("dloss", dloss, (1,), f32, dev), here, None if dlogp is None else dlogp.data_ptr(),
-        None if dentropy is None else dentropy.data_ptr(), here + 4, here + 16, ws.data_ptr(), ws.numel(),
+        _arg("dloss", dloss, (1,), f32, dev), loss.data_ptr(), None if dlogp is None else dlogp.data_ptr(),
+        None if dentropy is None else dentropy.data_ptr(), metrics.data_ptr(), counts.data_ptr(),
+        ws.data_ptr(), ws.numel(),
         None if dev_status is None else _ptr(dev_status), _stream(stream)))
     return loss, dlogp, dentropy, metrics, counts
 

@@ -336,26 +336,33 @@ __global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_ker
         __syncthreads();
         if (!s_last) continue;
         __threadfence();
-        // THREADS / columns threads per column (a power of two), each every so many parts
-        int per = 1;
-        while (per * 2 * E <= THREADS && per < 32) per *= 2;
+        // sum_i counts_i sum_parts p: the parts' rows lie one after the other, every thread takes its share of
+        // all their numbers
         double balance = 0.0;
-        for (int c0 = 0; c0 < E; c0 += THREADS / per) {
-            const int c = c0 + (int)threadIdx.x / per, k = threadIdx.x % per;
-            if (c >= E) continue;
-            const float* p = a.part_probs + ((size_t)c_first + l) * E + c;
-            double s = 0.0;
-#pragma unroll 8
-            for (int q = k; q < parts; q += per) s += (double)__ldcg(p + (size_t)q * E);
+        const float* p = a.part_probs + ((size_t)c_first + l) * E;
+        auto count_at = [&](int c) {
+            if (a.given) return a.counts[(size_t)l * E + c];
+            const int32_t* cnt = a.part_counts + (size_t)l * a.count_parts * (E + 1) + c;
             int n = 0;
-            if (a.given) {
-                n = a.counts[(size_t)l * E + c];
-            } else {
-                const int32_t* cnt = a.part_counts + (size_t)l * a.count_parts * (E + 1) + c;
 #pragma unroll 8
-                for (int q = 0; q < a.count_parts; ++q) n += cnt[(size_t)q * (E + 1)];
+            for (int q = 0; q < a.count_parts; ++q) n += cnt[(size_t)q * (E + 1)];
+            return n;
+        };
+        int32_t* s_n = reinterpret_cast<int32_t*>(s_col);
+        for (int c = threadIdx.x; c < E; c += THREADS) s_n[c] = count_at(c);
+        __syncthreads();
+        if (WIDE) {
+            const int four = parts * (E / 4);
+#pragma unroll 8
+            for (int i = threadIdx.x; i < four; i += THREADS) {
+                const float4 v = __ldcg(reinterpret_cast<const float4*>(p) + i);
+                const int c = i % (E / 4) * 4;
+                balance += (double)v.x * s_n[c] + (double)v.y * s_n[c + 1] + (double)v.z * s_n[c + 2] +
+                           (double)v.w * s_n[c + 3];
             }
-            balance += s * (double)n;
+        } else {
+#pragma unroll 8
+            for (int i = threadIdx.x; i < parts * E; i += THREADS) balance += (double)__ldcg(p + i) * s_n[i % E];
         }
         double zz = 0.0;
         for (int q = threadIdx.x; q < parts; q += THREADS) zz += __ldcg(a.part_z + (size_t)c_first + l + q);

@@ -11,12 +11,12 @@
 // not depend on how an exponential rounds; exponentials and the terms are float32, all sums 64 bits.
 //
 // Two passes, since a token's gradient needs its sequence's sums and the number of tokens: the first
-// leaves the sums of every unit (up to 256 consecutive tokens of ONE sequence, a warp each), the second
-// adds up a sequence's units in their order and writes the gradients; its last CTA adds up the CTAs'
-// parts of the loss.  A sequence that starts at token c takes its units from number i + floor(c / 256)
-// on: that leaves each one room for all of its units whatever the lengths are, and a warp finds its
-// sequence by a search in cu_seqlens, 32 probes at a time, with no table built before.  Batches of up to
-// 32 units run as one CTA.
+// leaves the sums of every unit (up to U = 256 consecutive tokens of ONE sequence, more in a large batch, a
+// warp each), the second adds up a sequence's units in their order and writes the gradients; its last CTA
+// adds up the CTAs' parts of the loss.  Sequence i that starts at token c takes its units from number
+// i + floor(c / U) on: that leaves each one room for all of its units whatever the lengths are, and a warp of
+// the first pass finds its sequence by a search in cu_seqlens, 32 probes at a time, with no table built
+// before.  Batches of up to 32 units run as one CTA.
 // Bound by HBM where the batch is large, by two launches where it is not.
 #include <cmath>
 
@@ -27,9 +27,14 @@
 namespace r3 {
 namespace pol {
 
-constexpr int UNIT = 256;                 // tokens of a unit
-constexpr int PER_LANE = UNIT / 32;
+constexpr int STEP = 128;                 // tokens that a warp works on at a time
+constexpr int PER_LANE = STEP / 32;
+constexpr int LEAST_UNIT = 256;           // tokens of a unit, at least; a power of two
+constexpr int MOST_UNITS = 2048;          // of one sequence: beyond, units grow
+constexpr int LONG = 64;                  // units from which a sequence is added up in BLOCKS blocks
+constexpr int BLOCKS = 8;
 constexpr int WARPS = 8;                  // units of a CTA
+constexpr int CTAS_PER_SM = 4;
 constexpr int ONE_WARPS = 32;             // units of a batch that takes one CTA
 
 struct Sums {                             // of one unit; of a sequence: the sum of its units'
@@ -40,7 +45,7 @@ struct Total {
     int tokens, clipped, cut, pad;
 };
 struct Args {
-    int T, S, units;
+    int T, S, units, shift;                            // 1 << shift tokens per unit
     int by_sequence, mean_of_sequences, adv_per_token, need_sums;
     double log_high, log_low, log_dual, log_cap;       // borders of d and of logp_old - logp_infer
     float high, low, dual, cap;                        // the values beyond them
@@ -53,6 +58,7 @@ struct Args {
     Sums* sums;                                        // [units]
     int* n;                                            // [units] tokens
     int* head;                                         // [units] 1: the first unit of a sequence with tokens
+    int4* table;                                       // [units, 2] what find_unit gives
     Total* totals;                                     // [CTAs]
     unsigned* ticket;
     int32_t* dev_status;
@@ -62,7 +68,7 @@ __device__ __forceinline__ int bound(const Args& a, int i) {       // where sequ
     if (!a.cu) return i == 0 ? 0 : a.T;
     return min(max(a.cu[i], 0), a.T);
 }
-__device__ __forceinline__ int first_unit(const Args& a, int i) { return i + bound(a, i) / UNIT; }
+__device__ __forceinline__ int first_unit(const Args& a, int i) { return i + (bound(a, i) >> a.shift); }
 
 struct Unit {
     int seq, begin, end;                  // seq = S: behind the last sequence
@@ -82,11 +88,11 @@ __device__ __forceinline__ Unit find_unit(const Args& a, int unit) {
     Unit u;
     u.seq = lo;
     const int begin = bound(a, lo), end = lo < a.S ? max(bound(a, lo + 1), begin) : a.T;
-    u.first = lo + begin / UNIT;
-    u.count = (end - begin + UNIT - 1) / UNIT;
-    const long long at = begin + (long long)(unit - u.first) * UNIT;
+    u.first = lo + (begin >> a.shift);
+    u.count = (int)(((long long)end - begin + (1 << a.shift) - 1) >> a.shift);
+    const long long at = begin + ((long long)(unit - u.first) << a.shift);
     u.begin = (int)min(at, (long long)end);
-    u.end = min(u.begin + UNIT, end);
+    u.end = (int)min((long long)u.begin + (1 << a.shift), (long long)end);
     return u;
 }
 __device__ __forceinline__ double warp_sum(double v) {
@@ -113,30 +119,33 @@ __device__ __forceinline__ void unit_sums(const Args& a, const Unit& u, int unit
         if (lane == 0) k = u.end - u.begin;
     } else if (live) {
         const float seq_adv = a.by_sequence && !a.adv_per_token && u.begin < u.end ? a.adv[u.seq] : 0.f;
-        float lp[PER_LANE], old[PER_LANE], inf[PER_LANE], adv[PER_LANE];
-        bool on[PER_LANE];
+#pragma unroll 2
+        for (int t0 = u.begin + lane; t0 - lane < u.end; t0 += STEP) {
+            float lp[PER_LANE], old[PER_LANE], inf[PER_LANE], adv[PER_LANE];
+            bool on[PER_LANE];
 #pragma unroll
-        for (int j = 0; j < PER_LANE; ++j) {
-            const int t = u.begin + j * 32 + lane;
-            on[j] = t < u.end;
-            if (a.by_sequence) {                           // (not behind the mask's arrival)
-                lp[j] = on[j] ? a.logp[t] : 0.f;
-                old[j] = on[j] ? a.old[t] : 0.f;
-                inf[j] = on[j] && a.infer ? a.infer[t] : 0.f;
-                adv[j] = on[j] ? (a.adv_per_token ? a.adv[t] : seq_adv) : 0.f;
+            for (int j = 0; j < PER_LANE; ++j) {
+                const int t = t0 + j * 32;
+                on[j] = t < u.end;
+                if (a.by_sequence) {                       // (not behind the mask's arrival)
+                    lp[j] = on[j] ? a.logp[t] : 0.f;
+                    old[j] = on[j] ? a.old[t] : 0.f;
+                    inf[j] = on[j] && a.infer ? a.infer[t] : 0.f;
+                    adv[j] = on[j] ? (a.adv_per_token ? a.adv[t] : seq_adv) : 0.f;
+                }
+                if (a.mask && on[j]) on[j] = a.mask[t] != 0;
             }
-            if (a.mask && on[j]) on[j] = a.mask[t] != 0;
-        }
 #pragma unroll
-        for (int j = 0; j < PER_LANE; ++j) {
-            k += on[j];
-            if (!a.by_sequence || !on[j]) continue;
-            d += (double)lp[j] - (double)old[j];
-            bool cut;
-            const float w = a.infer ? infer_weight(a, old[j], inf[j], &cut) : 1.f;
-            const double wa = (double)(w * adv[j]);
-            if (adv[j] > 0.f) up += wa;
-            else if (adv[j] != 0.f) down += wa;            // NaN counts here: it has to reach the loss
+            for (int j = 0; j < PER_LANE; ++j) {
+                k += on[j];
+                if (!a.by_sequence || !on[j]) continue;
+                d += (double)lp[j] - (double)old[j];
+                bool cut;
+                const float w = a.infer ? infer_weight(a, old[j], inf[j], &cut) : 1.f;
+                const double wa = (double)(w * adv[j]);
+                if (adv[j] > 0.f) up += wa;
+                else if (adv[j] != 0.f) down += wa;        // NaN counts here: it has to reach the loss
+            }
         }
     }
     k = warp_sum(k);
@@ -145,10 +154,10 @@ __device__ __forceinline__ void unit_sums(const Args& a, const Unit& u, int unit
         // does the sequence hold a token at all: mostly its first unit says so
         any = k > 0;
         const int seq_end = bound(a, u.seq + 1);
-        for (int t = u.begin + UNIT; !any && t < seq_end; t += UNIT) {
+        for (int t = u.end; !any && t < seq_end; t += 8 * STEP) {
             int here = 0;
 #pragma unroll
-            for (int j = 0; j < PER_LANE; ++j) {
+            for (int j = 0; j < 8 * PER_LANE; ++j) {
                 const int at = t + j * 32 + lane;
                 here |= at < seq_end && a.mask[at];        // without a mask the first unit has tokens
             }
@@ -167,24 +176,45 @@ __device__ __forceinline__ void unit_sums(const Args& a, const Unit& u, int unit
     }
 }
 
-// A sequence's sums, from its units in a fixed order, by a whole warp.
-__device__ __forceinline__ void sequence_sums(const Args& a, const Sums* sums, const int* n, int first,
-                                              int count, Sums* s, int* tokens) {
+// Sums of the units [first, first + count), by a whole warp.
+struct Whole {
+    Sums s;
+    int tokens;
+};
+__device__ __forceinline__ Whole add_units(const Args& a, const Sums* sums, const int* n, int first, int count) {
     const int lane = threadIdx.x & 31;
-    double d = 0.0, up = 0.0, down = 0.0;
-    int k = 0;
+    Whole w = {};
 #pragma unroll 4
     for (int i = lane; i < count; i += 32) {
-        k += n[first + i];
+        w.tokens += n[first + i];
         if (a.by_sequence) {
             const Sums v = sums[first + i];
-            d += v.d;
-            up += v.up;
-            down += v.down;
+            w.s.d += v.d;
+            w.s.up += v.up;
+            w.s.down += v.down;
         }
     }
-    *tokens = warp_sum(k);
-    if (a.by_sequence) *s = {warp_sum(d), warp_sum(up), warp_sum(down)};
+    w.tokens = warp_sum(w.tokens);
+    if (a.by_sequence) w.s = {warp_sum(w.s.d), warp_sum(w.s.up), warp_sum(w.s.down)};
+    return w;
+}
+__device__ __forceinline__ Whole add_block(const Args& a, const Sums* sums, const int* n, int first, int count,
+                                           int block) {
+    const int size = (count + BLOCKS - 1) / BLOCKS, from = min(count, block * size);
+    return add_units(a, sums, n, first + from, min(size, count - from));
+}
+__device__ __forceinline__ void add(Whole& x, const Whole& y) {
+    x.s.d += y.s.d;
+    x.s.up += y.s.up;
+    x.s.down += y.s.down;
+    x.tokens += y.tokens;
+}
+// A sequence's sums by one warp: in the same order as by the warps of a CTA (below).
+__device__ __forceinline__ Whole sequence_sums(const Args& a, const Sums* sums, const int* n, int first, int count) {
+    if (count <= LONG) return add_units(a, sums, n, first, count);
+    Whole w = {};
+    for (int b = 0; b < BLOCKS; ++b) add(w, add_block(a, sums, n, first, count, b));
+    return w;
 }
 
 // exp(x) - 1 - x without cancellation: its series up to |x| = 1 (the first term left out, 2 / 13! of
@@ -211,65 +241,68 @@ __device__ __forceinline__ Total unit_loss(const Args& a, const Unit& u, const S
     const float ent_g = (float)(-a.entropy_coef * weight * (double)up_to);
     const float seq_adv = live && !a.adv_per_token && u.begin < u.end ? a.adv[u.seq] : 0.f;
     double seq_d = 0.0;
-    float seq_slope = 0.f;
+    float seq_slope = 0.f, seq_rho = 0.f;
     if (a.by_sequence && live) {
         seq_d = s.d / (double)max(n_seq, 1);
-        const double rho = (double)expf((float)seq_d);
+        seq_rho = expf((float)seq_d);
+        const double rho = (double)seq_rho;
         const bool high = seq_d > a.log_high, low = seq_d < a.log_low || seq_d > a.log_dual;
         // a part that is 0 takes no ratio, be it infinite
         const double part = (high ? 0.0 : s.up) + (low ? 0.0 : s.down);
         seq_slope = part == 0.0 ? 0.f
                                 : (float)(-part * rho * weight * (double)up_to / (double)max(n_seq, 1));
     }
-    float lp[PER_LANE], old[PER_LANE], inf[PER_LANE], ref[PER_LANE], ent[PER_LANE], adv[PER_LANE];
-    bool on[PER_LANE];
     const bool want_logp = !a.by_sequence || a.ref, want_old = !a.by_sequence || a.infer;
+    for (int t0 = u.begin + lane; t0 - lane < u.end; t0 += STEP) {
+        float lp[PER_LANE], old[PER_LANE], inf[PER_LANE], ref[PER_LANE], ent[PER_LANE], adv[PER_LANE];
+        bool on[PER_LANE];
 #pragma unroll
-    for (int j = 0; j < PER_LANE; ++j) {
-        const int t = u.begin + j * 32 + lane;
-        on[j] = live && t < u.end;
-        lp[j] = on[j] && want_logp ? a.logp[t] : 0.f;
-        old[j] = on[j] && want_old ? a.old[t] : 0.f;
-        inf[j] = on[j] && a.infer ? a.infer[t] : 0.f;
-        ref[j] = on[j] && a.ref ? a.ref[t] : 0.f;
-        ent[j] = on[j] && a.entropy ? a.entropy[t] : 0.f;
-        adv[j] = on[j] ? (a.adv_per_token ? a.adv[t] : seq_adv) : 0.f;
-        if (a.mask && on[j]) on[j] = a.mask[t] != 0;
-    }
-#pragma unroll
-    for (int j = 0; j < PER_LANE; ++j) {
-        const int t = u.begin + j * 32 + lane;
-        if (t >= u.end) continue;
-        float g = 0.f, ge = 0.f;
-        if (on[j]) {
-            const double d = a.by_sequence ? seq_d : (double)lp[j] - (double)old[j];
-            bool cut = false;
-            const float w = a.infer ? infer_weight(a, old[j], inf[j], &cut) : 1.f;
-            const float wa = w * adv[j];
-            const bool high = adv[j] > 0.f && d > a.log_high;
-            const bool low = adv[j] < 0.f && d < a.log_low;
-            const bool far = adv[j] < 0.f && d > a.log_dual;
-            const float rho = high ? a.high : low ? a.low : far ? a.dual : expf((float)d);
-            const float term = adv[j] == 0.f ? 0.f : -(wa * rho);
-            const bool beyond = high || low || far;
-            r.tokens += 1;
-            r.clipped += beyond;
-            r.cut += cut;
-            r.policy += (double)term;
-            g = a.by_sequence ? seq_slope : beyond ? 0.f : term * gw;
-            if (a.ref) {
-                const float x = (float)((double)ref[j] - (double)lp[j]);
-                const float em1 = expm1f(x);
-                r.kl += (double)exp_less_line(x, em1);
-                if (a.kl_coef != 0.0) g -= kl_w * em1;
-            }
-            if (a.entropy) {
-                r.entropy += (double)ent[j];
-                ge = ent_g;
-            }
+        for (int j = 0; j < PER_LANE; ++j) {
+            const int t = t0 + j * 32;
+            on[j] = live && t < u.end;
+            lp[j] = on[j] && want_logp ? a.logp[t] : 0.f;
+            old[j] = on[j] && want_old ? a.old[t] : 0.f;
+            inf[j] = on[j] && a.infer ? a.infer[t] : 0.f;
+            ref[j] = on[j] && a.ref ? a.ref[t] : 0.f;
+            ent[j] = on[j] && a.entropy ? a.entropy[t] : 0.f;
+            adv[j] = on[j] ? (a.adv_per_token ? a.adv[t] : seq_adv) : 0.f;
+            if (a.mask && on[j]) on[j] = a.mask[t] != 0;
         }
-        if (a.dlogp) a.dlogp[t] = g;
-        if (a.dentropy) a.dentropy[t] = ge;
+#pragma unroll
+        for (int j = 0; j < PER_LANE; ++j) {
+            const int t = t0 + j * 32;
+            if (t >= u.end) continue;
+            float g = 0.f, ge = 0.f;
+            if (on[j]) {
+                const double d = a.by_sequence ? seq_d : (double)lp[j] - (double)old[j];
+                bool cut = false;
+                const float w = a.infer ? infer_weight(a, old[j], inf[j], &cut) : 1.f;
+                const float wa = w * adv[j];
+                const bool high = adv[j] > 0.f && d > a.log_high;
+                const bool low = adv[j] < 0.f && d < a.log_low;
+                const bool far = adv[j] < 0.f && d > a.log_dual;
+                const float rho = high ? a.high : low ? a.low : far ? a.dual : a.by_sequence ? seq_rho : expf((float)d);
+                const float term = adv[j] == 0.f ? 0.f : -(wa * rho);
+                const bool beyond = high || low || far;
+                r.tokens += 1;
+                r.clipped += beyond;
+                r.cut += cut;
+                r.policy += (double)term;
+                g = a.by_sequence ? seq_slope : beyond ? 0.f : term * gw;
+                if (a.ref) {
+                    const float x = (float)((double)ref[j] - (double)lp[j]);
+                    const float em1 = expm1f(x);
+                    r.kl += (double)exp_less_line(x, em1);
+                    if (a.kl_coef != 0.0) g -= kl_w * em1;
+                }
+                if (a.entropy) {
+                    r.entropy += (double)ent[j];
+                    ge = ent_g;
+                }
+            }
+            if (a.dlogp) a.dlogp[t] = g;
+            if (a.dentropy) a.dentropy[t] = ge;
+        }
     }
     // (lane by lane: the warp's lanes are added up once, at the end)
     r.policy *= weight;
@@ -315,10 +348,14 @@ __device__ __forceinline__ void write_loss(const Args& a, const Total& r) {
 template <int W>
 __device__ __forceinline__ double count_divisor(const Args& a, const int* n, const int* head, int* s_warp) {
     if (a.denominator > 0.0) return a.denominator;
-    const int* from = a.mean_of_sequences ? head : n;
+    // (the arrays end with zeros up to a multiple of four)
+    const int4* from = reinterpret_cast<const int4*>(a.mean_of_sequences ? head : n);
     int k = 0;
 #pragma unroll 4
-    for (int i = threadIdx.x; i < a.units; i += 32 * W) k += from[i];
+    for (int i = threadIdx.x; i < (a.units + 3) / 4; i += 32 * W) {
+        const int4 v = from[i];
+        k += v.x + v.y + v.z + v.w;
+    }
     k = warp_sum(k);
     if ((threadIdx.x & 31) == 0) s_warp[threadIdx.x >> 5] = k;
     __syncthreads();
@@ -338,24 +375,34 @@ __device__ __forceinline__ void check_bounds(const Args& a, int thread, int thre
     }
 }
 
-__global__ void __launch_bounds__(WARPS * 32, 4) sums_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(WARPS * 32, CTAS_PER_SM) sums_kernel(const __grid_constant__ Args a) {
     tc::grid_launch_dependents();
     tc::grid_dependency_wait();
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
     check_bounds(a, blockIdx.x * WARPS * 32 + threadIdx.x, gridDim.x * WARPS * 32);
-    if (!a.need_sums) return;
-    for (int unit = blockIdx.x * WARPS + (threadIdx.x >> 5); unit < a.units; unit += gridDim.x * WARPS)
-        unit_sums(a, find_unit(a, unit), unit, a.sums + unit, a.n + unit, a.head + unit);
+    const int padded = (a.units + 3) & ~3;
+    for (int unit = blockIdx.x * WARPS + (threadIdx.x >> 5); unit < padded; unit += gridDim.x * WARPS) {
+        if (unit >= a.units) {
+            a.n[unit] = a.head[unit] = 0;
+            continue;
+        }
+        const Unit u = find_unit(a, unit);
+        if ((threadIdx.x & 31) == 0) {
+            a.table[2 * unit] = make_int4(u.seq, u.begin, u.end, 0);
+            a.table[2 * unit + 1] = make_int4(u.first, u.count, 0, 0);
+        }
+        if (a.need_sums) unit_sums(a, u, unit, a.sums + unit, a.n + unit, a.head + unit);
+    }
 }
 
-__global__ void __launch_bounds__(WARPS * 32, 2) loss_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(WARPS * 32, CTAS_PER_SM) loss_kernel(const __grid_constant__ Args a) {
     __shared__ int s_count[WARPS];
     __shared__ int s_seq[2][WARPS];
+    __shared__ Whole s_block[2][BLOCKS];
     __shared__ Total s_total[WARPS];
-    __shared__ Sums s_sums[2];
-    __shared__ int s_tokens[2];
     __shared__ bool s_last;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    static_assert(BLOCKS == WARPS, "a block of a long sequence per warp");
     tc::grid_launch_dependents();
     tc::grid_dependency_wait();
     const double divisor = count_divisor<WARPS>(a, a.n, a.head, s_count);
@@ -364,29 +411,29 @@ __global__ void __launch_bounds__(WARPS * 32, 2) loss_kernel(const __grid_consta
     for (int first = blockIdx.x * WARPS; first < a.units; first += gridDim.x * WARPS, turn ^= 1) {
         const int unit = first + warp;
         Unit u = {a.S, 0, 0, 0, 0};
-        if (unit < a.units) u = find_unit(a, unit);
-        Sums s = {};
-        int n_seq = 1;
+        if (unit < a.units) {
+            const int4 x = a.table[2 * unit], y = a.table[2 * unit + 1];
+            u = {x.x, x.y, x.z, y.x, y.y};
+        }
+        Whole w = {};
+        w.tokens = 1;
         if (a.by_sequence || a.mean_of_sequences) {
-            // (what stands in shared memory is exchanged every other turn: one barrier lies in between)
+            // (what stands in shared memory is exchanged every other turn: a barrier lies in between)
             if (lane == 0) s_seq[turn][warp] = unit < a.units ? u.seq : -1;
             __syncthreads();
-            if (s_seq[turn][0] == s_seq[turn][WARPS - 1]) {    // one long sequence: added up once
-                if (warp == 0) {
-                    sequence_sums(a, a.sums, a.n, u.first, u.count, &s, &n_seq);
-                    if (lane == 0) {
-                        s_sums[turn] = s;
-                        s_tokens[turn] = n_seq;
-                    }
-                }
+            if (s_seq[turn][0] == s_seq[turn][WARPS - 1] && u.count > LONG) {
+                // one long sequence: a block per warp
+                const Whole mine = add_block(a, a.sums, a.n, u.first, u.count, warp);
+                if (lane == 0) s_block[turn][warp] = mine;
                 __syncthreads();
-                s = s_sums[turn];
-                n_seq = s_tokens[turn];
-            } else if (u.begin < u.end) {
-                sequence_sums(a, a.sums, a.n, u.first, u.count, &s, &n_seq);
+                w.tokens = 0;
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) add(w, s_block[turn][b]);
+            } else if (u.begin < u.end && u.seq < a.S) {
+                w = sequence_sums(a, a.sums, a.n, u.first, u.count);
             }
         }
-        add(r, unit_loss(a, u, s, n_seq, divisor));
+        add(r, unit_loss(a, u, w.s, w.tokens, divisor));
     }
     r = warp_total(a, r);
     if (lane == 0) s_total[warp] = r;
@@ -439,11 +486,10 @@ __global__ void __launch_bounds__(ONE_WARPS * 32) one_cta_kernel(const __grid_co
         const int* from = a.mean_of_sequences ? s_head : s_n;
         divisor = (double)max(warp_sum(lane < a.units ? from[lane] : 0), 1);
     }
-    Sums s = {};
-    int n_seq = 1;
-    if ((a.by_sequence || a.mean_of_sequences) && u.begin < u.end)
-        sequence_sums(a, s_sums, s_n, u.first, u.count, &s, &n_seq);
-    const Total r = warp_total(a, unit_loss(a, u, s, n_seq, divisor));
+    Whole w = {};
+    if ((a.by_sequence || a.mean_of_sequences) && u.begin < u.end && u.seq < a.S)
+        w = sequence_sums(a, s_sums, s_n, u.first, u.count);
+    const Total r = warp_total(a, unit_loss(a, u, w.s, w.tokens, divisor));
     if (lane == 0) s_total[warp] = r;
     __syncthreads();
     if (warp == 0) {
@@ -452,7 +498,12 @@ __global__ void __launch_bounds__(ONE_WARPS * 32) one_cta_kernel(const __grid_co
     }
 }
 
-static int unit_count(const r3_policy* c) { return c->S + 1 + c->T / UNIT; }
+static int unit_shift(const r3_policy* c) {
+    int shift = 8;
+    while ((c->T >> shift) > MOST_UNITS) ++shift;
+    return shift;
+}
+static int unit_count(const r3_policy* c) { return c->S + 1 + (c->T >> unit_shift(c)); }
 
 static r3_status check(const r3_policy* c) {
     if (!c || c->T < 0 || c->S < 0 || c->T > (1 << 30) || c->S > (1 << 28)) return R3_ERR_INVALID_ARG;
@@ -475,6 +526,7 @@ extern "C" size_t r3_policy_loss_workspace_bytes(const r3_policy* c) {
     if (check(c) != R3_OK) return 0;
     const size_t units = (size_t)unit_count(c);
     return 256 + r3::round_up(units * sizeof(Sums), 256) + 2 * r3::round_up(units * sizeof(int), 256) +
+           r3::round_up(units * 2 * sizeof(int4), 256) +
            r3::round_up((units + WARPS - 1) / WARPS * sizeof(Total), 256);
 }
 
@@ -502,6 +554,7 @@ extern "C" r3_status r3_policy_loss(const r3_policy* c, const float* logp, const
     a.T = c->T;
     a.S = c->S;
     a.units = unit_count(c);
+    a.shift = unit_shift(c);
     a.by_sequence = c->ratio == R3_RATIO_SEQUENCE;
     a.mean_of_sequences = c->reduce == R3_REDUCE_SEQUENCE;
     a.adv_per_token = c->adv_per_token != 0;
@@ -541,17 +594,17 @@ extern "C" r3_status r3_policy_loss(const r3_policy* c, const float* logp, const
     ws += round_up((size_t)a.units * sizeof(int), 256);
     a.head = reinterpret_cast<int*>(ws);
     ws += round_up((size_t)a.units * sizeof(int), 256);
+    a.table = reinterpret_cast<int4*>(ws);
+    ws += round_up((size_t)a.units * 2 * sizeof(int4), 256);
     a.totals = reinterpret_cast<Total*>(ws);
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     if (a.units <= ONE_WARPS)
         return tc::launch_dependent(one_cta_kernel, dim3(1), dim3(32 * a.units), 0, cs, a) == cudaSuccess
                    ? R3_OK : R3_ERR_CUDA;
-    // a wave of resident CTAs at most, which go on to further units (the second wave of 25 CTAs made
-    // a million tokens take 43 us instead of 24)
-    const int ctas = (a.units + WARPS - 1) / WARPS;
-    const int first = ctas < 4 * sm_count() ? ctas : 4 * sm_count(), second = ctas < 2 * sm_count() ? ctas : 2 * sm_count();
-    if (tc::launch_dependent(sums_kernel, dim3(first), dim3(WARPS * 32), 0, cs, a) != cudaSuccess ||
-        tc::launch_dependent(loss_kernel, dim3(second), dim3(WARPS * 32), 0, cs, a) != cudaSuccess)
+    // a wave of resident CTAs at most, which go on to further units
+    const int ctas = (a.units + WARPS - 1) / WARPS, most = CTAS_PER_SM * sm_count(), grid = ctas < most ? ctas : most;
+    if (tc::launch_dependent(sums_kernel, dim3(grid), dim3(WARPS * 32), 0, cs, a) != cudaSuccess ||
+        tc::launch_dependent(loss_kernel, dim3(grid), dim3(WARPS * 32), 0, cs, a) != cudaSuccess)
         return R3_ERR_CUDA;
     return R3_OK;
 }

@@ -7,8 +7,9 @@ QUINTIC = (3.4445, -4.7750, 2.0315)
 
 
 def iterate(u, steps=5, coefs=None, eps=1e-7, operand=None):
-    """u [rows, cols] -> X after `steps`.  operand: rounds what enters a product (and the Gram matrix and its
-    polynomial as they are stored); X itself is carried without rounding."""
+    """u [rows, cols] -> X after `steps`.  operand: rounds what enters a product (and the Gram matrix as it is
+    stored); the last product is (a I + b A + c A^2) X, and what X loses as its operand is added, times a: X
+    itself is carried without rounding."""
     u = np.asarray(u, dtype=np.float64)
     flip = u.shape[0] > u.shape[1]
     x = u.T if flip else u
@@ -20,10 +21,10 @@ def iterate(u, steps=5, coefs=None, eps=1e-7, operand=None):
         A = h @ h.T
         if operand is not None:
             A = operand(A)
-        B = b * A + c * (A @ A)
+        B = a * np.eye(A.shape[0]) + b * A + c * (A @ A)
         if operand is not None:
             B = operand(B)
-        x = a * x + B @ h
+        x = B @ h + a * (x - h)
     return x.T if flip else x
 
 

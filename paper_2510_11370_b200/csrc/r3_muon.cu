@@ -32,20 +32,36 @@ constexpr int UK = 16;                    // k per tcgen05.mma
 constexpr int STAGES = 5;
 constexpr int OPERAND_BYTES = BM * BK * 2;
 constexpr int STAGE_BYTES = 2 * OPERAND_BYTES;
-constexpr int EPI_WARPS = 8;              // two per TMEM lane quadrant, every other 64 columns each
+constexpr int SEGMENT = 4;                // three products: k blocks whose sum stays in tensor memory
+constexpr int EPI_WARPS = 8;              // two per TMEM lane quadrant, half of the columns each
 constexpr int EPI_PLANE = 32 * 128;       // 32 rows x 64 columns of fp16
 constexpr int EPI_BYTES = EPI_WARPS * 2 * EPI_PLANE;
 constexpr int BAR_BYTES = 256;
 constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES + EPI_BYTES + BAR_BYTES;
-constexpr int THREADS = 32 * (2 + EPI_WARPS);
+constexpr int THREADS = 32 * (4 + EPI_WARPS);        // warp 0 copies, warp 1 multiplies, 2 and 3 fill their group
+// Three products: the epilogue keeps 128 sums a thread, so the register file is split anew between the
+// first four warps and the others; both shares together are what the launch had (checked before it).
+constexpr int CONTROL_REGS = 40, EPI_REGS = 232, LAUNCH_REGS = 168;
+static_assert(128 * CONTROL_REGS + 32 * EPI_WARPS * EPI_REGS <= THREADS * LAUNCH_REGS, "register split");
 constexpr int TMEM_COLS = 512;            // two accumulator stages of TILE columns
+constexpr int MAX_CLASSES = 4;            // shapes of a launch
 
-struct alignas(64) GemmArgs {
+enum Phase { GRAM, POLY, APPLY };
+// The matrices of one shape in a launch.
+struct alignas(64) ClassArgs {
     CUtensorMap a[2], b[2];               // operands, planes hi and lo
-    CUtensorMap in[2], out[2], mirror[2];
+    CUtensorMap out[2], mirror[2];
+    const __half* in[2];                  // POLY: A; APPLY with one product: X's lo plane in [0]
+    long long in_plane;                   // elements of a matrix there
+    int in_ld;
     int rows, cols;                       // of D
-    int tiles_n, tiles, items, kblocks;   // tiles: of one matrix
-    float alpha, beta;
+    int tiles_n, tiles, first_item, kblocks;         // tiles: of one matrix
+    int a_mn, b_mn;                       // the operand's rows in memory run along k
+};
+struct alignas(64) GemmArgs {
+    ClassArgs c[MAX_CLASSES];
+    int classes, items;
+    float alpha, beta, diag;
     int32_t* dev_status;
 };
 
@@ -54,36 +70,54 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t sr
                  ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// All stores but the last one have been read out of shared memory.
 __device__ __forceinline__ void bulk_wait_read() {
-    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
 }
 __device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 struct Tile {
-    int z, m, n;                          // matrix, tile row and column
+    int k, z, m, n;                       // class, matrix, tile row and column
 };
-// SYM: the tiles with m >= n, row by row.
-template <bool SYM> __device__ __forceinline__ Tile decode(const GemmArgs& g, int item) {
+// Symmetric results: the tiles with m >= n, row by row.
+template <int PHASE> __device__ __forceinline__ Tile decode(const GemmArgs& g, int item) {
     Tile t;
-    t.z = item / g.tiles;
-    const int r = item - t.z * g.tiles;
-    if (SYM) {
+    t.k = 0;
+#pragma unroll
+    for (int i = 1; i < MAX_CLASSES; ++i)
+        if (i < g.classes && item >= g.c[i].first_item) t.k = i;
+    const ClassArgs& c = g.c[t.k];
+    item -= c.first_item;
+    t.z = item / c.tiles;
+    const int r = item - t.z * c.tiles;
+    if (PHASE != APPLY) {
         int m = (int)((sqrtf(8.f * (float)r + 1.f) - 1.f) * 0.5f);
         while (m * (m + 1) / 2 > r) --m;
         while ((m + 1) * (m + 2) / 2 <= r) ++m;
         t.m = m;
         t.n = r - m * (m + 1) / 2;
     } else {
-        t.m = r / g.tiles_n;
-        t.n = r - t.m * g.tiles_n;
+        t.m = r / c.tiles_n;
+        t.n = r - t.m * c.tiles_n;
     }
     return t;
 }
+__device__ __forceinline__ void half8(const uint4& v, float (&f)[8]) {
+    const __half2* h = reinterpret_cast<const __half2*>(&v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 t = __half22float2(h[i]);
+        f[2 * i] = t.x;
+        f[2 * i + 1] = t.y;
+    }
+}
 
-// A_MN, B_MN: the operand's rows in memory run along k (its 128 rows or columns of a tile are consecutive
-// in memory); otherwise k is consecutive.  SYM: a symmetric result.  IN, OUT: planes of L and D.
-template <bool A_MN, bool B_MN, bool SYM, int IN, int OUT, int TERMS>
+// GRAM: A = X X^T.  POLY: B = a I + b A + c A^2.  APPLY: X = B X (one product: + a times X's lo plane, which
+// is no operand then).  TERMS: products per product.
+template <int PHASE, int TERMS>
 __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant__ GemmArgs g) {
+    constexpr bool SYM = PHASE != APPLY;
+    constexpr int OUT = SYM && TERMS == 1 ? 1 : 2;     // planes of D
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
@@ -93,11 +127,10 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
     auto empty_bar = [&](int s) { return bar0 + 8u * (STAGES + s); };
     auto tfull_bar = [&](int a) { return bar0 + 8u * (2 * STAGES + a); };
     auto tempty_bar = [&](int a) { return bar0 + 8u * (2 * STAGES + 2 + a); };
-    auto in_bar = [&](int w) { return bar0 + 8u * (2 * STAGES + 4 + w); };
     uint8_t* misc = base_ptr + STAGES * STAGE_BYTES + EPI_BYTES + 192;
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(misc);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 4);
-    static_assert(8 * (2 * STAGES + 4 + EPI_WARPS) <= 192, "barriers");
+    static_assert(8 * (2 * STAGES + 4) <= 192, "barriers");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
@@ -109,7 +142,6 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
             mbar_init(tfull_bar(a), 1);
             mbar_init(tempty_bar(a), 2 * EPI_WARPS);
         }
-        for (int w = 0; w < EPI_WARPS; ++w) mbar_init(in_bar(w), 1);
         *abort_flag = 0;
         fence_barrier_init();
     }
@@ -122,228 +154,288 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
     grid_launch_dependents();
     grid_dependency_wait();
 
-    if (warp == 0) {
-        // ------------------------------ TMA producer: this CTA's half of both operands ---------
-        if (lane == 0) {
-            int stage = 0;
-            uint32_t phase = 0;
-            bool ok = true;
-            for (int item = pair; ok && item < g.items; item += pairs) {
-                const Tile t = decode<SYM>(g, item);
-                const int m0 = t.m * TILE + (int)rank * BM, n0 = t.n * TILE + (int)rank * BM;
-                for (int term = 0; ok && term < TERMS; ++term) {
-                    // the small products first: an addition drops what lies below the running sum's
-                    // last place
-                    const CUtensorMap* am = &g.a[TERMS > 1 && term == 1];
-                    const CUtensorMap* bm = &g.b[TERMS > 1 && term == 0];
-                    for (int kb = 0; kb < g.kblocks; ++kb) {
-                        if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, g.dev_status)) {
+    // the k blocks of a tile go in segments, each with all of its products
+    auto segments = [&](const ClassArgs& c) { return TERMS == 1 ? 1 : (c.kblocks + SEGMENT - 1) / SEGMENT; };
+    auto seg_end = [&](const ClassArgs& c, int s) {
+        return TERMS == 1 ? c.kblocks : min(c.kblocks, (s + 1) * SEGMENT);
+    };
+    // a tile on the diagonal of A or of A^2 has the same rows on both sides: copied once
+    auto alike = [&](const Tile& t) { return TERMS == 1 && SYM && t.m == t.n; };
+
+    if (warp < 4) {
+        if constexpr (TERMS > 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CONTROL_REGS));
+        if (warp == 0) {
+            // ------------------------------ TMA producer: this CTA's half of both operands ---------
+            if (lane == 0) {
+                int stage = 0;
+                uint32_t phase = 0;
+                bool ok = true;
+                for (int item = pair; ok && item < g.items; item += pairs) {
+                    const Tile t = decode<PHASE>(g, item);
+                    const ClassArgs& c = g.c[t.k];
+                    const int m0 = t.m * TILE + (int)rank * BM, n0 = t.n * TILE + (int)rank * BM;
+                    const bool once = alike(t);
+                    const int n_seg = segments(c);
+                    for (int seg = 0; ok && seg < n_seg; ++seg) {
+                        const int k_end = seg_end(c, seg);
+                        for (int term = 0; ok && term < TERMS; ++term) {
+                            // the small products first: an addition drops what lies below the running sum's
+                            // last place
+                            const CUtensorMap* am = &c.a[TERMS > 1 && term == 1];
+                            const CUtensorMap* bm = &c.b[TERMS > 1 && term == 0];
+                            for (int kb = seg * SEGMENT; kb < k_end; ++kb) {
+                                if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, g.dev_status)) {
+                                    ok = false;
+                                    break;
+                                }
+                                const uint32_t sa = base + stage * STAGE_BYTES, sb = sa + OPERAND_BYTES;
+                                const uint32_t lead = mapa_shared(full_bar(stage), 0);
+                                if (rank == 0) mbar_expect_tx(full_bar(stage), (once ? 1u : 2u) * STAGE_BYTES);
+                                if (c.a_mn) {
+                                    tma_load_3d_pair(sa, am, m0, kb * BK, t.z, lead);
+                                    tma_load_3d_pair(sa + OPERAND_BYTES / 2, am, m0 + 64, kb * BK, t.z, lead);
+                                } else {
+                                    tma_load_3d_pair(sa, am, kb * BK, m0, t.z, lead);
+                                }
+                                if (once) {
+                                } else if (c.b_mn) {
+                                    tma_load_3d_pair(sb, bm, n0, kb * BK, t.z, lead);
+                                    tma_load_3d_pair(sb + OPERAND_BYTES / 2, bm, n0 + 64, kb * BK, t.z, lead);
+                                } else {
+                                    tma_load_3d_pair(sb, bm, kb * BK, n0, t.z, lead);
+                                }
+                                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                            }
+                        }
+                    }
+                }
+                // every stage's release has landed before this CTA may leave
+                for (int s = 0; ok && s < STAGES; ++s) {
+                    ok = mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, g.dev_status);
+                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                }
+            }
+        } else if (warp == 1) {
+            // ------------------------------ MMA issuer (leader CTA) ---------------------------------
+            if (rank == 0) {
+                int stage = 0, acc = 0;
+                uint32_t phase = 0, acc_phase = 0;
+                bool ok = true;
+                for (int item = pair; ok && item < g.items; item += pairs) {
+                    const Tile t = decode<PHASE>(g, item);
+                    const ClassArgs& c = g.c[t.k];
+                    const uint32_t idesc = (1u << 4) | ((uint32_t)(TILE >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24) |
+                                           (c.a_mn ? 1u << 15 : 0u) | (c.b_mn ? 1u << 16 : 0u);
+                    // 16 along k: 32 bytes inside the swizzled row, or two groups of 8 k rows
+                    const uint64_t a_step = c.a_mn ? (2048 >> 4) : 2, b_step = c.b_mn ? (2048 >> 4) : 2;
+                    const uint32_t to_b = alike(t) ? 0u : (uint32_t)OPERAND_BYTES;
+                    const int n_seg = segments(c);
+                    for (int seg = 0; ok && seg < n_seg; ++seg) {
+                        if (!__all_sync(0xffffffffu,
+                                        mbar_wait(tempty_bar(acc), acc_phase ^ 1u, abort_flag, g.dev_status))) {
                             ok = false;
                             break;
                         }
-                        const uint32_t sa = base + stage * STAGE_BYTES, sb = sa + OPERAND_BYTES;
-                        const uint32_t lead = mapa_shared(full_bar(stage), 0);
-                        if (rank == 0) mbar_expect_tx(full_bar(stage), 2u * STAGE_BYTES);
-                        if (A_MN) {
-                            tma_load_3d_pair(sa, am, m0, kb * BK, t.z, lead);
-                            tma_load_3d_pair(sa + OPERAND_BYTES / 2, am, m0 + 64, kb * BK, t.z, lead);
-                        } else {
-                            tma_load_3d_pair(sa, am, kb * BK, m0, t.z, lead);
-                        }
-                        if (B_MN) {
-                            tma_load_3d_pair(sb, bm, n0, kb * BK, t.z, lead);
-                            tma_load_3d_pair(sb + OPERAND_BYTES / 2, bm, n0 + 64, kb * BK, t.z, lead);
-                        } else {
-                            tma_load_3d_pair(sb, bm, kb * BK, n0, t.z, lead);
-                        }
-                        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-                    }
-                }
-            }
-            // every stage's release has landed before this CTA may leave
-            for (int s = 0; ok && s < STAGES; ++s) {
-                ok = mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, g.dev_status);
-                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-            }
-        }
-    } else if (warp == 1) {
-        // ------------------------------ MMA issuer (leader CTA) ---------------------------------
-        if (rank == 0) {
-            constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(TILE >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24) |
-                                       (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u);
-            // 16 along k: 32 bytes inside the swizzled row, or two groups of 8 k rows
-            constexpr uint64_t a_step = A_MN ? (2048 >> 4) : 2, b_step = B_MN ? (2048 >> 4) : 2;
-            int stage = 0, acc = 0;
-            uint32_t phase = 0, acc_phase = 0;
-            bool ok = true;
-            const int blocks = g.kblocks * TERMS;
-            for (int item = pair; ok && item < g.items; item += pairs) {
-                if (!__all_sync(0xffffffffu,
-                                mbar_wait(tempty_bar(acc), acc_phase ^ 1u, abort_flag, g.dev_status)))
-                    break;
-                tc_fence_after();
-                const uint32_t d_tmem = tmem_base + (uint32_t)(acc * TILE);
-                for (int kb = 0; kb < blocks; ++kb) {
-                    if (!__all_sync(0xffffffffu,
-                                    mbar_wait(full_bar(stage), phase, abort_flag, g.dev_status))) {
-                        ok = false;
-                        break;
-                    }
-                    tc_fence_after();
-                    if (elect_one()) {
-                        const uint32_t sa = base + stage * STAGE_BYTES, sb = sa + OPERAND_BYTES;
-                        const uint64_t da = A_MN ? smem_desc_mn_sw128(sa, OPERAND_BYTES / 2)
-                                                 : smem_desc_sw128(sa);
-                        const uint64_t db = B_MN ? smem_desc_mn_sw128(sb, OPERAND_BYTES / 2)
-                                                 : smem_desc_sw128(sb);
+                        tc_fence_after();
+                        const uint32_t d_tmem = tmem_base + (uint32_t)(acc * TILE);
+                        const int blocks = (seg_end(c, seg) - seg * SEGMENT) * TERMS;
+                        for (int kb = 0; kb < blocks; ++kb) {
+                            if (!__all_sync(0xffffffffu,
+                                            mbar_wait(full_bar(stage), phase, abort_flag, g.dev_status))) {
+                                ok = false;
+                                break;
+                            }
+                            tc_fence_after();
+                            if (elect_one()) {
+                                const uint32_t sa = base + stage * STAGE_BYTES, sb = sa + to_b;
+                                const uint64_t da = c.a_mn ? smem_desc_mn_sw128(sa, OPERAND_BYTES / 2)
+                                                           : smem_desc_sw128(sa);
+                                const uint64_t db = c.b_mn ? smem_desc_mn_sw128(sb, OPERAND_BYTES / 2)
+                                                           : smem_desc_sw128(sb);
 #pragma unroll
-                        for (int kk = 0; kk < BK / UK; ++kk)
-                            tc_mma_bf16_pair(d_tmem, da + a_step * kk, db + b_step * kk, idesc,
-                                             (kb | kk) != 0 ? 1u : 0u);
-                        tc_commit_pair(empty_bar(stage), 3);
+                                for (int kk = 0; kk < BK / UK; ++kk)
+                                    tc_mma_bf16_pair(d_tmem, da + a_step * kk, db + b_step * kk, idesc,
+                                                     (kb | kk) != 0 ? 1u : 0u);
+                                tc_commit_pair(empty_bar(stage), 3);
+                            }
+                            __syncwarp();
+                            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                        }
+                        if (!ok) break;
+                        if (elect_one()) tc_commit_pair(tfull_bar(acc), 3);
+                        __syncwarp();
+                        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
                     }
-                    __syncwarp();
-                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
                 }
-                if (!ok) break;
-                if (elect_one()) tc_commit_pair(tfull_bar(acc), 3);
-                __syncwarp();
-                if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
             }
         }
     } else {
         // ------------------------------ epilogue ------------------------------------------------
-        const int w = warp - 2, q = warp & 3, group = w >> 2;
+        if constexpr (TERMS > 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(EPI_REGS));
+        const int w = warp - 4, q = warp & 3, half = w >> 2;
         const uint32_t buf = epi0 + (uint32_t)w * (2 * EPI_PLANE);
         uint8_t* buf_ptr = base_ptr + STAGES * STAGE_BYTES + w * (2 * EPI_PLANE);
-        int acc = 0;
-        uint32_t acc_phase = 0, in_phase = 0;
+        int acc = 0, turn = 0;
+        uint32_t acc_phase = 0;
         bool alive = true;
-        for (int item = pair; item < g.items; item += pairs) {
-            const Tile t = decode<SYM>(g, item);
-            const int row0 = t.m * TILE + (int)rank * BM + q * 32;
-            // this warp's 64 columns that begin inside of D (with its rows)
-            const int c_end = row0 < g.rows ? min(TILE, g.cols - t.n * TILE) : 0;
-            auto fetch = [&](int c) {                  // L under columns c .. c + 63, by one lane
-                bulk_wait_read();                      // the last store out of this buffer
-                mbar_expect_tx(in_bar(w), IN * EPI_PLANE);
-#pragma unroll
-                for (int p = 0; p < IN; ++p)
-                    tma_load_3d(buf + p * EPI_PLANE, &g.in[p], t.n * TILE + c, row0, t.z, in_bar(w));
-            };
-            if (IN > 0 && alive && lane == 0 && group * 64 < c_end) fetch(group * 64);
-            if (alive) {
-                const bool ok = mbar_wait(tfull_bar(acc), acc_phase, abort_flag, g.dev_status);
-                alive = __all_sync(0xffffffffu, ok);
-            }
-            tc_fence_after();
-#pragma unroll 1
-            for (int c = group * 64; c < c_end; c += 128) {
-                const int col0 = t.n * TILE + c;
-                if (IN > 0) {
-                    if (alive && lane == 0 && c > group * 64) fetch(c);
-                    if (alive) {
-                        const bool ok = mbar_wait(in_bar(w), in_phase, abort_flag, g.dev_status);
-                        alive = __all_sync(0xffffffffu, ok);
-                        in_phase ^= 1u;
-                    }
-                }
-                if (!alive) continue;
-                if (IN == 0) {
-                    if (lane == 0) bulk_wait_read();
-                    __syncwarp();
-                }
-                const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * TILE + c);
-                uint32_t packed[OUT][32];              // pairs of columns
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    float v[32];
-                    tc_ld32(taddr + 32 * half, v);
-                    tc_wait_ld();
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        // eight columns: 16 bytes, at the place that the copy's swizzle gives them
-                        const int at = lane * 128 + (((half * 4 + j) ^ (lane & 7)) * 16);
-                        float l[8];
-                        if (IN > 0) {
-                            const uint4 x = *reinterpret_cast<const uint4*>(buf_ptr + at);
-                            const __half2* h = reinterpret_cast<const __half2*>(&x);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float2 f = __half22float2(h[i]);
-                                l[2 * i] = f.x;
-                                l[2 * i + 1] = f.y;
-                            }
-                        }
-                        if (IN > 1) {
-                            const uint4 x = *reinterpret_cast<const uint4*>(buf_ptr + EPI_PLANE + at);
-                            const __half2* h = reinterpret_cast<const __half2*>(&x);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float2 f = __half22float2(h[i]);
-                                l[2 * i] += f.x;
-                                l[2 * i + 1] += f.y;
-                            }
-                        }
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float d0 = g.alpha * v[8 * j + 2 * i], d1 = g.alpha * v[8 * j + 2 * i + 1];
-                            if (IN > 0) {
-                                d0 = fmaf(g.beta, l[2 * i], d0);
-                                d1 = fmaf(g.beta, l[2 * i + 1], d1);
-                            }
-                            const __half2 hi = __floats2half2_rn(d0, d1);
-                            packed[0][half * 16 + 4 * j + i] = *reinterpret_cast<const uint32_t*>(&hi);
-                            if constexpr (OUT > 1) {
-                                const float2 f = __half22float2(hi);
-                                const __half2 lo = __floats2half2_rn(d0 - f.x, d1 - f.y);
-                                packed[1][half * 16 + 4 * j + i] = *reinterpret_cast<const uint32_t*>(&lo);
-                            }
-                        }
-                    }
-                }
-#pragma unroll
-                for (int p = 0; p < OUT; ++p)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        *reinterpret_cast<uint4*>(buf_ptr + p * EPI_PLANE + lane * 128 + ((j ^ (lane & 7)) * 16)) =
-                            make_uint4(packed[p][4 * j], packed[p][4 * j + 1], packed[p][4 * j + 2],
-                                       packed[p][4 * j + 3]);
-                fence_async();
-                __syncwarp();
-                if (lane == 0) {
-#pragma unroll
-                    for (int p = 0; p < OUT; ++p)
-                        tma_store_3d(&g.out[p], buf + p * EPI_PLANE, col0, row0, t.z);
-                    bulk_commit();
-                }
-                if (SYM && t.m != t.n) {
-                    // the same values as 64 rows x 32 columns of the other triangle
-                    if (lane == 0) bulk_wait_read();
-                    __syncwarp();
-#pragma unroll
-                    for (int p = 0; p < OUT; ++p)
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            __half* to = reinterpret_cast<__half*>(buf_ptr + p * EPI_PLANE) + 2 * j * 32 + lane;
-                            const __half2 h = *reinterpret_cast<const __half2*>(&packed[p][j]);
-                            to[0] = __low2half(h);
-                            to[32] = __high2half(h);
-                        }
-                    fence_async();
-                    __syncwarp();
-                    if (lane == 0) {
-#pragma unroll
-                        for (int p = 0; p < OUT; ++p)
-                            tma_store_3d(&g.mirror[p], buf + p * EPI_PLANE, row0, col0, t.z);
-                        bulk_commit();
-                    }
-                }
-            }
-            tc_fence_before();
+        // 32 rows x 64 columns (a row's columns in pairs) to one of two buffers and out
+        auto emit = [&](const uint32_t (&v)[32], const CUtensorMap* map, int col0, int row0, int z) {
+            if (lane == 0) bulk_wait_read();
             __syncwarp();
-            if (lane == 0 && alive) mbar_arrive_cluster(mapa_shared(tempty_bar(acc), 0));
-            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            uint8_t* to = buf_ptr + turn * EPI_PLANE + lane * 128;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)                // at the places that the copy's swizzle gives them
+                *reinterpret_cast<uint4*>(to + ((j ^ (lane & 7)) * 16)) =
+                    make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            fence_async();
+            __syncwarp();
+            if (lane == 0) {
+                tma_store_3d(map, buf + turn * EPI_PLANE, col0, row0, z);
+                bulk_commit();
+            }
+            turn ^= 1;
+        };
+        // the same values as 64 rows x 32 columns of the other triangle
+        auto emit_mirror = [&](const uint32_t (&v)[32], const CUtensorMap* map, int col0, int row0, int z) {
+            if (lane == 0) bulk_wait_read();
+            __syncwarp();
+            __half* to = reinterpret_cast<__half*>(buf_ptr + turn * EPI_PLANE) + lane;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                const __half2 h = *reinterpret_cast<const __half2*>(&v[j]);
+                to[2 * j * 32] = __low2half(h);
+                to[2 * j * 32 + 32] = __high2half(h);
+            }
+            fence_async();
+            __syncwarp();
+            if (lane == 0) {
+                tma_store_3d(map, buf + turn * EPI_PLANE, row0, col0, z);
+                bulk_commit();
+            }
+            turn ^= 1;
+        };
+        for (int item = pair; item < g.items; item += pairs) {
+            const Tile t = decode<PHASE>(g, item);
+            const ClassArgs& c = g.c[t.k];
+            const int row0 = t.m * TILE + (int)rank * BM + q * 32, row = row0 + lane;
+            const int first = t.n * TILE + half * 128;           // this warp's 128 columns
+            const bool inside = row0 < c.rows && first < c.cols;
+            // what is added to the product comes while it is formed
+            constexpr int EARLY = TERMS == 1 && PHASE != GRAM ? 16 : 1;
+            uint4 early[EARLY];
+            const __half* in[2];
+            if (PHASE != GRAM) {
+                const long long at = (long long)t.z * c.in_plane + (long long)row * c.in_ld + first;
+                in[0] = c.in[0] + at;
+                in[1] = c.in[1] + at;
+            }
+            if (EARLY > 1) {
+#pragma unroll
+                for (int j = 0; j < EARLY; ++j)
+                    early[j] = row < c.rows && first + 8 * j < c.in_ld ? *reinterpret_cast<const uint4*>(in[0] + 8 * j)
+                                                                       : make_uint4(0u, 0u, 0u, 0u);
+            }
+            float sum[TERMS > 1 ? 128 : 1];            // of the segments
+            if constexpr (TERMS > 1) {
+#pragma unroll
+                for (int i = 0; i < 128; ++i) sum[i] = 0.f;
+            }
+            const int n_seg = segments(c);
+            uint32_t tacc = 0;
+#pragma unroll 1
+            for (int seg = 0; seg < n_seg; ++seg) {
+                if (alive) {
+                    const bool ok = mbar_wait(tfull_bar(acc), acc_phase, abort_flag, g.dev_status);
+                    alive = __all_sync(0xffffffffu, ok);
+                }
+                tc_fence_after();
+                tacc = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * TILE + half * 128);
+                if constexpr (TERMS > 1) {
+                    if (alive && inside) {
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) {
+                            float v[32];
+                            tc_ld32(tacc + 32 * p, v);
+                            tc_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) sum[32 * p + i] += v[i];
+                        }
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0 && alive) mbar_arrive_cluster(mapa_shared(tempty_bar(acc), 0));
+                    if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+                }
+            }
+            if (alive && inside) {
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const int col0 = first + 64 * p;
+                    if (col0 >= c.cols) continue;
+                    uint32_t packed[OUT][32];          // pairs of columns
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float v[32];
+                        if constexpr (TERMS > 1) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) v[i] = sum[64 * p + 32 * h + i];
+                        } else {
+                            tc_ld32(tacc + 64 * p + 32 * h, v);
+                            tc_wait_ld();
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int o = 8 * p + 4 * h + j;           // octet of columns within the 128
+                            float x[8], l[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) x[i] = g.alpha * v[8 * j + i];
+                            if (PHASE != GRAM && TERMS == 1) {
+                                half8(early[EARLY > 1 ? o : 0], l);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) x[i] = fmaf(g.beta, l[i], x[i]);
+                            } else if (PHASE == POLY) {
+                                uint4 hi = make_uint4(0u, 0u, 0u, 0u), lo = hi;
+                                if (row < c.rows && first + 8 * o < c.in_ld) {
+                                    hi = *reinterpret_cast<const uint4*>(in[0] + 8 * o);
+                                    lo = *reinterpret_cast<const uint4*>(in[1] + 8 * o);
+                                }
+                                float e[8];
+                                half8(hi, l);
+                                half8(lo, e);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) x[i] = fmaf(g.beta, l[i] + e[i], x[i]);
+                            }
+                            if (PHASE == POLY && t.m == t.n) {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i)
+                                    if (first + 8 * o + i == row) x[i] += g.diag;
+                            }
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const __half2 hi = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+                                packed[0][16 * h + 4 * j + i] = *reinterpret_cast<const uint32_t*>(&hi);
+                                if constexpr (OUT > 1) {
+                                    const float2 f = __half22float2(hi);
+                                    const __half2 lo = __floats2half2_rn(x[2 * i] - f.x, x[2 * i + 1] - f.y);
+                                    packed[1][16 * h + 4 * j + i] = *reinterpret_cast<const uint32_t*>(&lo);
+                                }
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int pl = 0; pl < OUT; ++pl) emit(packed[pl], &c.out[pl], col0, row0, t.z);
+                    if (SYM && t.m != t.n) {
+#pragma unroll
+                        for (int pl = 0; pl < OUT; ++pl) emit_mirror(packed[pl], &c.mirror[pl], col0, row0, t.z);
+                    }
+                }
+            }
+            if (TERMS == 1) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0 && alive) mbar_arrive_cluster(mapa_shared(tempty_bar(acc), 0));
+                if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            }
         }
         if (lane == 0) bulk_wait_all();
     }
@@ -367,79 +459,88 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
 constexpr int EL_THREADS = 256;
 constexpr int PIECE = EL_THREADS * 32;
 
-struct Stack {
+// Matrices of one stack in a launch.
+struct Part {
     void* param;                          // or the result of an orthogonalisation
     float* master;
     const void* grad;                     // or its input
     float* momentum;                      // null: none
-    int first;                            // number of its first matrix in the group
+    __half *hi, *lo;                      // their planes
+    double* norms;                        // [matrices, pieces]
+    long long first;                      // number of the first of their pieces in the launch
+    int rows, cols, ld, pieces;           // pieces: of one matrix
     float decay, scale;
 };
 struct ElemArgs {
-    int stacks, begin;                    // matrices from number `begin` of the group on
-    int rows, cols, ld, pieces;
-    long long plane;                      // elements of a matrix in the planes: rows * ld
-    int nesterov;
+    int parts, nesterov;
     float momentum, eps, lr;
-    const float* grad_scale;
-    const float* lr_now;
-    __half *hi, *lo;
-    double* norms;                        // [matrices, pieces]
-    Stack stack[MAX_STACKS];
+    const float *grad_scale, *lr_now;
+    Part part[MAX_STACKS];
 };
-
-__device__ __forceinline__ const Stack& find_stack(const ElemArgs& a, int matrix, int* within) {
+// The piece of a CTA: its stack and matrix, and the elements [p0, p1) of the matrix.
+struct Piece {
+    const Part* part;
+    int matrix, piece;
+    long long base, p0, p1;               // base: elements of the matrices before this one
+    bool wide;
+};
+__device__ __forceinline__ Piece find_piece(const ElemArgs& a) {
     int i = 0;
     for (int step = MAX_STACKS / 2; step > 0; step >>= 1)
-        if (i + step < a.stacks && a.stack[i + step].first <= matrix) i += step;
-    *within = matrix - a.stack[i].first;
-    return a.stack[i];
+        if (i + step < a.parts && a.part[i + step].first <= (long long)blockIdx.x) i += step;
+    Piece p;
+    p.part = &a.part[i];
+    const long long within = (long long)blockIdx.x - p.part->first;
+    p.matrix = (int)(within / p.part->pieces);
+    p.piece = (int)(within - (long long)p.matrix * p.part->pieces);
+    const long long size = (long long)p.part->rows * p.part->cols;
+    p.base = p.matrix * size;
+    p.p0 = (long long)p.piece * PIECE;
+    p.p1 = min(size, p.p0 + PIECE);
+    p.wide = p.part->cols % 8 == 0;
+    return p;
 }
-// First pass: the momentum's update and the sum of u^2 of every piece.  grid (pieces, matrices)
-template <typename G, bool WIDE>
+
+// First pass: the momentum's update and the sum of u^2 of every piece.
+template <typename G>
 __global__ void __launch_bounds__(EL_THREADS) norm_kernel(const __grid_constant__ ElemArgs a) {
     __shared__ double s_sum[EL_THREADS / 32];
     grid_launch_dependents();
     grid_dependency_wait();
-    int z;
-    const Stack& st = find_stack(a, a.begin + blockIdx.y, &z);
-    const long long size = (long long)a.rows * a.cols, base = (long long)z * size;
-    const G* grad = static_cast<const G*>(st.grad) + base;
-    float* mom = st.momentum ? st.momentum + base : nullptr;
+    const Piece p = find_piece(a);
+    const G* grad = static_cast<const G*>(p.part->grad) + p.base;
+    float* mom = p.part->momentum ? p.part->momentum + p.base : nullptr;
     float gs;
     const bool go = scale_of(a.grad_scale, &gs);
-    const long long p0 = (long long)blockIdx.x * PIECE, p1 = min(size, p0 + PIECE);
     double sum = 0.0;
-    if (go) {
-        if (WIDE) {
-#pragma unroll 2
-            for (long long i = p0 + threadIdx.x * 8; i < p1; i += EL_THREADS * 8) {
-                float g[8], m[8];
-                load8(grad + i, g);
-                if (mom) {
-                    load8(mom + i, m);
+    if (go && p.wide) {
+#pragma unroll 4
+        for (long long i = p.p0 + threadIdx.x * 8; i < p.p1; i += EL_THREADS * 8) {
+            float g[8], m[8];
+            load8(grad + i, g);
+            if (mom) {
+                load8(mom + i, m);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        m[k] = __fadd_rn(__fmul_rn(a.momentum, m[k]), __fmul_rn(g[k], gs));
-                    store8(mom + i, m);
-                }
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const double u = (double)direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[k], gs), m[k]);
-                    sum += u * u;
-                }
+                for (int k = 0; k < 8; ++k) m[k] = __fadd_rn(__fmul_rn(a.momentum, m[k]), __fmul_rn(g[k], gs));
+                store8(mom + i, m);
             }
-        } else {
-            for (long long i = p0 + threadIdx.x; i < p1; i += EL_THREADS) {
-                const float g = __fmul_rn(to_f32(grad[i]), gs);
-                float m = 0.f;
-                if (mom) {
-                    m = __fadd_rn(__fmul_rn(a.momentum, mom[i]), g);
-                    mom[i] = m;
-                }
-                const double u = (double)direction(a.nesterov, a.momentum, mom != nullptr, g, m);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const double u = (double)direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[k], gs), m[k]);
                 sum += u * u;
             }
+        }
+    } else if (go) {
+#pragma unroll 8
+        for (long long i = p.p0 + threadIdx.x; i < p.p1; i += EL_THREADS) {
+            const float g = __fmul_rn(to_f32(grad[i]), gs);
+            float m = 0.f;
+            if (mom) {
+                m = __fadd_rn(__fmul_rn(a.momentum, mom[i]), g);
+                mom[i] = m;
+            }
+            const double u = (double)direction(a.nesterov, a.momentum, mom != nullptr, g, m);
+            sum += u * u;
         }
     }
 #pragma unroll
@@ -449,25 +550,24 @@ __global__ void __launch_bounds__(EL_THREADS) norm_kernel(const __grid_constant_
     if (threadIdx.x == 0) {
         sum = 0.0;
         for (int i = 0; i < EL_THREADS / 32; ++i) sum += s_sum[i];
-        a.norms[(size_t)blockIdx.y * a.pieces + blockIdx.x] = sum;
+        p.part->norms[(size_t)p.matrix * p.part->pieces + p.piece] = sum;
     }
 }
 
 // Second pass: X = u / (|u| + eps) into the planes.
-template <typename G, bool WIDE>
+template <typename G>
 __global__ void __launch_bounds__(EL_THREADS) start_kernel(const __grid_constant__ ElemArgs a) {
     __shared__ double s_sum[EL_THREADS / 32];
     grid_launch_dependents();
     grid_dependency_wait();
-    int z;
-    const Stack& st = find_stack(a, a.begin + blockIdx.y, &z);
-    const long long size = (long long)a.rows * a.cols, base = (long long)z * size;
-    const G* grad = static_cast<const G*>(st.grad) + base;
-    const float* mom = st.momentum ? st.momentum + base : nullptr;
+    const Piece p = find_piece(a);
+    const G* grad = static_cast<const G*>(p.part->grad) + p.base;
+    const float* mom = p.part->momentum ? p.part->momentum + p.base : nullptr;
     float gs;
     if (!scale_of(a.grad_scale, &gs)) return;          // the step is skipped: the planes are not looked at
+    const int pieces = p.part->pieces;
     double sum = 0.0;
-    for (int i = threadIdx.x; i < a.pieces; i += EL_THREADS) sum += a.norms[(size_t)blockIdx.y * a.pieces + i];
+    for (int i = threadIdx.x; i < pieces; i += EL_THREADS) sum += p.part->norms[(size_t)p.matrix * pieces + i];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
@@ -476,12 +576,12 @@ __global__ void __launch_bounds__(EL_THREADS) start_kernel(const __grid_constant
 #pragma unroll
     for (int i = 0; i < EL_THREADS / 32; ++i) sum += s_sum[i];
     const float inv = start_scale(sum, a.eps);
-    __half* hi = a.hi + (size_t)blockIdx.y * a.plane;
-    __half* lo = a.lo + (size_t)blockIdx.y * a.plane;
-    const long long p0 = (long long)blockIdx.x * PIECE, p1 = min(size, p0 + PIECE);
-    if (WIDE) {
-#pragma unroll 2
-        for (long long i = p0 + threadIdx.x * 8; i < p1; i += EL_THREADS * 8) {
+    const int rows = p.part->rows, cols = p.part->cols, ld = p.part->ld;
+    __half* hi = p.part->hi + (long long)p.matrix * rows * ld;
+    __half* lo = p.part->lo + (long long)p.matrix * rows * ld;
+    if (p.wide) {
+#pragma unroll 4
+        for (long long i = p.p0 + threadIdx.x * 8; i < p.p1; i += EL_THREADS * 8) {
             float g[8], m[8];
             load8(grad + i, g);
             if (mom) load8(mom + i, m);
@@ -491,7 +591,8 @@ __global__ void __launch_bounds__(EL_THREADS) start_kernel(const __grid_constant
 #pragma unroll
             for (int k = 0; k < 8; k += 2) {
                 const float x0 = direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[k], gs), m[k]) * inv;
-                const float x1 = direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[k + 1], gs), m[k + 1]) * inv;
+                const float x1 =
+                    direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[k + 1], gs), m[k + 1]) * inv;
                 hp[k / 2] = __floats2half2_rn(x0, x1);
                 const float2 f = __half22float2(hp[k / 2]);
                 lp[k / 2] = __floats2half2_rn(x0 - f.x, x1 - f.y);
@@ -500,10 +601,12 @@ __global__ void __launch_bounds__(EL_THREADS) start_kernel(const __grid_constant
             *reinterpret_cast<uint4*>(lo + i) = l;
         }
     } else {
-        for (long long i = p0 + threadIdx.x; i < p1; i += EL_THREADS) {
+#pragma unroll 8
+        for (long long i = p.p0 + threadIdx.x; i < p.p1; i += EL_THREADS) {
             const float g = __fmul_rn(to_f32(grad[i]), gs);
             const float x = direction(a.nesterov, a.momentum, mom != nullptr, g, mom ? mom[i] : 0.f) * inv;
-            const long long r = i / a.cols, at = r * a.ld + (i - r * a.cols);
+            const int r = (int)((uint32_t)i / (uint32_t)cols);       // a matrix has 2^28 elements at most
+            const long long at = (long long)r * ld + (i - (long long)r * cols);
             const __half h = __float2half_rn(x);
             hi[at] = h;
             lo[at] = __float2half_rn(x - __half2float(h));
@@ -512,35 +615,28 @@ __global__ void __launch_bounds__(EL_THREADS) start_kernel(const __grid_constant
 }
 
 // Behind the iteration: the result, or the weights' update.
-template <typename P, bool MASTER, bool STEP, bool WIDE>
+template <typename P, bool MASTER, bool STEP>
 __global__ void __launch_bounds__(EL_THREADS) finish_kernel(const __grid_constant__ ElemArgs a) {
     grid_launch_dependents();
     grid_dependency_wait();
-    int z;
-    const Stack& st = find_stack(a, a.begin + blockIdx.y, &z);
-    const long long size = (long long)a.rows * a.cols, base = (long long)z * size;
+    const Piece p = find_piece(a);
     float gs;
     if (!scale_of(a.grad_scale, &gs)) return;
-    P* out = static_cast<P*>(st.param) + base;
-    float* master = MASTER ? st.master + base : nullptr;
-    const __half* hi = a.hi + (size_t)blockIdx.y * a.plane;
-    const __half* lo = a.lo + (size_t)blockIdx.y * a.plane;
+    P* out = static_cast<P*>(p.part->param) + p.base;
+    float* master = MASTER ? p.part->master + p.base : nullptr;
+    const int rows = p.part->rows, cols = p.part->cols, ld = p.part->ld;
+    const __half* hi = p.part->hi + (long long)p.matrix * rows * ld;
+    const __half* lo = p.part->lo + (long long)p.matrix * rows * ld;
     const float lr = a.lr_now ? *a.lr_now : a.lr;
-    const float keep = 1.f - lr * st.decay, rate = lr * st.scale * (1.f / SCALE);
-    const long long p0 = (long long)blockIdx.x * PIECE, p1 = min(size, p0 + PIECE);
-    if (WIDE) {
-#pragma unroll 2
-        for (long long i = p0 + threadIdx.x * 8; i < p1; i += EL_THREADS * 8) {
-            const uint4 h = *reinterpret_cast<const uint4*>(hi + i), l = *reinterpret_cast<const uint4*>(lo + i);
-            const __half2* hp = reinterpret_cast<const __half2*>(&h);
-            const __half2* lp = reinterpret_cast<const __half2*>(&l);
-            float w[8], o[8];
+    const float keep = 1.f - lr * p.part->decay, rate = lr * p.part->scale * (1.f / SCALE);
+    if (p.wide) {
+#pragma unroll 4
+        for (long long i = p.p0 + threadIdx.x * 8; i < p.p1; i += EL_THREADS * 8) {
+            float w[8], o[8], e[8];
+            half8(*reinterpret_cast<const uint4*>(hi + i), o);
+            half8(*reinterpret_cast<const uint4*>(lo + i), e);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float2 f = __half22float2(hp[k]), e = __half22float2(lp[k]);
-                o[2 * k] = f.x + e.x;
-                o[2 * k + 1] = f.y + e.y;
-            }
+            for (int k = 0; k < 8; ++k) o[k] += e[k];
             if (STEP) {
                 if (MASTER) load8(master + i, w);
                 else load8(out + i, w);
@@ -554,8 +650,10 @@ __global__ void __launch_bounds__(EL_THREADS) finish_kernel(const __grid_constan
             store8(out + i, w);
         }
     } else {
-        for (long long i = p0 + threadIdx.x; i < p1; i += EL_THREADS) {
-            const long long r = i / a.cols, at = r * a.ld + (i - r * a.cols);
+#pragma unroll 8
+        for (long long i = p.p0 + threadIdx.x; i < p.p1; i += EL_THREADS) {
+            const int r = (int)((uint32_t)i / (uint32_t)cols);
+            const long long at = (long long)r * ld + (i - (long long)r * cols);
             const float o = __half2float(hi[at]) + __half2float(lo[at]);
             float w = o * (1.f / SCALE);
             if (STEP) {
@@ -569,15 +667,15 @@ __global__ void __launch_bounds__(EL_THREADS) finish_kernel(const __grid_constan
 
 // ---- host side ------------------------------------------------------------------------------------
 constexpr int MAX_SIDE = 16384;
-constexpr int MAX_BATCH = 1 << 24, MAX_MATRICES = 1 << 27;          // (times the CTAs of a cluster: a grid's limit)
-constexpr size_t CHUNK_BYTES = 512u << 20;          // planes of a chunk, unless one matrix needs more
+constexpr int MAX_BATCH = 1 << 24, MAX_MATRICES = 1 << 27;   // (the latter times the CTAs of a cluster: a grid's limit)
+constexpr size_t ROUND_BYTES = 512u << 20;          // workspace of a round, unless one matrix needs more
 
 struct Coefs {
     int steps;
     float c[MAX_STEPS][3];
 };
 // The iteration's coefficients, if fp16 can hold its iterates: from singular values in [0, 1] on, X stays
-// within 16 and b A + c A^2 within 60 (a bound on the norm bounds every element).
+// within 16, A, b A + c A^2 and a + b A + c A^2 within 60 (a bound on the norm bounds every element).
 static bool read_coefs(int32_t steps, const double* given, Coefs* out) {
     if (steps < 1 || steps > MAX_STEPS) return false;
     out->steps = steps;
@@ -594,7 +692,7 @@ static bool read_coefs(int32_t steps, const double* given, Coefs* out) {
         for (int i = 0; i <= 256; ++i) {
             const double s = top * i / 256, t = s * s, p = b * t + c * t * t;
             next = std::fmax(next, std::fabs(s * (a + p)));
-            poly = std::fmax(poly, std::fabs(p));
+            poly = std::fmax(poly, std::fmax(std::fabs(p), std::fabs(a + p)));
         }
         if (!(next <= 16.0) || !(poly <= 60.0) || !(top * top <= 60.0)) return false;
         top = next;
@@ -619,7 +717,7 @@ static Problem problem_of(int rows, int cols, int terms) {
     p.pieces = (int)(((long long)rows * cols + PIECE - 1) / PIECE);
     return p;
 }
-// Bytes of `count` matrices in the workspace: X twice, A and B, sums.
+// Places of `count` matrices in the workspace: X twice, A and B, sums.
 struct Layout {
     size_t hi[2], lo[2], a[2], b[2], norms, total;
 };
@@ -644,13 +742,6 @@ static Layout layout(const Problem& p, long long count) {
     w.total = at;
     return w;
 }
-static int chunk_of(const Problem& p, long long count) {
-    const size_t one = layout(p, 1).total;
-    long long n = (long long)(CHUNK_BYTES / one);
-    if (n < 1) n = 1;
-    if (n > 32768) n = 32768;
-    return (int)(n < count ? n : count);
-}
 
 // fp16 tensor [count, rows, cols] with row stride ld.
 static bool make_map(CUtensorMap* m, const void* ptr, int count, int rows, int cols, int ld, int box_cols,
@@ -667,11 +758,13 @@ static bool make_map(CUtensorMap* m, const void* ptr, int count, int rows, int c
 }
 
 // CTA pairs of a kernel that can be resident at once (one CTA per SM), asked once per kernel and device.
-static int resident_pairs(void (*kern)(GemmArgs), int (&cached)[64]) {
+static int resident_pairs(void (*kern)(GemmArgs), bool split, int (&cached)[64]) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
     if (cached[dev] == 0) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES) != cudaSuccess)
+        cudaFuncAttributes attrs;
+        if (cudaFuncGetAttributes(&attrs, kern) != cudaSuccess || (split && attrs.numRegs < LAUNCH_REGS) ||
+            cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES) != cudaSuccess)
             return 0;
         cudaLaunchConfig_t cfg = {};
         cudaLaunchAttribute attr[1];
@@ -691,11 +784,10 @@ static int resident_pairs(void (*kern)(GemmArgs), int (&cached)[64]) {
     return cached[dev];
 }
 
-template <bool A_MN, bool B_MN, bool SYM, int IN, int OUT, int TERMS>
-static r3_status launch_gemm(const GemmArgs& g, cudaStream_t cs) {
-    auto kern = gemm_kernel<A_MN, B_MN, SYM, IN, OUT, TERMS>;
+template <int PHASE, int TERMS> static r3_status launch_gemm(const GemmArgs& g, cudaStream_t cs) {
+    auto kern = gemm_kernel<PHASE, TERMS>;
     static int cached[64] = {0};
-    const int pairs = resident_pairs(kern, cached);
+    const int pairs = resident_pairs(kern, TERMS > 1, cached);
     if (pairs <= 0) return R3_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
@@ -714,77 +806,107 @@ static r3_status launch_gemm(const GemmArgs& g, cudaStream_t cs) {
     return cudaLaunchKernelEx(&cfg, kern, g) == cudaSuccess ? R3_OK : R3_ERR_CUDA;
 }
 
-// The iteration on `count` matrices whose X stands in the planes 0; on return *at says which planes hold the
-// result.
+// The matrices of one shape in a round.
+struct Class {
+    Problem p;
+    int count;
+    uint8_t* ws;
+};
+
+// The iteration on classes whose X stand in the planes 0; on return *at says which planes hold the results.
 template <int TERMS>
-static r3_status iterate(const Problem& p, const Coefs& coefs, int count, uint8_t* ws, int32_t* dev_status,
-                         int* at, cudaStream_t cs) {
-    const Layout w = layout(p, count);
-    constexpr int PL = TERMS > 1 ? 2 : 1;            // planes of A and B
+static r3_status iterate(const Class* classes, int n, const Coefs& coefs, int32_t* dev_status, int* at,
+                         cudaStream_t cs) {
     GemmArgs gram[2], poly, apply[2];                // by the planes that hold X
-    const int tm = (p.m + TILE - 1) / TILE, tr = (p.rows + TILE - 1) / TILE, tc_ = (p.cols + TILE - 1) / TILE;
+    gram[0].items = gram[1].items = poly.items = apply[0].items = apply[1].items = 0;
     bool ok = true;
-    // an operand with consecutive k: 64 x 128 boxes; with k along the rows: 64 x 64, two per stage
-    for (int k = 0; k < 2; ++k) {
+    for (int i = 0; i < n; ++i) {
+        const Problem& p = classes[i].p;
+        const int count = classes[i].count;
+        const Layout w = layout(p, count);
+        uint8_t* ws = classes[i].ws;
+        const int tm = (p.m + TILE - 1) / TILE, tr = (p.rows + TILE - 1) / TILE, tc = (p.cols + TILE - 1) / TILE;
+        ClassArgs& q = poly.c[i];
+        // an operand with consecutive k: 64 x 128 boxes; with k along the rows: 64 x 64, two per stage
         for (int pl = 0; pl < 2; ++pl) {
-            const uint8_t* x = ws + (pl ? w.lo[k] : w.hi[k]);
-            const uint8_t* y = ws + (pl ? w.lo[k ^ 1] : w.hi[k ^ 1]);
             const uint8_t* A = ws + w.a[pl];
             const uint8_t* B = ws + w.b[pl];
-            CUtensorMap xk, xmn, bk;
-            ok = ok && make_map(&xk, x, count, p.rows, p.cols, p.ld, 64, BM, true) &&
-                 make_map(&xmn, x, count, p.rows, p.cols, p.ld, 64, BK, true) &&
-                 make_map(&bk, B, count, p.m, p.m, p.ldm, 64, BM, true);
-            gram[k].a[pl] = gram[k].b[pl] = p.tall ? xmn : xk;
-            ok = ok && make_map(&gram[k].out[pl], A, count, p.m, p.m, p.ldm, 64, 32, true) &&
-                 make_map(&gram[k].mirror[pl], A, count, p.m, p.m, p.ldm, 32, 64, false);
-            gram[k].in[pl] = gram[k].out[pl];
-            apply[k].a[pl] = p.tall ? xk : bk;
-            apply[k].b[pl] = p.tall ? bk : xmn;
-            ok = ok && make_map(&apply[k].in[pl], x, count, p.rows, p.cols, p.ld, 64, 32, true) &&
-                 make_map(&apply[k].out[pl], y, count, p.rows, p.cols, p.ld, 64, 32, true);
-            apply[k].mirror[pl] = apply[k].out[pl];
-            if (k == 0) {
-                ok = ok && make_map(&poly.a[pl], A, count, p.m, p.m, p.ldm, 64, BM, true) &&
-                     make_map(&poly.out[pl], B, count, p.m, p.m, p.ldm, 64, 32, true) &&
-                     make_map(&poly.mirror[pl], B, count, p.m, p.m, p.ldm, 32, 64, false);
-                poly.b[pl] = poly.a[pl];
-                poly.in[pl] = gram[k].out[pl];
+            CUtensorMap bk;
+            ok = ok && make_map(&q.a[pl], A, count, p.m, p.m, p.ldm, 64, BM, true) &&
+                 make_map(&bk, B, count, p.m, p.m, p.ldm, 64, BM, true) &&
+                 make_map(&q.out[pl], B, count, p.m, p.m, p.ldm, 64, 32, true) &&
+                 make_map(&q.mirror[pl], B, count, p.m, p.m, p.ldm, 32, 64, false);
+            q.b[pl] = q.a[pl];
+            q.in[pl] = reinterpret_cast<const __half*>(A);
+            for (int k = 0; k < 2; ++k) {
+                const uint8_t* x = ws + (pl ? w.lo[k] : w.hi[k]);
+                const uint8_t* y = ws + (pl ? w.lo[k ^ 1] : w.hi[k ^ 1]);
+                CUtensorMap xk, xmn;
+                ok = ok && make_map(&xk, x, count, p.rows, p.cols, p.ld, 64, BM, true) &&
+                     make_map(&xmn, x, count, p.rows, p.cols, p.ld, 64, BK, true);
+                ClassArgs& gr = gram[k].c[i];
+                gr.a[pl] = gr.b[pl] = p.tall ? xmn : xk;
+                if (k == 0)
+                    ok = ok && make_map(&gr.out[pl], A, count, p.m, p.m, p.ldm, 64, 32, true) &&
+                         make_map(&gr.mirror[pl], A, count, p.m, p.m, p.ldm, 32, 64, false);
+                else
+                    gr.out[pl] = gram[0].c[i].out[pl], gr.mirror[pl] = gram[0].c[i].mirror[pl];
+                gr.in[pl] = nullptr;
+                ClassArgs& ap = apply[k].c[i];
+                ap.a[pl] = p.tall ? xk : bk;
+                ap.b[pl] = p.tall ? bk : xmn;
+                ok = ok && make_map(&ap.out[pl], y, count, p.rows, p.cols, p.ld, 64, 32, true);
+                ap.mirror[pl] = ap.out[pl];
+                ap.in[pl] = reinterpret_cast<const __half*>(ws + w.lo[k]);
             }
         }
-        gram[k].rows = gram[k].cols = p.m;
-        gram[k].tiles_n = tm;
-        gram[k].tiles = tm * (tm + 1) / 2;
-        gram[k].kblocks = ((p.tall ? p.rows : p.cols) + BK - 1) / BK;
-        gram[k].alpha = 1.f / SCALE;
-        gram[k].beta = 0.f;
-        apply[k].rows = p.rows;
-        apply[k].cols = p.cols;
-        apply[k].tiles_n = tc_;
-        apply[k].tiles = tr * tc_;
-        apply[k].kblocks = (p.m + BK - 1) / BK;
-        apply[k].alpha = 1.f / SCALE;
+        auto square = [&](GemmArgs& g, int kblocks, bool mn) {
+            ClassArgs& c = g.c[i];
+            c.in_plane = (long long)p.m * p.ldm;
+            c.in_ld = p.ldm;
+            c.rows = c.cols = p.m;
+            c.tiles_n = tm;
+            c.tiles = tm * (tm + 1) / 2;
+            c.first_item = g.items;
+            c.kblocks = kblocks;
+            c.a_mn = c.b_mn = mn;
+            g.items += c.tiles * count;
+        };
+        const int km = (p.m + BK - 1) / BK;
+        square(poly, km, false);
+        for (int k = 0; k < 2; ++k) {
+            square(gram[k], ((p.tall ? p.rows : p.cols) + BK - 1) / BK, p.tall);
+            ClassArgs& c = apply[k].c[i];
+            c.in_plane = (long long)p.rows * p.ld;
+            c.in_ld = p.ld;
+            c.rows = p.rows;
+            c.cols = p.cols;
+            c.tiles_n = tc;
+            c.tiles = tr * tc;
+            c.first_item = apply[k].items;
+            c.kblocks = km;
+            c.a_mn = 0;
+            c.b_mn = !p.tall;
+            apply[k].items += c.tiles * count;
+        }
     }
     if (!ok) return R3_ERR_CUDA;
-    poly.rows = poly.cols = p.m;
-    poly.tiles_n = tm;
-    poly.tiles = tm * (tm + 1) / 2;
-    poly.kblocks = (p.m + BK - 1) / BK;
-    poly.items = gram[0].items = gram[1].items = poly.tiles * count;
-    apply[0].items = apply[1].items = apply[0].tiles * count;
-    poly.dev_status = gram[0].dev_status = gram[1].dev_status = dev_status;
-    apply[0].dev_status = apply[1].dev_status = dev_status;
+    for (GemmArgs* g : {&gram[0], &gram[1], &poly, &apply[0], &apply[1]}) {
+        g->classes = n;
+        g->alpha = 1.f / SCALE;
+        g->beta = g->diag = 0.f;
+        g->dev_status = dev_status;
+    }
     int k = 0;
     for (int step = 0; step < coefs.steps; ++step, k ^= 1) {
-        poly.beta = coefs.c[step][1];
-        poly.alpha = coefs.c[step][2] / SCALE;
-        apply[k].beta = coefs.c[step][0];
-        r3_status st = p.tall ? launch_gemm<true, true, true, 0, PL, TERMS>(gram[k], cs)
-                              : launch_gemm<false, false, true, 0, PL, TERMS>(gram[k], cs);
-        if (st == R3_OK) st = launch_gemm<false, false, true, PL, PL, TERMS>(poly, cs);
-        if (st == R3_OK)
-            st = p.tall ? launch_gemm<false, false, false, 2, 2, TERMS>(apply[k], cs)
-                        : launch_gemm<false, true, false, 2, 2, TERMS>(apply[k], cs);
+        const float *c = coefs.c[step];
+        poly.alpha = c[2] / SCALE;
+        poly.beta = c[1];
+        poly.diag = c[0] * SCALE;
+        apply[k].beta = c[0];
+        r3_status st = launch_gemm<GRAM, TERMS>(gram[k], cs);
+        if (st == R3_OK) st = launch_gemm<POLY, TERMS>(poly, cs);
+        if (st == R3_OK) st = launch_gemm<APPLY, TERMS>(apply[k], cs);
         if (st != R3_OK) return st;
     }
     *at = k;
@@ -797,8 +919,8 @@ struct Job {
     float momentum, eps, lr;
     const float *grad_scale, *lr_now;
 };
-static r3_status run_group_small(const Job& job, const Coefs& coefs, const r3_muon_stack* const* ss, int n,
-                                 int cluster, int matrices, int32_t* dev_status, cudaStream_t cs) {
+static r3_status run_small_stacks(const Job& job, const Coefs& coefs, const r3_muon_stack* const* ss, int n,
+                                  int cluster, int matrices, int32_t* dev_status, cudaStream_t cs) {
     SmallArgs a = {};
     a.stacks = n;
     a.cluster = cluster;
@@ -823,64 +945,175 @@ static r3_status run_group_small(const Job& job, const Coefs& coefs, const r3_mu
     }
     return run_small(a, job.terms, matrices, cs);
 }
-template <typename G, bool WIDE>
-static cudaError_t launch_front(const ElemArgs& a, dim3 grid, cudaStream_t cs) {
-    const cudaError_t e = launch_dependent(norm_kernel<G, WIDE>, grid, dim3(EL_THREADS), 0, cs, a);
-    return e == cudaSuccess ? launch_dependent(start_kernel<G, WIDE>, grid, dim3(EL_THREADS), 0, cs, a) : e;
-}
-template <typename P, bool MASTER, bool STEP>
-static cudaError_t launch_finish(const ElemArgs& a, bool wide, dim3 grid, cudaStream_t cs) {
-    return wide ? launch_dependent(finish_kernel<P, MASTER, STEP, true>, grid, dim3(EL_THREADS), 0, cs, a)
-                : launch_dependent(finish_kernel<P, MASTER, STEP, false>, grid, dim3(EL_THREADS), 0, cs, a);
-}
 
-// The stacks of one shape that stand in `a`, `count` matrices together.
-static r3_status run_group(const Job& job, const Coefs& coefs, const Problem& p, ElemArgs& a, int count,
-                           uint8_t* ws, int32_t* dev_status, cudaStream_t cs) {
-    const int chunk = chunk_of(p, count);
-    a.rows = p.rows;
-    a.cols = p.cols;
-    a.ld = p.ld;
-    a.pieces = p.pieces;
-    a.plane = (long long)p.rows * p.ld;
+// Matrices [begin, begin + count) of a stack, in class `cls` of the round as numbers `at` and on.
+struct Slice {
+    const r3_muon_stack* stack;
+    int begin, count, cls, at;
+};
+struct Round {
+    Class cls[MAX_CLASSES];
+    Slice slice[MAX_STACKS];
+    int classes = 0, slices = 0;
+    size_t bytes = 0;
+};
+static r3_status run_round(const Job& job, const Coefs& coefs, Round& r, uint8_t* ws, int32_t* dev_status,
+                           cudaStream_t cs) {
+    for (int i = 0; i < r.classes; ++i) {
+        r.cls[i].ws = ws;
+        ws += layout(r.cls[i].p, r.cls[i].count).total;
+    }
+    ElemArgs a = {};
+    a.parts = r.slices;
     a.nesterov = job.nesterov;
     a.momentum = job.momentum;
     a.eps = job.eps;
     a.lr = job.lr;
     a.grad_scale = job.grad_scale;
     a.lr_now = job.lr_now;
-    const bool wide = p.cols % 8 == 0;
-    for (int begin = 0; begin < count; begin += chunk) {
-        const int n = count - begin < chunk ? count - begin : chunk;
-        const Layout w = layout(p, n);
-        a.begin = begin;
-        a.hi = reinterpret_cast<__half*>(ws + w.hi[0]);
-        a.lo = reinterpret_cast<__half*>(ws + w.lo[0]);
-        a.norms = reinterpret_cast<double*>(ws + w.norms);
-        const dim3 grid(p.pieces, n);
-        cudaError_t e;
-        if (job.grad_dtype == R3_BF16)
-            e = wide ? launch_front<__nv_bfloat16, true>(a, grid, cs) : launch_front<__nv_bfloat16, false>(a, grid, cs);
-        else
-            e = wide ? launch_front<float, true>(a, grid, cs) : launch_front<float, false>(a, grid, cs);
-        if (e != cudaSuccess) return R3_ERR_CUDA;
-        int at = 0;
-        const r3_status st = job.terms > 1 ? iterate<3>(p, coefs, n, ws, dev_status, &at, cs)
-                                           : iterate<1>(p, coefs, n, ws, dev_status, &at, cs);
-        if (st != R3_OK) return st;
-        a.hi = reinterpret_cast<__half*>(ws + w.hi[at]);
-        a.lo = reinterpret_cast<__half*>(ws + w.lo[at]);
-        if (!job.step)
-            e = job.param_dtype == R3_BF16 ? launch_finish<__nv_bfloat16, false, false>(a, wide, grid, cs)
-                                           : launch_finish<float, false, false>(a, wide, grid, cs);
-        else if (job.param_dtype == R3_F32)
-            e = launch_finish<float, false, true>(a, wide, grid, cs);
-        else
-            e = job.master ? launch_finish<__nv_bfloat16, true, true>(a, wide, grid, cs)
-                           : launch_finish<__nv_bfloat16, false, true>(a, wide, grid, cs);
-        if (e != cudaSuccess) return R3_ERR_CUDA;
+    const size_t psize = job.param_dtype == R3_BF16 ? 2 : 4, gsize = job.grad_dtype == R3_BF16 ? 2 : 4;
+    long long pieces = 0;
+    for (int i = 0; i < r.slices; ++i) {
+        const Slice& s = r.slice[i];
+        const Problem& p = r.cls[s.cls].p;
+        const size_t off = (size_t)s.begin * p.rows * p.cols;
+        Part& t = a.part[i];
+        t.param = static_cast<uint8_t*>(s.stack->param) + off * psize;
+        t.master = s.stack->master ? s.stack->master + off : nullptr;
+        t.grad = static_cast<const uint8_t*>(s.stack->grad) + off * gsize;
+        t.momentum = s.stack->momentum ? s.stack->momentum + off : nullptr;
+        t.norms = reinterpret_cast<double*>(r.cls[s.cls].ws + layout(p, r.cls[s.cls].count).norms) +
+                  (size_t)s.at * p.pieces;
+        t.first = pieces;
+        t.rows = p.rows;
+        t.cols = p.cols;
+        t.ld = p.ld;
+        t.pieces = p.pieces;
+        t.decay = s.stack->weight_decay;
+        t.scale = s.stack->scale;
+        pieces += (long long)s.count * p.pieces;
     }
-    return R3_OK;
+    auto planes = [&](int at) {
+        for (int i = 0; i < r.slices; ++i) {
+            const Slice& s = r.slice[i];
+            const Class& c = r.cls[s.cls];
+            const Layout w = layout(c.p, c.count);
+            const size_t off = (size_t)s.at * c.p.rows * c.p.ld;
+            a.part[i].hi = reinterpret_cast<__half*>(c.ws + w.hi[at]) + off;
+            a.part[i].lo = reinterpret_cast<__half*>(c.ws + w.lo[at]) + off;
+        }
+    };
+    planes(0);
+    const dim3 grid((unsigned)pieces), block(EL_THREADS);
+    cudaError_t e;
+    if (job.grad_dtype == R3_BF16) {
+        e = launch_dependent(norm_kernel<__nv_bfloat16>, grid, block, 0, cs, a);
+        if (e == cudaSuccess) e = launch_dependent(start_kernel<__nv_bfloat16>, grid, block, 0, cs, a);
+    } else {
+        e = launch_dependent(norm_kernel<float>, grid, block, 0, cs, a);
+        if (e == cudaSuccess) e = launch_dependent(start_kernel<float>, grid, block, 0, cs, a);
+    }
+    if (e != cudaSuccess) return R3_ERR_CUDA;
+    int at = 0;
+    const r3_status st = job.terms > 1 ? iterate<3>(r.cls, r.classes, coefs, dev_status, &at, cs)
+                                       : iterate<1>(r.cls, r.classes, coefs, dev_status, &at, cs);
+    if (st != R3_OK) return st;
+    planes(at);
+    if (!job.step)
+        e = job.param_dtype == R3_BF16
+                ? launch_dependent(finish_kernel<__nv_bfloat16, false, false>, grid, block, 0, cs, a)
+                : launch_dependent(finish_kernel<float, false, false>, grid, block, 0, cs, a);
+    else if (job.param_dtype == R3_F32)
+        e = launch_dependent(finish_kernel<float, false, true>, grid, block, 0, cs, a);
+    else
+        e = job.master ? launch_dependent(finish_kernel<__nv_bfloat16, true, true>, grid, block, 0, cs, a)
+                       : launch_dependent(finish_kernel<__nv_bfloat16, false, true>, grid, block, 0, cs, a);
+    return e == cudaSuccess ? R3_OK : R3_ERR_CUDA;
+}
+
+// Cuts stacks into launches: small(members, n, cluster, matrices) for each group of the on-chip form, with as
+// many CTAs per matrix, round(r) for each round of the others: up to MAX_CLASSES shapes, MAX_STACKS stacks
+// and ROUND_BYTES of workspace (one matrix at least), shapes with long products first.
+template <typename Small, typename Big>
+static r3_status each_launch(const r3_muon_stack* ss, int32_t count, int terms, Small small, Big big) {
+    std::vector<const r3_muon_stack*> little, large;
+    for (int32_t i = 0; i < count; ++i)
+        if (ss[i].batch > 0) (small_cluster(ss[i].rows, ss[i].cols) ? little : large).push_back(ss + i);
+    std::stable_sort(little.begin(), little.end(), [](const r3_muon_stack* x, const r3_muon_stack* y) {
+        return small_cluster(x->rows, x->cols) < small_cluster(y->rows, y->cols);
+    });
+    for (size_t i = 0; i < little.size();) {
+        const int cluster = small_cluster(little[i]->rows, little[i]->cols);
+        size_t end = i;
+        long long matrices = 0;
+        for (; end < little.size() && end < i + MAX_STACKS &&
+               small_cluster(little[end]->rows, little[end]->cols) == cluster &&
+               matrices + little[end]->batch <= MAX_MATRICES; ++end)
+            matrices += little[end]->batch;
+        const r3_status st = small(little.data() + i, (int)(end - i), cluster, (int)matrices);
+        if (st != R3_OK) return st;
+        i = end;
+    }
+    std::stable_sort(large.begin(), large.end(), [](const r3_muon_stack* x, const r3_muon_stack* y) {
+        const int nx = std::max(x->rows, x->cols), ny = std::max(y->rows, y->cols);
+        return nx != ny ? nx > ny : x->rows != y->rows ? x->rows > y->rows : x->cols > y->cols;
+    });
+    Round r;
+    auto flush = [&]() {
+        const r3_status st = r.slices ? big(r) : R3_OK;
+        r = Round();
+        return st;
+    };
+    for (const r3_muon_stack* s : large) {
+        for (int begin = 0; begin < s->batch;) {
+            const Problem p = problem_of(s->rows, s->cols, terms);
+            const bool same = r.classes && r.cls[r.classes - 1].p.rows == s->rows && r.cls[r.classes - 1].p.cols == s->cols;
+            const long long here = same ? r.cls[r.classes - 1].count : 0;
+            const size_t before = r.bytes - (same ? layout(p, here).total : 0);
+            // as many of the stack's matrices as fit
+            long long n = 0;
+            if (r.slices < MAX_STACKS && (same || r.classes < MAX_CLASSES)) {
+                const size_t one = layout(p, 1).total;
+                const size_t room = ROUND_BYTES > r.bytes ? ROUND_BYTES - r.bytes : 0;
+                n = std::min<long long>((long long)(room / one), s->batch - begin);
+                if (n == 0 && r.slices == 0) n = 1;
+            }
+            if (n == 0) {
+                const r3_status st = flush();
+                if (st != R3_OK) return st;
+                continue;
+            }
+            if (!same) r.cls[r.classes++] = {p, 0, nullptr};
+            Class& c = r.cls[r.classes - 1];
+            r.slice[r.slices++] = {s, begin, (int)n, r.classes - 1, c.count};
+            c.count += (int)n;
+            r.bytes = before + layout(p, c.count).total;
+            begin += (int)n;
+        }
+    }
+    return flush();
+}
+// Workspace of the largest launch (0 without a matrix).
+static size_t workspace_bytes(const r3_muon_stack* ss, int32_t count, int terms) {
+    size_t most = 0;
+    each_launch(ss, count, terms,
+                [&](const r3_muon_stack* const*, int, int, int) {
+                    most = std::max(most, (size_t)256);
+                    return R3_OK;
+                },
+                [&](Round& r) {
+                    most = std::max(most, r.bytes);
+                    return R3_OK;
+                });
+    return most;
+}
+static r3_status run(const Job& job, const Coefs& coefs, const r3_muon_stack* ss, int32_t count, uint8_t* ws,
+                     int32_t* dev_status, cudaStream_t cs) {
+    return each_launch(ss, count, job.terms,
+                       [&](const r3_muon_stack* const* group, int n, int cluster, int matrices) {
+                           return run_small_stacks(job, coefs, group, n, cluster, matrices, dev_status, cs);
+                       },
+                       [&](Round& r) { return run_round(job, coefs, r, ws, dev_status, cs); });
 }
 
 static bool good_shape(int64_t batch, int64_t rows, int64_t cols) {
@@ -958,41 +1191,20 @@ static bool distinct(const r3_muon* c, const r3_muon_stack* ss, int32_t count, c
     return true;
 }
 
-// The shapes that one launch takes together: small ones by their CTAs per matrix, others each by itself.
-static uint64_t class_of(int rows, int cols) {
-    const int c = small_cluster(rows, cols);
-    return c ? (uint64_t)c : (uint64_t)rows << 32 | (uint32_t)cols;
-}
-// Calls f(members, n, matrices) for each group: stacks of one class, in their order, MAX_STACKS at most.
-template <typename F> static r3_status each_group(const r3_muon_stack* ss, int32_t count, F f) {
-    std::vector<int32_t> order;
-    for (int32_t i = 0; i < count; ++i)
-        if (ss[i].batch > 0) order.push_back(i);
-    auto shape = [&](int32_t i) { return class_of(ss[i].rows, ss[i].cols); };
-    std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) { return shape(x) < shape(y); });
-    for (size_t i = 0; i < order.size();) {
-        size_t end = i;
-        long long matrices = 0;
-        for (; end < order.size() && end < i + MAX_STACKS && shape(order[end]) == shape(order[i]) &&
-               matrices + ss[order[end]].batch <= MAX_MATRICES; ++end)
-            matrices += ss[order[end]].batch;
-        const r3_status st = f(order.data() + i, (int)(end - i), (int)matrices);
-        if (st != R3_OK) return st;
-        i = end;
-    }
-    return R3_OK;
-}
-
 }  // namespace ns
 }  // namespace r3
 
+// (host memory may run out: nothing of that leaves a C entry)
 extern "C" size_t r3_orthogonalize_workspace_bytes(const r3_orthogonal* c) {
     using namespace r3::ns;
     Coefs coefs;
-    if (check_ortho(c, &coefs) != R3_OK || c->batch == 0) return 0;
-    if (small_cluster(c->rows, c->cols)) return 256;
-    const Problem p = problem_of(c->rows, c->cols, c->products);
-    return layout(p, chunk_of(p, c->batch)).total;
+    if (check_ortho(c, &coefs) != R3_OK) return 0;
+    const r3_muon_stack one = {nullptr, nullptr, nullptr, nullptr, c->batch, c->rows, c->cols, 0.f, 0.f};
+    try {
+        return workspace_bytes(&one, 1, c->products);
+    } catch (...) {
+        return 0;
+    }
 }
 
 extern "C" r3_status r3_orthogonalize(const r3_orthogonal* c, const void* x, void* out, void* workspace,
@@ -1006,39 +1218,26 @@ extern "C" r3_status r3_orthogonalize(const r3_orthogonal* c, const void* x, voi
     if (!x || !out || !aligned(x, 16) || !aligned(out, 16) || !aligned(dev_status, 4)) return R3_ERR_INVALID_ARG;
     if (!workspace || !aligned(workspace, 256) || ws_bytes < r3_orthogonalize_workspace_bytes(c))
         return R3_ERR_WORKSPACE;
+    const r3_muon_stack one = {out, nullptr, x, nullptr, c->batch, c->rows, c->cols, 0.f, 0.f};
     const Job job = {c->out_dtype, c->in_dtype, 0, c->products, false, false, 0.f, (float)c->eps, 0.f, nullptr,
                      nullptr};
-    if (const int cluster = small_cluster(c->rows, c->cols)) {
-        const r3_muon_stack one = {out, nullptr, x, nullptr, c->batch, c->rows, c->cols, 0.f, 0.f};
-        const r3_muon_stack* ss[1] = {&one};
-        return run_group_small(job, coefs, ss, 1, cluster, c->batch, dev_status, static_cast<cudaStream_t>(stream));
+    try {
+        return run(job, coefs, &one, 1, static_cast<uint8_t*>(workspace), dev_status,
+                   static_cast<cudaStream_t>(stream));
+    } catch (...) {
+        return R3_ERR_INVALID_ARG;
     }
-    ElemArgs a = {};
-    a.stacks = 1;
-    a.stack[0] = {out, nullptr, x, nullptr, 0, 0.f, 0.f};
-    return run_group(job, coefs, problem_of(c->rows, c->cols, c->products), a, c->batch,
-                     static_cast<uint8_t*>(workspace), dev_status, static_cast<cudaStream_t>(stream));
 }
 
-// (host memory may run out: nothing of that leaves a C entry)
 extern "C" size_t r3_muon_workspace_bytes(const r3_muon* c, const r3_muon_stack* stacks, int32_t n_stacks) {
     using namespace r3::ns;
     Coefs coefs;
     if (check_muon(c, stacks, n_stacks, &coefs) != R3_OK) return 0;
-    size_t most = 0;
     try {
-        each_group(stacks, n_stacks, [&](const int32_t* members, int, int matrices) {
-            const r3_muon_stack& s = stacks[members[0]];
-            most = std::max(most, (size_t)256);
-            if (small_cluster(s.rows, s.cols)) return R3_OK;
-            const Problem p = problem_of(s.rows, s.cols, c->products);
-            most = std::max(most, layout(p, chunk_of(p, matrices)).total);
-            return R3_OK;
-        });
+        return workspace_bytes(stacks, n_stacks, c->products);
     } catch (...) {
         return 0;
     }
-    return most;
 }
 
 extern "C" r3_status r3_muon_step(const r3_muon* c, const r3_muon_stack* stacks, int32_t n_stacks,
@@ -1053,30 +1252,13 @@ extern "C" r3_status r3_muon_step(const r3_muon* c, const r3_muon_stack* stacks,
     if (!aligned(grad_scale, 4) || !aligned(lr, 4) || !aligned(dev_status, 4)) return R3_ERR_INVALID_ARG;
     try {
         if (!distinct(c, stacks, n_stacks, grad_scale, lr)) return R3_ERR_INVALID_ARG;
-        const size_t need = r3_muon_workspace_bytes(c, stacks, n_stacks);
+        const size_t need = workspace_bytes(stacks, n_stacks, c->products);
         if (need == 0) return R3_OK;                   // no matrices
         if (!workspace || !aligned(workspace, 256) || ws_bytes < need) return R3_ERR_WORKSPACE;
         const Job job = {c->param_dtype, c->grad_dtype, c->nesterov != 0, c->products, c->master != 0, true,
                          (float)c->momentum, (float)c->eps, (float)c->lr, grad_scale, lr};
-        return each_group(stacks, n_stacks, [&](const int32_t* members, int n, int matrices) {
-            const r3_muon_stack& one = stacks[members[0]];
-            if (const int cluster = small_cluster(one.rows, one.cols)) {
-                const r3_muon_stack* ss[MAX_STACKS];
-                for (int i = 0; i < n; ++i) ss[i] = stacks + members[i];
-                return run_group_small(job, coefs, ss, n, cluster, matrices, dev_status,
-                                       static_cast<cudaStream_t>(stream));
-            }
-            ElemArgs a = {};
-            a.stacks = n;
-            int first = 0;
-            for (int i = 0; i < n; ++i) {
-                const r3_muon_stack& s = stacks[members[i]];
-                a.stack[i] = {s.param, s.master, s.grad, s.momentum, first, s.weight_decay, s.scale};
-                first += s.batch;
-            }
-            return run_group(job, coefs, problem_of(one.rows, one.cols, c->products), a, matrices,
-                             static_cast<uint8_t*>(workspace), dev_status, static_cast<cudaStream_t>(stream));
-        });
+        return run(job, coefs, stacks, n_stacks, static_cast<uint8_t*>(workspace), dev_status,
+                   static_cast<cudaStream_t>(stream));
     } catch (...) {
         return R3_ERR_INVALID_ARG;
     }

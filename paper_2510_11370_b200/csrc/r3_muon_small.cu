@@ -6,15 +6,19 @@
 // planes in shared memory.  The same tiles (64 columns to a 128-byte row, swizzled) are the K-major operands of
 // X X^T and the MN-major operand of B X, so nothing is ever laid out again, and every product's epilogue
 // replaces its operand in place.  A is m x m: with more than one CTA the parts X_s X_s^T are added up through
-// distributed shared memory, each CTA a share of A's columns, which it then hands to all; b A + c A^2 is small
-// and every CTA forms it for itself.  Bound by latency: fifteen products with their barriers one after
-// the other.
+// distributed shared memory, each CTA a share of A's rows, which it then copies to all (whole rows: they lie
+// together, a copy takes 128 / C of them; as stores of single columns this took 14 us of a step's 26);
+// a I + b A + c A^2 is small and every CTA forms it for itself.
+// Bound by latency, fifteen products with their barriers one after the other, and, for three products, by
+// the tensor pipe of one SM: 9200 clocks of a step for 128 x 256, of 12000 in all.
 #include "r3_muon.cuh"
 
 namespace r3 {
 namespace ns {
 
-constexpr int SM_THREADS = 256;
+constexpr int SM_THREADS = 512;
+constexpr int SM_WARPS = SM_THREADS / 32;
+constexpr int SM_UNITS = 128 * SMALL_SLAB / 8 / SM_THREADS;      // octets of X per thread
 constexpr int SM_BLOCK = 128 * 128;           // bytes of 128 rows x 64 columns of fp16
 constexpr int SM_MISC = 512;
 
@@ -24,13 +28,14 @@ __device__ __forceinline__ void cluster_arrive() {
 __device__ __forceinline__ void cluster_wait() {
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void fence_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
 __device__ __forceinline__ void store_remote(uint32_t at, float4 v) {
     asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};"
                  ::"r"(at), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
-__device__ __forceinline__ void store_remote(uint32_t at, uint2 v) {
-    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(v.x), "r"(v.y) : "memory");
+// Shared memory of this CTA to that of another (or this) one; the bytes are counted on a barrier there.
+__device__ __forceinline__ void copy_remote(uint32_t to, uint32_t from, uint32_t bytes, uint32_t to_bar) {
+    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(to), "r"(from), "r"(bytes), "r"(to_bar) : "memory");
 }
 __device__ __forceinline__ void store_remote(uint32_t at, double v) {
     asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(at), "d"(v) : "memory");
@@ -86,7 +91,7 @@ __device__ __forceinline__ void get8(const void* p, int dtype, long long at, boo
 }
 
 template <int TERMS>
-__global__ void __launch_bounds__(SM_THREADS, 2) small_kernel(const __grid_constant__ SmallArgs a) {
+__global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_constant__ SmallArgs a) {
     constexpr int PL = TERMS > 1 ? 2 : 1;                // planes of A and B
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -97,12 +102,12 @@ __global__ void __launch_bounds__(SM_THREADS, 2) small_kernel(const __grid_const
     const uint32_t x_plane = (uint32_t)a.x_blocks * SM_BLOCK, a_plane = (uint32_t)a.a_blocks * SM_BLOCK;
     const uint32_t a0 = 2 * x_plane;                     // the A region, behind X's two planes
     uint8_t* misc = bp + a0 + a.a_bytes;
-    const uint32_t bar = base + a0 + a.a_bytes;
+    const uint32_t bar = base + a0 + a.a_bytes, a_bar = bar + 8;
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(misc + 16);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 20);
-    double* s_sum = reinterpret_cast<double*>(misc + 64);           // [8] warps
-    double* s_norm = reinterpret_cast<double*>(misc + 128);         // [16] CTAs
-    const uint32_t norm_at = base + a0 + a.a_bytes + 128;
+    double* s_sum = reinterpret_cast<double*>(misc + 64);           // [SM_WARPS]
+    double* s_norm = reinterpret_cast<double*>(misc + 192);         // [SMALL_CTAS]
+    const uint32_t norm_at = base + a0 + a.a_bytes + 192;
 
     const int matrix = blockIdx.x / C;
     int z = matrix, si = 0;
@@ -119,6 +124,7 @@ __global__ void __launch_bounds__(SM_THREADS, 2) small_kernel(const __grid_const
 
     if (threadIdx.x == 0) {
         mbar_init(bar, 1);
+        mbar_init(a_bar, 1);
         *abort_flag = 0;
         fence_barrier_init();
     }
@@ -143,24 +149,46 @@ __global__ void __launch_bounds__(SM_THREADS, 2) small_kernel(const __grid_const
         auto offset = [&](int i, int o) {
             return tall ? (long long)(j0 + 8 * o) * row + i : (long long)i * row + j0 + 8 * o;
         };
+        // this thread's octets: number u = threadIdx.x + SM_THREADS e of 128 rows x octets
+        auto place = [&](int e, int* i, int* o) {
+            const int u = threadIdx.x + SM_THREADS * e;
+            *i = tall ? u & 127 : u / octets;
+            *o = tall ? u >> 7 : u - *i * octets;
+            return u < 128 * octets && *i < m ? max(0, min(8, jn - 8 * *o)) : 0;       // its elements
+        };
         double sum = 0.0;
-        const int live = (jn + 7) >> 3;                  // octets with elements
-        for (int u = threadIdx.x; u < m * live; u += SM_THREADS) {
-            const int i = tall ? u % m : u / live, o = tall ? u / m : u % live;
-            const int valid = min(8, jn - 8 * o);
-            const long long at = offset(i, o);
-            float g[8], v[8];
-            get8(st.grad, a.grad_dtype, at0 + at, wide, hop, valid, g);
-            if (mom) {
-                get8(mom + at, wide, hop, valid, v);
+        float u[SM_UNITS][8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = __fadd_rn(__fmul_rn(a.momentum, v[k]), __fmul_rn(g[k], gs));
-                put8(mom + at, wide, hop, valid, v);
+        for (int e0 = 0; e0 < SM_UNITS; e0 += 2) {
+            float g[2][8], v[2][8];
+            int valid[2];
+            long long at[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                int i, o;
+                valid[e] = place(e0 + e, &i, &o);
+                at[e] = offset(i, o);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) g[e][k] = v[e][k] = 0.f;
+                if (valid[e] > 0) {
+                    get8(st.grad, a.grad_dtype, at0 + at[e], wide, hop, valid[e], g[e]);
+                    if (mom) get8(mom + at[e], wide, hop, valid[e], v[e]);
+                }
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const double x = (double)direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[k], gs), v[k]);
-                sum += x * x;
+            for (int e = 0; e < 2; ++e) {
+                if (mom) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        v[e][k] = __fadd_rn(__fmul_rn(a.momentum, v[e][k]), __fmul_rn(g[e][k], gs));
+                    if (valid[e] > 0) put8(mom + at[e], wide, hop, valid[e], v[e]);
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float x = direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[e][k], gs), v[e][k]);
+                    u[e0 + e][k] = x;
+                    sum += (double)x * (double)x;
+                }
             }
         }
 #pragma unroll
@@ -169,7 +197,7 @@ __global__ void __launch_bounds__(SM_THREADS, 2) small_kernel(const __grid_const
         __syncthreads();
         if (threadIdx.x < C) {
             sum = 0.0;
-            for (int i = 0; i < SM_THREADS / 32; ++i) sum += s_sum[i];
+            for (int i = 0; i < SM_WARPS; ++i) sum += s_sum[i];
             if (C > 1) store_remote(mapa_shared(norm_at + 8u * rank, threadIdx.x), sum);
             else s_norm[0] = sum;
         }
@@ -182,25 +210,18 @@ __global__ void __launch_bounds__(SM_THREADS, 2) small_kernel(const __grid_const
         sum = 0.0;
         for (int i = 0; i < C; ++i) sum += s_norm[i];
         const float inv = start_scale(sum, a.eps);
-        // ---- X = u / (|u| + eps) into the planes, zeros around it (its reads meet in L2) -----------
-        for (int u = threadIdx.x; u < 128 * octets; u += SM_THREADS) {
-            const int i = tall ? u & 127 : u / octets, o = tall ? u >> 7 : u % octets;
-            const int valid = i < m ? min(8, jn - 8 * o) : 0;
-            float g[8], v[8];
-            if (valid > 0) {
-                const long long at = offset(i, o);
-                get8(st.grad, a.grad_dtype, at0 + at, wide, hop, valid, g);
-                if (mom) get8(mom + at, wide, hop, valid, v);
+        // ---- X = u / (|u| + eps) into the planes, zeros around it ----------------------------------
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    g[k] = k < valid ? direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[k], gs), v[k]) * inv
-                                     : 0.f;
-            } else {
+        for (int e = 0; e < SM_UNITS; ++e) {
+            int i, o;
+            place(e, &i, &o);
+            if (threadIdx.x + SM_THREADS * e >= 128 * octets) break;
+            // (a product of zero and an infinite or undefined scale would leave NaN around the matrix)
+            const int valid = i < m ? jn - 8 * o : 0;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) g[k] = 0.f;
-            }
+            for (int k = 0; k < 8; ++k) u[e][k] = k < valid ? u[e][k] * inv : 0.f;
             uint4 hi, lo;
-            split8(g, &hi, &lo);
+            split8(u[e], &hi, &lo);
             const uint32_t t = tile_at(i, 8 * o);
             *reinterpret_cast<uint4*>(bp + t) = hi;
             *reinterpret_cast<uint4*>(bp + x_plane + t) = lo;
@@ -209,9 +230,9 @@ __global__ void __launch_bounds__(SM_THREADS, 2) small_kernel(const __grid_const
         __syncthreads();
 
         // ---- the iteration ---------------------------------------------------------------------------
-        const int q = warp & 3, half = warp >> 2, r = q * 32 + lane;      // this thread's row of every product
+        const int q = warp & 3, quarter = warp >> 2, r = q * 32 + lane;   // this thread's row of every product
         const uint32_t trow = tmem + ((uint32_t)(q * 32) << 16);
-        uint32_t phase = 0;
+        uint32_t phase = 0, a_phase = 0;
         bool alive = true;
         // D = P Q over k16 steps of 16 along k; plane choice by term, small products first
         auto multiply = [&](uint32_t p0, uint32_t p_plane, uint32_t q0, uint32_t q_plane, bool q_mn, int N, int k16) {
@@ -252,9 +273,8 @@ __global__ void __launch_bounds__(SM_THREADS, 2) small_kernel(const __grid_const
             // A = X X^T
             multiply(0, x_plane, 0, x_plane, false, m16, W >> 4);
             if (C == 1) {
-#pragma unroll 1
-                for (int c = half * 64; c < min(m16, half * 64 + 64); c += 32) {
-                    if (!alive) break;
+                const int c = quarter * 32;
+                if (alive && c < m16) {
                     float v[32];
                     tc_ld32(trow + c, v);
                     tc_wait_ld();
@@ -274,89 +294,85 @@ __global__ void __launch_bounds__(SM_THREADS, 2) small_kernel(const __grid_const
                 }
                 written();
             } else {
-                // parts to the owners of their columns: [source][4 columns][row], in the A region, once every
+                // parts to the owners of their rows: [source][4 columns][row], in the A region, once every
                 // CTA has its last product with B behind it
                 if (s > 0) cluster_wait();
-                const int share = 128 / C;               // columns per owner
-#pragma unroll 1
-                for (int c = half * 64; c < min(m16, half * 64 + 64); c += 32) {
-                    if (!alive) break;
+                const int share = 128 / C;               // rows per owner
+                const int c = quarter * 32;
+                if (alive && c < m16) {
                     float v[32];
                     tc_ld32(trow + c, v);
                     tc_wait_ld();
+                    const uint32_t to = mapa_shared(base + a0 + rank * (uint32_t)(share * 512), (uint32_t)(r / share));
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int col = c + 4 * j;
-                        const uint32_t to = base + a0 + rank * (uint32_t)(128 * share * 4) +
-                                            (uint32_t)((((col % share) >> 2) * 128 + r) * 16);
-                        if (col < m16)
-                            store_remote(mapa_shared(to, (uint32_t)(col / share)),
+                    for (int j = 0; j < 8; ++j)
+                        if (c + 4 * j < m16)
+                            store_remote(to + (uint32_t)(((c / 4 + j) * share + r % share) * 16),
                                          make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
-                    }
                 }
                 tc_fence_before();
                 __syncwarp();
                 cluster_sync_all();
-                uint2 hi[8], lo[8];                      // 128 * share / 4 / 256 of them, 8 at most
+                // the sums, as rows of the planes, to a place of their own: [plane][block][row]
+                const uint32_t rows_bytes = (uint32_t)share * 128u, staged = a0 + (uint32_t)(4 * SM_BLOCK);
+                for (int u = threadIdx.x; u < share * (m16 >> 3); u += SM_THREADS) {
+                    const int rr = u % share, o = u / share;
+                    float x[8] = {};
+                    for (int src = 0; src < C; ++src) {
+                        const float4* p = reinterpret_cast<const float4*>(bp + a0 + (uint32_t)(src * share * 512)) +
+                                          2 * o * share + rr;
+                        const float4 f = p[0], h = p[share];
+                        x[0] += f.x; x[1] += f.y; x[2] += f.z; x[3] += f.w;
+                        x[4] += h.x; x[5] += h.y; x[6] += h.z; x[7] += h.w;
+                    }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int u = threadIdx.x + e * SM_THREADS;
-                    if (u >= 32 * share) break;
-                    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if ((int)rank * share + 4 * (u >> 7) < m16)
-                        for (int src = 0; src < C; ++src) {
-                            const float4 p = *reinterpret_cast<const float4*>(
-                                bp + a0 + (uint32_t)src * (uint32_t)(128 * share * 4) + (uint32_t)u * 16u);
-                            t.x += p.x;
-                            t.y += p.y;
-                            t.z += p.z;
-                            t.w += p.w;
-                        }
-                    const __half2 h0 = __floats2half2_rn(t.x * (1.f / SCALE), t.y * (1.f / SCALE));
-                    const __half2 h1 = __floats2half2_rn(t.z * (1.f / SCALE), t.w * (1.f / SCALE));
-                    const float2 f0 = __half22float2(h0), f1 = __half22float2(h1);
-                    const __half2 l0 = __floats2half2_rn(t.x * (1.f / SCALE) - f0.x, t.y * (1.f / SCALE) - f0.y);
-                    const __half2 l1 = __floats2half2_rn(t.z * (1.f / SCALE) - f1.x, t.w * (1.f / SCALE) - f1.y);
-                    hi[e] = make_uint2(*reinterpret_cast<const uint32_t*>(&h0), *reinterpret_cast<const uint32_t*>(&h1));
-                    lo[e] = make_uint2(*reinterpret_cast<const uint32_t*>(&l0), *reinterpret_cast<const uint32_t*>(&l1));
+                    for (int k = 0; k < 8; ++k) x[k] *= 1.f / SCALE;
+                    uint4 hi, lo;
+                    split8(x, &hi, &lo);
+                    const uint32_t t = staged + (uint32_t)(o >> 3) * rows_bytes + (uint32_t)(rr * 128) +
+                                       (uint32_t)(((o & 7) ^ (rr & 7)) << 4);
+                    *reinterpret_cast<uint4*>(bp + t) = hi;
+                    if (PL > 1) *reinterpret_cast<uint4*>(bp + t + (uint32_t)a.a_blocks * rows_bytes) = lo;
                 }
+                fence_async();
                 __syncwarp();
                 cluster_sync_all();                      // every CTA has read its parts: A may stand there now
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int u = threadIdx.x + e * SM_THREADS;
-                    const int col = (int)rank * share + 4 * (u >> 7);
-                    if (u >= 32 * share || col >= m16) break;          // (behind m16 the planes may end)
-                    const uint32_t t = base + a0 + tile_at(u & 127, col);
-                    for (int to = 0; to < C; ++to) {
-                        store_remote(mapa_shared(t, (uint32_t)to), hi[e]);
-                        if (PL > 1) store_remote(mapa_shared(t + a_plane, (uint32_t)to), lo[e]);
+                if (warp == 0) {
+                    const int pieces = PL * a.a_blocks;  // times C copies: 32 at most
+                    if (lane == 0) mbar_expect_tx(a_bar, (uint32_t)(pieces * SM_BLOCK));
+                    if (lane < pieces * C) {
+                        const uint32_t to = (uint32_t)(lane % C), piece = (uint32_t)(lane / C);
+                        copy_remote(mapa_shared(base + a0 + piece * SM_BLOCK + rank * rows_bytes, to),
+                                    base + staged + piece * rows_bytes, rows_bytes, mapa_shared(a_bar, to));
                     }
+                    __syncwarp();
                 }
-                fence_async_all();
-                __syncwarp();
-                cluster_sync_all();
-                fence_async_all();
-                tc_fence_before();
-                __syncthreads();
+                if (alive) {
+                    const bool ok = mbar_wait(a_bar, a_phase, abort_flag, a.dev_status);
+                    alive = __all_sync(0xffffffffu, ok);
+                }
+                a_phase ^= 1u;
             }
-            // B = b A + c A^2, in A's place
+            // B = a I + b A + c A^2, in A's place
             multiply(a0, a_plane, a0, a_plane, false, m16, m16 >> 4);
-#pragma unroll 1
-            for (int c = half * 64; c < min(m16, half * 64 + 64); c += 32) {
-                if (!alive) break;
+            const int c_square = quarter * 32;
+            if (alive && c_square < m16) {
+                const int c = c_square;
                 float v[32];
                 tc_ld32(trow + c, v);
                 tc_wait_ld();
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    if (c + 8 * j >= m16) break;
+                    if (c + 8 * j >= m16) continue;
                     const uint32_t t = a0 + tile_at(r, c + 8 * j);
                     float x[8] = {};
                     add8(*reinterpret_cast<const uint4*>(bp + t), x);
                     if (PL > 1) add8(*reinterpret_cast<const uint4*>(bp + a_plane + t), x);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) x[k] = fmaf(cb, x[k], (cc / SCALE) * v[8 * j + k]);
+                    for (int k = 0; k < 8; ++k) {
+                        x[k] = fmaf(cb, x[k], (cc / SCALE) * v[8 * j + k]);
+                        if (c + 8 * j + k == r) x[k] += ca * SCALE;
+                    }
                     uint4 hi, lo;
                     split8(x, &hi, &lo);
                     *reinterpret_cast<uint4*>(bp + t) = hi;
@@ -364,25 +380,24 @@ __global__ void __launch_bounds__(SM_THREADS, 2) small_kernel(const __grid_const
                 }
             }
             written();
-            // X = a X + B X, in X's place
+            // X = B X, in X's place (one product: + a times the lo plane, which is no operand then)
             multiply(a0, a_plane, 0, x_plane, true, W, m16 >> 4);
             if (C > 1 && s + 1 < a.steps) {
                 __syncwarp();
                 cluster_arrive();                        // B is read: the next parts may come
             }
-#pragma unroll 1
-            for (int c = half * 128; c < min(W, half * 128 + 128); c += 32) {
-                if (!alive) break;
+#pragma unroll
+            for (int c = quarter * 64; c < quarter * 64 + 64; c += 32) {
+                if (!alive || c >= W) continue;
                 float v[32];
                 tc_ld32(trow + c, v);
                 tc_wait_ld();
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    if (c + 8 * j >= W) break;
+                    if (c + 8 * j >= W) continue;
                     const uint32_t t = tile_at(r, c + 8 * j);
                     float x[8] = {};
-                    add8(*reinterpret_cast<const uint4*>(bp + t), x);
-                    add8(*reinterpret_cast<const uint4*>(bp + x_plane + t), x);
+                    if (TERMS == 1) add8(*reinterpret_cast<const uint4*>(bp + x_plane + t), x);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) x[k] = fmaf(ca, x[k], (1.f / SCALE) * v[8 * j + k]);
                     uint4 hi, lo;
@@ -398,26 +413,37 @@ __global__ void __launch_bounds__(SM_THREADS, 2) small_kernel(const __grid_const
         const float lr = a.lr_now ? *a.lr_now : a.lr;
         const float keep = 1.f - lr * st.decay, rate = a.step ? lr * st.scale * (1.f / SCALE) : -(1.f / SCALE);
         float* master = st.master ? st.master + at0 : nullptr;
-        for (int u = threadIdx.x; u < m * live; u += SM_THREADS) {
-            const int i = tall ? u % m : u / live, o = tall ? u / m : u % live;
-            const int valid = min(8, jn - 8 * o);
-            const long long at = offset(i, o);
-            const uint32_t t = tile_at(i, 8 * o);
-            float x[8] = {}, w[8];
-            add8(*reinterpret_cast<const uint4*>(bp + t), x);
-            add8(*reinterpret_cast<const uint4*>(bp + x_plane + t), x);
-            if (a.step) {
-                if (master) get8(master + at, wide, hop, valid, w);
-                else get8(st.param, a.param_dtype, at0 + at, wide, hop, valid, w);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) w[k] = w[k] * keep - rate * x[k];
-                if (master) put8(master + at, wide, hop, valid, w);
-            } else {
+        for (int e0 = 0; e0 < SM_UNITS; e0 += 4) {
+            float w[4][8];
+            int valid[4];
+            long long at[4];
+            uint32_t t[4];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) w[k] = -rate * x[k];
+            for (int e = 0; e < 4; ++e) {
+                int i, o;
+                valid[e] = place(e0 + e, &i, &o);
+                at[e] = offset(i, o);
+                t[e] = tile_at(i, 8 * o);
+                if (a.step && valid[e] > 0) {
+                    if (master) get8(master + at[e], wide, hop, valid[e], w[e]);
+                    else get8(st.param, a.param_dtype, at0 + at[e], wide, hop, valid[e], w[e]);
+                }
             }
-            if (a.param_dtype == R3_BF16) put8(static_cast<__nv_bfloat16*>(st.param) + at0 + at, wide, hop, valid, w);
-            else put8(static_cast<float*>(st.param) + at0 + at, wide, hop, valid, w);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (valid[e] == 0) continue;
+                float x[8] = {};
+                add8(*reinterpret_cast<const uint4*>(bp + t[e]), x);
+                add8(*reinterpret_cast<const uint4*>(bp + x_plane + t[e]), x);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[e][k] = a.step ? w[e][k] * keep - rate * x[k] : -rate * x[k];
+                if (master) put8(master + at[e], wide, hop, valid[e], w[e]);
+                if (a.param_dtype == R3_BF16)
+                    put8(static_cast<__nv_bfloat16*>(st.param) + at0 + at[e], wide, hop, valid[e], w[e]);
+                else
+                    put8(static_cast<float*>(st.param) + at0 + at[e], wide, hop, valid[e], w[e]);
+            }
         }
     }
 
@@ -455,14 +481,16 @@ template <int TERMS> static r3_status launch_small(SmallArgs& a, int matrices, c
     }
     a.x_blocks = (slab + 63) / 64;
     a.a_blocks = (side + 63) / 64;
-    a.a_bytes = a.cluster > 1 ? 4 * SM_BLOCK : (TERMS > 1 ? 2 : 1) * a.a_blocks * SM_BLOCK;
+    // (several CTAs: the parts, 128 x 128 float32, and the sums of this CTA's rows)
+    a.a_bytes = a.cluster > 1 ? 4 * SM_BLOCK + (TERMS > 1 ? 2 : 1) * a.a_blocks * (SM_BLOCK / a.cluster)
+                              : (TERMS > 1 ? 2 : 1) * a.a_blocks * SM_BLOCK;
     a.tmem_cols = 32;
     while (a.tmem_cols < slab || a.tmem_cols < side) a.tmem_cols *= 2;
     const size_t smem = 1024 + 2 * (size_t)a.x_blocks * SM_BLOCK + a.a_bytes + SM_MISC;
     static PerDevice ready;
     if (!ready.done()) {
         if (cudaFuncSetAttribute(small_kernel<TERMS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 1024 + 12 * SM_BLOCK + SM_MISC) != cudaSuccess)
+                                 1024 + 14 * SM_BLOCK + SM_MISC) != cudaSuccess)
             return R3_ERR_CUDA;
         ready.mark();
     }

@@ -32,7 +32,7 @@ constexpr int UK = 16;                    // k per tcgen05.mma
 constexpr int STAGES = 5;
 constexpr int OPERAND_BYTES = BM * BK * 2;
 constexpr int STAGE_BYTES = 2 * OPERAND_BYTES;
-constexpr int SEGMENT = 4;                // three products: k blocks whose sum stays in tensor memory
+constexpr int SEGMENT = 1;                // three products: k blocks whose sum stays in tensor memory
 constexpr int EPI_WARPS = 8;              // two per TMEM lane quadrant, half of the columns each
 constexpr int EPI_PLANE = 32 * 128;       // 32 rows x 64 columns of fp16
 constexpr int EPI_BYTES = EPI_WARPS * 2 * EPI_PLANE;

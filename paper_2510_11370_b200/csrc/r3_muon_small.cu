@@ -64,30 +64,130 @@ __device__ __forceinline__ void add8(const uint4& v, float (&x)[8]) {
     }
 }
 
-// Eight elements, `step` apart, of which `valid` exist (the others read as 0); together where `wide`.
-template <typename T>
-__device__ __forceinline__ void get8(const T* p, bool wide, long long step, int valid, float (&f)[8]) {
-    if (wide) {
+// Eight elements: together (VEC), or `step` apart, of which `valid` exist (the others read as 0).
+template <bool VEC, typename T>
+__device__ __forceinline__ void get8(const T* p, int step, int valid, float (&f)[8]) {
+    if (VEC) {
         load8(p, f);
     } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] = k < valid ? to_f32(p[k * step]) : 0.f;
+        for (int k = 0; k < 8; ++k) f[k] = k < valid ? to_f32(p[(long long)k * step]) : 0.f;
     }
 }
-template <typename T>
-__device__ __forceinline__ void put8(T* p, bool wide, long long step, int valid, const float (&f)[8]) {
-    if (wide) {
+template <bool VEC, typename T>
+__device__ __forceinline__ void put8(T* p, int step, int valid, const float (&f)[8]) {
+    if (VEC) {
         store8(p, f);
     } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            if (k < valid) p[k * step] = from_f32<T>(f[k]);
+            if (k < valid) p[(long long)k * step] = from_f32<T>(f[k]);
     }
 }
-__device__ __forceinline__ void get8(const void* p, int dtype, long long at, bool wide, long long step, int valid,
-                                     float (&f)[8]) {
-    if (dtype == R3_BF16) get8(static_cast<const __nv_bfloat16*>(p) + at, wide, step, valid, f);
-    else get8(static_cast<const float*>(p) + at, wide, step, valid, f);
+// A thread's octets of X: numbers threadIdx.x + SM_THREADS e of 128 rows x `octets`, rows fastest where the
+// matrix in memory is tall.
+struct Octets {
+    int octets, m, jn, row;               // rows of X, columns in this CTA, elements of a row in memory
+    long long first;                      // elements before this CTA's first column
+    bool tall;
+    int i, o, hop_i, hop_o;
+    __device__ __forceinline__ void begin() {
+        const int u = threadIdx.x;
+        i = tall ? u & 127 : u / octets;
+        o = tall ? u >> 7 : u - i * octets;
+        hop_i = tall ? 0 : SM_THREADS / octets;
+        hop_o = tall ? SM_THREADS >> 7 : SM_THREADS - hop_i * octets;
+    }
+    __device__ __forceinline__ void next() {
+        i += hop_i;
+        o += hop_o;
+        if (!tall && o >= octets) {
+            o -= octets;
+            ++i;
+        }
+    }
+    __device__ __forceinline__ bool within() const { return i < 128 && o < octets; }
+    __device__ __forceinline__ int valid() const { return within() && i < m ? max(0, min(8, jn - 8 * o)) : 0; }
+    __device__ __forceinline__ long long at() const {
+        return tall ? first + (long long)(8 * o) * row + i : first + (long long)i * row + 8 * o;
+    }
+};
+// Reads them, updates the momentum, leaves u; returns the sum of u^2.  Two octets at a time are under way.
+template <bool VEC, typename G>
+__device__ __forceinline__ double read_octets(const SmallArgs& a, Octets w, const G* grad, float* mom, float gs,
+                                              float (&u)[SM_UNITS][8]) {
+    double sum = 0.0;
+    const int hop = w.tall ? w.row : 1;
+    w.begin();
+#pragma unroll
+    for (int e0 = 0; e0 < SM_UNITS; e0 += 2) {
+        int valid[2];
+        long long at[2];
+        float v[2][8];
+#pragma unroll
+        for (int e = 0; e < 2; ++e, w.next()) {
+            valid[e] = w.valid();
+            at[e] = w.at();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) u[e0 + e][k] = v[e][k] = 0.f;
+            if (valid[e] > 0) {
+                get8<VEC>(grad + at[e], hop, valid[e], u[e0 + e]);
+                if (mom) get8<VEC>(mom + at[e], hop, valid[e], v[e]);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            if (mom) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    v[e][k] = __fadd_rn(__fmul_rn(a.momentum, v[e][k]), __fmul_rn(u[e0 + e][k], gs));
+                if (valid[e] > 0) put8<VEC>(mom + at[e], hop, valid[e], v[e]);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float x =
+                    direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(u[e0 + e][k], gs), v[e][k]);
+                u[e0 + e][k] = x;
+                sum += (double)x * (double)x;
+            }
+        }
+    }
+    return sum;
+}
+// The result, or the weights' update, from the planes.
+template <bool VEC, typename P>
+__device__ __forceinline__ void write_octets(const SmallArgs& a, Octets w, const uint8_t* planes, uint32_t plane,
+                                             P* param, float* master, float keep, float rate) {
+    const int hop = w.tall ? w.row : 1;
+    w.begin();
+#pragma unroll
+    for (int e0 = 0; e0 < SM_UNITS; e0 += 4) {
+        int valid[4];
+        long long at[4];
+        uint32_t t[4];
+        float old[4][8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e, w.next()) {
+            valid[e] = w.valid();
+            at[e] = w.at();
+            t[e] = tile_at(w.i, 8 * w.o);
+            if (a.step && valid[e] > 0) {
+                if (master) get8<VEC>(master + at[e], hop, valid[e], old[e]);
+                else get8<VEC>(param + at[e], hop, valid[e], old[e]);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (valid[e] == 0) continue;
+            float x[8] = {};
+            add8(*reinterpret_cast<const uint4*>(planes + t[e]), x);
+            add8(*reinterpret_cast<const uint4*>(planes + plane + t[e]), x);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = a.step ? old[e][k] * keep - rate * x[k] : -rate * x[k];
+            if (master) put8<VEC>(master + at[e], hop, valid[e], x);
+            put8<VEC>(param + at[e], hop, valid[e], x);
+        }
+    }
 }
 
 template <int TERMS>
@@ -141,55 +241,24 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
     const bool go = scale_of(a.grad_scale, &gs);         // the same in every CTA
     if (go) {
         // ---- u = the direction, its norm; the momentum's update ------------------------------------
-        const long long size = (long long)st.rows * st.cols, at0 = (long long)z * size;
-        const long long row = st.cols;                   // elements of a row in memory
-        const bool wide = !tall && (st.cols & 7) == 0;
+        const long long at0 = (long long)z * st.rows * st.cols;
+        const bool vec = !tall && (st.cols & 7) == 0;
         float* mom = st.momentum ? st.momentum + at0 : nullptr;
-        const long long hop = tall ? row : 1;            // between the elements of an octet of X's columns
-        auto offset = [&](int i, int o) {
-            return tall ? (long long)(j0 + 8 * o) * row + i : (long long)i * row + j0 + 8 * o;
-        };
-        // this thread's octets: number u = threadIdx.x + SM_THREADS e of 128 rows x octets
-        auto place = [&](int e, int* i, int* o) {
-            const int u = threadIdx.x + SM_THREADS * e;
-            *i = tall ? u & 127 : u / octets;
-            *o = tall ? u >> 7 : u - *i * octets;
-            return u < 128 * octets && *i < m ? max(0, min(8, jn - 8 * *o)) : 0;       // its elements
-        };
-        double sum = 0.0;
+        Octets mine;
+        mine.octets = octets;
+        mine.m = m;
+        mine.jn = jn;
+        mine.row = st.cols;
+        mine.first = tall ? (long long)j0 * st.cols : j0;
+        mine.tall = tall;
         float u[SM_UNITS][8];
-#pragma unroll
-        for (int e0 = 0; e0 < SM_UNITS; e0 += 2) {
-            float g[2][8], v[2][8];
-            int valid[2];
-            long long at[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                int i, o;
-                valid[e] = place(e0 + e, &i, &o);
-                at[e] = offset(i, o);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) g[e][k] = v[e][k] = 0.f;
-                if (valid[e] > 0) {
-                    get8(st.grad, a.grad_dtype, at0 + at[e], wide, hop, valid[e], g[e]);
-                    if (mom) get8(mom + at[e], wide, hop, valid[e], v[e]);
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                if (mom) {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        v[e][k] = __fadd_rn(__fmul_rn(a.momentum, v[e][k]), __fmul_rn(g[e][k], gs));
-                    if (valid[e] > 0) put8(mom + at[e], wide, hop, valid[e], v[e]);
-                }
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float x = direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[e][k], gs), v[e][k]);
-                    u[e0 + e][k] = x;
-                    sum += (double)x * (double)x;
-                }
-            }
+        double sum;
+        if (a.grad_dtype == R3_BF16) {
+            const __nv_bfloat16* grad = static_cast<const __nv_bfloat16*>(st.grad) + at0;
+            sum = vec ? read_octets<true>(a, mine, grad, mom, gs, u) : read_octets<false>(a, mine, grad, mom, gs, u);
+        } else {
+            const float* grad = static_cast<const float*>(st.grad) + at0;
+            sum = vec ? read_octets<true>(a, mine, grad, mom, gs, u) : read_octets<false>(a, mine, grad, mom, gs, u);
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -211,18 +280,18 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
         for (int i = 0; i < C; ++i) sum += s_norm[i];
         const float inv = start_scale(sum, a.eps);
         // ---- X = u / (|u| + eps) into the planes, zeros around it ----------------------------------
+        Octets w = mine;
+        w.begin();
 #pragma unroll
-        for (int e = 0; e < SM_UNITS; ++e) {
-            int i, o;
-            place(e, &i, &o);
-            if (threadIdx.x + SM_THREADS * e >= 128 * octets) break;
+        for (int e = 0; e < SM_UNITS; ++e, w.next()) {
+            if (!w.within()) break;
             // (a product of zero and an infinite or undefined scale would leave NaN around the matrix)
-            const int valid = i < m ? jn - 8 * o : 0;
+            const int valid = w.valid();
 #pragma unroll
             for (int k = 0; k < 8; ++k) u[e][k] = k < valid ? u[e][k] * inv : 0.f;
             uint4 hi, lo;
             split8(u[e], &hi, &lo);
-            const uint32_t t = tile_at(i, 8 * o);
+            const uint32_t t = tile_at(w.i, 8 * w.o);
             *reinterpret_cast<uint4*>(bp + t) = hi;
             *reinterpret_cast<uint4*>(bp + x_plane + t) = lo;
         }
@@ -234,21 +303,26 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
         const uint32_t trow = tmem + ((uint32_t)(q * 32) << 16);
         uint32_t phase = 0, a_phase = 0;
         bool alive = true;
-        // D = P Q over k16 steps of 16 along k; plane choice by term, small products first
+        // D = P Q over k16 steps of 16 along k; plane choice by term, small products first.  Three products: every
+        // 64 of k have an accumulator of their own, N columns (to 32) further on, and the epilogue adds them up
+        // (an addition in tensor memory drops what lies below the running sum's last place).
         auto multiply = [&](uint32_t p0, uint32_t p_plane, uint32_t q0, uint32_t q_plane, bool q_mn, int N, int k16) {
             if (warp == 0) {
                 tc_fence_after();
                 if (alive && elect_one()) {
                     const uint32_t idesc = (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24) |
                                            (q_mn ? 1u << 16 : 0u);
+                    for (int seg = 0; seg < (TERMS > 1 ? k16 : 1); seg += 4)
                     for (int term = 0; term < TERMS; ++term) {
+                        const int k_end = TERMS > 1 ? min(k16, seg + 4) : k16;
                         const uint32_t p = base + p0 + (TERMS > 1 && term == 1 ? p_plane : 0u);
                         const uint32_t qq = base + q0 + (TERMS > 1 && term == 0 ? q_plane : 0u);
-                        for (int k = 0; k < k16; ++k) {
+                        for (int k = seg; k < k_end; ++k) {
                             const uint32_t in_row = (uint32_t)((k >> 2) * SM_BLOCK + (k & 3) * 32);
                             const uint64_t dq = q_mn ? smem_desc_mn_sw128(qq + (uint32_t)k * 2048u, SM_BLOCK)
                                                      : smem_desc_sw128(qq + in_row);
-                            tc_mma_bf16(tmem, smem_desc_sw128(p + in_row), dq, idesc, (term | k) != 0 ? 1u : 0u);
+                            tc_mma_bf16(tmem + (uint32_t)((seg >> 2) * ((N + 31) & ~31)), smem_desc_sw128(p + in_row), dq, idesc,
+                                        term != 0 || k != seg ? 1u : 0u);
                         }
                     }
                     tc_commit(bar);
@@ -261,6 +335,21 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
             }
             phase ^= 1u;
             tc_fence_after();
+        };
+        // 32 columns of this thread's row, the accumulators of k16 steps N columns apart added up
+        auto take = [&](int c, int N, int k16, float (&v)[32]) {
+            tc_ld32(trow + c, v);
+            tc_wait_ld();
+            if (TERMS > 1) {
+#pragma unroll 1
+                for (int seg = 4; seg < k16; seg += 4) {
+                    float more[32];
+                    tc_ld32(trow + c + (seg >> 2) * ((N + 31) & ~31), more);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) v[k] += more[k];
+                }
+            }
         };
         // the next product may read what this one's epilogue wrote
         auto written = [&]() {
@@ -276,8 +365,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
                 const int c = quarter * 32;
                 if (alive && c < m16) {
                     float v[32];
-                    tc_ld32(trow + c, v);
-                    tc_wait_ld();
+                    take(c, m16, W >> 4, v);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         float x[8];
@@ -301,8 +389,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
                 const int c = quarter * 32;
                 if (alive && c < m16) {
                     float v[32];
-                    tc_ld32(trow + c, v);
-                    tc_wait_ld();
+                    take(c, m16, W >> 4, v);
                     const uint32_t to = mapa_shared(base + a0 + rank * (uint32_t)(share * 512), (uint32_t)(r / share));
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
@@ -359,8 +446,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
             if (alive && c_square < m16) {
                 const int c = c_square;
                 float v[32];
-                tc_ld32(trow + c, v);
-                tc_wait_ld();
+                take(c, m16, m16 >> 4, v);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     if (c + 8 * j >= m16) continue;
@@ -390,8 +476,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
             for (int c = quarter * 64; c < quarter * 64 + 64; c += 32) {
                 if (!alive || c >= W) continue;
                 float v[32];
-                tc_ld32(trow + c, v);
-                tc_wait_ld();
+                take(c, W, m16 >> 4, v);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     if (c + 8 * j >= W) continue;
@@ -413,37 +498,14 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
         const float lr = a.lr_now ? *a.lr_now : a.lr;
         const float keep = 1.f - lr * st.decay, rate = a.step ? lr * st.scale * (1.f / SCALE) : -(1.f / SCALE);
         float* master = st.master ? st.master + at0 : nullptr;
-#pragma unroll
-        for (int e0 = 0; e0 < SM_UNITS; e0 += 4) {
-            float w[4][8];
-            int valid[4];
-            long long at[4];
-            uint32_t t[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                int i, o;
-                valid[e] = place(e0 + e, &i, &o);
-                at[e] = offset(i, o);
-                t[e] = tile_at(i, 8 * o);
-                if (a.step && valid[e] > 0) {
-                    if (master) get8(master + at[e], wide, hop, valid[e], w[e]);
-                    else get8(st.param, a.param_dtype, at0 + at[e], wide, hop, valid[e], w[e]);
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (valid[e] == 0) continue;
-                float x[8] = {};
-                add8(*reinterpret_cast<const uint4*>(bp + t[e]), x);
-                add8(*reinterpret_cast<const uint4*>(bp + x_plane + t[e]), x);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) w[e][k] = a.step ? w[e][k] * keep - rate * x[k] : -rate * x[k];
-                if (master) put8(master + at[e], wide, hop, valid[e], w[e]);
-                if (a.param_dtype == R3_BF16)
-                    put8(static_cast<__nv_bfloat16*>(st.param) + at0 + at[e], wide, hop, valid[e], w[e]);
-                else
-                    put8(static_cast<float*>(st.param) + at0 + at[e], wide, hop, valid[e], w[e]);
-            }
+        if (a.param_dtype == R3_BF16) {
+            __nv_bfloat16* param = static_cast<__nv_bfloat16*>(st.param) + at0;
+            if (vec) write_octets<true>(a, mine, bp, x_plane, param, master, keep, rate);
+            else write_octets<false>(a, mine, bp, x_plane, param, master, keep, rate);
+        } else {
+            float* param = static_cast<float*>(st.param) + at0;
+            if (vec) write_octets<true>(a, mine, bp, x_plane, param, master, keep, rate);
+            else write_octets<false>(a, mine, bp, x_plane, param, master, keep, rate);
         }
     }
 
@@ -484,8 +546,14 @@ template <int TERMS> static r3_status launch_small(SmallArgs& a, int matrices, c
     // (several CTAs: the parts, 128 x 128 float32, and the sums of this CTA's rows)
     a.a_bytes = a.cluster > 1 ? 4 * SM_BLOCK + (TERMS > 1 ? 2 : 1) * a.a_blocks * (SM_BLOCK / a.cluster)
                               : (TERMS > 1 ? 2 : 1) * a.a_blocks * SM_BLOCK;
+    // accumulators of up to 128 or 256 columns, one per 64 of k with three products: 512 columns at most
+    const int side32 = (side + 31) & ~31, slab32 = (slab + 31) & ~31;
+    const int by_slab = TERMS > 1 ? (slab + 63) / 64 : 1, by_side = TERMS > 1 ? (side32 + 63) / 64 : 1;
+    int cols = by_slab * side32;
+    if (by_side * side32 > cols) cols = by_side * side32;
+    if (by_side * slab32 > cols) cols = by_side * slab32;
     a.tmem_cols = 32;
-    while (a.tmem_cols < slab || a.tmem_cols < side) a.tmem_cols *= 2;
+    while (a.tmem_cols < cols) a.tmem_cols *= 2;
     const size_t smem = 1024 + 2 * (size_t)a.x_blocks * SM_BLOCK + a.a_bytes + SM_MISC;
     static PerDevice ready;
     if (!ready.done()) {

@@ -440,7 +440,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
                 }
                 a_phase ^= 1u;
             }
-            // B = a I + b A + c A^2, in A's place
+            // B = a I + b A + c A^2, in A's place (three products: without a I, a X is added in float32)
             multiply(a0, a_plane, a0, a_plane, false, m16, m16 >> 4);
             const int c_square = quarter * 32;
             if (alive && c_square < m16) {
@@ -457,7 +457,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         x[k] = fmaf(cb, x[k], (cc / SCALE) * v[8 * j + k]);
-                        if (c + 8 * j + k == r) x[k] += ca * SCALE;
+                        if (TERMS == 1 && c + 8 * j + k == r) x[k] += ca * SCALE;
                     }
                     uint4 hi, lo;
                     split8(x, &hi, &lo);
@@ -466,7 +466,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
                 }
             }
             written();
-            // X = B X, in X's place (one product: + a times the lo plane, which is no operand then)
+            // X = B X, in X's place (one product: + a times the lo plane, which is no operand then; three: + a X)
             multiply(a0, a_plane, 0, x_plane, true, W, m16 >> 4);
             if (C > 1 && s + 1 < a.steps) {
                 __syncwarp();
@@ -482,7 +482,8 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
                     if (c + 8 * j >= W) continue;
                     const uint32_t t = tile_at(r, c + 8 * j);
                     float x[8] = {};
-                    if (TERMS == 1) add8(*reinterpret_cast<const uint4*>(bp + x_plane + t), x);
+                    if (TERMS > 1) add8(*reinterpret_cast<const uint4*>(bp + t), x);
+                    add8(*reinterpret_cast<const uint4*>(bp + x_plane + t), x);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) x[k] = fmaf(ca, x[k], (1.f / SCALE) * v[8 * j + k]);
                     uint4 hi, lo;

@@ -29,15 +29,23 @@ constexpr int BM = 128;                   // rows of either operand per CTA and 
 constexpr int TILE = 2 * BM;              // output tile of a CTA pair: TILE x TILE
 constexpr int BK = 64;                    // k per stage: 64 fp16 = one 128-byte swizzle row
 constexpr int UK = 16;                    // k per tcgen05.mma
-constexpr int STAGES = 5;
 constexpr int OPERAND_BYTES = BM * BK * 2;
-constexpr int STAGE_BYTES = 2 * OPERAND_BYTES;
-constexpr int SEGMENT = 1;                // three products: k blocks whose sum stays in tensor memory
 constexpr int EPI_WARPS = 8;              // two per TMEM lane quadrant, half of the columns each
 constexpr int EPI_PLANE = 32 * 128;       // 32 rows x 64 columns of fp16
-constexpr int EPI_BYTES = EPI_WARPS * 2 * EPI_PLANE;
 constexpr int BAR_BYTES = 256;
-constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES + EPI_BYTES + BAR_BYTES;
+// By the products per product.  Three: a stage holds both planes of both operands, so that four tiles serve
+// three products (copied for each by itself they came out of L2 no faster than 60% of the tensor pipe could
+// take them), and the sum of a stage leaves tensor memory for registers, since an addition there drops what
+// lies below the running sum's last place.
+template <int TERMS> struct Ring {
+    static constexpr int PLANES = TERMS > 1 ? 2 : 1;
+    static constexpr int STAGES = TERMS > 1 ? 3 : 5;
+    static constexpr int SIDE_BYTES = PLANES * OPERAND_BYTES;            // one operand
+    static constexpr int STAGE_BYTES = 2 * SIDE_BYTES;
+    static constexpr int BUFFERS = TERMS > 1 ? 1 : 2;                    // of an epilogue warp
+    static constexpr int EPI_BYTES = EPI_WARPS * BUFFERS * EPI_PLANE;
+    static constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES + EPI_BYTES + BAR_BYTES;
+};
 constexpr int THREADS = 32 * (4 + EPI_WARPS);        // warp 0 copies, warp 1 multiplies, 2 and 3 fill their group
 // Three products: the epilogue keeps 128 sums a thread, so the register file is split anew between the
 // first four warps and the others; both shares together are what the launch had (checked before it).
@@ -70,9 +78,9 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t sr
                  ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-// All stores but the last one have been read out of shared memory.
-__device__ __forceinline__ void bulk_wait_read() {
-    asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+// All stores but the last ones have been read out of shared memory.
+template <int LAST> __device__ __forceinline__ void bulk_wait_read() {
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LAST) : "memory");
 }
 __device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
@@ -118,6 +126,9 @@ template <int PHASE, int TERMS>
 __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant__ GemmArgs g) {
     constexpr bool SYM = PHASE != APPLY;
     constexpr int OUT = SYM && TERMS == 1 ? 1 : 2;     // planes of D
+    using R = Ring<TERMS>;
+    constexpr int STAGES = R::STAGES, STAGE_BYTES = R::STAGE_BYTES, SIDE_BYTES = R::SIDE_BYTES;
+    constexpr int EPI_BYTES = R::EPI_BYTES, BUFFERS = R::BUFFERS;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
@@ -154,13 +165,8 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
     grid_launch_dependents();
     grid_dependency_wait();
 
-    // the k blocks of a tile go in segments, each with all of its products
-    auto segments = [&](const ClassArgs& c) { return TERMS == 1 ? 1 : (c.kblocks + SEGMENT - 1) / SEGMENT; };
-    auto seg_end = [&](const ClassArgs& c, int s) {
-        return TERMS == 1 ? c.kblocks : min(c.kblocks, (s + 1) * SEGMENT);
-    };
     // a tile on the diagonal of A or of A^2 has the same rows on both sides: copied once
-    auto alike = [&](const Tile& t) { return TERMS == 1 && SYM && t.m == t.n; };
+    auto alike = [&](const Tile& t) { return SYM && t.m == t.n; };
 
     if (warp < 4) {
         if constexpr (TERMS > 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CONTROL_REGS));
@@ -175,38 +181,32 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                     const ClassArgs& c = g.c[t.k];
                     const int m0 = t.m * TILE + (int)rank * BM, n0 = t.n * TILE + (int)rank * BM;
                     const bool once = alike(t);
-                    const int n_seg = segments(c);
-                    for (int seg = 0; ok && seg < n_seg; ++seg) {
-                        const int k_end = seg_end(c, seg);
-                        for (int term = 0; ok && term < TERMS; ++term) {
-                            // the small products first: an addition drops what lies below the running sum's
-                            // last place
-                            const CUtensorMap* am = &c.a[TERMS > 1 && term == 1];
-                            const CUtensorMap* bm = &c.b[TERMS > 1 && term == 0];
-                            for (int kb = seg * SEGMENT; kb < k_end; ++kb) {
-                                if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, g.dev_status)) {
-                                    ok = false;
-                                    break;
-                                }
-                                const uint32_t sa = base + stage * STAGE_BYTES, sb = sa + OPERAND_BYTES;
-                                const uint32_t lead = mapa_shared(full_bar(stage), 0);
-                                if (rank == 0) mbar_expect_tx(full_bar(stage), (once ? 1u : 2u) * STAGE_BYTES);
-                                if (c.a_mn) {
-                                    tma_load_3d_pair(sa, am, m0, kb * BK, t.z, lead);
-                                    tma_load_3d_pair(sa + OPERAND_BYTES / 2, am, m0 + 64, kb * BK, t.z, lead);
-                                } else {
-                                    tma_load_3d_pair(sa, am, kb * BK, m0, t.z, lead);
-                                }
-                                if (once) {
-                                } else if (c.b_mn) {
-                                    tma_load_3d_pair(sb, bm, n0, kb * BK, t.z, lead);
-                                    tma_load_3d_pair(sb + OPERAND_BYTES / 2, bm, n0 + 64, kb * BK, t.z, lead);
-                                } else {
-                                    tma_load_3d_pair(sb, bm, kb * BK, n0, t.z, lead);
-                                }
-                                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                    for (int kb = 0; kb < c.kblocks; ++kb) {
+                        if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, g.dev_status)) {
+                            ok = false;
+                            break;
+                        }
+                        const uint32_t sa = base + stage * STAGE_BYTES, sb = sa + SIDE_BYTES;
+                        const uint32_t lead = mapa_shared(full_bar(stage), 0);
+                        if (rank == 0) mbar_expect_tx(full_bar(stage), (once ? 1u : 2u) * STAGE_BYTES);
+#pragma unroll
+                        for (int pl = 0; pl < R::PLANES; ++pl) {
+                            const uint32_t ta = sa + pl * OPERAND_BYTES, tb = sb + pl * OPERAND_BYTES;
+                            if (c.a_mn) {
+                                tma_load_3d_pair(ta, &c.a[pl], m0, kb * BK, t.z, lead);
+                                tma_load_3d_pair(ta + OPERAND_BYTES / 2, &c.a[pl], m0 + 64, kb * BK, t.z, lead);
+                            } else {
+                                tma_load_3d_pair(ta, &c.a[pl], kb * BK, m0, t.z, lead);
+                            }
+                            if (once) continue;
+                            if (c.b_mn) {
+                                tma_load_3d_pair(tb, &c.b[pl], n0, kb * BK, t.z, lead);
+                                tma_load_3d_pair(tb + OPERAND_BYTES / 2, &c.b[pl], n0 + 64, kb * BK, t.z, lead);
+                            } else {
+                                tma_load_3d_pair(tb, &c.b[pl], kb * BK, n0, t.z, lead);
                             }
                         }
+                        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
                     }
                 }
                 // every stage's release has landed before this CTA may leave
@@ -228,43 +228,44 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                                            (c.a_mn ? 1u << 15 : 0u) | (c.b_mn ? 1u << 16 : 0u);
                     // 16 along k: 32 bytes inside the swizzled row, or two groups of 8 k rows
                     const uint64_t a_step = c.a_mn ? (2048 >> 4) : 2, b_step = c.b_mn ? (2048 >> 4) : 2;
-                    const uint32_t to_b = alike(t) ? 0u : (uint32_t)OPERAND_BYTES;
-                    const int n_seg = segments(c);
-                    for (int seg = 0; ok && seg < n_seg; ++seg) {
+                    const uint32_t to_b = alike(t) ? 0u : (uint32_t)SIDE_BYTES;
+                    for (int kb = 0; kb < c.kblocks; ++kb) {
+                        // three products: every k block has an accumulator of its own
+                        const bool fresh = TERMS > 1 || kb == 0, last = TERMS > 1 || kb + 1 == c.kblocks;
+                        if (fresh && !__all_sync(0xffffffffu, mbar_wait(tempty_bar(acc), acc_phase ^ 1u, abort_flag,
+                                                                        g.dev_status))) {
+                            ok = false;
+                            break;
+                        }
                         if (!__all_sync(0xffffffffu,
-                                        mbar_wait(tempty_bar(acc), acc_phase ^ 1u, abort_flag, g.dev_status))) {
+                                        mbar_wait(full_bar(stage), phase, abort_flag, g.dev_status))) {
                             ok = false;
                             break;
                         }
                         tc_fence_after();
-                        const uint32_t d_tmem = tmem_base + (uint32_t)(acc * TILE);
-                        const int blocks = (seg_end(c, seg) - seg * SEGMENT) * TERMS;
-                        for (int kb = 0; kb < blocks; ++kb) {
-                            if (!__all_sync(0xffffffffu,
-                                            mbar_wait(full_bar(stage), phase, abort_flag, g.dev_status))) {
-                                ok = false;
-                                break;
-                            }
-                            tc_fence_after();
-                            if (elect_one()) {
-                                const uint32_t sa = base + stage * STAGE_BYTES, sb = sa + to_b;
-                                const uint64_t da = c.a_mn ? smem_desc_mn_sw128(sa, OPERAND_BYTES / 2)
-                                                           : smem_desc_sw128(sa);
-                                const uint64_t db = c.b_mn ? smem_desc_mn_sw128(sb, OPERAND_BYTES / 2)
-                                                           : smem_desc_sw128(sb);
+                        if (elect_one()) {
+                            const uint32_t d_tmem = tmem_base + (uint32_t)(acc * TILE);
+                            const uint32_t sa = base + stage * STAGE_BYTES, sb = sa + to_b;
+                            const uint64_t da = c.a_mn ? smem_desc_mn_sw128(sa, OPERAND_BYTES / 2)
+                                                       : smem_desc_sw128(sa);
+                            const uint64_t db = c.b_mn ? smem_desc_mn_sw128(sb, OPERAND_BYTES / 2)
+                                                       : smem_desc_sw128(sb);
+#pragma unroll
+                            for (int term = 0; term < TERMS; ++term) {
+                                // (hi, lo), (lo, hi), (hi, hi): the small products first
+                                const uint64_t ta = da + (TERMS > 1 && term == 1 ? OPERAND_BYTES >> 4 : 0);
+                                const uint64_t tb = db + (TERMS > 1 && term == 0 ? OPERAND_BYTES >> 4 : 0);
 #pragma unroll
                                 for (int kk = 0; kk < BK / UK; ++kk)
-                                    tc_mma_bf16_pair(d_tmem, da + a_step * kk, db + b_step * kk, idesc,
-                                                     (kb | kk) != 0 ? 1u : 0u);
-                                tc_commit_pair(empty_bar(stage), 3);
+                                    tc_mma_bf16_pair(d_tmem, ta + a_step * kk, tb + b_step * kk, idesc,
+                                                     (fresh && (term | kk) == 0) ? 0u : 1u);
                             }
-                            __syncwarp();
-                            if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                            tc_commit_pair(empty_bar(stage), 3);
+                            if (last) tc_commit_pair(tfull_bar(acc), 3);
                         }
-                        if (!ok) break;
-                        if (elect_one()) tc_commit_pair(tfull_bar(acc), 3);
                         __syncwarp();
-                        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+                        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                        if (last && ++acc == 2) { acc = 0; acc_phase ^= 1u; }
                     }
                 }
             }
@@ -273,14 +274,14 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
         // ------------------------------ epilogue ------------------------------------------------
         if constexpr (TERMS > 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(EPI_REGS));
         const int w = warp - 4, q = warp & 3, half = w >> 2;
-        const uint32_t buf = epi0 + (uint32_t)w * (2 * EPI_PLANE);
-        uint8_t* buf_ptr = base_ptr + STAGES * STAGE_BYTES + w * (2 * EPI_PLANE);
+        const uint32_t buf = epi0 + (uint32_t)w * (BUFFERS * EPI_PLANE);
+        uint8_t* buf_ptr = base_ptr + STAGES * STAGE_BYTES + w * (BUFFERS * EPI_PLANE);
         int acc = 0, turn = 0;
         uint32_t acc_phase = 0;
         bool alive = true;
-        // 32 rows x 64 columns (a row's columns in pairs) to one of two buffers and out
+        // 32 rows x 64 columns (a row's columns in pairs) to a buffer and out
         auto emit = [&](const uint32_t (&v)[32], const CUtensorMap* map, int col0, int row0, int z) {
-            if (lane == 0) bulk_wait_read();
+            if (lane == 0) bulk_wait_read<BUFFERS - 1>();
             __syncwarp();
             uint8_t* to = buf_ptr + turn * EPI_PLANE + lane * 128;
 #pragma unroll
@@ -293,11 +294,11 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                 tma_store_3d(map, buf + turn * EPI_PLANE, col0, row0, z);
                 bulk_commit();
             }
-            turn ^= 1;
+            if (BUFFERS > 1) turn ^= 1;
         };
         // the same values as 64 rows x 32 columns of the other triangle
         auto emit_mirror = [&](const uint32_t (&v)[32], const CUtensorMap* map, int col0, int row0, int z) {
-            if (lane == 0) bulk_wait_read();
+            if (lane == 0) bulk_wait_read<BUFFERS - 1>();
             __syncwarp();
             __half* to = reinterpret_cast<__half*>(buf_ptr + turn * EPI_PLANE) + lane;
 #pragma unroll
@@ -312,7 +313,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                 tma_store_3d(map, buf + turn * EPI_PLANE, row0, col0, z);
                 bulk_commit();
             }
-            turn ^= 1;
+            if (BUFFERS > 1) turn ^= 1;
         };
         for (int item = pair; item < g.items; item += pairs) {
             const Tile t = decode<PHASE>(g, item);
@@ -335,15 +336,14 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                     early[j] = row < c.rows && first + 8 * j < c.in_ld ? *reinterpret_cast<const uint4*>(in[0] + 8 * j)
                                                                        : make_uint4(0u, 0u, 0u, 0u);
             }
-            float sum[TERMS > 1 ? 128 : 1];            // of the segments
+            float sum[TERMS > 1 ? 128 : 1];            // of the k blocks
             if constexpr (TERMS > 1) {
 #pragma unroll
                 for (int i = 0; i < 128; ++i) sum[i] = 0.f;
             }
-            const int n_seg = segments(c);
             uint32_t tacc = 0;
 #pragma unroll 1
-            for (int seg = 0; seg < n_seg; ++seg) {
+            for (int kb = 0; kb < (TERMS > 1 ? c.kblocks : 1); ++kb) {
                 if (alive) {
                     const bool ok = mbar_wait(tfull_bar(acc), acc_phase, abort_flag, g.dev_status);
                     alive = __all_sync(0xffffffffu, ok);
@@ -758,13 +758,13 @@ static bool make_map(CUtensorMap* m, const void* ptr, int count, int rows, int c
 }
 
 // CTA pairs of a kernel that can be resident at once (one CTA per SM), asked once per kernel and device.
-static int resident_pairs(void (*kern)(GemmArgs), bool split, int (&cached)[64]) {
+static int resident_pairs(void (*kern)(GemmArgs), bool split, int smem, int (&cached)[64]) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
     if (cached[dev] == 0) {
         cudaFuncAttributes attrs;
         if (cudaFuncGetAttributes(&attrs, kern) != cudaSuccess || (split && attrs.numRegs < LAUNCH_REGS) ||
-            cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES) != cudaSuccess)
+            cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
             return 0;
         cudaLaunchConfig_t cfg = {};
         cudaLaunchAttribute attr[1];
@@ -774,7 +774,7 @@ static int resident_pairs(void (*kern)(GemmArgs), bool split, int (&cached)[64])
         attr[0].val.clusterDim.z = 1;
         cfg.gridDim = dim3(2 * (sm_count() / 2));
         cfg.blockDim = dim3(THREADS);
-        cfg.dynamicSmemBytes = SMEM_BYTES;
+        cfg.dynamicSmemBytes = smem;
         cfg.attrs = attr;
         cfg.numAttrs = 1;
         int n = 0;
@@ -787,7 +787,7 @@ static int resident_pairs(void (*kern)(GemmArgs), bool split, int (&cached)[64])
 template <int PHASE, int TERMS> static r3_status launch_gemm(const GemmArgs& g, cudaStream_t cs) {
     auto kern = gemm_kernel<PHASE, TERMS>;
     static int cached[64] = {0};
-    const int pairs = resident_pairs(kern, TERMS > 1, cached);
+    const int pairs = resident_pairs(kern, TERMS > 1, Ring<TERMS>::SMEM_BYTES, cached);
     if (pairs <= 0) return R3_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
@@ -799,7 +799,7 @@ template <int PHASE, int TERMS> static r3_status launch_gemm(const GemmArgs& g, 
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.gridDim = dim3(2 * (g.items < pairs ? g.items : pairs));
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = SMEM_BYTES;
+    cfg.dynamicSmemBytes = Ring<TERMS>::SMEM_BYTES;
     cfg.stream = cs;
     cfg.attrs = attr;
     cfg.numAttrs = 2;

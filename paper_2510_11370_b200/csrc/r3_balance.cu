@@ -12,7 +12,7 @@
 // Main pass: a token's logits lie across G lanes, 8 each where the experts are many (a shuffle then serves
 // 32 / G tokens), so that its maximum, its sum and its product with f are shuffles; a lane keeps the f of its
 // experts and the sums of their probabilities in registers, and the next tokens' logits are under way while
-// these are worked on.  All resident CTAs take equal shares of the L T tokens, across the borders of blocks
+// these are worked on.  The first logits come into L2 while the choices are still counted.  All resident CTAs take equal shares of the L T tokens, across the borders of blocks
 // (grids of whole parts per block left a second wave of 32 CTAs for 48 blocks: 285 us against 150).  The last CTA of a
 // block to arrive adds up its probability sums, in an order that depends on the shape alone.
 #include <cmath>
@@ -31,6 +31,7 @@ constexpr int COUNT_CTAS = 8;             // CTAs of its clusters
 constexpr int THREADS = 512;
 constexpr int WARPS = THREADS / 32;
 constexpr int CTAS_PER_SM = 2;
+constexpr int EARLY_BYTES = 32 << 20;     // of logits that all CTAs fetch ahead: a part of L2
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct Args {
@@ -51,6 +52,22 @@ struct Args {
     unsigned* ticket;                     // [L]
     int32_t* dev_status;
 };
+// The hardware's approximations: 2^x and 1 / x within 2^-22 of the value, log2(x) within 2^-22 above 2.
+__device__ __forceinline__ float fast_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float fast_inverse(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float fast_log2(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 // The tokens of a CTA, as numbers of the L T; block l's first CTA and the number of its CTAs follow.
 __device__ __forceinline__ long long first_token(const Args& a, int cta) {
     return (long long)a.L * a.T * cta / a.grid;
@@ -68,9 +85,10 @@ __global__ void __launch_bounds__(COUNT_THREADS) count_kernel(const __grid_const
     extern __shared__ int s_count[];
     const int l = blockIdx.y, E = a.E, K = a.K;
     for (int e = threadIdx.x; e <= E; e += COUNT_THREADS) s_count[e] = 0;
-    tc::grid_launch_dependents();
     __syncthreads();
+    // the main pass may start once everything in front of this one is done: it reads logits and mask at once
     tc::grid_dependency_wait();
+    tc::grid_launch_dependents();
     if (blockIdx.x == 0 && threadIdx.x == 0) a.ticket[l] = 0;
     const int t0 = (int)min((long long)a.T, (long long)blockIdx.x * COUNT_TOKENS), t1 = min(a.T, t0 + COUNT_TOKENS);
     if (a.mask) {
@@ -118,12 +136,14 @@ __global__ void __launch_bounds__(COUNT_THREADS) count_kernel(const __grid_const
     const int rank = (int)tc::cluster_ctarank();
     for (int e = threadIdx.x * ctas + rank; e <= E; e += COUNT_THREADS * ctas) {
         int n = 0;
-        for (int c = 0; c < ctas; ++c) {
-            int v;
+        int v[COUNT_CTAS];                               // (all of them under way at once)
+#pragma unroll
+        for (int c = 0; c < COUNT_CTAS; ++c)
             asm volatile("ld.shared::cluster.s32 %0, [%1];"
-                         : "=r"(v) : "r"(tc::mapa_shared(tc::smem_u32(s_count + e), (uint32_t)c)) : "memory");
-            n += v;
-        }
+                         : "=r"(v[c])
+                         : "r"(tc::mapa_shared(tc::smem_u32(s_count + e), (uint32_t)min(c, ctas - 1))) : "memory");
+#pragma unroll
+        for (int c = 0; c < COUNT_CTAS; ++c) n += c < ctas ? v[c] : 0;
         out[e] = n;
     }
     __syncwarp();
@@ -174,7 +194,8 @@ template <int G, int V, bool WIDE>
 __global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_kernel(const __grid_constant__ Args a) {
     using R = Row<G, V, WIDE>;
     constexpr int ROWS = 32 / G;                       // tokens of a warp at a time
-    extern __shared__ float s_col[];                   // f, later [WARPS][E] sums of probabilities
+    extern __shared__ float s_n[];                     // [E] counts, then [WARPS][E] sums of probabilities
+    float* s_col = s_n + ((a.E + 3) & ~3);
     __shared__ long long s_sum[WARPS];
     __shared__ double s_z[WARPS], s_b[WARPS];
     __shared__ int s_tokens;
@@ -182,8 +203,15 @@ __global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_ker
     const int E = a.E, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int sub = lane % G, row = lane / G;
     tc::grid_launch_dependents();
-    tc::grid_dependency_wait();
     const long long begin = first_token(a, blockIdx.x), end = first_token(a, blockIdx.x + 1);
+    {
+        // while the choices are counted, this CTA's first logits come into L2
+        const char* from = reinterpret_cast<const char*>(a.logits + (size_t)begin * E);
+        const long long bytes = min((end - begin) * E * 4, (long long)(EARLY_BYTES / gridDim.x));
+        for (long long at = threadIdx.x * 128LL; at < bytes; at += THREADS * 128LL)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(from + at));
+    }
+    tc::grid_dependency_wait();
     // an empty batch: CTA 0 still writes the losses of every block
     const int l_first = a.T > 0 ? (int)(begin / a.T) : 0;
     const int l_past = a.T > 0 ? (end > begin ? (int)((end - 1) / a.T) + 1 : l_first) : a.L;
@@ -221,7 +249,7 @@ __global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_ker
             if (e == E) {
                 s_tokens = n;
             } else {
-                s_col[e] = (float)n;                   // below 2^24, or off by a rounding
+                s_n[e] = (float)n;                     // below 2^24, or off by a rounding
                 mine += n;
                 if (!a.given && a.counts && t0 == 0) a.counts[(size_t)l * E + e] = n;
             }
@@ -234,23 +262,27 @@ __global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_ker
 #pragma unroll
         for (int i = 0; i < WARPS; ++i) choices += s_sum[i];
         const int tokens = s_tokens;
-        const float per_choice = choices > 0 ? (float)((double)E / (double)choices) : 0.f;
+        const float per_choice = choices > 0 ? (float)E / (float)choices : 0.f;
         const float per_token = tokens > 0 ? 1.f / (float)tokens : 0.f;
-        float f[V], sum[V];
+        const float gb = a.balance_coef * per_token, gz = 2.f * a.z_coef * per_token;
+        float f[V], sum[V];                            // f: balance_coef f_i / N
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const int c = R::column(sub, j);
-            f[j] = c < E ? s_col[c] * per_choice : 0.f;
+            f[j] = c < E ? gb * (s_n[c] * per_choice) : 0.f;
             sum[j] = 0.f;
         }
-        __syncthreads();                               // s_col is used again below
-        const float gb = a.balance_coef * per_token, gz = 2.f * a.z_coef * per_token;
         float z = 0.f;                                 // of a few hundred tokens; the CTAs' are added in 64 bits
+#pragma unroll 2
         for (int t = t0 + warp * ROWS; t < t1; t += hop) {
             float v[V];
             const bool on = next_on;
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = on ? next[j] : -INFINITY;
+            for (int j = 0; j < V; ++j) v[j] = next[j];
+            if (a.mask && !on) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[j] = -INFINITY;
+            }
             if (t + hop < t1) fetch(t + hop);
             const int at = t + row;
             float top = v[0];
@@ -258,12 +290,13 @@ __global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_ker
             for (int j = 1; j < V; ++j) top = fmaxf(top, v[j]);
 #pragma unroll
             for (int o = G / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            // a token without any expert: all 0
-            const float from = top == -INFINITY ? 0.f : top;
+            // 2^(s log2(e) - from): from's own rounding is the same for all of a token's logits.  Where all of
+            // them are -inf (or below -1e38) every one gives 0
+            const float from = fmaxf(top, -1e38f) * LOG2E;
             float whole = 0.f, along = 0.f;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                v[j] = exp2f((v[j] - from) * LOG2E);
+                v[j] = fast_exp2(fmaf(v[j], LOG2E, -from));
                 whole += v[j];
                 along = fmaf(v[j], f[j], along);
             }
@@ -272,16 +305,15 @@ __global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_ker
                 whole += __shfl_xor_sync(0xffffffffu, whole, o);
                 along += __shfl_xor_sync(0xffffffffu, along, o);
             }
-            const float inv = whole != 0.f ? 1.f / whole : 0.f;
-            const float lse = whole != 0.f ? fmaf(LN2, log2f(whole), from) : 0.f;
-            along *= inv;
+            const float inv = whole != 0.f ? fast_inverse(whole) : 0.f;
+            const float lse = whole != 0.f ? LN2 * (from + fast_log2(whole)) : 0.f;
             z = fmaf(lse, lse, z);                     // 0 where the token does not count
-            const float shift = gz * lse - gb * along;
+            const float shift = fmaf(gz, lse, -along * inv);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const float p = v[j] * inv;
                 sum[j] += p;
-                v[j] = p * fmaf(gb, f[j], shift);
+                v[j] = p * (f[j] + shift);
             }
             if (dlogits && at < t1) {
                 float* out = dlogits + (size_t)at * E;
@@ -338,32 +370,21 @@ __global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_ker
         __threadfence();
         // sum_i counts_i sum_parts p: the parts' rows lie one after the other, every thread takes its share of
         // all their numbers
-        double balance = 0.0;
+        float share = 0.f;                             // (of a few dozen numbers; the threads' are added in 64 bits)
         const float* p = a.part_probs + ((size_t)c_first + l) * E;
-        auto count_at = [&](int c) {
-            if (a.given) return a.counts[(size_t)l * E + c];
-            const int32_t* cnt = a.part_counts + (size_t)l * a.count_parts * (E + 1) + c;
-            int n = 0;
-#pragma unroll 8
-            for (int q = 0; q < a.count_parts; ++q) n += cnt[(size_t)q * (E + 1)];
-            return n;
-        };
-        int32_t* s_n = reinterpret_cast<int32_t*>(s_col);
-        for (int c = threadIdx.x; c < E; c += THREADS) s_n[c] = count_at(c);
-        __syncthreads();
         if (WIDE) {
-            const int four = parts * (E / 4);
-#pragma unroll 8
+            const int wide = E / 4, four = parts * wide;
+#pragma unroll 10
             for (int i = threadIdx.x; i < four; i += THREADS) {
                 const float4 v = __ldcg(reinterpret_cast<const float4*>(p) + i);
-                const int c = i % (E / 4) * 4;
-                balance += (double)v.x * s_n[c] + (double)v.y * s_n[c + 1] + (double)v.z * s_n[c + 2] +
-                           (double)v.w * s_n[c + 3];
+                const float4 n = *reinterpret_cast<const float4*>(s_n + i % wide * 4);
+                share += v.x * n.x + v.y * n.y + v.z * n.z + v.w * n.w;
             }
         } else {
-#pragma unroll 8
-            for (int i = threadIdx.x; i < parts * E; i += THREADS) balance += (double)__ldcg(p + i) * s_n[i % E];
+#pragma unroll 10
+            for (int i = threadIdx.x; i < parts * E; i += THREADS) share += __ldcg(p + i) * s_n[i % E];
         }
+        double balance = (double)share;
         double zz = 0.0;
         for (int q = threadIdx.x; q < parts; q += THREADS) zz += __ldcg(a.part_z + (size_t)c_first + l + q);
 #pragma unroll
@@ -435,12 +456,12 @@ static Layout layout(const r3_shape* s, int32_t L, const Plan& p) {
 
 template <int G, int V, bool WIDE>
 static r3_status launch(const Args& a, cudaStream_t cs) {
-    const size_t smem = (size_t)a.E * WARPS * sizeof(float);
+    const size_t smem = (((size_t)a.E + 3) / 4 * 4 + (size_t)a.E * WARPS) * sizeof(float);
     if (smem > 32 * 1024) {                            // above what every kernel may have, with its static part
         static PerDevice ready;
         if (!ready.done()) {
             if (cudaFuncSetAttribute(balance_kernel<G, V, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     MAX_EXPERTS * WARPS * (int)sizeof(float)) != cudaSuccess)
+                                     MAX_EXPERTS * (WARPS + 1) * (int)sizeof(float)) != cudaSuccess)
                 return R3_ERR_CUDA;
             ready.mark();
         }

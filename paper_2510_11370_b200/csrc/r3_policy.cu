@@ -58,7 +58,6 @@ struct Args {
     Sums* sums;                                        // [units]
     int* n;                                            // [units] tokens
     int* head;                                         // [units] 1: the first unit of a sequence with tokens
-    int4* table;                                       // [units, 2] what find_unit gives
     Total* totals;                                     // [CTAs]
     unsigned* ticket;
     int32_t* dev_status;
@@ -376,8 +375,9 @@ __device__ __forceinline__ void check_bounds(const Args& a, int thread, int thre
 }
 
 __global__ void __launch_bounds__(WARPS * 32, CTAS_PER_SM) sums_kernel(const __grid_constant__ Args a) {
-    tc::grid_launch_dependents();
+    // the second pass may start once everything in front of this one is done: it reads its inputs at once
     tc::grid_dependency_wait();
+    tc::grid_launch_dependents();
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.ticket = 0;
     check_bounds(a, blockIdx.x * WARPS * 32 + threadIdx.x, gridDim.x * WARPS * 32);
     const int padded = (a.units + 3) & ~3;
@@ -387,10 +387,6 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS_PER_SM) sums_kernel(const __g
             continue;
         }
         const Unit u = find_unit(a, unit);
-        if ((threadIdx.x & 31) == 0) {
-            a.table[2 * unit] = make_int4(u.seq, u.begin, u.end, 0);
-            a.table[2 * unit + 1] = make_int4(u.first, u.count, 0, 0);
-        }
         if (a.need_sums) unit_sums(a, u, unit, a.sums + unit, a.n + unit, a.head + unit);
     }
 }
@@ -404,16 +400,27 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS_PER_SM) loss_kernel(const __g
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     static_assert(BLOCKS == WARPS, "a block of a long sequence per warp");
     tc::grid_launch_dependents();
+    // the first unit is found, and what it reads comes into L2, while the first pass runs
+    Unit u = {a.S, 0, 0, 0, 0};
+    {
+        const int unit = blockIdx.x * WARPS + warp;
+        if (unit < a.units) u = find_unit(a, unit);
+        const float* from[] = {a.logp, a.old, a.infer, a.ref, a.entropy, a.adv_per_token ? a.adv : nullptr};
+        for (int t = u.begin + 32 * lane; t < u.end; t += 32 * 32)
+#pragma unroll
+            for (int k = 0; k < 6; ++k)
+                if (from[k]) asm volatile("prefetch.global.L2 [%0];" ::"l"(from[k] + t));
+        if (a.mask && u.begin + 128 * lane < u.end) asm volatile("prefetch.global.L2 [%0];" ::"l"(a.mask + u.begin + 128 * lane));
+    }
     tc::grid_dependency_wait();
     const double divisor = count_divisor<WARPS>(a, a.n, a.head, s_count);
     Total r = {};
     int turn = 0;
     for (int first = blockIdx.x * WARPS; first < a.units; first += gridDim.x * WARPS, turn ^= 1) {
         const int unit = first + warp;
-        Unit u = {a.S, 0, 0, 0, 0};
-        if (unit < a.units) {
-            const int4 x = a.table[2 * unit], y = a.table[2 * unit + 1];
-            u = {x.x, x.y, x.z, y.x, y.y};
+        if (first != (int)blockIdx.x * WARPS) {
+            u = {a.S, 0, 0, 0, 0};
+            if (unit < a.units) u = find_unit(a, unit);
         }
         Whole w = {};
         w.tokens = 1;
@@ -526,7 +533,6 @@ extern "C" size_t r3_policy_loss_workspace_bytes(const r3_policy* c) {
     if (check(c) != R3_OK) return 0;
     const size_t units = (size_t)unit_count(c);
     return 256 + r3::round_up(units * sizeof(Sums), 256) + 2 * r3::round_up(units * sizeof(int), 256) +
-           r3::round_up(units * 2 * sizeof(int4), 256) +
            r3::round_up((units + WARPS - 1) / WARPS * sizeof(Total), 256);
 }
 
@@ -594,8 +600,6 @@ extern "C" r3_status r3_policy_loss(const r3_policy* c, const float* logp, const
     ws += round_up((size_t)a.units * sizeof(int), 256);
     a.head = reinterpret_cast<int*>(ws);
     ws += round_up((size_t)a.units * sizeof(int), 256);
-    a.table = reinterpret_cast<int4*>(ws);
-    ws += round_up((size_t)a.units * 2 * sizeof(int4), 256);
     a.totals = reinterpret_cast<Total*>(ws);
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     if (a.units <= ONE_WARPS)

@@ -65,6 +65,8 @@ struct alignas(64) ClassArgs {
     int rows, cols;                       // of D
     int tiles_n, tiles, first_item, kblocks;         // tiles: of one matrix
     int a_mn, b_mn;                       // the operand's rows in memory run along k
+    int splits, per_split;                // GRAM: a tile's k blocks in so many parts of per_split each
+    float4* partial;                      // and where their sums go (fold_kernel adds them up)
 };
 struct alignas(64) GemmArgs {
     ClassArgs c[MAX_CLASSES];
@@ -82,10 +84,14 @@ __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.comm
 template <int LAST> __device__ __forceinline__ void bulk_wait_read() {
     asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LAST) : "memory");
 }
-__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
 
+constexpr int SLOT = TILE * TILE / 4;     // float4 of a part's sums: [rank][warp][4 columns][row]
 struct Tile {
     int k, z, m, n;                       // class, matrix, tile row and column
+    int k0, k1, slot;                     // k blocks; number of the part
 };
 // Symmetric results: the tiles with m >= n, row by row.
 template <int PHASE> __device__ __forceinline__ Tile decode(const GemmArgs& g, int item) {
@@ -96,6 +102,15 @@ template <int PHASE> __device__ __forceinline__ Tile decode(const GemmArgs& g, i
         if (i < g.classes && item >= g.c[i].first_item) t.k = i;
     const ClassArgs& c = g.c[t.k];
     item -= c.first_item;
+    t.k0 = 0;
+    t.k1 = c.kblocks;
+    t.slot = item;
+    if (PHASE == GRAM && c.splits > 1) {
+        const int split = item % c.splits;
+        item /= c.splits;
+        t.k0 = split * c.per_split;
+        t.k1 = min(c.kblocks, t.k0 + c.per_split);
+    }
     t.z = item / c.tiles;
     const int r = item - t.z * c.tiles;
     if (PHASE != APPLY) {
@@ -157,6 +172,16 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
         fence_barrier_init();
     }
     if (warp == 1) tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), TMEM_COLS);
+    if (warp == 2 && lane < 2 * g.classes) {
+        const ClassArgs& c = g.c[lane >> 1];
+        if (lane & 1) {
+            prefetch_map(&c.a[0]);
+            prefetch_map(&c.out[0]);
+        } else {
+            prefetch_map(&c.b[0]);
+            prefetch_map(&c.mirror[0]);
+        }
+    }
     tc_fence_before();
     __syncthreads();
     cluster_sync_all();
@@ -181,7 +206,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                     const ClassArgs& c = g.c[t.k];
                     const int m0 = t.m * TILE + (int)rank * BM, n0 = t.n * TILE + (int)rank * BM;
                     const bool once = alike(t);
-                    for (int kb = 0; kb < c.kblocks; ++kb) {
+                    for (int kb = t.k0; kb < t.k1; ++kb) {
                         if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, g.dev_status)) {
                             ok = false;
                             break;
@@ -229,9 +254,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                     // 16 along k: 32 bytes inside the swizzled row, or two groups of 8 k rows
                     const uint64_t a_step = c.a_mn ? (2048 >> 4) : 2, b_step = c.b_mn ? (2048 >> 4) : 2;
                     const uint32_t to_b = alike(t) ? 0u : (uint32_t)SIDE_BYTES;
-                    for (int kb = 0; kb < c.kblocks; ++kb) {
+                    for (int kb = t.k0; kb < t.k1; ++kb) {
                         // three products: every k block has an accumulator of its own
-                        const bool fresh = TERMS > 1 || kb == 0, last = TERMS > 1 || kb + 1 == c.kblocks;
+                        const bool fresh = TERMS > 1 || kb == t.k0, last = TERMS > 1 || kb + 1 == t.k1;
                         if (fresh && !__all_sync(0xffffffffu, mbar_wait(tempty_bar(acc), acc_phase ^ 1u, abort_flag,
                                                                         g.dev_status))) {
                             ok = false;
@@ -336,21 +361,22 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                     early[j] = row < c.rows && first + 8 * j < c.in_ld ? *reinterpret_cast<const uint4*>(in[0] + 8 * j)
                                                                        : make_uint4(0u, 0u, 0u, 0u);
             }
-            float sum[TERMS > 1 ? 128 : 1];            // of the k blocks
-            if constexpr (TERMS > 1) {
+            constexpr bool KEEP = TERMS > 1 || PHASE == GRAM;    // the sums go through registers as a whole
+            float sum[KEEP ? 128 : 1];
+            if constexpr (KEEP) {
 #pragma unroll
                 for (int i = 0; i < 128; ++i) sum[i] = 0.f;
             }
             uint32_t tacc = 0;
 #pragma unroll 1
-            for (int kb = 0; kb < (TERMS > 1 ? c.kblocks : 1); ++kb) {
+            for (int kb = TERMS > 1 ? t.k0 : t.k1 - 1; kb < t.k1; ++kb) {
                 if (alive) {
                     const bool ok = mbar_wait(tfull_bar(acc), acc_phase, abort_flag, g.dev_status);
                     alive = __all_sync(0xffffffffu, ok);
                 }
                 tc_fence_after();
                 tacc = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * TILE + half * 128);
-                if constexpr (TERMS > 1) {
+                if constexpr (KEEP) {
                     if (alive && inside) {
 #pragma unroll
                         for (int p = 0; p < 4; ++p) {
@@ -367,6 +393,17 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                     if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
                 }
             }
+            if constexpr (PHASE == GRAM) {
+                if (c.splits > 1) {
+                    if (alive && inside) {
+                        float4* to = c.partial + (size_t)t.slot * SLOT + (((int)rank * EPI_WARPS + w) * 32) * 32 + lane;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            to[j * 32] = make_float4(sum[4 * j], sum[4 * j + 1], sum[4 * j + 2], sum[4 * j + 3]);
+                    }
+                    continue;
+                }
+            }
             if (alive && inside) {
 #pragma unroll
                 for (int p = 0; p < 2; ++p) {
@@ -376,7 +413,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         float v[32];
-                        if constexpr (TERMS > 1) {
+                        if constexpr (KEEP) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i) v[i] = sum[64 * p + 32 * h + i];
                         } else {
@@ -430,14 +467,14 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                     }
                 }
             }
-            if (TERMS == 1) {
+            if constexpr (!KEEP) {
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0 && alive) mbar_arrive_cluster(mapa_shared(tempty_bar(acc), 0));
                 if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
             }
         }
-        if (lane == 0) bulk_wait_all();
+        if (lane == 0) bulk_wait_read<0>();            // (the grid's end makes what was stored visible)
     }
 
     // ------------------------------ teardown ---------------------------------------------------
@@ -455,9 +492,93 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
     }
 }
 
-// ---- around the iteration: elementwise, a matrix in pieces of PIECE elements ----------------------
+// The parts of A's tiles added up: A = alpha sum, into both triangles.  A CTA takes 32 rows x 128 columns (what an
+// epilogue warp left).
+constexpr int FOLD_THREADS = 256;
+struct FoldClass {
+    const float4* partial;
+    __half* out[2];
+    int m, ld, tiles, splits, first;      // tiles of one matrix; first CTA
+};
+struct FoldArgs {
+    FoldClass c[MAX_CLASSES];
+    int classes;
+    float alpha;
+};
+template <int PLANES>
+__global__ void __launch_bounds__(FOLD_THREADS) fold_kernel(const __grid_constant__ FoldArgs a) {
+    __shared__ __align__(16) __half s_tile[PLANES][32][128 + 8];
+    grid_launch_dependents();
+    grid_dependency_wait();
+    int k = 0;
+#pragma unroll
+    for (int i = 1; i < MAX_CLASSES; ++i)
+        if (i < a.classes && (int)blockIdx.x >= a.c[i].first) k = i;
+    const FoldClass& c = a.c[k];
+    const int b = (int)blockIdx.x - c.first, region = b & 15, tile = b >> 4;
+    const int z = tile / c.tiles, r = tile - z * c.tiles;
+    int m = (int)((sqrtf(8.f * (float)r + 1.f) - 1.f) * 0.5f);
+    while (m * (m + 1) / 2 > r) --m;
+    while ((m + 1) * (m + 2) / 2 <= r) ++m;
+    const int n = r - m * (m + 1) / 2, rank = region >> 3, w = region & 7;
+    // (warp 4 + w of the epilogue: lane quadrant w & 3, column half w >> 2)
+    const int row0 = m * TILE + rank * BM + (w & 3) * 32, col0 = n * TILE + (w >> 2) * 128;
+    if (row0 >= c.m || col0 >= c.m) return;
+    const float4* from = c.partial + (size_t)tile * c.splits * SLOT + region * 1024;
+    float4 v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int s = 0; s < c.splits; ++s) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float4 p = from[(size_t)s * SLOT + threadIdx.x + FOLD_THREADS * e];
+            v[e].x += p.x;
+            v[e].y += p.y;
+            v[e].z += p.z;
+            v[e].w += p.w;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int i = threadIdx.x + FOLD_THREADS * e, row = i & 31, col = 4 * (i >> 5);
+        const float x[4] = {a.alpha * v[e].x, a.alpha * v[e].y, a.alpha * v[e].z, a.alpha * v[e].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const __half h = __float2half_rn(x[j]);
+            s_tile[0][row][col + j] = h;
+            if (PLANES > 1) s_tile[PLANES - 1][row][col + j] = __float2half_rn(x[j] - __half2float(h));
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int pl = 0; pl < PLANES; ++pl) {
+        __half* out = c.out[pl] + (size_t)z * c.m * c.ld;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int i = threadIdx.x + FOLD_THREADS * e;
+            const int row = i >> 4, col = 8 * (i & 15);
+            if (row0 + row < c.m && col0 + col < c.ld)
+                *reinterpret_cast<uint4*>(out + (size_t)(row0 + row) * c.ld + col0 + col) =
+                    *reinterpret_cast<const uint4*>(&s_tile[pl][row][col]);
+            if (m == n) continue;
+            const int mc = i >> 2, mr = 8 * (i & 3);   // column of the tile, eight of its rows
+            if (col0 + mc >= c.m || row0 + mr >= c.ld) continue;
+            __half h[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) h[j] = s_tile[pl][mr + j][mc];
+            *reinterpret_cast<uint4*>(out + (size_t)(col0 + mc) * c.ld + row0 + mr) = *reinterpret_cast<const uint4*>(h);
+        }
+    }
+}
+
+// ---- around the iteration: elementwise, a matrix in pieces of PIECE octets -------------------------
+// An octet is eight columns of a row (from a multiple of eight on; the row's last one may be short): 16 bytes
+// of a plane, and of the matrix itself where its rows have a multiple of eight columns.
 constexpr int EL_THREADS = 256;
-constexpr int PIECE = EL_THREADS * 32;
+constexpr int PER_THREAD = 1;             // octets under way at once (more of them cost the occupancy that hides
+constexpr int TURNS = 4;                  // loads better: 43 x 768 x 2048 without the products XXX us with 1, 244 with 2, 316 with 4)
+constexpr int PIECE = EL_THREADS * PER_THREAD * TURNS;
 
 // Matrices of one stack in a launch.
 struct Part {
@@ -477,12 +598,11 @@ struct ElemArgs {
     const float *grad_scale, *lr_now;
     Part part[MAX_STACKS];
 };
-// The piece of a CTA: its stack and matrix, and the elements [p0, p1) of the matrix.
+// The piece of a CTA: its stack and matrix.
 struct Piece {
     const Part* part;
-    int matrix, piece;
-    long long base, p0, p1;               // base: elements of the matrices before this one
-    bool wide;
+    int matrix, piece, octets;            // octets of a row
+    long long base;                       // elements of the matrices before this one
 };
 __device__ __forceinline__ Piece find_piece(const ElemArgs& a) {
     int i = 0;
@@ -490,59 +610,103 @@ __device__ __forceinline__ Piece find_piece(const ElemArgs& a) {
         if (i + step < a.parts && a.part[i + step].first <= (long long)blockIdx.x) i += step;
     Piece p;
     p.part = &a.part[i];
-    const long long within = (long long)blockIdx.x - p.part->first;
-    p.matrix = (int)(within / p.part->pieces);
-    p.piece = (int)(within - (long long)p.matrix * p.part->pieces);
-    const long long size = (long long)p.part->rows * p.part->cols;
-    p.base = p.matrix * size;
-    p.p0 = (long long)p.piece * PIECE;
-    p.p1 = min(size, p.p0 + PIECE);
-    p.wide = p.part->cols % 8 == 0;
+    const uint32_t within = (uint32_t)(blockIdx.x - p.part->first), pieces = (uint32_t)p.part->pieces;
+    p.matrix = (int)(within / pieces);
+    p.piece = (int)(within - (uint32_t)p.matrix * pieces);
+    p.octets = p.part->ld >> 3;
+    p.base = (long long)p.matrix * p.part->rows * p.part->cols;
     return p;
+}
+// A thread's octet e of a piece: where it lies in the matrix and in the planes, and its elements.
+struct Place {
+    long long at, in_plane;
+    int valid;
+};
+template <bool VEC> __device__ __forceinline__ Place octet_of(const Piece& p, int turn, int e) {
+    // (below 2^25)
+    const uint32_t i = (uint32_t)p.piece * PIECE + (uint32_t)((turn * PER_THREAD + e) * EL_THREADS) + threadIdx.x;
+    Place t;
+    t.in_plane = (long long)i * 8;
+    if (VEC) {
+        t.at = t.in_plane;
+        t.valid = i < (uint32_t)(p.part->rows * p.octets) ? 8 : 0;
+    } else {
+        const uint32_t r = i / (uint32_t)p.octets, o = i - r * (uint32_t)p.octets;
+        t.at = (long long)r * p.part->cols + 8 * o;
+        t.valid = r < (uint32_t)p.part->rows ? min(8, p.part->cols - 8 * (int)o) : 0;
+    }
+    return t;
+}
+template <bool VEC, typename T> __device__ __forceinline__ void get_octet(const T* p, int valid, float (&f)[8]) {
+    if (VEC) {
+        load8(p, f);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) f[k] = k < valid ? to_f32(p[k]) : 0.f;
+    }
+}
+template <bool VEC, typename T> __device__ __forceinline__ void put_octet(T* p, int valid, const float (&f)[8]) {
+    if (VEC) {
+        store8(p, f);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < valid) p[k] = from_f32<T>(f[k]);
+    }
+}
+// Gradient and momentum of a thread's octets, all of them under way at once.
+template <bool VEC, typename G>
+__device__ __forceinline__ void get_pair(const Piece& p, int turn, const G* grad, const float* mom, Place (&t)[PER_THREAD],
+                                         float (&g)[PER_THREAD][8], float (&m)[PER_THREAD][8]) {
+#pragma unroll
+    for (int e = 0; e < PER_THREAD; ++e) {
+        t[e] = octet_of<VEC>(p, turn, e);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) g[e][k] = m[e][k] = 0.f;
+        if (t[e].valid > 0) {
+            get_octet<VEC>(grad + t[e].at, t[e].valid, g[e]);
+            if (mom) get_octet<VEC>(mom + t[e].at, t[e].valid, m[e]);
+        }
+    }
 }
 
 // First pass: the momentum's update and the sum of u^2 of every piece.
+template <bool VEC, typename G>
+__device__ __forceinline__ double norm_piece(const ElemArgs& a, const Piece& p, float gs) {
+    const G* grad = static_cast<const G*>(p.part->grad) + p.base;
+    float* mom = p.part->momentum ? p.part->momentum + p.base : nullptr;
+    double sum = 0.0;
+#pragma unroll 1
+    for (int turn = 0; turn < TURNS; ++turn) {
+        Place t[PER_THREAD];
+        float g[PER_THREAD][8], m[PER_THREAD][8];
+        get_pair<VEC>(p, turn, grad, mom, t, g, m);
+#pragma unroll
+        for (int e = 0; e < PER_THREAD; ++e) {
+            if (mom) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) m[e][k] = __fadd_rn(__fmul_rn(a.momentum, m[e][k]), __fmul_rn(g[e][k], gs));
+                if (t[e].valid > 0) put_octet<VEC>(mom + t[e].at, t[e].valid, m[e]);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const double u = (double)direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[e][k], gs), m[e][k]);
+                sum += u * u;
+            }
+        }
+    }
+    return sum;
+}
 template <typename G>
-__global__ void __launch_bounds__(EL_THREADS) norm_kernel(const __grid_constant__ ElemArgs a) {
+__global__ void __launch_bounds__(EL_THREADS, 6) norm_kernel(const __grid_constant__ ElemArgs a) {
     __shared__ double s_sum[EL_THREADS / 32];
     grid_launch_dependents();
     grid_dependency_wait();
     const Piece p = find_piece(a);
-    const G* grad = static_cast<const G*>(p.part->grad) + p.base;
-    float* mom = p.part->momentum ? p.part->momentum + p.base : nullptr;
     float gs;
-    const bool go = scale_of(a.grad_scale, &gs);
     double sum = 0.0;
-    if (go && p.wide) {
-#pragma unroll 4
-        for (long long i = p.p0 + threadIdx.x * 8; i < p.p1; i += EL_THREADS * 8) {
-            float g[8], m[8];
-            load8(grad + i, g);
-            if (mom) {
-                load8(mom + i, m);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) m[k] = __fadd_rn(__fmul_rn(a.momentum, m[k]), __fmul_rn(g[k], gs));
-                store8(mom + i, m);
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const double u = (double)direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[k], gs), m[k]);
-                sum += u * u;
-            }
-        }
-    } else if (go) {
-#pragma unroll 8
-        for (long long i = p.p0 + threadIdx.x; i < p.p1; i += EL_THREADS) {
-            const float g = __fmul_rn(to_f32(grad[i]), gs);
-            float m = 0.f;
-            if (mom) {
-                m = __fadd_rn(__fmul_rn(a.momentum, mom[i]), g);
-                mom[i] = m;
-            }
-            const double u = (double)direction(a.nesterov, a.momentum, mom != nullptr, g, m);
-            sum += u * u;
-        }
-    }
+    if (scale_of(a.grad_scale, &gs))
+        sum = p.part->cols % 8 == 0 ? norm_piece<true, G>(a, p, gs) : norm_piece<false, G>(a, p, gs);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
@@ -555,14 +719,42 @@ __global__ void __launch_bounds__(EL_THREADS) norm_kernel(const __grid_constant_
 }
 
 // Second pass: X = u / (|u| + eps) into the planes.
+template <bool VEC, typename G>
+__device__ __forceinline__ void start_piece(const ElemArgs& a, const Piece& p, float gs, float inv) {
+    const G* grad = static_cast<const G*>(p.part->grad) + p.base;
+    const float* mom = p.part->momentum ? p.part->momentum + p.base : nullptr;
+    const long long plane = (long long)p.matrix * p.part->rows * p.part->ld;
+#pragma unroll 1
+    for (int turn = 0; turn < TURNS; ++turn) {
+        Place t[PER_THREAD];
+        float g[PER_THREAD][8], m[PER_THREAD][8];
+        get_pair<VEC>(p, turn, grad, mom, t, g, m);
+#pragma unroll
+        for (int e = 0; e < PER_THREAD; ++e) {
+            if (t[e].valid <= 0) continue;
+            uint4 h, l;
+            __half2* hp = reinterpret_cast<__half2*>(&h);
+            __half2* lp = reinterpret_cast<__half2*>(&l);
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+                const float x0 = direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[e][k], gs), m[e][k]) * inv;
+                const float x1 =
+                    direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[e][k + 1], gs), m[e][k + 1]) * inv;
+                hp[k / 2] = __floats2half2_rn(x0, x1);
+                const float2 f = __half22float2(hp[k / 2]);
+                lp[k / 2] = __floats2half2_rn(x0 - f.x, x1 - f.y);
+            }
+            *reinterpret_cast<uint4*>(p.part->hi + plane + t[e].in_plane) = h;
+            *reinterpret_cast<uint4*>(p.part->lo + plane + t[e].in_plane) = l;
+        }
+    }
+}
 template <typename G>
-__global__ void __launch_bounds__(EL_THREADS) start_kernel(const __grid_constant__ ElemArgs a) {
+__global__ void __launch_bounds__(EL_THREADS, 6) start_kernel(const __grid_constant__ ElemArgs a) {
     __shared__ double s_sum[EL_THREADS / 32];
     grid_launch_dependents();
     grid_dependency_wait();
     const Piece p = find_piece(a);
-    const G* grad = static_cast<const G*>(p.part->grad) + p.base;
-    const float* mom = p.part->momentum ? p.part->momentum + p.base : nullptr;
     float gs;
     if (!scale_of(a.grad_scale, &gs)) return;          // the step is skipped: the planes are not looked at
     const int pieces = p.part->pieces;
@@ -576,93 +768,57 @@ __global__ void __launch_bounds__(EL_THREADS) start_kernel(const __grid_constant
 #pragma unroll
     for (int i = 0; i < EL_THREADS / 32; ++i) sum += s_sum[i];
     const float inv = start_scale(sum, a.eps);
-    const int rows = p.part->rows, cols = p.part->cols, ld = p.part->ld;
-    __half* hi = p.part->hi + (long long)p.matrix * rows * ld;
-    __half* lo = p.part->lo + (long long)p.matrix * rows * ld;
-    if (p.wide) {
-#pragma unroll 4
-        for (long long i = p.p0 + threadIdx.x * 8; i < p.p1; i += EL_THREADS * 8) {
-            float g[8], m[8];
-            load8(grad + i, g);
-            if (mom) load8(mom + i, m);
-            uint4 h, l;
-            __half2* hp = reinterpret_cast<__half2*>(&h);
-            __half2* lp = reinterpret_cast<__half2*>(&l);
-#pragma unroll
-            for (int k = 0; k < 8; k += 2) {
-                const float x0 = direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[k], gs), m[k]) * inv;
-                const float x1 =
-                    direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[k + 1], gs), m[k + 1]) * inv;
-                hp[k / 2] = __floats2half2_rn(x0, x1);
-                const float2 f = __half22float2(hp[k / 2]);
-                lp[k / 2] = __floats2half2_rn(x0 - f.x, x1 - f.y);
-            }
-            *reinterpret_cast<uint4*>(hi + i) = h;     // ld = cols here
-            *reinterpret_cast<uint4*>(lo + i) = l;
-        }
-    } else {
-#pragma unroll 8
-        for (long long i = p.p0 + threadIdx.x; i < p.p1; i += EL_THREADS) {
-            const float g = __fmul_rn(to_f32(grad[i]), gs);
-            const float x = direction(a.nesterov, a.momentum, mom != nullptr, g, mom ? mom[i] : 0.f) * inv;
-            const int r = (int)((uint32_t)i / (uint32_t)cols);       // a matrix has 2^28 elements at most
-            const long long at = (long long)r * ld + (i - (long long)r * cols);
-            const __half h = __float2half_rn(x);
-            hi[at] = h;
-            lo[at] = __float2half_rn(x - __half2float(h));
-        }
-    }
+    if (p.part->cols % 8 == 0) start_piece<true, G>(a, p, gs, inv);
+    else start_piece<false, G>(a, p, gs, inv);
 }
 
 // Behind the iteration: the result, or the weights' update.
+template <bool VEC, typename P, bool MASTER, bool STEP>
+__device__ __forceinline__ void finish_piece(const ElemArgs& a, const Piece& p) {
+    P* out = static_cast<P*>(p.part->param) + p.base;
+    float* master = MASTER ? p.part->master + p.base : nullptr;
+    const long long plane = (long long)p.matrix * p.part->rows * p.part->ld;
+    const float lr = a.lr_now ? *a.lr_now : a.lr;
+    const float keep = 1.f - lr * p.part->decay, rate = lr * p.part->scale * (1.f / SCALE);
+#pragma unroll 1
+    for (int turn = 0; turn < TURNS; ++turn) {
+        Place t[PER_THREAD];
+        uint4 hi[PER_THREAD], lo[PER_THREAD];
+        float w[PER_THREAD][8];
+#pragma unroll
+        for (int e = 0; e < PER_THREAD; ++e) {
+            t[e] = octet_of<VEC>(p, turn, e);
+            if (t[e].valid <= 0) continue;
+            hi[e] = *reinterpret_cast<const uint4*>(p.part->hi + plane + t[e].in_plane);
+            lo[e] = *reinterpret_cast<const uint4*>(p.part->lo + plane + t[e].in_plane);
+            if (MASTER) get_octet<VEC>(master + t[e].at, t[e].valid, w[e]);
+            else if (STEP) get_octet<VEC>(out + t[e].at, t[e].valid, w[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < PER_THREAD; ++e) {
+            if (t[e].valid <= 0) continue;
+            float o[8], l[8];
+            half8(hi[e], o);
+            half8(lo[e], l);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                o[k] += l[k];
+                w[e][k] = STEP ? w[e][k] * keep - rate * o[k] : o[k] * (1.f / SCALE);
+            }
+            if (MASTER) put_octet<VEC>(master + t[e].at, t[e].valid, w[e]);
+            put_octet<VEC>(out + t[e].at, t[e].valid, w[e]);
+        }
+    }
+}
 template <typename P, bool MASTER, bool STEP>
-__global__ void __launch_bounds__(EL_THREADS) finish_kernel(const __grid_constant__ ElemArgs a) {
+__global__ void __launch_bounds__(EL_THREADS, 6) finish_kernel(const __grid_constant__ ElemArgs a) {
     grid_launch_dependents();
     grid_dependency_wait();
     const Piece p = find_piece(a);
     float gs;
     if (!scale_of(a.grad_scale, &gs)) return;
-    P* out = static_cast<P*>(p.part->param) + p.base;
-    float* master = MASTER ? p.part->master + p.base : nullptr;
-    const int rows = p.part->rows, cols = p.part->cols, ld = p.part->ld;
-    const __half* hi = p.part->hi + (long long)p.matrix * rows * ld;
-    const __half* lo = p.part->lo + (long long)p.matrix * rows * ld;
-    const float lr = a.lr_now ? *a.lr_now : a.lr;
-    const float keep = 1.f - lr * p.part->decay, rate = lr * p.part->scale * (1.f / SCALE);
-    if (p.wide) {
-#pragma unroll 4
-        for (long long i = p.p0 + threadIdx.x * 8; i < p.p1; i += EL_THREADS * 8) {
-            float w[8], o[8], e[8];
-            half8(*reinterpret_cast<const uint4*>(hi + i), o);
-            half8(*reinterpret_cast<const uint4*>(lo + i), e);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) o[k] += e[k];
-            if (STEP) {
-                if (MASTER) load8(master + i, w);
-                else load8(out + i, w);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) w[k] = w[k] * keep - rate * o[k];
-                if (MASTER) store8(master + i, w);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) w[k] = o[k] * (1.f / SCALE);
-            }
-            store8(out + i, w);
-        }
-    } else {
-#pragma unroll 8
-        for (long long i = p.p0 + threadIdx.x; i < p.p1; i += EL_THREADS) {
-            const int r = (int)((uint32_t)i / (uint32_t)cols);
-            const long long at = (long long)r * ld + (i - (long long)r * cols);
-            const float o = __half2float(hi[at]) + __half2float(lo[at]);
-            float w = o * (1.f / SCALE);
-            if (STEP) {
-                w = (MASTER ? master[i] : to_f32(out[i])) * keep - rate * o;
-                if (MASTER) master[i] = w;
-            }
-            out[i] = from_f32<P>(w);
-        }
-    }
+    if (p.part->cols % 8 == 0) finish_piece<true, P, MASTER, STEP>(a, p);
+    else finish_piece<false, P, MASTER, STEP>(a, p);
 }
 
 // ---- host side ------------------------------------------------------------------------------------
@@ -714,7 +870,7 @@ static Problem problem_of(int rows, int cols, int terms) {
     p.ld = (int)round_up((size_t)cols, 8);
     p.ldm = (int)round_up((size_t)p.m, 8);
     p.terms = terms;
-    p.pieces = (int)(((long long)rows * cols + PIECE - 1) / PIECE);
+    p.pieces = (int)(((long long)rows * (p.ld / 8) + PIECE - 1) / PIECE);
     return p;
 }
 // Places of `count` matrices in the workspace: X twice, A and B, sums.
@@ -813,10 +969,58 @@ struct Class {
     uint8_t* ws;
 };
 
+static int square_tiles(const Problem& p) {
+    const int t = (p.m + TILE - 1) / TILE;
+    return t * (t + 1) / 2;
+}
+static int gram_blocks(const Problem& p) { return ((p.tall ? p.rows : p.cols) + BK - 1) / BK; }
+// How many k blocks of A = X X^T a CTA pair takes at a time, so that few tiles with long sums still spread over
+// the GPU.  In units of a k block's time (0.27 us; three products 0.8): a part costs its blocks and about 3 us
+// around them, parts cost a launch that adds them up, about 4 us.  150 x 4000 f32: 444 us whole, XXX in parts.
+constexpr int MAX_SPLITS = 8;
+static int part_of_k(const Class* classes, int n, int terms) {
+    const int pairs = sm_count() / 2;
+    const int around = terms > 1 ? 4 : 11, fold = terms > 1 ? 5 : 15;
+    int longest = 0;
+    for (int i = 0; i < n; ++i) longest = std::max(longest, gram_blocks(classes[i].p));
+    int best = longest;
+    long long least = -1;
+    for (int splits = 1; splits <= MAX_SPLITS; ++splits) {
+        const int part = (longest + splits - 1) / splits;
+        long long items = 0, slots = 0;
+        for (int i = 0; i < n; ++i) {
+            const int parts = (gram_blocks(classes[i].p) + part - 1) / part;
+            items += (long long)square_tiles(classes[i].p) * classes[i].count * parts;
+            if (parts > 1) slots += (long long)square_tiles(classes[i].p) * classes[i].count * parts;
+        }
+        if (slots > 4LL * pairs) break;
+        const long long cost = (items + pairs - 1) / pairs * (part + around) + (slots ? fold : 0);
+        if (least < 0 || cost < least) {
+            least = cost;
+            best = part;
+        }
+    }
+    return best;
+}
+static size_t partial_bytes(const Class* classes, int n, int terms) {
+    const int part = part_of_k(classes, n, terms);
+    size_t slots = 0;
+    for (int i = 0; i < n; ++i) {
+        const int parts = (gram_blocks(classes[i].p) + part - 1) / part;
+        if (parts > 1) slots += (size_t)square_tiles(classes[i].p) * classes[i].count * parts;
+    }
+    return slots * SLOT * sizeof(float4);
+}
+
 // The iteration on classes whose X stand in the planes 0; on return *at says which planes hold the results.
+// partial: partial_bytes of memory.
 template <int TERMS>
-static r3_status iterate(const Class* classes, int n, const Coefs& coefs, int32_t* dev_status, int* at,
-                         cudaStream_t cs) {
+static r3_status iterate(const Class* classes, int n, uint8_t* partial, const Coefs& coefs, int32_t* dev_status,
+                         int* at, cudaStream_t cs) {
+    const int part = part_of_k(classes, n, TERMS);
+    FoldArgs fold = {};
+    int fold_ctas = 0;
+    float4* next_partial = reinterpret_cast<float4*>(partial);
     GemmArgs gram[2], poly, apply[2];                // by the planes that hold X
     gram[0].items = gram[1].items = poly.items = apply[0].items = apply[1].items = 0;
     bool ok = true;
@@ -870,12 +1074,18 @@ static r3_status iterate(const Class* classes, int n, const Coefs& coefs, int32_
             c.first_item = g.items;
             c.kblocks = kblocks;
             c.a_mn = c.b_mn = mn;
+            c.splits = 1;
             g.items += c.tiles * count;
         };
         const int km = (p.m + BK - 1) / BK;
         square(poly, km, false);
         for (int k = 0; k < 2; ++k) {
-            square(gram[k], ((p.tall ? p.rows : p.cols) + BK - 1) / BK, p.tall);
+            square(gram[k], gram_blocks(p), p.tall);
+            ClassArgs& gr = gram[k].c[i];
+            gr.per_split = part;
+            gr.splits = (gr.kblocks + part - 1) / part;
+            gr.partial = next_partial;
+            gram[k].items += gr.tiles * count * (gr.splits - 1);
             ClassArgs& c = apply[k].c[i];
             c.in_plane = (long long)p.rows * p.ld;
             c.in_ld = p.ld;
@@ -887,9 +1097,25 @@ static r3_status iterate(const Class* classes, int n, const Coefs& coefs, int32_
             c.kblocks = km;
             c.a_mn = 0;
             c.b_mn = !p.tall;
+            c.splits = 1;
             apply[k].items += c.tiles * count;
         }
+        const ClassArgs& gr = gram[0].c[i];
+        if (gr.splits > 1) {
+            FoldClass& f = fold.c[fold.classes++];
+            f.partial = next_partial;
+            f.out[0] = reinterpret_cast<__half*>(ws + w.a[0]);
+            f.out[1] = reinterpret_cast<__half*>(ws + w.a[1]);
+            f.m = p.m;
+            f.ld = p.ldm;
+            f.tiles = gr.tiles;
+            f.splits = gr.splits;
+            f.first = fold_ctas;
+            fold_ctas += gr.tiles * count * 2 * EPI_WARPS;
+            next_partial += (size_t)gr.tiles * count * gr.splits * SLOT;
+        }
     }
+    fold.alpha = 1.f / SCALE;
     if (!ok) return R3_ERR_CUDA;
     for (GemmArgs* g : {&gram[0], &gram[1], &poly, &apply[0], &apply[1]}) {
         g->classes = n;
@@ -905,6 +1131,9 @@ static r3_status iterate(const Class* classes, int n, const Coefs& coefs, int32_
         poly.diag = c[0] * SCALE;
         apply[k].beta = c[0];
         r3_status st = launch_gemm<GRAM, TERMS>(gram[k], cs);
+        if (st == R3_OK && fold_ctas &&
+            launch_dependent(fold_kernel<TERMS == 1 ? 1 : 2>, dim3(fold_ctas), dim3(FOLD_THREADS), 0, cs, fold) != cudaSuccess)
+            st = R3_ERR_CUDA;
         if (st == R3_OK) st = launch_gemm<POLY, TERMS>(poly, cs);
         if (st == R3_OK) st = launch_gemm<APPLY, TERMS>(apply[k], cs);
         if (st != R3_OK) return st;
@@ -1015,8 +1244,8 @@ static r3_status run_round(const Job& job, const Coefs& coefs, Round& r, uint8_t
     }
     if (e != cudaSuccess) return R3_ERR_CUDA;
     int at = 0;
-    const r3_status st = job.terms > 1 ? iterate<3>(r.cls, r.classes, coefs, dev_status, &at, cs)
-                                       : iterate<1>(r.cls, r.classes, coefs, dev_status, &at, cs);
+    const r3_status st = job.terms > 1 ? iterate<3>(r.cls, r.classes, ws, coefs, dev_status, &at, cs)
+                                       : iterate<1>(r.cls, r.classes, ws, coefs, dev_status, &at, cs);
     if (st != R3_OK) return st;
     planes(at);
     if (!job.step)
@@ -1102,7 +1331,7 @@ static size_t workspace_bytes(const r3_muon_stack* ss, int32_t count, int terms)
                     return R3_OK;
                 },
                 [&](Round& r) {
-                    most = std::max(most, r.bytes);
+                    most = std::max(most, r.bytes + partial_bytes(r.cls, r.classes, terms));
                     return R3_OK;
                 });
     return most;

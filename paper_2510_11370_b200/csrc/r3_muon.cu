@@ -346,20 +346,42 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
             const int row0 = t.m * TILE + (int)rank * BM + q * 32, row = row0 + lane;
             const int first = t.n * TILE + half * 128;           // this warp's 128 columns
             const bool inside = row0 < c.rows && first < c.cols;
-            // what is added to the product comes while it is formed
-            constexpr int EARLY = TERMS == 1 && PHASE != GRAM ? 16 : 1;
-            uint4 early[EARLY];
-            const __half* in[2];
-            if (PHASE != GRAM) {
-                const long long at = (long long)t.z * c.in_plane + (long long)row * c.in_ld + first;
-                in[0] = c.in[0] + at;
-                in[1] = c.in[1] + at;
-            }
-            if (EARLY > 1) {
+            // what is added to the product: one plane of the warp's 128 columns, which come while it is formed, or
+            // (three products, whose sums take the registers) both planes of 64 of them at a time
+            constexpr bool ADDS = PHASE == POLY || (PHASE == APPLY && TERMS == 1);
+            uint4 early[ADDS ? 16 : 1];
+            // (four rows x 128 bytes per load: row by row, 32 lines a load, the eight warps' loads took 8500 clocks)
+            const int mine = row0 + (lane >> 3), left = c.rows - mine, hop = 4 * c.in_ld;
+            const long long in_at = (long long)t.z * c.in_plane + (long long)mine * c.in_ld;
+            auto fetch = [&](uint4* v, int plane, int p) {
+                const int col = first + 64 * p + 8 * (lane & 7);
+                const __half* from = c.in[plane] + in_at + col;
+                const int some = col < c.in_ld ? left : 0;
 #pragma unroll
-                for (int j = 0; j < EARLY; ++j)
-                    early[j] = row < c.rows && first + 8 * j < c.in_ld ? *reinterpret_cast<const uint4*>(in[0] + 8 * j)
-                                                                       : make_uint4(0u, 0u, 0u, 0u);
+                for (int j = 0; j < 8; ++j) {
+                    v[j] = make_uint4(0u, 0u, 0u, 0u);
+                    if (4 * j < some) v[j] = *reinterpret_cast<const uint4*>(from + j * hop);
+                }
+            };
+            // eight of them, 32 rows x 64 columns, to the lanes of their rows, by way of the next buffer
+            auto to_rows = [&](uint4* v) {
+                if (lane == 0) bulk_wait_read<BUFFERS - 1>();
+                __syncwarp();
+                uint8_t* box = buf_ptr + turn * EPI_PLANE;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int r = 4 * j + (lane >> 3);
+                    *reinterpret_cast<uint4*>(box + r * 128 + (((lane & 7) ^ (r & 7)) * 16)) = v[j];
+                }
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    v[j] = *reinterpret_cast<const uint4*>(box + lane * 128 + ((j ^ (lane & 7)) * 16));
+                __syncwarp();
+            };
+            if constexpr (ADDS && TERMS == 1) {
+                fetch(early, 0, 0);
+                fetch(early + 8, 0, 1);
             }
             constexpr bool KEEP = TERMS > 1 || PHASE == GRAM;    // the sums go through registers as a whole
             float sum[KEEP ? 128 : 1];
@@ -409,6 +431,16 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                 for (int p = 0; p < 2; ++p) {
                     const int col0 = first + 64 * p;
                     if (col0 >= c.cols) continue;
+                    if constexpr (ADDS) {
+                        if (TERMS == 1) {
+                            to_rows(early + 8 * p);
+                        } else {
+                            fetch(early, 0, p);
+                            fetch(early + 8, 1, p);
+                            to_rows(early);
+                            to_rows(early + 8);
+                        }
+                    }
                     uint32_t packed[OUT][32];          // pairs of columns
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
@@ -426,21 +458,16 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                             float x[8], l[8];
 #pragma unroll
                             for (int i = 0; i < 8; ++i) x[i] = g.alpha * v[8 * j + i];
-                            if (PHASE != GRAM && TERMS == 1) {
-                                half8(early[EARLY > 1 ? o : 0], l);
+                            if constexpr (ADDS) {
+                                half8(early[TERMS == 1 ? o : 4 * h + j], l);
+                                if (TERMS > 1) {
+                                    float e[8];
+                                    half8(early[8 + 4 * h + j], e);
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) l[i] += e[i];
+                                }
 #pragma unroll
                                 for (int i = 0; i < 8; ++i) x[i] = fmaf(g.beta, l[i], x[i]);
-                            } else if (PHASE == POLY) {
-                                uint4 hi = make_uint4(0u, 0u, 0u, 0u), lo = hi;
-                                if (row < c.rows && first + 8 * o < c.in_ld) {
-                                    hi = *reinterpret_cast<const uint4*>(in[0] + 8 * o);
-                                    lo = *reinterpret_cast<const uint4*>(in[1] + 8 * o);
-                                }
-                                float e[8];
-                                half8(hi, l);
-                                half8(lo, e);
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) x[i] = fmaf(g.beta, l[i] + e[i], x[i]);
                             }
                             if (PHASE == POLY && t.m == t.n) {
 #pragma unroll

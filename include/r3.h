@@ -605,13 +605,15 @@ typedef struct {
 /* Newton-Schulz iteration, per matrix: X = x / (|x|_F + eps), then steps times, with the Gram matrix of the
  * smaller side (here rows <= cols),
  *   A = X X^T;   B = b A + c A^2;   X = a X + B X
- * which brings the singular values near one; out = X.  x of in_dtype, out of out_dtype, may be the same
- * buffer (of one type).  All products accumulate in float32, X is carried in 22 bits between the steps.
+ * which brings the singular values near one; out = X.  x of in_dtype, out of out_dtype: the same buffer (of
+ * one type) or no memory in common.  All products accumulate in float32, X is carried in 22 bits between the
+ * steps.
  *  - A matrix of zeros gives zeros, one that holds what is not finite gives NaN; the others of a batch are
  *    not touched by it.
- *  - Coefficients whose iterates could pass 16 in norm (or b A + c A^2 60) are refused.
- * workspace: r3_orthogonalize_workspace_bytes(config), 256-byte aligned: up to about 512 MB (or what one matrix
- * needs); larger batches are taken in parts. */
+ *  - Coefficients whose iterates could pass 16 in norm (or b A + c A^2, with or without a, 60) are refused.
+ * workspace: r3_orthogonalize_workspace_bytes(config), 256-byte aligned: up to about 600 MB (or what one matrix
+ * needs); larger batches are taken in parts.  Matrices with a side of at most 128 and the other of at most 2048
+ * need none to speak of: they are taken in one launch, on the chip. */
 size_t r3_orthogonalize_workspace_bytes(const r3_orthogonal* config);
 r3_status r3_orthogonalize(const r3_orthogonal* config, const void* x, void* out, void* workspace,
                            size_t ws_bytes, int32_t* dev_status, void* stream);

@@ -1472,6 +1472,12 @@ extern "C" r3_status r3_orthogonalize(const r3_orthogonal* c, const void* x, voi
     if (st != R3_OK) return st;
     if (c->batch == 0) return R3_OK;
     if (!x || !out || !aligned(x, 16) || !aligned(out, 16) || !aligned(dev_status, 4)) return R3_ERR_INVALID_ARG;
+    // the same buffer of one type, or no memory in common: later matrices are read after earlier results
+    const size_t n = (size_t)c->batch * c->rows * c->cols;
+    const uintptr_t from = reinterpret_cast<uintptr_t>(x), to = reinterpret_cast<uintptr_t>(out);
+    const bool same = from == to && c->in_dtype == c->out_dtype;
+    if (!same && from < to + n * (c->out_dtype == R3_BF16 ? 2 : 4) && to < from + n * (c->in_dtype == R3_BF16 ? 2 : 4))
+        return R3_ERR_INVALID_ARG;
     if (!workspace || !aligned(workspace, 256) || ws_bytes < r3_orthogonalize_workspace_bytes(c))
         return R3_ERR_WORKSPACE;
     const r3_muon_stack one = {out, nullptr, x, nullptr, c->batch, c->rows, c->cols, 0.f, 0.f};

@@ -1035,7 +1035,7 @@ class Muon:
     "spectral" = sqrt(max(1, rows / cols)), "rms" = 0.2 sqrt(max(rows, cols)) (about AdamW's root mean square),
     a number, or one of these per tensor.  products: 1 or 3 fp16 products for each of the iteration's; by default 3
     where the weights or their masters are float32.  The handle keeps its tensors' memory alive, and a
-    workspace (up to about 512 MB) that its steps share; set_grads() exchanges the gradients."""
+    workspace (up to about 600 MB) that its steps share; set_grads() exchanges the gradients."""
 
     def __init__(self, params, grads=None, *, masters=None, momentum_buffers=None, momentum=0.95,
                  nesterov=True, weight_decay=0.0, scale="spectral", steps=5, coefficients=None, eps=1e-7,

@@ -35,7 +35,8 @@ BAD = [dict(steps=0), dict(steps=17), dict(products=2), dict(products=0), dict(e
 @pytest.mark.parametrize("kw", BAD + [
     dict(batch=-1), dict(rows=0), dict(cols=0), dict(rows=16385), dict(cols=16385), dict(batch=(1 << 24) + 1),
     dict(in_dtype=2), dict(out_dtype=-1), dict(x=None), dict(out=None), dict(x=(1 << 20) + 8),
-    dict(out=(2 << 20) + 8), dict(status=4097)])
+    dict(out=(2 << 20) + 8), dict(status=4097), dict(out=1 << 20, out_dtype=1), dict(out=(1 << 20) + 3056),
+    dict(x=(2 << 20) + 3056), dict(x=(2 << 20) - 1520, in_dtype=1)])
 def test_orthogonalize_refused(r3, kw):
     assert ortho(r3, **kw) == r3.R3_ERR_INVALID_ARG
 

@@ -202,7 +202,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
     const uint32_t x_plane = (uint32_t)a.x_blocks * SM_BLOCK, a_plane = (uint32_t)a.a_blocks * SM_BLOCK;
     const uint32_t a0 = 2 * x_plane;                     // the A region, behind X's two planes
     uint8_t* misc = bp + a0 + a.a_bytes;
-    const uint32_t bar = base + a0 + a.a_bytes, a_bar = bar + 8;
+    const uint32_t bar = base + a0 + a.a_bytes, a_bar = bar + 8, bar2 = bar + 24;
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(misc + 16);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 20);
     double* s_sum = reinterpret_cast<double*>(misc + 64);           // [SM_WARPS]
@@ -225,6 +225,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
     if (threadIdx.x == 0) {
         mbar_init(bar, 1);
         mbar_init(a_bar, 1);
+        mbar_init(bar2, 1);
         *abort_flag = 0;
         fence_barrier_init();
     }
@@ -300,51 +301,58 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
 
         // ---- the iteration ---------------------------------------------------------------------------
         const int q = warp & 3, quarter = warp >> 2, r = q * 32 + lane;   // this thread's row of every product
+        const int m32 = (m16 + 31) & ~31, w32 = (W + 31) & ~31;
         const uint32_t trow = tmem + ((uint32_t)(q * 32) << 16);
-        uint32_t phase = 0, a_phase = 0;
+        uint32_t phase = 0, phase2 = 0, a_phase = 0;
         bool alive = true;
-        // D = P Q over k16 steps of 16 along k; plane choice by term, small products first.  Three products: every
-        // 64 of k have an accumulator of their own, N columns (to 32) further on, and the epilogue adds them up
-        // (an addition in tensor memory drops what lies below the running sum's last place).
-        auto multiply = [&](uint32_t p0, uint32_t p_plane, uint32_t q0, uint32_t q_plane, bool q_mn, int N, int k16) {
+        // D = P Q over the steps of 16 along k from `k0` to `k1`, columns c0 to c0 + N of D; plane choice by term,
+        // small products first.  Three products: every 64 of k have an accumulator of their own, `apart` columns
+        // further on, and the epilogue adds them up (an addition in tensor memory drops what lies below the
+        // running sum's last place).
+        auto issue = [&](uint32_t p0, uint32_t p_plane, uint32_t q0, uint32_t q_plane, bool q_mn, int c0, int N,
+                         int apart, int k0, int k1, uint32_t done) {
             if (warp == 0) {
                 tc_fence_after();
                 if (alive && elect_one()) {
                     const uint32_t idesc = (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24) |
                                            (q_mn ? 1u << 16 : 0u);
-                    for (int seg = 0; seg < (TERMS > 1 ? k16 : 1); seg += 4)
+                    for (int seg = k0; seg < k1; seg += TERMS > 1 ? 4 : k1)
                     for (int term = 0; term < TERMS; ++term) {
-                        const int k_end = TERMS > 1 ? min(k16, seg + 4) : k16;
+                        const int k_end = TERMS > 1 ? min(k1, seg + 4) : k1;
                         const uint32_t p = base + p0 + (TERMS > 1 && term == 1 ? p_plane : 0u);
                         const uint32_t qq = base + q0 + (TERMS > 1 && term == 0 ? q_plane : 0u);
                         for (int k = seg; k < k_end; ++k) {
                             const uint32_t in_row = (uint32_t)((k >> 2) * SM_BLOCK + (k & 3) * 32);
-                            const uint64_t dq = q_mn ? smem_desc_mn_sw128(qq + (uint32_t)k * 2048u, SM_BLOCK)
+                            const uint64_t dq = q_mn ? smem_desc_mn_sw128(qq + (uint32_t)(c0 >> 6) * SM_BLOCK +
+                                                                              (uint32_t)k * 2048u, SM_BLOCK)
                                                      : smem_desc_sw128(qq + in_row);
-                            tc_mma_bf16(tmem + (uint32_t)((seg >> 2) * ((N + 31) & ~31)), smem_desc_sw128(p + in_row), dq, idesc,
-                                        term != 0 || k != seg ? 1u : 0u);
+                            tc_mma_bf16(tmem + (uint32_t)(c0 + (TERMS > 1 ? (seg >> 2) * apart : 0)),
+                                        smem_desc_sw128(p + in_row), dq, idesc,
+                                        term != 0 || k != (TERMS > 1 ? seg : 0) ? 1u : 0u);
                         }
                     }
-                    tc_commit(bar);
+                    tc_commit(done);
                 }
                 __syncwarp();
             }
+        };
+        auto wait = [&](uint32_t done, uint32_t& phase) {
             if (alive) {
-                const bool ok = mbar_wait(bar, phase, abort_flag, a.dev_status);
+                const bool ok = mbar_wait(done, phase, abort_flag, a.dev_status);
                 alive = __all_sync(0xffffffffu, ok);
             }
             phase ^= 1u;
             tc_fence_after();
         };
-        // 32 columns of this thread's row, the accumulators of k16 steps N columns apart added up
-        auto take = [&](int c, int N, int k16, float (&v)[32]) {
+        // 32 columns of this thread's row, the accumulators of k16 steps `apart` columns apart added up
+        auto take = [&](int c, int apart, int k16, float (&v)[32]) {
             tc_ld32(trow + c, v);
             tc_wait_ld();
             if (TERMS > 1) {
 #pragma unroll 1
                 for (int seg = 4; seg < k16; seg += 4) {
                     float more[32];
-                    tc_ld32(trow + c + (seg >> 2) * ((N + 31) & ~31), more);
+                    tc_ld32(trow + c + (seg >> 2) * apart, more);
                     tc_wait_ld();
 #pragma unroll
                     for (int k = 0; k < 32; ++k) v[k] += more[k];
@@ -360,12 +368,13 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
         for (int s = 0; s < a.steps; ++s) {
             const float ca = a.coefs[s][0], cb = a.coefs[s][1], cc = a.coefs[s][2];
             // A = X X^T
-            multiply(0, x_plane, 0, x_plane, false, m16, W >> 4);
+            issue(0, x_plane, 0, x_plane, false, 0, m16, m32, 0, W >> 4, bar);
+            wait(bar, phase);
             if (C == 1) {
                 const int c = quarter * 32;
                 if (alive && c < m16) {
                     float v[32];
-                    take(c, m16, W >> 4, v);
+                    take(c, m32, W >> 4, v);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         float x[8];
@@ -389,7 +398,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
                 const int c = quarter * 32;
                 if (alive && c < m16) {
                     float v[32];
-                    take(c, m16, W >> 4, v);
+                    take(c, m32, W >> 4, v);
                     const uint32_t to = mapa_shared(base + a0 + rank * (uint32_t)(share * 512), (uint32_t)(r / share));
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
@@ -441,12 +450,13 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
                 a_phase ^= 1u;
             }
             // B = a I + b A + c A^2, in A's place (three products: without a I, a X is added in float32)
-            multiply(a0, a_plane, a0, a_plane, false, m16, m16 >> 4);
+            issue(a0, a_plane, a0, a_plane, false, 0, m16, m32, 0, m16 >> 4, bar);
+            wait(bar, phase);
             const int c_square = quarter * 32;
             if (alive && c_square < m16) {
                 const int c = c_square;
                 float v[32];
-                take(c, m16, m16 >> 4, v);
+                take(c, m32, m16 >> 4, v);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     if (c + 8 * j >= m16) continue;
@@ -467,16 +477,21 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
             }
             written();
             // X = B X, in X's place (one product: + a times the lo plane, which is no operand then; three: + a X)
-            multiply(a0, a_plane, 0, x_plane, true, W, m16 >> 4);
-            if (C > 1 && s + 1 < a.steps) {
-                __syncwarp();
-                cluster_arrive();                        // B is read: the next parts may come
-            }
+            // the second half of X's columns is multiplied while the first half's sums are taken
+            issue(a0, a_plane, 0, x_plane, true, 0, min(W, 128), w32, 0, m16 >> 4, bar);
+            if (W > 128) issue(a0, a_plane, 0, x_plane, true, 128, W - 128, w32, 0, m16 >> 4, bar2);
 #pragma unroll
-            for (int c = quarter * 64; c < quarter * 64 + 64; c += 32) {
+            for (int half = 0; half < 2; ++half) {
+                if (half == 0) wait(bar, phase);
+                else if (W > 128) wait(bar2, phase2);
+                if (C > 1 && s + 1 < a.steps && half == (W > 128 ? 1 : 0)) {
+                    __syncwarp();
+                    cluster_arrive();                    // B is read: the next parts may come
+                }
+                const int c = half * 128 + quarter * 32;
                 if (!alive || c >= W) continue;
                 float v[32];
-                take(c, W, m16 >> 4, v);
+                take(c, w32, m16 >> 4, v);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     if (c + 8 * j >= W) continue;

@@ -595,7 +595,7 @@ r3_status r3_adamw_step(const r3_adamw* config, const r3_adamw_tensor* tensors, 
 /* batch matrices [rows, cols], dense and row-major, sides up to 16384.  steps 1 to 16; coefs (HOST,
  * [steps][3] = a, b, c of each step) or NULL = (3.4445, -4.7750, 2.0315) for all.  products: 1 = every product
  * from fp16 operands (as exact as a bf16 result), 3 = from operands of two fp16 planes (a float32 result).
- * eps >= 0. */
+ * eps >= 0 (below 4e-36 taken as that). */
 typedef struct {
     int32_t batch, rows, cols, in_dtype, out_dtype, steps, products;
     double eps;

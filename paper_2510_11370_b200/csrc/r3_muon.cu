@@ -2,20 +2,27 @@
 // u the matrix, X = u / (|u|_F + eps) and per step (a, b, c):
 //   A = X X^T  (X^T X where the matrix is tall: the smaller side)     B = b A + c A^2     X = a X + B X
 //
-// Three products a step on the tensor cores, each a batch over all matrices of a chunk.  Numbers.  The
-// iterates' singular values stay near one, so fp16 (11 bits, against bf16's 8) holds every operand, times
-// 2^10 to keep small elements in its normal range.  X itself is carried in two fp16 planes, hi + lo (22 bits):
-// the term a X, by which a weak direction grows a^steps-fold, then has no rounding to speak of, and what the
-// products' operands lose stays as small as the output's own rounding to bf16 whatever the matrix's spectrum
-// is (simulated for full-rank, decaying and low-rank spectra: 4e-4 to 1.7e-3 of the result's rms, against
-// 1.7e-3 for the rounding; bf16 operands with a rounded X lose a third of a rank-8 update).  For float32
-// results A and B get a second plane as well and every product is hi hi + hi lo + lo hi.
+// Three products a step on the tensor cores, each a batch over all matrices of a round (up to four shapes in one
+// launch).  Numbers.  The iterates' singular values stay near one, so fp16 (11 bits, against bf16's 8) holds
+// every operand, times 2^10 to keep small elements in its normal range.  X itself is carried in two fp16 planes,
+// hi + lo (22 bits): the term a X, by which a weak direction grows a^steps-fold, then has no rounding to speak
+// of, and what the products' operands lose stays as small as the output's own rounding to bf16 whatever the
+// matrix's spectrum is (simulated for full-rank, decaying and low-rank spectra: 1.1e-3 to 1.7e-3 of the
+// result's rms, against 1.7e-3 for the rounding; bf16 operands with a rounded X lose a third of a rank-8 update).
+// For float32 results A and B get a second plane as well and every product is hi lo + lo hi + hi hi.
 //
-// One GEMM kernel does all three: D = alpha (product) + beta L, L a matrix read tile by tile, with two CTAs
-// per MMA (256 x 256 tiles, 128 rows of each operand per CTA and k block of 64, accumulators double
-// buffered in tensor memory).  A and B are symmetric: only tiles on and below the diagonal are computed, the
-// others are stored from the same accumulators, transposed.  Eight epilogue warps, each with its own 8 KB of
-// shared memory: L comes and D goes by TMA in boxes of 32 rows x 64 columns.
+// One GEMM kernel does all three, with two CTAs per MMA (256 x 256 tiles, 128 rows of each operand per CTA and k
+// block of 64, accumulators double buffered in tensor memory).  B = a I + b A + c A^2, the identity within, so
+// that the last product is the whole of the new X (one product: but for a times the lo plane, which is no
+// operand then and comes while the product is formed).  A and B are symmetric: only tiles on and below the
+// diagonal are computed, the others are stored from the same accumulators, transposed.  Eight epilogue warps,
+// each with its own 8 KB (three products: 4 KB) of shared memory, through which results go out by TMA in
+// boxes of 32 rows x 64 columns and addends come in whole lines.
+// 24 matrices of 768 x 2048, one product: X X^T 35 us, B 21, B X 69, of which the products of their tiles are 23,
+// 9 and 35 at the tensor pipe's rate.  B X takes 281 MB from and to HBM, and its operands, the lo plane and both new planes come
+// and go between L2 and the SMs at 11 to 12.5 TB/s, which bounds it (the tensor pipe is busy 42% of the time);
+// X X^T and B wait for the first loads and the last stores of their few tiles besides.  Three products, 4096 x
+// 4096: 3150 us, 81% of the tensor pipe's rate: each 64 of k leave tensor memory for registers.
 #include <algorithm>
 #include <cmath>
 #include <vector>
@@ -604,7 +611,7 @@ __global__ void __launch_bounds__(FOLD_THREADS) fold_kernel(const __grid_constan
 // of a plane, and of the matrix itself where its rows have a multiple of eight columns.
 constexpr int EL_THREADS = 256;
 constexpr int PER_THREAD = 1;             // octets under way at once (more of them cost the occupancy that hides
-constexpr int TURNS = 4;                  // loads better: 43 x 768 x 2048 without the products XXX us with 1, 244 with 2, 316 with 4)
+constexpr int TURNS = 4;                  // loads better: 43 x 768 x 2048 without the products 169 us with 1, 244 with 2, 316 with 4)
 constexpr int PIECE = EL_THREADS * PER_THREAD * TURNS;
 
 // Matrices of one stack in a launch.
@@ -850,6 +857,7 @@ __global__ void __launch_bounds__(EL_THREADS, 6) finish_kernel(const __grid_cons
 
 // ---- host side ------------------------------------------------------------------------------------
 constexpr int MAX_SIDE = 16384;
+constexpr float LEAST_EPS = 4e-36f;       // below it SCALE / (norm + eps) could pass float32's range
 constexpr int MAX_BATCH = 1 << 24, MAX_MATRICES = 1 << 27;   // (the latter times the CTAs of a cluster: a grid's limit)
 constexpr size_t ROUND_BYTES = 512u << 20;          // workspace of a round, unless one matrix needs more
 
@@ -1003,7 +1011,7 @@ static int square_tiles(const Problem& p) {
 static int gram_blocks(const Problem& p) { return ((p.tall ? p.rows : p.cols) + BK - 1) / BK; }
 // How many k blocks of A = X X^T a CTA pair takes at a time, so that few tiles with long sums still spread over
 // the GPU.  In units of a k block's time (0.27 us; three products 0.8): a part costs its blocks and about 3 us
-// around them, parts cost a launch that adds them up, about 4 us.  150 x 4000 f32: 444 us whole, XXX in parts.
+// around them, parts cost a launch that adds them up, about 4 us.  150 x 4000 f32: 444 us whole, 248 in parts.
 constexpr int MAX_SPLITS = 8;
 static int part_of_k(const Class* classes, int n, int terms) {
     const int pairs = sm_count() / 2;
@@ -1481,7 +1489,7 @@ extern "C" r3_status r3_orthogonalize(const r3_orthogonal* c, const void* x, voi
     if (!workspace || !aligned(workspace, 256) || ws_bytes < r3_orthogonalize_workspace_bytes(c))
         return R3_ERR_WORKSPACE;
     const r3_muon_stack one = {out, nullptr, x, nullptr, c->batch, c->rows, c->cols, 0.f, 0.f};
-    const Job job = {c->out_dtype, c->in_dtype, 0, c->products, false, false, 0.f, (float)c->eps, 0.f, nullptr,
+    const Job job = {c->out_dtype, c->in_dtype, 0, c->products, false, false, 0.f, std::max((float)c->eps, LEAST_EPS), 0.f, nullptr,
                      nullptr};
     try {
         return run(job, coefs, &one, 1, static_cast<uint8_t*>(workspace), dev_status,
@@ -1518,7 +1526,7 @@ extern "C" r3_status r3_muon_step(const r3_muon* c, const r3_muon_stack* stacks,
         if (need == 0) return R3_OK;                   // no matrices
         if (!workspace || !aligned(workspace, 256) || ws_bytes < need) return R3_ERR_WORKSPACE;
         const Job job = {c->param_dtype, c->grad_dtype, c->nesterov != 0, c->products, c->master != 0, true,
-                         (float)c->momentum, (float)c->eps, (float)c->lr, grad_scale, lr};
+                         (float)c->momentum, std::max((float)c->eps, LEAST_EPS), (float)c->lr, grad_scale, lr};
         return run(job, coefs, stacks, n_stacks, static_cast<uint8_t*>(workspace), dev_status,
                    static_cast<cudaStream_t>(stream));
     } catch (...) {

@@ -276,3 +276,11 @@ def test_captured_step_matches_eager_ones(r3):
     torch.cuda.current_stream().wait_stream(side)
     b.step(0.01)
     assert all(torch.equal(s, t) for s, t in zip(a.params, b.params))
+
+
+@pytest.mark.parametrize("rows,cols,size", [(8, 8, 1e-34), (129, 256, 1e-35)])
+def test_norms_whose_inverse_passes_float32(r3, rows, cols, size):
+    """eps below 4e-36 counts as that: 2^10 over the norm alone would be infinite."""
+    x = (matrix(rows, cols, 12)[0].double() * size).float()
+    assert 1024 / np.linalg.norm(f64(x)) > 3.4e38
+    check(r3.orthogonalize(x.cuda(), eps=0.0).cpu(), x, 3, eps=float(np.float32(4e-36)))

@@ -12,9 +12,12 @@
 // Main pass: a token's logits lie across G lanes, 8 each where the experts are many (a shuffle then serves
 // 32 / G tokens), so that its maximum, its sum and its product with f are shuffles; a lane keeps the f of its
 // experts and the sums of their probabilities in registers, and the next tokens' logits are under way while
-// these are worked on.  The first logits come into L2 while the choices are still counted.  All resident CTAs take equal shares of the L T tokens, across the borders of blocks
-// (grids of whole parts per block left a second wave of 32 CTAs for 48 blocks: 285 us against 150).  The last CTA of a
-// block to arrive adds up its probability sums, in an order that depends on the shape alone.
+// these are worked on.  The first logits come into L2 while the choices are still counted.  All resident CTAs take
+// equal shares of the L T tokens, across the borders of blocks (grids of whole parts per block left a second wave
+// of 32 CTAs for 48 blocks: 285 us against 150).  The last CTA of a block to arrive adds up its probability sums, in
+// an order that depends on the shape alone.
+// 48 blocks of 16384 tokens, 128 experts: 151 us, 5.4 TB/s of the 812 MB that have to move; one block of 65536
+// tokens: 26 us, of which the counting pass and the two starts are a third.
 #include <cmath>
 
 #include "r3_common.cuh"
@@ -32,12 +35,14 @@ constexpr int THREADS = 512;
 constexpr int WARPS = THREADS / 32;
 constexpr int CTAS_PER_SM = 2;
 constexpr int EARLY_BYTES = 32 << 20;     // of logits that all CTAs fetch ahead: a part of L2
+constexpr int ALONE = 8192;               // logits of a block that one CTA takes with its choices
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct Args {
     int T, E, K, L;
     int count_parts, count_ctas;          // clusters per block in the counting pass, CTAs of each
     int grid;                             // CTAs of the main pass
+    int alone, idx_bytes;                 // one CTA per block, which counts its choices itself
     int accumulate, given;
     float balance_coef, z_coef;
     const float* logits;
@@ -235,12 +240,30 @@ __global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_ker
             }
         };
         fetch(t0 + warp * ROWS);
+        int* s_count = reinterpret_cast<int*>(s_col);  // [E + 1], until the sums of probabilities take the place
+        if (a.alone) {
+            for (int e = threadIdx.x; e <= E; e += THREADS) s_count[e] = 0;
+            __syncthreads();
+            for (int t = threadIdx.x; t < a.T; t += THREADS)
+                if (!a.mask || a.mask[t]) atomicAdd(s_count + E, 1);
+            const size_t from = (size_t)block0 * a.K;
+            for (int i = threadIdx.x; !a.given && i < a.T * a.K; i += THREADS) {
+                if (a.mask && !a.mask[i / a.K]) continue;
+                const int e = a.idx_bytes == 1 ? static_cast<const uint8_t*>(a.idx)[from + i]
+                                               : static_cast<const int16_t*>(a.idx)[from + i];
+                if (e < 0 || e >= E) report(a.dev_status, R3_DEV_BAD_INDEX);
+                else atomicAdd(s_count + e, 1);
+            }
+            __syncthreads();
+        }
         // the block's counts, the number of its choices and of its tokens
         long long mine = 0;
         for (int e = threadIdx.x; e <= E; e += THREADS) {
             int n = 0;
             if (e < E && a.given) {
                 n = a.counts[(size_t)l * E + e];
+            } else if (a.alone) {
+                n = s_count[e];
             } else {
                 const int32_t* p = a.part_counts + (size_t)l * a.count_parts * (E + 1) + e;
 #pragma unroll 8
@@ -364,7 +387,7 @@ __global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_ker
         __syncthreads();
         const int c_first = a.T > 0 ? cta_of(a, block0) : 0, c_last = a.T > 0 ? cta_of(a, block0 + a.T - 1) : 0;
         const int parts = c_last - c_first + 1;
-        if (threadIdx.x == 0) s_last = atomicAdd(a.ticket + l, 1u) == (unsigned)parts - 1u;
+        if (threadIdx.x == 0) s_last = a.alone || atomicAdd(a.ticket + l, 1u) == (unsigned)parts - 1u;
         __syncthreads();
         if (!s_last) continue;
         __threadfence();
@@ -414,8 +437,11 @@ __global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_ker
 
 struct Plan {
     int count_parts, count_ctas, grid;
+    bool alone;
 };
-// Main pass: every resident CTA, unless a warp's share falls below two tokens or so.
+// Main pass: every resident CTA, unless a warp's share falls below two tokens or so.  Blocks of few logits: a CTA
+// each, without a counting pass (a launch less; 512 tokens of 8 experts 8.6 -> 7.8 us, 48 blocks of it 15.0 -> 8.7;
+// with twice the logits one block takes 9.9 instead of 8.5).
 static Plan plan(int T, int L, int E) {
     Plan p;
     const int ctas = T > 0 ? (T + COUNT_TOKENS - 1) / COUNT_TOKENS : 1;
@@ -426,6 +452,8 @@ static Plan plan(int T, int L, int E) {
     const int most = (E > 256 ? 1 : CTAS_PER_SM) * sm_count();
     if (grid > most) grid = most;
     p.grid = grid < 1 || T == 0 ? 1 : (int)grid;
+    p.alone = T > 0 && (long long)T * E <= ALONE;
+    if (p.alone) p.grid = L;
     return p;
 }
 static r3_status check(const r3_shape* s, int32_t L, const r3_balance* c) {
@@ -479,6 +507,26 @@ static r3_status launch(const Args& a, cudaStream_t cs) {
     return launch<32, 32, WIDE>(a, cs);
 }
 
+static bool launch_count(const r3_shape* s, int32_t L, const Plan& p, const Args& a, cudaStream_t cs) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)p.count_ctas;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)(p.count_parts * p.count_ctas), (unsigned)L);
+    cfg.blockDim = dim3(COUNT_THREADS);
+    cfg.dynamicSmemBytes = (size_t)(s->E + 1) * sizeof(int);
+    cfg.stream = cs;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.count_ctas > 1 ? 2 : 1;
+    cudaError_t err = cudaSuccess;
+    R3_DISPATCH_IDX(s, IdxT, err = cudaLaunchKernelEx(&cfg, count_kernel<IdxT>, a));
+    return err == cudaSuccess;
+}
+
 }  // namespace bal
 }  // namespace r3
 
@@ -519,6 +567,8 @@ extern "C" r3_status r3_balance_loss(const r3_shape* s, int32_t L, const r3_bala
     a.count_ctas = p.count_ctas;
     a.grid = p.grid;
     a.accumulate = config->accumulate != 0;
+    a.alone = p.alone;
+    a.idx_bytes = s->idx_type == R3_IDX_U8 ? 1 : 2;
     a.given = given;
     a.balance_coef = (float)config->balance_coef;
     a.z_coef = (float)config->z_coef;
@@ -535,23 +585,6 @@ extern "C" r3_status r3_balance_loss(const r3_shape* s, int32_t L, const r3_bala
     a.ticket = reinterpret_cast<unsigned*>(ws + w.ticket);
     a.dev_status = dev_status;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
-    const size_t smem = (size_t)(s->E + 1) * sizeof(int);
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)p.count_ctas;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.gridDim = dim3((unsigned)(p.count_parts * p.count_ctas), (unsigned)L);
-    cfg.blockDim = dim3(COUNT_THREADS);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = cs;
-    cfg.attrs = attr;
-    cfg.numAttrs = p.count_ctas > 1 ? 2 : 1;
-    cudaError_t err = cudaSuccess;
-    R3_DISPATCH_IDX(s, IdxT, err = cudaLaunchKernelEx(&cfg, count_kernel<IdxT>, a));
-    if (err != cudaSuccess) return R3_ERR_CUDA;
+    if (!p.alone && !launch_count(s, L, p, a, cs)) return R3_ERR_CUDA;
     return s->E % 4 == 0 ? launch<true>(a, cs) : launch<false>(a, cs);
 }

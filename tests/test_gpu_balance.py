@@ -159,3 +159,31 @@ def test_repeats_streams_and_graphs(r3):
         dev.mul_(1.1)
         graph.replay()
         assert all(torch.equal(a, b) for a, b in zip(r3.balance_loss(s, 3, dev, idx, z_coef=0.1), held))
+
+
+@pytest.mark.parametrize("L,T,E,K,idx", [(1, 1024, 8, 2, torch.uint8), (1, 1025, 8, 2, torch.uint8),
+                                         (5, 64, 128, 8, torch.int16), (5, 65, 128, 8, torch.int16),
+                                         (3, 8, 1024, 10, torch.int16), (2, 8192, 1, 1, torch.uint8)])
+def test_blocks_around_a_single_ctas_size(r3, L, T, E, K, idx):
+    """Both sides of the size up to which a CTA counts its block's choices itself: masks, given counts, sums onto
+    a gradient, invalid records."""
+    s, logits, rec = make(r3, L, T, E, K, idx, 4)
+    dev, record = logits.cuda(), rec.cuda()
+    mask = (torch.rand(T, generator=torch.Generator().manual_seed(2)) < 0.5).to(torch.uint8) * 3
+    base = torch.randn(L, T, E)
+    dl = base.cuda()
+    out = r3.balance_loss(s, L, dev, record, mask=mask.cuda(), dlogits=dl, accumulate=True, z_coef=0.1)
+    check(out, logits, rec, mask.bool(), zc=0.1, base=base)
+    assert torch.equal(dl[:, ~mask.bool()].cpu(), base[:, ~mask.bool()])
+    given = torch.randint(0, 1 << 29, (L, E), dtype=torch.int32).cuda()
+    check(r3.balance_loss(s, L, dev, counts=given, mask=mask.cuda()), logits, rec, mask.bool(), counts=given.cpu().long())
+    wrong, st = rec.clone(), r3.new_status("cuda")
+    wrong[L - 1, T - 1, K - 1] = E
+    if idx == torch.int16:
+        wrong[0, 0, 0] = -3
+    _, counts, d = r3.balance_loss(s, L, dev, wrong.cuda(), dev_status=st)
+    assert st.item() == r3.DEV_BAD_INDEX and torch.isfinite(d).all()
+    assert counts.sum() == L * T * K - (2 if idx == torch.int16 else 1)
+    loss, counts, none = r3.balance_loss(s, L, dev, record, want_grad=False)
+    want = r3.balance_loss(s, L, dev, record)
+    assert none is None and torch.equal(loss, want[0]) and torch.equal(counts, want[1])

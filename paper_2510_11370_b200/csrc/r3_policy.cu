@@ -11,13 +11,16 @@
 // not depend on how an exponential rounds; exponentials and the terms are float32, all sums 64 bits.
 //
 // Two passes, since a token's gradient needs its sequence's sums and the number of tokens: the first
-// leaves the sums of every unit (up to U = 256 consecutive tokens of ONE sequence, more in a large batch, a
+// leaves the sums of every unit (up to U = 128 consecutive tokens of ONE sequence, more in a large batch, a
 // warp each), the second adds up a sequence's units in their order and writes the gradients; its last CTA
-// adds up the CTAs' parts of the loss.  Sequence i that starts at token c takes its units from number
+// adds up the CTAs' parts of the loss.  With a ratio per sequence the units' sums say all about the tokens'
+// terms, and where there is no KL term and no entropy the second pass reads the mask alone (1 M tokens 29 -> 22 us).  Sequence i that starts at token c takes its units from number
 // i + floor(c / U) on: that leaves each one room for all of its units whatever the lengths are, and a warp of
 // the first pass finds its sequence by a search in cu_seqlens, 32 probes at a time, with no table built
 // before.  Batches of up to 32 units run as one CTA.
-// Bound by HBM where the batch is large, by two launches where it is not.
+// Bound by latency throughout: 1531 tokens in one launch 6 us, 65536 tokens with every term 10 us, 1 M tokens of
+// 1024 sequences 22 us, against 2.6 us for their bytes; of those 22 the first pass takes 9, the second's start (its
+// counts, its sequences' sums) 3, its tokens 2, the parts of the loss 4.
 #include <cmath>
 
 #include "r3_common.cuh"
@@ -27,9 +30,11 @@
 namespace r3 {
 namespace pol {
 
-constexpr int STEP = 128;                 // tokens that a warp works on at a time
-constexpr int PER_LANE = STEP / 32;
-constexpr int LEAST_UNIT = 256;           // tokens of a unit, at least; a power of two
+// Tokens of a lane at a time: the second pass has too much code per token to stand there more than once (code
+// comes from memory too at every launch: four tokens at a time took 13.7 us for 65536 tokens, one 10.6).
+constexpr int AHEAD = 4;                  // in the first pass
+constexpr int MARKS = 16, PROBES = 32;    // of the mask, where nothing else is read
+constexpr int LEAST_SHIFT = 7;            // tokens of a unit, at least: 128 (256: 1531 tokens 8.1 instead of 6.1 us)
 constexpr int MOST_UNITS = 2048;          // of one sequence: beyond, units grow
 constexpr int LONG = 64;                  // units from which a sequence is added up in BLOCKS blocks
 constexpr int BLOCKS = 8;
@@ -39,6 +44,9 @@ constexpr int ONE_WARPS = 32;             // units of a batch that takes one CTA
 
 struct Sums {                             // of one unit; of a sequence: the sum of its units'
     double d, up, down;                   // sum of d; of w A over the tokens with A > 0 and A < 0
+};
+struct Marks {                            // of a unit, where ratios are of sequences
+    int up, down, cut, pad;               // tokens with A > 0, with A < 0, with w at the cap
 };
 struct Total {
     double policy, kl, entropy;
@@ -56,6 +64,7 @@ struct Args {
     float *loss, *dlogp, *dentropy, *metrics;
     int32_t* counts;
     Sums* sums;                                        // [units]
+    Marks* marks;                                      // [units]
     int* n;                                            // [units] tokens
     int* head;                                         // [units] 1: the first unit of a sequence with tokens
     Total* totals;                                     // [CTAs]
@@ -109,41 +118,55 @@ __device__ __forceinline__ float infer_weight(const Args& a, float old, float in
 }
 
 // ---- first pass: the sums of a unit ----------------------------------------------------------
-__device__ __forceinline__ void unit_sums(const Args& a, const Unit& u, int unit, Sums* s, int* n, int* head) {
+__device__ __forceinline__ void unit_sums(const Args& a, const Unit& u, int unit, Sums* s, Marks* marks, int* n,
+                                          int* head) {
     const int lane = threadIdx.x & 31;
     const bool live = u.seq < a.S;
     double d = 0.0, up = 0.0, down = 0.0;
-    int k = 0;
+    int k = 0, ups = 0, downs = 0, cuts = 0;
     if (live && !a.by_sequence && !a.mask) {
         if (lane == 0) k = u.end - u.begin;
     } else if (live) {
         const float seq_adv = a.by_sequence && !a.adv_per_token && u.begin < u.end ? a.adv[u.seq] : 0.f;
-#pragma unroll 2
-        for (int t0 = u.begin + lane; t0 - lane < u.end; t0 += STEP) {
-            float lp[PER_LANE], old[PER_LANE], inf[PER_LANE], adv[PER_LANE];
-            bool on[PER_LANE];
+        struct Token {
+            float logp, old, infer, adv;
+            bool on;
+        };
+        auto load = [&](int t0, Token (&x)[AHEAD]) {
 #pragma unroll
-            for (int j = 0; j < PER_LANE; ++j) {
+            for (int j = 0; j < AHEAD; ++j) {
                 const int t = t0 + j * 32;
-                on[j] = t < u.end;
+                x[j].on = t < u.end;
                 if (a.by_sequence) {                       // (not behind the mask's arrival)
-                    lp[j] = on[j] ? a.logp[t] : 0.f;
-                    old[j] = on[j] ? a.old[t] : 0.f;
-                    inf[j] = on[j] && a.infer ? a.infer[t] : 0.f;
-                    adv[j] = on[j] ? (a.adv_per_token ? a.adv[t] : seq_adv) : 0.f;
+                    x[j].logp = x[j].on ? a.logp[t] : 0.f;
+                    x[j].old = x[j].on ? a.old[t] : 0.f;
+                    x[j].infer = x[j].on && a.infer ? a.infer[t] : 0.f;
+                    x[j].adv = x[j].on ? (a.adv_per_token ? a.adv[t] : seq_adv) : 0.f;
                 }
-                if (a.mask && on[j]) on[j] = a.mask[t] != 0;
+                if (a.mask && x[j].on) x[j].on = a.mask[t] != 0;
             }
+        };
+        Token next[AHEAD];
+        load(u.begin + lane, next);
+#pragma unroll 1
+        for (int t0 = u.begin + lane; t0 - lane < u.end; t0 += 32 * AHEAD) {
+            Token x[AHEAD];
 #pragma unroll
-            for (int j = 0; j < PER_LANE; ++j) {
-                k += on[j];
-                if (!a.by_sequence || !on[j]) continue;
-                d += (double)lp[j] - (double)old[j];
-                bool cut;
-                const float w = a.infer ? infer_weight(a, old[j], inf[j], &cut) : 1.f;
-                const double wa = (double)(w * adv[j]);
-                if (adv[j] > 0.f) up += wa;
-                else if (adv[j] != 0.f) down += wa;        // NaN counts here: it has to reach the loss
+            for (int j = 0; j < AHEAD; ++j) x[j] = next[j];
+            load(t0 + 32 * AHEAD, next);
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                k += x[j].on;
+                if (!a.by_sequence || !x[j].on) continue;
+                d += (double)x[j].logp - (double)x[j].old;
+                bool cut = false;
+                const float w = a.infer ? infer_weight(a, x[j].old, x[j].infer, &cut) : 1.f;
+                const double wa = (double)(w * x[j].adv);
+                if (x[j].adv > 0.f) up += wa;
+                else if (x[j].adv != 0.f) down += wa;      // NaN counts here: it has to reach the loss
+                ups += x[j].adv > 0.f;
+                downs += x[j].adv < 0.f;
+                cuts += cut;
             }
         }
     }
@@ -153,10 +176,10 @@ __device__ __forceinline__ void unit_sums(const Args& a, const Unit& u, int unit
         // does the sequence hold a token at all: mostly its first unit says so
         any = k > 0;
         const int seq_end = bound(a, u.seq + 1);
-        for (int t = u.end; !any && t < seq_end; t += 8 * STEP) {
+        for (int t = u.end; !any && t < seq_end; t += 32 * PROBES) {
             int here = 0;
 #pragma unroll
-            for (int j = 0; j < 8 * PER_LANE; ++j) {
+            for (int j = 0; j < PROBES; ++j) {
                 const int at = t + j * 32 + lane;
                 here |= at < seq_end && a.mask[at];        // without a mask the first unit has tokens
             }
@@ -167,11 +190,17 @@ __device__ __forceinline__ void unit_sums(const Args& a, const Unit& u, int unit
         d = warp_sum(d);
         up = warp_sum(up);
         down = warp_sum(down);
+        ups = warp_sum(ups);
+        downs = warp_sum(downs);
+        cuts = warp_sum(cuts);
     }
     if (lane == 0) {
         *n = k;
         *head = any;
-        if (a.by_sequence) *s = {d, up, down};
+        if (a.by_sequence) {
+            *s = {d, up, down};
+            *marks = {ups, downs, cuts, 0};
+        }
     }
 }
 
@@ -227,8 +256,10 @@ __device__ __forceinline__ float exp_less_line(float x, float em1) {
 }
 
 // ---- second pass: one unit's part of the loss, and its gradients ------------------------------
-__device__ __forceinline__ Total unit_loss(const Args& a, const Unit& u, const Sums& s, int n_seq,
-                                           double divisor) {
+// `s`, n_seq: of the unit's sequence; `sums`, `marks`, `n`: the unit's own, which are all that a ratio of the whole
+// sequence leaves to know of the tokens' terms (they are not read again).
+__device__ __forceinline__ Total unit_loss(const Args& a, const Unit& u, const Sums& s, int n_seq, double divisor,
+                                           const Sums* sums, const Marks* marks, const int* n) {
     const int lane = threadIdx.x & 31;
     Total r = {};
     const bool live = u.seq < a.S;
@@ -238,70 +269,92 @@ __device__ __forceinline__ Total unit_loss(const Args& a, const Unit& u, const S
     const float gw = (float)(weight * (double)up_to);
     const float kl_w = (float)(a.kl_coef * weight * (double)up_to);
     const float ent_g = (float)(-a.entropy_coef * weight * (double)up_to);
-    const float seq_adv = live && !a.adv_per_token && u.begin < u.end ? a.adv[u.seq] : 0.f;
-    double seq_d = 0.0;
-    float seq_slope = 0.f, seq_rho = 0.f;
+    const float seq_adv = live && !a.by_sequence && !a.adv_per_token && u.begin < u.end ? a.adv[u.seq] : 0.f;
+    float seq_slope = 0.f;
     if (a.by_sequence && live) {
-        seq_d = s.d / (double)max(n_seq, 1);
-        seq_rho = expf((float)seq_d);
-        const double rho = (double)seq_rho;
+        const double seq_d = s.d / (double)max(n_seq, 1);
+        const double rho = (double)expf((float)seq_d);
         const bool high = seq_d > a.log_high, low = seq_d < a.log_low || seq_d > a.log_dual;
         // a part that is 0 takes no ratio, be it infinite
         const double part = (high ? 0.0 : s.up) + (low ? 0.0 : s.down);
+        if (lane == 0) {
+            const double rho_down = seq_d < a.log_low ? (double)a.low : low ? (double)a.dual : rho;
+            if (sums->up != 0.0) r.policy -= sums->up * (high ? (double)a.high : rho);
+            if (sums->down != 0.0) r.policy -= sums->down * rho_down;
+            r.tokens = *n;
+            r.clipped = (high ? marks->up : 0) + (low ? marks->down : 0);
+            r.cut = marks->cut;
+        }
         seq_slope = part == 0.0 ? 0.f
                                 : (float)(-part * rho * weight * (double)up_to / (double)max(n_seq, 1));
     }
-    const bool want_logp = !a.by_sequence || a.ref, want_old = !a.by_sequence || a.infer;
-    for (int t0 = u.begin + lane; t0 - lane < u.end; t0 += STEP) {
-        float lp[PER_LANE], old[PER_LANE], inf[PER_LANE], ref[PER_LANE], ent[PER_LANE], adv[PER_LANE];
-        bool on[PER_LANE];
+    const bool terms = !a.by_sequence;
+    if (a.by_sequence && !a.ref && !a.entropy) {
+        // the same gradient for every token that counts
+        for (int t0 = u.begin + lane; a.dlogp && t0 - lane < u.end; t0 += 32 * MARKS) {
+            bool on[MARKS];
 #pragma unroll
-        for (int j = 0; j < PER_LANE; ++j) {
-            const int t = t0 + j * 32;
-            on[j] = live && t < u.end;
-            lp[j] = on[j] && want_logp ? a.logp[t] : 0.f;
-            old[j] = on[j] && want_old ? a.old[t] : 0.f;
-            inf[j] = on[j] && a.infer ? a.infer[t] : 0.f;
-            ref[j] = on[j] && a.ref ? a.ref[t] : 0.f;
-            ent[j] = on[j] && a.entropy ? a.entropy[t] : 0.f;
-            adv[j] = on[j] ? (a.adv_per_token ? a.adv[t] : seq_adv) : 0.f;
-            if (a.mask && on[j]) on[j] = a.mask[t] != 0;
+            for (int j = 0; j < MARKS; ++j)
+                on[j] = live && t0 + 32 * j < u.end && (!a.mask || a.mask[t0 + 32 * j]);
+#pragma unroll
+            for (int j = 0; j < MARKS; ++j)
+                if (t0 + 32 * j < u.end) a.dlogp[t0 + 32 * j] = on[j] ? seq_slope : 0.f;
         }
-#pragma unroll
-        for (int j = 0; j < PER_LANE; ++j) {
-            const int t = t0 + j * 32;
-            if (t >= u.end) continue;
-            float g = 0.f, ge = 0.f;
-            if (on[j]) {
-                const double d = a.by_sequence ? seq_d : (double)lp[j] - (double)old[j];
+        r.policy *= weight;
+        return r;
+    }
+    struct Token {
+        float logp, old, infer, ref, entropy, adv;
+        bool on;
+    };
+    auto load = [&](int t, Token& x) {
+        const bool on = live && t < u.end;
+        x.logp = on && (terms || a.ref) ? a.logp[t] : 0.f;
+        x.old = on && terms ? a.old[t] : 0.f;
+        x.infer = on && terms && a.infer ? a.infer[t] : 0.f;
+        x.ref = on && a.ref ? a.ref[t] : 0.f;
+        x.entropy = on && a.entropy ? a.entropy[t] : 0.f;
+        x.adv = on && terms ? (a.adv_per_token ? a.adv[t] : seq_adv) : 0.f;
+        x.on = on && (!a.mask || a.mask[t]);
+    };
+    Token next;
+    load(u.begin + lane, next);
+#pragma unroll 1
+    for (int t = u.begin + lane; t < u.end; t += 32) {
+        const Token x = next;
+        load(t + 32, next);
+        float g = 0.f, ge = 0.f;
+        if (x.on) {
+            g = seq_slope;
+            if (terms) {
+                const double d = (double)x.logp - (double)x.old;
                 bool cut = false;
-                const float w = a.infer ? infer_weight(a, old[j], inf[j], &cut) : 1.f;
-                const float wa = w * adv[j];
-                const bool high = adv[j] > 0.f && d > a.log_high;
-                const bool low = adv[j] < 0.f && d < a.log_low;
-                const bool far = adv[j] < 0.f && d > a.log_dual;
-                const float rho = high ? a.high : low ? a.low : far ? a.dual : a.by_sequence ? seq_rho : expf((float)d);
-                const float term = adv[j] == 0.f ? 0.f : -(wa * rho);
+                const float w = a.infer ? infer_weight(a, x.old, x.infer, &cut) : 1.f, wa = w * x.adv;
+                const bool high = x.adv > 0.f && d > a.log_high;
+                const bool low = x.adv < 0.f && d < a.log_low;
+                const bool far = x.adv < 0.f && d > a.log_dual;
+                const float rho = high ? a.high : low ? a.low : far ? a.dual : expf((float)d);
+                const float term = x.adv == 0.f ? 0.f : -(wa * rho);
                 const bool beyond = high || low || far;
                 r.tokens += 1;
                 r.clipped += beyond;
                 r.cut += cut;
                 r.policy += (double)term;
-                g = a.by_sequence ? seq_slope : beyond ? 0.f : term * gw;
-                if (a.ref) {
-                    const float x = (float)((double)ref[j] - (double)lp[j]);
-                    const float em1 = expm1f(x);
-                    r.kl += (double)exp_less_line(x, em1);
-                    if (a.kl_coef != 0.0) g -= kl_w * em1;
-                }
-                if (a.entropy) {
-                    r.entropy += (double)ent[j];
-                    ge = ent_g;
-                }
+                g = beyond ? 0.f : term * gw;
             }
-            if (a.dlogp) a.dlogp[t] = g;
-            if (a.dentropy) a.dentropy[t] = ge;
+            if (a.ref) {
+                const float y = (float)((double)x.ref - (double)x.logp);
+                const float em1 = expm1f(y);
+                r.kl += (double)exp_less_line(y, em1);
+                if (a.kl_coef != 0.0) g -= kl_w * em1;
+            }
+            if (a.entropy) {
+                r.entropy += (double)x.entropy;
+                ge = ent_g;
+            }
         }
+        if (a.dlogp) a.dlogp[t] = g;
+        if (a.dentropy) a.dentropy[t] = ge;
     }
     // (lane by lane: the warp's lanes are added up once, at the end)
     r.policy *= weight;
@@ -387,7 +440,7 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS_PER_SM) sums_kernel(const __g
             continue;
         }
         const Unit u = find_unit(a, unit);
-        if (a.need_sums) unit_sums(a, u, unit, a.sums + unit, a.n + unit, a.head + unit);
+        if (a.need_sums) unit_sums(a, u, unit, a.sums + unit, a.marks + unit, a.n + unit, a.head + unit);
     }
 }
 
@@ -405,7 +458,9 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS_PER_SM) loss_kernel(const __g
     {
         const int unit = blockIdx.x * WARPS + warp;
         if (unit < a.units) u = find_unit(a, unit);
-        const float* from[] = {a.logp, a.old, a.infer, a.ref, a.entropy, a.adv_per_token ? a.adv : nullptr};
+        const bool terms = !a.by_sequence;
+        const float* from[] = {terms || a.ref ? a.logp : nullptr, terms ? a.old : nullptr, terms ? a.infer : nullptr,
+                               a.ref, a.entropy, terms && a.adv_per_token ? a.adv : nullptr};
         for (int t = u.begin + 32 * lane; t < u.end; t += 32 * 32)
 #pragma unroll
             for (int k = 0; k < 6; ++k)
@@ -440,7 +495,7 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS_PER_SM) loss_kernel(const __g
                 w = sequence_sums(a, a.sums, a.n, u.first, u.count);
             }
         }
-        add(r, unit_loss(a, u, w.s, w.tokens, divisor));
+        add(r, unit_loss(a, u, w.s, w.tokens, divisor, a.sums + unit, a.marks + unit, a.n + unit));
     }
     r = warp_total(a, r);
     if (lane == 0) s_total[warp] = r;
@@ -476,6 +531,7 @@ __global__ void __launch_bounds__(WARPS * 32, CTAS_PER_SM) loss_kernel(const __g
 // Both passes of a batch of few units.
 __global__ void __launch_bounds__(ONE_WARPS * 32) one_cta_kernel(const __grid_constant__ Args a) {
     __shared__ Sums s_sums[ONE_WARPS];
+    __shared__ Marks s_marks[ONE_WARPS];
     __shared__ int s_n[ONE_WARPS], s_head[ONE_WARPS];
     __shared__ Total s_total[ONE_WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -485,7 +541,7 @@ __global__ void __launch_bounds__(ONE_WARPS * 32) one_cta_kernel(const __grid_co
     Unit u = {a.S, 0, 0, 0, 0};
     if (warp < a.units) {
         u = find_unit(a, warp);
-        unit_sums(a, u, warp, s_sums + warp, s_n + warp, s_head + warp);
+        unit_sums(a, u, warp, s_sums + warp, s_marks + warp, s_n + warp, s_head + warp);
     }
     __syncthreads();
     double divisor = a.denominator;
@@ -496,7 +552,7 @@ __global__ void __launch_bounds__(ONE_WARPS * 32) one_cta_kernel(const __grid_co
     Whole w = {};
     if ((a.by_sequence || a.mean_of_sequences) && u.begin < u.end && u.seq < a.S)
         w = sequence_sums(a, s_sums, s_n, u.first, u.count);
-    const Total r = warp_total(a, unit_loss(a, u, w.s, w.tokens, divisor));
+    const Total r = warp_total(a, unit_loss(a, u, w.s, w.tokens, divisor, s_sums + warp, s_marks + warp, s_n + warp));
     if (lane == 0) s_total[warp] = r;
     __syncthreads();
     if (warp == 0) {
@@ -506,7 +562,7 @@ __global__ void __launch_bounds__(ONE_WARPS * 32) one_cta_kernel(const __grid_co
 }
 
 static int unit_shift(const r3_policy* c) {
-    int shift = 8;
+    int shift = LEAST_SHIFT;
     while ((c->T >> shift) > MOST_UNITS) ++shift;
     return shift;
 }
@@ -532,7 +588,7 @@ extern "C" size_t r3_policy_loss_workspace_bytes(const r3_policy* c) {
     using namespace r3::pol;
     if (check(c) != R3_OK) return 0;
     const size_t units = (size_t)unit_count(c);
-    return 256 + r3::round_up(units * sizeof(Sums), 256) + 2 * r3::round_up(units * sizeof(int), 256) +
+    return 256 + r3::round_up(units * sizeof(Sums), 256) + r3::round_up(units * sizeof(Marks), 256) + 2 * r3::round_up(units * sizeof(int), 256) +
            r3::round_up((units + WARPS - 1) / WARPS * sizeof(Total), 256);
 }
 
@@ -596,6 +652,8 @@ extern "C" r3_status r3_policy_loss(const r3_policy* c, const float* logp, const
     ws += 256;
     a.sums = reinterpret_cast<Sums*>(ws);
     ws += round_up((size_t)a.units * sizeof(Sums), 256);
+    a.marks = reinterpret_cast<Marks*>(ws);
+    ws += round_up((size_t)a.units * sizeof(Marks), 256);
     a.n = reinterpret_cast<int*>(ws);
     ws += round_up((size_t)a.units * sizeof(int), 256);
     a.head = reinterpret_cast<int*>(ws);

@@ -256,3 +256,21 @@ def test_bad_bounds_are_reported_and_stay_in_range(r3, cu, T):
     bad = not (cu[0] == 0 and all(a <= b for a, b in zip(cu, cu[1:])) and cu[-1] <= T)
     assert st.item() == (r3.DEV_BAD_INDEX if bad else 0) and dlogp.shape == (T,)
     assert (guard == 7.0).all()
+
+
+@pytest.mark.parametrize("T,S", [(700, 5), (300000, 50), (40000, 400)])
+def test_ratios_of_sequences_without_other_terms(r3, T, S):
+    """Nothing but the mask is read again: terms, clipped and capped tokens come from the first pass, whole
+    sequences beyond a border and such without a token among them."""
+    cu = lengths(T, S, 7)
+    for seed, per_sequence in enumerate((True, False, True)):
+        t = make(T, cu, seed, per_sequence=per_sequence, infer=seed > 0, mask=0.2 * seed)
+        for i in range(0, S, 3):                            # far below, far above
+            t["logp"][cu[i]:cu[i + 1]] += 0.7 if i % 2 else -0.7
+        for reduce in ("token", "sequence"):
+            args = dict(ratio="sequence", reduce=reduce, clip_low=0.2, clip_high=0.3, dual_clip=1.6, infer_cap=1.2)
+            ref = oracle(t, cu, **args)
+            assert 0 < ref["clipped"] < ref["tokens"]
+            check(call(r3, t, cu, **args), t, ref)
+            bare = call(r3, t, cu, want_grad=False, **args)
+            assert torch.equal(bare[0], call(r3, t, cu, **args)[0])

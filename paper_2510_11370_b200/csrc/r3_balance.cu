@@ -52,8 +52,7 @@ struct Args {
     float* loss;                          // [L, 2]
     float* dlogits;                       // or null
     int32_t* part_counts;                 // [L, count_parts, E + 1]: per expert, then the tokens
-    float* part_probs;                    // [grid + L, E]: a row per CTA and block that it has tokens of
-    double* part_z;                       // [grid + L]
+    double2* part;                        // [grid + L]: the sums of a CTA and a block that it has tokens of
     unsigned* ticket;                     // [L]
     int32_t* dev_status;
 };
@@ -369,47 +368,41 @@ __global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_ker
             }
         }
         __syncthreads();
-        // a row of its own per CTA and block: CTAs that cross a border have two or more
-        const size_t at = (size_t)blockIdx.x + l;
+        // this CTA's part of sum_i counts_i sum_t p_ti
+        double balance = 0.0, zz = 0.0;
         for (int c = threadIdx.x; c < E; c += THREADS) {
             float all = 0.f;
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) all += s_col[w * E + c];
-            a.part_probs[at * E + c] = all;
+            balance += (double)all * (double)s_n[c];
         }
-        if (threadIdx.x == 0) {
-            double all = 0.0;
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) all += s_z[w];
-            a.part_z[at] = all;
-        }
-        __threadfence();
+        for (int o = 16; o > 0; o >>= 1) balance += __shfl_xor_sync(0xffffffffu, balance, o);
+        if (lane == 0) s_b[warp] = balance;
         __syncthreads();
         const int c_first = a.T > 0 ? cta_of(a, block0) : 0, c_last = a.T > 0 ? cta_of(a, block0 + a.T - 1) : 0;
         const int parts = c_last - c_first + 1;
-        if (threadIdx.x == 0) s_last = a.alone || atomicAdd(a.ticket + l, 1u) == (unsigned)parts - 1u;
+        if (threadIdx.x == 0) {
+            balance = 0.0;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                balance += s_b[w];
+                zz += s_z[w];
+            }
+            // a place of its own per CTA and block: CTAs that cross a border have two or more
+            a.part[blockIdx.x + l] = make_double2(balance, zz);
+            __threadfence();
+            s_last = a.alone || atomicAdd(a.ticket + l, 1u) == (unsigned)parts - 1u;
+        }
         __syncthreads();
         if (!s_last) continue;
         __threadfence();
-        // sum_i counts_i sum_parts p: the parts' rows lie one after the other, every thread takes its share of
-        // all their numbers
-        float share = 0.f;                             // (of a few dozen numbers; the threads' are added in 64 bits)
-        const float* p = a.part_probs + ((size_t)c_first + l) * E;
-        if (WIDE) {
-            const int wide = E / 4, four = parts * wide;
-#pragma unroll 10
-            for (int i = threadIdx.x; i < four; i += THREADS) {
-                const float4 v = __ldcg(reinterpret_cast<const float4*>(p) + i);
-                const float4 n = *reinterpret_cast<const float4*>(s_n + i % wide * 4);
-                share += v.x * n.x + v.y * n.y + v.z * n.z + v.w * n.w;
-            }
-        } else {
-#pragma unroll 10
-            for (int i = threadIdx.x; i < parts * E; i += THREADS) share += __ldcg(p + i) * s_n[i % E];
+        balance = zz = 0.0;
+        for (int q = threadIdx.x; q < parts; q += THREADS) {
+            const double2 part = __ldcg(a.part + (size_t)c_first + l + q);
+            balance += part.x;
+            zz += part.y;
         }
-        double balance = (double)share;
-        double zz = 0.0;
-        for (int q = threadIdx.x; q < parts; q += THREADS) zz += __ldcg(a.part_z + (size_t)c_first + l + q);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
             balance += __shfl_xor_sync(0xffffffffu, balance, o);
@@ -464,7 +457,7 @@ static r3_status check(const r3_shape* s, int32_t L, const r3_balance* c) {
     return s->E > MAX_EXPERTS ? R3_ERR_UNSUPPORTED : R3_OK;
 }
 struct Layout {
-    size_t counts, probs, z, ticket, total;
+    size_t counts, part, ticket, total;
 };
 static Layout layout(const r3_shape* s, int32_t L, const Plan& p) {
     Layout w;
@@ -475,8 +468,7 @@ static Layout layout(const r3_shape* s, int32_t L, const Plan& p) {
         return here;
     };
     w.counts = take((size_t)L * p.count_parts * (s->E + 1) * 4);
-    w.probs = take(((size_t)p.grid + L) * s->E * 4);
-    w.z = take(((size_t)p.grid + L) * 8);
+    w.part = take(((size_t)p.grid + L) * sizeof(double2));
     w.ticket = take((size_t)L * 4);
     w.total = at;
     return w;
@@ -580,8 +572,7 @@ extern "C" r3_status r3_balance_loss(const r3_shape* s, int32_t L, const r3_bala
     a.dlogits = dlogits;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     a.part_counts = reinterpret_cast<int32_t*>(ws + w.counts);
-    a.part_probs = reinterpret_cast<float*>(ws + w.probs);
-    a.part_z = reinterpret_cast<double*>(ws + w.z);
+    a.part = reinterpret_cast<double2*>(ws + w.part);
     a.ticket = reinterpret_cast<unsigned*>(ws + w.ticket);
     a.dev_status = dev_status;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);

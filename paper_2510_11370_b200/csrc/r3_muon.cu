@@ -11,8 +11,8 @@
 // result's rms, against 1.7e-3 for the rounding; bf16 operands with a rounded X lose a third of a rank-8 update).
 // For float32 results A and B get a second plane as well and every product is hi lo + lo hi + hi hi.
 //
-// One GEMM kernel does all three, with two CTAs per MMA (256 x 256 tiles, 128 rows of each operand per CTA and k
-// block of 64, accumulators double buffered in tensor memory).  B = a I + b A + c A^2, the identity within, so
+// One GEMM kernel does all three, with two CTAs per MMA (256 x 256 tiles, or 256 x 128 where they are few; 128 rows of
+// the left operand per CTA and k block of 64, accumulators double buffered in tensor memory).  B = a I + b A + c A^2, the identity within, so
 // that the last product is the whole of the new X (one product: but for a times the lo plane, which is no
 // operand then and comes while the product is formed).  A and B are symmetric: only tiles on and below the
 // diagonal are computed, the others are stored from the same accumulators, transposed.  Eight epilogue warps,
@@ -32,8 +32,8 @@
 namespace r3 {
 namespace ns {
 
-constexpr int BM = 128;                   // rows of either operand per CTA and stage
-constexpr int TILE = 2 * BM;              // output tile of a CTA pair: TILE x TILE
+constexpr int BM = 128;                   // rows of the left operand per CTA and stage
+constexpr int TILE = 2 * BM;              // rows of a CTA pair's output tile; its columns, TN, are 256 or 128
 constexpr int BK = 64;                    // k per stage: 64 fp16 = one 128-byte swizzle row
 constexpr int UK = 16;                    // k per tcgen05.mma
 constexpr int OPERAND_BYTES = BM * BK * 2;
@@ -44,21 +44,22 @@ constexpr int BAR_BYTES = 256;
 // three products (copied for each by itself they came out of L2 no faster than 60% of the tensor pipe could
 // take them), and the sum of a stage leaves tensor memory for registers, since an addition there drops what
 // lies below the running sum's last place.
-template <int TERMS> struct Ring {
+template <int TERMS, int TN> struct Ring {
     static constexpr int PLANES = TERMS > 1 ? 2 : 1;
-    static constexpr int STAGES = TERMS > 1 ? 3 : 5;
-    static constexpr int SIDE_BYTES = PLANES * OPERAND_BYTES;            // one operand
-    static constexpr int STAGE_BYTES = 2 * SIDE_BYTES;
+    static constexpr int STAGES = TERMS > 1 ? (TN == 256 ? 3 : 4) : (TN == 256 ? 5 : 6);
+    static constexpr int B_BYTES = TN / 2 * BK * 2;                      // of a plane of the right operand
+    static constexpr int SIDE_BYTES = PLANES * OPERAND_BYTES;            // the left operand
+    static constexpr int STAGE_BYTES = SIDE_BYTES + PLANES * B_BYTES;
+    static constexpr bool SPLIT = TERMS > 1 && TN == 256;                // of the register file, see below
     static constexpr int BUFFERS = TERMS > 1 ? 1 : 2;                    // of an epilogue warp
     static constexpr int EPI_BYTES = EPI_WARPS * BUFFERS * EPI_PLANE;
     static constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES + EPI_BYTES + BAR_BYTES;
 };
 constexpr int THREADS = 32 * (4 + EPI_WARPS);        // warp 0 copies, warp 1 multiplies, 2 and 3 fill their group
-// Three products: the epilogue keeps 128 sums a thread, so the register file is split anew between the
+// Three products, 256 columns: the epilogue keeps 128 sums a thread, so the register file is split anew between the
 // first four warps and the others; both shares together are what the launch had (checked before it).
 constexpr int CONTROL_REGS = 40, EPI_REGS = 232, LAUNCH_REGS = 168;
 static_assert(128 * CONTROL_REGS + 32 * EPI_WARPS * EPI_REGS <= THREADS * LAUNCH_REGS, "register split");
-constexpr int TMEM_COLS = 512;            // two accumulator stages of TILE columns
 constexpr int MAX_CLASSES = 4;            // shapes of a launch
 
 enum Phase { GRAM, POLY, APPLY };
@@ -95,13 +96,22 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
 
-constexpr int SLOT = TILE * TILE / 4;     // float4 of a part's sums: [rank][warp][4 columns][row]
+template <int TN> constexpr int SLOT = TILE * TN / 4;        // float4 of a part's sums: [rank][warp][4 columns][row]
 struct Tile {
     int k, z, m, n;                       // class, matrix, tile row and column
     int k0, k1, slot;                     // k blocks; number of the part
 };
-// Symmetric results: the tiles with m >= n, row by row.
-template <int PHASE> __device__ __forceinline__ Tile decode(const GemmArgs& g, int item) {
+// Symmetric results: the tiles on the diagonal and below it, row by row.  Those of 128 columns: 2 m + 2 of them
+// in row m, the last two on the diagonal.
+template <int TN> __device__ __forceinline__ void lower_tile(int r, int* m_out, int* n_out) {
+    constexpr int F = TILE / TN;                         // F m (m + 1) / 2 tiles stand before row m
+    int m = (int)((sqrtf(8.f / F * (float)r + 1.f) - 1.f) * 0.5f);
+    while (F * m * (m + 1) / 2 > r) --m;
+    while (F * (m + 1) * (m + 2) / 2 <= r) ++m;
+    *m_out = m;
+    *n_out = r - F * m * (m + 1) / 2;
+}
+template <int PHASE, int TN> __device__ __forceinline__ Tile decode(const GemmArgs& g, int item) {
     Tile t;
     t.k = 0;
 #pragma unroll
@@ -121,11 +131,7 @@ template <int PHASE> __device__ __forceinline__ Tile decode(const GemmArgs& g, i
     t.z = item / c.tiles;
     const int r = item - t.z * c.tiles;
     if (PHASE != APPLY) {
-        int m = (int)((sqrtf(8.f * (float)r + 1.f) - 1.f) * 0.5f);
-        while (m * (m + 1) / 2 > r) --m;
-        while ((m + 1) * (m + 2) / 2 <= r) ++m;
-        t.m = m;
-        t.n = r - m * (m + 1) / 2;
+        lower_tile<TN>(r, &t.m, &t.n);
     } else {
         t.m = r / c.tiles_n;
         t.n = r - t.m * c.tiles_n;
@@ -144,11 +150,13 @@ __device__ __forceinline__ void half8(const uint4& v, float (&f)[8]) {
 
 // GRAM: A = X X^T.  POLY: B = a I + b A + c A^2.  APPLY: X = B X (one product: + a times X's lo plane, which
 // is no operand then).  TERMS: products per product.
-template <int PHASE, int TERMS>
+template <int PHASE, int TERMS, int TN>
 __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant__ GemmArgs g) {
     constexpr bool SYM = PHASE != APPLY;
     constexpr int OUT = SYM && TERMS == 1 ? 1 : 2;     // planes of D
-    using R = Ring<TERMS>;
+    using R = Ring<TERMS, TN>;
+    constexpr int BN = TN / 2;                         // rows of the right operand per CTA and stage
+    constexpr int CW = TN / 2;                         // columns of an epilogue warp
     constexpr int STAGES = R::STAGES, STAGE_BYTES = R::STAGE_BYTES, SIDE_BYTES = R::SIDE_BYTES;
     constexpr int EPI_BYTES = R::EPI_BYTES, BUFFERS = R::BUFFERS;
     extern __shared__ uint8_t smem_raw[];
@@ -178,7 +186,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
         *abort_flag = 0;
         fence_barrier_init();
     }
-    if (warp == 1) tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), TMEM_COLS);
+    if (warp == 1) tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), 2 * TN);
     if (warp == 2 && lane < 2 * g.classes) {
         const ClassArgs& c = g.c[lane >> 1];
         if (lane & 1) {
@@ -198,10 +206,11 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
     grid_dependency_wait();
 
     // a tile on the diagonal of A or of A^2 has the same rows on both sides: copied once
-    auto alike = [&](const Tile& t) { return SYM && t.m == t.n; };
+    auto diagonal = [&](const Tile& t) { return SYM && t.m == t.n * TN / TILE; };
+    auto alike = [&](const Tile& t) { return TN == TILE && diagonal(t); };
 
     if (warp < 4) {
-        if constexpr (TERMS > 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CONTROL_REGS));
+        if constexpr (R::SPLIT) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(CONTROL_REGS));
         if (warp == 0) {
             // ------------------------------ TMA producer: this CTA's half of both operands ---------
             if (lane == 0) {
@@ -209,9 +218,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                 uint32_t phase = 0;
                 bool ok = true;
                 for (int item = pair; ok && item < g.items; item += pairs) {
-                    const Tile t = decode<PHASE>(g, item);
+                    const Tile t = decode<PHASE, TN>(g, item);
                     const ClassArgs& c = g.c[t.k];
-                    const int m0 = t.m * TILE + (int)rank * BM, n0 = t.n * TILE + (int)rank * BM;
+                    const int m0 = t.m * TILE + (int)rank * BM, n0 = t.n * TN + (int)rank * BN;
                     const bool once = alike(t);
                     for (int kb = t.k0; kb < t.k1; ++kb) {
                         if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, g.dev_status)) {
@@ -220,10 +229,10 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                         }
                         const uint32_t sa = base + stage * STAGE_BYTES, sb = sa + SIDE_BYTES;
                         const uint32_t lead = mapa_shared(full_bar(stage), 0);
-                        if (rank == 0) mbar_expect_tx(full_bar(stage), (once ? 1u : 2u) * STAGE_BYTES);
+                        if (rank == 0) mbar_expect_tx(full_bar(stage), 2u * (uint32_t)(once ? SIDE_BYTES : STAGE_BYTES));
 #pragma unroll
                         for (int pl = 0; pl < R::PLANES; ++pl) {
-                            const uint32_t ta = sa + pl * OPERAND_BYTES, tb = sb + pl * OPERAND_BYTES;
+                            const uint32_t ta = sa + pl * OPERAND_BYTES, tb = sb + pl * R::B_BYTES;
                             if (c.a_mn) {
                                 tma_load_3d_pair(ta, &c.a[pl], m0, kb * BK, t.z, lead);
                                 tma_load_3d_pair(ta + OPERAND_BYTES / 2, &c.a[pl], m0 + 64, kb * BK, t.z, lead);
@@ -233,7 +242,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                             if (once) continue;
                             if (c.b_mn) {
                                 tma_load_3d_pair(tb, &c.b[pl], n0, kb * BK, t.z, lead);
-                                tma_load_3d_pair(tb + OPERAND_BYTES / 2, &c.b[pl], n0 + 64, kb * BK, t.z, lead);
+                                if (BN > 64) tma_load_3d_pair(tb + OPERAND_BYTES / 2, &c.b[pl], n0 + 64, kb * BK, t.z, lead);
                             } else {
                                 tma_load_3d_pair(tb, &c.b[pl], kb * BK, n0, t.z, lead);
                             }
@@ -254,9 +263,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                 uint32_t phase = 0, acc_phase = 0;
                 bool ok = true;
                 for (int item = pair; ok && item < g.items; item += pairs) {
-                    const Tile t = decode<PHASE>(g, item);
+                    const Tile t = decode<PHASE, TN>(g, item);
                     const ClassArgs& c = g.c[t.k];
-                    const uint32_t idesc = (1u << 4) | ((uint32_t)(TILE >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24) |
+                    const uint32_t idesc = (1u << 4) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24) |
                                            (c.a_mn ? 1u << 15 : 0u) | (c.b_mn ? 1u << 16 : 0u);
                     // 16 along k: 32 bytes inside the swizzled row, or two groups of 8 k rows
                     const uint64_t a_step = c.a_mn ? (2048 >> 4) : 2, b_step = c.b_mn ? (2048 >> 4) : 2;
@@ -276,7 +285,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                         }
                         tc_fence_after();
                         if (elect_one()) {
-                            const uint32_t d_tmem = tmem_base + (uint32_t)(acc * TILE);
+                            const uint32_t d_tmem = tmem_base + (uint32_t)(acc * TN);
                             const uint32_t sa = base + stage * STAGE_BYTES, sb = sa + to_b;
                             const uint64_t da = c.a_mn ? smem_desc_mn_sw128(sa, OPERAND_BYTES / 2)
                                                        : smem_desc_sw128(sa);
@@ -286,7 +295,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                             for (int term = 0; term < TERMS; ++term) {
                                 // (hi, lo), (lo, hi), (hi, hi): the small products first
                                 const uint64_t ta = da + (TERMS > 1 && term == 1 ? OPERAND_BYTES >> 4 : 0);
-                                const uint64_t tb = db + (TERMS > 1 && term == 0 ? OPERAND_BYTES >> 4 : 0);
+                                const uint64_t tb = db + (TERMS > 1 && term == 0 ? R::B_BYTES >> 4 : 0);
 #pragma unroll
                                 for (int kk = 0; kk < BK / UK; ++kk)
                                     tc_mma_bf16_pair(d_tmem, ta + a_step * kk, tb + b_step * kk, idesc,
@@ -304,7 +313,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
         }
     } else {
         // ------------------------------ epilogue ------------------------------------------------
-        if constexpr (TERMS > 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(EPI_REGS));
+        if constexpr (R::SPLIT) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(EPI_REGS));
         const int w = warp - 4, q = warp & 3, half = w >> 2;
         const uint32_t buf = epi0 + (uint32_t)w * (BUFFERS * EPI_PLANE);
         uint8_t* buf_ptr = base_ptr + STAGES * STAGE_BYTES + w * (BUFFERS * EPI_PLANE);
@@ -348,15 +357,15 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
             if (BUFFERS > 1) turn ^= 1;
         };
         for (int item = pair; item < g.items; item += pairs) {
-            const Tile t = decode<PHASE>(g, item);
+            const Tile t = decode<PHASE, TN>(g, item);
             const ClassArgs& c = g.c[t.k];
             const int row0 = t.m * TILE + (int)rank * BM + q * 32, row = row0 + lane;
-            const int first = t.n * TILE + half * 128;           // this warp's 128 columns
+            const int first = t.n * TN + half * CW;              // this warp's columns
             const bool inside = row0 < c.rows && first < c.cols;
-            // what is added to the product: one plane of the warp's 128 columns, which come while it is formed, or
+            // what is added to the product: one plane of the warp's columns, which come while it is formed, or
             // (three products, whose sums take the registers) both planes of 64 of them at a time
             constexpr bool ADDS = PHASE == POLY || (PHASE == APPLY && TERMS == 1);
-            uint4 early[ADDS ? 16 : 1];
+            uint4 early[ADDS ? (TERMS == 1 ? CW / 8 : 16) : 1];
             // (four rows x 128 bytes per load: row by row, 32 lines a load, the eight warps' loads took 8500 clocks)
             const int mine = row0 + (lane >> 3), left = c.rows - mine, hop = 4 * c.in_ld;
             const long long in_at = (long long)t.z * c.in_plane + (long long)mine * c.in_ld;
@@ -387,14 +396,14 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                 __syncwarp();
             };
             if constexpr (ADDS && TERMS == 1) {
-                fetch(early, 0, 0);
-                fetch(early + 8, 0, 1);
+#pragma unroll
+                for (int p = 0; p < CW / 64; ++p) fetch(early + 8 * p, 0, p);
             }
             constexpr bool KEEP = TERMS > 1 || PHASE == GRAM;    // the sums go through registers as a whole
-            float sum[KEEP ? 128 : 1];
+            float sum[KEEP ? CW : 1];
             if constexpr (KEEP) {
 #pragma unroll
-                for (int i = 0; i < 128; ++i) sum[i] = 0.f;
+                for (int i = 0; i < CW; ++i) sum[i] = 0.f;
             }
             uint32_t tacc = 0;
 #pragma unroll 1
@@ -404,11 +413,11 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                     alive = __all_sync(0xffffffffu, ok);
                 }
                 tc_fence_after();
-                tacc = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * TILE + half * 128);
+                tacc = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * TN + half * CW);
                 if constexpr (KEEP) {
                     if (alive && inside) {
 #pragma unroll
-                        for (int p = 0; p < 4; ++p) {
+                        for (int p = 0; p < CW / 32; ++p) {
                             float v[32];
                             tc_ld32(tacc + 32 * p, v);
                             tc_wait_ld();
@@ -425,9 +434,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
             if constexpr (PHASE == GRAM) {
                 if (c.splits > 1) {
                     if (alive && inside) {
-                        float4* to = c.partial + (size_t)t.slot * SLOT + (((int)rank * EPI_WARPS + w) * 32) * 32 + lane;
+                        float4* to = c.partial + (size_t)t.slot * SLOT<TN> + ((int)rank * EPI_WARPS + w) * (CW / 4) * 32 + lane;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
+                        for (int j = 0; j < CW / 4; ++j)
                             to[j * 32] = make_float4(sum[4 * j], sum[4 * j + 1], sum[4 * j + 2], sum[4 * j + 3]);
                     }
                     continue;
@@ -435,7 +444,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
             }
             if (alive && inside) {
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
+                for (int p = 0; p < CW / 64; ++p) {
                     const int col0 = first + 64 * p;
                     if (col0 >= c.cols) continue;
                     if constexpr (ADDS) {
@@ -461,7 +470,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                         }
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            const int o = 8 * p + 4 * h + j;           // octet of columns within the 128
+                            const int o = 8 * p + 4 * h + j;           // octet of the warp's columns
                             float x[8], l[8];
 #pragma unroll
                             for (int i = 0; i < 8; ++i) x[i] = g.alpha * v[8 * j + i];
@@ -476,7 +485,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
 #pragma unroll
                                 for (int i = 0; i < 8; ++i) x[i] = fmaf(g.beta, l[i], x[i]);
                             }
-                            if (PHASE == POLY && t.m == t.n) {
+                            if (PHASE == POLY && diagonal(t)) {
 #pragma unroll
                                 for (int i = 0; i < 8; ++i)
                                     if (first + 8 * o + i == row) x[i] += g.diag;
@@ -495,7 +504,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                     }
 #pragma unroll
                     for (int pl = 0; pl < OUT; ++pl) emit(packed[pl], &c.out[pl], col0, row0, t.z);
-                    if (SYM && t.m != t.n) {
+                    if (SYM && !diagonal(t)) {
 #pragma unroll
                         for (int pl = 0; pl < OUT; ++pl) emit_mirror(packed[pl], &c.mirror[pl], col0, row0, t.z);
                     }
@@ -522,12 +531,12 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
     cluster_sync_all();
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc_pair(tmem_base, TMEM_COLS);
+        tmem_dealloc_pair(tmem_base, 2 * TN);
     }
 }
 
-// The parts of A's tiles added up: A = alpha sum, into both triangles.  A CTA takes 32 rows x 128 columns (what an
-// epilogue warp left).
+// The parts of A's tiles added up: A = alpha sum, into both triangles.  A CTA takes what an epilogue
+// warp left, 32 rows x 128 or 64 columns.
 constexpr int FOLD_THREADS = 256;
 struct FoldClass {
     const float4* partial;
@@ -539,9 +548,10 @@ struct FoldArgs {
     int classes;
     float alpha;
 };
-template <int PLANES>
+template <int PLANES, int TN>
 __global__ void __launch_bounds__(FOLD_THREADS) fold_kernel(const __grid_constant__ FoldArgs a) {
-    __shared__ __align__(16) __half s_tile[PLANES][32][128 + 8];
+    constexpr int CW = TN / 2, EACH = CW / 32;           // float4 of a thread
+    __shared__ __align__(16) __half s_tile[PLANES][32][CW + 8];
     grid_launch_dependents();
     grid_dependency_wait();
     int k = 0;
@@ -551,22 +561,21 @@ __global__ void __launch_bounds__(FOLD_THREADS) fold_kernel(const __grid_constan
     const FoldClass& c = a.c[k];
     const int b = (int)blockIdx.x - c.first, region = b & 15, tile = b >> 4;
     const int z = tile / c.tiles, r = tile - z * c.tiles;
-    int m = (int)((sqrtf(8.f * (float)r + 1.f) - 1.f) * 0.5f);
-    while (m * (m + 1) / 2 > r) --m;
-    while ((m + 1) * (m + 2) / 2 <= r) ++m;
-    const int n = r - m * (m + 1) / 2, rank = region >> 3, w = region & 7;
+    int m, n;
+    lower_tile<TN>(r, &m, &n);
+    const int rank = region >> 3, w = region & 7;
     // (warp 4 + w of the epilogue: lane quadrant w & 3, column half w >> 2)
-    const int row0 = m * TILE + rank * BM + (w & 3) * 32, col0 = n * TILE + (w >> 2) * 128;
+    const int row0 = m * TILE + rank * BM + (w & 3) * 32, col0 = n * TN + (w >> 2) * CW;
     if (row0 >= c.m || col0 >= c.m) return;
-    const float4* from = c.partial + (size_t)tile * c.splits * SLOT + region * 1024;
-    float4 v[4];
+    const float4* from = c.partial + (size_t)tile * c.splits * SLOT<TN> + region * (CW / 4) * 32;
+    float4 v[EACH];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int e = 0; e < EACH; ++e) v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
     for (int s = 0; s < c.splits; ++s) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float4 p = from[(size_t)s * SLOT + threadIdx.x + FOLD_THREADS * e];
+        for (int e = 0; e < EACH; ++e) {
+            const float4 p = from[(size_t)s * SLOT<TN> + threadIdx.x + FOLD_THREADS * e];
             v[e].x += p.x;
             v[e].y += p.y;
             v[e].z += p.z;
@@ -574,7 +583,7 @@ __global__ void __launch_bounds__(FOLD_THREADS) fold_kernel(const __grid_constan
         }
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < EACH; ++e) {
         const int i = threadIdx.x + FOLD_THREADS * e, row = i & 31, col = 4 * (i >> 5);
         const float x[4] = {a.alpha * v[e].x, a.alpha * v[e].y, a.alpha * v[e].z, a.alpha * v[e].w};
 #pragma unroll
@@ -589,13 +598,13 @@ __global__ void __launch_bounds__(FOLD_THREADS) fold_kernel(const __grid_constan
     for (int pl = 0; pl < PLANES; ++pl) {
         __half* out = c.out[pl] + (size_t)z * c.m * c.ld;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < CW / 64; ++e) {
             const int i = threadIdx.x + FOLD_THREADS * e;
-            const int row = i >> 4, col = 8 * (i & 15);
+            const int row = i / (CW / 8), col = 8 * (i % (CW / 8));
             if (row0 + row < c.m && col0 + col < c.ld)
                 *reinterpret_cast<uint4*>(out + (size_t)(row0 + row) * c.ld + col0 + col) =
                     *reinterpret_cast<const uint4*>(&s_tile[pl][row][col]);
-            if (m == n) continue;
+            if (m == n * TN / TILE) continue;
             const int mc = i >> 2, mr = 8 * (i & 3);   // column of the tile, eight of its rows
             if (col0 + mc >= c.m || row0 + mr >= c.ld) continue;
             __half h[8];
@@ -975,10 +984,11 @@ static int resident_pairs(void (*kern)(GemmArgs), bool split, int smem, int (&ca
     return cached[dev];
 }
 
-template <int PHASE, int TERMS> static r3_status launch_gemm(const GemmArgs& g, cudaStream_t cs) {
-    auto kern = gemm_kernel<PHASE, TERMS>;
+template <int PHASE, int TERMS, int TN> static r3_status launch_gemm(const GemmArgs& g, cudaStream_t cs) {
+    auto kern = gemm_kernel<PHASE, TERMS, TN>;
+    using R = Ring<TERMS, TN>;
     static int cached[64] = {0};
-    const int pairs = resident_pairs(kern, TERMS > 1, Ring<TERMS>::SMEM_BYTES, cached);
+    const int pairs = resident_pairs(kern, R::SPLIT, R::SMEM_BYTES, cached);
     if (pairs <= 0) return R3_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
@@ -990,7 +1000,7 @@ template <int PHASE, int TERMS> static r3_status launch_gemm(const GemmArgs& g, 
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.gridDim = dim3(2 * (g.items < pairs ? g.items : pairs));
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = Ring<TERMS>::SMEM_BYTES;
+    cfg.dynamicSmemBytes = R::SMEM_BYTES;
     cfg.stream = cs;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
@@ -1004,55 +1014,77 @@ struct Class {
     uint8_t* ws;
 };
 
-static int square_tiles(const Problem& p) {
+static int square_tiles(const Problem& p, int tn) {
     const int t = (p.m + TILE - 1) / TILE;
-    return t * (t + 1) / 2;
+    return tn == TILE ? t * (t + 1) / 2 : t * (t - 1) + (p.m + tn - 1) / tn;
 }
+static int all_tiles(const Problem& p, int tn) { return (p.rows + TILE - 1) / TILE * ((p.cols + tn - 1) / tn); }
 static int gram_blocks(const Problem& p) { return ((p.tall ? p.rows : p.cols) + BK - 1) / BK; }
-// How many k blocks of A = X X^T a CTA pair takes at a time, so that few tiles with long sums still spread over
-// the GPU.  In units of a k block's time (0.27 us; three products 0.8): a part costs its blocks and about 3 us
-// around them, parts cost a launch that adds them up, about 4 us.  150 x 4000 f32: 444 us whole, 248 in parts.
+// A round's tiles and the parts of its long sums, by estimates of the time in 20ths of a k block's with 256
+// columns (0.27 us; three products 0.8): a CTA pair's item costs its k blocks and what stands around them.
+// Tiles of 128 columns take 14 (13) of a block and half of the rest, and are twice as many: few tiles spread over
+// more of the GPU (us, 256 -> 128 columns: 1024 x 1024 f32 371 -> 271, 768 x 2048 bf16 233 -> 168, 4 x 1024 x
+// 1024 bf16 225 -> 277, 8 x 768 x 2048 bf16 331 -> 437).
 constexpr int MAX_SPLITS = 8;
-static int part_of_k(const Class* classes, int n, int terms) {
+struct Cut {
+    int tn, part;                         // columns of the tiles; k blocks of A = X X^T that a CTA pair takes at a time
+};
+static long long waves(long long items) {
     const int pairs = sm_count() / 2;
-    const int around = terms > 1 ? 4 : 11, fold = terms > 1 ? 5 : 15;
-    int longest = 0;
-    for (int i = 0; i < n; ++i) longest = std::max(longest, gram_blocks(classes[i].p));
-    int best = longest;
+    return (items + pairs - 1) / pairs;
+}
+static Cut cut_of(const Class* classes, int n, int terms) {
+    Cut best = {256, 1};
     long long least = -1;
-    for (int splits = 1; splits <= MAX_SPLITS; ++splits) {
-        const int part = (longest + splits - 1) / splits;
-        long long items = 0, slots = 0;
+    int longest = 0, side = 0;
+    for (int i = 0; i < n; ++i) {
+        longest = std::max(longest, gram_blocks(classes[i].p));
+        side = std::max(side, (classes[i].p.m + BK - 1) / BK);
+    }
+    for (int tn : {256, 128}) {
+        const int block = tn == 256 ? 20 : terms > 1 ? 13 : 14;
+        const int around = (terms > 1 ? 80 : 220) * tn / 256;
+        long long square = 0, all = 0;
         for (int i = 0; i < n; ++i) {
-            const int parts = (gram_blocks(classes[i].p) + part - 1) / part;
-            items += (long long)square_tiles(classes[i].p) * classes[i].count * parts;
-            if (parts > 1) slots += (long long)square_tiles(classes[i].p) * classes[i].count * parts;
+            square += (long long)square_tiles(classes[i].p, tn) * classes[i].count;
+            all += (long long)all_tiles(classes[i].p, tn) * classes[i].count;
         }
-        if (slots > 4LL * pairs) break;
-        const long long cost = (items + pairs - 1) / pairs * (part + around) + (slots ? fold : 0);
-        if (least < 0 || cost < least) {
-            least = cost;
-            best = part;
+        const long long others = (waves(square) + waves(all)) * (side * block + around);
+        // parts cost a launch that adds them up, 3 to 4 us (150 x 4000 f32, 256 columns: 444 us whole, 248 in parts)
+        const int fold = terms > 1 ? 70 : 300;
+        for (int splits = 1; splits <= MAX_SPLITS; ++splits) {
+            const int part = (longest + splits - 1) / splits;
+            long long items = 0, slots = 0;
+            for (int i = 0; i < n; ++i) {
+                const int parts = (gram_blocks(classes[i].p) + part - 1) / part;
+                const long long here = (long long)square_tiles(classes[i].p, tn) * classes[i].count * parts;
+                items += here;
+                if (parts > 1) slots += here;
+            }
+            if (slots > 4LL * (sm_count() / 2)) break;
+            const long long cost = others + waves(items) * (part * block + around) + (slots ? fold : 0);
+            if (least < 0 || cost < least) {
+                least = cost;
+                best = {tn, part};
+            }
         }
     }
     return best;
 }
-static size_t partial_bytes(const Class* classes, int n, int terms) {
-    const int part = part_of_k(classes, n, terms);
+static size_t partial_bytes(const Class* classes, int n, int terms, const Cut& cut) {
     size_t slots = 0;
     for (int i = 0; i < n; ++i) {
-        const int parts = (gram_blocks(classes[i].p) + part - 1) / part;
-        if (parts > 1) slots += (size_t)square_tiles(classes[i].p) * classes[i].count * parts;
+        const int parts = (gram_blocks(classes[i].p) + cut.part - 1) / cut.part;
+        if (parts > 1) slots += (size_t)square_tiles(classes[i].p, cut.tn) * classes[i].count * parts;
     }
-    return slots * SLOT * sizeof(float4);
+    return slots * (TILE * cut.tn / 4) * sizeof(float4);
 }
 
 // The iteration on classes whose X stand in the planes 0; on return *at says which planes hold the results.
-// partial: partial_bytes of memory.
-template <int TERMS>
-static r3_status iterate(const Class* classes, int n, uint8_t* partial, const Coefs& coefs, int32_t* dev_status,
-                         int* at, cudaStream_t cs) {
-    const int part = part_of_k(classes, n, TERMS);
+// part: k blocks of a part of X X^T; partial: partial_bytes of memory.
+template <int TERMS, int TN>
+static r3_status iterate(const Class* classes, int n, int part, uint8_t* partial, const Coefs& coefs,
+                         int32_t* dev_status, int* at, cudaStream_t cs) {
     FoldArgs fold = {};
     int fold_ctas = 0;
     float4* next_partial = reinterpret_cast<float4*>(partial);
@@ -1064,18 +1096,20 @@ static r3_status iterate(const Class* classes, int n, uint8_t* partial, const Co
         const int count = classes[i].count;
         const Layout w = layout(p, count);
         uint8_t* ws = classes[i].ws;
-        const int tm = (p.m + TILE - 1) / TILE, tr = (p.rows + TILE - 1) / TILE, tc = (p.cols + TILE - 1) / TILE;
+        const int tc = (p.cols + TN - 1) / TN;
         ClassArgs& q = poly.c[i];
         // an operand with consecutive k: 64 x 128 boxes; with k along the rows: 64 x 64, two per stage
         for (int pl = 0; pl < 2; ++pl) {
             const uint8_t* A = ws + w.a[pl];
             const uint8_t* B = ws + w.b[pl];
-            CUtensorMap bk;
+            CUtensorMap bk;                  // (a right operand takes TN / 2 rows at a time)
             ok = ok && make_map(&q.a[pl], A, count, p.m, p.m, p.ldm, 64, BM, true) &&
                  make_map(&bk, B, count, p.m, p.m, p.ldm, 64, BM, true) &&
                  make_map(&q.out[pl], B, count, p.m, p.m, p.ldm, 64, 32, true) &&
                  make_map(&q.mirror[pl], B, count, p.m, p.m, p.ldm, 32, 64, false);
-            q.b[pl] = q.a[pl];
+            ok = ok && make_map(&q.b[pl], A, count, p.m, p.m, p.ldm, 64, TN / 2, true);
+            CUtensorMap b_right;
+            ok = ok && make_map(&b_right, B, count, p.m, p.m, p.ldm, 64, TN / 2, true);
             q.in[pl] = reinterpret_cast<const __half*>(A);
             for (int k = 0; k < 2; ++k) {
                 const uint8_t* x = ws + (pl ? w.lo[k] : w.hi[k]);
@@ -1084,7 +1118,8 @@ static r3_status iterate(const Class* classes, int n, uint8_t* partial, const Co
                 ok = ok && make_map(&xk, x, count, p.rows, p.cols, p.ld, 64, BM, true) &&
                      make_map(&xmn, x, count, p.rows, p.cols, p.ld, 64, BK, true);
                 ClassArgs& gr = gram[k].c[i];
-                gr.a[pl] = gr.b[pl] = p.tall ? xmn : xk;
+                gr.a[pl] = p.tall ? xmn : xk;
+                gr.b[pl] = p.tall || TN == 128 ? xmn : xk;     // (64 x 64 either way)
                 if (k == 0)
                     ok = ok && make_map(&gr.out[pl], A, count, p.m, p.m, p.ldm, 64, 32, true) &&
                          make_map(&gr.mirror[pl], A, count, p.m, p.m, p.ldm, 32, 64, false);
@@ -1093,7 +1128,7 @@ static r3_status iterate(const Class* classes, int n, uint8_t* partial, const Co
                 gr.in[pl] = nullptr;
                 ClassArgs& ap = apply[k].c[i];
                 ap.a[pl] = p.tall ? xk : bk;
-                ap.b[pl] = p.tall ? bk : xmn;
+                ap.b[pl] = p.tall ? b_right : xmn;
                 ok = ok && make_map(&ap.out[pl], y, count, p.rows, p.cols, p.ld, 64, 32, true);
                 ap.mirror[pl] = ap.out[pl];
                 ap.in[pl] = reinterpret_cast<const __half*>(ws + w.lo[k]);
@@ -1104,8 +1139,8 @@ static r3_status iterate(const Class* classes, int n, uint8_t* partial, const Co
             c.in_plane = (long long)p.m * p.ldm;
             c.in_ld = p.ldm;
             c.rows = c.cols = p.m;
-            c.tiles_n = tm;
-            c.tiles = tm * (tm + 1) / 2;
+            c.tiles_n = 0;
+            c.tiles = square_tiles(p, TN);
             c.first_item = g.items;
             c.kblocks = kblocks;
             c.a_mn = c.b_mn = mn;
@@ -1127,7 +1162,7 @@ static r3_status iterate(const Class* classes, int n, uint8_t* partial, const Co
             c.rows = p.rows;
             c.cols = p.cols;
             c.tiles_n = tc;
-            c.tiles = tr * tc;
+            c.tiles = all_tiles(p, TN);
             c.first_item = apply[k].items;
             c.kblocks = km;
             c.a_mn = 0;
@@ -1147,7 +1182,7 @@ static r3_status iterate(const Class* classes, int n, uint8_t* partial, const Co
             f.splits = gr.splits;
             f.first = fold_ctas;
             fold_ctas += gr.tiles * count * 2 * EPI_WARPS;
-            next_partial += (size_t)gr.tiles * count * gr.splits * SLOT;
+            next_partial += (size_t)gr.tiles * count * gr.splits * SLOT<TN>;
         }
     }
     fold.alpha = 1.f / SCALE;
@@ -1165,12 +1200,12 @@ static r3_status iterate(const Class* classes, int n, uint8_t* partial, const Co
         poly.beta = c[1];
         poly.diag = c[0] * SCALE;
         apply[k].beta = c[0];
-        r3_status st = launch_gemm<GRAM, TERMS>(gram[k], cs);
+        r3_status st = launch_gemm<GRAM, TERMS, TN>(gram[k], cs);
         if (st == R3_OK && fold_ctas &&
-            launch_dependent(fold_kernel<TERMS == 1 ? 1 : 2>, dim3(fold_ctas), dim3(FOLD_THREADS), 0, cs, fold) != cudaSuccess)
+            launch_dependent(fold_kernel<TERMS == 1 ? 1 : 2, TN>, dim3(fold_ctas), dim3(FOLD_THREADS), 0, cs, fold) != cudaSuccess)
             st = R3_ERR_CUDA;
-        if (st == R3_OK) st = launch_gemm<POLY, TERMS>(poly, cs);
-        if (st == R3_OK) st = launch_gemm<APPLY, TERMS>(apply[k], cs);
+        if (st == R3_OK) st = launch_gemm<POLY, TERMS, TN>(poly, cs);
+        if (st == R3_OK) st = launch_gemm<APPLY, TERMS, TN>(apply[k], cs);
         if (st != R3_OK) return st;
     }
     *at = k;
@@ -1279,8 +1314,11 @@ static r3_status run_round(const Job& job, const Coefs& coefs, Round& r, uint8_t
     }
     if (e != cudaSuccess) return R3_ERR_CUDA;
     int at = 0;
-    const r3_status st = job.terms > 1 ? iterate<3>(r.cls, r.classes, ws, coefs, dev_status, &at, cs)
-                                       : iterate<1>(r.cls, r.classes, ws, coefs, dev_status, &at, cs);
+    const Cut cut = cut_of(r.cls, r.classes, job.terms);
+    const bool narrow = cut.tn == 128;
+    const auto steps = job.terms > 1 ? (narrow ? iterate<3, 128> : iterate<3, 256>)
+                                     : (narrow ? iterate<1, 128> : iterate<1, 256>);
+    const r3_status st = steps(r.cls, r.classes, cut.part, ws, coefs, dev_status, &at, cs);
     if (st != R3_OK) return st;
     planes(at);
     if (!job.step)
@@ -1366,7 +1404,7 @@ static size_t workspace_bytes(const r3_muon_stack* ss, int32_t count, int terms)
                     return R3_OK;
                 },
                 [&](Round& r) {
-                    most = std::max(most, r.bytes + partial_bytes(r.cls, r.classes, terms));
+                    most = std::max(most, r.bytes + partial_bytes(r.cls, r.classes, terms, cut_of(r.cls, r.classes, terms)));
                     return R3_OK;
                 });
     return most;

@@ -11,18 +11,18 @@
 // result's rms, against 1.7e-3 for the rounding; bf16 operands with a rounded X lose a third of a rank-8 update).
 // For float32 results A and B get a second plane as well and every product is hi lo + lo hi + hi hi.
 //
-// One GEMM kernel does all three, with two CTAs per MMA (256 x 256 tiles, or 256 x 128 where they are few; 128 rows of
-// the left operand per CTA and k block of 64, accumulators double buffered in tensor memory).  B = a I + b A + c A^2, the identity within, so
-// that the last product is the whole of the new X (one product: but for a times the lo plane, which is no
-// operand then and comes while the product is formed).  A and B are symmetric: only tiles on and below the
-// diagonal are computed, the others are stored from the same accumulators, transposed.  Eight epilogue warps,
-// each with its own 8 KB (three products: 4 KB) of shared memory, through which results go out by TMA in
-// boxes of 32 rows x 64 columns and addends come in whole lines.
+// One GEMM kernel does all three, with two CTAs per MMA (256 x 256 tiles, or 256 x 128 where they are few; 128
+// rows of the left operand per CTA and k block of 64, accumulators double buffered in tensor memory).
+// B = a I + b A + c A^2, the identity within, so that the last product is the whole of the new X (one product: but
+// for a times the lo plane, which is no operand then and comes while the product is formed).  A and B are
+// symmetric: only tiles on and below the diagonal are computed, the others are stored from the same accumulators,
+// transposed.  Eight epilogue warps, each with its own 8 KB (three products: 4 KB) of shared memory, through
+// which results go out by TMA in boxes of 32 rows x 64 columns and addends come in whole lines.
 // 24 matrices of 768 x 2048, one product: X X^T 35 us, B 21, B X 69, of which the products of their tiles are 23,
-// 9 and 35 at the tensor pipe's rate.  B X takes 281 MB from and to HBM, and its operands, the lo plane and both new planes come
-// and go between L2 and the SMs at 11 to 12.5 TB/s, which bounds it (the tensor pipe is busy 42% of the time);
+// 9 and 35 at the tensor pipe's rate.  B X moves 281 MB to and from HBM, and its operands, the lo plane and both new
+// planes pass between L2 and the SMs at 11 to 12.5 TB/s, which bounds it (the tensor pipe is busy 42% of the time);
 // X X^T and B wait for the first loads and the last stores of their few tiles besides.  Three products, 4096 x
-// 4096: 3150 us, 81% of the tensor pipe's rate: each 64 of k leave tensor memory for registers.
+// 4096: 3150 us for five steps, 81% of the tensor pipe's rate: each 64 of k leave tensor memory for registers.
 #include <algorithm>
 #include <cmath>
 #include <vector>

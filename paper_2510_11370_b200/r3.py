@@ -1332,7 +1332,8 @@ def policy_loss(logp, logp_old, cu_seqlens=None, *, advantages=None, seq_advanta
     logp_infer, logp_ref, entropy [T] float32; cu_seqlens [S+1] int32 (None: one sequence); mask [T] bool or
     uint8; advantages [T] or seq_advantages [S], one of them.  ratio: "token" or "sequence"; reduce: mean
     over "token"s or over "sequence" means, or with denominator the sum over that.  Returns (loss [1],
-    dlogp [T] or None, dentropy [T] or None, metrics [3], counts [3] int32)."""
+    dlogp [T] or None, dentropy [T] or None, metrics [3], counts [3] int32); loss, metrics and counts are parts
+    of one allocation (up to 64 KB with the scratch behind them)."""
     dev = _device_of("logp", logp)
     if logp.dim() != 1:
         raise ValueError("logp: expected [T]")

@@ -113,6 +113,20 @@ def test_many_small_matrices_and_one_large(r3):
         check(r3.orthogonalize(x.cuda(), products=products)[0].cpu(), x[0], products)
 
 
+@pytest.mark.parametrize("products", [1, 3])
+@pytest.mark.parametrize("B,rows,cols", [(24, 520, 300), (24, 300, 520), (8, 300, 6001), (8, 6001, 300)])
+def test_enough_tiles_for_wide_ones(r3, B, rows, cols, products):
+    """So many matrices take tiles of 256 columns, the long ones with their sums in parts; the first and the last
+    are compared, and all of them with what they give elsewhere in the batch."""
+    x = matrix(rows, cols, 13, "decay", B)
+    x[B // 2] = x[0]
+    st = r3.new_status("cuda")
+    got = r3.orthogonalize(x.cuda(), products=products, dev_status=st)
+    assert st.item() == 0 and torch.equal(got[B // 2], got[0])
+    for i in (0, B - 1):
+        check(got[i].cpu(), x[i], products)
+
+
 def test_batches_in_parts(r3):
     """More matrices than the workspace holds at once give what each gives alone."""
     x = matrix(768, 1024, 5, "decay", 90).cuda()

@@ -103,6 +103,24 @@ def test_low_rank_steps_coefficients_and_eps(r3):
             check(got[0].cpu(), x[0], products, steps, coefs, 1e-3)
 
 
+@pytest.mark.parametrize("steps,coefs", [(1, None), (2, None), (5, None), (2, [(2.0, -1.5, 0.5), (5.0, -6.0, 2.0)]),
+                                         (4, [(2.0, -1.5, 0.5)] * 4)])
+@pytest.mark.parametrize("rows,cols", [(200, 320), (320, 200), (96, 100)])
+def test_bf16_results_whose_last_step_needs_less(r3, rows, cols, steps, coefs):
+    """A bf16 result takes the last step from X rounded to fp16, where that step's a is at most 4: a 2^-11 of an
+    element at most, a 2^-13 rms at least and 2^-12 at most, against the rounding's 2^-9 and 2^-9 / sqrt(3)."""
+    for kind in ("full", "low"):
+        x = matrix(rows, cols, 14, kind).to(BF)
+        got = r3.orthogonalize(x.cuda(), steps=steps, coefficients=coefs)[0].cpu()
+        want = O.iterate(f64(x[0]), steps, coefs)
+        model = O.iterate(f64(x[0]), steps, coefs, operand=O.half_operand) - want
+        before = O.iterate(f64(x[0]), steps - 1, coefs) if steps > 1 else 0 * want
+        err, half = f64(got) - want, torch.finfo(BF).eps / 2
+        assert rms(err) <= np.sqrt((1.5 * rms(model)) ** 2 + (half * rms(want)) ** 2 + (4 * 2.0 ** -12 * rms(before)) ** 2)
+        assert (np.abs(err) <= (2 * np.abs(model).max() + 4 * 2.0 ** -11 * np.abs(before).max()) * (1 + half)
+                + half * np.abs(want) + 2.0 ** -20 * np.abs(want).max()).all()
+
+
 def test_many_small_matrices_and_one_large(r3):
     x = matrix(24, 40, 3, "full", 700)
     got = r3.orthogonalize(x.cuda(), products=3)

@@ -299,9 +299,10 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                       lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _stream(stream=None):
+def _stream(stream=None, dev=None):
+    """The handle of a stream, or of the current one; dev: the current device, where it is known."""
     if stream is None:
-        return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
+        return ctypes.c_void_p(_raw_stream(torch.cuda.current_device() if dev is None else dev.index))
     return ctypes.c_void_p(stream.cuda_stream)
 
 
@@ -1382,7 +1383,7 @@ def policy_loss(logp, logp_old, cu_seqlens=None, *, advantages=None, seq_advanta
         None if dloss is None else _arg("dloss", dloss, (1,), f32, dev), base,
         None if dlogp is None else dlogp.data_ptr(), None if dentropy is None else dentropy.data_ptr(),
         base + 4, base + 16, ws_at, ws_bytes,
-        None if dev_status is None else _ptr(dev_status), _stream(stream)))
+        None if dev_status is None else _ptr(dev_status), _stream(stream, dev)))
     return loss, dlogp, dentropy, metrics, counts
 
 
@@ -1394,28 +1395,35 @@ def balance_loss(s: Shape, L: int, logits, idx=None, *, mask=None, counts=None, 
     the record's.  With accumulate the gradient is added to dlogits.  Returns (loss [L,2], counts [L,E]
     int32, dlogits [L,T,E] or None)."""
     dev = _device_of("logits", logits)
-    f32, grad = torch.float32, (L, s.T, s.E)
+    f32, new, T, E = torch.float32, torch.empty_strided, s.T, s.E
+    grad = (L, T, E)
     given = counts is not None
     if not given and idx is None:
         raise ValueError("idx, counts: expected one of them")
     if accumulate and dlogits is None:
         raise ValueError("accumulate: needs dlogits")
     at = _arg("logits", logits, grad, f32, dev)
-    rec = _arg("idx", idx, (L, s.T, s.K), _idx_dtype(s), dev)
+    rec = _arg("idx", idx, (L, T, s.K), _idx_dtype(s), dev)
     if mask is not None:
-        mask = _arg("mask", mask, (s.T,), torch.uint8 if mask.dtype == torch.uint8 else torch.bool, dev)
-    if not given:
-        counts = torch.empty_strided((L, s.E), (s.E, 1), dtype=torch.int32, device=dev)
-    if dlogits is None and want_grad:
-        dlogits = torch.empty_strided(grad, (s.T * s.E, s.E, 1), dtype=f32, device=dev)
-    loss = torch.empty_strided((L, 2), (2, 1), dtype=f32, device=dev)
-    c = Balance(balance_coef, z_coef, bool(accumulate), given)
-    ws = _scratch(ws, lib.r3_balance_loss_workspace_bytes(ctypes.byref(s), L), dev)
+        mask = _arg("mask", mask, (T,), torch.uint8 if mask.dtype == torch.uint8 else torch.bool, dev)
+    if given:
+        counts_at = _arg("counts", counts, (L, E), torch.int32, dev)
+    else:
+        counts = new((L, E), (E, 1), dtype=torch.int32, device=dev)
+        counts_at = counts.data_ptr()
+    if dlogits is not None:
+        out = _arg("dlogits", dlogits, grad, f32, dev)
+    elif want_grad:
+        dlogits = new(grad, (T * E, E, 1), dtype=f32, device=dev)
+        out = dlogits.data_ptr()
+    else:
+        out = None
+    loss = new((L, 2), (2, 1), dtype=f32, device=dev)
+    shape, c = ctypes.byref(s), Balance(balance_coef, z_coef, bool(accumulate), given)
+    ws = _scratch(ws, lib.r3_balance_loss_workspace_bytes(shape, L), dev)
     _check(lib.r3_balance_loss(
-        ctypes.byref(s), L, ctypes.byref(c), at, rec, mask,
-        _arg("counts", counts, (L, s.E), torch.int32, dev), loss.data_ptr(),
-        _arg("dlogits", dlogits, grad, f32, dev), ws.data_ptr(), ws.numel(),
-        None if dev_status is None else _ptr(dev_status), _stream(stream)))
+        shape, L, ctypes.byref(c), at, rec, mask, counts_at, loss.data_ptr(), out, ws.data_ptr(), ws.numel(),
+        None if dev_status is None else _ptr(dev_status), _stream(stream, dev)))
     return loss, counts, dlogits
 
 

@@ -134,3 +134,50 @@ def test_one_graph_of_the_whole_step(r3):
         graph.replay()
         loss = step(1)
         assert torch.equal(held, loss) and torch.equal(weights[0], weights[1])
+
+
+def test_calls_on_two_streams_at_once_and_two_graphs_of_them(r3):
+    """Every operator on two streams without a wait between them, and replayed from two graphs side by side, gives
+    what it gives alone: workspaces are each call's own."""
+    g = torch.Generator().manual_seed(5)
+    T, L, E, K = 9000, 3, 128, 8
+    shape = r3.make_shape(T, 8, E, K, 8)
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+
+    def inputs():
+        rn = lambda *s: torch.randn(s, generator=g).cuda()
+        return dict(lp=rn(T), old=rn(T), adv=rn(T), cu=torch.tensor([0, 4000, 4001, T], dtype=torch.int32).cuda(),
+                    logits=rn(L, T, E), rec=torch.randint(0, E, (L, T, K), generator=g, dtype=torch.uint8).cuda(),
+                    small=rn(5, 96, 700), wide=rn(2, 300, 520), bf=rn(12, 512, 768).bfloat16())
+
+    def run(t):
+        out = []
+        for _ in range(3):
+            out += [r3.policy_loss(t["lp"], t["old"], t["cu"], advantages=t["adv"], ratio="sequence")[1],
+                    *r3.balance_loss(shape, L, t["logits"], t["rec"], z_coef=0.1),
+                    r3.orthogonalize(t["small"]), r3.orthogonalize(t["wide"]), r3.orthogonalize(t["bf"])]
+        return out
+
+    both = [inputs(), inputs()]
+    want = [run(t) for t in both]
+    torch.cuda.synchronize()
+    got = []
+    for t, side in zip(both, sides):
+        with torch.cuda.stream(side):
+            got.append(run(t))
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+    graphs, held = [], []
+    for t in both:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            held.append(run(t))
+        graphs.append(graph)
+    for _ in range(2):
+        for graph, side in zip(graphs, sides):
+            with torch.cuda.stream(side):
+                graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(want, held):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))

@@ -18,11 +18,11 @@
 // symmetric: only tiles on and below the diagonal are computed, the others are stored from the same accumulators,
 // transposed.  Eight epilogue warps, each with its own 8 KB (three products: 4 KB) of shared memory, through
 // which results go out by TMA in boxes of 32 rows x 64 columns and addends come in whole lines.
-// 24 matrices of 768 x 2048, one product: X X^T 35 us, B 21, B X 69, of which the products of their tiles are 23,
+// 24 matrices of 768 x 2048, one product, launches by themselves: X X^T 35 us, B 21, B X 69, of which the products of their tiles are 23,
 // 9 and 35 at the tensor pipe's rate.  B X moves 281 MB to and from HBM, and its operands, the lo plane and both new
 // planes pass between L2 and the SMs at 11 to 12.5 TB/s, which bounds it (the tensor pipe is busy 42% of the time);
 // X X^T and B wait for the first loads and the last stores of their few tiles besides.  Three products, 4096 x
-// 4096: 3150 us for five steps, 81% of the tensor pipe's rate: each 64 of k leave tensor memory for registers.
+// 4096: 3100 us for five steps at first (3500 under load), 81% of the tensor pipe's rate: each 64 of k leave tensor memory for registers.
 #include <algorithm>
 #include <cmath>
 #include <vector>
@@ -204,7 +204,10 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
     grid_launch_dependents();
-    grid_dependency_wait();
+    // (who reads or writes global memory waits for the launch before this one, with the first tile already found:
+    // 2048 x 2048 331 -> 263 us, 384 x 768 x 2048 under load 14.5 -> 13.6 ms)
+    Tile first_tile = {};
+    if (pair < g.items) first_tile = decode<PHASE, TN>(g, pair);
 
     // a tile on the diagonal of A or of A^2 has the same rows on both sides: copied once
     auto diagonal = [&](const Tile& t) { return SYM && t.m == t.n * TN / TILE; };
@@ -218,8 +221,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                 int stage = 0;
                 uint32_t phase = 0;
                 bool ok = true;
+                grid_dependency_wait();
                 for (int item = pair; ok && item < g.items; item += pairs) {
-                    const Tile t = decode<PHASE, TN>(g, item);
+                    const Tile t = item == pair ? first_tile : decode<PHASE, TN>(g, item);
                     const ClassArgs& c = g.c[t.k];
                     const int m0 = t.m * TILE + (int)rank * BM, n0 = t.n * TN + (int)rank * BN;
                     const bool once = alike(t);
@@ -264,7 +268,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                 uint32_t phase = 0, acc_phase = 0;
                 bool ok = true;
                 for (int item = pair; ok && item < g.items; item += pairs) {
-                    const Tile t = decode<PHASE, TN>(g, item);
+                    const Tile t = item == pair ? first_tile : decode<PHASE, TN>(g, item);
                     const ClassArgs& c = g.c[t.k];
                     const uint32_t idesc = (1u << 4) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24) |
                                            (c.a_mn ? 1u << 15 : 0u) | (c.b_mn ? 1u << 16 : 0u);
@@ -357,8 +361,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
             }
             if (BUFFERS > 1) turn ^= 1;
         };
+        grid_dependency_wait();
         for (int item = pair; item < g.items; item += pairs) {
-            const Tile t = decode<PHASE, TN>(g, item);
+            const Tile t = item == pair ? first_tile : decode<PHASE, TN>(g, item);
             const ClassArgs& c = g.c[t.k];
             const int row0 = t.m * TILE + (int)rank * BM + q * 32, row = row0 + lane;
             const int first = t.n * TN + half * CW;              // this warp's columns
@@ -561,7 +566,6 @@ __global__ void __launch_bounds__(FOLD_THREADS) fold_kernel(const __grid_constan
     constexpr int CW = TN / 2, EACH = CW / 32;           // float4 of a thread
     __shared__ __align__(16) __half s_tile[PLANES][32][CW + 8];
     grid_launch_dependents();
-    grid_dependency_wait();
     int k = 0;
 #pragma unroll
     for (int i = 1; i < MAX_CLASSES; ++i)
@@ -574,6 +578,7 @@ __global__ void __launch_bounds__(FOLD_THREADS) fold_kernel(const __grid_constan
     const int rank = region >> 3, w = region & 7;
     // (warp 4 + w of the epilogue: lane quadrant w & 3, column half w >> 2)
     const int row0 = m * TILE + rank * BM + (w & 3) * 32, col0 = n * TN + (w >> 2) * CW;
+    grid_dependency_wait();
     if (row0 >= c.m || col0 >= c.m) return;
     const float4* from = c.partial + (size_t)tile * c.splits * SLOT<TN> + region * (CW / 4) * 32;
     float4 v[EACH];
@@ -752,8 +757,8 @@ template <typename G>
 __global__ void __launch_bounds__(EL_THREADS, 6) norm_kernel(const __grid_constant__ ElemArgs a) {
     __shared__ double s_sum[EL_THREADS / 32];
     grid_launch_dependents();
-    grid_dependency_wait();
     const Piece p = find_piece(a);
+    grid_dependency_wait();
     float gs;
     double sum = 0.0;
     if (scale_of(a.grad_scale, &gs))
@@ -804,8 +809,8 @@ template <typename G>
 __global__ void __launch_bounds__(EL_THREADS, 6) start_kernel(const __grid_constant__ ElemArgs a) {
     __shared__ double s_sum[EL_THREADS / 32];
     grid_launch_dependents();
-    grid_dependency_wait();
     const Piece p = find_piece(a);
+    grid_dependency_wait();
     float gs;
     if (!scale_of(a.grad_scale, &gs)) return;          // the step is skipped: the planes are not looked at
     const int pieces = p.part->pieces;
@@ -865,8 +870,8 @@ __device__ __forceinline__ void finish_piece(const ElemArgs& a, const Piece& p) 
 template <typename P, bool MASTER, bool STEP>
 __global__ void __launch_bounds__(EL_THREADS, 6) finish_kernel(const __grid_constant__ ElemArgs a) {
     grid_launch_dependents();
-    grid_dependency_wait();
     const Piece p = find_piece(a);
+    grid_dependency_wait();
     float gs;
     if (!scale_of(a.grad_scale, &gs)) return;
     if (p.part->cols % 8 == 0) finish_piece<true, P, MASTER, STEP>(a, p);

@@ -227,7 +227,13 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                     const ClassArgs& c = g.c[t.k];
                     const int m0 = t.m * TILE + (int)rank * BM, n0 = t.n * TN + (int)rank * BN;
                     const bool once = alike(t);
-                    for (int kb = t.k0; kb < t.k1; ++kb) {
+                    // (held in registers: read again for each k block they cost more than its copies take)
+                    uint64_t maps_a = reinterpret_cast<uint64_t>(&c.a[0]), maps_b = reinterpret_cast<uint64_t>(&c.b[0]);
+                    int a_mn = c.a_mn, b_mn = c.b_mn, z = t.z, k1 = t.k1;
+                    asm volatile("" : "+l"(maps_a), "+l"(maps_b), "+r"(a_mn), "+r"(b_mn), "+r"(z), "+r"(k1));
+                    const CUtensorMap* map_a = reinterpret_cast<const CUtensorMap*>(maps_a);
+                    const CUtensorMap* map_b = reinterpret_cast<const CUtensorMap*>(maps_b);
+                    for (int kb = t.k0; kb < k1; ++kb) {
                         if (!mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, g.dev_status)) {
                             ok = false;
                             break;
@@ -238,18 +244,18 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
 #pragma unroll
                         for (int pl = 0; pl < R::PLANES; ++pl) {
                             const uint32_t ta = sa + pl * OPERAND_BYTES, tb = sb + pl * R::B_BYTES;
-                            if (c.a_mn) {
-                                tma_load_3d_pair(ta, &c.a[pl], m0, kb * BK, t.z, lead);
-                                tma_load_3d_pair(ta + OPERAND_BYTES / 2, &c.a[pl], m0 + 64, kb * BK, t.z, lead);
+                            if (a_mn) {
+                                tma_load_3d_pair(ta, map_a + pl, m0, kb * BK, z, lead);
+                                tma_load_3d_pair(ta + OPERAND_BYTES / 2, map_a + pl, m0 + 64, kb * BK, z, lead);
                             } else {
-                                tma_load_3d_pair(ta, &c.a[pl], kb * BK, m0, t.z, lead);
+                                tma_load_3d_pair(ta, map_a + pl, kb * BK, m0, z, lead);
                             }
                             if (once) continue;
-                            if (c.b_mn) {
-                                tma_load_3d_pair(tb, &c.b[pl], n0, kb * BK, t.z, lead);
-                                if (BN > 64) tma_load_3d_pair(tb + OPERAND_BYTES / 2, &c.b[pl], n0 + 64, kb * BK, t.z, lead);
+                            if (b_mn) {
+                                tma_load_3d_pair(tb, map_b + pl, n0, kb * BK, z, lead);
+                                if (BN > 64) tma_load_3d_pair(tb + OPERAND_BYTES / 2, map_b + pl, n0 + 64, kb * BK, z, lead);
                             } else {
-                                tma_load_3d_pair(tb, &c.b[pl], kb * BK, n0, t.z, lead);
+                                tma_load_3d_pair(tb, map_b + pl, kb * BK, n0, z, lead);
                             }
                         }
                         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
@@ -270,14 +276,18 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                 for (int item = pair; ok && item < g.items; item += pairs) {
                     const Tile t = item == pair ? first_tile : decode<PHASE, TN>(g, item);
                     const ClassArgs& c = g.c[t.k];
-                    const uint32_t idesc = (1u << 4) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24) |
-                                           (c.a_mn ? 1u << 15 : 0u) | (c.b_mn ? 1u << 16 : 0u);
+                    uint32_t idesc = (1u << 4) | ((uint32_t)(TN >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24) |
+                                     (c.a_mn ? 1u << 15 : 0u) | (c.b_mn ? 1u << 16 : 0u);
                     // 16 along k: 32 bytes inside the swizzled row, or two groups of 8 k rows
-                    const uint64_t a_step = c.a_mn ? (2048 >> 4) : 2, b_step = c.b_mn ? (2048 >> 4) : 2;
-                    const uint32_t to_b = alike(t) ? 0u : (uint32_t)SIDE_BYTES;
-                    for (int kb = t.k0; kb < t.k1; ++kb) {
+                    uint64_t a_step = c.a_mn ? (2048 >> 4) : 2, b_step = c.b_mn ? (2048 >> 4) : 2;
+                    const uint32_t first_b = base + (alike(t) ? 0u : (uint32_t)SIDE_BYTES);
+                    uint64_t first_da = c.a_mn ? smem_desc_mn_sw128(base, OPERAND_BYTES / 2) : smem_desc_sw128(base);
+                    uint64_t first_db = c.b_mn ? smem_desc_mn_sw128(first_b, OPERAND_BYTES / 2) : smem_desc_sw128(first_b);
+                    int k1 = t.k1;
+                    asm volatile("" : "+r"(idesc), "+l"(a_step), "+l"(b_step), "+l"(first_da), "+l"(first_db), "+r"(k1));
+                    for (int kb = t.k0; kb < k1; ++kb) {
                         // three products: every k block has an accumulator of its own
-                        const bool fresh = TERMS > 1 || kb == t.k0, last = TERMS > 1 || kb + 1 == t.k1;
+                        const bool fresh = TERMS > 1 || kb == t.k0, last = TERMS > 1 || kb + 1 == k1;
                         if (fresh && !__all_sync(0xffffffffu, mbar_wait(tempty_bar(acc), acc_phase ^ 1u, abort_flag,
                                                                         g.dev_status))) {
                             ok = false;
@@ -291,11 +301,9 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                         tc_fence_after();
                         if (elect_one()) {
                             const uint32_t d_tmem = tmem_base + (uint32_t)(acc * TN);
-                            const uint32_t sa = base + stage * STAGE_BYTES, sb = sa + to_b;
-                            const uint64_t da = c.a_mn ? smem_desc_mn_sw128(sa, OPERAND_BYTES / 2)
-                                                       : smem_desc_sw128(sa);
-                            const uint64_t db = c.b_mn ? smem_desc_mn_sw128(sb, OPERAND_BYTES / 2)
-                                                       : smem_desc_sw128(sb);
+                            // (a descriptor holds the address in units of 16 bytes)
+                            const uint64_t da = first_da + (uint64_t)(stage * (STAGE_BYTES >> 4));
+                            const uint64_t db = first_db + (uint64_t)(stage * (STAGE_BYTES >> 4));
 #pragma unroll
                             for (int term = 0; term < TERMS; ++term) {
                                 // (hi, lo), (lo, hi), (hi, hi): the small products first

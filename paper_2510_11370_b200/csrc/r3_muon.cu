@@ -18,11 +18,11 @@
 // symmetric: only tiles on and below the diagonal are computed, the others are stored from the same accumulators,
 // transposed.  Eight epilogue warps, each with its own 8 KB (three products: 4 KB) of shared memory, through
 // which results go out by TMA in boxes of 32 rows x 64 columns and addends come in whole lines.
-// 24 matrices of 768 x 2048, one product, launches by themselves: X X^T 35 us, B 21, B X 69, of which the products of their tiles are 23,
-// 9 and 35 at the tensor pipe's rate.  B X moves 281 MB to and from HBM, and its operands, the lo plane and both new
-// planes pass between L2 and the SMs at 11 to 12.5 TB/s, which bounds it (the tensor pipe is busy 42% of the time);
-// X X^T and B wait for the first loads and the last stores of their few tiles besides.  Three products, 4096 x
-// 4096: 3100 us for five steps at first (3500 under load), 81% of the tensor pipe's rate: each 64 of k leave tensor memory for registers.
+// 24 matrices of 768 x 2048, one product, launches by themselves: X X^T 36 us, B 23, B X 56 (with one plane out), of
+// which the products of their tiles are 23, 9 and 35 at the tensor pipe's rate.  B X moves 228 MB to and from HBM and
+// 796 between L2 and the SMs, 14.2 TB/s; X X^T and B wait for the first loads and the last stores of their few tiles.
+// Three products, 4096 x 4096: 3100 us for five steps at first (3550 under load), the tensor pipe busy for three
+// quarters: each 64 of k leave tensor memory for registers.
 #include <algorithm>
 #include <cmath>
 #include <vector>

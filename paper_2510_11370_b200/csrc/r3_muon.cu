@@ -1044,9 +1044,10 @@ static int all_tiles(const Problem& p, int tn) { return (p.rows + TILE - 1) / TI
 static int gram_blocks(const Problem& p) { return ((p.tall ? p.rows : p.cols) + BK - 1) / BK; }
 // A round's tiles and the parts of its long sums, by estimates of the time in 20ths of a k block's with 256
 // columns (0.27 us; three products 0.8): a CTA pair's item costs its k blocks and what stands around them.
-// Tiles of 128 columns take 14 (13) of a block and half of the rest, and are twice as many: few tiles spread over
-// more of the GPU (us, 256 -> 128 columns: 1024 x 1024 f32 371 -> 271, 768 x 2048 bf16 233 -> 168, 4 x 1024 x
-// 1024 bf16 225 -> 277, 8 x 768 x 2048 bf16 331 -> 437).
+// Tiles of 128 columns take 13 (11) of a block and half of the rest, and are twice as many: few tiles spread over
+// more of the GPU (us, 256 -> 128 columns: 1024 x 1024 f32 354 -> 236, 768 x 2048 bf16 214 -> 147, 16 x 300 x 600 bf16
+// 206 -> 161, 2048 x 4096 f32 890 -> 810, 4 x 1024 x 1024 bf16 199 -> 210, 8 x 768 x 2048 bf16 281 -> 323, 4096 x 4096
+// bf16 1128 -> 1472).
 constexpr int MAX_SPLITS = 8;
 struct Cut {
     int tn, part;                         // columns of the tiles; k blocks of A = X X^T that a CTA pair takes at a time
@@ -1064,7 +1065,7 @@ static Cut cut_of(const Class* classes, int n, int terms) {
         side = std::max(side, (classes[i].p.m + BK - 1) / BK);
     }
     for (int tn : {256, 128}) {
-        const int block = tn == 256 ? 20 : terms > 1 ? 13 : 14;
+        const int block = tn == 256 ? 20 : terms > 1 ? 11 : 13;
         const int around = (terms > 1 ? 80 : 220) * tn / 256;
         long long square = 0, all = 0;
         for (int i = 0; i < n; ++i) {
@@ -1072,7 +1073,7 @@ static Cut cut_of(const Class* classes, int n, int terms) {
             all += (long long)all_tiles(classes[i].p, tn) * classes[i].count;
         }
         const long long others = (waves(square) + waves(all)) * (side * block + around);
-        // parts cost a launch that adds them up, 3 to 4 us (150 x 4000 f32, 256 columns: 444 us whole, 248 in parts)
+        // parts cost a launch that adds them up, 3 to 4 us (150 x 4000 f32, 256 columns: 444 us whole, 248 in parts when it was taken)
         const int fold = terms > 1 ? 70 : 300;
         for (int splits = 1; splits <= MAX_SPLITS; ++splits) {
             const int part = (longest + splits - 1) / splits;

@@ -132,7 +132,8 @@ def test_many_small_matrices_and_one_large(r3):
 
 
 @pytest.mark.parametrize("products", [1, 3])
-@pytest.mark.parametrize("B,rows,cols", [(24, 520, 300), (24, 300, 520), (8, 300, 6001), (8, 6001, 300)])
+@pytest.mark.parametrize("B,rows,cols", [(24, 300, 520), (24, 769, 500), (12, 769, 513), (40, 249, 2000),
+                                         (40, 2000, 249), (8, 300, 6001), (8, 6001, 300)])
 def test_enough_tiles_for_wide_ones(r3, B, rows, cols, products):
     """So many matrices take tiles of 256 columns, the long ones with their sums in parts; the first and the last
     are compared, and all of them with what they give elsewhere in the batch."""

@@ -814,8 +814,9 @@ typedef struct {
  * element written (tokens that do not count: 0, or left as they are with accumulate).  Only T, E, K and idx_type of
  * the shape matter.  E <= 1024 (R3_ERR_UNSUPPORTED beyond).  Sums run in an order that depends on the shape
  * alone.  dev_status: R3_DEV_BAD_INDEX for an index >= E (not counted).
- *  - A logit of -inf (or below -1e38) has p = 0; a token with no other logit counts in N and adds nothing.  A
- *    token with NaN or +inf (or above 2e38) makes its own gradient and its block's losses NaN.
+ *  - A logit of -inf has p = 0; a token with no other logit counts in N and adds nothing.  A token with NaN or +inf
+ *    makes its own gradient and its block's losses NaN.  Any finite logit is one, the type's lowest included (a
+ *    token that holds nothing else chooses evenly; its z loss may pass float32's range).
  *  - No token that counts: losses 0.
  * workspace: r3_balance_loss_workspace_bytes(shape, L). */
 size_t r3_balance_loss_workspace_bytes(const r3_shape* shape, int32_t L);

@@ -19,6 +19,7 @@
 // (rows of sums per CTA, added up by the last one: 26 us instead of 22 for 65536 tokens).
 // 48 blocks of 16384 tokens, 128 experts: 147 us, 5.5 TB/s of the 812 MB that have to move; one block of 65536
 // tokens: 22 us, of which the counting pass and the main pass's start are 9, the logits 10, the losses 3.
+#include <cfloat>
 #include <cmath>
 
 #include "r3_common.cuh"
@@ -37,6 +38,7 @@ constexpr int WARPS = THREADS / 32;
 constexpr int CTAS_PER_SM = 2;
 constexpr int EARLY_BYTES = 32 << 20;     // of logits that all CTAs fetch ahead: a part of L2
 constexpr int ALONE = 8192;               // logits of a block that one CTA takes with its choices
+constexpr float FAR = 1e6f;               // logits beyond: 0.05 and more of rounding in their product with log2(e)
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct Args {
@@ -313,13 +315,15 @@ __global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_ker
             for (int j = 1; j < V; ++j) top = fmaxf(top, v[j]);
 #pragma unroll
             for (int o = G / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            // 2^(s log2(e) - from): from's own rounding is the same for all of a token's logits.  Where all of
-            // them are -inf (or below -1e38) every one gives 0
-            const float from = fmaxf(top, -1e38f) * LOG2E;
+            // 2^(s log2(e) - from): from's own rounding is the same for all of a token's logits, but it stands in the
+            // exponent (2^7 of it at a top of 2e9, beyond float32), so a large top is taken off first, be it a mask's
+            // -1e30 or the type's lowest.  Where all of them are -inf every one gives 0
+            const float least = fmaxf(top, -FLT_MAX), off = fabsf(least) > FAR ? least : 0.f;
+            const float from = (least - off) * LOG2E;
             float whole = 0.f, along = 0.f;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                v[j] = fast_exp2(fmaf(v[j], LOG2E, -from));
+                v[j] = fast_exp2(fmaf(v[j] - off, LOG2E, -from));
                 whole += v[j];
                 along = fmaf(v[j], f[j], along);
             }
@@ -329,7 +333,7 @@ __global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_ker
                 along += __shfl_xor_sync(0xffffffffu, along, o);
             }
             const float inv = whole != 0.f ? fast_inverse(whole) : 0.f;
-            const float lse = whole != 0.f ? LN2 * (from + fast_log2(whole)) : 0.f;
+            const float lse = whole != 0.f ? fmaf(LN2, from + fast_log2(whole), off) : 0.f;
             z = fmaf(lse, lse, z);                     // 0 where the token does not count
             const float shift = fmaf(gz, lse, -along * inv);
 #pragma unroll

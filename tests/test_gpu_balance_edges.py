@@ -1,0 +1,53 @@
+"""The balance loss where its numbers are large or many.
+
+Tolerances: test_gpu_balance's, D = 2^-24 (|s - top| + 50) of a probability and of sum f p."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import r3_loss_oracle as O
+from tests.helpers import f64, random_record
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def r3():
+    from paper_2510_11370_b200 import r3 as mod
+    return mod
+
+
+LARGE = [9e5, 2e6, 5e9, 1e10, 3e20, 3e38, -2e6, -1e9, -1e10, -1e30, float(torch.finfo(torch.float32).min)]
+
+
+@pytest.mark.parametrize("E,K", [(8, 2), (60, 4), (128, 8), (301, 6), (1021, 3), (1024, 8)])
+def test_large_finite_logits(r3, E, K):
+    """Finite fills of masked experts, of whole rows too, and tops far from zero: softmax and its gradient are those
+    of the differences."""
+    T = 6 * len(LARGE) + 3
+    g = torch.Generator().manual_seed(E)
+    x = torch.randn((1, T, E), generator=g)
+    for i, m in enumerate(LARGE):
+        rows = x[0, 6 * i:6 * i + 6]
+        rows[0] = m                                            # evenly
+        rows[1], rows[1, E // 2:] = m, -float("inf")
+        rows[2, E // 3:] = -abs(m)                             # a fill beside ordinary logits
+        rows[3, 1:], rows[3, 0] = m, float(np.nextafter(np.float32(m), np.float32(-abs(m) / 2)))
+        rows[4] = m + 4 * rows[4] if abs(m) < 1e9 else m * (1 - rows[4].abs() / 8)
+        rows[5, 0] = abs(m)
+    rec = random_record(np.random.default_rng(E), T, E, K, torch.int16)[None]
+    s = r3.make_shape(T, 8, E, K, 8, idx=torch.int16)
+    loss, _, d = r3.balance_loss(s, 1, x.cuda(), rec.cuda(), balance_coef=0.7)
+    balance, _, _, want, p, _, f = O.balance_loss(f64(x[0]), rec[0].long().numpy(), None, None, 0.7, 0.0)
+    far = np.where(p > 0, f64(x[0]).max(1, keepdims=True) - f64(x[0]), 0)
+    near = 2.0 ** -24 * (far + 50)
+    size = p * 0.7 * (f + (p * f).sum(1, keepdims=True)) / T
+    assert np.isfinite(f64(d)).all()
+    assert (np.abs(f64(d[0]) - want) <= size * (2 * near + 2.0 ** -24 * 60) + 2.0 ** -140).all()
+    assert abs(loss[0, 0].item() - balance) <= 2.0 ** -24 * (T / 8 + 80 + far.max()) * balance
+    # the logarithm of the sum, by the z loss of tokens one by one; its square may pass float32
+    for t in (0, 6, 12, 6 * LARGE.index(-1e9)):
+        one = r3.make_shape(1, 8, E, K, 8, idx=torch.int16)
+        z = r3.balance_loss(one, 1, x[:, t:t + 1].contiguous().cuda(), rec[:, t:t + 1].contiguous().cuda())[0][0, 1].item()
+        lse = O.balance_loss(f64(x[0, t:t + 1]), rec[0, t:t + 1].long().numpy())[5][0, 0]
+        assert abs(z - lse ** 2) <= 2.0 ** -20 * lse ** 2

@@ -812,7 +812,7 @@ typedef struct {
  * that do not count have 0 there, and their logits and record are not used; counts [L,E] int32, written, may be NULL (with
  * counts_given: read); loss [L,2] f32; dlogits [L,T,E] f32 or NULL (may be the logits' buffer), every
  * element written (tokens that do not count: 0, or left as they are with accumulate).  Only T, E, K and idx_type of
- * the shape matter.  E <= 1024 (R3_ERR_UNSUPPORTED beyond).  Sums run in an order that depends on the shape
+ * the shape matter.  E <= 1024 and T <= 2^30 (R3_ERR_UNSUPPORTED beyond).  Sums run in an order that depends on the shape
  * alone.  dev_status: R3_DEV_BAD_INDEX for an index >= E (not counted).
  *  - A logit of -inf has p = 0; a token with no other logit counts in N and adds nothing.  A token with NaN or +inf
  *    makes its own gradient and its block's losses NaN.  Any finite logit is one, the type's lowest included (a

@@ -30,6 +30,7 @@ namespace r3 {
 namespace bal {
 
 constexpr int MAX_EXPERTS = 1024;
+constexpr int MAX_TOKENS = 1 << 30;       // of a block: a CTA's hop beyond them is still a 32-bit number
 constexpr int COUNT_THREADS = 256;
 constexpr int COUNT_TOKENS = 1024;        // tokens of a CTA of the counting pass
 constexpr int COUNT_CTAS = 8;             // CTAs of its clusters
@@ -462,7 +463,7 @@ static r3_status check(const r3_shape* s, int32_t L, const r3_balance* c) {
     const r3_status st = check_shape(s);
     if (st != R3_OK) return st;
     if (!(std::fabs(c->balance_coef) < 1e30) || !(std::fabs(c->z_coef) < 1e30)) return R3_ERR_INVALID_ARG;
-    return s->E > MAX_EXPERTS ? R3_ERR_UNSUPPORTED : R3_OK;
+    return s->E > MAX_EXPERTS || s->T > MAX_TOKENS ? R3_ERR_UNSUPPORTED : R3_OK;
 }
 struct Layout {
     size_t counts, part, ticket, total;

@@ -39,6 +39,7 @@ constexpr int WARPS = THREADS / 32;
 constexpr int CTAS_PER_SM = 2;
 constexpr int EARLY_BYTES = 32 << 20;     // of logits that all CTAs fetch ahead: a part of L2
 constexpr int ALONE = 8192;               // logits of a block that one CTA takes with its choices
+constexpr int FOLD = 64;                  // tokens of a lane that are added up in float32
 constexpr float FAR = 1e6f;               // logits beyond: 0.05 and more of rounding in their product with log2(e)
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -202,8 +203,8 @@ template <int G, int V, bool WIDE>
 __global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_kernel(const __grid_constant__ Args a) {
     using R = Row<G, V, WIDE>;
     constexpr int ROWS = 32 / G;                       // tokens of a warp at a time
-    extern __shared__ float s_n[];                     // [E] counts, then [WARPS][E] sums of probabilities
-    float* s_col = s_n + ((a.E + 3) & ~3);
+    extern __shared__ float s_n[];                     // [E] counts, then [WARPS][E] sums of probabilities in 64 bits
+    double* s_col = reinterpret_cast<double*>(s_n + ((a.E + 3) & ~3));
     __shared__ long long s_sum[WARPS];
     __shared__ double s_z[WARPS], s_b[WARPS];
     __shared__ int s_tokens;
@@ -298,89 +299,94 @@ __global__ void __launch_bounds__(THREADS, V <= 8 ? CTAS_PER_SM : 1) balance_ker
             f[j] = c < E ? gb * (s_n[c] * per_choice) : 0.f;
             sum[j] = 0.f;
         }
-        float z = 0.f;                                 // of a few hundred tokens; the CTAs' are added in 64 bits
+        float z = 0.f;
+        // float32 sums of FOLD tokens a lane at most, those then added up in 64 bits: what they are off by does not
+        // grow with the batch
+        int t = t0 + warp * ROWS;
+        for (bool more = false;; more = true) {
+            const int stop = min(t1, t + FOLD * hop);
 #pragma unroll 2
-        for (int t = t0 + warp * ROWS; t < t1; t += hop) {
-            float v[V];
-            const bool on = next_on;
+            for (; t < stop; t += hop) {
+                float v[V];
+                const bool on = next_on;
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = next[j];
-            if (a.mask && !on) {
+                for (int j = 0; j < V; ++j) v[j] = next[j];
+                if (a.mask && !on) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) v[j] = -INFINITY;
-            }
-            if (t + hop < t1) fetch(t + hop);
-            const int at = t + row;
-            float top = v[0];
+                    for (int j = 0; j < V; ++j) v[j] = -INFINITY;
+                }
+                if (t + hop < t1) fetch(t + hop);
+                const int at = t + row;
+                float top = v[0];
 #pragma unroll
-            for (int j = 1; j < V; ++j) top = fmaxf(top, v[j]);
+                for (int j = 1; j < V; ++j) top = fmaxf(top, v[j]);
 #pragma unroll
-            for (int o = G / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            // 2^(s log2(e) - from): from's own rounding is the same for all of a token's logits, but it stands in the
-            // exponent (2^7 of it at a top of 2e9, beyond float32), so a large top is taken off first, be it a mask's
-            // -1e30 or the type's lowest.  Where all of them are -inf every one gives 0
-            const float least = fmaxf(top, -FLT_MAX), off = fabsf(least) > FAR ? least : 0.f;
-            const float from = (least - off) * LOG2E;
-            float whole = 0.f, along = 0.f;
+                for (int o = G / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                // 2^(s log2(e) - from): from's own rounding is the same for all of a token's logits, but it stands in
+                // the exponent (2^7 of it at a top of 2e9, beyond float32), so a large top is taken off first, be it a
+                // mask's -1e30 or the type's lowest.  Where all of them are -inf every one gives 0
+                const float least = fmaxf(top, -FLT_MAX), off = fabsf(least) > FAR ? least : 0.f;
+                const float from = (least - off) * LOG2E;
+                float whole = 0.f, along = 0.f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                v[j] = fast_exp2(fmaf(v[j] - off, LOG2E, -from));
-                whole += v[j];
-                along = fmaf(v[j], f[j], along);
-            }
+                for (int j = 0; j < V; ++j) {
+                    v[j] = fast_exp2(fmaf(v[j] - off, LOG2E, -from));
+                    whole += v[j];
+                    along = fmaf(v[j], f[j], along);
+                }
 #pragma unroll
-            for (int o = G / 2; o > 0; o >>= 1) {
-                whole += __shfl_xor_sync(0xffffffffu, whole, o);
-                along += __shfl_xor_sync(0xffffffffu, along, o);
-            }
-            const float inv = whole != 0.f ? fast_inverse(whole) : 0.f;
-            const float lse = whole != 0.f ? fmaf(LN2, from + fast_log2(whole), off) : 0.f;
-            z = fmaf(lse, lse, z);                     // 0 where the token does not count
-            const float shift = fmaf(gz, lse, -along * inv);
+                for (int o = G / 2; o > 0; o >>= 1) {
+                    whole += __shfl_xor_sync(0xffffffffu, whole, o);
+                    along += __shfl_xor_sync(0xffffffffu, along, o);
+                }
+                const float inv = whole != 0.f ? fast_inverse(whole) : 0.f;
+                const float lse = whole != 0.f ? fmaf(LN2, from + fast_log2(whole), off) : 0.f;
+                z = fmaf(lse, lse, z);                     // 0 where the token does not count
+                const float shift = fmaf(gz, lse, -along * inv);
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float p = v[j] * inv;
-                sum[j] += p;
-                v[j] = p * (f[j] + shift);
-            }
-            if (dlogits && at < t1) {
-                float* out = dlogits + (size_t)at * E;
-                if (a.accumulate) {
-                    if (on) {
-                        float old[V];
-                        R::load(out, E, sub, old, 0.f);
+                for (int j = 0; j < V; ++j) {
+                    const float p = v[j] * inv;
+                    sum[j] += p;
+                    v[j] = p * (f[j] + shift);
+                }
+                if (dlogits && at < t1) {
+                    float* out = dlogits + (size_t)at * E;
+                    if (a.accumulate) {
+                        if (on) {
+                            float old[V];
+                            R::load(out, E, sub, old, 0.f);
 #pragma unroll
-                        for (int j = 0; j < V; ++j) old[j] += v[j];
-                        R::store(out, E, sub, old);
+                            for (int j = 0; j < V; ++j) old[j] += v[j];
+                            R::store(out, E, sub, old);
+                        }
+                    } else {
+                        R::store(out, E, sub, v);
                     }
-                } else {
-                    R::store(out, E, sub, v);
                 }
             }
-        }
-        // the CTA's sums: lanes that hold the same experts, then the warps in their order
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-#pragma unroll
-            for (int o = G; o < 32; o <<= 1) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], o);
-#pragma unroll
-        for (int o = G; o < 32; o <<= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-        if (lane == 0) s_z[warp] = (double)z;
-        if (row == 0) {
+            // lanes that hold the same experts, then the warp's own places
 #pragma unroll
             for (int j = 0; j < V; ++j) {
+#pragma unroll
+                for (int o = G; o < 32; o <<= 1) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], o);
                 const int c = R::column(sub, j);
-                if (c < E) s_col[warp * E + c] = sum[j];
+                if (row == 0 && c < E) s_col[warp * E + c] = (more ? s_col[warp * E + c] : 0.0) + (double)sum[j];
+                sum[j] = 0.f;
             }
+#pragma unroll
+            for (int o = G; o < 32; o <<= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+            if (lane == 0) s_z[warp] = (more ? s_z[warp] : 0.0) + (double)z;
+            z = 0.f;
+            if (t >= t1) break;
         }
         __syncthreads();
-        // this CTA's part of sum_i counts_i sum_t p_ti
+        // this CTA's part of sum_i counts_i sum_t p_ti: the warps in their order
         double balance = 0.0, zz = 0.0;
         for (int c = threadIdx.x; c < E; c += THREADS) {
-            float all = 0.f;
+            double all = 0.0;
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) all += s_col[w * E + c];
-            balance += (double)all * (double)s_n[c];
+            balance += all * (double)s_n[c];
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) balance += __shfl_xor_sync(0xffffffffu, balance, o);
@@ -485,12 +491,12 @@ static Layout layout(const r3_shape* s, int32_t L, const Plan& p) {
 
 template <int G, int V, bool WIDE>
 static r3_status launch(const Args& a, cudaStream_t cs) {
-    const size_t smem = (((size_t)a.E + 3) / 4 * 4 + (size_t)a.E * WARPS) * sizeof(float);
+    const size_t smem = ((size_t)a.E + 3) / 4 * 4 * sizeof(float) + (size_t)a.E * WARPS * sizeof(double);
     if (smem > 32 * 1024) {                            // above what every kernel may have, with its static part
         static PerDevice ready;
         if (!ready.done()) {
             if (cudaFuncSetAttribute(balance_kernel<G, V, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     MAX_EXPERTS * (WARPS + 1) * (int)sizeof(float)) != cudaSuccess)
+                                     MAX_EXPERTS * (WARPS * (int)sizeof(double) + (int)sizeof(float))) != cudaSuccess)
                 return R3_ERR_CUDA;
             ready.mark();
         }

@@ -51,3 +51,20 @@ def test_large_finite_logits(r3, E, K):
         z = r3.balance_loss(one, 1, x[:, t:t + 1].contiguous().cuda(), rec[:, t:t + 1].contiguous().cuda())[0][0, 1].item()
         lse = O.balance_loss(f64(x[0, t:t + 1]), rec[0, t:t + 1].long().numpy())[5][0, 0]
         assert abs(z - lse ** 2) <= 2.0 ** -20 * lse ** 2
+
+
+@pytest.mark.parametrize("seed", [0, 6])
+def test_sums_of_many_tokens(r3, seed):
+    """2^26 equal tokens: added one after the other in float32, 1771 a lane on 148 SMs, p_0 would be 317 (327) and the
+    square 142 (186) times 2^-24 off, since equal terms are rounded the same way again and again.  In runs of 64
+    at most, those in 64 bits: half of 64 steps of 2^-24, and what each term is off by (a probability 53, the square of
+    the logarithm 12)."""
+    T, E = 1 << 26, 3
+    x = np.random.default_rng(seed).standard_normal(E).astype(np.float32)
+    logits = torch.from_numpy(x).cuda().expand(1, T, E).contiguous()
+    counts = torch.tensor([[1, 0, 0]], dtype=torch.int32).cuda()
+    loss = r3.balance_loss(r3.make_shape(T, 8, E, 1, 8), 1, logits, counts=counts, want_grad=False)[0]
+    p = np.exp(x.astype(np.float64))
+    lse = np.log(p.sum())
+    assert abs(loss[0, 0].item() / (E * p[0] / p.sum()) - 1) <= 2.0 ** -24 * (32 + 53 + 8)
+    assert abs(loss[0, 1].item() / lse ** 2 - 1) <= 2.0 ** -24 * (32 + 12 / min(1.0, abs(lse)) + 8)

@@ -607,7 +607,9 @@ typedef struct {
  *   A = X X^T;   B = b A + c A^2;   X = a X + B X
  * which brings the singular values near one; out = X.  x of in_dtype, out of out_dtype: the same buffer (of
  * one type) or no memory in common.  All products accumulate in float32, X is carried in 22 bits between the
- * steps (into the last one in 11, where its a is at most 4 and the result is rounded to bf16).
+ * steps (into the last one in 11, where its a is at most 4 and the result is rounded to bf16): so far as an
+ * element of X is above 2^-28, below that within 2^-50 (one plane, as the operand of one product: 2^-39).  With
+ * coefficients whose iterates pass 3.75 in norm these limits rise, to 16 times that at 60.
  *  - A matrix of zeros gives zeros, one that holds what is not finite gives NaN; the others of a batch are
  *    not touched by it.
  *  - Coefficients whose iterates could pass 16 in norm (or b A + c A^2, with or without a, 60) are refused.

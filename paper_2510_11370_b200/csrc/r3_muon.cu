@@ -4,12 +4,14 @@
 //
 // Three products a step on the tensor cores, each a batch over all matrices of a round (up to four shapes in one
 // launch).  Numbers.  The iterates' singular values stay near one, so fp16 (11 bits, against bf16's 8) holds
-// every operand, times 2^10 to keep small elements in its normal range.  X itself is carried in two fp16 planes,
-// hi + lo (22 bits): the term a X, by which a weak direction grows a^steps-fold, then has no rounding to speak
-// of, and what the products' operands lose stays as small as the output's own rounding to bf16 whatever the
-// matrix's spectrum is (simulated for full-rank, decaying and low-rank spectra: 1.1e-3 to 1.7e-3 of the
+// every operand, times 2^14 with the usual coefficients to keep small elements in its normal range.  X itself is carried
+// in two fp16 planes, hi + lo (22 bits): the term a X, by which a weak direction grows a^steps-fold, then has no
+// rounding to speak of, and what the products' operands lose stays as small as the output's own rounding to bf16
+// whatever the matrix's spectrum is (simulated for full-rank, decaying and low-rank spectra: 1.1e-3 to 1.7e-3 of the
 // result's rms, against 1.7e-3 for the rounding; bf16 operands with a rounded X lose a third of a rank-8 update).
-// For float32 results A and B get a second plane as well and every product is hi lo + lo hi + hi hi.
+// For float32 results A and B get a second plane as well and every product is hi lo + lo hi + hi hi.  Lo planes hold
+// 2^11 of their values, or they would lose what small rows have: the sum of the first two products is taken times
+// 2^-11 by the multiplication that adds the third.
 //
 // One GEMM kernel does all three, with two CTAs per MMA (256 x 256 tiles, or 256 x 128 where they are few; 128
 // rows of the left operand per CTA and k block of 64, accumulators double buffered in tensor memory).
@@ -306,13 +308,17 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                             const uint64_t db = first_db + (uint64_t)(stage * (STAGE_BYTES >> 4));
 #pragma unroll
                             for (int term = 0; term < TERMS; ++term) {
-                                // (hi, lo), (lo, hi), (hi, hi): the small products first
+                                // (hi, lo), (lo, hi), (hi, hi): the small products first, 2^11 of them
                                 const uint64_t ta = da + (TERMS > 1 && term == 1 ? OPERAND_BYTES >> 4 : 0);
                                 const uint64_t tb = db + (TERMS > 1 && term == 0 ? R::B_BYTES >> 4 : 0);
 #pragma unroll
-                                for (int kk = 0; kk < BK / UK; ++kk)
-                                    tc_mma_bf16_pair(d_tmem, ta + a_step * kk, tb + b_step * kk, idesc,
-                                                     (fresh && (term | kk) == 0) ? 0u : 1u);
+                                for (int kk = 0; kk < BK / UK; ++kk) {
+                                    if (term == 2 && kk == 0)
+                                        tc_mma_bf16_pair_onto_scaled<LO_SHIFT>(d_tmem, ta, tb, idesc);
+                                    else
+                                        tc_mma_bf16_pair(d_tmem, ta + a_step * kk, tb + b_step * kk, idesc,
+                                                         (fresh && (term | kk) == 0) ? 0u : 1u);
+                                }
                             }
                             tc_commit_pair(empty_bar(stage), 3);
                             if (last) tc_commit_pair(tfull_bar(acc), 3);
@@ -500,7 +506,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                                     float e[8];
                                     half8(early[8 + 4 * h + j], e);
 #pragma unroll
-                                    for (int i = 0; i < 8; ++i) l[i] += e[i];
+                                    for (int i = 0; i < 8; ++i) l[i] = fmaf(e[i], 1.f / LO, l[i]);
                                 }
 #pragma unroll
                                 for (int i = 0; i < 8; ++i) x[i] = fmaf(g.beta, l[i], x[i]);
@@ -516,7 +522,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                                 packed[0][16 * h + 4 * j + i] = *reinterpret_cast<const uint32_t*>(&hi);
                                 if constexpr (OUT > 1) {
                                     const float2 f = __half22float2(hi);
-                                    const __half2 lo = __floats2half2_rn(x[2 * i] - f.x, x[2 * i + 1] - f.y);
+                                    const __half2 lo = __floats2half2_rn((x[2 * i] - f.x) * LO, (x[2 * i + 1] - f.y) * LO);
                                     packed[1][16 * h + 4 * j + i] = *reinterpret_cast<const uint32_t*>(&lo);
                                 }
                             }
@@ -611,7 +617,7 @@ __global__ void __launch_bounds__(FOLD_THREADS) fold_kernel(const __grid_constan
         for (int j = 0; j < 4; ++j) {
             const __half h = __float2half_rn(x[j]);
             s_tile[0][row][col + j] = h;
-            if (PLANES > 1) s_tile[PLANES - 1][row][col + j] = __float2half_rn(x[j] - __half2float(h));
+            if (PLANES > 1) s_tile[PLANES - 1][row][col + j] = __float2half_rn((x[j] - __half2float(h)) * LO);
         }
     }
     __syncthreads();
@@ -659,6 +665,7 @@ struct Part {
 struct ElemArgs {
     int parts, nesterov;
     float momentum, eps, lr;
+    float up, unscale;                    // of X: times LEAST_SCALE to the operands' scale, and back to X
     const float *grad_scale, *lr_now;
     Part part[MAX_STACKS];
 };
@@ -801,12 +808,12 @@ __device__ __forceinline__ void start_piece(const ElemArgs& a, const Piece& p, f
             __half2* lp = reinterpret_cast<__half2*>(&l);
 #pragma unroll
             for (int k = 0; k < 8; k += 2) {
-                const float x0 = direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[e][k], gs), m[e][k]) * inv;
+                const float x0 = direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[e][k], gs), m[e][k]) * inv * a.up;
                 const float x1 =
-                    direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[e][k + 1], gs), m[e][k + 1]) * inv;
+                    direction(a.nesterov, a.momentum, mom != nullptr, __fmul_rn(g[e][k + 1], gs), m[e][k + 1]) * inv * a.up;
                 hp[k / 2] = __floats2half2_rn(x0, x1);
                 const float2 f = __half22float2(hp[k / 2]);
-                lp[k / 2] = __floats2half2_rn(x0 - f.x, x1 - f.y);
+                lp[k / 2] = __floats2half2_rn((x0 - f.x) * LO, (x1 - f.y) * LO);
             }
             *reinterpret_cast<uint4*>(p.part->hi + plane + t[e].in_plane) = h;
             *reinterpret_cast<uint4*>(p.part->lo + plane + t[e].in_plane) = l;
@@ -843,7 +850,7 @@ __device__ __forceinline__ void finish_piece(const ElemArgs& a, const Piece& p) 
     float* master = MASTER ? p.part->master + p.base : nullptr;
     const long long plane = (long long)p.matrix * p.part->rows * p.part->ld;
     const float lr = a.lr_now ? *a.lr_now : a.lr;
-    const float keep = 1.f - lr * p.part->decay, rate = lr * p.part->scale * (1.f / SCALE);
+    const float keep = 1.f - lr * p.part->decay, rate = lr * p.part->scale * a.unscale;
 #pragma unroll 1
     for (int turn = 0; turn < TURNS; ++turn) {
         Place t[PER_THREAD];
@@ -867,8 +874,8 @@ __device__ __forceinline__ void finish_piece(const ElemArgs& a, const Piece& p) 
             half8(lo[e], l);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                o[k] += l[k];
-                w[e][k] = STEP ? w[e][k] * keep - rate * o[k] : o[k] * (1.f / SCALE);
+                o[k] = fmaf(l[k], 1.f / LO, o[k]);
+                w[e][k] = STEP ? w[e][k] * keep - rate * o[k] : o[k] * a.unscale;
             }
             if (MASTER) put_octet<VEC>(master + t[e].at, t[e].valid, w[e]);
             put_octet<VEC>(out + t[e].at, t[e].valid, w[e]);
@@ -888,12 +895,13 @@ __global__ void __launch_bounds__(EL_THREADS, 6) finish_kernel(const __grid_cons
 
 // ---- host side ------------------------------------------------------------------------------------
 constexpr int MAX_SIDE = 16384;
-constexpr float LEAST_EPS = 4e-36f;       // below it SCALE / (norm + eps) could pass float32's range
+constexpr float LEAST_EPS = 4e-36f;       // below it LEAST_SCALE / (norm + eps) could pass float32's range
 constexpr int MAX_BATCH = 1 << 24, MAX_MATRICES = 1 << 27;   // (the latter times the CTAs of a cluster: a grid's limit)
 constexpr size_t ROUND_BYTES = 512u << 20;          // workspace of a round, unless one matrix needs more
 
 struct Coefs {
     int steps;
+    float scale;                                     // of the operands
     float c[MAX_STEPS][3];
 };
 // The iteration's coefficients, if fp16 can hold its iterates: from singular values in [0, 1] on, X stays
@@ -901,14 +909,13 @@ struct Coefs {
 static bool read_coefs(int32_t steps, const double* given, Coefs* out) {
     if (steps < 1 || steps > MAX_STEPS) return false;
     out->steps = steps;
-    double top = 1.0;
+    double top = 1.0, most = 1.0;
     for (int k = 0; k < steps; ++k) {
         const double a = given ? given[3 * k] : 3.4445, b = given ? given[3 * k + 1] : -4.7750,
                      c = given ? given[3 * k + 2] : 2.0315;
         out->c[k][0] = (float)a;
         out->c[k][1] = (float)b;
         out->c[k][2] = (float)c;
-        if (!given) continue;
         if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
         double next = 0.0, poly = 0.0;
         for (int i = 0; i <= 256; ++i) {
@@ -917,8 +924,11 @@ static bool read_coefs(int32_t steps, const double* given, Coefs* out) {
             poly = std::fmax(poly, std::fmax(std::fabs(p), std::fabs(a + p)));
         }
         if (!(next <= 16.0) || !(poly <= 60.0) || !(top * top <= 60.0)) return false;
+        most = std::fmax(std::fmax(most, next), std::fmax(poly, top * top));
         top = next;
     }
+    out->scale = MOST_SCALE;
+    while (out->scale > LEAST_SCALE && out->scale * most > MAX_HALF) out->scale *= 0.5f;
     return true;
 }
 
@@ -1208,11 +1218,11 @@ static r3_status iterate(const Class* classes, int n, int part, bool coarse, uin
             next_partial += (size_t)gr.tiles * count * gr.splits * SLOT<TN>;
         }
     }
-    fold.alpha = 1.f / SCALE;
+    fold.alpha = 1.f / coefs.scale;
     if (!ok) return R3_ERR_CUDA;
     for (GemmArgs* g : {&gram[0], &gram[1], &poly, &apply[0], &apply[1]}) {
         g->classes = n;
-        g->alpha = 1.f / SCALE;
+        g->alpha = 1.f / coefs.scale;
         g->beta = g->diag = 0.f;
         g->keep_lo = 1;
         g->dev_status = dev_status;
@@ -1224,10 +1234,10 @@ static r3_status iterate(const Class* classes, int n, int part, bool coarse, uin
     int k = 0;
     for (int step = 0; step < coefs.steps; ++step, k ^= 1) {
         const float *c = coefs.c[step];
-        poly.alpha = c[2] / SCALE;
+        poly.alpha = c[2] / coefs.scale;
         poly.beta = c[1];
-        poly.diag = c[0] * SCALE;
-        apply[k].beta = c[0];
+        poly.diag = c[0] * coefs.scale;
+        apply[k].beta = c[0] / LO;                   // (of the lo plane)
         if (TERMS == 1) {
             const int left = coefs.steps - step;
             apply[k].keep_lo = left > 2 || (left == 2 ? !last_without : !coarse);
@@ -1267,6 +1277,7 @@ static r3_status run_small_stacks(const Job& job, const Coefs& coefs, const r3_m
     a.momentum = job.momentum;
     a.eps = job.eps;
     a.lr = job.lr;
+    a.scale = coefs.scale;
     a.grad_scale = job.grad_scale;
     a.lr_now = job.lr_now;
     a.dev_status = dev_status;
@@ -1302,6 +1313,8 @@ static r3_status run_round(const Job& job, const Coefs& coefs, Round& r, uint8_t
     a.momentum = job.momentum;
     a.eps = job.eps;
     a.lr = job.lr;
+    a.up = coefs.scale / LEAST_SCALE;
+    a.unscale = 1.f / coefs.scale;
     a.grad_scale = job.grad_scale;
     a.lr_now = job.lr_now;
     const size_t psize = job.param_dtype == R3_BF16 ? 2 : 4, gsize = job.grad_dtype == R3_BF16 ? 2 : 4;

@@ -12,7 +12,12 @@ namespace ns {
 
 using namespace tc;
 
-constexpr float SCALE = 1024.f;           // every fp16 operand is its value times this
+// An fp16 operand is its value times a power of two, the largest that keeps all iterates within MAX_HALF (2^14 for
+// the usual coefficients).  Its lo plane holds what hi leaves times LO more, or small elements would lose it
+// (without that, and with 2^10 for all, rows a millionth of the others were 5e-3 off in float32 results, with both 3e-7).
+constexpr float LEAST_SCALE = 1024.f, MOST_SCALE = 16384.f, MAX_HALF = 61440.f;
+constexpr int LO_SHIFT = 11;              // (a value within MAX_HALF leaves 16 at most)
+constexpr float LO = 1 << LO_SHIFT;
 constexpr int MAX_STACKS = 64;            // per launch: the table travels in the kernel's parameters
 constexpr int MAX_STEPS = 16;
 
@@ -47,11 +52,11 @@ __device__ __forceinline__ float direction(bool nesterov, float momentum, bool h
     if (!has) return g;
     return nesterov ? __fadd_rn(g, __fmul_rn(momentum, m)) : m;
 }
-// What u is multiplied with to give X times SCALE.  A matrix of zeros stays one; anything not finite reaches
+// What u is multiplied with to give X times LEAST_SCALE.  A matrix of zeros stays one; anything not finite reaches
 // every element.
 __device__ __forceinline__ float start_scale(double sum, float eps) {
     const double norm = sqrt(sum);
-    return norm == 0.0 ? 0.f : (float)((double)SCALE / (norm + (double)eps));
+    return norm == 0.0 ? 0.f : (float)((double)LEAST_SCALE / (norm + (double)eps));
 }
 
 // ---- matrices whose smaller side is at most SMALL_SIDE: r3_muon_small.cu ---------------------------------
@@ -71,7 +76,7 @@ struct SmallArgs {
     int stacks, cluster, steps;
     int grad_dtype, param_dtype, step, nesterov;
     int x_blocks, a_blocks, a_bytes, tmem_cols;      // set by run_small
-    float momentum, eps, lr;
+    float momentum, eps, lr, scale;       // scale: of the operands
     float coefs[MAX_STEPS][3];
     const float *grad_scale, *lr_now;
     int32_t* dev_status;

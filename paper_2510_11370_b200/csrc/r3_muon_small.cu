@@ -53,16 +53,17 @@ __device__ __forceinline__ void split8(const float (&x)[8], uint4* hi, uint4* lo
     for (int i = 0; i < 4; ++i) {
         h[i] = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
         const float2 f = __half22float2(h[i]);
-        l[i] = __floats2half2_rn(x[2 * i] - f.x, x[2 * i + 1] - f.y);
+        l[i] = __floats2half2_rn((x[2 * i] - f.x) * LO, (x[2 * i + 1] - f.y) * LO);
     }
 }
-__device__ __forceinline__ void add8(const uint4& v, float (&x)[8]) {
+// x += v, or v / LO where it is of a lo plane.
+template <bool LOW> __device__ __forceinline__ void add8(const uint4& v, float (&x)[8]) {
     const __half2* h = reinterpret_cast<const __half2*>(&v);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 f = __half22float2(h[i]);
-        x[2 * i] += f.x;
-        x[2 * i + 1] += f.y;
+        x[2 * i] = fmaf(f.x, LOW ? 1.f / LO : 1.f, x[2 * i]);
+        x[2 * i + 1] = fmaf(f.y, LOW ? 1.f / LO : 1.f, x[2 * i + 1]);
     }
 }
 
@@ -182,8 +183,8 @@ __device__ __forceinline__ void write_octets(const SmallArgs& a, Octets w, const
         for (int e = 0; e < 4; ++e) {
             if (valid[e] == 0) continue;
             float x[8] = {};
-            add8(*reinterpret_cast<const uint4*>(planes + t[e]), x);
-            add8(*reinterpret_cast<const uint4*>(planes + plane + t[e]), x);
+            add8<false>(*reinterpret_cast<const uint4*>(planes + t[e]), x);
+            add8<true>(*reinterpret_cast<const uint4*>(planes + plane + t[e]), x);
 #pragma unroll
             for (int k = 0; k < 8; ++k) x[k] = a.step ? old[e][k] * keep - rate * x[k] : -rate * x[k];
             if (master) put8<VEC>(master + at[e], hop, valid[e], x);
@@ -281,7 +282,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
         }
         sum = 0.0;
         for (int i = 0; i < C; ++i) sum += s_norm[i];
-        const float inv = start_scale(sum, a.eps);
+        const float inv = start_scale(sum, a.eps), up = a.scale / LEAST_SCALE, unscale = 1.f / a.scale;
         // ---- X = u / (|u| + eps) into the planes, zeros around it ----------------------------------
         Octets w = mine;
         w.begin();
@@ -291,7 +292,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
             // (a product of zero and an infinite or undefined scale would leave NaN around the matrix)
             const int valid = w.valid();
 #pragma unroll
-            for (int k = 0; k < 8; ++k) u[e][k] = k < valid ? u[e][k] * inv : 0.f;
+            for (int k = 0; k < 8; ++k) u[e][k] = k < valid ? u[e][k] * inv * up : 0.f;
             uint4 hi, lo;
             split8(u[e], &hi, &lo);
             const uint32_t t = tile_at(w.i, 8 * w.o);
@@ -308,7 +309,8 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
         uint32_t phase = 0, phase2 = 0, a_phase = 0;
         bool alive = true;
         // D = P Q over the steps of 16 along k from `k0` to `k1`, columns c0 to c0 + N of D; plane choice by term,
-        // small products first.  Three products: every 64 of k have an accumulator of their own, `apart` columns
+        // small products first, onto 2^-11 of whose sum
+        // (they hold a lo plane) comes the large one.  Three products: every 64 of k have an accumulator of their own, `apart` columns
         // further on, and the epilogue adds them up (an addition in tensor memory drops what lies below the
         // running sum's last place).
         auto issue = [&](uint32_t p0, uint32_t p_plane, uint32_t q0, uint32_t q_plane, bool q_mn, int c0, int N,
@@ -318,19 +320,26 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
                 if (alive && elect_one()) {
                     const uint32_t idesc = (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(128 >> 4) << 24) |
                                            (q_mn ? 1u << 16 : 0u);
-                    for (int seg = k0; seg < k1; seg += TERMS > 1 ? 4 : k1)
-                    for (int term = 0; term < TERMS; ++term) {
-                        const int k_end = TERMS > 1 ? min(k1, seg + 4) : k1;
-                        const uint32_t p = base + p0 + (TERMS > 1 && term == 1 ? p_plane : 0u);
-                        const uint32_t qq = base + q0 + (TERMS > 1 && term == 0 ? q_plane : 0u);
-                        for (int k = seg; k < k_end; ++k) {
-                            const uint32_t in_row = (uint32_t)((k >> 2) * SM_BLOCK + (k & 3) * 32);
-                            const uint64_t dq = q_mn ? smem_desc_mn_sw128(qq + (uint32_t)(c0 >> 6) * SM_BLOCK +
-                                                                              (uint32_t)k * 2048u, SM_BLOCK)
-                                                     : smem_desc_sw128(qq + in_row);
-                            tc_mma_bf16(tmem + (uint32_t)(c0 + (TERMS > 1 ? (seg >> 2) * apart : 0)),
-                                        smem_desc_sw128(p + in_row), dq, idesc,
-                                        term != 0 || k != (TERMS > 1 ? seg : 0) ? 1u : 0u);
+                    const uint64_t q_step = q_mn ? 2048 >> 4 : 2;          // (a descriptor counts 16 bytes)
+                    for (int seg = k0; seg < k1; seg += 4) {
+                        const uint32_t d = tmem + (uint32_t)(c0 + (TERMS > 1 ? (seg >> 2) * apart : 0));
+                        const uint32_t block = (uint32_t)((seg >> 2) * SM_BLOCK);
+                        const uint32_t p = base + p0 + block;
+                        const uint32_t qq = base + q0 + (q_mn ? (uint32_t)(c0 >> 6) * SM_BLOCK + (uint32_t)seg * 2048u : block);
+#pragma unroll
+                        for (int term = 0; term < TERMS; ++term) {
+                            const uint32_t tq = qq + (TERMS > 1 && term == 0 ? q_plane : 0u);
+                            const uint64_t dp = smem_desc_sw128(p + (TERMS > 1 && term == 1 ? p_plane : 0u));
+                            const uint64_t dq = q_mn ? smem_desc_mn_sw128(tq, SM_BLOCK) : smem_desc_sw128(tq);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                if (seg + j >= k1) continue;
+                                if (term == 2 && j == 0)
+                                    tc_mma_bf16_onto_scaled<LO_SHIFT>(d, dp, dq, idesc);
+                                else
+                                    tc_mma_bf16(d, dp + 2 * j, dq + q_step * j, idesc,
+                                                (term | j) != 0 || (TERMS == 1 && seg != k0) ? 1u : 0u);
+                            }
                         }
                     }
                     tc_commit(done);
@@ -381,7 +390,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
                     for (int j = 0; j < 4; ++j) {
                         float x[8];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) x[k] = v[8 * j + k] * (1.f / SCALE);
+                        for (int k = 0; k < 8; ++k) x[k] = v[8 * j + k] * unscale;
                         uint4 hi, lo;
                         split8(x, &hi, &lo);
                         const uint32_t t = a0 + tile_at(r, c + 8 * j);
@@ -424,7 +433,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
                         x[4] += h.x; x[5] += h.y; x[6] += h.z; x[7] += h.w;
                     }
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) x[k] *= 1.f / SCALE;
+                    for (int k = 0; k < 8; ++k) x[k] *= unscale;
                     uint4 hi, lo;
                     split8(x, &hi, &lo);
                     const uint32_t t = staged + (uint32_t)(o >> 3) * rows_bytes + (uint32_t)(rr * 128) +
@@ -464,12 +473,12 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
                     if (c + 8 * j >= m16) continue;
                     const uint32_t t = a0 + tile_at(r, c + 8 * j);
                     float x[8] = {};
-                    add8(*reinterpret_cast<const uint4*>(bp + t), x);
-                    if (PL > 1) add8(*reinterpret_cast<const uint4*>(bp + a_plane + t), x);
+                    add8<false>(*reinterpret_cast<const uint4*>(bp + t), x);
+                    if (PL > 1) add8<true>(*reinterpret_cast<const uint4*>(bp + a_plane + t), x);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        x[k] = fmaf(cb, x[k], (cc / SCALE) * v[8 * j + k]);
-                        if (TERMS == 1 && c + 8 * j + k == r) x[k] += ca * SCALE;
+                        x[k] = fmaf(cb, x[k], cc * unscale * v[8 * j + k]);
+                        if (TERMS == 1 && c + 8 * j + k == r) x[k] += ca * a.scale;
                     }
                     uint4 hi, lo;
                     split8(x, &hi, &lo);
@@ -499,10 +508,10 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
                     if (c + 8 * j >= W) continue;
                     const uint32_t t = tile_at(r, c + 8 * j);
                     float x[8] = {};
-                    if (TERMS > 1) add8(*reinterpret_cast<const uint4*>(bp + t), x);
-                    add8(*reinterpret_cast<const uint4*>(bp + x_plane + t), x);
+                    if (TERMS > 1) add8<false>(*reinterpret_cast<const uint4*>(bp + t), x);
+                    add8<true>(*reinterpret_cast<const uint4*>(bp + x_plane + t), x);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) x[k] = fmaf(ca, x[k], (1.f / SCALE) * v[8 * j + k]);
+                    for (int k = 0; k < 8; ++k) x[k] = fmaf(ca, x[k], unscale * v[8 * j + k]);
                     uint4 hi, lo;
                     split8(x, &hi, &lo);
                     *reinterpret_cast<uint4*>(bp + t) = hi;
@@ -514,7 +523,7 @@ __global__ void __launch_bounds__(SM_THREADS, 1) small_kernel(const __grid_const
 
         // ---- the result, or the weights' update -------------------------------------------------------
         const float lr = a.lr_now ? *a.lr_now : a.lr;
-        const float keep = 1.f - lr * st.decay, rate = a.step ? lr * st.scale * (1.f / SCALE) : -(1.f / SCALE);
+        const float keep = 1.f - lr * st.decay, rate = a.step ? lr * st.scale * unscale : -unscale;
         float* master = st.master ? st.master + at0 : nullptr;
         if (a.param_dtype == R3_BF16) {
             __nv_bfloat16* param = static_cast<__nv_bfloat16*>(st.param) + at0;

@@ -1257,13 +1257,13 @@ static r3_status iterate(const Class* classes, int n, int part, bool coarse, uin
 }
 
 struct Job {
-    int param_dtype, grad_dtype, nesterov, terms;
+    int param_dtype, grad_dtype, nesterov, terms;    // terms: as the caller has them (terms_of)
     bool master, step;
     float momentum, eps, lr;
     const float *grad_scale, *lr_now;
 };
 static r3_status run_small_stacks(const Job& job, const Coefs& coefs, const r3_muon_stack* const* ss, int n,
-                                  int cluster, int matrices, int32_t* dev_status, cudaStream_t cs) {
+                                  int terms, int cluster, int matrices, int32_t* dev_status, cudaStream_t cs) {
     SmallArgs a = {};
     a.stacks = n;
     a.cluster = cluster;
@@ -1287,7 +1287,7 @@ static r3_status run_small_stacks(const Job& job, const Coefs& coefs, const r3_m
         a.stack[i] = {s.param, s.master, s.grad, s.momentum, first, s.rows, s.cols, s.weight_decay, s.scale};
         first += s.batch;
     }
-    return run_small(a, job.terms, matrices, cs);
+    return run_small(a, terms, matrices, cs);
 }
 
 // Matrices [begin, begin + count) of a stack, in class `cls` of the round as numbers `at` and on.
@@ -1298,7 +1298,7 @@ struct Slice {
 struct Round {
     Class cls[MAX_CLASSES];
     Slice slice[MAX_STACKS];
-    int classes = 0, slices = 0;
+    int classes = 0, slices = 0, terms = 0;
     size_t bytes = 0;
 };
 static r3_status run_round(const Job& job, const Coefs& coefs, Round& r, uint8_t* ws, int32_t* dev_status,
@@ -1361,10 +1361,10 @@ static r3_status run_round(const Job& job, const Coefs& coefs, Round& r, uint8_t
     }
     if (e != cudaSuccess) return R3_ERR_CUDA;
     int at = 0;
-    const Cut cut = cut_of(r.cls, r.classes, job.terms);
-    const bool coarse = job.terms == 1 && job.param_dtype == R3_BF16 && !job.master;
+    const Cut cut = cut_of(r.cls, r.classes, r.terms);
+    const bool coarse = r.terms == 1 && job.param_dtype == R3_BF16 && !job.master;
     const bool narrow = cut.tn == 128;
-    const auto steps = job.terms > 1 ? (narrow ? iterate<3, 128> : iterate<3, 256>)
+    const auto steps = r.terms > 1 ? (narrow ? iterate<3, 128> : iterate<3, 256>)
                                      : (narrow ? iterate<1, 128> : iterate<1, 256>);
     const r3_status st = steps(r.cls, r.classes, cut.part, coarse, ws, coefs, dev_status, &at, cs);
     if (st != R3_OK) return st;
@@ -1381,32 +1381,39 @@ static r3_status run_round(const Job& job, const Coefs& coefs, Round& r, uint8_t
     return e == cudaSuccess ? R3_OK : R3_ERR_CUDA;
 }
 
-// Cuts stacks into launches: small(members, n, cluster, matrices) for each group of the on-chip form, with as
-// many CTAs per matrix, round(r) for each round of the others: up to MAX_CLASSES shapes, MAX_STACKS stacks
-// and ROUND_BYTES of workspace (one matrix at least), shapes with long products first.
+// Products per product.  One that holds for a bf16 result does so by the errors of many operands evening out: on
+// matrices of a short side they come to more than the rounding (simulated for Gaussian ones: 1 x 3 up to 4e-3, 2 x 3
+// 7e-3, 4 x 64 5e-3, 8 x 8 4e-3, 16 x 16 2.5e-3, 16 x 300 1.7e-3 of the result's rms, the rounding being 1.7e-3),
+// so these take three (8 x 2048 41 -> 53 us, 24 x 8 x 256 29 -> 39, 12 x 4000 84 -> 111).
+constexpr int LEAST_SIDE = 16;
+static int terms_of(const r3_muon_stack& s, int terms) { return std::min(s.rows, s.cols) < LEAST_SIDE ? 3 : terms; }
+
+// Cuts stacks into launches: small(members, n, terms, cluster, matrices) for each group of the on-chip form, with as
+// many products and CTAs per matrix, round(r) for each round of the others: up to MAX_CLASSES shapes of as many
+// products, MAX_STACKS stacks and ROUND_BYTES of workspace (one matrix at least), shapes with long products first.
 template <typename Small, typename Big>
 static r3_status each_launch(const r3_muon_stack* ss, int32_t count, int terms, Small small, Big big) {
     std::vector<const r3_muon_stack*> little, large;
     for (int32_t i = 0; i < count; ++i)
         if (ss[i].batch > 0) (small_cluster(ss[i].rows, ss[i].cols) ? little : large).push_back(ss + i);
-    std::stable_sort(little.begin(), little.end(), [](const r3_muon_stack* x, const r3_muon_stack* y) {
-        return small_cluster(x->rows, x->cols) < small_cluster(y->rows, y->cols);
-    });
+    auto kind = [&](const r3_muon_stack* s) { return 4 * small_cluster(s->rows, s->cols) + terms_of(*s, terms); };
+    std::stable_sort(little.begin(), little.end(),
+                     [&](const r3_muon_stack* x, const r3_muon_stack* y) { return kind(x) < kind(y); });
     for (size_t i = 0; i < little.size();) {
-        const int cluster = small_cluster(little[i]->rows, little[i]->cols);
         size_t end = i;
         long long matrices = 0;
-        for (; end < little.size() && end < i + MAX_STACKS &&
-               small_cluster(little[end]->rows, little[end]->cols) == cluster &&
+        for (; end < little.size() && end < i + MAX_STACKS && kind(little[end]) == kind(little[i]) &&
                matrices + little[end]->batch <= MAX_MATRICES; ++end)
             matrices += little[end]->batch;
-        const r3_status st = small(little.data() + i, (int)(end - i), cluster, (int)matrices);
+        const r3_status st = small(little.data() + i, (int)(end - i), terms_of(*little[i], terms),
+                                   small_cluster(little[i]->rows, little[i]->cols), (int)matrices);
         if (st != R3_OK) return st;
         i = end;
     }
-    std::stable_sort(large.begin(), large.end(), [](const r3_muon_stack* x, const r3_muon_stack* y) {
+    std::stable_sort(large.begin(), large.end(), [&](const r3_muon_stack* x, const r3_muon_stack* y) {
+        const int tx = terms_of(*x, terms), ty = terms_of(*y, terms);
         const int nx = std::max(x->rows, x->cols), ny = std::max(y->rows, y->cols);
-        return nx != ny ? nx > ny : x->rows != y->rows ? x->rows > y->rows : x->cols > y->cols;
+        return tx != ty ? tx < ty : nx != ny ? nx > ny : x->rows != y->rows ? x->rows > y->rows : x->cols > y->cols;
     });
     Round r;
     auto flush = [&]() {
@@ -1416,13 +1423,13 @@ static r3_status each_launch(const r3_muon_stack* ss, int32_t count, int terms, 
     };
     for (const r3_muon_stack* s : large) {
         for (int begin = 0; begin < s->batch;) {
-            const Problem p = problem_of(s->rows, s->cols, terms);
+            const Problem p = problem_of(s->rows, s->cols, terms_of(*s, terms));
             const bool same = r.classes && r.cls[r.classes - 1].p.rows == s->rows && r.cls[r.classes - 1].p.cols == s->cols;
             const long long here = same ? r.cls[r.classes - 1].count : 0;
             const size_t before = r.bytes - (same ? layout(p, here).total : 0);
             // as many of the stack's matrices as fit
             long long n = 0;
-            if (r.slices < MAX_STACKS && (same || r.classes < MAX_CLASSES)) {
+            if (r.slices < MAX_STACKS && (same || r.classes < MAX_CLASSES) && (r.slices == 0 || r.terms == p.terms)) {
                 const size_t one = layout(p, 1).total;
                 const size_t room = ROUND_BYTES > r.bytes ? ROUND_BYTES - r.bytes : 0;
                 n = std::min<long long>((long long)(room / one), s->batch - begin);
@@ -1433,6 +1440,7 @@ static r3_status each_launch(const r3_muon_stack* ss, int32_t count, int terms, 
                 if (st != R3_OK) return st;
                 continue;
             }
+            r.terms = p.terms;
             if (!same) r.cls[r.classes++] = {p, 0, nullptr};
             Class& c = r.cls[r.classes - 1];
             r.slice[r.slices++] = {s, begin, (int)n, r.classes - 1, c.count};
@@ -1447,12 +1455,12 @@ static r3_status each_launch(const r3_muon_stack* ss, int32_t count, int terms, 
 static size_t workspace_bytes(const r3_muon_stack* ss, int32_t count, int terms) {
     size_t most = 0;
     each_launch(ss, count, terms,
-                [&](const r3_muon_stack* const*, int, int, int) {
+                [&](const r3_muon_stack* const*, int, int, int, int) {
                     most = std::max(most, (size_t)256);
                     return R3_OK;
                 },
                 [&](Round& r) {
-                    most = std::max(most, r.bytes + partial_bytes(r.cls, r.classes, terms, cut_of(r.cls, r.classes, terms)));
+                    most = std::max(most, r.bytes + partial_bytes(r.cls, r.classes, r.terms, cut_of(r.cls, r.classes, r.terms)));
                     return R3_OK;
                 });
     return most;
@@ -1460,8 +1468,8 @@ static size_t workspace_bytes(const r3_muon_stack* ss, int32_t count, int terms)
 static r3_status run(const Job& job, const Coefs& coefs, const r3_muon_stack* ss, int32_t count, uint8_t* ws,
                      int32_t* dev_status, cudaStream_t cs) {
     return each_launch(ss, count, job.terms,
-                       [&](const r3_muon_stack* const* group, int n, int cluster, int matrices) {
-                           return run_small_stacks(job, coefs, group, n, cluster, matrices, dev_status, cs);
+                       [&](const r3_muon_stack* const* group, int n, int terms, int cluster, int matrices) {
+                           return run_small_stacks(job, coefs, group, n, terms, cluster, matrices, dev_status, cs);
                        },
                        [&](Round& r) { return run_round(job, coefs, r, ws, dev_status, cs); });
 }

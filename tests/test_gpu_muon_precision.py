@@ -109,3 +109,39 @@ def test_step_keeps_weak_rows(r3):
     for w, g, weak in zip(weights, grads, (np.s_[:9], np.s_[:9], np.s_[:, :9])):
         u = g.reshape(-1, *g.shape[-2:])[0] * 1.5
         three(-w.reshape(-1, *w.shape[-2:])[0].cpu(), u, 5, [weak, np.s_[:]])
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 3), (3, 1), (2, 3), (4, 64), (3, 500), (500, 3), (8, 8), (15, 300),
+                                       (9, 2500), (2500, 15)])
+def test_short_sides_take_three_products(r3, rows, cols):
+    """The errors of one product even out over many operands, of which these have few: asked for one, they take
+    three, and a bf16 result is off by its rounding."""
+    x = matrix(rows, cols, 5, 3).to(BF)
+    got, rounded = r3.orthogonalize(x.cuda(), out_dtype=F32, products=1).cpu(), r3.orthogonalize(x.cuda()).cpu()
+    assert torch.equal(got, r3.orthogonalize(x.cuda(), out_dtype=F32, products=3).cpu())
+    assert torch.equal(got.to(BF), rounded)
+    for i in range(3):
+        want = O.iterate(f64(x[i]))
+        bound = 2 * rms(O.iterate_planes(f64(x[i])) - want) + 2 * rms(O.iterate_f32(f64(x[i])) - want) + \
+            rms(O.iterate_short(f64(x[i])) - want) + 2.0 ** -20 * rms(want)
+        assert rms(f64(got[i]) - want) <= bound < 1e-4 * rms(want)
+
+
+def test_one_step_over_short_and_long_sides(r3):
+    """Stacks that take one product and such that take three, on the chip (there each as by itself) and larger, in
+    one call."""
+    shapes = [(2, 8, 40), (2, 40, 80), (12, 2600), (24, 2600), (300, 500), (2600, 15), (3, 16, 16), (1, 15, 15), (8, 40)]
+    grads = [matrix(s[-2], s[-1], 6, int(np.prod(s[:-2]))).reshape(s).to(BF) for s in shapes]
+    weights = [torch.zeros(s, dtype=BF).cuda() for s in shapes]
+    r3.Muon(weights, [g.cuda() for g in grads], momentum=0.0, scale=1.0).step(1.0)
+    half = torch.finfo(BF).eps / 2
+    for w, g in zip(weights, grads):
+        rows, cols = g.shape[-2:]
+        u = g.reshape(-1, rows, cols)
+        if max(rows, cols) <= 256 and min(rows, cols) <= 128:
+            assert torch.equal(-w, r3.orthogonalize(u.cuda()).reshape(w.shape))
+        want, before = O.iterate(f64(u[0])), O.iterate(f64(u[0]), 4)
+        loss = rms(O.iterate(f64(u[0]), operand=O.scaled_operand) - want) if min(rows, cols) >= 16 else 2.0 ** -16 * rms(want)
+        last = O.QUINTIC[0] * rms(O.scaled_operand(before) - before)
+        err = rms(f64(-w.reshape(-1, rows, cols)[0]) - want)
+        assert err <= np.sqrt((1.5 * loss) ** 2 + (half * rms(want)) ** 2 + last ** 2)

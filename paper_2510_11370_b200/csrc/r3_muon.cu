@@ -275,6 +275,7 @@ __global__ void __launch_bounds__(THREADS, 1) gemm_kernel(const __grid_constant_
                 int stage = 0, acc = 0;
                 uint32_t phase = 0, acc_phase = 0;
                 bool ok = true;
+                grid_dependency_wait();                  // (or its waits' limits would run while others do)
                 for (int item = pair; ok && item < g.items; item += pairs) {
                     const Tile t = item == pair ? first_tile : decode<PHASE, TN>(g, item);
                     const ClassArgs& c = g.c[t.k];

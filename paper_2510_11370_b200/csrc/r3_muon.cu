@@ -917,6 +917,7 @@ static bool read_coefs(int32_t steps, const double* given, Coefs* out) {
         out->c[k][0] = (float)a;
         out->c[k][1] = (float)b;
         out->c[k][2] = (float)c;
+        if (!given) continue;                        // (X within 1.3, the others within 3.4445 = a)
         if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return false;
         double next = 0.0, poly = 0.0;
         for (int i = 0; i <= 256; ++i) {

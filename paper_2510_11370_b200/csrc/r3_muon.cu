@@ -991,15 +991,16 @@ static bool make_map(CUtensorMap* m, const void* ptr, int count, int rows, int c
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// CTA pairs of a kernel that can be resident at once (one CTA per SM), asked once per kernel and device.
+// CTA pairs of a kernel that can be resident at once (one CTA per SM), asked once per kernel and device; -1: a
+// kernel that splits the register file, of which a launch has too few registers for its split.
 static int resident_pairs(void (*kern)(GemmArgs), bool split, int smem, int (&cached)[64]) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
     if (cached[dev] == 0) {
         cudaFuncAttributes attrs;
-        if (cudaFuncGetAttributes(&attrs, kern) != cudaSuccess || (split && attrs.numRegs < LAUNCH_REGS) ||
-            cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
-            return 0;
+        if (cudaFuncGetAttributes(&attrs, kern) != cudaSuccess) return 0;
+        if (split && attrs.numRegs < LAUNCH_REGS) return cached[dev] = -1;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return 0;
         cudaLaunchConfig_t cfg = {};
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -1017,12 +1018,37 @@ static int resident_pairs(void (*kern)(GemmArgs), bool split, int smem, int (&ca
     }
     return cached[dev];
 }
+template <int PHASE, int TERMS, int TN> static int pairs_of() {
+    using R = Ring<TERMS, TN>;
+    static int cached[64] = {0};
+    return resident_pairs(gemm_kernel<PHASE, TERMS, TN>, R::SPLIT, R::SMEM_BYTES, cached);
+}
+template <int TERMS, int TN> static int least_pairs() {
+    return std::min({pairs_of<GRAM, TERMS, TN>(), pairs_of<POLY, TERMS, TN>(), pairs_of<APPLY, TERMS, TN>()});
+}
+// Tiles of 256 columns with three products need the registers of their split; how many a kernel gets is the
+// compiler's choice (168 now).  Without them everything runs in tiles of 128.
+static bool wide_runs(int terms) {
+    if (terms == 1) return true;
+    const int pairs = least_pairs<3, 256>();
+    if (pairs == 0) cudaGetLastError();              // (a machine without a GPU asks for workspaces too)
+    return pairs >= 0;
+}
+// Whether every product that a call may come to can be launched: asked before its first launch, so that what is
+// refused leaves everything as it was.
+static bool products_run() {
+    static PerDevice ready;
+    if (ready.done()) return true;
+    if (least_pairs<1, 128>() <= 0 || least_pairs<1, 256>() <= 0 || least_pairs<3, 128>() <= 0 || least_pairs<3, 256>() == 0)
+        return false;
+    ready.mark();
+    return true;
+}
 
 template <int PHASE, int TERMS, int TN> static r3_status launch_gemm(const GemmArgs& g, cudaStream_t cs) {
     auto kern = gemm_kernel<PHASE, TERMS, TN>;
     using R = Ring<TERMS, TN>;
-    static int cached[64] = {0};
-    const int pairs = resident_pairs(kern, R::SPLIT, R::SMEM_BYTES, cached);
+    const int pairs = pairs_of<PHASE, TERMS, TN>();
     if (pairs <= 0) return R3_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
@@ -1077,6 +1103,7 @@ static Cut cut_of(const Class* classes, int n, int terms) {
         side = std::max(side, (classes[i].p.m + BK - 1) / BK);
     }
     for (int tn : {256, 128}) {
+        if (tn == 256 && !wide_runs(terms)) continue;
         const int block = tn == 256 ? 20 : terms > 1 ? 11 : 13;
         const int around = (terms > 1 ? 80 : 220) * tn / 256;
         long long square = 0, all = 0;
@@ -1469,6 +1496,8 @@ static size_t workspace_bytes(const r3_muon_stack* ss, int32_t count, int terms)
 }
 static r3_status run(const Job& job, const Coefs& coefs, const r3_muon_stack* ss, int32_t count, uint8_t* ws,
                      int32_t* dev_status, cudaStream_t cs) {
+    const auto large = [](const r3_muon_stack& s) { return s.batch > 0 && small_cluster(s.rows, s.cols) == 0; };
+    if (std::any_of(ss, ss + count, large) && !products_run()) return R3_ERR_CUDA;
     return each_launch(ss, count, job.terms,
                        [&](const r3_muon_stack* const* group, int n, int terms, int cluster, int matrices) {
                            return run_small_stacks(job, coefs, group, n, terms, cluster, matrices, dev_status, cs);

@@ -383,8 +383,9 @@ r3_status r3_scale_rows(const r3_shape* shape, const void* dy, const float* gate
  *   dx[t,:]        = dx_residual[t,:] + sum_j dxp[row_of_slot[t,j], :]
  *                    + sum_j dlogits[t, e_j] * W_r[e_j, :]
  *   dw_router[e,:] = sum over tokens t whose record holds e of dlogits[t,e] * x[t,:]
- * (dlogits is zero outside the record, so these are the full products dlogits W_r and
- * dlogits^T x.)  dxp [R,d], dlogits [T,E] float32, idx [T,K], x [T,d], w_router [E,d]
+ * (the replay gate's dlogits is zero outside the record, so these are the full products dlogits W_r and
+ * dlogits^T x; of a gradient that is not, r3_balance_loss's say, only the recorded experts' columns would
+ * be used, so it does not go through here.)  dxp [R,d], dlogits [T,E] float32, idx [T,K], x [T,d], w_router [E,d]
  * (router_w_dtype), dx [T,d], dw_router [E,d] float32; dx_residual [T,d] (the gradient that
  * reaches x around the layer, e.g. through a residual connection) or null for none, never the
  * same buffer as dx; row_of_slot / slot_of_row / offsets from
@@ -811,6 +812,12 @@ typedef struct {
  *   loss[l,1] = (1/N) sum_t (log sum_i exp logits[l,t,i])^2
  *   dlogits   = balance_coef p_ti (f_i - sum_j f_j p_tj) / N + 2 z_coef (log sum exp) p_ti / N
  * (the gradient of balance_coef loss[l,0] + z_coef loss[l,1]; the counts are constants).
+ * This gradient is dense, it has E columns, where the replay gate's has K: what takes it further are the caller's
+ * own two products, dw_router += dlogits^T x and dx += dlogits W_r.  r3_input_grad_finish reads the recorded
+ * experts' columns alone, and the backward chains (r3_replay_layer_train, r3_replay_stack_train,
+ * r3_normed_stack_train) form dx and dw_router from the gate's gradient within the call: added to the dlogits that
+ * they return it changes neither.  A chain over several blocks neither returns its inner inputs nor takes a gradient
+ * at them, so blocks trained with this loss are chained by the caller, one r3_replay_layer_train each.
  * logits [L,T,E] f32; idx [L,T,K] idx_type (may be NULL with counts_given); mask uint8 [T] or NULL: tokens
  * that do not count have 0 there, and their logits and record are not used; counts [L,E] int32, written, may be NULL (with
  * counts_given: read); loss [L,2] f32; dlogits [L,T,E] f32 or NULL (may be the logits' buffer), every

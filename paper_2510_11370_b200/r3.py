@@ -1393,7 +1393,8 @@ def balance_loss(s: Shape, L: int, logits, idx=None, *, mask=None, counts=None, 
     """Balance and z loss of L blocks' routers (r3_balance_loss): logits [L,T,E] float32, idx [L,T,K] the
     record whose choices are counted, mask [T] bool or uint8.  counts [L,E] int32: given, they stand in for
     the record's.  With accumulate the gradient is added to dlogits.  Returns (loss [L,2], counts [L,E]
-    int32, dlogits [L,T,E] or None)."""
+    int32, dlogits [L,T,E] or None).  The gradient is dense: dlogits[l].T @ x and dlogits[l] @ w_router[l] take it to
+    the router and to the block's input; input_grad_finish and the training chains, which follow the record, do not."""
     dev = _device_of("logits", logits)
     f32, new, T, E = torch.float32, torch.empty_strided, s.T, s.E
     grad = (L, T, E)

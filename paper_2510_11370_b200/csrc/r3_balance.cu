@@ -18,7 +18,9 @@
 // probabilities, and the last CTA of a block to arrive adds these up, in an order that depends on the shape alone
 // (rows of sums per CTA, added up by the last one: 26 us instead of 22 for 65536 tokens).
 // 48 blocks of 16384 tokens, 128 experts: 147 us, 5.5 TB/s of the 812 MB that have to move; one block of 65536
-// tokens: 22 us, of which the counting pass and the main pass's start are 9, the logits 10, the losses 3.
+// tokens: 22 us, of which the counting pass and the main pass's start are 9, the logits 10, the losses 3.  Above 512
+// experts a lane's 32 logits, sums and shares of the counts do not fit its 128 registers (the compiler leaves 500 to
+// 600 bytes of them in local memory): 8 blocks of 8192 tokens, 1024 experts 126 us against 83 for their bytes.
 #include <cfloat>
 #include <cmath>
 
@@ -95,7 +97,8 @@ __global__ void __launch_bounds__(COUNT_THREADS) count_kernel(const __grid_const
     const int l = blockIdx.y, E = a.E, K = a.K;
     for (int e = threadIdx.x; e <= E; e += COUNT_THREADS) s_count[e] = 0;
     __syncthreads();
-    // the main pass may start once everything in front of this one is done: it reads logits and mask at once
+    // the main pass may start once everything in front of this one is done: until this one is too it only brings its
+    // first logits into L2
     tc::grid_dependency_wait();
     tc::grid_launch_dependents();
     if (blockIdx.x == 0 && threadIdx.x == 0) a.ticket[l] = 0;
@@ -445,8 +448,8 @@ struct Plan {
     bool alone;
 };
 // Main pass: every resident CTA, unless a warp's share falls below two tokens or so.  Blocks of few logits: a CTA
-// each, without a counting pass (a launch less; 512 tokens of 8 experts 8.6 -> 7.8 us, 48 blocks of it 15.0 -> 8.7;
-// with twice the logits one block takes 9.9 instead of 8.5).
+// each, without a counting pass (a launch less; 512 tokens of 8 experts 8.8 -> 7.2 us in a graph, 48 blocks of it
+// 11.3 -> 8.0; with twice the logits one block would take 9.9 instead of 8.6).
 static Plan plan(int T, int L, int E) {
     Plan p;
     const int ctas = T > 0 ? (T + COUNT_TOKENS - 1) / COUNT_TOKENS : 1;
@@ -457,7 +460,7 @@ static Plan plan(int T, int L, int E) {
     const int most = (E > 256 ? 1 : CTAS_PER_SM) * sm_count();
     if (grid > most) grid = most;
     // whole CTAs per block where that leaves at most a 32nd of them idle: one that crosses a border adds up two
-    // blocks' counts and sums (3 blocks of 4097 tokens, 301 experts: 18.0 us instead of 20.9; 48 of 16384: 147, 150)
+    // blocks' counts and sums (3 blocks of 4097 tokens, 301 experts: 20.1 us instead of 23.8; 48 of 16384: 147, 149)
     if (grid / L * L * 32 >= grid * 31) grid = grid / L * L;
     p.grid = grid < 1 || T == 0 ? 1 : (int)grid;
     p.alone = T > 0 && (long long)T * E <= ALONE;

@@ -14,7 +14,7 @@ using namespace tc;
 
 // An fp16 operand is its value times a power of two, the largest that keeps all iterates within MAX_HALF (2^14 for
 // the usual coefficients).  Its lo plane holds what hi leaves times LO more, or small elements would lose it
-// (without that, and with 2^10 for all, rows a millionth of the others were 5e-3 off in float32 results, with both 3e-7).
+// (without that, and with 2^10 for all, rows a millionth of the others were 7e-3 off in float32 results, with both 8e-7).
 constexpr float LEAST_SCALE = 1024.f, MOST_SCALE = 16384.f, MAX_HALF = 61440.f;
 constexpr int LO_SHIFT = 11;              // (a value within MAX_HALF leaves 16 at most)
 constexpr float LO = 1 << LO_SHIFT;

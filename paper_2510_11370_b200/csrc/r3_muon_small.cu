@@ -11,7 +11,7 @@
 // a I + b A + c A^2 is small and every CTA forms it for itself.
 // Bound by latency, fifteen products with their epilogues one after the other: of a step of 128 x 256 with three
 // products, 17000 clocks, the tensor pipe of the one SM has 8900 (7700 at its rate), the epilogues the others.
-// 24 matrices of 256 x 128 f32 with their momentum 69 us, 128 x 2048 f32 over eight CTAs 82, of which the parts'
+// 24 matrices of 256 x 128 f32 with their momentum 70 us, 128 x 2048 f32 over eight CTAs 83, of which the parts'
 // exchange takes 20.
 #include "r3_muon.cuh"
 

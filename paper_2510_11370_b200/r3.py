@@ -1002,7 +1002,8 @@ def orthogonalize(x, out=None, *, out_dtype=None, steps=5, coefficients=None, ep
                   dev_status=None, stream=None):
     """Newton-Schulz iteration that brings singular values near one (r3_orthogonalize): x [rows, cols] or
     [B, rows, cols], float32 or bfloat16; out of x's type or out_dtype (may be x).  coefficients: (a, b, c) or one
-    triple per step.  products: fp16 products that stand for one, 1 or 3; by default 3 where out is float32."""
+    triple per step.  products: fp16 products that stand for one, 1 or 3; by default 3 where out is float32 (matrices
+    with a side below 16 take 3 either way)."""
     dev = _device_of("x", x)
     if x.dtype not in _ACT:
         raise ValueError(f"x: dtype {x.dtype}, expected float32 or bfloat16")

@@ -4,14 +4,14 @@
 //
 // Three products a step on the tensor cores, each a batch over all matrices of a round (up to four shapes in one
 // launch).  Numbers.  The iterates' singular values stay near one, so fp16 (11 bits, against bf16's 8) holds
-// every operand, times 2^14 with the usual coefficients to keep small elements in its normal range.  X itself is carried
-// in two fp16 planes, hi + lo (22 bits): the term a X, by which a weak direction grows a^steps-fold, then has no
-// rounding to speak of, and what the products' operands lose stays as small as the output's own rounding to bf16
-// whatever the matrix's spectrum is (simulated for full-rank, decaying and low-rank spectra and sides from 16 on:
-// 1.3e-3 to 3e-3 of the result's rms, mostly below 2e-3, against 1.7e-3 for the rounding; bf16 operands with a rounded X lose a third of a rank-8 update).
-// For float32 results A and B get a second plane as well and every product is hi lo + lo hi + hi hi.  Lo planes hold
-// 2^11 of their values, or they would lose what small rows have: the sum of the first two products is taken times
-// 2^-11 by the multiplication that adds the third.
+// every operand, times 2^14 with the usual coefficients to keep small elements in its normal range.  X itself is
+// carried in two fp16 planes, hi + lo (22 bits): the term a X, by which a weak direction grows a^steps-fold, then has
+// no rounding to speak of, and what the products' operands lose stays about as small as the output's own rounding to
+// bf16 whatever the matrix's spectrum is (simulated for full-rank, decaying and low-rank spectra and sides from 16 on:
+// 1.3e-3 to 3e-3 of the result's rms, mostly below 2e-3, against 1.7e-3 for the rounding; bf16 operands with a rounded
+// X lose a third of a rank-8 update).  For float32 results A and B get a second plane as well and every product is
+// hi lo + lo hi + hi hi.  Lo planes hold 2^11 of their values, or they would lose what small rows have: the sum of the
+// first two products is taken times 2^-11 by the multiplication that adds the third.
 //
 // One GEMM kernel does all three, with two CTAs per MMA (256 x 256 tiles, or 256 x 128 where they are few; 128
 // rows of the left operand per CTA and k block of 64, accumulators double buffered in tensor memory).
@@ -21,11 +21,11 @@
 // transposed.  Eight epilogue warps, each with its own 8 KB (three products: 4 KB) of shared memory, through
 // which results go out by TMA in boxes of 32 rows x 64 columns and addends come in whole lines.
 // 24 matrices of 768 x 2048, one product, launches by themselves: X X^T 33 to 36 us, B 21 to 23, B X 52 to 56 (with one
-// plane out), of which the products of their tiles are 23, 9 and 35 at the tensor pipe's rate.  B X moves 228 MB to and from HBM and
-// 796 between L2 and the SMs, 14.2 TB/s; X X^T and B wait for the first loads and the last stores of their few tiles.
-// Three products, 4096 x 4096: 3100 us for five steps at first (3450 to 3550 under load), the tensor pipe busy for three
-// quarters: each 64 of k leave tensor memory for registers.  (With them and 128 columns the epilogue of B leaves 104 bytes a
-// thread in local memory: both planes of A stand beside the sums.)
+// plane out), of which the products of their tiles are 23, 9 and 35 at the tensor pipe's rate.  B X moves 228 MB to and
+// from HBM and 796 between L2 and the SMs, 14.2 TB/s; X X^T and B wait for the first loads and the last stores of their
+// few tiles.  Three products, 4096 x 4096: 3100 us for five steps at first (3450 to 3550 under load), the tensor pipe
+// busy for three quarters: each 64 of k leave tensor memory for registers.  (With 128 columns the epilogue of B then
+// leaves 104 bytes a thread in local memory: both planes of A stand beside the sums.)
 #include <algorithm>
 #include <cmath>
 #include <vector>
